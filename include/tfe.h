@@ -494,6 +494,49 @@ tfe_status tfe_assign_residency(const uint32_t *count, int64_t N, int64_t gpu_sl
                                 int32_t *init_slot, int64_t *tiers, void *stream);
 
 /*
+ * Rows of logits.  The calls below work on DEVICE matrices of vocabulary logits, one row per position,
+ * row r starting `ld` elements after row r - 1 (ld >= V, at most 2^34; rows need no alignment beyond the
+ * element's own), as fp32 or bf16.  They come from a head (tfe_head_buffers, tfe_matmul_fp8) or from the model
+ * itself.  A logit at or below -1e30 is a masked one: -inf, or the lowest value of either type.
+ * These calls keep no state, allocate nothing, never synchronise and may be captured into a CUDA graph; they
+ * work on the current device, which has to be the one that holds the buffers.  Calls on different streams are
+ * independent.  Argument errors are found on the host before anything is launched.
+ */
+enum { TFE_DTYPE_BF16 = 0, TFE_DTYPE_F32 = 1 };
+#define TFE_ROWS_MAX (1 << 27)
+
+/*
+ * Distillation of a teacher's top logits (paper Sec. 4.4: the early-exit projection predicts the full model's
+ * next tokens; the paper gives no training rule, this is the library's: the divergence from the teacher's
+ * distribution over its K best tokens to the predictor's over the whole vocabulary).  Per row, with q the
+ * softmax of teacher_logits / tau over the row's valid entries and lse = ln sum_v exp(z_v / tau):
+ *     loss = tau^2 * sum_k q_k (ln q_k - z[id_k] / tau + lse)
+ *     grad_v = grad_loss * tau * (exp(z_v / tau - lse) - sum of q_k with id_k = v)
+ *
+ *   logits           DEVICE [N][ld], dtype TFE_DTYPE_*;  0 <= N <= TFE_ROWS_MAX.
+ *   teacher_ids      DEVICE int32 [N][K];  an id outside [0, V) is no entry.  Equal ids in a row are terms of their own in
+ *                    the loss and add up in the gradient.
+ *   teacher_logits   DEVICE float [N][K];  logits or log-probabilities (q does not change by a constant), such as the
+ *                    logarithm of tfe_head_topk's probabilities; -inf is a weight of zero.
+ *   K, tau           1 <= K <= TFE_DISTILL_MAX_TOP;  1e-6 <= tau <= 1e6.
+ *   loss, lse        DEVICE float [N].  Sums run in fp32 and are joined in fp64; each result is rounded once.
+ *   grad_loss        DEVICE float [N]: the gradient that arrives at each row's loss.
+ *   grad_logits      DEVICE [N][ld_grad] of the logits' type, rounded once; may be the logits themselves (same
+ *                    pointer and ld_grad = ld), and must not touch them otherwise.  Elements beyond V stay as they were.
+ * A row without a teacher weight, or without an unmasked logit, has loss 0 and gradient 0 (lse = -inf for the
+ * latter), and so has a row whose grad_loss is 0.  A masked logit has probability 0; a teacher weight on it makes the
+ * loss +inf and its gradient -grad_loss * tau * q.  NaN propagates.  One launch each.  Errors: INVALID_ARG, CUDA.
+ */
+#define TFE_DISTILL_MAX_TOP 1024
+tfe_status tfe_distill_forward(const void *logits, int32_t dtype, int32_t N, int32_t V, int64_t ld,
+                               const int32_t *teacher_ids, const float *teacher_logits, int32_t K, float tau,
+                               float *loss, float *lse, void *stream);
+tfe_status tfe_distill_backward(const void *logits, int32_t dtype, int32_t N, int32_t V, int64_t ld,
+                                const int32_t *teacher_ids, const float *teacher_logits, int32_t K, float tau,
+                                const float *lse, const float *grad_loss, void *grad_logits, int64_t ld_grad,
+                                void *stream);
+
+/*
  * Streaming copy (the paper has no counterpart: a yardstick for the measurements, not a step of the method).
  * Copies `bytes` bytes from `src` to `dst` (DEVICE, 16-byte aligned, bytes a multiple of 16, ranges must not
  * overlap) with the load / store instructions the lookup kernels stream hidden states with, one asynchronous

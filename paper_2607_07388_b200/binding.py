@@ -35,7 +35,7 @@ EXPORTS = ["tfe_index_build", "tfe_index_build_device", "tfe_cache_install", "tf
            "tfe_cache_policy_enable", "tfe_cache_select_victims", "tfe_cache_select_victims_device",
            "tfe_cache_stats", "tfe_head_create", "tfe_head_destroy", "tfe_head_topk", "tfe_head_buffers",
            "tfe_head_status", "tfe_head_geometry", "tfe_mine_ngrams", "tfe_mine_workspace_bytes", "tfe_assign_residency", "tfe_stream_copy",
-           "tfe_cache_select_tuning"]
+           "tfe_cache_select_tuning", "tfe_distill_forward", "tfe_distill_backward"]
 
 
 class TfeConfig(C.Structure):
@@ -115,12 +115,16 @@ def lib() -> C.CDLL:
         L.tfe_mine_workspace_bytes.restype = i64
         L.tfe_stream_copy.argtypes = [vp, vp, i64, vp]
         L.tfe_cache_select_tuning.argtypes = [vp, i32, i32, i32]
+        f32 = C.c_float
+        L.tfe_distill_forward.argtypes = [vp, i32, i32, i32, i64, vp, vp, i32, f32, vp, vp, vp]
+        L.tfe_distill_backward.argtypes = [vp, i32, i32, i32, i64, vp, vp, i32, f32, vp, vp, vp, i64, vp]
         for name in ("tfe_index_build", "tfe_index_build_device", "tfe_cache_install", "tfe_cache_install_device", "tfe_lookup_inject", "tfe_lookup_inject_host",
                      "tfe_miss_list", "tfe_miss_list_device", "tfe_index_geometry", "tfe_launch_geometry",
                      "tfe_set_tuning", "tfe_lookup_inject_noalloc", "tfe_prefetch_candidates",
                      "tfe_cache_policy_enable", "tfe_cache_select_victims", "tfe_cache_select_victims_device",
                      "tfe_cache_stats", "tfe_head_create", "tfe_head_topk", "tfe_head_buffers", "tfe_head_status",
-                     "tfe_head_geometry", "tfe_mine_ngrams", "tfe_assign_residency", "tfe_cache_select_tuning"):
+                     "tfe_head_geometry", "tfe_mine_ngrams", "tfe_assign_residency", "tfe_cache_select_tuning",
+                     "tfe_distill_forward", "tfe_distill_backward"):
             getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -423,3 +427,24 @@ def tfe_assign_residency(count, N: int, gpu_slots: int, host_min_count: int, ini
 def tfe_stream_copy(dst, src, nbytes: int, stream=None):
     """Streaming device copy of nbytes (a multiple of 16) bytes: the benchmark's same-footprint yardstick."""
     _check(lib().tfe_stream_copy(_addr(dst), _addr(src), int(nbytes), _stream(stream)), "tfe_stream_copy")
+
+
+# -- rows of logits -----------------------------------------------------------------------------
+DTYPE_BF16, DTYPE_F32 = 0, 1
+ROWS_MAX = 1 << 27
+DISTILL_MAX_TOP = 1024
+
+
+def tfe_distill_forward(logits, dtype: int, N: int, V: int, ld: int, teacher_ids, teacher_logits, K: int, tau: float,
+                        loss, lse, stream=None) -> None:
+    """`logits` is an address: rows `ld` elements apart."""
+    _check(lib().tfe_distill_forward(logits, dtype, N, V, ld, _addr(teacher_ids), _addr(teacher_logits), K, tau,
+                                     _addr(loss), _addr(lse), _stream(stream)), "tfe_distill_forward")
+
+
+def tfe_distill_backward(logits, dtype: int, N: int, V: int, ld: int, teacher_ids, teacher_logits, K: int, tau: float,
+                         lse, grad_loss, grad_logits, ld_grad: int, stream=None) -> None:
+    """`logits` and `grad_logits` are addresses: rows `ld` and `ld_grad` elements apart."""
+    _check(lib().tfe_distill_backward(logits, dtype, N, V, ld, _addr(teacher_ids), _addr(teacher_logits), K, tau,
+                                      _addr(lse), _addr(grad_loss), grad_logits, ld_grad, _stream(stream)),
+           "tfe_distill_backward")

@@ -16,6 +16,7 @@
 #include <vector>
 
 #include "../../include/tfe.h"
+#include "tfe_internal.h"
 #include "tfe_kernels.cuh"
 
 namespace {
@@ -346,6 +347,17 @@ tfe_status ensure_entries(tfe_ctx *c, int64_t entries)
 }
 
 }  // namespace
+
+tfe_status tfe_note_cuda(cudaError_t e, const char *what)
+{
+    if (e == cudaSuccess) return TFE_OK;
+    try {
+        cuda_failed(e, what);
+    } catch (...) {                     // no memory for the text: the status still says it
+        (void)cudaGetLastError();
+    }
+    return TFE_ERR_CUDA;
+}
 
 extern "C" {
 

@@ -1,0 +1,442 @@
+// Distillation of a teacher's top logits into a predictor over the whole vocabulary: the loss that trains an early-exit
+// projection (paper Sec. 4.4: W_pref predicts the full model's next tokens) and its gradient.
+//
+// Per row, with student logits z[0..V), teacher entries (id_k, t_k), k < K, and temperature tau:
+//     lse  = ln sum_v exp(z_v / tau)                          q = softmax over the valid k of t_k / tau
+//     loss = tau^2 sum_k q_k (ln q_k - z[id_k] / tau + lse)   (tau^2 times the divergence from q to the student)
+//     grad = g tau (exp(z_v / tau - lse) - sum of q_k with id_k = v)
+//
+//   tfe_distill_forward_kernel   one pass over the row: running maximum and sum of exponentials.  A row is taken by a
+//                                warp, by a block, or by a cluster of blocks whose partial results meet in the shared
+//                                memory of the first.  A warp of the row's first block does the K teacher entries in
+//                                64 bits while the others stream.
+//   tfe_distill_backward_kernel  one pass: read the logit, write the gradient.  A block owns its slice of the row, so
+//                                the entries with a teacher weight are corrected by the block itself after its stream
+//                                (equal ids are summed by the first of them, in order: no atomics), from logits it
+//                                saved before; the gradient may therefore overwrite the logits.
+//
+// Both are bound by HBM.
+#include <cooperative_groups.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+
+#include "../../include/tfe.h"
+#include "tfe_internal.h"
+#include "tfe_rows.cuh"
+
+namespace {
+
+using namespace tfe_rows;
+namespace cg = cooperative_groups;
+
+constexpr int kBlock = 512;             // threads of a block that takes (a slice of) one row
+constexpr int kSmallBlock = 256;        // ... and of one whose warps take a row each
+constexpr int kMaxTop = TFE_DISTILL_MAX_TOP;
+constexpr double kLog2e = 1.4426950408889634;
+
+struct DistillParams {
+    const void *logits; int64_t ld;
+    int32_t N, V, K;
+    float tau;
+    const int32_t *ids; const float *t;
+    float *loss, *lse;                  // forward
+    const float *lse_in, *grad_loss;    // backward
+    void *grad; int64_t ld_grad;
+    int32_t slices;                     // blocks per row
+};
+
+__device__ __forceinline__ bool teacher_valid(int32_t id, int32_t V) { return id >= 0 && id < V; }
+
+// A warp's view of a row's teacher entries: the largest valid t and sum of exp((t - largest) / tau).  NaN among the
+// valid entries makes the sum NaN.  No valid entry, or all of them -inf: sum 0.
+__device__ __forceinline__ void teacher_norm(const DistillParams &p, int64_t row, int lane, float &top, double &sum)
+{
+    top = -INFINITY;
+    const int64_t at = row * p.K;
+    for (int k = lane; k < p.K; k += 32)
+        if (teacher_valid(p.ids[at + k], p.V)) top = fmaxf(top, p.t[at + k]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    sum = 0.0;
+    for (int k = lane; k < p.K; k += 32)
+        if (teacher_valid(p.ids[at + k], p.V)) {
+            const float t = p.t[at + k];
+            if (t != -INFINITY) sum += exp(((double)t - (double)top) / (double)p.tau);
+        }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+}
+
+// Folds (m2, s2) into (m, s), both sums relative to their maxima in the logits' own units.
+__device__ __forceinline__ void fold(float &m, float &s, float m2, float s2, float c)
+{
+    const float top = fmaxf(m, m2);
+    s = s * exp2_approx((m - top) * c) + s2 * exp2_approx((m2 - top) * c);
+    m = top;
+}
+
+// Running maximum and sum of exp2((z - m) c) over this thread's elements of a slice.  The maximum starts at the mask
+// value; the difference is taken before the scale so that rows of masked values never meet inf - inf.
+template <typename T, int U>
+__device__ __forceinline__ void stream_row(const T *row, int64_t n, int slice, int slices, int tid, int threads, float c, float &m, float &s)
+{
+    constexpr int E = Elem<T>::kPerVec;
+    const Cut cut = cut_row(row, n);
+    const uint4 *body = reinterpret_cast<const uint4 *>(row + cut.head);
+    const int64_t v0 = cut.n_vec * slice / slices, v1 = cut.n_vec * (slice + 1) / slices;
+    m = kMasked;
+    s = 0.f;
+    auto take = [&](float z) {
+        if (z > m) { s *= exp2_approx((m - z) * c); m = z; }
+        s += exp2_approx((z - m) * c);
+    };
+    if (slice == 0) for (int64_t i = tid; i < cut.head; i += threads) take(Elem<T>::get(row + i));
+    if (slice == slices - 1)
+        for (int64_t i = cut.head + cut.n_vec * E + tid; i < n; i += threads) take(Elem<T>::get(row + i));
+    for (int64_t v = v0 + tid; v < v1; v += (int64_t)U * threads) {
+        uint4 raw[U];
+        float f[U][E];
+        float top = m;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (v + (int64_t)u * threads < v1) raw[u] = load_stream(body + v + (int64_t)u * threads);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (v + (int64_t)u * threads < v1) {
+                Elem<T>::unpack(raw[u], f[u]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) f[u][e] = -INFINITY;
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) top = fmaxf(top, f[u][e]);
+        }
+        if (top > m) { s *= exp2_approx((m - top) * c); m = top; }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float part = 0.f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) part += exp2_approx((f[u][e] - m) * c);
+            s += part;
+        }
+    }
+}
+
+// sum_k q_k (ln q_k - z[id_k] / tau) in 64 bits, on every lane; +inf where a teacher weight meets a masked logit
+template <typename T>
+__device__ __forceinline__ double teacher_term(const DistillParams &p, const T *row, int64_t r, int lane, bool &any)
+{
+    float top;
+    double sum;
+    teacher_norm(p, r, lane, top, sum);
+    any = !(sum == 0.0);
+    if (!any) return 0.0;
+    const double log_sum = log(sum);
+    double term = 0.0;
+    const int64_t at = r * p.K;
+    for (int k = lane; k < p.K; k += 32) {
+        const int32_t id = p.ids[at + k];
+        if (!teacher_valid(id, p.V)) continue;
+        const float t = p.t[at + k];
+        if (t == -INFINITY) continue;
+        const float z = Elem<T>::get(row + id);
+        const double log_q = ((double)t - (double)top) / (double)p.tau - log_sum, q = exp(log_q);
+        if (q > 0.0 || isnan(q)) term += z <= kMasked ? INFINITY : q * (log_q - (double)z / (double)p.tau);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) term += __shfl_xor_sync(0xFFFFFFFFu, term, o);
+    return term;
+}
+
+__device__ __forceinline__ void finish_row(const DistillParams &p, int64_t r, float m, float s, double term, bool any)
+{
+    // m still at the mask value: no logit above it (s counts masked ones then); NaN has made s NaN
+    const bool empty = m <= kMasked && !isnan(s);
+    const double lse = empty ? -INFINITY : (double)m / (double)p.tau + log((double)s);
+    p.lse[r] = (float)lse;
+    p.loss[r] = !any || empty ? 0.f : (float)((double)p.tau * (double)p.tau * (term + lse));
+}
+
+template <typename T, bool kWarpRows>
+__global__ void __launch_bounds__(kWarpRows ? kSmallBlock : kBlock)
+tfe_distill_forward_kernel(const DistillParams p)
+{
+    const float c = (float)(kLog2e / (double)p.tau);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if constexpr (kWarpRows) {
+        const int64_t r = (int64_t)blockIdx.x * (kSmallBlock / 32) + warp;
+        if (r >= p.N) return;
+        const T *row = static_cast<const T *>(p.logits) + r * p.ld;
+        float m, s;
+        stream_row<T, 2>(row, p.V, 0, 1, lane, 32, c, m, s);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) fold(m, s, __shfl_xor_sync(0xFFFFFFFFu, m, o), __shfl_xor_sync(0xFFFFFFFFu, s, o), c);
+        bool any;
+        const double term = teacher_term<T>(p, row, r, lane, any);
+        if (lane == 0) finish_row(p, r, m, s, term, any);
+    } else {
+        __shared__ float s_m[kBlock / 32], s_s[kBlock / 32];
+        __shared__ float2 s_part;
+        const int64_t r = blockIdx.x / p.slices;
+        const int slice = (int)(blockIdx.x % p.slices);
+        const T *row = static_cast<const T *>(p.logits) + r * p.ld;
+        double term = 0.0;
+        bool any = false;
+        if (slice == 0 && warp == 0) term = teacher_term<T>(p, row, r, lane, any);
+        float m, s;
+        stream_row<T, 4>(row, p.V, slice, p.slices, threadIdx.x, kBlock, c, m, s);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) fold(m, s, __shfl_xor_sync(0xFFFFFFFFu, m, o), __shfl_xor_sync(0xFFFFFFFFu, s, o), c);
+        if (lane == 0) { s_m[warp] = m; s_s[warp] = s; }
+        __syncthreads();
+        if (warp == 0) {
+            m = lane < kBlock / 32 ? s_m[lane] : kMasked;
+            s = lane < kBlock / 32 ? s_s[lane] : 0.f;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) fold(m, s, __shfl_xor_sync(0xFFFFFFFFu, m, o), __shfl_xor_sync(0xFFFFFFFFu, s, o), c);
+            if (lane == 0) s_part = make_float2(m, s);
+        }
+        if (p.slices > 1) {
+            cg::cluster_group cluster = cg::this_cluster();
+            cluster.sync();
+            if (slice == 0 && threadIdx.x == 0) {
+                for (int b = 1; b < p.slices; ++b) {
+                    const float2 other = *cluster.map_shared_rank(&s_part, b);
+                    fold(m, s, other.x, other.y, c);
+                }
+            }
+            cluster.sync();                 // a block's shared memory lives until its partner has read it
+        }
+        if (slice == 0 && threadIdx.x == 0) finish_row(p, r, m, s, term, any);
+    }
+}
+
+// ------------------------------------------------------------------ gradient
+
+// One row, or one slice of it, by `threads` threads that sync with `sync`.
+template <typename T, int U, typename Sync>
+__device__ __forceinline__ void backward_row(const DistillParams &p, int64_t r, int slice, int tid, int threads, bool first_warp,
+                                             int32_t *s_id, float *s_q, float *s_z, float *s_norm, Sync sync)
+{
+    constexpr int E = Elem<T>::kPerVec;
+    const T *row = static_cast<const T *>(p.logits) + r * p.ld;
+    T *out = static_cast<T *>(p.grad) + r * p.ld_grad;
+    const int lane = threadIdx.x & 31;
+    const float g = p.grad_loss[r], lse = p.lse_in[r];
+    const Cut cut = cut_row(row, p.V);
+    const int64_t v0 = cut.n_vec * slice / p.slices, v1 = cut.n_vec * (slice + 1) / p.slices;
+    // this slice's elements: [e0, e1), the head and the tail with the first and the last slice
+    const int64_t e0 = slice == 0 ? 0 : cut.head + v0 * E, e1 = slice == p.slices - 1 ? (int64_t)p.V : cut.head + v1 * E;
+    const bool same_cut = ((reinterpret_cast<uintptr_t>(row) ^ reinterpret_cast<uintptr_t>(out)) & 15u) == 0;
+
+    if (first_warp) {
+        float top;
+        double sum;
+        teacher_norm(p, r, lane, top, sum);
+        if (lane == 0) { s_norm[0] = top; s_norm[1] = sum == 0.0 ? 0.f : (float)(1.0 / sum); }
+    }
+    sync();
+    const float t_top = s_norm[0], t_inv = s_norm[1];
+    const bool live = g != 0.f && t_inv != 0.f && lse != -INFINITY;
+    if (live) {
+        const int64_t at = r * p.K;
+        for (int k = tid; k < p.K; k += threads) {
+            const int32_t id = p.ids[at + k];
+            const bool mine = id >= e0 && id < e1;
+            s_id[k] = mine ? id : -1;
+            if (mine) {
+                const float t = p.t[at + k];
+                s_q[k] = t == -INFINITY ? 0.f : (float)exp(((double)t - (double)t_top) / (double)p.tau) * t_inv;
+                s_z[k] = Elem<T>::get(row + id);
+            }
+        }
+    }
+    sync();
+
+    const float coef = g * p.tau, c = (float)(kLog2e / (double)p.tau), shift = (float)((double)lse * kLog2e);
+    auto prob = [&](float z) { return z <= kMasked ? 0.f : exp2_approx(fmaf(z, c, -shift)); };
+    if (!live) {
+        if (same_cut) {
+            for (int64_t i = e0 + tid; i < (slice == 0 ? cut.head : e0); i += threads) Elem<T>::put(out + i, 0.f);
+            for (int64_t i = cut.head + v1 * E + tid; i < e1; i += threads) Elem<T>::put(out + i, 0.f);
+            uint4 *ob = reinterpret_cast<uint4 *>(out + cut.head);
+            for (int64_t v = v0 + tid; v < v1; v += threads) __stcs(ob + v, make_uint4(0, 0, 0, 0));
+        } else {
+            for (int64_t i = e0 + tid; i < e1; i += threads) Elem<T>::put(out + i, 0.f);
+        }
+        return;
+    }
+    if (same_cut) {
+        if (slice == 0) for (int64_t i = tid; i < cut.head; i += threads) Elem<T>::put(out + i, coef * prob(Elem<T>::get(row + i)));
+        for (int64_t i = cut.head + v1 * E + tid; i < e1; i += threads) Elem<T>::put(out + i, coef * prob(Elem<T>::get(row + i)));
+        const uint4 *body = reinterpret_cast<const uint4 *>(row + cut.head);
+        uint4 *ob = reinterpret_cast<uint4 *>(out + cut.head);
+        for (int64_t v = v0 + tid; v < v1; v += (int64_t)U * threads) {
+            uint4 raw[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (v + (int64_t)u * threads < v1) raw[u] = load_stream(body + v + (int64_t)u * threads);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (v + (int64_t)u * threads < v1) {
+                    float f[E];
+                    Elem<T>::unpack(raw[u], f);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) f[e] = coef * prob(f[e]);
+                    __stcs(ob + v + (int64_t)u * threads, Elem<T>::pack(f));
+                }
+        }
+    } else {
+        for (int64_t i = e0 + tid; i < e1; i += threads) Elem<T>::put(out + i, coef * prob(Elem<T>::get(row + i)));
+    }
+    sync();
+    for (int k = tid; k < p.K; k += threads) {
+        const int32_t id = s_id[k];
+        if (id < 0) continue;
+        float q = 0.f;
+        bool first = true;
+        for (int j = 0; j < p.K; ++j)
+            if (s_id[j] == id) {
+                if (j < k) first = false;
+                q += s_q[j];
+            }
+        if (first) Elem<T>::put(out + id, coef * (prob(s_z[k]) - q));
+    }
+}
+
+template <typename T, bool kWarpRows>
+__global__ void __launch_bounds__(kWarpRows ? kSmallBlock : kBlock)
+tfe_distill_backward_kernel(const DistillParams p)
+{
+    extern __shared__ float s_raw[];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int per_row = 3 * p.K + 2;
+    if constexpr (kWarpRows) {
+        const int64_t r = (int64_t)blockIdx.x * (kSmallBlock / 32) + warp;
+        if (r >= p.N) return;
+        float *mine = s_raw + warp * per_row;
+        backward_row<T, 2>(p, r, 0, lane, 32, true, reinterpret_cast<int32_t *>(mine), mine + p.K, mine + 2 * p.K, mine + 3 * p.K,
+                           [] { __syncwarp(); });
+    } else {
+        backward_row<T, 4>(p, blockIdx.x / p.slices, (int)(blockIdx.x % p.slices), threadIdx.x, kBlock, warp == 0,
+                           reinterpret_cast<int32_t *>(s_raw), s_raw + p.K, s_raw + 2 * p.K, s_raw + 3 * p.K, [] { __syncthreads(); });
+    }
+}
+
+// ------------------------------------------------------------------ host side
+
+size_t elem_size(int32_t dtype) { return dtype == TFE_DTYPE_BF16 ? 2 : 4; }
+
+bool row_args_ok(const void *x, int32_t dtype, int32_t N, int32_t V, int64_t ld)
+{
+    if (dtype != TFE_DTYPE_BF16 && dtype != TFE_DTYPE_F32) return false;
+    if (N < 0 || N > TFE_ROWS_MAX || V < 1 || ld < V || ld > (1ll << 34)) return false;
+    return N == 0 || (x && reinterpret_cast<uintptr_t>(x) % elem_size(dtype) == 0);
+}
+
+// Warps take rows of up to this many bytes; beyond, a block per row and, with few rows, several.
+constexpr int64_t kWarpRowBytes = 8192;
+
+int32_t slices_for(int32_t N, int64_t row_bytes, int sms)
+{
+    int32_t s = 1;
+    while (s < 8 && (int64_t)N * s < 2 * sms && row_bytes / (2 * s) >= 16384) s *= 2;
+    return s;
+}
+
+template <typename F>
+tfe_status launch_rows(F kernel, int grid, int block, int cluster, size_t smem, cudaStream_t stream, const DistillParams &p)
+{
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)cluster;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)grid); cfg.blockDim = dim3((unsigned)block); cfg.dynamicSmemBytes = smem; cfg.stream = stream;
+    cfg.attrs = attr; cfg.numAttrs = cluster > 1 ? 1 : 0;
+    return tfe_note_cuda(cudaLaunchKernelEx(&cfg, kernel, p), "distillation launch");
+}
+
+tfe_status device_sms(int *sms)
+{
+    int dev = 0;
+    tfe_status st = tfe_note_cuda(cudaGetDevice(&dev), "cudaGetDevice");
+    return st != TFE_OK ? st : tfe_note_cuda(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev), "cudaDeviceGetAttribute");
+}
+
+bool teacher_args_ok(int32_t N, int32_t K, float tau, const int32_t *ids, const float *t)
+{
+    if (K < 1 || K > kMaxTop || !(tau > 0.f) || tau > 1e6f || tau < 1e-6f) return false;
+    return N == 0 || (ids && t && reinterpret_cast<uintptr_t>(ids) % 4 == 0 && reinterpret_cast<uintptr_t>(t) % 4 == 0);
+}
+
+}  // namespace
+
+extern "C" {
+
+tfe_status tfe_distill_forward(const void *logits, int32_t dtype, int32_t N, int32_t V, int64_t ld, const int32_t *teacher_ids,
+                               const float *teacher_logits, int32_t K, float tau, float *loss, float *lse, void *stream_)
+{
+    if (!row_args_ok(logits, dtype, N, V, ld) || !teacher_args_ok(N, K, tau, teacher_ids, teacher_logits)) return TFE_ERR_INVALID_ARG;
+    if (N == 0) return TFE_OK;
+    if (!loss || !lse) return TFE_ERR_INVALID_ARG;
+    int sms = 0;
+    if (tfe_status st = device_sms(&sms)) return st;
+    DistillParams p{};
+    p.logits = logits; p.ld = ld; p.N = N; p.V = V; p.K = K; p.tau = tau; p.ids = teacher_ids; p.t = teacher_logits;
+    p.loss = loss; p.lse = lse;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    const int64_t row_bytes = (int64_t)V * (int64_t)elem_size(dtype);
+    if (row_bytes <= kWarpRowBytes) {
+        p.slices = 1;
+        const int grid = (N + kSmallBlock / 32 - 1) / (kSmallBlock / 32);
+        return dtype == TFE_DTYPE_BF16 ? launch_rows(tfe_distill_forward_kernel<__nv_bfloat16, true>, grid, kSmallBlock, 1, 0, stream, p)
+                                       : launch_rows(tfe_distill_forward_kernel<float, true>, grid, kSmallBlock, 1, 0, stream, p);
+    }
+    p.slices = slices_for(N, row_bytes, sms);
+    return dtype == TFE_DTYPE_BF16 ? launch_rows(tfe_distill_forward_kernel<__nv_bfloat16, false>, N * p.slices, kBlock, p.slices, 0, stream, p)
+                                   : launch_rows(tfe_distill_forward_kernel<float, false>, N * p.slices, kBlock, p.slices, 0, stream, p);
+}
+
+tfe_status tfe_distill_backward(const void *logits, int32_t dtype, int32_t N, int32_t V, int64_t ld, const int32_t *teacher_ids,
+                                const float *teacher_logits, int32_t K, float tau, const float *lse, const float *grad_loss,
+                                void *grad_logits, int64_t ld_grad, void *stream_)
+{
+    if (!row_args_ok(logits, dtype, N, V, ld) || !teacher_args_ok(N, K, tau, teacher_ids, teacher_logits)) return TFE_ERR_INVALID_ARG;
+    if (!row_args_ok(grad_logits, dtype, N, V, ld_grad)) return TFE_ERR_INVALID_ARG;
+    if (N == 0) return TFE_OK;
+    if (!lse || !grad_loss) return TFE_ERR_INVALID_ARG;
+    // the same rows in place, or buffers that do not touch
+    if (grad_logits == logits) {
+        if (ld_grad != ld) return TFE_ERR_INVALID_ARG;
+    } else {
+        const uintptr_t a0 = reinterpret_cast<uintptr_t>(logits), b0 = reinterpret_cast<uintptr_t>(grad_logits);
+        const uintptr_t es = elem_size(dtype);
+        const uintptr_t a1 = a0 + ((uintptr_t)(N - 1) * (uintptr_t)ld + (uintptr_t)V) * es;
+        const uintptr_t b1 = b0 + ((uintptr_t)(N - 1) * (uintptr_t)ld_grad + (uintptr_t)V) * es;
+        if (a0 < b1 && b0 < a1) return TFE_ERR_INVALID_ARG;
+    }
+    int sms = 0;
+    if (tfe_status st = device_sms(&sms)) return st;
+    DistillParams p{};
+    p.logits = logits; p.ld = ld; p.N = N; p.V = V; p.K = K; p.tau = tau; p.ids = teacher_ids; p.t = teacher_logits;
+    p.lse_in = lse; p.grad_loss = grad_loss; p.grad = grad_logits; p.ld_grad = ld_grad;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    const int64_t row_bytes = (int64_t)V * (int64_t)elem_size(dtype);
+    const size_t per_row = (size_t)(3 * K + 2) * sizeof(float);
+    if (row_bytes <= kWarpRowBytes && K <= 256) {
+        p.slices = 1;
+        const int rows = kSmallBlock / 32, grid = (N + rows - 1) / rows;
+        return dtype == TFE_DTYPE_BF16
+                   ? launch_rows(tfe_distill_backward_kernel<__nv_bfloat16, true>, grid, kSmallBlock, 1, per_row * rows, stream, p)
+                   : launch_rows(tfe_distill_backward_kernel<float, true>, grid, kSmallBlock, 1, per_row * rows, stream, p);
+    }
+    p.slices = slices_for(N, row_bytes, sms);
+    return dtype == TFE_DTYPE_BF16
+               ? launch_rows(tfe_distill_backward_kernel<__nv_bfloat16, false>, N * p.slices, kBlock, 1, per_row, stream, p)
+               : launch_rows(tfe_distill_backward_kernel<float, false>, N * p.slices, kBlock, 1, per_row, stream, p);
+}
+
+}  // extern "C"

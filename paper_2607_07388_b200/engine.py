@@ -5,6 +5,7 @@ Nothing is computed here -- every call goes straight to libtfe.so.
 """
 from __future__ import annotations
 
+import contextlib
 from dataclasses import dataclass
 
 import numpy as np
@@ -221,3 +222,109 @@ def assign_residency(count: torch.Tensor, gpu_slots: int, host_min_count: int = 
     init_slot = torch.empty(max(count.numel(), 1), dtype=torch.int32, device=count.device)
     tiers = tfe.tfe_assign_residency(count, count.numel(), gpu_slots, host_min_count, init_slot, stream)
     return init_slot[:count.numel()], tiers
+
+
+# ---- rows of logits ----------------------------------------------------------------------------
+
+_ROW_DTYPES = {torch.bfloat16: tfe.DTYPE_BF16, torch.float32: tfe.DTYPE_F32}
+
+
+def _require(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+@contextlib.contextmanager
+def _elsewhere(device: torch.device, stream):
+    """The operands' device made current and, with a stream given, results allocated for that stream."""
+    with torch.cuda.device(device):
+        if stream is None:
+            yield
+        else:
+            with torch.cuda.stream(torch.cuda.ExternalStream(stream, device) if isinstance(stream, int) else stream):
+                yield
+
+
+_HERE = contextlib.nullcontext()
+
+
+def _issue(device: torch.device, stream):
+    """Where a call is issued: nothing to change for the common case of the current device and stream."""
+    return _HERE if stream is None and device.index == torch.cuda.current_device() else _elsewhere(device, stream)
+
+
+def _row_matrix(t: torch.Tensor, what: str):
+    """(rows, columns, elements between rows) of a 2-D CUDA matrix whose rows are contiguous."""
+    _require(t.is_cuda and t.dim() == 2 and t.dtype in _ROW_DTYPES, f"{what}: a 2-D bf16 or fp32 CUDA tensor is needed")
+    n, v = t.shape
+    _require(v >= 1 and (t.stride(1) == 1 or v == 1), f"{what}: rows must be contiguous")
+    ld = t.stride(0) if n > 1 else v
+    _require(ld >= v, f"{what}: rows must not overlap")
+    return n, v, ld
+
+
+def _vector(t: torch.Tensor, shape, dtype, device, what: str):
+    _require(t.shape == shape and t.dtype == dtype and t.device == device and t.is_contiguous(),
+             f"{what}: a contiguous {dtype} tensor of shape {tuple(shape)} on {device} is needed")
+
+
+def _teacher(logits, teacher_ids, teacher_logits):
+    n, v, ld = _row_matrix(logits, "logits")
+    _require(teacher_ids.dim() == 2, "teacher_ids: [rows, K] is needed")
+    shape = (n, teacher_ids.shape[1])
+    _vector(teacher_ids, shape, torch.int32, logits.device, "teacher_ids")
+    _vector(teacher_logits, shape, torch.float32, logits.device, "teacher_logits")
+    return n, v, ld, shape[1]
+
+
+def distill_forward(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_logits: torch.Tensor, tau: float = 1.0, *,
+                    stream=None):
+    """(loss, lse), fp32 [N] each: the divergence from the teacher's top logits to the rows of `logits` [N, V] (see
+    tfe_distill_forward), and the log-sum-exp of logits / tau that the gradient needs."""
+    n, v, ld, k = _teacher(logits, teacher_ids, teacher_logits)
+    with _issue(logits.device, stream):
+        loss = torch.empty(n, dtype=torch.float32, device=logits.device)
+        lse = torch.empty(n, dtype=torch.float32, device=logits.device)
+        tfe.tfe_distill_forward(logits.data_ptr(), _ROW_DTYPES[logits.dtype], n, v, ld, teacher_ids, teacher_logits, k,
+                                tau, loss, lse, stream)
+    return loss, lse
+
+
+def distill_backward(grad_loss: torch.Tensor, logits: torch.Tensor, teacher_ids: torch.Tensor,
+                     teacher_logits: torch.Tensor, lse: torch.Tensor, tau: float = 1.0, *,
+                     out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """The gradient [N, V] of sum(grad_loss * loss) with respect to the logits.  `out`: where it goes, of the logits'
+    shape and type; `out=logits` overwrites them."""
+    n, v, ld, k = _teacher(logits, teacher_ids, teacher_logits)
+    _vector(grad_loss, (n,), torch.float32, logits.device, "grad_loss")
+    _vector(lse, (n,), torch.float32, logits.device, "lse")
+    with _issue(logits.device, stream):
+        if out is None:
+            out = torch.empty((n, v), dtype=logits.dtype, device=logits.device)
+        on, ov, ld_out = _row_matrix(out, "out")
+        _require((on, ov) == (n, v) and out.dtype == logits.dtype and out.device == logits.device,
+                 "out: the logits' shape, type and device are needed")
+        tfe.tfe_distill_backward(logits.data_ptr(), _ROW_DTYPES[logits.dtype], n, v, ld, teacher_ids, teacher_logits, k,
+                                 tau, lse, grad_loss, out.data_ptr(), ld_out, stream)
+    return out
+
+
+class _DistillLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, teacher_ids, teacher_logits, tau):
+        loss, lse = distill_forward(logits, teacher_ids, teacher_logits, tau)
+        ctx.save_for_backward(logits, teacher_ids, teacher_logits, lse)
+        ctx.tau = tau
+        return loss
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_loss):
+        logits, ids, t, lse = ctx.saved_tensors
+        return distill_backward(grad_loss.contiguous(), logits, ids, t, lse, ctx.tau), None, None, None
+
+
+def distill_loss(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_logits: torch.Tensor, tau: float = 1.0) -> torch.Tensor:
+    """distill_forward's loss [N] as a node of autograd: the gradient goes to the logits, none to the teacher.  Reduce it
+    as the training wants, e.g. ``(distill_loss(z, ids, t) * weight).sum()``."""
+    return _DistillLoss.apply(logits, teacher_ids, teacher_logits, tau)

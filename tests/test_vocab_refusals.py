@@ -1,0 +1,34 @@
+"""Refusals of the calls on rows of logits: found on the host, before any device call (nothing here needs a GPU)."""
+import pytest
+
+P = 0x1000                                  # an address that is never touched
+
+
+@pytest.fixture(scope="module")
+def tfe():
+    from paper_2607_07388_b200 import binding, build
+    build.build()
+    binding.lib()
+    return binding
+
+
+def test_distillation(tfe):
+    L = tfe.lib()
+
+    def forward(logits=P, dtype=1, N=2, V=8, ld=8, ids=P, t=P, K=4, tau=1.0, loss=P, lse=P):
+        return L.tfe_distill_forward(logits, dtype, N, V, ld, ids, t, K, tau, loss, lse, None)
+
+    def backward(logits=P, dtype=1, N=2, V=8, ld=8, ids=P, t=P, K=4, tau=1.0, lse=P, g=P, grad=2 * P, ld_grad=8):
+        return L.tfe_distill_backward(logits, dtype, N, V, ld, ids, t, K, tau, lse, g, grad, ld_grad, None)
+
+    both = [dict(dtype=2), dict(dtype=-1), dict(N=-1), dict(N=tfe.ROWS_MAX + 1), dict(V=0), dict(ld=7), dict(ld=1 << 40),
+            dict(logits=None), dict(logits=P + 2), dict(dtype=0, logits=P + 1), dict(ids=None), dict(ids=P + 2), dict(t=None),
+            dict(t=P + 1), dict(K=0), dict(K=tfe.DISTILL_MAX_TOP + 1), dict(tau=0.0), dict(tau=-1.0), dict(tau=float("nan")),
+            dict(tau=float("inf")), dict(lse=None)]
+    for kw in both + [dict(loss=None)]:
+        assert forward(**kw) == tfe.TFE_ERR_INVALID_ARG, kw
+    for kw in both + [dict(g=None), dict(grad=None), dict(grad=P + 32), dict(grad=P - 32), dict(grad=P, ld_grad=9), dict(ld_grad=7),
+                      dict(grad=2 * P + 2)]:
+        assert backward(**kw) == tfe.TFE_ERR_INVALID_ARG, kw
+    assert forward(N=0, logits=None, ids=None, t=None, loss=None, lse=None) == tfe.TFE_OK
+    assert backward(N=0, logits=None, ids=None, t=None, lse=None, g=None, grad=None) == tfe.TFE_OK
