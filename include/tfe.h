@@ -506,6 +506,37 @@ enum { TFE_DTYPE_BF16 = 0, TFE_DTYPE_F32 = 1 };
 #define TFE_ROWS_MAX (1 << 27)
 
 /*
+ * tfe_sample_tokens -- the next token of every sequence from its logits and one given random number per sequence
+ * (the lookups are keyed by the token ids that decoding produces; the paper names no sampling rule).  Per row, in
+ * the order of descending logits, equal logits by ascending id, with w_i = exp((z_i - z_max) / temperature):
+ *     min-p   entries with w_i >= min_p                               (min_p <= 0: all of them)
+ *     top-k   the first top_k of those                                (top_k <= 0: all)
+ *     top-p   the shortest prefix of those whose sum of w reaches top_p of theirs; at least one entry (top_p >= 1: all)
+ *     token   the first entry of those whose running sum exceeds u of theirs;  prob = its w over their sum.
+ * A temperature that is not greater than 0 takes the first entry (prob 1).  Masked (-inf) and NaN logits are never
+ * drawn; a row without any other gives token -1 and prob 0.  Logits of +inf, if any, share the draw.  (The lowest value of
+ * a type needs no rule here: its weight is 0 next to any other logit.)
+ *
+ *   logits        DEVICE [B][ld], dtype TFE_DTYPE_*;  0 <= B <= TFE_ROWS_MAX, 1 <= V <= TFE_SAMPLE_MAX_VOCAB.
+ *   params        HOST; four DEVICE arrays of B values, or NULL for: temperature 1, no restriction.  Values
+ *                 outside a parameter's range act as its nearest end; NaN as "no restriction" (temperature: greedy).
+ *   u             DEVICE float [B], in [0, 1): values outside are brought to the nearest end, NaN to 0.
+ *   tokens, prob  DEVICE int32 [B], DEVICE float [B] (prob may be NULL).
+ * Weights are evaluated in fp64 and summed as integers, so a row's result does not depend on the rest of the batch, on
+ * its place in it, or on the order of any addition.  One launch.  Errors: INVALID_ARG, CUDA.
+ */
+#define TFE_SAMPLE_MAX_VOCAB (1 << 24)
+typedef struct {
+    const float   *temperature;
+    const int32_t *top_k;
+    const float   *top_p;
+    const float   *min_p;
+} tfe_sample_params;
+tfe_status tfe_sample_tokens(const void *logits, int32_t dtype, int32_t B, int32_t V, int64_t ld,
+                             const tfe_sample_params *params, const float *u, int32_t *tokens, float *prob,
+                             void *stream);
+
+/*
  * Distillation of a teacher's top logits (paper Sec. 4.4: the early-exit projection predicts the full model's
  * next tokens; the paper gives no training rule, this is the library's: the divergence from the teacher's
  * distribution over its K best tokens to the predictor's over the whole vocabulary).  Per row, with q the

@@ -35,7 +35,7 @@ EXPORTS = ["tfe_index_build", "tfe_index_build_device", "tfe_cache_install", "tf
            "tfe_cache_policy_enable", "tfe_cache_select_victims", "tfe_cache_select_victims_device",
            "tfe_cache_stats", "tfe_head_create", "tfe_head_destroy", "tfe_head_topk", "tfe_head_buffers",
            "tfe_head_status", "tfe_head_geometry", "tfe_mine_ngrams", "tfe_mine_workspace_bytes", "tfe_assign_residency", "tfe_stream_copy",
-           "tfe_cache_select_tuning", "tfe_distill_forward", "tfe_distill_backward"]
+           "tfe_cache_select_tuning", "tfe_distill_forward", "tfe_distill_backward", "tfe_sample_tokens"]
 
 
 class TfeConfig(C.Structure):
@@ -51,6 +51,10 @@ class TfeInjectParams(C.Structure):
 
 class TfePrefetchParams(C.Structure):
     _fields_ = [("benefit_host", C.c_float), ("benefit_ssd", C.c_float), ("budget", C.c_int32)]
+
+
+class TfeSampleParams(C.Structure):
+    _fields_ = [("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p)]
 
 
 class TfeError(RuntimeError):
@@ -116,6 +120,7 @@ def lib() -> C.CDLL:
         L.tfe_stream_copy.argtypes = [vp, vp, i64, vp]
         L.tfe_cache_select_tuning.argtypes = [vp, i32, i32, i32]
         f32 = C.c_float
+        L.tfe_sample_tokens.argtypes = [vp, i32, i32, i32, i64, C.POINTER(TfeSampleParams), vp, vp, vp, vp]
         L.tfe_distill_forward.argtypes = [vp, i32, i32, i32, i64, vp, vp, i32, f32, vp, vp, vp]
         L.tfe_distill_backward.argtypes = [vp, i32, i32, i32, i64, vp, vp, i32, f32, vp, vp, vp, i64, vp]
         for name in ("tfe_index_build", "tfe_index_build_device", "tfe_cache_install", "tfe_cache_install_device", "tfe_lookup_inject", "tfe_lookup_inject_host",
@@ -124,7 +129,7 @@ def lib() -> C.CDLL:
                      "tfe_cache_policy_enable", "tfe_cache_select_victims", "tfe_cache_select_victims_device",
                      "tfe_cache_stats", "tfe_head_create", "tfe_head_topk", "tfe_head_buffers", "tfe_head_status",
                      "tfe_head_geometry", "tfe_mine_ngrams", "tfe_assign_residency", "tfe_cache_select_tuning",
-                     "tfe_distill_forward", "tfe_distill_backward"):
+                     "tfe_distill_forward", "tfe_distill_backward", "tfe_sample_tokens"):
             getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -433,6 +438,15 @@ def tfe_stream_copy(dst, src, nbytes: int, stream=None):
 DTYPE_BF16, DTYPE_F32 = 0, 1
 ROWS_MAX = 1 << 27
 DISTILL_MAX_TOP = 1024
+SAMPLE_MAX_VOCAB = 1 << 24
+
+
+def tfe_sample_tokens(logits, dtype: int, B: int, V: int, ld: int, u, tokens, prob=None, *, temperature=None, top_k=None,
+                      top_p=None, min_p=None, stream=None) -> None:
+    """`logits` is an address: rows `ld` elements apart."""
+    p = TfeSampleParams(_addr(temperature), _addr(top_k), _addr(top_p), _addr(min_p))
+    _check(lib().tfe_sample_tokens(logits, dtype, B, V, ld, C.byref(p), _addr(u), _addr(tokens), _addr(prob),
+                                   _stream(stream)), "tfe_sample_tokens")
 
 
 def tfe_distill_forward(logits, dtype: int, N: int, V: int, ld: int, teacher_ids, teacher_logits, K: int, tau: float,

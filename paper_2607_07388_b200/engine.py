@@ -268,6 +268,27 @@ def _vector(t: torch.Tensor, shape, dtype, device, what: str):
              f"{what}: a contiguous {dtype} tensor of shape {tuple(shape)} on {device} is needed")
 
 
+def sample_tokens(logits: torch.Tensor, u: torch.Tensor, *, temperature: torch.Tensor | None = None,
+                  top_k: torch.Tensor | None = None, top_p: torch.Tensor | None = None, min_p: torch.Tensor | None = None,
+                  stream=None):
+    """(token int32 [B], prob float32 [B]): one draw per row of `logits` [B, V] by the numbers `u` [B] in [0, 1), after
+    temperature, min-p, top-k and top-p (see tfe_sample_tokens).  The settings are device tensors of B values
+    (top_k int32, the others fp32) or None."""
+    b, v, ld = _row_matrix(logits, "logits")
+    dev = logits.device
+    _vector(u, (b,), torch.float32, dev, "u")
+    for t, dtype, what in ((temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"),
+                           (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p")):
+        if t is not None:
+            _vector(t, (b,), dtype, dev, what)
+    with _issue(dev, stream):
+        token = torch.empty(b, dtype=torch.int32, device=dev)
+        prob = torch.empty(b, dtype=torch.float32, device=dev)
+        tfe.tfe_sample_tokens(logits.data_ptr(), _ROW_DTYPES[logits.dtype], b, v, ld, u, token, prob,
+                              temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p, stream=stream)
+    return token, prob
+
+
 def _teacher(logits, teacher_ids, teacher_logits):
     n, v, ld = _row_matrix(logits, "logits")
     _require(teacher_ids.dim() == 2, "teacher_ids: [rows, K] is needed")

@@ -32,3 +32,19 @@ def test_distillation(tfe):
         assert backward(**kw) == tfe.TFE_ERR_INVALID_ARG, kw
     assert forward(N=0, logits=None, ids=None, t=None, loss=None, lse=None) == tfe.TFE_OK
     assert backward(N=0, logits=None, ids=None, t=None, lse=None, g=None, grad=None) == tfe.TFE_OK
+
+
+def test_sampling(tfe):
+    import ctypes as C
+    L = tfe.lib()
+
+    def sample(logits=P, dtype=1, B=2, V=8, ld=8, params=(None, None, None, None), u=P, tokens=P, prob=None):
+        prm = None if params is None else C.byref(tfe.TfeSampleParams(*params))
+        return L.tfe_sample_tokens(logits, dtype, B, V, ld, prm, u, tokens, prob, None)
+
+    for kw in (dict(dtype=2), dict(B=-1), dict(B=tfe.ROWS_MAX + 1), dict(V=0), dict(V=tfe.SAMPLE_MAX_VOCAB + 1, ld=1 << 30), dict(ld=7),
+               dict(ld=1 << 40), dict(logits=None), dict(logits=P + 2), dict(u=None), dict(u=P + 1), dict(tokens=None), dict(tokens=P + 2),
+               dict(prob=P + 2), dict(params=None), dict(params=(P + 1, None, None, None)), dict(params=(None, P + 2, None, None)),
+               dict(params=(None, None, P + 3, None)), dict(params=(None, None, None, P + 1))):
+        assert sample(**kw) == tfe.TFE_ERR_INVALID_ARG, kw
+    assert sample(B=0, logits=None, u=None, tokens=None) == tfe.TFE_OK
