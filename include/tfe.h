@@ -506,6 +506,36 @@ enum { TFE_DTYPE_BF16 = 0, TFE_DTYPE_F32 = 1 };
 #define TFE_ROWS_MAX (1 << 27)
 
 /*
+ * The vocabulary product in 8 bits: the head's contraction (paper Sec. 4.4) with one byte per weight.  Both operands
+ * are e4m3 with an fp32 scale for each block of 128 columns: per row for activations, per 128 rows for weights.
+ *
+ * tfe_quantize_fp8 -- x DEVICE [R][ld], dtype TFE_DTYPE_*, to q DEVICE e4m3 [R][C] (rows side by side) and
+ * scale DEVICE float [ceil(R / block_rows)][ceil(C / 128)];  block_rows 1 (activations) or 128 (weights);
+ * 1 <= C <= TFE_FP8_MAX_COLS, fewer than 2^31 blocks.  scale = max(largest |x| of the block / 448, 2^-126) and
+ * q = x / scale, the quotients correctly rounded to fp32 and then to the nearest e4m3 (ties to even).  A
+ * block that holds an infinity or NaN has it as its scale and reads back as NaN.  One launch.
+ *
+ * tfe_matmul_fp8 --
+ *     out[m][n] = sum_b a_scale[m][b] * w_scale[n / 128][b] * (sum of a[m][k] * w[n][k] over block b's 128 k)
+ *   a DEVICE e4m3 [M][lda], a_scale DEVICE float [M][kb];  w DEVICE e4m3 [N][ldw], w_scale DEVICE float
+ *   [ceil(N / 128)][kb], kb = ceil(K / 128);  out DEVICE [M][ldo], fp32 or bf16.  0 <= M, 1 <= N <= TFE_ROWS_MAX,
+ *   1 <= K <= TFE_FP8_MAX_COLS; a and w 16-byte aligned, lda and ldw multiples of 16.  A block's products are
+ *   summed by the tensor cores, blocks in fp32, and the result is rounded once.  Elements of out beyond N stay as
+ *   they were.  One launch.
+ *
+ * tfe_matmul_fp8_status -- synchronises `stream` and reads the library's status word on the current device: 0, or
+ * bits set by waits inside the kernel that ran out (1 loader, 2 MMA issuer, 4 scales, 8 epilogue); then INTERNAL.
+ * Errors of all three: INVALID_ARG, CUDA.
+ */
+#define TFE_FP8_MAX_COLS (1 << 16)
+tfe_status tfe_quantize_fp8(const void *x, int32_t dtype, int32_t R, int32_t C, int64_t ld, int32_t block_rows,
+                            void *q, float *scale, void *stream);
+tfe_status tfe_matmul_fp8(const void *a, int64_t lda, const float *a_scale, int32_t M, const void *w, int64_t ldw,
+                          const float *w_scale, int32_t N, int32_t K, void *out, int32_t out_dtype, int64_t ldo,
+                          void *stream);
+tfe_status tfe_matmul_fp8_status(uint32_t *device_flags, void *stream);
+
+/*
  * tfe_sample_tokens -- the next token of every sequence from its logits and one given random number per sequence
  * (the lookups are keyed by the token ids that decoding produces; the paper names no sampling rule).  Per row, in
  * the order of descending logits, equal logits by ascending id, with w_i = exp((z_i - z_max) / temperature):

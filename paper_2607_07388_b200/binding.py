@@ -35,7 +35,8 @@ EXPORTS = ["tfe_index_build", "tfe_index_build_device", "tfe_cache_install", "tf
            "tfe_cache_policy_enable", "tfe_cache_select_victims", "tfe_cache_select_victims_device",
            "tfe_cache_stats", "tfe_head_create", "tfe_head_destroy", "tfe_head_topk", "tfe_head_buffers",
            "tfe_head_status", "tfe_head_geometry", "tfe_mine_ngrams", "tfe_mine_workspace_bytes", "tfe_assign_residency", "tfe_stream_copy",
-           "tfe_cache_select_tuning", "tfe_distill_forward", "tfe_distill_backward", "tfe_sample_tokens"]
+           "tfe_cache_select_tuning", "tfe_distill_forward", "tfe_distill_backward", "tfe_sample_tokens",
+           "tfe_quantize_fp8", "tfe_matmul_fp8", "tfe_matmul_fp8_status"]
 
 
 class TfeConfig(C.Structure):
@@ -120,6 +121,9 @@ def lib() -> C.CDLL:
         L.tfe_stream_copy.argtypes = [vp, vp, i64, vp]
         L.tfe_cache_select_tuning.argtypes = [vp, i32, i32, i32]
         f32 = C.c_float
+        L.tfe_quantize_fp8.argtypes = [vp, i32, i32, i32, i64, i32, vp, vp, vp]
+        L.tfe_matmul_fp8.argtypes = [vp, i64, vp, i32, vp, i64, vp, i32, i32, vp, i32, i64, vp]
+        L.tfe_matmul_fp8_status.argtypes = [C.POINTER(C.c_uint32), vp]
         L.tfe_sample_tokens.argtypes = [vp, i32, i32, i32, i64, C.POINTER(TfeSampleParams), vp, vp, vp, vp]
         L.tfe_distill_forward.argtypes = [vp, i32, i32, i32, i64, vp, vp, i32, f32, vp, vp, vp]
         L.tfe_distill_backward.argtypes = [vp, i32, i32, i32, i64, vp, vp, i32, f32, vp, vp, vp, i64, vp]
@@ -129,7 +133,8 @@ def lib() -> C.CDLL:
                      "tfe_cache_policy_enable", "tfe_cache_select_victims", "tfe_cache_select_victims_device",
                      "tfe_cache_stats", "tfe_head_create", "tfe_head_topk", "tfe_head_buffers", "tfe_head_status",
                      "tfe_head_geometry", "tfe_mine_ngrams", "tfe_assign_residency", "tfe_cache_select_tuning",
-                     "tfe_distill_forward", "tfe_distill_backward", "tfe_sample_tokens"):
+                     "tfe_distill_forward", "tfe_distill_backward", "tfe_sample_tokens", "tfe_quantize_fp8",
+                     "tfe_matmul_fp8", "tfe_matmul_fp8_status"):
             getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -462,3 +467,28 @@ def tfe_distill_backward(logits, dtype: int, N: int, V: int, ld: int, teacher_id
     _check(lib().tfe_distill_backward(logits, dtype, N, V, ld, _addr(teacher_ids), _addr(teacher_logits), K, tau,
                                       _addr(lse), _addr(grad_loss), grad_logits, ld_grad, _stream(stream)),
            "tfe_distill_backward")
+
+
+# -- the vocabulary product in 8 bits -----------------------------------------------------------
+FP8_MAX_COLS = 1 << 16
+
+
+def tfe_quantize_fp8(x, dtype: int, R: int, C_: int, ld: int, block_rows: int, q, scale, stream=None) -> None:
+    """`x` and `q` are addresses; x has rows `ld` elements apart, q has them side by side."""
+    _check(lib().tfe_quantize_fp8(x, dtype, R, C_, ld, block_rows, q, _addr(scale), _stream(stream)), "tfe_quantize_fp8")
+
+
+def tfe_matmul_fp8(a, lda: int, a_scale, M: int, w, ldw: int, w_scale, N: int, K: int, out, out_dtype: int, ldo: int,
+                   stream=None) -> None:
+    """`a`, `w` and `out` are addresses of matrices with rows lda, ldw and ldo elements apart."""
+    _check(lib().tfe_matmul_fp8(a, lda, _addr(a_scale), M, w, ldw, _addr(w_scale), N, K, out, out_dtype, ldo,
+                                _stream(stream)), "tfe_matmul_fp8")
+
+
+def tfe_matmul_fp8_status(stream=None) -> int:
+    """Synchronises; returns the device status word (0 = no wait ran out)."""
+    flags = C.c_uint32(0)
+    st = lib().tfe_matmul_fp8_status(C.byref(flags), _stream(stream))
+    if st not in (TFE_OK, TFE_ERR_INTERNAL):
+        _check(st, "tfe_matmul_fp8_status")
+    return flags.value

@@ -1,0 +1,552 @@
+// The vocabulary product with both sides in e4m3 and an fp32 scale for each block of 128 along d: the early-exit head's
+// contraction (paper Sec. 4.4) at half the bytes, and the conversion that makes its operands.
+//
+//   tfe_quantize_rows_kernel     activations: a scale per row and 128 columns.  16 lanes hold a group in registers, so the
+//                                input is read once.
+//   tfe_quantize_blocks_kernel   weights: a scale per 128 rows and 128 columns; one block holds the 128 x 128 piece.
+//   tfe_matmul_fp8_kernel        out[m][n] = sum_b sa[m][b] sb[n / 128][b] (sum over the 128 k of block b of a[m][k] w[n][k])
+//
+// The product is a persistent, warp-specialised tcgen05 kernel.  The weights' rows are the MMA's M (128), the
+// activations' rows its N (16..256): a thread of the epilogue then owns one vocabulary row, stores of one activation row are
+// contiguous across a warp, and few activation rows waste no tensor memory.  The scales change every 128 k, so an
+// accumulator in tensor memory only ever holds one block's partial sum: the epilogue warps read it, multiply by the two scales
+// and add it to fp32 sums in registers while the next block's MMAs run into another accumulator.  The sums over blocks are
+// thereby plain fp32 additions whatever the precision of the tensor core's own accumulation.
+//
+// Few activation rows (one tile): the read of the weights bounds the call, and the vocabulary is cut into equal row ranges,
+// one per SM, each walked in tiles of 128.  Many: tiles of 128 rows are dealt out in turn.
+#include <cuda_fp8.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+
+#include "../../include/tfe.h"
+#include "tfe_internal.h"
+#include "tfe_rows.cuh"
+#include "tfe_tc.cuh"
+
+namespace {
+
+using tfe_rows::Elem;
+
+// ------------------------------------------------------------------ conversion
+
+constexpr int kQuantThreads = 256;
+constexpr int kGroupLanes = 16;                 // lanes that share a group of 128 columns: 8 consecutive elements each
+
+struct QuantParams {
+    const void *x; int64_t ld;
+    int32_t R, C, kb;                           // kb: groups of 128 columns
+    uint8_t *q;                                 // [R][C]
+    float *scale;
+};
+
+__device__ __forceinline__ float scale_of(uint32_t amax_bits)
+{
+    // the bit pattern orders like the value, NaN above infinity: a block that holds either has that as its scale
+    const float amax = __uint_as_float(amax_bits), s = __fdiv_rn(amax, 448.f);
+    return amax_bits >= 0x7F800000u ? amax : fmaxf(s, 0x1p-126f);
+}
+__device__ __forceinline__ uint32_t to_e4m3x4(float a, float b, float c, float d, float s)
+{
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(__fdiv_rn(a, s), __fdiv_rn(b, s)), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(__fdiv_rn(c, s), __fdiv_rn(d, s)), __NV_SATFINITE, __NV_E4M3);
+    return lo | (hi << 16);
+}
+
+// Elements 8 l .. 8 l + 7 of a group whose first column is c0 (kVector: whole 16-byte vectors), zeros beyond the row.
+template <typename T, bool kVector>
+__device__ __forceinline__ void load8(const QuantParams &p, int64_t row, int32_t c0, int l, float (&f)[8])
+{
+    const T *at = static_cast<const T *>(p.x) + row * p.ld + c0;
+    if constexpr (kVector) {
+        const bool in = c0 + 8 * l < p.C;
+        constexpr int E = Elem<T>::kPerVec;
+#pragma unroll
+        for (int h = 0; h < 8 / E; ++h) {
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (in) v = tfe_rows::load_stream(reinterpret_cast<const uint4 *>(at + 8 * l) + h);
+            float part[E];
+            Elem<T>::unpack(v, part);
+#pragma unroll
+            for (int e = 0; e < E; ++e) f[h * E + e] = part[e];
+        }
+    } else {                                    // lane l: columns l, l + 16, ...
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = c0 + l + 16 * e < p.C ? Elem<T>::get(at + l + 16 * e) : 0.f;
+    }
+}
+template <bool kVector>
+__device__ __forceinline__ void store8(const QuantParams &p, int64_t row, int32_t c0, int l, const float (&f)[8], float s)
+{
+    uint8_t *at = p.q + row * p.C + c0;
+    const uint32_t lo = to_e4m3x4(f[0], f[1], f[2], f[3], s), hi = to_e4m3x4(f[4], f[5], f[6], f[7], s);
+    if constexpr (kVector) {
+        if (c0 + 8 * l < p.C) *reinterpret_cast<uint2 *>(at + 8 * l) = make_uint2(lo, hi);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (c0 + l + 16 * e < p.C) at[l + 16 * e] = (uint8_t)((e < 4 ? lo : hi) >> (8 * (e & 3)));
+    }
+}
+__device__ __forceinline__ uint32_t amax8(const float (&f)[8])
+{
+    uint32_t m = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(f[e]) & 0x7FFFFFFFu);
+    return m;
+}
+
+template <typename T, bool kVector>
+__global__ void __launch_bounds__(kQuantThreads)
+tfe_quantize_rows_kernel(const QuantParams p)
+{
+    const int l = threadIdx.x & (kGroupLanes - 1);
+    const uint32_t groups = (uint32_t)p.R * (uint32_t)p.kb;
+    const uint32_t g = (blockIdx.x * kQuantThreads + threadIdx.x) / kGroupLanes;
+    if (g >= groups) return;                    // half-warps leave as a whole
+    const uint32_t half = 0xFFFFu << (threadIdx.x & 16);
+    const uint32_t row = g / (uint32_t)p.kb, b = g - row * (uint32_t)p.kb;
+    float f[8];
+    load8<T, kVector>(p, row, (int32_t)(b * 128), l, f);
+    uint32_t m = amax8(f);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(half, m, o));
+    const float s = scale_of(m);
+    store8<kVector>(p, row, (int32_t)(b * 128), l, f, s);
+    if (l == 0) p.scale[g] = s;
+}
+
+template <typename T, bool kVector>
+__global__ void __launch_bounds__(kQuantThreads)
+tfe_quantize_blocks_kernel(const QuantParams p)
+{
+    constexpr int kRowsAtOnce = kQuantThreads / kGroupLanes, kTurns = 128 / kRowsAtOnce;
+    __shared__ uint32_t s_max[kQuantThreads / 32];
+    const int l = threadIdx.x & (kGroupLanes - 1), hw = threadIdx.x / kGroupLanes;
+    const uint32_t rb = blockIdx.x / (uint32_t)p.kb, b = blockIdx.x - rb * (uint32_t)p.kb;
+    float f[kTurns][8];
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+        const int64_t row = (int64_t)rb * 128 + i * kRowsAtOnce + hw;
+        if (row < p.R) {
+            load8<T, kVector>(p, row, (int32_t)(b * 128), l, f[i]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[i][e] = 0.f;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) m = max(m, amax8(f[i]));
+    m = __reduce_max_sync(0xFFFFFFFFu, m);
+    if ((threadIdx.x & 31) == 0) s_max[threadIdx.x >> 5] = m;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kQuantThreads / 32; ++w) m = max(m, s_max[w]);
+    const float s = scale_of(m);
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+        const int64_t row = (int64_t)rb * 128 + i * kRowsAtOnce + hw;
+        if (row < p.R) store8<kVector>(p, row, (int32_t)(b * 128), l, f[i], s);
+    }
+    if (threadIdx.x == 0) p.scale[blockIdx.x] = s;
+}
+
+// ------------------------------------------------------------------ product
+
+constexpr int kTileRows = 128;                  // weight rows per tile (MMA M)
+constexpr int kBlockK = 128;                    // bytes of a row per stage: one scale block, one 128-byte swizzle row
+constexpr int kUmmaK = 32;                      // e4m3 elements per tcgen05.mma
+constexpr int kMaxStages = 12;
+constexpr int kScaleRing = 4;
+constexpr int kEpilogueWarps = 8;               // two per lane quarter of tensor memory, half of the columns each
+constexpr int kMatmulThreads = 32 * (3 + kEpilogueWarps);
+constexpr int kMatmulSmem = 216 * 1024;         // stages; the rest of an SM's 227 KB is the static arrays and alignment
+
+// bits of the device status word
+constexpr uint32_t kTimeoutLoader = 1u, kTimeoutMma = 2u, kTimeoutScales = 4u, kTimeoutEpilogue = 8u;
+__device__ uint32_t g_matmul_status;
+
+struct MatmulParams {
+    int32_t M, N, kb;                           // activation rows, weight rows, blocks of 128 along k
+    int32_t stages;
+    int32_t m_tiles;
+    int64_t n_units;                            // dealt out: tiles; else unused
+    int32_t rows_per_cta, tail_rows;            // ranges: rows of a CTA, rows of its last short tile
+    const float *a_scale, *b_scale;             // [M][kb], [ceil(N / 128)][kb]
+    void *out; int64_t ldo;
+};
+
+// A CTA's units of work: kRanges: tiles of its own row range; else every gridDim.x-th of all (row tile, m tile).
+template <bool kRanges, int TN>
+struct Units {
+    const MatmulParams &p;
+    int64_t r0, r1;
+    __device__ __forceinline__ Units(const MatmulParams &p_) : p(p_)
+    {
+        r0 = (int64_t)blockIdx.x * p.rows_per_cta;
+        r1 = min((int64_t)p.N, r0 + p.rows_per_cta);
+    }
+    __device__ __forceinline__ bool get(int64_t i, int64_t &n0, int32_t &valid, int32_t &m0) const
+    {
+        if constexpr (kRanges) {
+            n0 = r0 + i * kTileRows;
+            valid = (int32_t)min((int64_t)kTileRows, r1 - n0);
+            m0 = 0;
+            return valid > 0;
+        } else {
+            const int64_t u = blockIdx.x + i * gridDim.x;
+            const int64_t nt = u / p.m_tiles;
+            n0 = nt * kTileRows;
+            valid = (int32_t)min((int64_t)kTileRows, p.N - n0);
+            m0 = (int32_t)(u - nt * p.m_tiles) * TN;
+            return u < p.n_units;
+        }
+    }
+};
+
+// D[tmem] (+)= A[smem] * B[smem]^T, e4m3 inputs, fp32 accumulate; issued by one thread.
+__device__ __forceinline__ void umma_e4m3(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+        :
+        : "r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// Instruction descriptor of kind::f8f6f4: D fp32 (bits [4,6) = 1), A and B e4m3 ([7,10) = [10,13) = 0), both K-major,
+// N >> 3 at [17,23), M >> 4 at [24,29).
+__host__ __device__ constexpr uint32_t umma_idesc_e4m3(uint32_t M, uint32_t N) { return (1u << 4) | ((N >> 3) << 17) | ((M >> 4) << 24); }
+
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&v)[8])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+                 : "r"(taddr)
+                 : "memory");
+}
+
+template <int TN, bool kRanges, typename Out>
+__global__ void __launch_bounds__(kMatmulThreads, 1)
+tfe_matmul_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_w_tail,
+                      const __grid_constant__ CUtensorMap map_a, const MatmulParams p)
+{
+    constexpr int kBuffers = TN == 256 ? 2 : 4;         // accumulators of TN columns
+    constexpr uint32_t kTmemCols = kBuffers * TN;       // 64 .. 512, a power of two
+    constexpr int kCols = TN / 2;                       // columns of an epilogue warp
+    constexpr uint32_t kStageBytes = kTileRows * 128u + TN * 128u;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_acc_full[kBuffers], s_acc_empty[kBuffers];
+    __shared__ __align__(8) uint64_t s_sc_full[kScaleRing], s_sc_empty[kScaleRing], s_drain;
+    __shared__ __align__(16) float s_scale[kScaleRing][TN];
+    __shared__ uint32_t s_tmem_base;
+    __shared__ volatile uint32_t s_abort;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < p.stages; ++s) { mbar_init(smem_u32(&s_full[s]), 1); mbar_init(smem_u32(&s_empty[s]), 1); }
+        for (int a = 0; a < kBuffers; ++a) { mbar_init(smem_u32(&s_acc_full[a]), 1); mbar_init(smem_u32(&s_acc_empty[a]), kEpilogueWarps); }
+        for (int a = 0; a < kScaleRing; ++a) { mbar_init(smem_u32(&s_sc_full[a]), 32); mbar_init(smem_u32(&s_sc_empty[a]), kEpilogueWarps); }
+        mbar_init(smem_u32(&s_drain), 1);
+        s_abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc(smem_u32(&s_tmem_base), kTmemCols);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = s_tmem_base;
+    const Units<kRanges, TN> units(p);
+    int64_t n0;
+    int32_t valid, m0;
+
+    if (warp == 0) {
+        // ============================ TMA producer ============================
+        if (lane == 0) {
+            // weights are read once when there is one tile of activation rows, else again by the tiles beside this one
+            const uint64_t hint_w = kRanges ? 0x12F0000000000000ull : 0x14F0000000000000ull, hint_a = 0x14F0000000000000ull;
+            uint32_t stage = 0, phase = 0, issued = 0;
+            bool ok = true;
+            for (int64_t i = 0; ok && units.get(i, n0, valid, m0); ++i) {
+                const bool tail = kRanges && valid < kTileRows && valid == p.tail_rows;
+                const uint32_t w_bytes = tail ? (uint32_t)p.tail_rows * 128u : kTileRows * 128u;
+                for (int32_t kb = 0; kb < p.kb; ++kb) {
+                    if (!mbar_wait(smem_u32(&s_empty[stage]), phase ^ 1u, &s_abort)) {
+                        atomicOr(&g_matmul_status, kTimeoutLoader);
+                        s_abort = 1;
+                        ok = false;
+                        break;
+                    }
+                    const uint32_t bar = smem_u32(&s_full[stage]), dst = smem_base + stage * kStageBytes;
+                    mbar_expect_tx(bar, w_bytes + TN * 128u);
+                    tma_load_2d(dst, tail ? &map_w_tail : &map_w, bar, kb * kBlockK, (int32_t)n0, hint_w);
+                    tma_load_2d(dst + kTileRows * 128u, &map_a, bar, kb * kBlockK, m0, hint_a);
+                    ++issued;
+                    if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
+                }
+            }
+            if (!ok)                            // copies in flight land before the shared memory goes
+                for (uint32_t s = 0; s < (uint32_t)p.stages; ++s) {
+                    const uint32_t fills = (issued + (uint32_t)p.stages - 1u - s) / (uint32_t)p.stages;
+                    for (uint32_t t = 0; fills && t < TC_WAIT_LIMIT && !mbar_try_wait(smem_u32(&s_full[s]), (fills - 1u) & 1u); ++t) { }
+                }
+        }
+    } else if (warp == 1) {
+        // ============================ MMA issuer ==============================
+        if (lane == 0) {
+            constexpr uint32_t idesc = umma_idesc_e4m3(kTileRows, TN);
+            uint32_t stage = 0, phase = 0, buf = 0, buf_phase = 0;
+            bool ok = true;
+            for (int64_t i = 0; ok && units.get(i, n0, valid, m0); ++i) {
+                for (int32_t kb = 0; kb < p.kb; ++kb) {
+                    if (!mbar_wait(smem_u32(&s_acc_empty[buf]), buf_phase ^ 1u, &s_abort) ||
+                        !mbar_wait(smem_u32(&s_full[stage]), phase, &s_abort)) {
+                        atomicOr(&g_matmul_status, kTimeoutMma);
+                        s_abort = 1;
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint32_t w_addr = smem_base + stage * kStageBytes;
+                    const uint64_t w_desc = umma_desc_sw128(w_addr), a_desc = umma_desc_sw128(w_addr + kTileRows * 128u);
+#pragma unroll
+                    for (int k = 0; k < kBlockK / kUmmaK; ++k)      // 32 bytes further along the swizzled row: +2 in the address field
+                        umma_e4m3(tmem_base + buf * TN, w_desc + (uint64_t)(2 * k), a_desc + (uint64_t)(2 * k), idesc, k > 0 ? 1u : 0u);
+                    umma_commit(smem_u32(&s_empty[stage]));
+                    umma_commit(smem_u32(&s_acc_full[buf]));
+                    if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
+                    if (++buf == kBuffers) { buf = 0; buf_phase ^= 1u; }
+                }
+            }
+            if (!ok) {                          // MMAs in flight end before their tensor memory is freed
+                umma_commit(smem_u32(&s_drain));
+                for (uint32_t t = 0; t < TC_WAIT_LIMIT && !mbar_try_wait(smem_u32(&s_drain), 0); ++t) { }
+            }
+        }
+    } else if (warp == 2) {
+        // ============================ activation scales =======================
+        uint32_t st = 0, phase = 0;
+        bool ok = true;
+        for (int64_t i = 0; ok && units.get(i, n0, valid, m0); ++i) {
+            for (int32_t kb = 0; kb < p.kb; ++kb) {
+                float v[(TN + 31) / 32];
+                const float sb = kRanges ? 1.f : __ldg(p.b_scale + (n0 / 128) * p.kb + kb);
+#pragma unroll
+                for (int c = 0; c < (TN + 31) / 32; ++c) {
+                    const int32_t m = m0 + c * 32 + lane;
+                    v[c] = m < p.M ? __ldg(p.a_scale + (int64_t)m * p.kb + kb) * sb : 0.f;
+                }
+                ok = mbar_wait(smem_u32(&s_sc_empty[st]), phase ^ 1u, &s_abort);
+                if (!__all_sync(0xFFFFFFFFu, ok)) {
+                    if (lane == 0) atomicOr(&g_matmul_status, kTimeoutScales);
+                    s_abort = 1;
+                    ok = false;
+                    break;
+                }
+#pragma unroll
+                for (int c = 0; c < (TN + 31) / 32; ++c)
+                    if (c * 32 + lane < TN) s_scale[st][c * 32 + lane] = v[c];
+                mbar_arrive(smem_u32(&s_sc_full[st]));
+                if (++st == kScaleRing) { st = 0; phase ^= 1u; }
+            }
+        }
+    } else {
+        // ============================ epilogue ================================
+        const uint32_t quarter = (uint32_t)warp & 3u;               // tensor-memory lanes 32 * quarter .. + 31
+        const int32_t c0 = ((warp - 3) >> 2) * kCols;               // this warp's columns
+        const int32_t row_in_tile = (int32_t)(quarter * 32u) + lane;
+        constexpr int kChunk = kCols >= 16 ? 16 : 8;
+        uint32_t st = 0, phase = 0, buf = 0, buf_phase = 0;
+        bool ok = true;
+        for (int64_t i = 0; ok && units.get(i, n0, valid, m0); ++i) {
+            const int64_t n = n0 + row_in_tile;
+            float acc[kCols];
+#pragma unroll
+            for (int j = 0; j < kCols; ++j) acc[j] = 0.f;
+            const float *sb_row = p.b_scale + (row_in_tile < valid ? n / 128 : n0 / 128) * p.kb;
+            float sb_next = kRanges ? __ldg(sb_row) : 1.f;
+            for (int32_t kb = 0; kb < p.kb; ++kb) {
+                const float sb = sb_next;
+                if (kRanges && kb + 1 < p.kb) sb_next = __ldg(sb_row + kb + 1);
+                ok = mbar_wait(smem_u32(&s_sc_full[st]), phase, &s_abort) && mbar_wait(smem_u32(&s_acc_full[buf]), buf_phase, &s_abort);
+                if (!__all_sync(0xFFFFFFFFu, ok)) {
+                    if (lane == 0) atomicOr(&g_matmul_status, kTimeoutEpilogue);
+                    s_abort = 1;
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
+                const uint32_t taddr = tmem_base + ((quarter * 32u) << 16) + buf * TN + (uint32_t)c0;
+#pragma unroll
+                for (int c = 0; c < kCols; c += kChunk) {
+                    uint32_t v[kChunk];
+                    if constexpr (kChunk == 16) tmem_ld16(taddr + (uint32_t)c, v); else tmem_ld8(taddr + (uint32_t)c, v);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < kChunk; j += 4) {
+                        const float4 sa = *reinterpret_cast<const float4 *>(&s_scale[st][c0 + c + j]);
+                        acc[c + j] = fmaf(__uint_as_float(v[j]), kRanges ? sa.x * sb : sa.x, acc[c + j]);
+                        acc[c + j + 1] = fmaf(__uint_as_float(v[j + 1]), kRanges ? sa.y * sb : sa.y, acc[c + j + 1]);
+                        acc[c + j + 2] = fmaf(__uint_as_float(v[j + 2]), kRanges ? sa.z * sb : sa.z, acc[c + j + 2]);
+                        acc[c + j + 3] = fmaf(__uint_as_float(v[j + 3]), kRanges ? sa.w * sb : sa.w, acc[c + j + 3]);
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) { mbar_arrive(smem_u32(&s_acc_empty[buf])); mbar_arrive(smem_u32(&s_sc_empty[st])); }
+                if (++st == kScaleRing) { st = 0; phase ^= 1u; }
+                if (++buf == kBuffers) { buf = 0; buf_phase ^= 1u; }
+            }
+            if (ok && row_in_tile < valid) {
+                Out *at = static_cast<Out *>(p.out) + (int64_t)(m0 + c0) * p.ldo + n;
+                const int32_t left = p.M - m0 - c0;
+#pragma unroll
+                for (int j = 0; j < kCols; ++j)
+                    if (j < left) Elem<Out>::put(at + (int64_t)j * p.ldo, acc[j]);
+            }
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        __syncwarp();
+        tc_fence_after();
+        tmem_dealloc(tmem_base, kTmemCols);
+    }
+}
+
+// ------------------------------------------------------------------ host side
+
+// e4m3 matrix [rows][cols], rows `ld` bytes apart; box = 128 columns x box_rows rows, 128-byte swizzle, zeros outside
+bool make_map_fp8(CUtensorMap *map, const void *base, int64_t rows, int64_t cols, int64_t ld, uint32_t box_rows)
+{
+    encode_tiled_fn enc = get_encode_tiled();
+    if (!enc) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)ld};
+    const cuuint32_t box[2] = {(cuuint32_t)kBlockK, box_rows};
+    const cuuint32_t estr[2] = {1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int TN, bool kRanges, typename Out>
+tfe_status launch_matmul(int grid, cudaStream_t stream, const CUtensorMap &w, const CUtensorMap &w_tail, const CUtensorMap &a, MatmulParams p)
+{
+    constexpr size_t stage = kTileRows * 128 + TN * 128;
+    p.stages = (int32_t)std::min<size_t>(kMaxStages, (kMatmulSmem - 1024) / stage);
+    auto kernel = tfe_matmul_fp8_kernel<TN, kRanges, Out>;
+    const size_t smem = (size_t)p.stages * stage + 1024;
+    if (tfe_status st = tfe_note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem), "product attribute")) return st;
+    kernel<<<grid, kMatmulThreads, smem, stream>>>(w, w_tail, a, p);
+    return tfe_note_cuda(cudaGetLastError(), "product launch");
+}
+
+template <int TN, bool kRanges>
+tfe_status launch_matmul(int32_t out_dtype, int grid, cudaStream_t stream, const CUtensorMap &w, const CUtensorMap &w_tail, const CUtensorMap &a,
+                         const MatmulParams &p)
+{
+    return out_dtype == TFE_DTYPE_BF16 ? launch_matmul<TN, kRanges, __nv_bfloat16>(grid, stream, w, w_tail, a, p)
+                                       : launch_matmul<TN, kRanges, float>(grid, stream, w, w_tail, a, p);
+}
+
+bool aligned(const void *ptr, uintptr_t to) { return ptr && reinterpret_cast<uintptr_t>(ptr) % to == 0; }
+
+}  // namespace
+
+extern "C" {
+
+tfe_status tfe_quantize_fp8(const void *x, int32_t dtype, int32_t R, int32_t C, int64_t ld, int32_t block_rows, void *q, float *scale, void *stream_)
+{
+    if (dtype != TFE_DTYPE_BF16 && dtype != TFE_DTYPE_F32) return TFE_ERR_INVALID_ARG;
+    if (block_rows != 1 && block_rows != 128) return TFE_ERR_INVALID_ARG;
+    if (R < 0 || C < 1 || C > TFE_FP8_MAX_COLS || ld < C || ld > (1ll << 34)) return TFE_ERR_INVALID_ARG;
+    QuantParams p{};
+    p.kb = (C + 127) / 128;
+    const int64_t groups = ((int64_t)R + block_rows - 1) / block_rows * p.kb;
+    if (groups > 0x7FFFFFFFll) return TFE_ERR_INVALID_ARG;
+    if (R == 0) return TFE_OK;
+    const int es = dtype == TFE_DTYPE_BF16 ? 2 : 4;
+    if (!aligned(x, es) || !q || !aligned(scale, 4)) return TFE_ERR_INVALID_ARG;
+    p.x = x; p.ld = ld; p.R = R; p.C = C; p.q = static_cast<uint8_t *>(q); p.scale = scale;
+    // 16-byte loads and 8-byte stores where every row starts on such a boundary
+    const bool vec = aligned(x, 16) && ld * es % 16 == 0 && C % 8 == 0 && aligned(q, 8);
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    const unsigned grid = block_rows == 1 ? (unsigned)((groups * kGroupLanes + kQuantThreads - 1) / kQuantThreads) : (unsigned)groups;
+    auto go = [&](auto rows_kernel, auto blocks_kernel) {
+        if (block_rows == 1) rows_kernel<<<grid, kQuantThreads, 0, stream>>>(p);
+        else blocks_kernel<<<grid, kQuantThreads, 0, stream>>>(p);
+    };
+    if (dtype == TFE_DTYPE_BF16) {
+        if (vec) go(tfe_quantize_rows_kernel<__nv_bfloat16, true>, tfe_quantize_blocks_kernel<__nv_bfloat16, true>);
+        else go(tfe_quantize_rows_kernel<__nv_bfloat16, false>, tfe_quantize_blocks_kernel<__nv_bfloat16, false>);
+    } else {
+        if (vec) go(tfe_quantize_rows_kernel<float, true>, tfe_quantize_blocks_kernel<float, true>);
+        else go(tfe_quantize_rows_kernel<float, false>, tfe_quantize_blocks_kernel<float, false>);
+    }
+    return tfe_note_cuda(cudaGetLastError(), "conversion launch");
+}
+
+tfe_status tfe_matmul_fp8(const void *a, int64_t lda, const float *a_scale, int32_t M, const void *w, int64_t ldw, const float *w_scale, int32_t N,
+                          int32_t K, void *out, int32_t out_dtype, int64_t ldo, void *stream_)
+{
+    if (out_dtype != TFE_DTYPE_BF16 && out_dtype != TFE_DTYPE_F32) return TFE_ERR_INVALID_ARG;
+    if (M < 0 || M > TFE_ROWS_MAX || N < 1 || N > TFE_ROWS_MAX || K < 1 || K > TFE_FP8_MAX_COLS) return TFE_ERR_INVALID_ARG;
+    if (lda < K || lda % 16 != 0 || lda > (1ll << 34) || ldw < K || ldw % 16 != 0 || ldw > (1ll << 34) || ldo < N || ldo > (1ll << 34))
+        return TFE_ERR_INVALID_ARG;
+    if (M == 0) return TFE_OK;
+    if (!aligned(a, 16) || !aligned(w, 16) || !aligned(a_scale, 4) || !aligned(w_scale, 4) || !aligned(out, out_dtype == TFE_DTYPE_BF16 ? 2 : 4))
+        return TFE_ERR_INVALID_ARG;
+    int dev = 0, sms = 0;
+    if (tfe_status st = tfe_note_cuda(cudaGetDevice(&dev), "cudaGetDevice")) return st;
+    if (tfe_status st = tfe_note_cuda(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev), "cudaDeviceGetAttribute")) return st;
+    MatmulParams p{};
+    p.M = M; p.N = N; p.kb = (K + kBlockK - 1) / kBlockK;
+    p.a_scale = a_scale; p.b_scale = w_scale; p.out = out; p.ldo = ldo;
+    const int tn = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : 256;
+    int grid;
+    uint32_t tail = 8;
+    if (M <= tn) {
+        p.m_tiles = 1;
+        p.rows_per_cta = (int32_t)((((int64_t)N + sms - 1) / sms + 7) / 8 * 8);
+        grid = (int)(((int64_t)N + p.rows_per_cta - 1) / p.rows_per_cta);
+        p.tail_rows = p.rows_per_cta % kTileRows;
+        if (p.tail_rows) tail = (uint32_t)p.tail_rows;
+    } else {
+        p.m_tiles = (M + tn - 1) / tn;
+        p.n_units = ((int64_t)N + kTileRows - 1) / kTileRows * p.m_tiles;
+        grid = (int)std::min<int64_t>(sms, p.n_units);
+    }
+    CUtensorMap map_w, map_w_tail, map_a;
+    if (!make_map_fp8(&map_w, w, N, K, ldw, kTileRows) || !make_map_fp8(&map_w_tail, w, N, K, ldw, tail) || !make_map_fp8(&map_a, a, M, K, lda, (uint32_t)tn))
+        return tfe_note_cuda(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    switch (tn) {
+    case 16: return launch_matmul<16, true>(out_dtype, grid, stream, map_w, map_w_tail, map_a, p);
+    case 32: return launch_matmul<32, true>(out_dtype, grid, stream, map_w, map_w_tail, map_a, p);
+    case 64: return launch_matmul<64, true>(out_dtype, grid, stream, map_w, map_w_tail, map_a, p);
+    case 128: return launch_matmul<128, true>(out_dtype, grid, stream, map_w, map_w_tail, map_a, p);
+    default:
+        return p.m_tiles == 1 ? launch_matmul<256, true>(out_dtype, grid, stream, map_w, map_w_tail, map_a, p)
+                              : launch_matmul<256, false>(out_dtype, grid, stream, map_w, map_w_tail, map_a, p);
+    }
+}
+
+tfe_status tfe_matmul_fp8_status(uint32_t *device_flags, void *stream_)
+{
+    if (!device_flags) return TFE_ERR_INVALID_ARG;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    void *at = nullptr;
+    if (tfe_status st = tfe_note_cuda(cudaGetSymbolAddress(&at, g_matmul_status), "cudaGetSymbolAddress")) return st;
+    if (tfe_status st = tfe_note_cuda(cudaMemcpyAsync(device_flags, at, sizeof(uint32_t), cudaMemcpyDeviceToHost, stream), "cudaMemcpyAsync")) return st;
+    if (tfe_status st = tfe_note_cuda(cudaStreamSynchronize(stream), "cudaStreamSynchronize")) return st;
+    return *device_flags ? TFE_ERR_INTERNAL : TFE_OK;
+}
+
+}  // extern "C"

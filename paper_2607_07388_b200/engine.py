@@ -268,6 +268,72 @@ def _vector(t: torch.Tensor, shape, dtype, device, what: str):
              f"{what}: a contiguous {dtype} tensor of shape {tuple(shape)} on {device} is needed")
 
 
+def quantize_fp8(x: torch.Tensor, block_rows: int = 1, *, stream=None):
+    """(q float8_e4m3fn [R, C], scale float32): `x` [R, C] in 8 bits with a scale for every `block_rows` x 128 values -- 1
+    for activations, 128 for weights (see tfe_quantize_fp8)."""
+    r, c, ld = _row_matrix(x, "x")
+    _require(block_rows in (1, 128), "block_rows: 1 or 128")
+    with _issue(x.device, stream):
+        q = torch.empty((r, c), dtype=torch.float8_e4m3fn, device=x.device)
+        scale = torch.empty((-(-r // block_rows), -(-c // 128)), dtype=torch.float32, device=x.device)
+        tfe.tfe_quantize_fp8(x.data_ptr(), _ROW_DTYPES[x.dtype], r, c, ld, block_rows, q.data_ptr(), scale, stream)
+    return q, scale
+
+
+def _fp8_matrix(t: torch.Tensor, what: str):
+    _require(t.is_cuda and t.dim() == 2 and t.dtype == torch.float8_e4m3fn, f"{what}: a 2-D float8_e4m3fn CUDA tensor is needed")
+    n, k = t.shape
+    ld = t.stride(0) if n > 1 else -(-k // 16) * 16
+    _require(k >= 1 and (t.stride(1) == 1 or k == 1) and ld >= k and ld % 16 == 0 and t.data_ptr() % 16 == 0,
+             f"{what}: contiguous rows that start on 16-byte boundaries are needed")
+    return n, k, ld
+
+
+def matmul_fp8(a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, *,
+               out_dtype: torch.dtype = torch.float32, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """a [M, K] times the transpose of w [N, K], both as quantize_fp8 makes them (block_rows 1 and 128): [M, N] in fp32 or
+    bf16 (see tfe_matmul_fp8).  `out`: where it goes instead of a new tensor."""
+    m, k, lda = _fp8_matrix(a, "a")
+    n, kw, ldw = _fp8_matrix(w, "w")
+    dev = a.device
+    _require(n >= 1 and kw == k and w.device == dev, "w: the width and device of a are needed")
+    kb = -(-k // 128)
+    _vector(a_scale, (m, kb), torch.float32, dev, "a_scale")
+    _vector(w_scale, (-(-n // 128), kb), torch.float32, dev, "w_scale")
+    with _issue(dev, stream):
+        if out is None:
+            _require(out_dtype in _ROW_DTYPES, "out_dtype: bfloat16 or float32")
+            out = torch.empty((m, n), dtype=out_dtype, device=dev)
+        om, on, ldo = _row_matrix(out, "out")
+        _require((om, on) == (m, n) and out.device == dev, "out: [M, N] on the operands' device is needed")
+        tfe.tfe_matmul_fp8(a.data_ptr(), lda, a_scale, m, w.data_ptr(), ldw, w_scale, n, k, out.data_ptr(),
+                           _ROW_DTYPES[out.dtype], ldo, stream)
+    return out
+
+
+class QuantizedHead:
+    """The vocabulary projection in 8 bits: half the bytes of EarlyExitHead's weights to read per call, logits instead of a
+    top-K.  ``w``: bf16 or fp32 [V, d], d a multiple of 16; it is converted once and not kept."""
+
+    def __init__(self, w: torch.Tensor):
+        _require(w.dim() == 2 and w.shape[1] % 16 == 0, "w: [V, d] with d a multiple of 16 is needed")
+        self.V, self.d = w.shape
+        self.w, self.w_scale = quantize_fp8(w, block_rows=128)
+
+    def logits(self, hidden: torch.Tensor, out_dtype: torch.dtype = torch.float32, out: torch.Tensor | None = None, *,
+               stream=None) -> torch.Tensor:
+        """[B, V] logits of `hidden` [B, d], whose rows are converted within the call."""
+        _require(hidden.dim() == 2 and hidden.shape[1] == self.d, f"hidden: [B, {self.d}] is needed")
+        with _issue(hidden.device, stream):
+            q, scale = quantize_fp8(hidden, block_rows=1)
+            return matmul_fp8(q, scale, self.w, self.w_scale, out_dtype=out_dtype, out=out)
+
+    def sample(self, hidden: torch.Tensor, u: torch.Tensor, *, stream=None, **settings):
+        """(token, prob) of one draw per row of `hidden` by `u` (see sample_tokens for the settings)."""
+        with _issue(hidden.device, stream):
+            return sample_tokens(self.logits(hidden), u, **settings)
+
+
 def sample_tokens(logits: torch.Tensor, u: torch.Tensor, *, temperature: torch.Tensor | None = None,
                   top_k: torch.Tensor | None = None, top_p: torch.Tensor | None = None, min_p: torch.Tensor | None = None,
                   stream=None):

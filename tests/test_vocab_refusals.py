@@ -48,3 +48,29 @@ def test_sampling(tfe):
                dict(params=(None, None, P + 3, None)), dict(params=(None, None, None, P + 1))):
         assert sample(**kw) == tfe.TFE_ERR_INVALID_ARG, kw
     assert sample(B=0, logits=None, u=None, tokens=None) == tfe.TFE_OK
+
+
+def test_conversion_and_product_in_8_bits(tfe):
+    import ctypes as C
+    L = tfe.lib()
+
+    def quantize(x=P, dtype=1, R=2, C_=8, ld=8, block_rows=1, q=P, scale=P):
+        return L.tfe_quantize_fp8(x, dtype, R, C_, ld, block_rows, q, scale, None)
+
+    for kw in (dict(dtype=2), dict(R=-1), dict(C_=0), dict(C_=tfe.FP8_MAX_COLS + 1, ld=1 << 20), dict(ld=7), dict(ld=1 << 40), dict(block_rows=0),
+               dict(block_rows=64), dict(x=None), dict(x=P + 2), dict(q=None), dict(scale=None), dict(scale=P + 2),
+               dict(R=(1 << 31) - 1, C_=256, ld=256)):
+        assert quantize(**kw) == tfe.TFE_ERR_INVALID_ARG, kw
+    assert quantize(R=0, x=None, q=None, scale=None) == tfe.TFE_OK
+
+    def product(a=P, lda=64, sa=P, M=2, w=P, ldw=64, sw=P, N=8, K=64, out=P, dtype=1, ldo=8):
+        return L.tfe_matmul_fp8(a, lda, sa, M, w, ldw, sw, N, K, out, dtype, ldo, None)
+
+    for kw in (dict(a=None), dict(a=P + 8), dict(lda=63), dict(lda=72), dict(lda=1 << 40), dict(sa=None), dict(sa=P + 2), dict(M=-1),
+               dict(M=tfe.ROWS_MAX + 1), dict(w=None), dict(w=P + 4), dict(ldw=48), dict(ldw=65), dict(sw=None), dict(sw=P + 1), dict(N=0),
+               dict(N=tfe.ROWS_MAX + 1, ldo=1 << 30), dict(K=0), dict(K=65), dict(K=tfe.FP8_MAX_COLS + 1, lda=1 << 20, ldw=1 << 20),
+               dict(out=None), dict(out=P + 2), dict(dtype=2), dict(dtype=-1), dict(ldo=7), dict(ldo=1 << 40)):
+        assert product(**kw) == tfe.TFE_ERR_INVALID_ARG, kw
+    assert product(M=0, a=None, sa=None, w=None, sw=None, out=None) == tfe.TFE_OK
+    assert L.tfe_matmul_fp8_status(None, None) == tfe.TFE_ERR_INVALID_ARG
+    assert L.tfe_matmul_fp8_status.argtypes[0] == C.POINTER(C.c_uint32)
