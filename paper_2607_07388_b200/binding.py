@@ -153,10 +153,17 @@ def _addr(x):
     return x.data_ptr()
 
 
+_raw_stream = None      # torch's current stream of a device as a plain address: (device index) -> int
+
+
 def _stream(stream):
     if stream is None:
+        global _raw_stream
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        if _raw_stream is None:         # torch's own shortcut makes no stream object: 0.4 us instead of 3.2 us a call
+            _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+                (lambda device: torch.cuda.current_stream(device).cuda_stream)
+        return _raw_stream(torch.cuda.current_device())
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 

@@ -7,20 +7,22 @@
 //     top-k   the first k entries; their mass is S1
 //     top-p   the shortest prefix of them with a mass of at least p S1; its mass is S2
 //     draw    the first entry whose running mass exceeds u S2
-// No sort of the row: a histogram of counts and masses over (z_max - z) / T locates each search's bin, and only that
-// bin's entries (or, where the kept prefix is short, all entries up to it) are collected and sorted.
+// No sort of the row.  One pass counts the entries by bins of (z_max - z) / T, with the sum of their offsets in the bin; a
+// bin's mass is then known to about 1e-5 of the total (its count times the weight at its mean), which names for every search
+// the bin, seldom two, that holds its end.  One more pass sums the exact mass above those bins and collects their entries,
+// which the first block sorts and searches.  Where the kept prefix is short all of it is collected and no sum is needed.
+// Bins with more entries than the list (long runs of equal logits) send the row through an exact selection by key digits.
 //
-// A row is taken by a cluster of blocks, each holding its slice of the logits in shared memory where it fits, so the row
-// is read from HBM once; the histograms are added over distributed shared memory and the first block decides.
+// A row is taken by a cluster of blocks, many rows by a block each; a slice that fits stays in shared memory.
 //
 // Numbers: a token's choice turns on sums of up to 10^5 nearly equal weights, next to borders 10^-5 apart, so weights are
-// evaluated in 64 bits (relative error about 1e-14) and summed as 64-bit integers in units of 2^-shift -- exact, and the
-// same in any order.  What bounds the kernel is that arithmetic (about 20 fp64 operations a logit) and the latency of
-// its steps, not the read of the logits.
+// evaluated in 64 bits (relative error below 1e-14) and summed as 64-bit integers in units of 2^-shift -- exact, and the
+// same in any order.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <cstddef>
 #include <cstdint>
 
 #include "../../include/tfe.h"
@@ -34,7 +36,7 @@ namespace cg = cooperative_groups;
 typedef unsigned long long u64;
 
 constexpr int kThreads = 512;
-constexpr int kBins = 2048;
+constexpr int kBins = 4096;
 constexpr int kList = 1024;             // entries that are collected and sorted at once
 constexpr float kRange = 32.f;          // weights below exp(-32) share the last bin
 
@@ -63,99 +65,114 @@ __device__ __forceinline__ float key_logit(u64 key)
 }
 __device__ __forceinline__ int32_t key_index(u64 key) { return (int32_t)~(uint32_t)key; }
 
-// exp(x) for x <= 0 in 64 bits: x = n ln 2 + r, |r| <= ln 2 / 2, Taylor's series of exp(r) to the 11th power (the first
-// term left out is below 7e-15), scaled by 2^n.  exp(0) is 1 exactly; 0 below -700.
-__device__ __forceinline__ double exp64(double x)
-{
-    if (!(x > -700.0)) return 0.0;
-    const double n = rint(x * 1.4426950408889634);
-    double r = fma(n, -0.693147180559945286, x);         // ln 2 in two parts
-    r = fma(n, -2.31904681384629956e-17, r);
-    double p = 1.0 / 39916800.0;
-    p = fma(p, r, 1.0 / 3628800.0);
-    p = fma(p, r, 1.0 / 362880.0);
-    p = fma(p, r, 1.0 / 40320.0);
-    p = fma(p, r, 1.0 / 5040.0);
-    p = fma(p, r, 1.0 / 720.0);
-    p = fma(p, r, 1.0 / 120.0);
-    p = fma(p, r, 1.0 / 24.0);
-    p = fma(p, r, 1.0 / 6.0);
-    p = fma(p, r, 0.5);
-    p = fma(p, r, 1.0);
-    p = fma(p, r, 1.0);
-    return __hiloint2double(__double2hiint(p) + ((int)n << 20), __double2loint(p));
-}
-
 struct RowRule {
-    double inv_t, cut;                  // entries with z < cut are out
-    double scale;                       // 2^shift
-    float top, inv_t32, bins_per;       // bin = (top - z) * inv_t32 * bins_per
+    double top, a;                      // a = 16 log2(e) / T
+    float topf, cut;                    // entries with z < cut are out; cut is finite or +inf, so -inf and NaN always are
+    float bins;                         // 256 bins per unit of top - z
+    float reach;                        // beyond this difference nothing of a weight is left
+    int shift;
 };
 
-__device__ __forceinline__ u64 mass_of(const RowRule &q, float z)
+constexpr double kWhole = 4503599627370496.0;           // 2^52: what is added to it is rounded to a whole number
+
+// w 2^shift rounded to a whole number (kRound) or not, with w = exp((z - top) / T) in 64 bits: y = 16 log2 w = n + f, n
+// whole, |f| <= 1/2, so w = 2^(n / 16) 2^(f / 16); the first factor from a table of 2^(j / 16) (16 entries, so that a warp's
+// reads never meet in a bank) and an exponent, the second by Taylor's series to the sixth power (|f| ln 2 / 16 is at most
+// 0.0217; the first term left out is below 5e-16).  The maximum weighs 2^shift exactly.  For logits within reach only.
+template <bool kRound>
+__device__ __forceinline__ double weight_of(const RowRule &q, const double *table, float z)
 {
-    // an infinite maximum: its equals weigh 1, the rest nothing; an infinite temperature: all finite logits weigh 1
-    const double x = z == q.top ? 0.0 : ((double)z - (double)q.top) * q.inv_t;
-    return (u64)__double2ull_rn(exp64(x) * q.scale);
+    const double y = ((double)fminf(z, 3.402823466e38f) - q.top) * q.a;
+    constexpr double magic = 1.5 * kWhole;              // the low bits hold the whole number, negative ones too
+    const double shifted = y + magic;
+    const int n = __double2loint(shifted);
+    const double f = y - (shifted - magic);
+    constexpr double c = 0.6931471805599453 / 16;
+    double p = c * c * c * c * c * c / 720;
+    p = fma(p, f, c * c * c * c * c / 120);
+    p = fma(p, f, c * c * c * c / 24);
+    p = fma(p, f, c * c * c / 6);
+    p = fma(p, f, c * c / 2);
+    p = fma(p, f, c);
+    p = fma(p, f, 1.0);
+    p *= table[n & 15];
+    const double e = __hiloint2double((int)((uint32_t)(n & ~15) << 16) + ((1023 + q.shift) << 20), 0);
+    return kRound ? fma(p, e, kWhole) - kWhole : p * e;
 }
-__device__ __forceinline__ bool kept(const RowRule &q, float z) { return z > -INFINITY && (double)z >= q.cut; }   // false for NaN
-__device__ __forceinline__ int bin_of(const RowRule &q, float z)
+__device__ __forceinline__ u64 whole_bits(double x)     // of a whole number below 2^52
 {
-    const float t = z == q.top ? 0.f : (q.top - z) * q.inv_t32 * q.bins_per;      // not increasing in z; may be +inf, or NaN (0 * inf: bin 0)
-    return t < (float)kBins ? (int)t : (t >= (float)kBins ? kBins - 1 : 0);
+    return (u64)__double_as_longlong(x + kWhole) & 0xFFFFFFFFFFFFFull;
+}
+__device__ __forceinline__ bool in_reach(const RowRule &q, float z) { return !(q.topf - z > q.reach); }
+__device__ __forceinline__ u64 mass_of(const RowRule &q, const double *table, float z)
+{
+    return in_reach(q, z) ? whole_bits(weight_of<true>(q, table, z)) : 0;
 }
 
+// Place of a kept logit: 256 times its distance from the maximum in bins, rounded; the bin is place >> 8.  Not decreasing
+// as z falls.  What lies beyond the last bin is in it.
+__device__ __forceinline__ uint32_t place_of(const RowRule &q, float z)
+{
+    return __float_as_uint(fminf((q.topf - z) * q.bins, (float)(256 * kBins - 1)) + 8388608.f) & 0x7FFFFFu;
+}
 
 enum { kOpDone = 0, kOpCollect = 1, kOpDigits = 2 };
+enum { kTopK = 0, kTopP = 1, kDraw = 2, kSearches = 3 };
 struct Command {                        // what the first block asks of its cluster
     int op;
-    int lo, hi;                         // bins concerned
+    int by_bins;                        // kOpCollect: by the bins below, or by (key & mask) == prefix
+    int sums;                           // by bins: 0 no masses, 1 those below the searches' bins, 2 of all entries too
+    uint32_t lo[kSearches], hi[kSearches];      // by bins: places [lo, hi) of the searches (hi <= lo: none)
     int shift;                          // kOpDigits: histogram of (key >> shift) & 255
     u64 prefix, mask;                   // only entries with (key & mask) == prefix
 };
 
 struct alignas(16) Shared {
-    u64 mass[kBins];                    // histogram; afterwards, in the first block, its running sums
     u64 list[kList];
+    u64 run[kList];                     // in the first block: running masses of the sorted list
     u64 digit_mass[256];
-    u64 warp64[kThreads / 32];
-    u64 best;                           // greatest key of the slice
+    double table[16];                   // 2^(j / 16)
+    u64 warp64[kSearches][kThreads / 32];
+    u64 below[kSearches];               // masses below the top-p and the draw's bins, and of all entries
     u64 found_mass, found_key;
     Command cmd;
-    uint32_t count[kBins];
+    alignas(16) uint32_t count[kBins];  // entries; afterwards, in the first block, running sums
+    union { alignas(16) uint32_t offset[kBins]; alignas(16) float estimate[kBins]; };   // sums of place & 255; afterwards running masses by estimate
     uint32_t digit_count[256];
     uint32_t warp32[kThreads / 32];
+    float warp_f[kThreads / 32];
     uint32_t fill;
-    float low;                          // least logit above -inf of the slice
+    float warp_top[kThreads / 32];
+    float top, low;                     // greatest logit of the slice, and the least unmasked one
+    int32_t first;                      // index of the first greatest logit
     uint32_t found_count;
     int found_at;
+    uint32_t from_i[kSearches], to_i[kSearches], before_n[kSearches];   // of each search: its entries in the sorted list, those before
+    bool too_many;                      // for the list: the bins are not collected
 };
+static_assert(offsetof(Shared, count) % 16 == 0 && offsetof(Shared, offset) % 16 == 0 && sizeof(Shared) % 16 == 0, "16-byte accesses");
 
-// Inclusive sums over the block in thread order.  All threads call it; the shared scratch is free again on return.
-__device__ __forceinline__ void block_scan(Shared &s, uint32_t &c, u64 &m)
+// Inclusive sums over the block in thread order.  All threads call it; the scratch is free again on return.
+template <typename A>
+__device__ __forceinline__ A block_scan(A *scratch, A x)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t oc = __shfl_up_sync(0xFFFFFFFFu, c, o);
-        const u64 om = __shfl_up_sync(0xFFFFFFFFu, m, o);
-        if (lane >= o) { c += oc; m += om; }
+        const A other = __shfl_up_sync(0xFFFFFFFFu, x, o);
+        if (lane >= o) x += other;
     }
-    if (lane == 31) { s.warp32[warp] = c; s.warp64[warp] = m; }
+    if (lane == 31) scratch[warp] = x;
     __syncthreads();
-    uint32_t wc = lane < kThreads / 32 ? s.warp32[lane] : 0;
-    u64 wm = lane < kThreads / 32 ? s.warp64[lane] : 0;
+    A w = lane < kThreads / 32 ? scratch[lane] : A(0);
 #pragma unroll
     for (int o = 1; o < kThreads / 32; o <<= 1) {
-        const uint32_t oc = __shfl_up_sync(0xFFFFFFFFu, wc, o);
-        const u64 om = __shfl_up_sync(0xFFFFFFFFu, wm, o);
-        if (lane >= o) { wc += oc; wm += om; }
+        const A other = __shfl_up_sync(0xFFFFFFFFu, w, o);
+        if (lane >= o) w += other;
     }
-    if (warp > 0) {
-        c += __shfl_sync(0xFFFFFFFFu, wc, warp - 1);
-        m += __shfl_sync(0xFFFFFFFFu, wm, warp - 1);
-    }
+    const A before = __shfl_sync(0xFFFFFFFFu, w, warp > 0 ? warp - 1 : 0);
     __syncthreads();
+    return warp > 0 ? x + before : x;
 }
 
 // A search's goal: the first entry of the order at which the running count (kind 0) or mass (1: at least, 2: more than)
@@ -170,16 +187,53 @@ struct Goal {
     }
 };
 
-// Descending bitonic sort of s.list[0..n); the rest up to a power of two is padded with 0 (no key).
+// The first i in [0, n) at which `met` holds, n if none; `met` stays true once it is.  Every thread takes the same way.
+template <typename F>
+__device__ __forceinline__ uint32_t first_of(uint32_t n, F met)
+{
+    uint32_t lo = 0, hi = n;
+    while (lo < hi) {
+        const uint32_t mid = (lo + hi) >> 1;
+        if (met(mid)) hi = mid; else lo = mid + 1;
+    }
+    return lo;
+}
+
+// Descending bitonic sort of s.list[0..n).  Up to a list entry per thread the entries stay in registers: partners within a
+// warp meet by shuffles, others through the list; longer lists are sorted in shared memory.
 __device__ __forceinline__ void sort_list(Shared &s, uint32_t n)
 {
-    uint32_t size = 2;
+    const uint32_t tid = threadIdx.x;
+    uint32_t size = 32;
     while (size < n) size <<= 1;
-    for (uint32_t i = n + threadIdx.x; i < size; i += kThreads) s.list[i] = 0;
+    if (n <= (uint32_t)kThreads) {
+        u64 key = tid < n ? s.list[tid] : 0;            // 0 is no key: it goes last
+        for (uint32_t k = 2; k <= size; k <<= 1) {
+            const bool descending = (tid & k) == 0;
+            for (uint32_t j = k >> 1; j > 0; j >>= 1) {
+                u64 other;
+                if (j >= 32) {
+                    __syncthreads();
+                    s.list[tid] = key;
+                    __syncthreads();
+                    other = s.list[tid ^ j];
+                } else {
+                    other = __shfl_xor_sync(0xFFFFFFFFu, key, j);
+                }
+                const bool first = (tid & j) == 0;      // the one of the pair that comes first takes the greater, if descending
+                key = (first == descending) == (key > other) ? key : other;
+            }
+        }
+        __syncthreads();
+        s.list[tid] = key;
+        __syncthreads();
+        return;
+    }
+    for (uint32_t i = n + tid; i < size; i += kThreads) s.list[i] = 0;
     __syncthreads();
     for (uint32_t k = 2; k <= size; k <<= 1)
         for (uint32_t j = k >> 1; j > 0; j >>= 1) {
-            for (uint32_t t = threadIdx.x; t < size / 2; t += kThreads) {
+            for (uint32_t t = tid; t < size / 2; t += kThreads) {
                 const uint32_t i = 2 * t - (t & (j - 1)), l = i + j;
                 const u64 a = s.list[i], b = s.list[l];
                 const bool descending = (i & k) == 0;
@@ -189,6 +243,7 @@ __device__ __forceinline__ void sort_list(Shared &s, uint32_t n)
         }
 }
 
+constexpr int kGroup = 8;               // entries that a thread takes at a time
 constexpr int kPerThread = kList / kThreads;       // list entries of a thread, consecutive
 constexpr int kBinsPerThread = kBins / kThreads;
 
@@ -207,246 +262,290 @@ tfe_sample_kernel(const SampleParams p)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const T *row = static_cast<const T *>(p.logits) + r * p.ld;
 
-    // ---- this block's slice, its greatest key and its least logit
+    // ---- this block's slice: whole vectors, and with the first and the last block the row's ends
     const Cut cut = cut_row(row, p.V);
-    const int32_t v0 = (int32_t)(cut.n_vec * part / p.blocks), v1 = (int32_t)(cut.n_vec * (part + 1) / p.blocks);
-    const int32_t body0 = (int32_t)cut.head + v0 * E, body1 = (int32_t)cut.head + v1 * E;
-    const int32_t e0 = leader ? 0 : body0, e1 = part == p.blocks - 1 ? p.V : body1;
-    const bool resident = body1 - body0 + 2 * E <= p.slice_cap;
-    u64 best = 0;
-    float low = INFINITY;
-    auto see = [&](float z, int32_t i) {
-        if (z > -INFINITY) {            // false for NaN
-            const u64 key = entry_key(z, i);
-            best = key > best ? key : best;
-            low = fminf(low, z);
+    const int32_t v0 = (int32_t)(cut.n_vec * part / p.blocks), n_vec = (int32_t)(cut.n_vec * (part + 1) / p.blocks) - v0;
+    const int32_t body0 = (int32_t)cut.head + v0 * E;
+    const int32_t head_n = leader ? (int32_t)cut.head : 0, tail0 = (int32_t)(cut.head + cut.n_vec * E);
+    const int32_t ends = head_n + (part == p.blocks - 1 ? p.V - tail0 : 0);
+    const bool resident = n_vec * E <= p.slice_cap;
+    const uint4 *from = reinterpret_cast<const uint4 *>(row + cut.head) + v0;
+    uint4 *keep = reinterpret_cast<uint4 *>(slice);
+    auto end_index = [&](int t) { return t < head_n ? t : tail0 + t - head_n; };
+    // every entry of the slice, kGroup at a time: take(f, at), f[u * E + e] being entry at[u] + e; NaN where there is none
+    constexpr int U = kGroup / E;
+    auto sweep = [&](const uint4 *vectors, auto take) {
+        constexpr int step = U * kThreads;
+        for (int32_t v = tid; v < n_vec + tid + (ends ? step : 0); v += step) {
+            float f[kGroup];
+            int32_t at[U];
+            const bool body = v - tid < n_vec;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                uint4 raw = make_uint4(0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu);
+                if (body && v + u * kThreads < n_vec) raw = vectors[v + u * kThreads];
+                at[u] = body0 + (v + u * kThreads) * E;
+                float part_f[E];
+                Elem<T>::unpack(raw, part_f);
+#pragma unroll
+                for (int e = 0; e < E; ++e) f[u * E + e] = part_f[e];
+            }
+            if (!body) {                                // the row's ends, in a turn of their own
+                if (tid < ends) { at[0] = end_index(tid); f[0] = Elem<T>::get(row + at[0]); }
+                take(f, at);
+                break;
+            }
+            take(f, at);
         }
     };
+
+    // ---- its greatest and its least logit
+    float top = -INFINITY, low = INFINITY;
     {
-        const uint4 *body = reinterpret_cast<const uint4 *>(row + cut.head);
-        uint4 *keep = reinterpret_cast<uint4 *>(slice + E);
-        for (int32_t v = v0 + tid; v < v1; v += kThreads) {
-            const uint4 raw = load_stream(body + v);
-            if (resident) keep[v - v0] = raw;
-            float f[E];
-            Elem<T>::unpack(raw, f);
+        auto see = [&](float z) {                       // fmaxf drops NaN
+            top = fmaxf(top, z);
+            low = fminf(low, z > kMasked ? z : INFINITY);
+        };
+        constexpr int U = 4;
+        for (int32_t v = tid; v < n_vec; v += U * kThreads) {
+            uint4 raw[U];
 #pragma unroll
-            for (int e = 0; e < E; ++e) see(f[e], (int32_t)cut.head + v * E + e);
+            for (int u = 0; u < U; ++u) {
+                raw[u] = make_uint4(0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu);
+                if (v + u * kThreads < n_vec) raw[u] = load_stream(from + v + u * kThreads);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (resident && v + u * kThreads < n_vec) keep[v + u * kThreads] = raw[u];
+                float f[E];
+                Elem<T>::unpack(raw[u], f);
+#pragma unroll
+                for (int e = 0; e < E; ++e) see(f[e]);
+            }
         }
-        for (int32_t i = e0 + tid; i < body0; i += kThreads) {
-            if (resident) slice[E + i - body0] = row[i];
-            see(Elem<T>::get(row + i), i);
-        }
-        for (int32_t i = body1 + tid; i < e1; i += kThreads) {
-            if (resident) slice[E + i - body0] = row[i];
-            see(Elem<T>::get(row + i), i);
-        }
+        if (tid < ends) see(Elem<T>::get(row + end_index(tid)));
     }
-    for (int i = tid; i < kBins; i += kThreads) { s.mass[i] = 0; s.count[i] = 0; }
+    for (int i = tid; i < kBins; i += kThreads) { s.count[i] = 0; s.offset[i] = 0; }
+    if (tid < 16) s.table[tid] = exp2((double)tid / 16);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
-        const u64 other = __shfl_xor_sync(0xFFFFFFFFu, best, o);
-        best = other > best ? other : best;
+        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
         low = fminf(low, __shfl_xor_sync(0xFFFFFFFFu, low, o));
     }
-    if (lane == 0) { s.warp64[warp] = best; s.warp32[warp] = __float_as_uint(low); }
+    if (lane == 0) { s.warp_f[warp] = low; s.warp_top[warp] = top; }
     __syncthreads();
     if (warp == 0) {
-        best = lane < kThreads / 32 ? s.warp64[lane] : 0;
-        low = lane < kThreads / 32 ? __uint_as_float(s.warp32[lane]) : INFINITY;
+        top = lane < kThreads / 32 ? s.warp_top[lane] : -INFINITY;
+        low = lane < kThreads / 32 ? s.warp_f[lane] : INFINITY;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
-            const u64 other = __shfl_xor_sync(0xFFFFFFFFu, best, o);
-            best = other > best ? other : best;
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
             low = fminf(low, __shfl_xor_sync(0xFFFFFFFFu, low, o));
         }
-        if (lane == 0) { s.best = best; s.low = low; }
+        if (lane == 0) { s.top = top; s.low = low; s.first = 0x7FFFFFFF; }
     }
     cluster.sync();
-    best = 0;
+    top = -INFINITY;
     low = INFINITY;
     for (int b = 0; b < p.blocks; ++b) {
-        const u64 other = *cluster.map_shared_rank(&s.best, b);
-        best = other > best ? other : best;
+        top = fmaxf(top, *cluster.map_shared_rank(&s.top, b));
         low = fminf(low, *cluster.map_shared_rank(&s.low, b));
     }
 
     // ---- the row's rule
     const float T_ = p.temperature ? p.temperature[r] : 1.f;
-    const int32_t k = p.top_k ? p.top_k[r] : 0;
-    const float top_p = p.top_p ? p.top_p[r] : 1.f, min_p = p.min_p ? p.min_p[r] : 0.f;
-    const float u = fminf(fmaxf(p.u[r], 0.f), 1.f - 0x1p-24f);          // NaN: 0
-    if (best == 0 || !(T_ > 0.f)) {                                     // nothing to draw from, or greedy: the same in every block
-        if (leader && tid == 0) {
-            p.tokens[r] = best == 0 ? -1 : key_index(best);
-            if (p.prob) p.prob[r] = best == 0 ? 0.f : 1.f;
+    if (!(top > -INFINITY) || !(T_ > 0.f)) {            // nothing to draw from, or greedy: the same in every block
+        if (top > -INFINITY) {
+            int32_t first = 0x7FFFFFFF;
+            sweep(resident ? keep : from, [&](const float (&f)[kGroup], const int32_t (&at)[U]) {
+#pragma unroll
+                for (int e = 0; e < kGroup; ++e)
+                    if (f[e] == top) first = min(first, at[e / E] + e % E);
+            });
+            first = __reduce_min_sync(0xFFFFFFFFu, first);
+            if (lane == 0 && first != 0x7FFFFFFF) atomicMin(&s.first, first);
         }
         cluster.sync();
+        if (leader && tid == 0) {
+            int32_t first = 0x7FFFFFFF;
+            for (int b = 0; b < p.blocks; ++b) first = min(first, *cluster.map_shared_rank(&s.first, b));
+            p.tokens[r] = top > -INFINITY ? first : -1;
+            if (p.prob) p.prob[r] = top > -INFINITY ? 1.f : 0.f;
+        }
+        cluster.sync();                 // a block's shared memory lives until the first has read it
         return;
     }
+    const float min_p = p.min_p ? p.min_p[r] : 0.f;
     RowRule q;
-    q.top = key_logit(best);
-    q.inv_t = 1.0 / (double)T_;
-    q.inv_t32 = 1.f / T_;
-    q.cut = !(min_p > 0.f) ? -INFINITY : min_p >= 1.f ? (double)q.top : __dadd_rn((double)q.top, __dmul_rn((double)T_, log((double)min_p)));
-    if (isnan(q.cut)) q.cut = (double)q.top;                            // infinite maximum and infinite temperature
-    q.scale = ldexp(1.0, p.shift);
-    q.bins_per = (float)kBins / fminf(kRange, (q.top - low) * q.inv_t32);     // 0 / 0 and the like: fminf drops NaN
-    const T *src = resident ? slice + E - body0 : row;
-
-    // ---- counts and masses by bin
-    for (int32_t i = e0 + tid; i < e1; i += kThreads) {
-        const float z = Elem<T>::get(src + i);
-        if (kept(q, z)) {
-            const int b = bin_of(q, z);
-            atomicAdd(&s.count[b], 1u);
-            const u64 m = mass_of(q, z);
-            if (m) atomicAdd(&s.mass[b], m);
-        }
+    q.topf = top;
+    q.top = (double)fminf(q.topf, 3.402823466e38f);
+    q.a = 16 * 1.4426950408889634 / (double)T_;
+    q.shift = p.shift;
+    q.reach = 0.69314718f * (float)(p.shift + 2) * T_;
+    {
+        const double least = !(min_p > 0.f) ? -INFINITY
+                             : min_p >= 1.f ? (double)q.topf : __dadd_rn((double)q.topf, __dmul_rn((double)T_, log((double)min_p)));
+        q.cut = fmaxf(__double2float_ru(least), -3.402823466e38f);          // NaN (infinite maximum and temperature): the lowest
+        if (q.topf == INFINITY) q.cut = INFINITY;                           // its equals share the draw, whatever the temperature
     }
+    const float inv_t = 1.f / T_;
+    float range = fminf(kRange, (q.topf - low) * inv_t);                    // NaN: kRange
+    if (!(range >= 0.f)) range = kRange;                                    // no unmasked logit
+    const float width = range / (float)(kBins - 2);                         // of a bin, in units of -ln w
+    // the last bin is for what lies beyond the range: masked logits, weights below exp(-kRange); it is estimated to weigh nothing
+    q.bins = fminf(256.f * (float)(kBins - 2) / range * inv_t, 3.402823466e38f);  // T tiny, or all logits equal: one step is all bins
+    if (!(inv_t > 0.f)) q.bins = 0.f;                                       // T infinite: all in the first bin
+    const uint4 *src = resident ? keep : from;
+
+    // ---- counts by bin
+    sweep(src, [&](const float (&f)[kGroup], const int32_t (&)[U]) {
+#pragma unroll
+        for (int e = 0; e < kGroup; ++e) {
+            const uint32_t place = place_of(q, f[e]);
+            if (f[e] >= q.cut) {
+                atomicAdd(&s.count[place >> 8], 1u);
+                atomicAdd(&s.offset[place >> 8], place & 255u);
+            }
+        }
+    });
     cluster.sync();
-    if (p.blocks > 1) {
+    if (p.blocks > 1) {                 // every block adds up its share of the bins
         const int share = kBins / p.blocks;
         for (int i = tid; i < share; i += kThreads) {
             const int b = part * share + i;
-            uint32_t c = 0;
-            u64 m = 0;
-            for (int o = 0; o < p.blocks; ++o) { c += cluster.map_shared_rank(s.count, o)[b]; m += cluster.map_shared_rank(s.mass, o)[b]; }
-            s.count[b] = c; s.mass[b] = m;
+            uint32_t c = 0, o = 0;
+            for (int other = 0; other < p.blocks; ++other) {
+                c += cluster.map_shared_rank(s.count, other)[b];
+                o += cluster.map_shared_rank(s.offset, other)[b];
+            }
+            s.count[b] = c; s.offset[b] = o;
         }
         cluster.sync();
-        if (leader)
+        if (leader) {
+#pragma unroll 4
             for (int b = share + tid; b < kBins; b += kThreads) {
                 s.count[b] = cluster.map_shared_rank(s.count, b / share)[b];
-                s.mass[b] = cluster.map_shared_rank(s.mass, b / share)[b];
+                s.offset[b] = cluster.map_shared_rank(s.offset, b / share)[b];
             }
-        __syncthreads();
+            __syncthreads();
+        }
     }
 
-    // ---- the searches: the first block decides, every block looks through its slice
-    enum { kTopK = 0, kTopP = 1, kDraw = 2, kAll = 3 };
-    uint32_t total_n = 0, base_n = 0, list_n = 0;
-    u64 total_m = 0, base_m = 0, limit = 0;             // limit: mass of the prefix that is still in
-    int stage = kDraw, list_lo = 0, list_hi = -1;       // bins that the sorted list holds whole
-    bool k_on = false, p_on = false;
-    u64 run_m[kPerThread];                              // running mass of this thread's list entries
+    // ---- the first block decides, every block looks through its slice
+    uint32_t base_n = 0, list_n = 0;
+    u64 base_m = 0, limit = 0;                          // limit: mass of the prefix that is still in
+    int stage = kDraw;
 
+    auto share_of = [&](int st) {       // of the limit: what top-p wants reached, or the draw exceeded
+        return st == kTopP ? fmaxf(p.top_p[r], 0.f) : fminf(fmaxf(p.u[r], 0.f), 1.f - 0x1p-24f);      // NaN: 0
+    };
     auto goal_of = [&](int st) {
         Goal g;
         g.kind = st == kTopK ? 0 : st == kTopP ? 1 : 2;
-        g.count = (uint32_t)k;
-        g.mass = st == kTopP ? (double)fmaxf(top_p, 0.f) * (double)limit : (double)u * (double)limit;
+        g.count = st == kTopK ? (uint32_t)p.top_k[r] : 0;
+        g.mass = st == kTopK ? 0.0 : (double)share_of(st) * (double)limit;
         return g;
     };
-    // the first bin whose running sums meet the goal (there is one); sets base_n / base_m to the sums before it
-    auto find_bin = [&](const Goal &g) {
-#pragma unroll
-        for (int j = 0; j < kBinsPerThread; ++j) {
-            const int b = tid * kBinsPerThread + j;
-            const uint32_t c0 = b ? s.count[b - 1] : 0;
-            const u64 m0 = b ? s.mass[b - 1] : 0;
-            if (g.met(s.count[b], s.mass[b]) && (b == 0 || !g.met(c0, m0))) { s.found_at = b; s.found_count = c0; s.found_mass = m0; }
-        }
-        __syncthreads();
-        const int b = min(max(s.found_at, 0), kBins - 1);
-        base_n = s.found_count; base_m = s.found_mass;
-        __syncthreads();
-        return b;
+    auto next_stage = [&](int st) { return st == kTopK && p.top_p && p.top_p[r] < 1.f ? (int)kTopP : (int)kDraw; };
+    auto digits = [&](int shift, u64 prefix, u64 mask) {
+        if (tid == 0) { s.cmd.op = kOpDigits; s.cmd.shift = shift; s.cmd.prefix = prefix; s.cmd.mask = mask; }
     };
-    auto command = [&](int op, int lo, int hi, int shift, u64 prefix, u64 mask) {
-        if (tid == 0) { s.cmd.op = op; s.cmd.lo = lo; s.cmd.hi = hi; s.cmd.shift = shift; s.cmd.prefix = prefix; s.cmd.mask = mask; }
-    };
-    // the entry of the sorted list at which the goal is met: running mass and key
-    auto find_entry = [&](const Goal &g, u64 &mass, u64 &key) {
-#pragma unroll
-        for (int j = 0; j < kPerThread; ++j) {
-            const uint32_t i = (uint32_t)(tid * kPerThread + j);
-            if (i < list_n) {
-                const u64 own = mass_of(q, key_logit(s.list[i]));
-                if (g.met(base_n + i + 1, base_m + run_m[j]) && (i == 0 || !g.met(base_n + i, base_m + run_m[j] - own))) {
-                    s.found_mass = base_m + run_m[j];
-                    s.found_key = s.list[i];
-                }
-            }
-        }
-        __syncthreads();
-        mass = s.found_mass; key = s.found_key;
-        __syncthreads();
-    };
-    // starts the search of `stage`, and goes on through the searches that the list at hand answers
-    auto advance = [&](bool first) {
-        for (;;) {
-            if (!first) {
-                u64 mass, key;
-                find_entry(goal_of(stage), mass, key);
-                if (stage == kDraw) {
-                    if (tid == 0) {
-                        p.tokens[r] = key_index(key);
-                        const float z = key_logit(key);
-                        const double x = z == q.top ? 0.0 : ((double)z - (double)q.top) * q.inv_t;
-                        if (p.prob) p.prob[r] = (float)(exp64(x) * q.scale / (double)limit);
-                    }
-                    command(kOpDone, 0, -1, 0, 0, 0);
-                    return;
-                }
-                limit = mass;
-                stage = stage == kTopK && p_on ? kTopP : kDraw;
-            }
-            const int b = find_bin(goal_of(stage));
-            if (list_lo <= b && b <= list_hi) {
-                base_n = list_lo ? s.count[list_lo - 1] : 0;
-                base_m = list_lo ? s.mass[list_lo - 1] : 0;
-                first = false;
-                continue;
-            }
-            const uint32_t inside = s.count[b] - base_n;
-            if (inside <= (uint32_t)kList) {
-                list_lo = list_hi = b;
-                command(kOpCollect, b, b, 0, 0, 0);
-            } else {
-                list_lo = 0; list_hi = -1;
-                command(kOpDigits, b, b, 56, 0, 0);
-            }
-            return;
-        }
+    // The entry at which the goal of `stage` is met, among list entries [i0, i1) with base_n entries of mass base_m before
+    // them.  False if it is not among them.
+    auto find_entry = [&](uint32_t i0, uint32_t i1, u64 &mass, u64 &key) {
+        if (i1 <= i0) return false;
+        const Goal g = goal_of(stage);
+        const u64 off = base_m - (i0 ? s.run[i0 - 1] : 0);
+        const uint32_t i = i0 + first_of(i1 - i0, [&](uint32_t j) { return g.met(base_n + j + 1, off + s.run[i0 + j]); });
+        if (i >= i1 || (base_n > 0 && i == i0 && g.met(base_n, base_m))) return false;
+        mass = off + s.run[i];
+        key = s.list[i];
+        return true;
     };
 
     if (leader) {
-        // running sums over the bins
+        // running counts, and running masses estimated from the bins' means
         uint32_t c[kBinsPerThread], c_sum = 0;
-        u64 m[kBinsPerThread], m_sum = 0;
+        float m[kBinsPerThread], m_sum = 0.f;
+        uint4 *counts = reinterpret_cast<uint4 *>(s.count + tid * kBinsPerThread), *offsets = reinterpret_cast<uint4 *>(s.offset + tid * kBinsPerThread);
 #pragma unroll
-        for (int j = 0; j < kBinsPerThread; ++j) {
-            c_sum += s.count[tid * kBinsPerThread + j]; c[j] = c_sum;
-            m_sum += s.mass[tid * kBinsPerThread + j]; m[j] = m_sum;
-        }
-        uint32_t c_run = c_sum;
-        u64 m_run = m_sum;
-        block_scan(s, c_run, m_run);
+        for (int h = 0; h < kBinsPerThread / 4; ++h) {
+            const uint4 cv = counts[h], ov = offsets[h];
+            const uint32_t cc[4] = {cv.x, cv.y, cv.z, cv.w}, oo[4] = {ov.x, ov.y, ov.z, ov.w};
 #pragma unroll
-        for (int j = 0; j < kBinsPerThread; ++j) {
-            s.count[tid * kBinsPerThread + j] = c_run - c_sum + c[j];
-            s.mass[tid * kBinsPerThread + j] = m_run - m_sum + m[j];
-        }
-        __syncthreads();
-        total_n = s.count[kBins - 1];
-        total_m = s.mass[kBins - 1];
-        limit = total_m;
-        k_on = k > 0 && (uint32_t)k < total_n;
-        p_on = top_p < 1.f;
-        stage = k_on ? kTopK : p_on ? kTopP : kDraw;
-        // a short prefix is collected whole: one list answers every search
-        bool whole = false;
-        if (stage != kDraw) {
-            const int b = find_bin(goal_of(stage));
-            if (s.count[b] <= (uint32_t)kList) {
-                whole = true;
-                base_n = 0; base_m = 0;
-                list_lo = 0; list_hi = b;
-                command(kOpCollect, 0, b, 0, 0, 0);
+            for (int j = 0; j < 4; ++j) {
+                const float n = (float)cc[j], mean = (float)(tid * kBinsPerThread + h * 4 + j) + __fdividef((float)oo[j], 256.f * n);
+                m_sum += cc[j] && tid * kBinsPerThread + h * 4 + j < kBins - 1 ? n * __expf(-width * mean) : 0.f;
+                c_sum += cc[j];
+                c[h * 4 + j] = c_sum;
+                m[h * 4 + j] = m_sum;
             }
         }
-        if (!whole) advance(true);
+        const uint32_t c_before = block_scan(s.warp32, c_sum) - c_sum;
+        const float m_before = block_scan(s.warp_f, m_sum) - m_sum;
+#pragma unroll
+        for (int h = 0; h < kBinsPerThread / 4; ++h) {
+            counts[h] = make_uint4(c[4 * h] + c_before, c[4 * h + 1] + c_before, c[4 * h + 2] + c_before, c[4 * h + 3] + c_before);
+            float4 *e = reinterpret_cast<float4 *>(s.estimate + tid * kBinsPerThread);
+            e[h] = make_float4(m[4 * h] + m_before, m[4 * h + 1] + m_before, m[4 * h + 2] + m_before, m[4 * h + 3] + m_before);
+        }
+        __syncthreads();
+        const int32_t k = p.top_k ? p.top_k[r] : 0;
+        const bool k_on = k > 0 && (uint32_t)k < s.count[kBins - 1];
+        stage = k_on ? kTopK : next_stage(kTopK);
+        uint32_t from_i[kSearches] = {0, 0, 0}, to_i[kSearches] = {0, 0, 0}, before_n[kSearches] = {0, 0, 0};
+
+        // ---- bins [lo, hi) of every search
+        uint32_t lo[kSearches] = {0, 0, 0}, hi[kSearches] = {0, 0, 0};
+        float kept_m = s.estimate[kBins - 1], spare = 0.f;      // mass that is still in, and by how much it may be more
+        bool whole = false;
+        auto counted = [&](uint32_t b) { return b ? s.count[b - 1] : 0; };       // entries in the bins before b
+        for (int st = stage;; st = next_stage(st)) {
+            if (st == kTopK) {
+                const uint32_t b = first_of(kBins - 1, [&](uint32_t i) { return s.count[i] >= (uint32_t)k; });
+                const float m0 = b ? s.estimate[b - 1] : 0.f;
+                kept_m = m0 + (s.estimate[b] - m0) * ((float)((uint32_t)k - counted(b)) / (float)(s.count[b] - counted(b)));
+                lo[st] = b; hi[st] = b + 1;             // exact: counts
+            } else {
+                const float share = share_of(st), slack = 2e-5f * s.estimate[kBins - 1];
+                const float least = share * kept_m - slack, most = share * (kept_m + spare) + slack;
+                lo[st] = first_of(kBins - 1, [&](uint32_t i) { return s.estimate[i] > least; });
+                hi[st] = first_of(kBins - 1, [&](uint32_t i) { return s.estimate[i] > most; }) + 1;
+                kept_m = share * kept_m;
+                spare = share * spare + __expf(-width * (float)lo[st]);      // the entry that reaches the goal is part
+            }
+            if (st == stage && st != kDraw && s.count[hi[st] - 1] <= (uint32_t)kList) {
+                whole = true;                           // a short prefix is collected whole
+                for (int t = 0; t < kSearches; ++t) { hi[t] = hi[st]; lo[t] = 0; }
+                for (int t = 0; t < kSearches; ++t) { from_i[t] = 0; to_i[t] = s.count[hi[st] - 1]; before_n[t] = 0; }
+                break;
+            }
+            if (st == kDraw) break;
+        }
+        uint32_t need = whole ? to_i[0] : 0;
+        if (!whole) {                                   // where each search's entries stand in the sorted list of all
+            uint32_t end = 0;                           // bins before `end` are in the list, or above every search's
+#pragma unroll
+            for (int st = kDraw; st >= kTopK; --st)
+                if (hi[st] > lo[st]) {
+                    before_n[st] = counted(lo[st]);
+                    const uint32_t shared = lo[st] < end ? counted(min(end, hi[st])) - counted(lo[st]) : 0;
+                    const uint32_t beyond = lo[st] < end && end > hi[st] ? counted(end) - counted(hi[st]) : 0;
+                    from_i[st] = need - shared - beyond;
+                    to_i[st] = from_i[st] + counted(hi[st]) - counted(lo[st]);
+                    need = max(need, to_i[st]);
+                    end = max(end, hi[st]);
+                }
+        }
+        const bool too_many = need > (uint32_t)kList;
+        if (tid == 0) {
+            s.too_many = too_many;
+            for (int st = 0; st < kSearches; ++st) { s.from_i[st] = from_i[st]; s.to_i[st] = to_i[st]; s.before_n[st] = before_n[st]; }
+            s.cmd.op = kOpCollect;
+            s.cmd.by_bins = 1;
+            s.cmd.sums = !k_on ? 2 : whole ? 0 : 1;
+            for (int st = 0; st < kSearches; ++st) { s.cmd.lo[st] = 256 * lo[st]; s.cmd.hi[st] = too_many ? 0 : 256 * hi[st]; }
+        }
     }
 
     for (;;) {
@@ -456,48 +555,161 @@ tfe_sample_kernel(const SampleParams p)
         if (tid == 0) s.fill = 0;
         if (cmd.op == kOpDigits && tid < 256) { s.digit_count[tid] = 0; s.digit_mass[tid] = 0; }
         __syncthreads();
-        for (int32_t i = e0 + tid; i < e1; i += kThreads) {
-            const float z = Elem<T>::get(src + i);
-            if (!kept(q, z)) continue;
-            const int b = bin_of(q, z);
-            if (b < cmd.lo || b > cmd.hi) continue;
-            const u64 key = entry_key(z, i);
-            if ((key & cmd.mask) != cmd.prefix) continue;
-            if (cmd.op == kOpCollect) {
-                const uint32_t at = atomicAdd(&s.fill, 1u);
-                if (at < (uint32_t)kList) s.list[at] = key;
+        auto push = [&](u64 key) {
+            const uint32_t at = atomicAdd(&s.fill, 1u);
+            if (at < (uint32_t)kList) s.list[at] = key;
+        };
+        if (cmd.op == kOpDigits) {
+            sweep(src, [&](const float (&f)[kGroup], const int32_t (&at)[U]) {
+#pragma unroll 1
+                for (int e = 0; e < kGroup; ++e) {
+                    if (!(f[e] >= q.cut)) continue;
+                    const u64 key = entry_key(f[e], at[e / E] + e % E);
+                    if ((key & cmd.mask) != cmd.prefix) continue;
+                    const int d = (int)((key >> cmd.shift) & 255u);
+                    atomicAdd(&s.digit_count[d], 1u);
+                    atomicAdd(&s.digit_mass[d], mass_of(q, s.table, f[e]));
+                }
+            });
+        } else if (!cmd.by_bins) {
+            sweep(src, [&](const float (&f)[kGroup], const int32_t (&at)[U]) {
+#pragma unroll 1
+                for (int e = 0; e < kGroup; ++e) {
+                    const u64 key = entry_key(f[e], at[e / E] + e % E);
+                    if (f[e] >= q.cut && (key & cmd.mask) == cmd.prefix) push(key);
+                }
+            });
+        } else {
+            // all searches' places in one span; which of them an entry belongs to is asked of the few inside
+            uint32_t span_lo = 0xFFFFFFFFu, span_hi = 0;
+#pragma unroll
+            for (int st = 0; st < kSearches; ++st)
+                if (cmd.hi[st] > cmd.lo[st]) { span_lo = min(span_lo, cmd.lo[st]); span_hi = max(span_hi, cmd.hi[st]); }
+            const uint32_t span = span_hi > span_lo ? span_hi - span_lo : 0;
+            auto collect = [&](uint32_t hits, const float (&f)[kGroup], const int32_t (&at)[U]) {
+                if (!hits) return;
+#pragma unroll
+                for (int e = 0; e < kGroup; ++e)
+                    if (hits >> e & 1u) {
+                        const uint32_t place = place_of(q, f[e]);
+                        bool in = false;
+#pragma unroll
+                        for (int st = 0; st < kSearches; ++st) in = in || (place >= cmd.lo[st] && place < cmd.hi[st]);
+                        if (in) push(entry_key(f[e], at[e / E] + e % E));
+                    }
+            };
+            if (cmd.sums == 0) {
+                sweep(src, [&](const float (&f)[kGroup], const int32_t (&at)[U]) {
+                    uint32_t hits = 0;
+#pragma unroll
+                    for (int e = 0; e < kGroup; ++e) hits |= f[e] >= q.cut && place_of(q, f[e]) - span_lo < span ? 1u << e : 0u;
+                    collect(hits, f, at);
+                });
             } else {
-                const int d = (int)((key >> cmd.shift) & 255u);
-                atomicAdd(&s.digit_count[d], 1u);
-                atomicAdd(&s.digit_mass[d], mass_of(q, z));
+                // masses below the draw's bins, below top-p's, and of all entries (or those below top-k's): whole numbers of at most
+                // 2^46, a group of them exact in a double, then added up as integers
+                const uint32_t lo_all = cmd.sums == 2 ? 0xFFFFFFFFu : cmd.lo[kTopK], lo_p = cmd.lo[kTopP], lo_u = cmd.lo[kDraw];
+                u64 sum_u = 0, sum_p = 0, sum_all = 0;
+                sweep(src, [&](const float (&f)[kGroup], const int32_t (&at)[U]) {
+                    double part_u = 0.0, part_p = 0.0, part_all = 0.0;
+                    uint32_t hits = 0;
+#pragma unroll
+                    for (int e = 0; e < kGroup; ++e) {
+                        const uint32_t place = place_of(q, f[e]);
+                        const bool in = f[e] >= q.cut;
+                        const double w = weight_of<true>(q, s.table, f[e]);
+                        const bool weighs = in && !(q.topf - f[e] > q.reach);
+                        if (weighs && place < lo_all) part_all += w;
+                        if (weighs && place < lo_p) part_p += w;
+                        if (weighs && place < lo_u) part_u += w;
+                        hits |= in && place - span_lo < span ? 1u << e : 0u;
+                    }
+                    sum_all += whole_bits(part_all);
+                    sum_p += whole_bits(part_p);
+                    sum_u += whole_bits(part_u);
+                    collect(hits, f, at);
+                });
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) {
+                    sum_all += __shfl_xor_sync(0xFFFFFFFFu, sum_all, o);
+                    sum_p += __shfl_xor_sync(0xFFFFFFFFu, sum_p, o);
+                    sum_u += __shfl_xor_sync(0xFFFFFFFFu, sum_u, o);
+                }
+                if (lane == 0) { s.warp64[0][warp] = sum_all; s.warp64[1][warp] = sum_p; s.warp64[2][warp] = sum_u; }
+                __syncthreads();
+                if (tid < kSearches) {
+                    u64 total = 0;
+                    for (int w = 0; w < kThreads / 32; ++w) total += s.warp64[tid][w];
+                    s.below[tid] = total;
+                }
             }
         }
         cluster.sync();
         if (!leader) continue;
         if (cmd.op == kOpCollect) {
-            list_n = min(s.fill, (uint32_t)kList);
-            for (int b = 1; b < p.blocks; ++b) {
-                const uint32_t n = *cluster.map_shared_rank(&s.fill, b);
-                const u64 *theirs = cluster.map_shared_rank(s.list, b);
-                for (uint32_t i = tid; i < n; i += kThreads)
-                    if (list_n + i < (uint32_t)kList) s.list[list_n + i] = theirs[i];
-                list_n = min(list_n + n, (uint32_t)kList);
-            }
+            uint32_t n_of[8];
+#pragma unroll
+            for (int b = 0; b < 8; ++b) n_of[b] = b < p.blocks ? *cluster.map_shared_rank(&s.fill, b) : 0;
+            list_n = n_of[0];
+#pragma unroll
+            for (int b = 1; b < 8; ++b)
+                if (b < p.blocks) {
+                    const u64 *theirs = cluster.map_shared_rank(s.list, b);
+                    for (uint32_t i = tid; i < n_of[b] && list_n + i < (uint32_t)kList; i += kThreads) s.list[list_n + i] = theirs[i];
+                    list_n += n_of[b];
+                }
+            list_n = min(list_n, (uint32_t)kList);
             __syncthreads();
             sort_list(s, list_n);
-            uint32_t none = 0;
-            u64 sum = 0;
+            u64 sum = 0, own[kPerThread];
 #pragma unroll
             for (int j = 0; j < kPerThread; ++j) {
                 const uint32_t i = (uint32_t)(tid * kPerThread + j);
-                if (i < list_n) sum += mass_of(q, key_logit(s.list[i]));
-                run_m[j] = sum;
+                if (i < list_n) sum += mass_of(q, s.table, key_logit(s.list[i]));
+                own[j] = sum;
             }
-            u64 run = sum;
-            block_scan(s, none, run);
+            const u64 before = block_scan(s.warp64[0], sum) - sum;
 #pragma unroll
-            for (int j = 0; j < kPerThread; ++j) run_m[j] += run - sum;
-            advance(false);
+            for (int j = 0; j < kPerThread; ++j) s.run[tid * kPerThread + j] = own[j] + before;
+            __syncthreads();
+            u64 key = 0, mass = 1;
+            bool done = true;
+            if (cmd.by_bins) {
+                u64 below[kSearches] = {0, 0, 0};
+                if (cmd.sums)
+                    for (int b = 0; b < p.blocks; ++b)
+#pragma unroll
+                        for (int i = 0; i < kSearches; ++i) below[i] += cluster.map_shared_rank(s.below, b)[i];
+                if (stage != kTopK) limit = below[0];
+                done = !s.too_many;
+                while (done) {
+                    base_n = s.before_n[stage];
+                    base_m = stage == kTopK ? below[0] : stage == kTopP ? below[1] : below[2];
+                    done = find_entry(s.from_i[stage], min(s.to_i[stage], list_n), mass, key);
+                    if (!done || stage == kDraw) break;
+                    limit = mass;
+                    stage = next_stage(stage);
+                }
+            } else {
+                // a selection by digits ends on the goal's entry
+                if (!find_entry(0, list_n, mass, key)) { key = list_n ? s.list[0] : entry_key(q.topf, 0); mass = limit; }
+                if (stage != kDraw) {                   // the next search, by digits again
+                    limit = mass;
+                    stage = next_stage(stage);
+                    done = false;
+                }
+            }
+            if (done) {
+                if (tid == 0) {
+                    p.tokens[r] = key_index(key);
+                    const float z = key_logit(key);
+                    if (p.prob) p.prob[r] = in_reach(q, z) ? (float)(weight_of<false>(q, s.table, z) / (double)limit) : 0.f;
+                    s.cmd.op = kOpDone;
+                }
+            } else {
+                base_n = 0; base_m = 0;
+                digits(56, 0, 0);
+            }
         } else {
             // digits in descending order: thread t holds digit 255 - t
             const int d = 255 - tid;
@@ -505,11 +717,13 @@ tfe_sample_kernel(const SampleParams p)
             u64 m = 0;
             if (tid < 256)
                 for (int b = 0; b < p.blocks; ++b) { c += cluster.map_shared_rank(s.digit_count, b)[d]; m += cluster.map_shared_rank(s.digit_mass, b)[d]; }
-            uint32_t c_run = c;
-            u64 m_run = m;
-            block_scan(s, c_run, m_run);
+            const uint32_t c_run = block_scan(s.warp32, c);
+            const u64 m_run = block_scan(s.warp64[0], m);
             const Goal g = goal_of(stage);
-            if (tid < 256 && c && g.met(base_n + c_run, base_m + m_run) && !(c_run > c && g.met(base_n + c_run - c, base_m + m_run - m))) {
+            if (tid == 0) { s.found_at = 0; s.found_count = 0; s.found_key = 0; s.found_mass = 0; }
+            __syncthreads();
+            if (tid < 256 && c && g.met(base_n + c_run, base_m + m_run) &&
+                (base_n + c_run - c == 0 || !g.met(base_n + c_run - c, base_m + m_run - m))) {
                 s.found_at = d; s.found_count = c; s.found_key = (u64)(c_run - c); s.found_mass = m_run - m;
             }
             __syncthreads();
@@ -518,8 +732,11 @@ tfe_sample_kernel(const SampleParams p)
             base_n += (uint32_t)s.found_key;
             base_m += s.found_mass;
             __syncthreads();
-            if (inside <= (uint32_t)kList || cmd.shift == 0) command(kOpCollect, cmd.lo, cmd.hi, 0, prefix, mask);
-            else command(kOpDigits, cmd.lo, cmd.hi, cmd.shift - 8, prefix, mask);
+            if (inside <= (uint32_t)kList || cmd.shift == 0) {
+                if (tid == 0) { s.cmd.op = kOpCollect; s.cmd.by_bins = 0; s.cmd.prefix = prefix; s.cmd.mask = mask; }
+            } else {
+                digits(cmd.shift - 8, prefix, mask);
+            }
         }
     }
     cluster.sync();                     // the first block's command is read by now
@@ -542,18 +759,20 @@ extern "C" tfe_status tfe_sample_tokens(const void *logits, int32_t dtype, int32
     p.logits = logits; p.ld = ld; p.B = B; p.V = V;
     p.temperature = params->temperature; p.top_k = params->top_k; p.top_p = params->top_p; p.min_p = params->min_p; p.u = u;
     p.tokens = tokens; p.prob = prob;
-    // up to 8 blocks a row, none with less than 2,048 logits
+    int dev = 0, sms = 0;
+    if (tfe_status st = tfe_note_cuda(cudaGetDevice(&dev), "cudaGetDevice")) return st;
+    if (tfe_status st = tfe_note_cuda(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev), "cudaDeviceGetAttribute")) return st;
+    // up to 8 blocks a row while two blocks per SM have room for all rows, none with less than 2,048 logits
     p.blocks = 1;
-    while (p.blocks < 8 && V / (2 * p.blocks) >= 2048) p.blocks *= 2;
+    while (p.blocks < 8 && V / (2 * p.blocks) >= 2048 && (int64_t)B * 2 * p.blocks <= 2 * sms) p.blocks *= 2;
     // masses sum to less than 2^63
     int bits = 0;
     while ((1ll << bits) < V) ++bits;
     p.shift = std::min(46, 62 - bits);
-    // the slice and the parts of a vector at both its ends; two blocks per SM where that is possible
-    const int per_vec = 16 / es;
-    const int64_t want = ((int64_t)V / per_vec / p.blocks + 1) * per_vec + 2 * per_vec;
-    const int64_t room = (226 * 1024 - (int64_t)sizeof(Shared)) / es;
-    p.slice_cap = want <= room ? (int32_t)want : 0;
+    // a slice stays in shared memory where that leaves every SM the blocks it would otherwise have
+    const int64_t want = ((int64_t)V * es / 16 / p.blocks + 1) * (16 / es);
+    const int64_t room = ((int64_t)B * p.blocks <= sms ? 226 : 112) * 1024 - (int64_t)sizeof(Shared);
+    p.slice_cap = want * es <= room ? (int32_t)want : 0;
     const size_t smem = sizeof(Shared) + (size_t)p.slice_cap * es;
     auto kernel = dtype == TFE_DTYPE_BF16 ? tfe_sample_kernel<__nv_bfloat16> : tfe_sample_kernel<float>;
     if (tfe_status st = tfe_note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024), "sampling attribute")) return st;

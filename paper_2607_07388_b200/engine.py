@@ -253,39 +253,53 @@ def _issue(device: torch.device, stream):
     return _HERE if stream is None and device.index == torch.cuda.current_device() else _elsewhere(device, stream)
 
 
+# The checks below build their messages only when they fail: a decode step makes these calls by the thousand.
+
+
 def _row_matrix(t: torch.Tensor, what: str):
-    """(rows, columns, elements between rows) of a 2-D CUDA matrix whose rows are contiguous."""
-    _require(t.is_cuda and t.dim() == 2 and t.dtype in _ROW_DTYPES, f"{what}: a 2-D bf16 or fp32 CUDA tensor is needed")
+    """(rows, columns, elements between rows, the library's type number) of a 2-D CUDA matrix with contiguous rows."""
+    kind = _ROW_DTYPES.get(t.dtype)
+    if kind is None or not t.is_cuda or t.dim() != 2:
+        raise ValueError(f"{what}: a 2-D bf16 or fp32 CUDA tensor is needed")
     n, v = t.shape
-    _require(v >= 1 and (t.stride(1) == 1 or v == 1), f"{what}: rows must be contiguous")
-    ld = t.stride(0) if n > 1 else v
-    _require(ld >= v, f"{what}: rows must not overlap")
-    return n, v, ld
+    ld, step = t.stride()
+    if v < 1 or (step != 1 and v != 1):
+        raise ValueError(f"{what}: rows must be contiguous and not empty")
+    if n <= 1:
+        ld = v
+    elif ld < v:
+        raise ValueError(f"{what}: rows must not overlap")
+    return n, v, ld, kind
 
 
-def _vector(t: torch.Tensor, shape, dtype, device, what: str):
-    _require(t.shape == shape and t.dtype == dtype and t.device == device and t.is_contiguous(),
-             f"{what}: a contiguous {dtype} tensor of shape {tuple(shape)} on {device} is needed")
+def _vector(t: torch.Tensor, shape, dtype, device, what: str) -> int:
+    """The address of a contiguous tensor of this shape, type and device."""
+    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous {dtype} tensor of shape {tuple(shape)} on {device} is needed")
+    return t.data_ptr()
 
 
 def quantize_fp8(x: torch.Tensor, block_rows: int = 1, *, stream=None):
     """(q float8_e4m3fn [R, C], scale float32): `x` [R, C] in 8 bits with a scale for every `block_rows` x 128 values -- 1
     for activations, 128 for weights (see tfe_quantize_fp8)."""
-    r, c, ld = _row_matrix(x, "x")
+    r, c, ld, kind = _row_matrix(x, "x")
     _require(block_rows in (1, 128), "block_rows: 1 or 128")
     with _issue(x.device, stream):
         q = torch.empty((r, c), dtype=torch.float8_e4m3fn, device=x.device)
         scale = torch.empty((-(-r // block_rows), -(-c // 128)), dtype=torch.float32, device=x.device)
-        tfe.tfe_quantize_fp8(x.data_ptr(), _ROW_DTYPES[x.dtype], r, c, ld, block_rows, q.data_ptr(), scale, stream)
+        tfe.tfe_quantize_fp8(x.data_ptr(), kind, r, c, ld, block_rows, q.data_ptr(), scale.data_ptr(), stream)
     return q, scale
 
 
 def _fp8_matrix(t: torch.Tensor, what: str):
-    _require(t.is_cuda and t.dim() == 2 and t.dtype == torch.float8_e4m3fn, f"{what}: a 2-D float8_e4m3fn CUDA tensor is needed")
+    if not t.is_cuda or t.dim() != 2 or t.dtype != torch.float8_e4m3fn:
+        raise ValueError(f"{what}: a 2-D float8_e4m3fn CUDA tensor is needed")
     n, k = t.shape
-    ld = t.stride(0) if n > 1 else -(-k // 16) * 16
-    _require(k >= 1 and (t.stride(1) == 1 or k == 1) and ld >= k and ld % 16 == 0 and t.data_ptr() % 16 == 0,
-             f"{what}: contiguous rows that start on 16-byte boundaries are needed")
+    ld, step = t.stride()
+    if n <= 1:
+        ld = -(-k // 16) * 16
+    if k < 1 or (step != 1 and k != 1) or ld < k or ld % 16 != 0 or t.data_ptr() % 16 != 0:
+        raise ValueError(f"{what}: contiguous rows that start on 16-byte boundaries are needed")
     return n, k, ld
 
 
@@ -298,16 +312,15 @@ def matmul_fp8(a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale:
     dev = a.device
     _require(n >= 1 and kw == k and w.device == dev, "w: the width and device of a are needed")
     kb = -(-k // 128)
-    _vector(a_scale, (m, kb), torch.float32, dev, "a_scale")
-    _vector(w_scale, (-(-n // 128), kb), torch.float32, dev, "w_scale")
+    a_s = _vector(a_scale, (m, kb), torch.float32, dev, "a_scale")
+    w_s = _vector(w_scale, (-(-n // 128), kb), torch.float32, dev, "w_scale")
     with _issue(dev, stream):
         if out is None:
             _require(out_dtype in _ROW_DTYPES, "out_dtype: bfloat16 or float32")
             out = torch.empty((m, n), dtype=out_dtype, device=dev)
-        om, on, ldo = _row_matrix(out, "out")
-        _require((om, on) == (m, n) and out.device == dev, "out: [M, N] on the operands' device is needed")
-        tfe.tfe_matmul_fp8(a.data_ptr(), lda, a_scale, m, w.data_ptr(), ldw, w_scale, n, k, out.data_ptr(),
-                           _ROW_DTYPES[out.dtype], ldo, stream)
+        om, on, ldo, kind = _row_matrix(out, "out")
+        _require(om == m and on == n and out.device == dev, "out: [M, N] on the operands' device is needed")
+        tfe.tfe_matmul_fp8(a.data_ptr(), lda, a_s, m, w.data_ptr(), ldw, w_s, n, k, out.data_ptr(), kind, ldo, stream)
     return out
 
 
@@ -340,40 +353,41 @@ def sample_tokens(logits: torch.Tensor, u: torch.Tensor, *, temperature: torch.T
     """(token int32 [B], prob float32 [B]): one draw per row of `logits` [B, V] by the numbers `u` [B] in [0, 1), after
     temperature, min-p, top-k and top-p (see tfe_sample_tokens).  The settings are device tensors of B values
     (top_k int32, the others fp32) or None."""
-    b, v, ld = _row_matrix(logits, "logits")
+    b, v, ld, kind = _row_matrix(logits, "logits")
     dev = logits.device
-    _vector(u, (b,), torch.float32, dev, "u")
-    for t, dtype, what in ((temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"),
-                           (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p")):
-        if t is not None:
-            _vector(t, (b,), dtype, dev, what)
+    shape, f32 = (b,), torch.float32
+    ua = _vector(u, shape, f32, dev, "u")
+    t = None if temperature is None else _vector(temperature, shape, f32, dev, "temperature")
+    k = None if top_k is None else _vector(top_k, shape, torch.int32, dev, "top_k")
+    p = None if top_p is None else _vector(top_p, shape, f32, dev, "top_p")
+    m = None if min_p is None else _vector(min_p, shape, f32, dev, "min_p")
     with _issue(dev, stream):
         token = torch.empty(b, dtype=torch.int32, device=dev)
-        prob = torch.empty(b, dtype=torch.float32, device=dev)
-        tfe.tfe_sample_tokens(logits.data_ptr(), _ROW_DTYPES[logits.dtype], b, v, ld, u, token, prob,
-                              temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p, stream=stream)
+        prob = torch.empty(b, dtype=f32, device=dev)
+        tfe.tfe_sample_tokens(logits.data_ptr(), kind, b, v, ld, ua, token.data_ptr(), prob.data_ptr(),
+                              temperature=t, top_k=k, top_p=p, min_p=m, stream=stream)
     return token, prob
 
 
 def _teacher(logits, teacher_ids, teacher_logits):
-    n, v, ld = _row_matrix(logits, "logits")
+    n, v, ld, kind = _row_matrix(logits, "logits")
     _require(teacher_ids.dim() == 2, "teacher_ids: [rows, K] is needed")
     shape = (n, teacher_ids.shape[1])
-    _vector(teacher_ids, shape, torch.int32, logits.device, "teacher_ids")
-    _vector(teacher_logits, shape, torch.float32, logits.device, "teacher_logits")
-    return n, v, ld, shape[1]
+    ids = _vector(teacher_ids, shape, torch.int32, logits.device, "teacher_ids")
+    t = _vector(teacher_logits, shape, torch.float32, logits.device, "teacher_logits")
+    return (logits.data_ptr(), kind, n, v, ld, ids, t, shape[1])
 
 
 def distill_forward(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_logits: torch.Tensor, tau: float = 1.0, *,
                     stream=None):
     """(loss, lse), fp32 [N] each: the divergence from the teacher's top logits to the rows of `logits` [N, V] (see
     tfe_distill_forward), and the log-sum-exp of logits / tau that the gradient needs."""
-    n, v, ld, k = _teacher(logits, teacher_ids, teacher_logits)
-    with _issue(logits.device, stream):
-        loss = torch.empty(n, dtype=torch.float32, device=logits.device)
-        lse = torch.empty(n, dtype=torch.float32, device=logits.device)
-        tfe.tfe_distill_forward(logits.data_ptr(), _ROW_DTYPES[logits.dtype], n, v, ld, teacher_ids, teacher_logits, k,
-                                tau, loss, lse, stream)
+    rows = _teacher(logits, teacher_ids, teacher_logits)
+    dev, n = logits.device, rows[2]
+    with _issue(dev, stream):
+        loss = torch.empty(n, dtype=torch.float32, device=dev)
+        lse = torch.empty(n, dtype=torch.float32, device=dev)
+        tfe.tfe_distill_forward(*rows, tau, loss.data_ptr(), lse.data_ptr(), stream)
     return loss, lse
 
 
@@ -382,17 +396,17 @@ def distill_backward(grad_loss: torch.Tensor, logits: torch.Tensor, teacher_ids:
                      out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """The gradient [N, V] of sum(grad_loss * loss) with respect to the logits.  `out`: where it goes, of the logits'
     shape and type; `out=logits` overwrites them."""
-    n, v, ld, k = _teacher(logits, teacher_ids, teacher_logits)
-    _vector(grad_loss, (n,), torch.float32, logits.device, "grad_loss")
-    _vector(lse, (n,), torch.float32, logits.device, "lse")
-    with _issue(logits.device, stream):
+    rows = _teacher(logits, teacher_ids, teacher_logits)
+    dev, n, v = logits.device, rows[2], rows[3]
+    g = _vector(grad_loss, (n,), torch.float32, dev, "grad_loss")
+    norm = _vector(lse, (n,), torch.float32, dev, "lse")
+    with _issue(dev, stream):
         if out is None:
-            out = torch.empty((n, v), dtype=logits.dtype, device=logits.device)
-        on, ov, ld_out = _row_matrix(out, "out")
-        _require((on, ov) == (n, v) and out.dtype == logits.dtype and out.device == logits.device,
+            out = torch.empty((n, v), dtype=logits.dtype, device=dev)
+        on, ov, ld_out, kind = _row_matrix(out, "out")
+        _require(on == n and ov == v and kind == rows[1] and out.device == dev,
                  "out: the logits' shape, type and device are needed")
-        tfe.tfe_distill_backward(logits.data_ptr(), _ROW_DTYPES[logits.dtype], n, v, ld, teacher_ids, teacher_logits, k,
-                                 tau, lse, grad_loss, out.data_ptr(), ld_out, stream)
+        tfe.tfe_distill_backward(*rows, tau, norm, g, out.data_ptr(), ld_out, stream)
     return out
 
 
