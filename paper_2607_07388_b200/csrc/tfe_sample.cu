@@ -69,20 +69,19 @@ struct RowRule {
     double top, a;                      // a = 16 log2(e) / T
     float topf, cut;                    // entries with z < cut are out; cut is finite or +inf, so -inf and NaN always are
     float bins;                         // 256 bins per unit of top - z
-    float reach;                        // beyond this difference nothing of a weight is left
-    int shift;
+    float floor;                        // at and below this logit nothing of a weight is left: 2^shift w rounds to 0
 };
 
 constexpr double kWhole = 4503599627370496.0;           // 2^52: what is added to it is rounded to a whole number
 
-// w 2^shift rounded to a whole number (kRound) or not, with w = exp((z - top) / T) in 64 bits: y = 16 log2 w = n + f, n
-// whole, |f| <= 1/2, so w = 2^(n / 16) 2^(f / 16); the first factor from a table of 2^(j / 16) (16 entries, so that a warp's
-// reads never meet in a bank) and an exponent, the second by Taylor's series to the sixth power (|f| ln 2 / 16 is at most
-// 0.0217; the first term left out is below 5e-16).  The maximum weighs 2^shift exactly.  For logits within reach only.
-template <bool kRound>
-__device__ __forceinline__ double weight_of(const RowRule &q, const double *table, float z)
+// w 2^shift + plus, with w = exp((z - top) / T) in 64 bits: y = 16 log2 w = n + f, n whole, |f| <= 1/2, so
+// w = 2^(n / 16) 2^(f / 16); the first factor from a table of 2^(shift + j / 16) (16 entries, so that a warp's reads never
+// meet in a bank) with n's multiples of 16 added to its exponent, the second by Taylor's series to the sixth power (|f| ln 2
+// / 16 is at most 0.0217; the first term left out is below 5e-16).  The maximum weighs 2^shift exactly.  Finite for any z.
+// plus = 2^52 rounds to a whole number, which stands in the result's low 52 bits.
+__device__ __forceinline__ double weight_of(const RowRule &q, const double *table, float z, double plus)
 {
-    const double y = ((double)fminf(z, 3.402823466e38f) - q.top) * q.a;
+    const double y = ((double)fminf(fmaxf(z, q.floor), 3.402823466e38f) - q.top) * q.a;
     constexpr double magic = 1.5 * kWhole;              // the low bits hold the whole number, negative ones too
     const double shifted = y + magic;
     const int n = __double2loint(shifted);
@@ -95,19 +94,11 @@ __device__ __forceinline__ double weight_of(const RowRule &q, const double *tabl
     p = fma(p, f, c * c / 2);
     p = fma(p, f, c);
     p = fma(p, f, 1.0);
-    p *= table[n & 15];
-    const double e = __hiloint2double((int)((uint32_t)(n & ~15) << 16) + ((1023 + q.shift) << 20), 0);
-    return kRound ? fma(p, e, kWhole) - kWhole : p * e;
+    const double t = table[n & 15];
+    return fma(p, __hiloint2double(__double2hiint(t) + (int)((uint32_t)(n & ~15) << 16), __double2loint(t)), plus);
 }
-__device__ __forceinline__ u64 whole_bits(double x)     // of a whole number below 2^52
-{
-    return (u64)__double_as_longlong(x + kWhole) & 0xFFFFFFFFFFFFFull;
-}
-__device__ __forceinline__ bool in_reach(const RowRule &q, float z) { return !(q.topf - z > q.reach); }
-__device__ __forceinline__ u64 mass_of(const RowRule &q, const double *table, float z)
-{
-    return in_reach(q, z) ? whole_bits(weight_of<true>(q, table, z)) : 0;
-}
+__device__ __forceinline__ u64 whole_of(double x) { return (u64)__double_as_longlong(x) & 0xFFFFFFFFFFFFFull; }    // after plus = kWhole
+__device__ __forceinline__ u64 mass_of(const RowRule &q, const double *table, float z) { return whole_of(weight_of(q, table, z, kWhole)); }
 
 // Place of a kept logit: 256 times its distance from the maximum in bins, rounded; the bin is place >> 8.  Not decreasing
 // as z falls.  What lies beyond the last bin is in it.
@@ -131,7 +122,7 @@ struct alignas(16) Shared {
     u64 list[kList];
     u64 run[kList];                     // in the first block: running masses of the sorted list
     u64 digit_mass[256];
-    double table[16];                   // 2^(j / 16)
+    double table[16];                   // 2^(shift + j / 16)
     u64 warp64[kSearches][kThreads / 32];
     u64 below[kSearches];               // masses below the top-p and the draw's bins, and of all entries
     u64 found_mass, found_key;
@@ -243,7 +234,32 @@ __device__ __forceinline__ void sort_list(Shared &s, uint32_t n)
         }
 }
 
-constexpr int kGroup = 8;               // entries that a thread takes at a time
+// The greatest and the least unmasked value of a vector; NaN counts for neither.
+template <typename T>
+__device__ __forceinline__ void see_vector(const uint4 &raw, float &top, float &low)
+{
+    if constexpr (sizeof(T) == 2) {                     // in pairs
+        const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+        const __nv_bfloat162 masked = __float2bfloat162_rn(kMasked);
+        __nv_bfloat162 hi, lo;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 x = *reinterpret_cast<const __nv_bfloat162 *>(&w[i]);
+            const uint32_t open = __hgt2_mask(x, masked), y = (w[i] & open) | (0x7F807F80u & ~open);      // masked ones: +inf
+            const __nv_bfloat162 z = *reinterpret_cast<const __nv_bfloat162 *>(&y);
+            hi = i ? __hmax2(hi, x) : x;
+            lo = i ? __hmin2(lo, z) : z;
+        }
+        top = fmaxf(top, fmaxf(__low2float(hi), __high2float(hi)));
+        low = fminf(low, fminf(__low2float(lo), __high2float(lo)));
+    } else {
+        float f[4];
+        Elem<float>::unpack(raw, f);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { top = fmaxf(top, f[e]); low = fminf(low, f[e] > kMasked ? f[e] : INFINITY); }
+    }
+}
+
 constexpr int kPerThread = kList / kThreads;       // list entries of a thread, consecutive
 constexpr int kBinsPerThread = kBins / kThreads;
 
@@ -272,30 +288,35 @@ tfe_sample_kernel(const SampleParams p)
     const uint4 *from = reinterpret_cast<const uint4 *>(row + cut.head) + v0;
     uint4 *keep = reinterpret_cast<uint4 *>(slice);
     auto end_index = [&](int t) { return t < head_n ? t : tail0 + t - head_n; };
-    // every entry of the slice, kGroup at a time: take(f, at), f[u * E + e] being entry at[u] + e; NaN where there is none
-    constexpr int U = kGroup / E;
+    // every entry of the slice, four at a time: take(f, i), f[e] being entry i + e; NaN where there is none
     auto sweep = [&](const uint4 *vectors, auto take) {
-        constexpr int step = U * kThreads;
-        for (int32_t v = tid; v < n_vec + tid + (ends ? step : 0); v += step) {
-            float f[kGroup];
-            int32_t at[U];
-            const bool body = v - tid < n_vec;
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                uint4 raw = make_uint4(0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu);
-                if (body && v + u * kThreads < n_vec) raw = vectors[v + u * kThreads];
-                at[u] = body0 + (v + u * kThreads) * E;
-                float part_f[E];
-                Elem<T>::unpack(raw, part_f);
-#pragma unroll
-                for (int e = 0; e < E; ++e) f[u * E + e] = part_f[e];
+        auto take_vector = [&](const uint4 &raw, int32_t i) {
+            if constexpr (E == 4) {
+                float f[4];
+                Elem<T>::unpack(raw, f);
+                take(f, i);
+            } else {
+#pragma unroll 1
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t a = h ? raw.z : raw.x, b = h ? raw.w : raw.y;
+                    const float f[4] = {__uint_as_float(a << 16), __uint_as_float(a & 0xFFFF0000u), __uint_as_float(b << 16), __uint_as_float(b & 0xFFFF0000u)};
+                    take(f, i + 4 * h);
+                }
             }
-            if (!body) {                                // the row's ends, in a turn of their own
-                if (tid < ends) { at[0] = end_index(tid); f[0] = Elem<T>::get(row + at[0]); }
-                take(f, at);
-                break;
-            }
-            take(f, at);
+        };
+        uint4 next = make_uint4(0, 0, 0, 0);            // one load ahead
+        if (tid < n_vec) next = vectors[tid];
+#pragma unroll 1
+        for (int32_t v = tid; v < n_vec; v += kThreads) {
+            const uint4 raw = next;
+            if (v + kThreads < n_vec) next = vectors[v + kThreads];
+            take_vector(raw, body0 + v * E);
+        }
+        if (ends && tid < 32) {                         // the row's ends, fewer than 2 E: a turn of their own
+            const int32_t i = tid < ends ? end_index(tid) : 0;
+            const float f[4] = {tid < ends ? Elem<T>::get(row + i) : __uint_as_float(0x7FFFFFFFu), __uint_as_float(0x7FFFFFFFu),
+                                __uint_as_float(0x7FFFFFFFu), __uint_as_float(0x7FFFFFFFu)};
+            take(f, i);
         }
     };
 
@@ -317,16 +338,13 @@ tfe_sample_kernel(const SampleParams p)
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 if (resident && v + u * kThreads < n_vec) keep[v + u * kThreads] = raw[u];
-                float f[E];
-                Elem<T>::unpack(raw[u], f);
-#pragma unroll
-                for (int e = 0; e < E; ++e) see(f[e]);
+                see_vector<T>(raw[u], top, low);
             }
         }
         if (tid < ends) see(Elem<T>::get(row + end_index(tid)));
     }
     for (int i = tid; i < kBins; i += kThreads) { s.count[i] = 0; s.offset[i] = 0; }
-    if (tid < 16) s.table[tid] = exp2((double)tid / 16);
+    if (tid < 16) s.table[tid] = exp2((double)tid / 16 + p.shift);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
@@ -357,10 +375,10 @@ tfe_sample_kernel(const SampleParams p)
     if (!(top > -INFINITY) || !(T_ > 0.f)) {            // nothing to draw from, or greedy: the same in every block
         if (top > -INFINITY) {
             int32_t first = 0x7FFFFFFF;
-            sweep(resident ? keep : from, [&](const float (&f)[kGroup], const int32_t (&at)[U]) {
+            sweep(resident ? keep : from, [&](const float (&f)[4], int32_t i) {
 #pragma unroll
-                for (int e = 0; e < kGroup; ++e)
-                    if (f[e] == top) first = min(first, at[e / E] + e % E);
+                for (int e = 0; e < 4; ++e)
+                    if (f[e] == top) first = min(first, i + e);
             });
             first = __reduce_min_sync(0xFFFFFFFFu, first);
             if (lane == 0 && first != 0x7FFFFFFF) atomicMin(&s.first, first);
@@ -380,13 +398,15 @@ tfe_sample_kernel(const SampleParams p)
     q.topf = top;
     q.top = (double)fminf(q.topf, 3.402823466e38f);
     q.a = 16 * 1.4426950408889634 / (double)T_;
-    q.shift = p.shift;
-    q.reach = 0.69314718f * (float)(p.shift + 2) * T_;
     {
         const double least = !(min_p > 0.f) ? -INFINITY
                              : min_p >= 1.f ? (double)q.topf : __dadd_rn((double)q.topf, __dmul_rn((double)T_, log((double)min_p)));
         q.cut = fmaxf(__double2float_ru(least), -3.402823466e38f);          // NaN (infinite maximum and temperature): the lowest
         if (q.topf == INFINITY) q.cut = INFINITY;                           // its equals share the draw, whatever the temperature
+        // -ln w = ln 2 (shift + 2): a quarter of the unit.  Where that is less than a step of the maximum, nothing else weighs.
+        const double reach = 0.6931471805599453 * (double)(p.shift + 2) * (double)T_;
+        q.floor = fmaxf(__double2float_rd((double)q.topf - reach), -3.402823466e38f);
+        if (!(q.floor < q.topf)) { q.cut = q.topf; q.floor = q.topf; }
     }
     const float inv_t = 1.f / T_;
     float range = fminf(kRange, (q.topf - low) * inv_t);                    // NaN: kRange
@@ -398,9 +418,9 @@ tfe_sample_kernel(const SampleParams p)
     const uint4 *src = resident ? keep : from;
 
     // ---- counts by bin
-    sweep(src, [&](const float (&f)[kGroup], const int32_t (&)[U]) {
+    sweep(src, [&](const float (&f)[4], int32_t) {
 #pragma unroll
-        for (int e = 0; e < kGroup; ++e) {
+        for (int e = 0; e < 4; ++e) {
             const uint32_t place = place_of(q, f[e]);
             if (f[e] >= q.cut) {
                 atomicAdd(&s.count[place >> 8], 1u);
@@ -560,11 +580,11 @@ tfe_sample_kernel(const SampleParams p)
             if (at < (uint32_t)kList) s.list[at] = key;
         };
         if (cmd.op == kOpDigits) {
-            sweep(src, [&](const float (&f)[kGroup], const int32_t (&at)[U]) {
+            sweep(src, [&](const float (&f)[4], int32_t at) {
 #pragma unroll 1
-                for (int e = 0; e < kGroup; ++e) {
+                for (int e = 0; e < 4; ++e) {
                     if (!(f[e] >= q.cut)) continue;
-                    const u64 key = entry_key(f[e], at[e / E] + e % E);
+                    const u64 key = entry_key(f[e], at + e);
                     if ((key & cmd.mask) != cmd.prefix) continue;
                     const int d = (int)((key >> cmd.shift) & 255u);
                     atomicAdd(&s.digit_count[d], 1u);
@@ -572,10 +592,10 @@ tfe_sample_kernel(const SampleParams p)
                 }
             });
         } else if (!cmd.by_bins) {
-            sweep(src, [&](const float (&f)[kGroup], const int32_t (&at)[U]) {
+            sweep(src, [&](const float (&f)[4], int32_t at) {
 #pragma unroll 1
-                for (int e = 0; e < kGroup; ++e) {
-                    const u64 key = entry_key(f[e], at[e / E] + e % E);
+                for (int e = 0; e < 4; ++e) {
+                    const u64 key = entry_key(f[e], at + e);
                     if (f[e] >= q.cut && (key & cmd.mask) == cmd.prefix) push(key);
                 }
             });
@@ -586,48 +606,44 @@ tfe_sample_kernel(const SampleParams p)
             for (int st = 0; st < kSearches; ++st)
                 if (cmd.hi[st] > cmd.lo[st]) { span_lo = min(span_lo, cmd.lo[st]); span_hi = max(span_hi, cmd.hi[st]); }
             const uint32_t span = span_hi > span_lo ? span_hi - span_lo : 0;
-            auto collect = [&](uint32_t hits, const float (&f)[kGroup], const int32_t (&at)[U]) {
-                if (!hits) return;
+            auto collect = [&](const float (&f)[4], int32_t at) {
 #pragma unroll
-                for (int e = 0; e < kGroup; ++e)
-                    if (hits >> e & 1u) {
-                        const uint32_t place = place_of(q, f[e]);
-                        bool in = false;
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t place = place_of(q, f[e]);
+                    bool in = false;
 #pragma unroll
-                        for (int st = 0; st < kSearches; ++st) in = in || (place >= cmd.lo[st] && place < cmd.hi[st]);
-                        if (in) push(entry_key(f[e], at[e / E] + e % E));
-                    }
+                    for (int st = 0; st < kSearches; ++st) in = in || (place >= cmd.lo[st] && place < cmd.hi[st]);
+                    if (in && f[e] >= q.cut) push(entry_key(f[e], at + e));
+                }
             };
             if (cmd.sums == 0) {
-                sweep(src, [&](const float (&f)[kGroup], const int32_t (&at)[U]) {
-                    uint32_t hits = 0;
+                sweep(src, [&](const float (&f)[4], int32_t at) {
+                    bool any = false;
 #pragma unroll
-                    for (int e = 0; e < kGroup; ++e) hits |= f[e] >= q.cut && place_of(q, f[e]) - span_lo < span ? 1u << e : 0u;
-                    collect(hits, f, at);
+                    for (int e = 0; e < 4; ++e) any = any || place_of(q, f[e]) - span_lo < span;
+                    if (any) collect(f, at);
                 });
             } else {
                 // masses below the draw's bins, below top-p's, and of all entries (or those below top-k's): whole numbers of at most
-                // 2^46, a group of them exact in a double, then added up as integers
+                // 2^46, four of them exact in a double, then added up as integers
                 const uint32_t lo_all = cmd.sums == 2 ? 0xFFFFFFFFu : cmd.lo[kTopK], lo_p = cmd.lo[kTopP], lo_u = cmd.lo[kDraw];
                 u64 sum_u = 0, sum_p = 0, sum_all = 0;
-                sweep(src, [&](const float (&f)[kGroup], const int32_t (&at)[U]) {
-                    double part_u = 0.0, part_p = 0.0, part_all = 0.0;
-                    uint32_t hits = 0;
+                sweep(src, [&](const float (&f)[4], int32_t at) {
+                    double part_u = kWhole, part_p = kWhole, part_all = kWhole;
+                    bool any = false;
 #pragma unroll
-                    for (int e = 0; e < kGroup; ++e) {
-                        const uint32_t place = place_of(q, f[e]);
-                        const bool in = f[e] >= q.cut;
-                        const double w = weight_of<true>(q, s.table, f[e]);
-                        const bool weighs = in && !(q.topf - f[e] > q.reach);
-                        if (weighs && place < lo_all) part_all += w;
-                        if (weighs && place < lo_p) part_p += w;
-                        if (weighs && place < lo_u) part_u += w;
-                        hits |= in && place - span_lo < span ? 1u << e : 0u;
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t place = f[e] >= q.cut ? place_of(q, f[e]) : 0xFFFFFFFFu;
+                        const double w = weight_of(q, s.table, f[e], kWhole) - kWhole;
+                        part_all = fma(w, __hiloint2double(place < lo_all ? 0x3FF00000 : 0, 0), part_all);      // times 1 or 0
+                        part_p = fma(w, __hiloint2double(place < lo_p ? 0x3FF00000 : 0, 0), part_p);
+                        part_u = fma(w, __hiloint2double(place < lo_u ? 0x3FF00000 : 0, 0), part_u);
+                        any = any || place - span_lo < span;
                     }
-                    sum_all += whole_bits(part_all);
-                    sum_p += whole_bits(part_p);
-                    sum_u += whole_bits(part_u);
-                    collect(hits, f, at);
+                    sum_all += whole_of(part_all);
+                    sum_p += whole_of(part_p);
+                    sum_u += whole_of(part_u);
+                    if (any) collect(f, at);
                 });
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) {
@@ -703,7 +719,7 @@ tfe_sample_kernel(const SampleParams p)
                 if (tid == 0) {
                     p.tokens[r] = key_index(key);
                     const float z = key_logit(key);
-                    if (p.prob) p.prob[r] = in_reach(q, z) ? (float)(weight_of<false>(q, s.table, z) / (double)limit) : 0.f;
+                    if (p.prob) p.prob[r] = (float)(weight_of(q, s.table, z, 0.0) / (double)limit);
                     s.cmd.op = kOpDone;
                 }
             } else {
