@@ -242,3 +242,25 @@ def test_empty_batch_and_refusals():
         engine.quantize_fp8(torch.zeros((4, 64), dtype=torch.float16, device=DEV))
     with pytest.raises(ValueError):
         engine.QuantizedHead(torch.zeros((4, 72), device=DEV))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_conversion_next_to_the_rounding_borders(kind):
+    """Values whose quotients lie on the borders between e4m3 values and next to them, for many scales: half a million
+    quotients bit for bit, of scales over the whole range."""
+    from paper_2607_07388_b200 import engine
+    rng = np.random.default_rng(77)
+    r = 4096
+    x = np.zeros((r, 128), np.float32)
+    big = np.exp2(rng.uniform(-120, 120, r)).astype(np.float32)
+    border = (E4M3[:-1] + E4M3[1:]) / 2
+    for i in range(r):
+        s = np.float32(big[i] / np.float32(448))
+        x[i, 1:] = (rng.choice(border, 127) * np.float64(s)).astype(np.float32)
+        x[i, 1:] = (x[i, 1:].view(np.int32) + rng.integers(-2, 3, 127).astype(np.int32)).view(np.float32)
+        x[i, 0] = big[i]
+    xt = torch.from_numpy(x).to(TYPES[kind])
+    q, scale = engine.quantize_fp8(xt.to(DEV))
+    bits, _, s = quantize64(xt.float().numpy(), 1)
+    assert np.array_equal(scale.cpu().numpy(), s)
+    assert np.array_equal(q.view(torch.uint8).cpu().numpy() & 0x7F, bits)
