@@ -56,20 +56,20 @@ __device__ __forceinline__ float scale_of(uint32_t amax_bits)
 struct Divisor {
     float s, r;
     bool fast;
-    __device__ __forceinline__ float by_steps(float x) const
+    __device__ __forceinline__ float2 two(float a, float b) const
     {
-        float q = __fmul_rn(x, r);
-        q = __fmaf_rn(__fmaf_rn(-q, s, x), r, q);
-        return __fmaf_rn(__fmaf_rn(-q, s, x), r, q);
+        if (!fast) return make_float2(__fdiv_rn(a, s), __fdiv_rn(b, s));
+        const float2 x = make_float2(a, b), rr = make_float2(r, r), minus = make_float2(-s, -s);
+        float2 q = __fmul2_rn(x, rr);           // both in one instruction
+        q = __ffma2_rn(__ffma2_rn(q, minus, x), rr, q);
+        return __ffma2_rn(__ffma2_rn(q, minus, x), rr, q);
     }
     __device__ __forceinline__ uint32_t to_e4m3x4(float a, float b, float c, float d) const
     {
-        const uint32_t lo = __nv_cvt_float2_to_fp8x2(fast ? make_float2(by_steps(a), by_steps(b)) : make_float2(__fdiv_rn(a, s), __fdiv_rn(b, s)), __NV_SATFINITE, __NV_E4M3);
-        const uint32_t hi = __nv_cvt_float2_to_fp8x2(fast ? make_float2(by_steps(c), by_steps(d)) : make_float2(__fdiv_rn(c, s), __fdiv_rn(d, s)), __NV_SATFINITE, __NV_E4M3);
+        const uint32_t lo = __nv_cvt_float2_to_fp8x2(two(a, b), __NV_SATFINITE, __NV_E4M3), hi = __nv_cvt_float2_to_fp8x2(two(c, d), __NV_SATFINITE, __NV_E4M3);
         return lo | (hi << 16);
     }
 };
-
 __device__ __forceinline__ Divisor divisor(float s) { return {s, __fdiv_rn(1.f, s), s >= 0x1p-90f && s <= 0x1p100f}; }
 
 // Eight elements of a group as they were read: 8 l .. 8 l + 7 for lane l (kVector: whole 16-byte vectors), or l, l + 16, ...;
@@ -157,8 +157,9 @@ tfe_quantize_rows_kernel(const QuantParams p)
     if (l == 0) p.scale[g] = s;
 }
 
+// Four blocks per SM (64 registers) for bf16: 93 us for 151,936 x 1,024 against 99 us with three.
 template <typename T, bool kVector>
-__global__ void __launch_bounds__(kQuantThreads)
+__global__ void __launch_bounds__(kQuantThreads, sizeof(T) == 2 ? 4 : 2)
 tfe_quantize_blocks_kernel(const QuantParams p)
 {
     constexpr int kRowsAtOnce = kQuantThreads / kGroupLanes, kTurns = 128 / kRowsAtOnce;
