@@ -6,15 +6,20 @@
 //   tfe_quantize_blocks_kernel   weights: a scale per 128 rows and 128 columns; one block holds the 128 x 128 piece.
 //   tfe_matmul_fp8_kernel        out[m][n] = sum_b sa[m][b] sb[n / 128][b] (sum over the 128 k of block b of a[m][k] w[n][k])
 //
-// The product is a persistent, warp-specialised tcgen05 kernel.  The weights' rows are the MMA's M (128), the
-// activations' rows its N (16..256): a thread of the epilogue then owns one vocabulary row, stores of one activation row are
-// contiguous across a warp, and few activation rows waste no tensor memory.  The scales change every 128 k, so an
-// accumulator in tensor memory only ever holds one block's partial sum: the epilogue warps read it, multiply by the two scales
-// and add it to fp32 sums in registers while the next block's MMAs run into another accumulator.  The sums over blocks are
-// thereby plain fp32 additions whatever the precision of the tensor core's own accumulation.
+// The products are persistent, warp-specialised tcgen05 kernels.  The scales change every 128 k, so an accumulator in tensor
+// memory only ever holds one block's partial sum: the epilogue warps read it, multiply by the two scales and add it to fp32
+// sums in registers while the next block's MMAs run into another accumulator.  The sums over blocks are thereby plain fp32
+// additions whatever the precision of the tensor core's own accumulation.
 //
-// Few activation rows (one tile): the read of the weights bounds the call, and the vocabulary is cut into equal row ranges,
-// one per SM, each walked in tiles of 128.  Many: tiles of 128 rows are dealt out in turn.
+//   tfe_matmul_fp8_few_kernel    up to 128 activation rows: the read of the weights bounds the call.  The weights' rows are the
+//                                MMA's M (128), the activations' its N (16..128), so few rows waste neither tensor memory nor
+//                                epilogue work, and a warp's stores of one activation row are contiguous.  The vocabulary is cut
+//                                into equal row ranges, one per SM, each walked in tiles of 128.
+//   tfe_matmul_fp8_many_kernel   more: the operands' way from L2 and the epilogue bound the call.  The activations' rows are the
+//                                MMA's M (128), the weights' its N (256): a thread owns one activation row,
+//                                so a block's scale is one number for all its columns.  Finished rows leave by asynchronous
+//                                bulk copies while the next tile is summed.
+//
 #include <cuda_fp8.h>
 #include <cuda_runtime.h>
 
@@ -188,13 +193,15 @@ tfe_quantize_blocks_kernel(const QuantParams p)
 
 // ------------------------------------------------------------------ product
 
-constexpr int kTileRows = 128;                  // weight rows per tile (MMA M)
+constexpr int kFewRows = 128;                   // up to here the weights' rows are the MMA's M
+constexpr int kTileRows = 128;                  // rows of a tile on that side
 constexpr int kBlockK = 128;                    // bytes of a row per stage: one scale block, one 128-byte swizzle row
 constexpr int kUmmaK = 32;                      // e4m3 elements per tcgen05.mma
 constexpr int kMaxStages = 12;
 constexpr int kScaleRing = 4;
-constexpr int kEpilogueWarps = 8;               // two per lane quarter of tensor memory, half of the columns each
-constexpr int kMatmulThreads = 32 * (3 + kEpilogueWarps);
+// Few rows: epilogue warps per lane quarter of tensor memory; they share its columns.
+__host__ __device__ constexpr int quarter_warps(int tn) { return tn >= 128 ? 4 : 2; }
+__host__ __device__ constexpr int matmul_threads(int tn) { return 32 * (3 + 4 * quarter_warps(tn)); }
 constexpr int kMatmulSmem = 216 * 1024;         // stages; the rest of an SM's 227 KB is the static arrays and alignment
 
 // bits of the device status word
@@ -203,40 +210,12 @@ __device__ uint32_t g_matmul_status;
 
 struct MatmulParams {
     int32_t M, N, kb;                           // activation rows, weight rows, blocks of 128 along k
-    int32_t stages;
-    int32_t m_tiles;
-    int64_t n_units;                            // dealt out: tiles; else unused
-    int32_t rows_per_cta, tail_rows;            // ranges: rows of a CTA, rows of its last short tile
+    int32_t stages;                             // few rows
+    int32_t rows_per_cta, tail_rows;            // few rows: weight rows of a CTA, rows of its last short tile
+    int32_t m_tiles;                            // many rows: tiles of activation rows
+    int64_t n_units;                            // ... and all tiles
     const float *a_scale, *b_scale;             // [M][kb], [ceil(N / 128)][kb]
     void *out; int64_t ldo;
-};
-
-// A CTA's units of work: kRanges: tiles of its own row range; else every gridDim.x-th of all (row tile, m tile).
-template <bool kRanges, int TN>
-struct Units {
-    const MatmulParams &p;
-    int64_t r0, r1;
-    __device__ __forceinline__ Units(const MatmulParams &p_) : p(p_)
-    {
-        r0 = (int64_t)blockIdx.x * p.rows_per_cta;
-        r1 = min((int64_t)p.N, r0 + p.rows_per_cta);
-    }
-    __device__ __forceinline__ bool get(int64_t i, int64_t &n0, int32_t &valid, int32_t &m0) const
-    {
-        if constexpr (kRanges) {
-            n0 = r0 + i * kTileRows;
-            valid = (int32_t)min((int64_t)kTileRows, r1 - n0);
-            m0 = 0;
-            return valid > 0;
-        } else {
-            const int64_t u = blockIdx.x + i * gridDim.x;
-            const int64_t nt = u / p.m_tiles;
-            n0 = nt * kTileRows;
-            valid = (int32_t)min((int64_t)kTileRows, p.N - n0);
-            m0 = (int32_t)(u - nt * p.m_tiles) * TN;
-            return u < p.n_units;
-        }
-    }
 };
 
 // D[tmem] (+)= A[smem] * B[smem]^T, e4m3 inputs, fp32 accumulate; issued by one thread.
@@ -254,6 +233,18 @@ __device__ __forceinline__ void umma_e4m3(uint32_t d_tmem, uint64_t a_desc, uint
 // N >> 3 at [17,23), M >> 4 at [24,29).
 __host__ __device__ constexpr uint32_t umma_idesc_e4m3(uint32_t M, uint32_t N) { return (1u << 4) | ((N >> 3) << 17) | ((M >> 4) << 24); }
 
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&v)[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+          "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]),
+          "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]),
+          "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+        : "r"(taddr)
+        : "memory");
+}
 __device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&v)[8])
 {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
@@ -262,14 +253,15 @@ __device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&v)[8])
                  : "memory");
 }
 
-template <int TN, bool kRanges, typename Out>
-__global__ void __launch_bounds__(kMatmulThreads, 1)
-tfe_matmul_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_w_tail,
+template <int TN, typename Out>
+__global__ void __launch_bounds__(matmul_threads(TN), 1)
+tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_w_tail,
                       const __grid_constant__ CUtensorMap map_a, const MatmulParams p)
 {
-    constexpr int kBuffers = TN == 256 ? 2 : 4;         // accumulators of TN columns
+    constexpr int kBuffers = 4;                         // accumulators of TN columns
     constexpr uint32_t kTmemCols = kBuffers * TN;       // 64 .. 512, a power of two
-    constexpr int kCols = TN / 2;                       // columns of an epilogue warp
+    constexpr int kEpilogueWarps = 4 * quarter_warps(TN);
+    constexpr int kCols = TN / quarter_warps(TN);       // columns of an epilogue warp
     constexpr uint32_t kStageBytes = kTileRows * 128u + TN * 128u;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_acc_full[kBuffers], s_acc_empty[kBuffers];
@@ -293,19 +285,21 @@ tfe_matmul_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = s_tmem_base;
-    const Units<kRanges, TN> units(p);
-    int64_t n0;
-    int32_t valid, m0;
+    // this CTA's weight rows, and its tiles of them
+    const int64_t r0 = (int64_t)blockIdx.x * p.rows_per_cta;
+    const int32_t n_rows = (int32_t)min((int64_t)p.rows_per_cta, p.N - r0), n_tiles = (n_rows + kTileRows - 1) / kTileRows;
 
     if (warp == 0) {
         // ============================ TMA producer ============================
         if (lane == 0) {
-            // weights are read once when there is one tile of activation rows, else again by the tiles beside this one
-            const uint64_t hint_w = kRanges ? 0x12F0000000000000ull : 0x14F0000000000000ull, hint_a = 0x14F0000000000000ull;
+            const uint64_t hint_w = 0x12F0000000000000ull;          // evict first: the weights are read once
+            const uint64_t hint_a = 0x14F0000000000000ull;          // evict last: the activations are read by every tile
             uint32_t stage = 0, phase = 0, issued = 0;
             bool ok = true;
-            for (int64_t i = 0; ok && units.get(i, n0, valid, m0); ++i) {
-                const bool tail = kRanges && valid < kTileRows && valid == p.tail_rows;
+            for (int32_t t = 0; ok && t < n_tiles; ++t) {
+                const int32_t valid = min(kTileRows, n_rows - t * kTileRows);
+                // a short last tile is fetched with the short box: only its rows are read
+                const bool tail = valid < kTileRows && valid == p.tail_rows;
                 const uint32_t w_bytes = tail ? (uint32_t)p.tail_rows * 128u : kTileRows * 128u;
                 for (int32_t kb = 0; kb < p.kb; ++kb) {
                     if (!mbar_wait(smem_u32(&s_empty[stage]), phase ^ 1u, &s_abort)) {
@@ -316,8 +310,8 @@ tfe_matmul_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                     }
                     const uint32_t bar = smem_u32(&s_full[stage]), dst = smem_base + stage * kStageBytes;
                     mbar_expect_tx(bar, w_bytes + TN * 128u);
-                    tma_load_2d(dst, tail ? &map_w_tail : &map_w, bar, kb * kBlockK, (int32_t)n0, hint_w);
-                    tma_load_2d(dst + kTileRows * 128u, &map_a, bar, kb * kBlockK, m0, hint_a);
+                    tma_load_2d(dst, tail ? &map_w_tail : &map_w, bar, kb * kBlockK, (int32_t)(r0 + (int64_t)t * kTileRows), hint_w);
+                    tma_load_2d(dst + kTileRows * 128u, &map_a, bar, kb * kBlockK, 0, hint_a);
                     ++issued;
                     if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
                 }
@@ -334,7 +328,7 @@ tfe_matmul_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
             constexpr uint32_t idesc = umma_idesc_e4m3(kTileRows, TN);
             uint32_t stage = 0, phase = 0, buf = 0, buf_phase = 0;
             bool ok = true;
-            for (int64_t i = 0; ok && units.get(i, n0, valid, m0); ++i) {
+            for (int32_t t = 0; ok && t < n_tiles; ++t) {
                 for (int32_t kb = 0; kb < p.kb; ++kb) {
                     if (!mbar_wait(smem_u32(&s_acc_empty[buf]), buf_phase ^ 1u, &s_abort) ||
                         !mbar_wait(smem_u32(&s_full[stage]), phase, &s_abort)) {
@@ -364,15 +358,11 @@ tfe_matmul_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
         // ============================ activation scales =======================
         uint32_t st = 0, phase = 0;
         bool ok = true;
-        for (int64_t i = 0; ok && units.get(i, n0, valid, m0); ++i) {
+        for (int32_t t = 0; ok && t < n_tiles; ++t) {
             for (int32_t kb = 0; kb < p.kb; ++kb) {
                 float v[(TN + 31) / 32];
-                const float sb = kRanges ? 1.f : __ldg(p.b_scale + (n0 / 128) * p.kb + kb);
 #pragma unroll
-                for (int c = 0; c < (TN + 31) / 32; ++c) {
-                    const int32_t m = m0 + c * 32 + lane;
-                    v[c] = m < p.M ? __ldg(p.a_scale + (int64_t)m * p.kb + kb) * sb : 0.f;
-                }
+                for (int c = 0; c < (TN + 31) / 32; ++c) v[c] = c * 32 + lane < p.M ? __ldg(p.a_scale + (int64_t)(c * 32 + lane) * p.kb + kb) : 0.f;
                 ok = mbar_wait(smem_u32(&s_sc_empty[st]), phase ^ 1u, &s_abort);
                 if (!__all_sync(0xFFFFFFFFu, ok)) {
                     if (lane == 0) atomicOr(&g_matmul_status, kTimeoutScales);
@@ -392,19 +382,20 @@ tfe_matmul_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
         const uint32_t quarter = (uint32_t)warp & 3u;               // tensor-memory lanes 32 * quarter .. + 31
         const int32_t c0 = ((warp - 3) >> 2) * kCols;               // this warp's columns
         const int32_t row_in_tile = (int32_t)(quarter * 32u) + lane;
-        constexpr int kChunk = kCols >= 16 ? 16 : 8;
+        constexpr int kChunk = kCols >= 32 ? 32 : kCols;
         uint32_t st = 0, phase = 0, buf = 0, buf_phase = 0;
         bool ok = true;
-        for (int64_t i = 0; ok && units.get(i, n0, valid, m0); ++i) {
-            const int64_t n = n0 + row_in_tile;
-            float acc[kCols];
+        for (int32_t t = 0; ok && t < n_tiles; ++t) {
+            const int64_t n0 = r0 + (int64_t)t * kTileRows;
+            const int32_t valid = min(kTileRows, n_rows - t * kTileRows);
+            float2 acc[kCols / 2];
 #pragma unroll
-            for (int j = 0; j < kCols; ++j) acc[j] = 0.f;
-            const float *sb_row = p.b_scale + (row_in_tile < valid ? n / 128 : n0 / 128) * p.kb;
-            float sb_next = kRanges ? __ldg(sb_row) : 1.f;
+            for (int j = 0; j < kCols / 2; ++j) acc[j] = make_float2(0.f, 0.f);
+            const float *sb_row = p.b_scale + (row_in_tile < valid ? (n0 + row_in_tile) / 128 : n0 / 128) * p.kb;
+            float sb_next = __ldg(sb_row);
             for (int32_t kb = 0; kb < p.kb; ++kb) {
-                const float sb = sb_next;
-                if (kRanges && kb + 1 < p.kb) sb_next = __ldg(sb_row + kb + 1);
+                const float2 sb = make_float2(sb_next, sb_next);
+                if (kb + 1 < p.kb) sb_next = __ldg(sb_row + kb + 1);
                 ok = mbar_wait(smem_u32(&s_sc_full[st]), phase, &s_abort) && mbar_wait(smem_u32(&s_acc_full[buf]), buf_phase, &s_abort);
                 if (!__all_sync(0xFFFFFFFFu, ok)) {
                     if (lane == 0) atomicOr(&g_matmul_status, kTimeoutEpilogue);
@@ -417,15 +408,19 @@ tfe_matmul_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
 #pragma unroll
                 for (int c = 0; c < kCols; c += kChunk) {
                     uint32_t v[kChunk];
-                    if constexpr (kChunk == 16) tmem_ld16(taddr + (uint32_t)c, v); else tmem_ld8(taddr + (uint32_t)c, v);
+                    if constexpr (kChunk == 32) tmem_ld32(taddr + (uint32_t)c, v);
+                    else if constexpr (kChunk == 16) tmem_ld16(taddr + (uint32_t)c, v);
+                    else tmem_ld8(taddr + (uint32_t)c, v);
                     tmem_ld_wait();
 #pragma unroll
                     for (int j = 0; j < kChunk; j += 4) {
                         const float4 sa = *reinterpret_cast<const float4 *>(&s_scale[st][c0 + c + j]);
-                        acc[c + j] = fmaf(__uint_as_float(v[j]), kRanges ? sa.x * sb : sa.x, acc[c + j]);
-                        acc[c + j + 1] = fmaf(__uint_as_float(v[j + 1]), kRanges ? sa.y * sb : sa.y, acc[c + j + 1]);
-                        acc[c + j + 2] = fmaf(__uint_as_float(v[j + 2]), kRanges ? sa.z * sb : sa.z, acc[c + j + 2]);
-                        acc[c + j + 3] = fmaf(__uint_as_float(v[j + 3]), kRanges ? sa.w * sb : sa.w, acc[c + j + 3]);
+                        float2 lo = make_float2(sa.x, sa.y), hi = make_float2(sa.z, sa.w);
+                        lo = __fmul2_rn(lo, sb);
+                        hi = __fmul2_rn(hi, sb);
+                        float2 &x = acc[(c + j) / 2], &y = acc[(c + j) / 2 + 1];
+                        x = __ffma2_rn(make_float2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), lo, x);
+                        y = __ffma2_rn(make_float2(__uint_as_float(v[j + 2]), __uint_as_float(v[j + 3])), hi, y);
                     }
                 }
                 tc_fence_before();
@@ -435,11 +430,13 @@ tfe_matmul_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                 if (++buf == kBuffers) { buf = 0; buf_phase ^= 1u; }
             }
             if (ok && row_in_tile < valid) {
-                Out *at = static_cast<Out *>(p.out) + (int64_t)(m0 + c0) * p.ldo + n;
-                const int32_t left = p.M - m0 - c0;
+                Out *at = static_cast<Out *>(p.out) + (int64_t)c0 * p.ldo + n0 + row_in_tile;
+                const int32_t left = p.M - c0;
 #pragma unroll
-                for (int j = 0; j < kCols; ++j)
-                    if (j < left) Elem<Out>::put(at + (int64_t)j * p.ldo, acc[j]);
+                for (int j = 0; j < kCols; ++j) {
+                    if (j < left) Elem<Out>::put(at, j & 1 ? acc[j / 2].y : acc[j / 2].x);
+                    at += p.ldo;
+                }
             }
         }
     }
@@ -450,6 +447,264 @@ tfe_matmul_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
         __syncwarp();
         tc_fence_after();
         tmem_dealloc(tmem_base, kTmemCols);
+    }
+}
+
+// ------------------------------------------------------------------ product, many activation rows
+
+constexpr int kManyEpilogueWarps = 8;           // two per lane quarter, half of the tile's columns each
+constexpr int kManyThreads = 32 * (4 + kManyEpilogueWarps);
+// Registers per thread: the first four warps give most of theirs to the epilogue's.  The sum, 128 x 40 + 256 x 216, must not
+// exceed what the block is launched with (384 x 168); the host checks that before the launch.
+constexpr int kManyFewRegs = 40, kManyManyRegs = 216;
+constexpr int kRowWords = 64;                   // 32-bit words of a thread's part of a row: 128 bf16 or 64 fp32
+constexpr int kRowPitch = 4 * kRowWords + 16;   // bytes between the rows of an epilogue warp's outgoing area: 16-byte writes without conflicts
+
+constexpr int kManyN = 256;                     // weight rows of a tile (MMA N)
+constexpr int kManyCols = kManyN / 2;           // columns of an epilogue warp: one scale block of the weights
+constexpr int kManyStages = 3;
+constexpr uint32_t kManyStageBytes = kTileRows * 128u + kManyN * 128u;
+constexpr size_t kManySmem = 1024 + (size_t)kManyStages * kManyStageBytes + (size_t)kManyEpilogueWarps * 32 * kRowPitch;
+
+__device__ __forceinline__ void bulk_store(void *to, uint32_t from_smem, uint32_t bytes)
+{
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(to), "r"(from_smem), "r"(bytes) : "memory");
+}
+
+// Part of a thread's finished output row, kCols columns in registers, to `at`.  The 16-byte blocks of the output that it covers
+// whole go through the thread's own row in shared memory and an asynchronous bulk copy, which leaves the load/store path to
+// others; the words are first shifted (by registers: the distance to a boundary is the thread's own) so that both sides are
+// aligned.  What is left at the two ends, up to 15 bytes each, is stored directly in pieces of 2, 4 and 8 bytes.  `cols` of the
+// columns exist.
+template <typename Out, int kCols>
+__device__ __forceinline__ void send_row(Out *at, const float2 *acc, int32_t cols, uint32_t row_smem)
+{
+    static_assert(kCols * sizeof(Out) == kRowWords * 4, "the columns fill the row");
+    constexpr int E = 16 / (int)sizeof(Out);                                    // elements per 16 bytes
+    const uint32_t past = (uint32_t)(reinterpret_cast<uintptr_t>(at) & 15u) / (uint32_t)sizeof(Out);
+    const int32_t head = past ? E - (int32_t)past : 0, tail = (int32_t)past;    // (kCols is a multiple of E)
+    auto element = [&](int i) { return i & 1 ? acc[i / 2].y : acc[i / 2].x; };
+    if (cols < kCols) {                                                         // the last columns of the matrix
+#pragma unroll
+        for (int i = 0; i < kCols; ++i)
+            if (i < cols) Elem<Out>::put(at + i, element(i));
+        return;
+    }
+    const bool odd = sizeof(Out) == 2 && (head & 1);
+    // word j of the part from its first 4-byte boundary on: one fp32, or two bf16 (elements 2 j + 1 and 2 j + 2 if odd)
+    auto word = [&](int j) -> uint32_t {
+        if (j >= kRowWords) return 0u;
+        if constexpr (sizeof(Out) == 4) {
+            return __float_as_uint(element(j));
+        } else {
+            const float second = j + 1 < kRowWords ? element((2 * j + 2) % kCols) : 0.f;
+            const __nv_bfloat162 h = __floats2bfloat162_rn(odd ? element(2 * j + 1) : element(2 * j), odd ? second : element(2 * j + 1));
+            return *reinterpret_cast<const uint32_t *>(&h);
+        }
+    };
+    if constexpr (sizeof(Out) == 4) {
+        if (head & 1) *reinterpret_cast<uint32_t *>(at) = word(0);
+        if (head & 2) *reinterpret_cast<uint2 *>(at + (head & 1)) = head & 1 ? make_uint2(word(1), word(2)) : make_uint2(word(0), word(1));
+    } else {
+        if (odd) Elem<Out>::put(at, element(0));
+        if (head & 2) *reinterpret_cast<uint32_t *>(at + (head & 1)) = word(0);
+        if (head & 4) *reinterpret_cast<uint2 *>(at + (head & 3)) = head & 2 ? make_uint2(word(1), word(2)) : make_uint2(word(0), word(1));
+    }
+    const int32_t shift = head * (int32_t)sizeof(Out) / 4;                      // 0..3 words
+    uint32_t w[4];                                                              // four words at a time: few registers beside the sums
+#pragma unroll
+    for (int c = 0; c < kRowWords; c += 4) {
+        uint32_t v[6];
+#pragma unroll
+        for (int i = 0; i < 6; ++i) v[i] = shift & 1 ? word(c + i + 1) : word(c + i);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = shift & 2 ? v[i + 2] : v[i];
+        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(row_smem + 4 * c), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    bulk_store(at + head, row_smem, past ? 4 * kRowWords - 16 : 4 * kRowWords);
+    // the tail starts on a 16-byte boundary, with the last four words
+    Out *end = at + kCols - tail;
+    if constexpr (sizeof(Out) == 4) {
+        if (tail & 2) *reinterpret_cast<uint2 *>(end) = make_uint2(w[0], w[1]);
+        if (tail & 1) *reinterpret_cast<uint32_t *>(end + (tail & 2)) = tail & 2 ? w[2] : w[0];
+    } else {
+        if (tail & 4) *reinterpret_cast<uint2 *>(end) = make_uint2(w[0], w[1]);
+        if (tail & 2) *reinterpret_cast<uint32_t *>(end + (tail & 4)) = tail & 4 ? w[2] : w[0];
+        if (tail & 1) {
+            const uint32_t lo = tail & 2 ? w[1] : w[0], hi = tail & 2 ? w[3] : w[2];
+            end[tail - 1] = __ushort_as_bfloat16((unsigned short)(tail & 4 ? hi : lo));
+        }
+    }
+}
+
+template <typename Out>
+__global__ void __launch_bounds__(kManyThreads, 1)
+tfe_matmul_fp8_many_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_a, const MatmulParams p)
+{
+    constexpr int kStages = kManyStages, kN = kManyN, kCols = kManyCols, kBuffers = 512 / kN;
+    constexpr int kRounds = kCols * (int)sizeof(Out) / (4 * kRowWords);         // outgoing rows full of a thread's columns
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_acc_full[kBuffers], s_acc_empty[kBuffers], s_drain;
+    __shared__ uint32_t s_tmem_base;
+    __shared__ volatile uint32_t s_abort;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) { mbar_init(smem_u32(&s_full[s]), 1); mbar_init(smem_u32(&s_empty[s]), 1); }
+        for (int a = 0; a < kBuffers; ++a) { mbar_init(smem_u32(&s_acc_full[a]), 1); mbar_init(smem_u32(&s_acc_empty[a]), kManyEpilogueWarps); }
+        mbar_init(smem_u32(&s_drain), 1);
+        s_abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc(smem_u32(&s_tmem_base), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = s_tmem_base;
+
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kManyFewRegs));
+        if (warp == 0 && lane == 0) {
+            // ============================ TMA producer ============================
+            const uint64_t hint = 0x14F0000000000000ull;            // evict last: both operands are read by other tiles too
+            uint32_t stage = 0, phase = 0, issued = 0;
+            bool ok = true;
+            for (int64_t u = blockIdx.x; ok && u < p.n_units; u += gridDim.x) {
+                const int64_t nt = u / p.m_tiles;
+                const int32_t n0 = (int32_t)(nt * kN), m0 = (int32_t)(u - nt * p.m_tiles) * kTileRows;
+                for (int32_t kb = 0; kb < p.kb; ++kb) {
+                    if (!mbar_wait(smem_u32(&s_empty[stage]), phase ^ 1u, &s_abort)) {
+                        atomicOr(&g_matmul_status, kTimeoutLoader);
+                        s_abort = 1;
+                        ok = false;
+                        break;
+                    }
+                    const uint32_t bar = smem_u32(&s_full[stage]), dst = smem_base + stage * kManyStageBytes;
+                    mbar_expect_tx(bar, kManyStageBytes);
+                    tma_load_2d(dst, &map_a, bar, kb * kBlockK, m0, hint);
+                    tma_load_2d(dst + kTileRows * 128u, &map_w, bar, kb * kBlockK, n0, hint);
+                    ++issued;
+                    if (++stage == kStages) { stage = 0; phase ^= 1u; }
+                }
+            }
+            if (!ok)                            // copies in flight land before the shared memory goes
+                for (uint32_t s = 0; s < kStages; ++s) {
+                    const uint32_t fills = (issued + kStages - 1u - s) / kStages;
+                    for (uint32_t t = 0; fills && t < TC_WAIT_LIMIT && !mbar_try_wait(smem_u32(&s_full[s]), (fills - 1u) & 1u); ++t) { }
+                }
+        } else if (warp == 1 && lane == 0) {
+            // ============================ MMA issuer ==============================
+            constexpr uint32_t idesc = umma_idesc_e4m3(kTileRows, kN);
+            uint32_t stage = 0, phase = 0, buf = 0, buf_phase = 0;
+            bool ok = true;
+            for (int64_t u = blockIdx.x; ok && u < p.n_units; u += gridDim.x)
+                for (int32_t kb = 0; kb < p.kb; ++kb) {
+                    if (!mbar_wait(smem_u32(&s_acc_empty[buf]), buf_phase ^ 1u, &s_abort) ||
+                        !mbar_wait(smem_u32(&s_full[stage]), phase, &s_abort)) {
+                        atomicOr(&g_matmul_status, kTimeoutMma);
+                        s_abort = 1;
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint32_t a_addr = smem_base + stage * kManyStageBytes;
+                    const uint64_t a_desc = umma_desc_sw128(a_addr), w_desc = umma_desc_sw128(a_addr + kTileRows * 128u);
+#pragma unroll
+                    for (int k = 0; k < kBlockK / kUmmaK; ++k)
+                        umma_e4m3(tmem_base + buf * kN, a_desc + (uint64_t)(2 * k), w_desc + (uint64_t)(2 * k), idesc, k > 0 ? 1u : 0u);
+                    umma_commit(smem_u32(&s_empty[stage]));
+                    umma_commit(smem_u32(&s_acc_full[buf]));
+                    if (++stage == kStages) { stage = 0; phase ^= 1u; }
+                    if (++buf == kBuffers) { buf = 0; buf_phase ^= 1u; }
+                }
+            if (!ok) {                          // MMAs in flight end before their tensor memory is freed
+                umma_commit(smem_u32(&s_drain));
+                for (uint32_t t = 0; t < TC_WAIT_LIMIT && !mbar_try_wait(smem_u32(&s_drain), 0); ++t) { }
+            }
+        }
+    } else {
+        // ============================ epilogue ================================
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyManyRegs));
+        const int e = warp - 4;
+        const uint32_t quarter = (uint32_t)warp & 3u;               // tensor-memory lanes 32 * quarter .. + 31
+        const int32_t c0 = (e >> 2) * kCols;                        // this warp's columns, all in one scale block of the weights
+        const uint32_t row_smem = smem_base + kStages * kManyStageBytes + (uint32_t)((e * 32 + lane) * kRowPitch);
+        uint32_t buf = 0, buf_phase = 0;
+        bool ok = true;
+        for (int64_t u = blockIdx.x; ok && u < p.n_units; u += gridDim.x) {
+            const int64_t nt = u / p.m_tiles;
+            const int64_t n0 = nt * kN + c0;
+            const int32_t m0 = (int32_t)(u - nt * p.m_tiles) * kTileRows + (int32_t)quarter * 32;
+            const float *sa_row = p.a_scale + (int64_t)min(m0 + lane, p.M - 1) * p.kb;
+            const float *sb_row = p.b_scale + min(n0, (int64_t)p.N - 1) / 128 * p.kb;
+            float2 acc[kCols / 2];
+#pragma unroll
+            for (int j = 0; j < kCols / 2; ++j) acc[j] = make_float2(0.f, 0.f);
+            // Scales of four blocks at a time, loaded while the four before are used (a register that waits for a load stalls even
+            // a move, so they are touched only then).
+            float scales[4], sa[4], sb[4];
+            auto fetch = [&](int32_t kb) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    sa[i] = kb + i < p.kb ? __ldg(sa_row + kb + i) : 0.f;
+                    sb[i] = kb + i < p.kb ? __ldg(sb_row + kb + i) : 0.f;
+                }
+            };
+            fetch(0);
+            for (int32_t kb = 0; kb < p.kb; ++kb) {
+                if ((kb & 3) == 0) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) scales[i] = sa[i] * sb[i];
+                    fetch(kb + 4);
+                }
+                const float2 scale = make_float2(scales[0], scales[0]);
+                scales[0] = scales[1]; scales[1] = scales[2]; scales[2] = scales[3];
+                ok = mbar_wait(smem_u32(&s_acc_full[buf]), buf_phase, &s_abort);
+                if (!__all_sync(0xFFFFFFFFu, ok)) {
+                    if (lane == 0) atomicOr(&g_matmul_status, kTimeoutEpilogue);
+                    s_abort = 1;
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
+                const uint32_t taddr = tmem_base + ((quarter * 32u) << 16) + buf * kN + (uint32_t)c0;
+#pragma unroll
+                for (int c = 0; c < kCols; c += 16) {
+                    uint32_t v[16];
+                    tmem_ld16(taddr + (uint32_t)c, v);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 16; j += 2)
+                        acc[(c + j) / 2] = __ffma2_rn(make_float2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), scale, acc[(c + j) / 2]);
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&s_acc_empty[buf]));
+                if (++buf == kBuffers) { buf = 0; buf_phase ^= 1u; }
+            }
+            if (!ok) break;
+            const int64_t left = (int64_t)p.N - n0;
+#pragma unroll
+            for (int round = 0; round < kRounds; ++round) {
+                constexpr int kPart = kCols / kRounds;
+                asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // this thread's last row has left its place
+                if (left > round * kPart && m0 + lane < p.M)
+                    send_row<Out, kPart>(static_cast<Out *>(p.out) + (int64_t)(m0 + lane) * p.ldo + n0 + round * kPart, acc + round * (kPart / 2),
+                                         (int32_t)min((int64_t)kPart, left - round * kPart), row_smem);
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+            }
+        }
+        asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        __syncwarp();
+        tc_fence_after();
+        tmem_dealloc(tmem_base, 512);
     }
 }
 
@@ -468,24 +723,41 @@ bool make_map_fp8(CUtensorMap *map, const void *base, int64_t rows, int64_t cols
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int TN, bool kRanges, typename Out>
-tfe_status launch_matmul(int grid, cudaStream_t stream, const CUtensorMap &w, const CUtensorMap &w_tail, const CUtensorMap &a, MatmulParams p)
+template <int TN, typename Out>
+tfe_status launch_few(int grid, cudaStream_t stream, const CUtensorMap &w, const CUtensorMap &w_tail, const CUtensorMap &a, MatmulParams p)
 {
     constexpr size_t stage = kTileRows * 128 + TN * 128;
     p.stages = (int32_t)std::min<size_t>(kMaxStages, (kMatmulSmem - 1024) / stage);
-    auto kernel = tfe_matmul_fp8_kernel<TN, kRanges, Out>;
+    auto kernel = tfe_matmul_fp8_few_kernel<TN, Out>;
     const size_t smem = (size_t)p.stages * stage + 1024;
     if (tfe_status st = tfe_note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem), "product attribute")) return st;
-    kernel<<<grid, kMatmulThreads, smem, stream>>>(w, w_tail, a, p);
+    kernel<<<grid, matmul_threads(TN), smem, stream>>>(w, w_tail, a, p);
     return tfe_note_cuda(cudaGetLastError(), "product launch");
 }
 
-template <int TN, bool kRanges>
-tfe_status launch_matmul(int32_t out_dtype, int grid, cudaStream_t stream, const CUtensorMap &w, const CUtensorMap &w_tail, const CUtensorMap &a,
-                         const MatmulParams &p)
+template <int TN>
+tfe_status launch_few(int32_t out_dtype, int grid, cudaStream_t stream, const CUtensorMap &w, const CUtensorMap &w_tail, const CUtensorMap &a,
+                      const MatmulParams &p)
 {
-    return out_dtype == TFE_DTYPE_BF16 ? launch_matmul<TN, kRanges, __nv_bfloat16>(grid, stream, w, w_tail, a, p)
-                                       : launch_matmul<TN, kRanges, float>(grid, stream, w, w_tail, a, p);
+    return out_dtype == TFE_DTYPE_BF16 ? launch_few<TN, __nv_bfloat16>(grid, stream, w, w_tail, a, p) : launch_few<TN, float>(grid, stream, w, w_tail, a, p);
+}
+
+template <typename Out>
+tfe_status launch_many(int sms, cudaStream_t stream, const void *w, int64_t ldw, const void *a, int64_t lda, int32_t K, MatmulParams p)
+{
+    auto kernel = tfe_matmul_fp8_many_kernel<Out>;
+    // the registers that its warps ask for have to be there (they would wait for good)
+    cudaFuncAttributes attr;
+    if (tfe_status st = tfe_note_cuda(cudaFuncGetAttributes(&attr, kernel), "product attributes")) return st;
+    if (attr.numRegs * kManyThreads < 128 * kManyFewRegs + 32 * kManyEpilogueWarps * kManyManyRegs) return TFE_ERR_INTERNAL;
+    if (tfe_status st = tfe_note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kManySmem), "product attribute")) return st;
+    p.m_tiles = (p.M + kTileRows - 1) / kTileRows;
+    p.n_units = ((int64_t)p.N + kManyN - 1) / kManyN * p.m_tiles;
+    CUtensorMap map_w, map_a;
+    if (!make_map_fp8(&map_w, w, p.N, K, ldw, kManyN) || !make_map_fp8(&map_a, a, p.M, K, lda, kTileRows))
+        return tfe_note_cuda(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+    kernel<<<(unsigned)std::min<int64_t>(sms, p.n_units), kManyThreads, kManySmem, stream>>>(map_w, map_a, p);
+    return tfe_note_cuda(cudaGetLastError(), "product launch");
 }
 
 bool aligned(const void *ptr, uintptr_t to) { return ptr && reinterpret_cast<uintptr_t>(ptr) % to == 0; }
@@ -541,32 +813,23 @@ tfe_status tfe_matmul_fp8(const void *a, int64_t lda, const float *a_scale, int3
     MatmulParams p{};
     p.M = M; p.N = N; p.kb = (K + kBlockK - 1) / kBlockK;
     p.a_scale = a_scale; p.b_scale = w_scale; p.out = out; p.ldo = ldo;
-    const int tn = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : 256;
-    int grid;
-    uint32_t tail = 8;
-    if (M <= tn) {
-        p.m_tiles = 1;
-        p.rows_per_cta = (int32_t)((((int64_t)N + sms - 1) / sms + 7) / 8 * 8);
-        grid = (int)(((int64_t)N + p.rows_per_cta - 1) / p.rows_per_cta);
-        p.tail_rows = p.rows_per_cta % kTileRows;
-        if (p.tail_rows) tail = (uint32_t)p.tail_rows;
-    } else {
-        p.m_tiles = (M + tn - 1) / tn;
-        p.n_units = ((int64_t)N + kTileRows - 1) / kTileRows * p.m_tiles;
-        grid = (int)std::min<int64_t>(sms, p.n_units);
-    }
-    CUtensorMap map_w, map_w_tail, map_a;
-    if (!make_map_fp8(&map_w, w, N, K, ldw, kTileRows) || !make_map_fp8(&map_w_tail, w, N, K, ldw, tail) || !make_map_fp8(&map_a, a, M, K, lda, (uint32_t)tn))
-        return tfe_note_cuda(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    CUtensorMap map_w, map_a;
+    if (M > kFewRows)
+        return out_dtype == TFE_DTYPE_BF16 ? launch_many<__nv_bfloat16>(sms, stream, w, ldw, a, lda, K, p) : launch_many<float>(sms, stream, w, ldw, a, lda, K, p);
+    const int tn = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
+    p.rows_per_cta = (int32_t)((((int64_t)N + sms - 1) / sms + 7) / 8 * 8);
+    p.tail_rows = p.rows_per_cta % kTileRows;
+    const int grid = (int)(((int64_t)N + p.rows_per_cta - 1) / p.rows_per_cta);
+    CUtensorMap map_w_tail;
+    if (!make_map_fp8(&map_w, w, N, K, ldw, kTileRows) || !make_map_fp8(&map_w_tail, w, N, K, ldw, p.tail_rows ? (uint32_t)p.tail_rows : 8u) ||
+        !make_map_fp8(&map_a, a, M, K, lda, (uint32_t)tn))
+        return tfe_note_cuda(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
     switch (tn) {
-    case 16: return launch_matmul<16, true>(out_dtype, grid, stream, map_w, map_w_tail, map_a, p);
-    case 32: return launch_matmul<32, true>(out_dtype, grid, stream, map_w, map_w_tail, map_a, p);
-    case 64: return launch_matmul<64, true>(out_dtype, grid, stream, map_w, map_w_tail, map_a, p);
-    case 128: return launch_matmul<128, true>(out_dtype, grid, stream, map_w, map_w_tail, map_a, p);
-    default:
-        return p.m_tiles == 1 ? launch_matmul<256, true>(out_dtype, grid, stream, map_w, map_w_tail, map_a, p)
-                              : launch_matmul<256, false>(out_dtype, grid, stream, map_w, map_w_tail, map_a, p);
+    case 16: return launch_few<16>(out_dtype, grid, stream, map_w, map_w_tail, map_a, p);
+    case 32: return launch_few<32>(out_dtype, grid, stream, map_w, map_w_tail, map_a, p);
+    case 64: return launch_few<64>(out_dtype, grid, stream, map_w, map_w_tail, map_a, p);
+    default: return launch_few<128>(out_dtype, grid, stream, map_w, map_w_tail, map_a, p);
     }
 }
 
