@@ -11,8 +11,8 @@
 // sums in registers while the next block's MMAs run into another accumulator.  The sums over blocks are thereby plain fp32
 // additions whatever the precision of the tensor core's own accumulation.
 //
-//   tfe_matmul_fp8_few_kernel    up to 128 activation rows: the read of the weights bounds the call.  The weights' rows are the
-//                                MMA's M (128), the activations' its N (16..128), so few rows waste neither tensor memory nor
+//   tfe_matmul_fp8_few_kernel    up to 64 activation rows: the read of the weights bounds the call.  The weights' rows are the
+//                                MMA's M (128), the activations' its N (16..64), so few rows waste neither tensor memory nor
 //                                epilogue work, and a warp's stores of one activation row are contiguous.  The vocabulary is cut
 //                                into equal row ranges, one per SM, each walked in tiles of 128.
 //   tfe_matmul_fp8_many_kernel   more: the operands' way from L2 and the epilogue bound the call.  The activations' rows are the
@@ -193,16 +193,21 @@ tfe_quantize_blocks_kernel(const QuantParams p)
 
 // ------------------------------------------------------------------ product
 
-constexpr int kFewRows = 128;                   // up to here the weights' rows are the MMA's M
+// Up to here the weights' rows are the MMA's M.  100 x 151,936 x 1,024 to fp32 takes 51.5 us that way (padded to 128 columns)
+// and 48.7 us the other, 128 rows to bf16 51.6 and 45.5 us; 64 rows 38.6 and 47.5 us.
+constexpr int kFewRows = 64;
 constexpr int kTileRows = 128;                  // rows of a tile on that side
 constexpr int kBlockK = 128;                    // bytes of a row per stage: one scale block, one 128-byte swizzle row
 constexpr int kUmmaK = 32;                      // e4m3 elements per tcgen05.mma
 constexpr int kMaxStages = 12;
 constexpr int kScaleRing = 4;
-// Few rows: epilogue warps per lane quarter of tensor memory; they share its columns.
-__host__ __device__ constexpr int quarter_warps(int tn) { return tn >= 128 ? 4 : 2; }
-__host__ __device__ constexpr int matmul_threads(int tn) { return 32 * (3 + 4 * quarter_warps(tn)); }
-constexpr int kMatmulSmem = 216 * 1024;         // stages; the rest of an SM's 227 KB is the static arrays and alignment
+// Few rows: scale blocks that are loaded, multiplied and read back together.  A step of the thread that issues the MMAs costs
+// about 330 cycles for its waits and commits besides 60 for each MMA, and a block's share of the HBM bandwidth is 630:
+// 1 x 151,936 x 1,024 takes 38 us with one block per step, 29 us with four.
+__host__ __device__ constexpr int group_blocks(int tn) { return tn <= 32 ? 4 : 2; }
+constexpr int kFewEpilogueWarps = 8;            // two per lane quarter of tensor memory, half of its columns each
+constexpr int kFewThreads = 32 * (3 + kFewEpilogueWarps);
+constexpr int kMatmulSmem = 224 * 1024;         // stages; the rest of an SM's 227 KB is the static arrays
 
 // bits of the device status word
 constexpr uint32_t kTimeoutLoader = 1u, kTimeoutMma = 2u, kTimeoutScales = 4u, kTimeoutEpilogue = 8u;
@@ -254,19 +259,19 @@ __device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&v)[8])
 }
 
 template <int TN, typename Out>
-__global__ void __launch_bounds__(matmul_threads(TN), 1)
+__global__ void __launch_bounds__(kFewThreads, 1)
 tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_w_tail,
                       const __grid_constant__ CUtensorMap map_a, const MatmulParams p)
 {
-    constexpr int kBuffers = 4;                         // accumulators of TN columns
-    constexpr uint32_t kTmemCols = kBuffers * TN;       // 64 .. 512, a power of two
-    constexpr int kEpilogueWarps = 4 * quarter_warps(TN);
-    constexpr int kCols = TN / quarter_warps(TN);       // columns of an epilogue warp
-    constexpr uint32_t kStageBytes = kTileRows * 128u + TN * 128u;
+    constexpr int kGroup = group_blocks(TN);            // scale blocks that every role takes at a time
+    constexpr int kBuffers = 4;                         // sets of kGroup accumulators of TN columns
+    constexpr uint32_t kTmemCols = kBuffers * kGroup * TN;      // 256 or 512
+    constexpr int kEpilogueWarps = kFewEpilogueWarps, kCols = TN / 2;   // columns of an epilogue warp
+    constexpr uint32_t kBlockBytes = kTileRows * 128u + TN * 128u, kStageBytes = kGroup * kBlockBytes;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_acc_full[kBuffers], s_acc_empty[kBuffers];
     __shared__ __align__(8) uint64_t s_sc_full[kScaleRing], s_sc_empty[kScaleRing], s_drain;
-    __shared__ __align__(16) float s_scale[kScaleRing][TN];
+    __shared__ __align__(16) float s_scale[kScaleRing][kGroup][TN];
     __shared__ uint32_t s_tmem_base;
     __shared__ volatile uint32_t s_abort;
 
@@ -301,7 +306,7 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
                 // a short last tile is fetched with the short box: only its rows are read
                 const bool tail = valid < kTileRows && valid == p.tail_rows;
                 const uint32_t w_bytes = tail ? (uint32_t)p.tail_rows * 128u : kTileRows * 128u;
-                for (int32_t kb = 0; kb < p.kb; ++kb) {
+                for (int32_t kb = 0; kb < p.kb; kb += kGroup) {
                     if (!mbar_wait(smem_u32(&s_empty[stage]), phase ^ 1u, &s_abort)) {
                         atomicOr(&g_matmul_status, kTimeoutLoader);
                         s_abort = 1;
@@ -309,9 +314,12 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
                         break;
                     }
                     const uint32_t bar = smem_u32(&s_full[stage]), dst = smem_base + stage * kStageBytes;
-                    mbar_expect_tx(bar, w_bytes + TN * 128u);
-                    tma_load_2d(dst, tail ? &map_w_tail : &map_w, bar, kb * kBlockK, (int32_t)(r0 + (int64_t)t * kTileRows), hint_w);
-                    tma_load_2d(dst + kTileRows * 128u, &map_a, bar, kb * kBlockK, 0, hint_a);
+                    const int32_t blocks = min(kGroup, p.kb - kb);
+                    mbar_expect_tx(bar, (uint32_t)blocks * (w_bytes + TN * 128u));
+                    for (int32_t g = 0; g < blocks; ++g) {
+                        tma_load_2d(dst + g * kBlockBytes, tail ? &map_w_tail : &map_w, bar, (kb + g) * kBlockK, (int32_t)(r0 + (int64_t)t * kTileRows), hint_w);
+                        tma_load_2d(dst + g * kBlockBytes + kTileRows * 128u, &map_a, bar, (kb + g) * kBlockK, 0, hint_a);
+                    }
                     ++issued;
                     if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
                 }
@@ -329,7 +337,7 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
             uint32_t stage = 0, phase = 0, buf = 0, buf_phase = 0;
             bool ok = true;
             for (int32_t t = 0; ok && t < n_tiles; ++t) {
-                for (int32_t kb = 0; kb < p.kb; ++kb) {
+                for (int32_t kb = 0; kb < p.kb; kb += kGroup) {
                     if (!mbar_wait(smem_u32(&s_acc_empty[buf]), buf_phase ^ 1u, &s_abort) ||
                         !mbar_wait(smem_u32(&s_full[stage]), phase, &s_abort)) {
                         atomicOr(&g_matmul_status, kTimeoutMma);
@@ -338,11 +346,15 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
                         break;
                     }
                     tc_fence_after();
-                    const uint32_t w_addr = smem_base + stage * kStageBytes;
-                    const uint64_t w_desc = umma_desc_sw128(w_addr), a_desc = umma_desc_sw128(w_addr + kTileRows * 128u);
 #pragma unroll
-                    for (int k = 0; k < kBlockK / kUmmaK; ++k)      // 32 bytes further along the swizzled row: +2 in the address field
-                        umma_e4m3(tmem_base + buf * TN, w_desc + (uint64_t)(2 * k), a_desc + (uint64_t)(2 * k), idesc, k > 0 ? 1u : 0u);
+                    for (int g = 0; g < kGroup; ++g) {
+                        if (g > 0 && kb + g >= p.kb) break;
+                        const uint32_t w_addr = smem_base + stage * kStageBytes + g * kBlockBytes;
+                        const uint64_t w_desc = umma_desc_sw128(w_addr), a_desc = umma_desc_sw128(w_addr + kTileRows * 128u);
+#pragma unroll
+                        for (int k = 0; k < kBlockK / kUmmaK; ++k)  // 32 bytes further along the swizzled row: +2 in the address field
+                            umma_e4m3(tmem_base + (buf * kGroup + g) * TN, w_desc + (uint64_t)(2 * k), a_desc + (uint64_t)(2 * k), idesc, k > 0 ? 1u : 0u);
+                    }
                     umma_commit(smem_u32(&s_empty[stage]));
                     umma_commit(smem_u32(&s_acc_full[buf]));
                     if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
@@ -359,10 +371,14 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
         uint32_t st = 0, phase = 0;
         bool ok = true;
         for (int32_t t = 0; ok && t < n_tiles; ++t) {
-            for (int32_t kb = 0; kb < p.kb; ++kb) {
-                float v[(TN + 31) / 32];
+            for (int32_t kb = 0; kb < p.kb; kb += kGroup) {
+                constexpr int kPer = (TN + 31) / 32;
+                float v[kGroup][kPer];
 #pragma unroll
-                for (int c = 0; c < (TN + 31) / 32; ++c) v[c] = c * 32 + lane < p.M ? __ldg(p.a_scale + (int64_t)(c * 32 + lane) * p.kb + kb) : 0.f;
+                for (int g = 0; g < kGroup; ++g)
+#pragma unroll
+                    for (int c = 0; c < kPer; ++c)
+                        v[g][c] = c * 32 + lane < p.M && kb + g < p.kb ? __ldg(p.a_scale + (int64_t)(c * 32 + lane) * p.kb + kb + g) : 0.f;
                 ok = mbar_wait(smem_u32(&s_sc_empty[st]), phase ^ 1u, &s_abort);
                 if (!__all_sync(0xFFFFFFFFu, ok)) {
                     if (lane == 0) atomicOr(&g_matmul_status, kTimeoutScales);
@@ -371,8 +387,10 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
                     break;
                 }
 #pragma unroll
-                for (int c = 0; c < (TN + 31) / 32; ++c)
-                    if (c * 32 + lane < TN) s_scale[st][c * 32 + lane] = v[c];
+                for (int g = 0; g < kGroup; ++g)
+#pragma unroll
+                    for (int c = 0; c < kPer; ++c)
+                        if (c * 32 + lane < TN) s_scale[st][g][c * 32 + lane] = v[g][c];
                 mbar_arrive(smem_u32(&s_sc_full[st]));
                 if (++st == kScaleRing) { st = 0; phase ^= 1u; }
             }
@@ -382,7 +400,6 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
         const uint32_t quarter = (uint32_t)warp & 3u;               // tensor-memory lanes 32 * quarter .. + 31
         const int32_t c0 = ((warp - 3) >> 2) * kCols;               // this warp's columns
         const int32_t row_in_tile = (int32_t)(quarter * 32u) + lane;
-        constexpr int kChunk = kCols >= 32 ? 32 : kCols;
         uint32_t st = 0, phase = 0, buf = 0, buf_phase = 0;
         bool ok = true;
         for (int32_t t = 0; ok && t < n_tiles; ++t) {
@@ -392,10 +409,17 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
 #pragma unroll
             for (int j = 0; j < kCols / 2; ++j) acc[j] = make_float2(0.f, 0.f);
             const float *sb_row = p.b_scale + (row_in_tile < valid ? (n0 + row_in_tile) / 128 : n0 / 128) * p.kb;
-            float sb_next = __ldg(sb_row);
-            for (int32_t kb = 0; kb < p.kb; ++kb) {
-                const float2 sb = make_float2(sb_next, sb_next);
-                if (kb + 1 < p.kb) sb_next = __ldg(sb_row + kb + 1);
+            float sb_next[kGroup];                                  // loaded a group ahead
+            auto fetch = [&](int32_t kb) {
+#pragma unroll
+                for (int g = 0; g < kGroup; ++g) sb_next[g] = kb + g < p.kb ? __ldg(sb_row + kb + g) : 0.f;
+            };
+            fetch(0);
+            for (int32_t kb = 0; kb < p.kb; kb += kGroup) {
+                float sb[kGroup];
+#pragma unroll
+                for (int g = 0; g < kGroup; ++g) sb[g] = sb_next[g];
+                fetch(kb + kGroup);
                 ok = mbar_wait(smem_u32(&s_sc_full[st]), phase, &s_abort) && mbar_wait(smem_u32(&s_acc_full[buf]), buf_phase, &s_abort);
                 if (!__all_sync(0xFFFFFFFFu, ok)) {
                     if (lane == 0) atomicOr(&g_matmul_status, kTimeoutEpilogue);
@@ -404,23 +428,26 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
                     break;
                 }
                 tc_fence_after();
-                const uint32_t taddr = tmem_base + ((quarter * 32u) << 16) + buf * TN + (uint32_t)c0;
+                const uint32_t taddr = tmem_base + ((quarter * 32u) << 16) + buf * kGroup * TN + (uint32_t)c0;
+                uint32_t v[kGroup][kCols];                          // all of the group's reads under way together
 #pragma unroll
-                for (int c = 0; c < kCols; c += kChunk) {
-                    uint32_t v[kChunk];
-                    if constexpr (kChunk == 32) tmem_ld32(taddr + (uint32_t)c, v);
-                    else if constexpr (kChunk == 16) tmem_ld16(taddr + (uint32_t)c, v);
-                    else tmem_ld8(taddr + (uint32_t)c, v);
-                    tmem_ld_wait();
+                for (int g = 0; g < kGroup; ++g) {
+                    if (g > 0 && kb + g >= p.kb) break;
+                    if constexpr (kCols == 32) tmem_ld32(taddr + (uint32_t)(g * TN), v[g]);
+                    else if constexpr (kCols == 16) tmem_ld16(taddr + (uint32_t)(g * TN), v[g]);
+                    else tmem_ld8(taddr + (uint32_t)(g * TN), v[g]);
+                }
+                tmem_ld_wait();
 #pragma unroll
-                    for (int j = 0; j < kChunk; j += 4) {
-                        const float4 sa = *reinterpret_cast<const float4 *>(&s_scale[st][c0 + c + j]);
-                        float2 lo = make_float2(sa.x, sa.y), hi = make_float2(sa.z, sa.w);
-                        lo = __fmul2_rn(lo, sb);
-                        hi = __fmul2_rn(hi, sb);
-                        float2 &x = acc[(c + j) / 2], &y = acc[(c + j) / 2 + 1];
-                        x = __ffma2_rn(make_float2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), lo, x);
-                        y = __ffma2_rn(make_float2(__uint_as_float(v[j + 2]), __uint_as_float(v[j + 3])), hi, y);
+                for (int g = 0; g < kGroup; ++g) {
+                    if (g > 0 && kb + g >= p.kb) break;
+                    const float2 s2 = make_float2(sb[g], sb[g]);
+#pragma unroll
+                    for (int j = 0; j < kCols; j += 4) {
+                        const float4 sa = *reinterpret_cast<const float4 *>(&s_scale[st][g][c0 + j]);
+                        const float2 lo = __fmul2_rn(make_float2(sa.x, sa.y), s2), hi = __fmul2_rn(make_float2(sa.z, sa.w), s2);
+                        acc[j / 2] = __ffma2_rn(make_float2(__uint_as_float(v[g][j]), __uint_as_float(v[g][j + 1])), lo, acc[j / 2]);
+                        acc[j / 2 + 1] = __ffma2_rn(make_float2(__uint_as_float(v[g][j + 2]), __uint_as_float(v[g][j + 3])), hi, acc[j / 2 + 1]);
                     }
                 }
                 tc_fence_before();
@@ -726,12 +753,12 @@ bool make_map_fp8(CUtensorMap *map, const void *base, int64_t rows, int64_t cols
 template <int TN, typename Out>
 tfe_status launch_few(int grid, cudaStream_t stream, const CUtensorMap &w, const CUtensorMap &w_tail, const CUtensorMap &a, MatmulParams p)
 {
-    constexpr size_t stage = kTileRows * 128 + TN * 128;
+    constexpr size_t stage = (size_t)group_blocks(TN) * (kTileRows * 128 + TN * 128);
     p.stages = (int32_t)std::min<size_t>(kMaxStages, (kMatmulSmem - 1024) / stage);
     auto kernel = tfe_matmul_fp8_few_kernel<TN, Out>;
     const size_t smem = (size_t)p.stages * stage + 1024;
     if (tfe_status st = tfe_note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem), "product attribute")) return st;
-    kernel<<<grid, matmul_threads(TN), smem, stream>>>(w, w_tail, a, p);
+    kernel<<<grid, kFewThreads, smem, stream>>>(w, w_tail, a, p);
     return tfe_note_cuda(cudaGetLastError(), "product launch");
 }
 
@@ -817,7 +844,7 @@ tfe_status tfe_matmul_fp8(const void *a, int64_t lda, const float *a_scale, int3
     CUtensorMap map_w, map_a;
     if (M > kFewRows)
         return out_dtype == TFE_DTYPE_BF16 ? launch_many<__nv_bfloat16>(sms, stream, w, ldw, a, lda, K, p) : launch_many<float>(sms, stream, w, ldw, a, lda, K, p);
-    const int tn = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
+    const int tn = M <= 16 ? 16 : M <= 32 ? 32 : 64;
     p.rows_per_cta = (int32_t)((((int64_t)N + sms - 1) / sms + 7) / 8 * 8);
     p.tail_rows = p.rows_per_cta % kTileRows;
     const int grid = (int)(((int64_t)N + p.rows_per_cta - 1) / p.rows_per_cta);
@@ -828,8 +855,7 @@ tfe_status tfe_matmul_fp8(const void *a, int64_t lda, const float *a_scale, int3
     switch (tn) {
     case 16: return launch_few<16>(out_dtype, grid, stream, map_w, map_w_tail, map_a, p);
     case 32: return launch_few<32>(out_dtype, grid, stream, map_w, map_w_tail, map_a, p);
-    case 64: return launch_few<64>(out_dtype, grid, stream, map_w, map_w_tail, map_a, p);
-    default: return launch_few<128>(out_dtype, grid, stream, map_w, map_w_tail, map_a, p);
+    default: return launch_few<64>(out_dtype, grid, stream, map_w, map_w_tail, map_a, p);
     }
 }
 

@@ -511,13 +511,18 @@ tfe_sample_kernel(const SampleParams p)
         }
         __syncthreads();
         const int32_t k = p.top_k ? p.top_k[r] : 0;
-        const bool k_on = k > 0 && (uint32_t)k < s.count[kBins - 1];
+        // a k-th entry in the last bin restricts nothing: what is there weighs nothing (the range's end is below the unit of the
+        // masses, and masked logits are, unless the temperature is beyond any use)
+        const bool last_is_nothing = range == kRange || mass_of(q, s.table, kMasked) == 0;
+        const uint32_t countable = last_is_nothing ? s.count[kBins - 2] : s.count[kBins - 1];
+        const bool k_on = k > 0 && (uint32_t)k < s.count[kBins - 1] && ((uint32_t)k <= countable || !last_is_nothing);
         stage = k_on ? kTopK : next_stage(kTopK);
         uint32_t from_i[kSearches] = {0, 0, 0}, to_i[kSearches] = {0, 0, 0}, before_n[kSearches] = {0, 0, 0};
 
         // ---- bins [lo, hi) of every search
         uint32_t lo[kSearches] = {0, 0, 0}, hi[kSearches] = {0, 0, 0};
         float kept_m = s.estimate[kBins - 1], spare = 0.f;      // mass that is still in, and by how much it may be more
+        uint32_t behind = kBins;                                // no search ends behind the one before it
         bool whole = false;
         auto counted = [&](uint32_t b) { return b ? s.count[b - 1] : 0; };       // entries in the bins before b
         for (int st = stage;; st = next_stage(st)) {
@@ -525,12 +530,14 @@ tfe_sample_kernel(const SampleParams p)
                 const uint32_t b = first_of(kBins - 1, [&](uint32_t i) { return s.count[i] >= (uint32_t)k; });
                 const float m0 = b ? s.estimate[b - 1] : 0.f;
                 kept_m = m0 + (s.estimate[b] - m0) * ((float)((uint32_t)k - counted(b)) / (float)(s.count[b] - counted(b)));
-                lo[st] = b; hi[st] = b + 1;             // exact: counts
+                lo[st] = b; hi[st] = behind = b + 1;    // exact: counts
             } else {
                 const float share = share_of(st), slack = 2e-5f * s.estimate[kBins - 1];
                 const float least = share * kept_m - slack, most = share * (kept_m + spare) + slack;
                 lo[st] = first_of(kBins - 1, [&](uint32_t i) { return s.estimate[i] > least; });
-                hi[st] = first_of(kBins - 1, [&](uint32_t i) { return s.estimate[i] > most; }) + 1;
+                hi[st] = min(first_of(kBins - 1, [&](uint32_t i) { return s.estimate[i] > most; }) + 1, behind);
+                lo[st] = min(lo[st], hi[st] - 1);
+                behind = hi[st];
                 kept_m = share * kept_m;
                 spare = share * spare + __expf(-width * (float)lo[st]);      // the entry that reaches the goal is part
             }
@@ -784,7 +791,7 @@ extern "C" tfe_status tfe_sample_tokens(const void *logits, int32_t dtype, int32
     // masses sum to less than 2^63
     int bits = 0;
     while ((1ll << bits) < V) ++bits;
-    p.shift = std::min(46, 62 - bits);
+    p.shift = std::min(45, 62 - bits);                  // exp(-kRange) rounds to nothing
     // a slice stays in shared memory where that leaves every SM the blocks it would otherwise have
     const int64_t want = ((int64_t)V * es / 16 / p.blocks + 1) * (16 / es);
     const int64_t room = ((int64_t)B * p.blocks <= sms ? 226 : 112) * 1024 - (int64_t)sizeof(Shared);
