@@ -112,6 +112,7 @@ enum { kTopK = 0, kTopP = 1, kDraw = 2, kSearches = 3 };
 struct Command {                        // what the first block asks of its cluster
     int op;
     int by_bins;                        // kOpCollect: by the bins below, or by (key & mask) == prefix
+    int first;                          // by bins: the first collection of the row
     int sums;                           // by bins: 0 no masses, 1 those below the searches' bins, 2 of all entries too
     uint32_t lo[kSearches], hi[kSearches];      // by bins: places [lo, hi) of the searches (hi <= lo: none)
     int shift;                          // kOpDigits: histogram of (key >> shift) & 255
@@ -483,6 +484,70 @@ tfe_sample_kernel(const SampleParams p)
         return true;
     };
 
+    // The bins [lo, hi) in which the searches from `stage` on end, as many of them as the list has room for, and what to do.
+    auto plan = [&](bool first) {
+        uint32_t from_i[kSearches] = {0, 0, 0}, to_i[kSearches] = {0, 0, 0}, before_n[kSearches] = {0, 0, 0};
+        uint32_t lo[kSearches] = {0, 0, 0}, hi[kSearches] = {0, 0, 0};
+        // mass that is still in, and by how much it may be more
+        float kept_m = first ? s.estimate[kBins - 1] : (float)limit * exp2f((float)-p.shift), spare = 0.f;
+        uint32_t behind = kBins;                                // no search ends behind the one before it
+        bool whole = false;
+        auto counted = [&](uint32_t b) { return b ? s.count[b - 1] : 0; };       // entries in the bins before b
+        for (int st = stage;; st = next_stage(st)) {
+            if (st == kTopK) {
+                const uint32_t k = (uint32_t)p.top_k[r], b = first_of(kBins - 1, [&](uint32_t i) { return s.count[i] >= k; });
+                const float m0 = b ? s.estimate[b - 1] : 0.f;
+                kept_m = m0 + (s.estimate[b] - m0) * ((float)(k - counted(b)) / (float)(s.count[b] - counted(b)));
+                lo[st] = b; hi[st] = behind = b + 1;    // exact: counts
+            } else {
+                const float share = share_of(st), slack = 1e-5f * s.estimate[kBins - 1];
+                const float least = share * kept_m - slack, most = share * (kept_m + spare) + slack;
+                lo[st] = first_of(kBins - 1, [&](uint32_t i) { return s.estimate[i] > least; });
+                hi[st] = min(first_of(kBins - 1, [&](uint32_t i) { return s.estimate[i] > most; }) + 1, behind);
+                lo[st] = min(lo[st], hi[st] - 1);
+                behind = hi[st];
+                kept_m = share * kept_m;
+                spare = share * spare + __expf(-width * (float)lo[st]);      // the entry that reaches the goal is part
+            }
+            if (st == stage && st != kDraw && s.count[hi[st] - 1] <= (uint32_t)kList) {
+                whole = true;                           // a short prefix is collected whole
+                for (int t = 0; t < kSearches; ++t) { hi[t] = hi[st]; lo[t] = 0; }
+                for (int t = 0; t < kSearches; ++t) { from_i[t] = 0; to_i[t] = s.count[hi[st] - 1]; before_n[t] = 0; }
+                break;
+            }
+            if (st == kDraw) break;
+        }
+        bool too_many = false;
+        for (int last = kDraw; !whole; --last) {        // where each search's entries stand in the sorted list of all
+            uint32_t need = 0, end = 0;                 // bins before `end` are in the list, or above every search's
+#pragma unroll
+            for (int st = kDraw; st >= kTopK; --st) {
+                if (st > last) hi[st] = lo[st] = from_i[st] = to_i[st] = 0;      // no room: a later pass
+                if (hi[st] > lo[st]) {
+                    before_n[st] = counted(lo[st]);
+                    const uint32_t shared = lo[st] < end ? counted(min(end, hi[st])) - counted(lo[st]) : 0;
+                    const uint32_t beyond = lo[st] < end && end > hi[st] ? counted(end) - counted(hi[st]) : 0;
+                    from_i[st] = need - shared - beyond;
+                    to_i[st] = from_i[st] + counted(hi[st]) - counted(lo[st]);
+                    need = max(need, to_i[st]);
+                    end = max(end, hi[st]);
+                }
+            }
+            too_many = need > (uint32_t)kList;
+            if (!too_many || last <= stage) break;
+        }
+        __syncthreads();                                // the last plan and command have been read
+        if (tid == 0) {
+            s.too_many = too_many;
+            for (int st = 0; st < kSearches; ++st) { s.from_i[st] = from_i[st]; s.to_i[st] = to_i[st]; s.before_n[st] = before_n[st]; }
+            s.cmd.op = kOpCollect;
+            s.cmd.by_bins = 1;
+            s.cmd.first = first;
+            s.cmd.sums = !first || stage != kTopK ? 2 : whole ? 0 : 1;
+            for (int st = 0; st < kSearches; ++st) { s.cmd.lo[st] = 256 * lo[st]; s.cmd.hi[st] = too_many ? 0 : 256 * hi[st]; }
+        }
+    };
+
     if (leader) {
         // running counts, and running masses estimated from the bins' means
         uint32_t c[kBinsPerThread], c_sum = 0;
@@ -517,62 +582,7 @@ tfe_sample_kernel(const SampleParams p)
         const uint32_t countable = last_is_nothing ? s.count[kBins - 2] : s.count[kBins - 1];
         const bool k_on = k > 0 && (uint32_t)k < s.count[kBins - 1] && ((uint32_t)k <= countable || !last_is_nothing);
         stage = k_on ? kTopK : next_stage(kTopK);
-        uint32_t from_i[kSearches] = {0, 0, 0}, to_i[kSearches] = {0, 0, 0}, before_n[kSearches] = {0, 0, 0};
-
-        // ---- bins [lo, hi) of every search
-        uint32_t lo[kSearches] = {0, 0, 0}, hi[kSearches] = {0, 0, 0};
-        float kept_m = s.estimate[kBins - 1], spare = 0.f;      // mass that is still in, and by how much it may be more
-        uint32_t behind = kBins;                                // no search ends behind the one before it
-        bool whole = false;
-        auto counted = [&](uint32_t b) { return b ? s.count[b - 1] : 0; };       // entries in the bins before b
-        for (int st = stage;; st = next_stage(st)) {
-            if (st == kTopK) {
-                const uint32_t b = first_of(kBins - 1, [&](uint32_t i) { return s.count[i] >= (uint32_t)k; });
-                const float m0 = b ? s.estimate[b - 1] : 0.f;
-                kept_m = m0 + (s.estimate[b] - m0) * ((float)((uint32_t)k - counted(b)) / (float)(s.count[b] - counted(b)));
-                lo[st] = b; hi[st] = behind = b + 1;    // exact: counts
-            } else {
-                const float share = share_of(st), slack = 2e-5f * s.estimate[kBins - 1];
-                const float least = share * kept_m - slack, most = share * (kept_m + spare) + slack;
-                lo[st] = first_of(kBins - 1, [&](uint32_t i) { return s.estimate[i] > least; });
-                hi[st] = min(first_of(kBins - 1, [&](uint32_t i) { return s.estimate[i] > most; }) + 1, behind);
-                lo[st] = min(lo[st], hi[st] - 1);
-                behind = hi[st];
-                kept_m = share * kept_m;
-                spare = share * spare + __expf(-width * (float)lo[st]);      // the entry that reaches the goal is part
-            }
-            if (st == stage && st != kDraw && s.count[hi[st] - 1] <= (uint32_t)kList) {
-                whole = true;                           // a short prefix is collected whole
-                for (int t = 0; t < kSearches; ++t) { hi[t] = hi[st]; lo[t] = 0; }
-                for (int t = 0; t < kSearches; ++t) { from_i[t] = 0; to_i[t] = s.count[hi[st] - 1]; before_n[t] = 0; }
-                break;
-            }
-            if (st == kDraw) break;
-        }
-        uint32_t need = whole ? to_i[0] : 0;
-        if (!whole) {                                   // where each search's entries stand in the sorted list of all
-            uint32_t end = 0;                           // bins before `end` are in the list, or above every search's
-#pragma unroll
-            for (int st = kDraw; st >= kTopK; --st)
-                if (hi[st] > lo[st]) {
-                    before_n[st] = counted(lo[st]);
-                    const uint32_t shared = lo[st] < end ? counted(min(end, hi[st])) - counted(lo[st]) : 0;
-                    const uint32_t beyond = lo[st] < end && end > hi[st] ? counted(end) - counted(hi[st]) : 0;
-                    from_i[st] = need - shared - beyond;
-                    to_i[st] = from_i[st] + counted(hi[st]) - counted(lo[st]);
-                    need = max(need, to_i[st]);
-                    end = max(end, hi[st]);
-                }
-        }
-        const bool too_many = need > (uint32_t)kList;
-        if (tid == 0) {
-            s.too_many = too_many;
-            for (int st = 0; st < kSearches; ++st) { s.from_i[st] = from_i[st]; s.to_i[st] = to_i[st]; s.before_n[st] = before_n[st]; }
-            s.cmd.op = kOpCollect;
-            s.cmd.by_bins = 1;
-            s.cmd.sums = !k_on ? 2 : whole ? 0 : 1;
-            for (int st = 0; st < kSearches; ++st) { s.cmd.lo[st] = 256 * lo[st]; s.cmd.hi[st] = too_many ? 0 : 256 * hi[st]; }
-        }
+        plan(true);
     }
 
     for (;;) {
@@ -696,16 +706,20 @@ tfe_sample_kernel(const SampleParams p)
             for (int j = 0; j < kPerThread; ++j) s.run[tid * kPerThread + j] = own[j] + before;
             __syncthreads();
             u64 key = 0, mass = 1;
-            bool done = true;
+            bool done = true, later = false;
             if (cmd.by_bins) {
                 u64 below[kSearches] = {0, 0, 0};
                 if (cmd.sums)
                     for (int b = 0; b < p.blocks; ++b)
 #pragma unroll
                         for (int i = 0; i < kSearches; ++i) below[i] += cluster.map_shared_rank(s.below, b)[i];
-                if (stage != kTopK) limit = below[0];
+                if (cmd.first && stage != kTopK) limit = below[0];
                 done = !s.too_many;
                 while (done) {
+                    if (s.to_i[stage] == 0) {           // this search was left for another pass, and starts from an exact limit
+                        later = true;
+                        break;
+                    }
                     base_n = s.before_n[stage];
                     base_m = stage == kTopK ? below[0] : stage == kTopP ? below[1] : below[2];
                     done = find_entry(s.from_i[stage], min(s.to_i[stage], list_n), mass, key);
@@ -722,7 +736,9 @@ tfe_sample_kernel(const SampleParams p)
                     done = false;
                 }
             }
-            if (done) {
+            if (later) {
+                plan(false);
+            } else if (done) {
                 if (tid == 0) {
                     p.tokens[r] = key_index(key);
                     const float z = key_logit(key);

@@ -231,3 +231,17 @@ def test_empty_batch_and_refusals():
                      ((z, u), dict(top_k=u)), ((z, u), dict(temperature=u[:1])), ((z, u), dict(top_p=0.9 * u.double()))):
         with pytest.raises(ValueError):
             engine.sample_tokens(*args, **kw)
+
+
+@pytest.mark.parametrize("repeats", [300, 600, 1030])
+def test_values_that_many_entries_share(repeats):
+    """Every value held by 300, 600 or 1,030 entries: both searches' bins fit the list of 1,024 together, one after the other, or
+    not at all."""
+    rng = np.random.default_rng(repeats)
+    v, b = 150_000 // repeats * repeats, 10
+    values = np.linspace(-4, 4, v // repeats).astype(np.float32)
+    z = torch.from_numpy(np.stack([rng.permutation(np.repeat(values, repeats)) for _ in range(b)]))
+    u = rng.random(b).astype(np.float32)
+    check(z, u, p=np.full(b, 0.9))
+    check(z, u, p=np.full(b, 0.5), k=np.full(b, v // 2 + 17))
+    check(z, u, k=np.full(b, 20_000), T=np.full(b, 2.0))
