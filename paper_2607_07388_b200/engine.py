@@ -245,15 +245,16 @@ def _elsewhere(device: torch.device, stream):
                 yield
 
 
-_HERE = contextlib.nullcontext()
+# A decode step makes the calls below by the thousand: checks build their messages only when they fail, and the common case
+# of the current device and stream goes without a context.
 
 
-def _issue(device: torch.device, stream):
-    """Where a call is issued: nothing to change for the common case of the current device and stream."""
-    return _HERE if stream is None and device.index == torch.cuda.current_device() else _elsewhere(device, stream)
+def _here(device: torch.device, stream) -> bool:
+    return stream is None and device.index == torch.cuda.current_device()
 
 
-# The checks below build their messages only when they fail: a decode step makes these calls by the thousand.
+def _where(device: torch.device, stream) -> int:
+    return tfe.current_stream_address(device.index) if stream is None else tfe._stream(stream)
 
 
 def _row_matrix(t: torch.Tensor, what: str):
@@ -282,12 +283,20 @@ def _vector(t: torch.Tensor, shape, dtype, device, what: str) -> int:
 def quantize_fp8(x: torch.Tensor, block_rows: int = 1, *, stream=None):
     """(q float8_e4m3fn [R, C], scale float32): `x` [R, C] in 8 bits with a scale for every `block_rows` x 128 values -- 1
     for activations, 128 for weights (see tfe_quantize_fp8)."""
+    if not _here(x.device, stream):
+        with _elsewhere(x.device, stream):
+            return _quantize_fp8(x, block_rows, stream)
+    return _quantize_fp8(x, block_rows, None)
+
+
+def _quantize_fp8(x, block_rows, stream):
     r, c, ld, kind = _row_matrix(x, "x")
-    _require(block_rows in (1, 128), "block_rows: 1 or 128")
-    with _issue(x.device, stream):
-        q = torch.empty((r, c), dtype=torch.float8_e4m3fn, device=x.device)
-        scale = torch.empty((-(-r // block_rows), -(-c // 128)), dtype=torch.float32, device=x.device)
-        tfe.tfe_quantize_fp8(x.data_ptr(), kind, r, c, ld, block_rows, q.data_ptr(), scale.data_ptr(), stream)
+    if block_rows != 1 and block_rows != 128:
+        raise ValueError("block_rows: 1 or 128")
+    dev = x.device
+    q = torch.empty(r, c, dtype=torch.float8_e4m3fn, device=dev)
+    scale = torch.empty(-(-r // block_rows), -(-c // 128), dtype=torch.float32, device=dev)
+    tfe.tfe_quantize_fp8(x.data_ptr(), kind, r, c, ld, block_rows, q.data_ptr(), scale.data_ptr(), _where(dev, stream))
     return q, scale
 
 
@@ -307,20 +316,31 @@ def matmul_fp8(a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale:
                out_dtype: torch.dtype = torch.float32, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """a [M, K] times the transpose of w [N, K], both as quantize_fp8 makes them (block_rows 1 and 128): [M, N] in fp32 or
     bf16 (see tfe_matmul_fp8).  `out`: where it goes instead of a new tensor."""
+    if not _here(a.device, stream):
+        with _elsewhere(a.device, stream):
+            return _matmul_fp8(a, a_scale, w, w_scale, out_dtype, out, stream)
+    return _matmul_fp8(a, a_scale, w, w_scale, out_dtype, out, None)
+
+
+def _matmul_fp8(a, a_scale, w, w_scale, out_dtype, out, stream):
     m, k, lda = _fp8_matrix(a, "a")
     n, kw, ldw = _fp8_matrix(w, "w")
     dev = a.device
-    _require(n >= 1 and kw == k and w.device == dev, "w: the width and device of a are needed")
+    if n < 1 or kw != k or w.device != dev:
+        raise ValueError("w: the width and device of a are needed")
     kb = -(-k // 128)
     a_s = _vector(a_scale, (m, kb), torch.float32, dev, "a_scale")
     w_s = _vector(w_scale, (-(-n // 128), kb), torch.float32, dev, "w_scale")
-    with _issue(dev, stream):
-        if out is None:
-            _require(out_dtype in _ROW_DTYPES, "out_dtype: bfloat16 or float32")
-            out = torch.empty((m, n), dtype=out_dtype, device=dev)
+    if out is None:
+        if out_dtype not in _ROW_DTYPES:
+            raise ValueError("out_dtype: bfloat16 or float32")
+        out = torch.empty(m, n, dtype=out_dtype, device=dev)
+        ldo, kind = n, _ROW_DTYPES[out_dtype]
+    else:
         om, on, ldo, kind = _row_matrix(out, "out")
-        _require(om == m and on == n and out.device == dev, "out: [M, N] on the operands' device is needed")
-        tfe.tfe_matmul_fp8(a.data_ptr(), lda, a_s, m, w.data_ptr(), ldw, w_s, n, k, out.data_ptr(), kind, ldo, stream)
+        if om != m or on != n or out.device != dev:
+            raise ValueError("out: [M, N] on the operands' device is needed")
+    tfe.tfe_matmul_fp8(a.data_ptr(), lda, a_s, m, w.data_ptr(), ldw, w_s, n, k, out.data_ptr(), kind, ldo, _where(dev, stream))
     return out
 
 
@@ -336,15 +356,20 @@ class QuantizedHead:
     def logits(self, hidden: torch.Tensor, out_dtype: torch.dtype = torch.float32, out: torch.Tensor | None = None, *,
                stream=None) -> torch.Tensor:
         """[B, V] logits of `hidden` [B, d], whose rows are converted within the call."""
-        _require(hidden.dim() == 2 and hidden.shape[1] == self.d, f"hidden: [B, {self.d}] is needed")
-        with _issue(hidden.device, stream):
-            q, scale = quantize_fp8(hidden, block_rows=1)
-            return matmul_fp8(q, scale, self.w, self.w_scale, out_dtype=out_dtype, out=out)
+        if hidden.dim() != 2 or hidden.shape[1] != self.d:
+            raise ValueError(f"hidden: [B, {self.d}] is needed")
+        if not _here(hidden.device, stream):
+            with _elsewhere(hidden.device, stream):
+                return self.logits(hidden, out_dtype, out)
+        q, scale = quantize_fp8(hidden, 1)
+        return matmul_fp8(q, scale, self.w, self.w_scale, out_dtype=out_dtype, out=out)
 
     def sample(self, hidden: torch.Tensor, u: torch.Tensor, *, stream=None, **settings):
         """(token, prob) of one draw per row of `hidden` by `u` (see sample_tokens for the settings)."""
-        with _issue(hidden.device, stream):
-            return sample_tokens(self.logits(hidden), u, **settings)
+        if not _here(hidden.device, stream):
+            with _elsewhere(hidden.device, stream):
+                return self.sample(hidden, u, **settings)
+        return sample_tokens(self.logits(hidden), u, **settings)
 
 
 def sample_tokens(logits: torch.Tensor, u: torch.Tensor, *, temperature: torch.Tensor | None = None,
@@ -353,6 +378,13 @@ def sample_tokens(logits: torch.Tensor, u: torch.Tensor, *, temperature: torch.T
     """(token int32 [B], prob float32 [B]): one draw per row of `logits` [B, V] by the numbers `u` [B] in [0, 1), after
     temperature, min-p, top-k and top-p (see tfe_sample_tokens).  The settings are device tensors of B values
     (top_k int32, the others fp32) or None."""
+    if not _here(logits.device, stream):
+        with _elsewhere(logits.device, stream):
+            return _sample_tokens(logits, u, temperature, top_k, top_p, min_p, stream)
+    return _sample_tokens(logits, u, temperature, top_k, top_p, min_p, None)
+
+
+def _sample_tokens(logits, u, temperature, top_k, top_p, min_p, stream):
     b, v, ld, kind = _row_matrix(logits, "logits")
     dev = logits.device
     shape, f32 = (b,), torch.float32
@@ -361,11 +393,10 @@ def sample_tokens(logits: torch.Tensor, u: torch.Tensor, *, temperature: torch.T
     k = None if top_k is None else _vector(top_k, shape, torch.int32, dev, "top_k")
     p = None if top_p is None else _vector(top_p, shape, f32, dev, "top_p")
     m = None if min_p is None else _vector(min_p, shape, f32, dev, "min_p")
-    with _issue(dev, stream):
-        token = torch.empty(b, dtype=torch.int32, device=dev)
-        prob = torch.empty(b, dtype=f32, device=dev)
-        tfe.tfe_sample_tokens(logits.data_ptr(), kind, b, v, ld, ua, token.data_ptr(), prob.data_ptr(),
-                              temperature=t, top_k=k, top_p=p, min_p=m, stream=stream)
+    token = torch.empty(b, dtype=torch.int32, device=dev)
+    prob = u.new_empty(b)
+    tfe.tfe_sample_tokens(logits.data_ptr(), kind, b, v, ld, ua, token.data_ptr(), prob.data_ptr(),
+                          temperature=t, top_k=k, top_p=p, min_p=m, stream=_where(dev, stream))
     return token, prob
 
 
@@ -382,12 +413,17 @@ def distill_forward(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_log
                     stream=None):
     """(loss, lse), fp32 [N] each: the divergence from the teacher's top logits to the rows of `logits` [N, V] (see
     tfe_distill_forward), and the log-sum-exp of logits / tau that the gradient needs."""
+    if not _here(logits.device, stream):
+        with _elsewhere(logits.device, stream):
+            return _distill_forward(logits, teacher_ids, teacher_logits, tau, stream)
+    return _distill_forward(logits, teacher_ids, teacher_logits, tau, None)
+
+
+def _distill_forward(logits, teacher_ids, teacher_logits, tau, stream):
     rows = _teacher(logits, teacher_ids, teacher_logits)
     dev, n = logits.device, rows[2]
-    with _issue(dev, stream):
-        loss = torch.empty(n, dtype=torch.float32, device=dev)
-        lse = torch.empty(n, dtype=torch.float32, device=dev)
-        tfe.tfe_distill_forward(*rows, tau, loss.data_ptr(), lse.data_ptr(), stream)
+    loss, lse = teacher_logits.new_empty(n), teacher_logits.new_empty(n)
+    tfe.tfe_distill_forward(*rows, tau, loss.data_ptr(), lse.data_ptr(), _where(dev, stream))
     return loss, lse
 
 
@@ -396,17 +432,24 @@ def distill_backward(grad_loss: torch.Tensor, logits: torch.Tensor, teacher_ids:
                      out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """The gradient [N, V] of sum(grad_loss * loss) with respect to the logits.  `out`: where it goes, of the logits'
     shape and type; `out=logits` overwrites them."""
+    if not _here(logits.device, stream):
+        with _elsewhere(logits.device, stream):
+            return _distill_backward(grad_loss, logits, teacher_ids, teacher_logits, lse, tau, out, stream)
+    return _distill_backward(grad_loss, logits, teacher_ids, teacher_logits, lse, tau, out, None)
+
+
+def _distill_backward(grad_loss, logits, teacher_ids, teacher_logits, lse, tau, out, stream):
     rows = _teacher(logits, teacher_ids, teacher_logits)
-    dev, n, v = logits.device, rows[2], rows[3]
+    dev, kind, n, v = logits.device, rows[1], rows[2], rows[3]
     g = _vector(grad_loss, (n,), torch.float32, dev, "grad_loss")
     norm = _vector(lse, (n,), torch.float32, dev, "lse")
-    with _issue(dev, stream):
-        if out is None:
-            out = torch.empty((n, v), dtype=logits.dtype, device=dev)
-        on, ov, ld_out, kind = _row_matrix(out, "out")
-        _require(on == n and ov == v and kind == rows[1] and out.device == dev,
-                 "out: the logits' shape, type and device are needed")
-        tfe.tfe_distill_backward(*rows, tau, norm, g, out.data_ptr(), ld_out, stream)
+    if out is None:
+        out, ld_out = logits.new_empty(n, v), v
+    else:
+        on, ov, ld_out, out_kind = _row_matrix(out, "out")
+        if on != n or ov != v or out_kind != kind or out.device != dev:
+            raise ValueError("out: the logits' shape, type and device are needed")
+    tfe.tfe_distill_backward(*rows, tau, norm, g, out.data_ptr(), ld_out, _where(dev, stream))
     return out
 
 
