@@ -197,6 +197,7 @@ template <typename T, bool kWarpRows>
 __global__ void __launch_bounds__(kWarpRows ? kSmallBlock : kBlock, kWarpRows ? 4 : 3)
 tfe_distill_forward_kernel(const DistillParams p)
 {
+    tfe_wait_for_stream();
     const float c = (float)(kLog2e / (double)p.tau);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if constexpr (kWarpRows) {
@@ -346,6 +347,7 @@ template <typename T, bool kWarpRows>
 __global__ void __launch_bounds__(kWarpRows ? kSmallBlock : kBlock)
 tfe_distill_backward_kernel(const DistillParams p)
 {
+    tfe_wait_for_stream();
     extern __shared__ float s_raw[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int per_row = 3 * p.K + 2;
@@ -385,14 +387,7 @@ int32_t slices_for(int32_t N, int64_t row_bytes, int sms)
 template <typename F>
 tfe_status launch_rows(F kernel, int grid, int block, int cluster, size_t smem, cudaStream_t stream, const DistillParams &p)
 {
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)cluster;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)grid); cfg.blockDim = dim3((unsigned)block); cfg.dynamicSmemBytes = smem; cfg.stream = stream;
-    cfg.attrs = attr; cfg.numAttrs = cluster > 1 ? 1 : 0;
-    return tfe_note_cuda(cudaLaunchKernelEx(&cfg, kernel, p), "distillation launch");
+    return tfe_launch_serial(kernel, (unsigned)grid, (unsigned)block, (unsigned)cluster, smem, stream, "distillation launch", p);
 }
 
 tfe_status device_sms(int *sms)

@@ -146,6 +146,7 @@ template <typename T, bool kVector>
 __global__ void __launch_bounds__(kQuantThreads)
 tfe_quantize_rows_kernel(const QuantParams p)
 {
+    tfe_wait_for_stream();
     const int l = threadIdx.x & (kGroupLanes - 1);
     const uint32_t groups = (uint32_t)p.R * (uint32_t)p.kb;
     const uint32_t g = (blockIdx.x * kQuantThreads + threadIdx.x) / kGroupLanes;
@@ -169,6 +170,7 @@ tfe_quantize_blocks_kernel(const QuantParams p)
 {
     constexpr int kRowsAtOnce = kQuantThreads / kGroupLanes, kTurns = 128 / kRowsAtOnce;
     __shared__ uint32_t s_max[kQuantThreads / 32];
+    tfe_wait_for_stream();
     const int l = threadIdx.x & (kGroupLanes - 1), hw = threadIdx.x / kGroupLanes;
     const uint32_t rb = blockIdx.x / (uint32_t)p.kb, b = blockIdx.x - rb * (uint32_t)p.kb;
     const int64_t row0 = (int64_t)rb * 128 + hw;
@@ -290,6 +292,7 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = s_tmem_base;
+    tfe_wait_for_stream();
     // this CTA's weight rows, and its tiles of them
     const int64_t r0 = (int64_t)blockIdx.x * p.rows_per_cta;
     const int32_t n_rows = (int32_t)min((int64_t)p.rows_per_cta, p.N - r0), n_tiles = (n_rows + kTileRows - 1) / kTileRows;
@@ -590,6 +593,7 @@ tfe_matmul_fp8_many_kernel(const __grid_constant__ CUtensorMap map_w, const __gr
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = s_tmem_base;
+    tfe_wait_for_stream();
 
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kManyFewRegs));
@@ -758,8 +762,7 @@ tfe_status launch_few(int grid, cudaStream_t stream, const CUtensorMap &w, const
     auto kernel = tfe_matmul_fp8_few_kernel<TN, Out>;
     const size_t smem = (size_t)p.stages * stage + 1024;
     if (tfe_status st = tfe_note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem), "product attribute")) return st;
-    kernel<<<grid, kFewThreads, smem, stream>>>(w, w_tail, a, p);
-    return tfe_note_cuda(cudaGetLastError(), "product launch");
+    return tfe_launch_serial(kernel, (unsigned)grid, kFewThreads, 1, smem, stream, "product launch", w, w_tail, a, p);
 }
 
 template <int TN>
@@ -783,8 +786,7 @@ tfe_status launch_many(int sms, cudaStream_t stream, const void *w, int64_t ldw,
     CUtensorMap map_w, map_a;
     if (!make_map_fp8(&map_w, w, p.N, K, ldw, kManyN) || !make_map_fp8(&map_a, a, p.M, K, lda, kTileRows))
         return tfe_note_cuda(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
-    kernel<<<(unsigned)std::min<int64_t>(sms, p.n_units), kManyThreads, kManySmem, stream>>>(map_w, map_a, p);
-    return tfe_note_cuda(cudaGetLastError(), "product launch");
+    return tfe_launch_serial(kernel, (unsigned)std::min<int64_t>(sms, p.n_units), kManyThreads, 1, kManySmem, stream, "product launch", map_w, map_a, p);
 }
 
 bool aligned(const void *ptr, uintptr_t to) { return ptr && reinterpret_cast<uintptr_t>(ptr) % to == 0; }
@@ -811,17 +813,13 @@ tfe_status tfe_quantize_fp8(const void *x, int32_t dtype, int32_t R, int32_t C, 
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     const unsigned grid = block_rows == 1 ? (unsigned)((groups * kGroupLanes + kQuantThreads - 1) / kQuantThreads) : (unsigned)groups;
     auto go = [&](auto rows_kernel, auto blocks_kernel) {
-        if (block_rows == 1) rows_kernel<<<grid, kQuantThreads, 0, stream>>>(p);
-        else blocks_kernel<<<grid, kQuantThreads, 0, stream>>>(p);
+        return tfe_launch_serial(block_rows == 1 ? rows_kernel : blocks_kernel, grid, kQuantThreads, 1, 0, stream, "conversion launch", p);
     };
-    if (dtype == TFE_DTYPE_BF16) {
-        if (vec) go(tfe_quantize_rows_kernel<__nv_bfloat16, true>, tfe_quantize_blocks_kernel<__nv_bfloat16, true>);
-        else go(tfe_quantize_rows_kernel<__nv_bfloat16, false>, tfe_quantize_blocks_kernel<__nv_bfloat16, false>);
-    } else {
-        if (vec) go(tfe_quantize_rows_kernel<float, true>, tfe_quantize_blocks_kernel<float, true>);
-        else go(tfe_quantize_rows_kernel<float, false>, tfe_quantize_blocks_kernel<float, false>);
-    }
-    return tfe_note_cuda(cudaGetLastError(), "conversion launch");
+    if (dtype == TFE_DTYPE_BF16)
+        return vec ? go(tfe_quantize_rows_kernel<__nv_bfloat16, true>, tfe_quantize_blocks_kernel<__nv_bfloat16, true>)
+                   : go(tfe_quantize_rows_kernel<__nv_bfloat16, false>, tfe_quantize_blocks_kernel<__nv_bfloat16, false>);
+    return vec ? go(tfe_quantize_rows_kernel<float, true>, tfe_quantize_blocks_kernel<float, true>)
+               : go(tfe_quantize_rows_kernel<float, false>, tfe_quantize_blocks_kernel<float, false>);
 }
 
 tfe_status tfe_matmul_fp8(const void *a, int64_t lda, const float *a_scale, int32_t M, const void *w, int64_t ldw, const float *w_scale, int32_t N,

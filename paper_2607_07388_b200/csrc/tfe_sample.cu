@@ -268,6 +268,7 @@ template <typename T>
 __global__ void __launch_bounds__(kThreads, 2)
 tfe_sample_kernel(const SampleParams p)
 {
+    tfe_wait_for_stream();
     extern __shared__ __align__(16) uint8_t smem[];
     Shared &s = *reinterpret_cast<Shared *>(smem);
     T *slice = reinterpret_cast<T *>(smem + sizeof(Shared));
@@ -815,13 +816,5 @@ extern "C" tfe_status tfe_sample_tokens(const void *logits, int32_t dtype, int32
     const size_t smem = sizeof(Shared) + (size_t)p.slice_cap * es;
     auto kernel = dtype == TFE_DTYPE_BF16 ? tfe_sample_kernel<__nv_bfloat16> : tfe_sample_kernel<float>;
     if (tfe_status st = tfe_note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024), "sampling attribute")) return st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)p.blocks;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)B * (unsigned)p.blocks); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = smem;
-    cfg.stream = static_cast<cudaStream_t>(stream_);
-    cfg.attrs = attr; cfg.numAttrs = 1;
-    return tfe_note_cuda(cudaLaunchKernelEx(&cfg, kernel, p), "sampling launch");
+    return tfe_launch_serial(kernel, (unsigned)B * (unsigned)p.blocks, kThreads, (unsigned)p.blocks, smem, static_cast<cudaStream_t>(stream_), "sampling launch", p);
 }
