@@ -733,9 +733,11 @@ tfe_sample_kernel(const SampleParams p)
                         for (int i = 0; i < kSearches; ++i) below[i] += cluster.map_shared_rank(s.below, b)[i];
                 if (cmd.first && stage != kTopK) limit = below[0];
                 done = !s.too_many;
+                const int planned = stage;
                 while (done) {
-                    if (s.to_i[stage] == 0) {           // this search was left for another pass, and starts from an exact limit
-                        later = true;
+                    if (s.to_i[stage] == 0) {           // this search was left for another pass, and starts from an exact limit;
+                        later = stage != planned;       // or the estimate named empty bins: by digits (every pass ends a search)
+                        done = later;
                         break;
                     }
                     base_n = s.before_n[stage];

@@ -245,3 +245,32 @@ def test_values_that_many_entries_share(repeats):
     check(z, u, p=np.full(b, 0.9))
     check(z, u, p=np.full(b, 0.5), k=np.full(b, v // 2 + 17))
     check(z, u, k=np.full(b, 20_000), T=np.full(b, 2.0))
+
+
+def bins_that_round_up():
+    """A row whose estimated mass is 1.4e-5 too low.  With a least weight of exp(-32), 256 * 4,094 / 32 places make a unit of logit:
+    nearly all entries lie half a place (0.51) beyond a whole one, and count as half a place further.  The last two filled bins
+    hold 1,000 entries each, too many for one list."""
+    unit = np.float32(256 * 4094 / 32)
+    at = lambda place, n: np.full(n, -np.float32((place + 0.51) / unit), np.float32)
+    body = [at(256 * b + 128, 1000) for b in (10, 11, 12, 13, 14)]
+    total = sum(float(np.exp(x.astype(np.float64)).sum()) for x in body) + 1
+    far = int(-math.log(total * 1.19e-5 / 1000) * float(unit)) // 256     # the bin in which 1,000 entries weigh 1.19e-5 of the row
+    return np.concatenate([[np.float32(0)], *body, at(256 * (far - 1) + 128, 1000), at(256 * far + 128, 1000), [np.float32(-32)]]).astype(np.float32)
+
+
+def test_an_estimate_that_ends_too_early():
+    """The draw, searched for in a pass of its own from the exact mass, is to end behind all that the estimates say there is: the
+    bins named for it are empty, and the row goes on by digits."""
+    z = bins_that_round_up()
+    unit = np.float32(256 * 4094 / 32)
+    place = np.rint((-z * unit).astype(np.float32)).astype(np.int64)
+    low = np.exp(-place.astype(np.float64) / float(unit)).sum() / np.exp(z.astype(np.float64)).sum()
+    assert 1 - 1.53e-5 < low < 1 - 1.3e-5 and np.bincount(place >> 8).max() == 1000
+    rng = np.random.default_rng(4)
+    rows = 6
+    zs = torch.from_numpy(np.stack([z] + [rng.permutation(z) for _ in range(rows - 1)]))
+    u = np.array([1 - 2.0 ** -19, 1 - 2.0 ** -19, 1 - 2.0 ** -20, 1 - 2.0 ** -18, 1 - 2.0 ** -24, 0.5])
+    check(zs, u, p=np.array([1 - 2.0 ** -20] * 5 + [0.99]))
+    check(zs, u)
+    check(zs, u, k=np.array([len(z) - 1] * rows), p=np.array([1 - 2.0 ** -20] * rows))
