@@ -498,9 +498,10 @@ tfe_status tfe_assign_residency(const uint32_t *count, int64_t N, int64_t gpu_sl
  * row r starting `ld` elements after row r - 1 (ld >= V, at most 2^34; rows need no alignment beyond the
  * element's own), as fp32 or bf16.  They come from a head (tfe_head_buffers, tfe_matmul_fp8) or from the model
  * itself.  A logit at or below -1e30 is a masked one: -inf, or the lowest value of either type.
- * These calls keep no state, allocate nothing, never synchronise and may be captured into a CUDA graph; they
+ * These calls keep no state (but tfe_matmul_fp8's status word), allocate nothing, never synchronise and may be captured into a CUDA graph; they
  * work on the current device, which has to be the one that holds the buffers.  Calls on different streams are
- * independent.  Argument errors are found on the host before anything is launched.
+ * independent.  Argument errors are found on the host before anything is launched.  Results must not touch
+ * operands unless a call says that they may.
  */
 enum { TFE_DTYPE_BF16 = 0, TFE_DTYPE_F32 = 1 };
 #define TFE_ROWS_MAX (1 << 27)
@@ -521,7 +522,7 @@ enum { TFE_DTYPE_BF16 = 0, TFE_DTYPE_F32 = 1 };
  *   [ceil(N / 128)][kb], kb = ceil(K / 128);  out DEVICE [M][ldo], fp32 or bf16.  0 <= M, 1 <= N <= TFE_ROWS_MAX,
  *   1 <= K <= TFE_FP8_MAX_COLS; a and w 16-byte aligned, lda and ldw multiples of 16.  A block's products are
  *   summed by the tensor cores, blocks in fp32, and the result is rounded once.  Elements of out beyond N stay as
- *   they were.  out must not touch the operands.  One launch.
+ *   they were.  One launch.
  *
  * tfe_matmul_fp8_status -- synchronises `stream` and reads the library's status word on the current device: 0, or
  * bits set by waits inside the kernel that ran out (1 loader, 2 MMA issuer, 4 scales, 8 epilogue); then INTERNAL.

@@ -340,6 +340,10 @@ def _matmul_fp8(a, a_scale, w, w_scale, out_dtype, out, stream):
         om, on, ldo, kind = _row_matrix(out, "out")
         if om != m or on != n or out.device != dev:
             raise ValueError("out: [M, N] on the operands' device is needed")
+        at, end = out.data_ptr(), out.data_ptr() + ((m - 1) * ldo + n) * out.element_size()
+        for t, rows, ld in ((a, m, lda), (w, n, ldw)):
+            if m and at < t.data_ptr() + (rows - 1) * ld + k and t.data_ptr() < end:
+                raise ValueError("out: must not touch the operands")
     tfe.tfe_matmul_fp8(a.data_ptr(), lda, a_s, m, w.data_ptr(), ldw, w_s, n, k, out.data_ptr(), kind, ldo, _where(dev, stream))
     return out
 

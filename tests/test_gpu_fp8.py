@@ -264,3 +264,21 @@ def test_conversion_next_to_the_rounding_borders(kind):
     bits, _, s = quantize64(xt.float().numpy(), 1)
     assert np.array_equal(scale.cpu().numpy(), s)
     assert np.array_equal(q.view(torch.uint8).cpu().numpy() & 0x7F, bits)
+
+
+def test_output_on_its_operands_is_refused():
+    """`out` over the bytes of an operand: refused.  Beside it in the same storage: taken."""
+    from paper_2607_07388_b200 import engine
+    a, sa, w, sw = (x.to(DEV) for x in operands(2, 4, 128, 256))
+    room = torch.zeros(4 * 256 + 4 * 128 * 4, dtype=torch.uint8, device=DEV)
+    inside = room[: 4 * 256].view(4, 256).view(torch.float8_e4m3fn)
+    inside.copy_(a)
+    at = lambda first: room[first: first + 4 * 128 * 2].view(torch.bfloat16).view(4, 128)
+    for first in (0, 1008):
+        with pytest.raises(ValueError):
+            engine.matmul_fp8(inside, sa, w, sw, out=at(first))
+    over_w = w.reshape(-1).view(torch.uint8)[-1024:].view(torch.bfloat16).view(4, 128)
+    with pytest.raises(ValueError):
+        engine.matmul_fp8(a, sa, w, sw, out=over_w)
+    want = engine.matmul_fp8(a, sa, w, sw, out_dtype=torch.bfloat16)
+    assert torch.equal(engine.matmul_fp8(inside, sa, w, sw, out=at(1024)), want)
