@@ -121,6 +121,7 @@ struct Command {                        // what the first block asks of its clus
     uint32_t lo[kSearches], hi[kSearches];      // by bins: places [lo, hi) of the searches (hi <= lo: none)
     int shift;                          // kOpDigits: histogram of (key >> shift) & 255
     u64 prefix, mask;                   // only entries with (key & mask) == prefix
+    u64 each;                           // kOpDigits: the mass of every one of them, if they are equal logits; otherwise 0
 };
 
 struct alignas(16) Shared {
@@ -145,7 +146,9 @@ struct alignas(16) Shared {
     int found_at;
     uint32_t from_i[kSearches], to_i[kSearches], before_n[kSearches];   // of each search: its entries in the sorted list, those before
     bool too_many;                      // for the list: the bins are not collected
+    int small;                          // bf16: a kept logit is too small for the bins by value
 };
+static_assert(offsetof(Shared, offset) == offsetof(Shared, count) + sizeof(uint32_t) * kBins, "one array of 2 kBins for the bins by value");
 static_assert(offsetof(Shared, count) % 16 == 0 && offsetof(Shared, offset) % 16 == 0 && sizeof(Shared) % 16 == 0, "16-byte accesses");
 
 // Inclusive sums over the block in thread order.  All threads call it; the scratch is free again on return.
@@ -372,7 +375,7 @@ tfe_sample_kernel(const SampleParams p)
             top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
             low = fminf(low, __shfl_xor_sync(0xFFFFFFFFu, low, o));
         }
-        if (lane == 0) { s.top = top; s.low = low; s.first = 0x7FFFFFFF; }
+        if (lane == 0) { s.top = top; s.low = low; s.first = 0x7FFFFFFF; s.small = 0; }
     }
     cluster.sync();
     top = -INFINITY;
@@ -429,25 +432,59 @@ tfe_sample_kernel(const SampleParams p)
     if (!(inv_t > 0.f)) q.bins = 0.f;                                       // T infinite: all in the first bin
     const uint4 *src = resident ? keep : from;
 
-    // ---- counts by bin; the last one, where masked logits and all weights of a cold row beyond the range meet, in registers
-    uint32_t in_last = 0;
-    sweep(src, [&](const float (&f)[4], int32_t) {
+    // ---- bf16: counts by value.  A bin holds one value -- 31 binades of either sign, 128 values each, and zero -- so that the
+    // masses of the bins, and with them every search's end, are exact without weighing the entries one by one.  Rows with a kept
+    // logit below those binades but zero (of 152,000 normal ones one row in a thousand) take the bins by distance.  Logits at
+    // which nothing of a weight is left are not counted: they end no search but one by count, whose mass they do not change.
+    bool by_value = sizeof(T) == 2 && q.topf < INFINITY;
+    const float least = fmaxf(fmaxf(q.cut, q.floor), q.floor > kMasked ? low : -INFINITY);
+    const int below_binades = max(0, (int)max(__float_as_uint(top) << 1 >> 24, __float_as_uint(least) << 1 >> 24) - 30) << 7;
+    uint32_t *by_values = reinterpret_cast<uint32_t *>(smem + offsetof(Shared, count));      // 2 kBins, `count` and `offset`
+    auto value_at = [&](uint32_t at) {                  // of a bin; bins in descending order
+        const uint32_t h = at < (uint32_t)kBins ? kBins - 1 - at : at - kBins;
+        return h == 0 ? 0.f : __uint_as_float((h - 128 + below_binades) << 16 | (at < (uint32_t)kBins ? 0u : 0x80000000u));
+    };
+    if (by_value) {
+        bool small = false;
+        sweep(src, [&](const float (&f)[4], int32_t) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const uint32_t place = place_of(q, f[e]);
-            if (f[e] >= q.cut) {
-                if (place < 256u * (kBins - 1)) {
-                    atomicAdd(&s.count[place >> 8], 1u);
-                    atomicAdd(&s.offset[place >> 8], place & 255u);
-                } else {
-                    ++in_last;
+            for (int e = 0; e < 4; ++e) {
+                const int mag = (int)(__float_as_uint(f[e]) << 1 >> 17), above = mag - below_binades;
+                const bool kept = f[e] >= least, tiny = above < 0 || mag == 0;
+                const int h = tiny ? 0 : min(above + 128, kBins - 1);
+                small = small || (kept && tiny && mag != 0);
+                if (kept) atomicAdd(&by_values[f[e] < 0.f ? kBins + h : kBins - 1 - h], 1u);
+            }
+        });
+        if (small) s.small = 1;
+        cluster.sync();
+        for (int b = 0; b < p.blocks; ++b) by_value = by_value && *cluster.map_shared_rank(&s.small, b) == 0;
+        if (!by_value)
+            for (int i = tid; i < kBins; i += kThreads) { s.count[i] = 0; s.offset[i] = 0; }
+        __syncthreads();
+    }
+
+    // ---- counts by bin; the last one, where masked logits and all weights of a cold row beyond the range meet, in registers
+    if (!by_value) {
+        uint32_t in_last = 0;
+        sweep(src, [&](const float (&f)[4], int32_t) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t place = place_of(q, f[e]);
+                if (f[e] >= q.cut) {
+                    if (place < 256u * (kBins - 1)) {
+                        atomicAdd(&s.count[place >> 8], 1u);
+                        atomicAdd(&s.offset[place >> 8], place & 255u);
+                    } else {
+                        ++in_last;
+                    }
                 }
             }
-        }
-    });
-    in_last = __reduce_add_sync(0xFFFFFFFFu, in_last);
-    if (lane == 0 && in_last) atomicAdd(&s.count[kBins - 1], in_last);
-    cluster.sync();
+        });
+        in_last = __reduce_add_sync(0xFFFFFFFFu, in_last);
+        if (lane == 0 && in_last) atomicAdd(&s.count[kBins - 1], in_last);
+        cluster.sync();
+    }
     if (p.blocks > 1) {                 // every block adds up its share of the bins
         const int share = kBins / p.blocks;
         for (int i = tid; i < share; i += kThreads) {
@@ -486,8 +523,8 @@ tfe_sample_kernel(const SampleParams p)
         return g;
     };
     auto next_stage = [&](int st) { return st == kTopK && p.top_p && p.top_p[r] < 1.f ? (int)kTopP : (int)kDraw; };
-    auto digits = [&](int shift, u64 prefix, u64 mask) {
-        if (tid == 0) { s.cmd.op = kOpDigits; s.cmd.shift = shift; s.cmd.prefix = prefix; s.cmd.mask = mask; }
+    auto digits = [&](int shift, u64 prefix, u64 mask, u64 each) {
+        if (tid == 0) { s.cmd.op = kOpDigits; s.cmd.shift = shift; s.cmd.prefix = prefix; s.cmd.mask = mask; s.cmd.each = each; }
     };
     // The entry at which the goal of `stage` is met, among list entries [i0, i1) with base_n entries of mass base_m before
     // them.  False if it is not among them.
@@ -566,7 +603,74 @@ tfe_sample_kernel(const SampleParams p)
         }
     };
 
-    if (leader) {
+    if (leader && by_value) {
+        const uint32_t *counts = by_values + tid * 2 * kBinsPerThread;
+        uint32_t c_sum = 0;
+        u64 m_sum = 0;
+#pragma unroll 1
+        for (int j = 0; j < 2 * kBinsPerThread; ++j)
+            if (const uint32_t n = counts[j]) {
+                c_sum += n;
+                m_sum += n * mass_of(q, s.table, value_at(tid * 2 * kBinsPerThread + j));
+            }
+        const uint32_t c_run = block_scan(s.warp32, c_sum);
+        const u64 m_run = block_scan(s.warp64[0], m_sum);
+        if (tid == kThreads - 1) { s.found_count = c_run; s.found_mass = m_run; }
+        __syncthreads();
+        const int32_t k = p.top_k ? p.top_k[r] : 0;
+        stage = k > 0 && (uint32_t)k < s.found_count ? kTopK : next_stage(kTopK);
+        limit = s.found_mass;
+        int at;
+        uint32_t n;
+        for (;;) {                                      // at most three searches
+            __syncthreads();
+            if (tid == 0) s.found_at = -1;
+            __syncthreads();
+            const Goal g = goal_of(stage);
+            uint32_t n0 = c_run - c_sum;
+            u64 m0 = m_run - m_sum;
+            if (c_sum && g.met(c_run, m_run) && (n0 == 0 || !g.met(n0, m0))) {
+                for (int j = 0; j < 2 * kBinsPerThread; ++j) {
+                    const uint32_t here = counts[j];
+                    if (!here) continue;
+                    const u64 each = mass_of(q, s.table, value_at(tid * 2 * kBinsPerThread + j));
+                    if (g.met(n0 + here, m0 + here * each)) {
+                        const uint32_t i = first_of(here - 1, [&](uint32_t x) { return g.met(n0 + x + 1, m0 + (x + 1) * each); });
+                        s.found_at = tid * 2 * kBinsPerThread + j;
+                        s.found_count = here;
+                        s.found_mass = m0 + (i + 1) * each;
+                        s.found_key = m0;
+                        s.before_n[0] = n0;
+                        break;
+                    }
+                    n0 += here;
+                    m0 += here * each;
+                }
+            }
+            __syncthreads();
+            at = s.found_at;
+            n = s.found_count;
+            if (at < 0 || stage == kDraw) break;
+            limit = s.found_mass;
+            stage = next_stage(stage);
+        }
+        if (at < 0) {
+            digits(56, 0, 0, 0);
+        } else {                                        // the drawn value is known: which of its entries, in index order
+            base_n = s.before_n[0];
+            base_m = s.found_key;
+            const float z = value_at(at);
+            int bits = 8;                               // of an index
+            while (bits < 32 && (p.V - 1) >> bits) ++bits;
+            const u64 prefix = entry_key(z, 0) & 0xFFFFFFFF00000000ull;
+            if (n <= (uint32_t)kList) {
+                if (tid == 0) { s.cmd.op = kOpCollect; s.cmd.by_bins = 0; s.cmd.prefix = prefix; s.cmd.mask = 0xFFFFFFFF00000000ull; }
+            } else {                                    // the bits that all indexes have alike are ones in a key
+                const u64 alike = 0xFFFFFFFFull >> bits << bits;
+                digits(bits - 8, prefix | alike, 0xFFFFFFFF00000000ull | alike, mass_of(q, s.table, z));
+            }
+        }
+    } else if (leader) {
         // running counts, and running masses estimated from the bins' means
         uint32_t c[kBinsPerThread], c_sum = 0;
         float m[kBinsPerThread], m_sum = 0.f;
@@ -614,8 +718,13 @@ tfe_sample_kernel(const SampleParams p)
             const uint32_t at = atomicAdd(&s.fill, 1u);
             if (at < (uint32_t)kList) s.list[at] = key;
         };
+        // where the prefix names a logit, four entries at a time are passed over if none has it
+        const bool one_value = cmd.mask >> 32 == 0xFFFFFFFFu;
+        const float value = key_logit(cmd.prefix);
+        auto none = [&](const float (&f)[4]) { return one_value && f[0] != value && f[1] != value && f[2] != value && f[3] != value; };
         if (cmd.op == kOpDigits) {
             sweep(src, [&](const float (&f)[4], int32_t at) {
+                if (none(f)) return;
 #pragma unroll 1
                 for (int e = 0; e < 4; ++e) {
                     if (!(f[e] >= q.cut)) continue;
@@ -623,11 +732,12 @@ tfe_sample_kernel(const SampleParams p)
                     if ((key & cmd.mask) != cmd.prefix) continue;
                     const int d = (int)((key >> cmd.shift) & 255u);
                     atomicAdd(&s.digit_count[d], 1u);
-                    atomicAdd(&s.digit_mass[d], mass_of(q, s.table, f[e]));
+                    if (!cmd.each) atomicAdd(&s.digit_mass[d], mass_of(q, s.table, f[e]));
                 }
             });
         } else if (!cmd.by_bins) {
             sweep(src, [&](const float (&f)[4], int32_t at) {
+                if (none(f)) return;
 #pragma unroll 1
                 for (int e = 0; e < 4; ++e) {
                     const u64 key = entry_key(f[e], at + e);
@@ -767,7 +877,7 @@ tfe_sample_kernel(const SampleParams p)
                 }
             } else {
                 base_n = 0; base_m = 0;
-                digits(56, 0, 0);
+                digits(56, 0, 0, 0);
             }
         } else {
             // digits in descending order: thread t holds digit 255 - t
@@ -776,6 +886,7 @@ tfe_sample_kernel(const SampleParams p)
             u64 m = 0;
             if (tid < 256)
                 for (int b = 0; b < p.blocks; ++b) { c += cluster.map_shared_rank(s.digit_count, b)[d]; m += cluster.map_shared_rank(s.digit_mass, b)[d]; }
+            if (cmd.each) m = c * cmd.each;
             const uint32_t c_run = block_scan(s.warp32, c);
             const u64 m_run = block_scan(s.warp64[0], m);
             const Goal g = goal_of(stage);
@@ -794,7 +905,7 @@ tfe_sample_kernel(const SampleParams p)
             if (inside <= (uint32_t)kList || cmd.shift == 0) {
                 if (tid == 0) { s.cmd.op = kOpCollect; s.cmd.by_bins = 0; s.cmd.prefix = prefix; s.cmd.mask = mask; }
             } else {
-                digits(cmd.shift - 8, prefix, mask);
+                digits(cmd.shift - 8, prefix, mask, cmd.each);
             }
         }
     }
