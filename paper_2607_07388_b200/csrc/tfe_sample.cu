@@ -438,25 +438,26 @@ tfe_sample_kernel(const SampleParams p)
     // which nothing of a weight is left are not counted: they end no search but one by count, whose mass they do not change.
     bool by_value = sizeof(T) == 2 && q.topf < INFINITY;
     const float least = fmaxf(fmaxf(q.cut, q.floor), q.floor > kMasked ? low : -INFINITY);
-    const int below_binades = max(0, (int)max(__float_as_uint(top) << 1 >> 24, __float_as_uint(least) << 1 >> 24) - 30) << 7;
+    const int below_binades = max(1, (int)max(__float_as_uint(top) << 1 >> 24, __float_as_uint(least) << 1 >> 24) - 30) << 7;
     uint32_t *by_values = reinterpret_cast<uint32_t *>(smem + offsetof(Shared, count));      // 2 kBins, `count` and `offset`
     auto value_at = [&](uint32_t at) {                  // of a bin; bins in descending order
         const uint32_t h = at < (uint32_t)kBins ? kBins - 1 - at : at - kBins;
         return h == 0 ? 0.f : __uint_as_float((h - 128 + below_binades) << 16 | (at < (uint32_t)kBins ? 0u : 0x80000000u));
     };
     if (by_value) {
-        bool small = false;
+        const int up = kBins - 1 - 128 + below_binades;
         sweep(src, [&](const float (&f)[4], int32_t) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int mag = (int)(__float_as_uint(f[e]) << 1 >> 17), above = mag - below_binades;
-                const bool kept = f[e] >= least, tiny = above < 0 || mag == 0;
-                const int h = tiny ? 0 : min(above + 128, kBins - 1);
-                small = small || (kept && tiny && mag != 0);
-                if (kept) atomicAdd(&by_values[f[e] < 0.f ? kBins + h : kBins - 1 - h], 1u);
+                const int mag = (int)(__float_as_uint(f[e]) << 1 >> 17);
+                // h is 0 for zero, 128 and more for what the binades hold, and between for what they do not
+                const int back = min(up - mag, max(kBins - 1 - mag, kBins - 2));        // kBins - 1 - h
+                const int at = (back ^ ((int)__float_as_uint(f[e]) >> 31)) & (2 * kBins - 1);           // negative: kBins + h
+                if (f[e] >= least) atomicAdd(&by_values[at], 1u);
             }
         });
-        if (small) s.small = 1;
+        __syncthreads();
+        if (tid < 127 && (by_values[kBins - 2 - tid] | by_values[kBins + 1 + tid])) s.small = 1;        // h of 1 to 127
         cluster.sync();
         for (int b = 0; b < p.blocks; ++b) by_value = by_value && *cluster.map_shared_rank(&s.small, b) == 0;
         if (!by_value)
@@ -607,6 +608,8 @@ tfe_sample_kernel(const SampleParams p)
         const uint32_t *counts = by_values + tid * 2 * kBinsPerThread;
         uint32_t c_sum = 0;
         u64 m_sum = 0;
+        if (tid == 0) { by_values[kBins - 1] += by_values[kBins]; by_values[kBins] = 0; }      // -0 and +0 are equal logits
+        __syncthreads();
 #pragma unroll 1
         for (int j = 0; j < 2 * kBinsPerThread; ++j)
             if (const uint32_t n = counts[j]) {
