@@ -446,16 +446,27 @@ tfe_sample_kernel(const SampleParams p)
     };
     if (by_value) {
         const int up = kBins - 1 - 128 + below_binades;
-        sweep(src, [&](const float (&f)[4], int32_t) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int mag = (int)(__float_as_uint(f[e]) << 1 >> 17);
-                // h is 0 for zero, 128 and more for what the binades hold, and between for what they do not
-                const int back = min(up - mag, max(kBins - 1 - mag, kBins - 2));        // kBins - 1 - h
-                const int at = (back ^ ((int)__float_as_uint(f[e]) >> 31)) & (2 * kBins - 1);           // negative: kBins + h
-                if (f[e] >= least) atomicAdd(&by_values[at], 1u);
-            }
-        });
+        const __nv_bfloat162 least2 = __bfloat162bfloat162(__float2bfloat16_ru(least));
+        const uint32_t up2 = (uint32_t)((up - 32767) & 0xFFFF) * 0x10001u, one2 = (uint32_t)((kBins - 1 - 32767) & 0xFFFF) * 0x10001u;
+        constexpr uint32_t two2 = (uint32_t)(kBins - 2) * 0x10001u;
+        // two logits at a time.  With mag the bits but the sign, h is 0 for zero, mag - below_binades + 128 for what the binades
+        // hold, and 1 to 127 for what they do not: kBins - 1 - h = min(up - mag, max(kBins - 1 - mag, kBins - 2)).
+        auto count_pair = [&](uint32_t w) {
+            const uint32_t back = __viaddmin_s16x2(~w & 0x7FFF7FFFu, up2, __viaddmax_s16x2(~w & 0x7FFF7FFFu, one2, two2));
+            const uint32_t at = (back ^ __vcmplts2(w, 0)) & (uint32_t)(2 * kBins - 1) * 0x10001u;         // negative: kBins + h
+            const uint32_t kept = __hge2_mask(*reinterpret_cast<const __nv_bfloat162 *>(&w), least2);
+            if (kept & 0xFFFFu) atomicAdd(&by_values[at & 0xFFFFu], 1u);
+            if (kept >> 16) atomicAdd(&by_values[at >> 16], 1u);
+        };
+        uint4 next = make_uint4(0, 0, 0, 0);            // one load ahead
+        if (tid < n_vec) next = src[tid];
+#pragma unroll 1
+        for (int32_t v = tid; v < n_vec; v += kThreads) {
+            const uint4 raw = next;
+            if (v + kThreads < n_vec) next = src[v + kThreads];
+            count_pair(raw.x); count_pair(raw.y); count_pair(raw.z); count_pair(raw.w);
+        }
+        if (tid < ends) count_pair(0xFFFF0000u | __float_as_uint(Elem<T>::get(row + end_index(tid))) >> 16);      // and a NaN
         __syncthreads();
         if (tid < 127 && (by_values[kBins - 2 - tid] | by_values[kBins + 1 + tid])) s.small = 1;        // h of 1 to 127
         cluster.sync();
@@ -610,12 +621,12 @@ tfe_sample_kernel(const SampleParams p)
         u64 m_sum = 0;
         if (tid == 0) { by_values[kBins - 1] += by_values[kBins]; by_values[kBins] = 0; }      // -0 and +0 are equal logits
         __syncthreads();
-#pragma unroll 1
-        for (int j = 0; j < 2 * kBinsPerThread; ++j)
-            if (const uint32_t n = counts[j]) {
-                c_sum += n;
-                m_sum += n * mass_of(q, s.table, value_at(tid * 2 * kBinsPerThread + j));
-            }
+#pragma unroll 4
+        for (int j = 0; j < 2 * kBinsPerThread; ++j) {
+            const uint32_t n = counts[j];
+            c_sum += n;
+            if (__any_sync(0xFFFFFFFFu, n)) m_sum += n * mass_of(q, s.table, value_at(tid * 2 * kBinsPerThread + j));
+        }
         const uint32_t c_run = block_scan(s.warp32, c_sum);
         const u64 m_run = block_scan(s.warp64[0], m_sum);
         if (tid == kThreads - 1) { s.found_count = c_run; s.found_mass = m_run; }
@@ -632,22 +643,31 @@ tfe_sample_kernel(const SampleParams p)
             const Goal g = goal_of(stage);
             uint32_t n0 = c_run - c_sum;
             u64 m0 = m_run - m_sum;
-            if (c_sum && g.met(c_run, m_run) && (n0 == 0 || !g.met(n0, m0))) {
-                for (int j = 0; j < 2 * kBinsPerThread; ++j) {
-                    const uint32_t here = counts[j];
-                    if (!here) continue;
-                    const u64 each = mass_of(q, s.table, value_at(tid * 2 * kBinsPerThread + j));
-                    if (g.met(n0 + here, m0 + here * each)) {
-                        const uint32_t i = first_of(here - 1, [&](uint32_t x) { return g.met(n0 + x + 1, m0 + (x + 1) * each); });
-                        s.found_at = tid * 2 * kBinsPerThread + j;
-                        s.found_count = here;
-                        s.found_mass = m0 + (i + 1) * each;
-                        s.found_key = m0;
-                        s.before_n[0] = n0;
-                        break;
-                    }
-                    n0 += here;
-                    m0 += here * each;
+            const uint32_t in = __ballot_sync(0xFFFFFFFFu, c_sum && g.met(c_run, m_run) && (n0 == 0 || !g.met(n0, m0)));
+            if (in) {                                   // this warp has the end: its bins, one per lane
+                static_assert(2 * kBinsPerThread <= 32, "a thread's bins fit a warp");
+                const int of = __ffs(in) - 1, bin = ((tid & ~31) + of) * 2 * kBinsPerThread + lane;
+                n0 = __shfl_sync(0xFFFFFFFFu, n0, of);
+                m0 = __shfl_sync(0xFFFFFFFFu, m0, of);
+                const uint32_t here = lane < 2 * kBinsPerThread ? by_values[bin] : 0;
+                const u64 each = here ? mass_of(q, s.table, value_at(bin)) : 0;
+                uint32_t n1 = here;
+                u64 m1 = here * each;
+#pragma unroll
+                for (int o = 1; o < 2 * kBinsPerThread; o <<= 1) {
+                    const uint32_t n_up = __shfl_up_sync(0xFFFFFFFFu, n1, o);
+                    const u64 m_up = __shfl_up_sync(0xFFFFFFFFu, m1, o);
+                    if (lane >= o) { n1 += n_up; m1 += m_up; }
+                }
+                n1 += n0 - here;                        // before this bin
+                m1 += m0 - here * each;
+                if (here && g.met(n1 + here, m1 + here * each) && (n1 == 0 || !g.met(n1, m1))) {
+                    const uint32_t i = first_of(here - 1, [&](uint32_t x) { return g.met(n1 + x + 1, m1 + (x + 1) * each); });
+                    s.found_at = bin;
+                    s.found_count = here;
+                    s.found_mass = m1 + (i + 1) * each;
+                    s.found_key = m1;
+                    s.before_n[0] = n1;
                 }
             }
             __syncthreads();
@@ -738,6 +758,32 @@ tfe_sample_kernel(const SampleParams p)
                     if (!cmd.each) atomicAdd(&s.digit_mass[d], mass_of(q, s.table, f[e]));
                 }
             });
+        } else if (sizeof(T) == 2 && !cmd.by_bins && one_value) {       // in pairs, several loads at once
+            const __nv_bfloat162 value2 = __float2bfloat162_rn(value);
+            auto take_pair = [&](uint32_t w, int32_t at) {
+                const uint32_t is = __heq2_mask(*reinterpret_cast<const __nv_bfloat162 *>(&w), value2);
+                if (is & 0xFFFFu) if (const u64 key = entry_key(value, at); (key & cmd.mask) == cmd.prefix) push(key);
+                if (is >> 16) if (const u64 key = entry_key(value, at + 1); (key & cmd.mask) == cmd.prefix) push(key);
+            };
+            constexpr int U = 4;
+#pragma unroll 1
+            for (int32_t v = tid; v < n_vec; v += U * kThreads) {
+                uint4 raw[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    raw[u] = make_uint4(0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu);
+                    if (v + u * kThreads < n_vec) raw[u] = src[v + u * kThreads];
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    auto is = [&](uint32_t w) { return __heq2_mask(*reinterpret_cast<const __nv_bfloat162 *>(&w), value2); };
+                    if (is(raw[u].x) | is(raw[u].y) | is(raw[u].z) | is(raw[u].w)) {
+                        const int32_t at = body0 + (v + u * kThreads) * E;
+                        take_pair(raw[u].x, at); take_pair(raw[u].y, at + 2); take_pair(raw[u].z, at + 4); take_pair(raw[u].w, at + 6);
+                    }
+                }
+            }
+            if (tid < ends) take_pair(0xFFFF0000u | __float_as_uint(Elem<T>::get(row + end_index(tid))) >> 16, end_index(tid));
         } else if (!cmd.by_bins) {
             sweep(src, [&](const float (&f)[4], int32_t at) {
                 if (none(f)) return;
