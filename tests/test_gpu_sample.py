@@ -274,3 +274,42 @@ def test_an_estimate_that_ends_too_early():
     check(zs, u, p=np.array([1 - 2.0 ** -20] * 5 + [0.99]))
     check(zs, u)
     check(zs, u, k=np.array([len(z) - 1] * rows), p=np.array([1 - 2.0 ** -20] * rows))
+
+
+@pytest.mark.parametrize("v", [30, 5000, 300_000])
+@pytest.mark.parametrize("scale", [1.0, 2.0 ** -100, 2.0 ** 60])
+def test_bf16_values_of_every_size(v, scale):
+    """Logits of any exponent beside each other, zeros of both signs and denormals among them: rows that are counted by value, and rows
+    whose small logits do not fit the values counted."""
+    rng = np.random.default_rng(v)
+    b = 12
+    z = rng.standard_normal((b, v)) * 3
+    z[2:4] *= np.exp2(rng.integers(-40, 1, (2, v)))             # down to far below the 31 binades
+    z[4:8] = np.where(rng.random((4, v)) < 0.6, rng.choice([0.0, -0.0], (4, v)), z[4:8])
+    z[6, ::5] = 2.0 ** -130
+    z[7, ::7] = -2.0 ** -133
+    z[8] = -np.abs(z[8])
+    z[9] = np.abs(z[9]) + 1
+    z[10] = np.where(rng.random(v) < 0.5, 0.0, -2.0 ** -126)
+    z[11] = np.where(rng.random(v) < 0.5, -0.0, -1e30)
+    t = np.full(b, scale, np.float32)
+    z = torch.from_numpy(z * np.where(z == 0, 1, scale)).to(torch.bfloat16)
+    pick = lambda *choices: rng.choice(choices, b)
+    check(z, rng.random(b), T=t)
+    check(z, rng.random(b), T=t, p=pick(0.3, 0.9, 0.999))
+    check(z, rng.random(b), T=t, k=pick(1, 7, v // 2, v - 1, v), p=pick(0.5, 1.0), mp=pick(0.0, 0.01, 1.0))
+    check(z, np.where(np.arange(b) % 2, 0.0, 1 - 2.0 ** -24), T=t * 1e-3)
+
+
+@pytest.mark.parametrize("v", [1100, 20_000, 262_144, 270_000, 1_100_000])
+def test_bf16_draw_among_many_equals(v):
+    """The drawn value held by more entries than the list: its entry is found by the digits of its index."""
+    rng = np.random.default_rng(v)
+    z = rng.choice([2.0, 1.0, -0.5], (4, v), p=[0.3, 0.6, 0.1]).astype(np.float32)
+    z[1] = rng.choice([0.0, -0.0], v)
+    z[2] = 3.0
+    z[3, : v // 2] = -np.inf
+    z = torch.from_numpy(z).to(torch.bfloat16)
+    for u in (0.0, 0.37, 0.81, 1 - 2.0 ** -24):
+        check(z, np.full(4, u))
+        check(z, np.full(4, u), k=np.array([v // 2, v // 3, v - 1, v // 5]), p=np.array([0.7, 1.0, 0.9, 0.5]))
