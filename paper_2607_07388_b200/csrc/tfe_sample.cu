@@ -88,7 +88,8 @@ constexpr double kWhole = 4503599627370496.0;           // 2^52: what is added t
 // w 2^shift + plus, with w = exp((z - top) / T) in 64 bits: y = 16 log2 w = n + f, n whole, |f| <= 1/2, so
 // w = 2^(n / 16) 2^(f / 16); the first factor from a table of 2^(shift + j / 16) (16 entries, so that a warp's reads never
 // meet in a bank) with n's multiples of 16 added to its exponent, the second by Taylor's series to the sixth power (|f| ln 2
-// / 16 is at most 0.0217; the first term left out is below 5e-16).  The maximum weighs 2^shift exactly.  Finite for any z.
+// / 16 is at most 0.0217; the first term left out is below 5e-16).  The maximum weighs 2^shift exactly.  A z below the floor is
+// weighed at the floor, which lies at most 4 (shift + 2) below 0 in log2 w: n fits the exponent for any z.
 // plus = 2^52 rounds to a whole number, which stands in the result's low 52 bits.
 __device__ __forceinline__ double weight_of(const RowRule &q, const double *table, float z, double plus)
 {
@@ -425,10 +426,13 @@ tfe_sample_kernel(const SampleParams p)
                              : min_p >= 1.f ? (double)q.topf : __dadd_rn((double)q.topf, __dmul_rn((double)T_, log((double)min_p)));
         q.cut = fmaxf(__double2float_ru(least), -3.402823466e38f);          // NaN (infinite maximum and temperature): the lowest
         if (q.topf == INFINITY) q.cut = INFINITY;                           // its equals share the draw, whatever the temperature
-        // -ln w = ln 2 (shift + 2): a quarter of the unit.  Where that is less than a step of the maximum, nothing else weighs.
+        // -ln w = ln 2 (shift + 2): a quarter of the unit.  What lies beyond that reach weighs nothing.
         const double reach = 0.6931471805599453 * (double)(p.shift + 2) * (double)T_;
-        q.floor = fmaxf(__double2float_rd((double)q.topf - reach), -3.402823466e38f);
-        if (!(q.floor < q.topf)) { q.cut = q.topf; q.floor = q.topf; }
+        // So does the next logit below the maximum where it lies beyond the reach: weighed at that step, it would leave the range
+        // of weight_of's exponent.  Otherwise a step is at most the reach, and rounding the floor down adds less than three of it.
+        const double end = (double)q.topf - reach;
+        q.floor = fmaxf(__double2float_rd(end), -3.402823466e38f);
+        if (!((double)nextafterf(q.topf, -INFINITY) > end)) { q.cut = q.topf; q.floor = q.topf; }
     }
     const float inv_t = 1.f / T_;
     float range = fminf(kRange, (q.topf - low) * inv_t);                    // NaN: kRange

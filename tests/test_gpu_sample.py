@@ -313,3 +313,31 @@ def test_bf16_draw_among_many_equals(v):
     for u in (0.0, 0.37, 0.81, 1 - 2.0 ** -24):
         check(z, np.full(4, u))
         check(z, np.full(4, u), k=np.array([v // 2, v // 3, v - 1, v // 5]), p=np.array([0.7, 1.0, 0.9, 0.5]))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("top", [0.7, 5.0, 12.3, 1000.0, 5e4, 1e10, -5.0, -1e10])
+@pytest.mark.parametrize("v", [700, 40_000])
+def test_small_temperatures(kind, top, v):
+    """Temperatures from those at which many logits weigh down to those at which one step below the maximum weighs nothing.  Three
+    equal maxima, the logits one to eight steps below them, and the rest far away."""
+    rng = np.random.default_rng(v)
+    T = (np.abs(top) * 10.0 ** -np.arange(0.0, 24.0)).astype(np.float32)
+    b = len(T)
+    t = torch.tensor(top, dtype=torch.float32).to(TYPES[kind])
+    near = [t]
+    for _ in range(8):
+        near.append(torch.nextafter(near[-1], torch.tensor(float("-inf"), dtype=TYPES[kind])))
+    z = (float(t) - np.abs(rng.standard_normal((b, v))) * abs(top) * 1e-2).astype(np.float32)
+    z = torch.from_numpy(z).to(TYPES[kind])
+    z = torch.where(z >= t, near[8], z)
+    at = rng.permutation(v)[:11]
+    z[:, at[:3]] = t
+    z[:, at[3:]] = torch.stack(near[1:])
+    some = rng.permutation(v)[: v // 3]
+    z[1::2, some] = torch.where(z[1::2, some] < near[8], torch.finfo(TYPES[kind]).min, z[1::2, some])       # every other row: masked ones too
+    for u in (0.0, 0.5, 0.9, 0.999):
+        check(z, np.full(b, u), T=T)
+    check(z, rng.random(b), T=T, k=rng.choice([1, 2, 3, 5, v // 2], b), p=rng.choice([0.3, 0.9, 1.0], b))
+    check(z, rng.random(b), T=T, p=np.full(b, 0.6), mp=rng.choice([0.0, 0.1, 1.0], b))
+    check(z, rng.random(b), T=np.array([1e-30, 1e-38, 1e-45, 1e-9, 1e-10, 1e-11] * 4, np.float32))
