@@ -733,8 +733,8 @@ tfe_sample_kernel(const SampleParams p)
         __syncthreads();
         const int32_t k = p.top_k ? p.top_k[r] : 0;
         // a k-th entry in the last bin restricts nothing: what is there weighs nothing (the range's end is below the unit of the
-        // masses, and masked logits are, unless the temperature is beyond any use)
-        const bool last_is_nothing = range == kRange || mass_of(q, s.table, kMasked) == 0;
+        // masses, and masked logits are, unless the temperature is beyond any use).  Infinite maxima are there too, and weigh.
+        const bool last_is_nothing = q.topf < INFINITY && (range == kRange || mass_of(q, s.table, kMasked) == 0);
         const uint32_t countable = last_is_nothing ? s.count[kBins - 2] : s.count[kBins - 1];
         const bool k_on = k > 0 && (uint32_t)k < s.count[kBins - 1] && ((uint32_t)k <= countable || !last_is_nothing);
         stage = k_on ? kTopK : next_stage(kTopK);

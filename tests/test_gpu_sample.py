@@ -341,3 +341,27 @@ def test_small_temperatures(kind, top, v):
     check(z, rng.random(b), T=T, k=rng.choice([1, 2, 3, 5, v // 2], b), p=rng.choice([0.3, 0.9, 1.0], b))
     check(z, rng.random(b), T=T, p=np.full(b, 0.6), mp=rng.choice([0.0, 0.1, 1.0], b))
     check(z, rng.random(b), T=np.array([1e-30, 1e-38, 1e-45, 1e-9, 1e-10, 1e-11] * 4, np.float32))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("v", [50, 5000, 60_000])
+def test_top_k_among_infinite_logits(kind, v):
+    """Rows with two, three, a fifth of or nothing but +inf logits: top-k and top-p cut among them by index."""
+    rng = np.random.default_rng(v)
+    b = 8
+    z = rng.standard_normal((b, v)).astype(np.float32)
+    z[0, [v // 3, v - 2]] = np.inf
+    z[1, [4, 9, v - 1]] = np.inf
+    z[2, rng.permutation(v)[: v // 5]] = np.inf
+    z[3] = np.inf
+    z[4, [0, 1, 2]] = np.inf; z[4, 10:] = -np.inf; z[4, 5] = np.nan
+    z[5, rng.permutation(v)[: v // 2]] = np.inf; z[5, ::7] = np.nan
+    z[6, v // 2:] = np.inf
+    z[7, 3] = np.inf
+    z = torch.from_numpy(z).to(TYPES[kind])
+    for u in (0.0, 0.4, 0.9, 1 - 2.0 ** -24):
+        for k in (1, 2, 3, 7, max(8, v // 11), v // 3, v - 1):
+            check(z, np.full(b, u), k=np.full(b, k))
+            check(z, np.full(b, u), k=np.full(b, k), p=np.full(b, 0.7), T=np.full(b, 0.5))
+    check(z, rng.random(b), k=np.full(b, 2), T=np.full(b, np.inf))
+    check(z, rng.random(b), k=np.full(b, 2), mp=np.full(b, 0.3), T=np.full(b, 1e-12))
