@@ -149,7 +149,7 @@ tfe_quantize_rows_kernel(const QuantParams p)
     tfe_wait_for_stream();
     const int l = threadIdx.x & (kGroupLanes - 1);
     const uint32_t groups = (uint32_t)p.R * (uint32_t)p.kb;
-    const uint32_t g = (blockIdx.x * kQuantThreads + threadIdx.x) / kGroupLanes;
+    const uint32_t g = blockIdx.x * (kQuantThreads / kGroupLanes) + threadIdx.x / kGroupLanes;     // fits 32 bits, the thread's number does not
     if (g >= groups) return;                    // half-warps leave as a whole
     const uint32_t half = 0xFFFFu << (threadIdx.x & 16);
     const uint32_t row = g / (uint32_t)p.kb, b = g - row * (uint32_t)p.kb;

@@ -282,3 +282,22 @@ def test_output_on_its_operands_is_refused():
         engine.matmul_fp8(a, sa, w, sw, out=over_w)
     want = engine.matmul_fp8(a, sa, w, sw, out_dtype=torch.bfloat16)
     assert torch.equal(engine.matmul_fp8(inside, sa, w, sw, out=at(1024)), want)
+
+
+def test_conversion_of_more_groups_than_32_bits_of_threads():
+    """2^28 groups are 2^32 threads: the rows beyond are converted like the first."""
+    from paper_2607_07388_b200 import engine
+    r = (1 << 28) + 1000
+    x = torch.full((r, 1), 3.0, dtype=torch.bfloat16, device=DEV)
+    ends = [(0, 1000), ((1 << 28) - 500, (1 << 28) + 500), (r - 1000, r)]
+    rng = np.random.default_rng(28)
+    given = [torch.from_numpy(rng.standard_normal((b - a, 1)).astype(np.float32)).to(torch.bfloat16) for a, b in ends]
+    for (a, b), part in zip(ends, given):
+        x[a:b] = part.to(DEV)
+    q, scale = engine.quantize_fp8(x)
+    for a, b in ends:
+        bits, sign, s = quantize64(x[a:b].float().cpu().numpy(), 1)
+        assert np.array_equal(scale[a:b].cpu().numpy(), s)
+        got = q[a:b].view(torch.uint8).cpu().numpy()
+        assert np.array_equal(got & 0x7F, bits) and np.array_equal(got >> 7, sign)
+    assert int((scale == np.float32(3) / np.float32(448)).sum()) >= r - 3000
