@@ -227,6 +227,7 @@ def assign_residency(count: torch.Tensor, gpu_slots: int, host_min_count: int = 
 # ---- rows of logits ----------------------------------------------------------------------------
 
 _ROW_DTYPES = {torch.bfloat16: tfe.DTYPE_BF16, torch.float32: tfe.DTYPE_F32}
+_SIZE_MAX = (1 << 31) - 1           # ctypes cuts a larger size to its low 32 bits
 
 
 def _require(ok: bool, what: str):
@@ -263,6 +264,8 @@ def _row_matrix(t: torch.Tensor, what: str):
     if kind is None or not t.is_cuda or t.dim() != 2:
         raise ValueError(f"{what}: a 2-D bf16 or fp32 CUDA tensor is needed")
     n, v = t.shape
+    if n > _SIZE_MAX or v > _SIZE_MAX:
+        raise ValueError(f"{what}: more than 2^31 - 1 rows or columns")
     ld, step = t.stride()
     if v < 1 or (step != 1 and v != 1):
         raise ValueError(f"{what}: rows must be contiguous and not empty")
@@ -304,6 +307,8 @@ def _fp8_matrix(t: torch.Tensor, what: str):
     if not t.is_cuda or t.dim() != 2 or t.dtype != torch.float8_e4m3fn:
         raise ValueError(f"{what}: a 2-D float8_e4m3fn CUDA tensor is needed")
     n, k = t.shape
+    if n > _SIZE_MAX or k > _SIZE_MAX:
+        raise ValueError(f"{what}: more than 2^31 - 1 rows or columns")
     ld, step = t.stride()
     if n <= 1:
         ld = -(-k // 16) * 16

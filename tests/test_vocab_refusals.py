@@ -74,3 +74,25 @@ def test_conversion_and_product_in_8_bits(tfe):
     assert product(M=0, a=None, sa=None, w=None, sw=None, out=None) == tfe.TFE_OK
     assert L.tfe_matmul_fp8_status(None, None) == tfe.TFE_ERR_INVALID_ARG
     assert L.tfe_matmul_fp8_status.argtypes[0] == C.POINTER(C.c_uint32)
+
+
+def test_sizes_beyond_32_bits():
+    """The library takes 32-bit sizes, and a call through ctypes cuts larger ones down without a word: the package refuses them."""
+    import ctypes as C
+    from types import SimpleNamespace
+
+    import torch
+
+    from paper_2607_07388_b200 import engine
+    assert C.c_int32((1 << 32) + 5).value == 5
+
+    def matrix(rows, cols, dtype):                  # no such memory is needed: sizes are looked at first
+        return SimpleNamespace(dtype=dtype, is_cuda=True, shape=(rows, cols), dim=lambda: 2, stride=lambda: (cols, 1), data_ptr=lambda: P)
+
+    for rows, cols in (((1 << 32) + 5, 16), (1 << 31, 16), (1, (1 << 32) + 16), (3, 1 << 31)):
+        with pytest.raises(ValueError):
+            engine._row_matrix(matrix(rows, cols, torch.bfloat16), "x")
+        with pytest.raises(ValueError):
+            engine._fp8_matrix(matrix(rows, cols, torch.float8_e4m3fn), "a")
+    assert engine._row_matrix(matrix((1 << 31) - 1, 16, torch.float32), "x") == ((1 << 31) - 1, 16, 16, engine.tfe.DTYPE_F32)
+    assert engine._fp8_matrix(matrix((1 << 31) - 1, 16, torch.float8_e4m3fn), "a") == ((1 << 31) - 1, 16, 16)
