@@ -524,9 +524,18 @@ enum { TFE_DTYPE_BF16 = 0, TFE_DTYPE_F32 = 1 };
  *   summed by the tensor cores, blocks in fp32, and the result is rounded once.  Elements of out beyond N stay as
  *   they were.  One launch.
  *
- * tfe_matmul_fp8_status -- synchronises `stream` and reads the library's status word on the current device: 0, or
- * bits set by waits inside the kernel that ran out (1 loader, 2 MMA issuer, 4 scales, 8 epilogue); then INTERNAL.
- * Errors of all three: INVALID_ARG, CUDA.
+ *   Every wait inside the kernel is bounded.  Should one run out, the results that the call has not stored by then are NaN,
+ *   from which tfe_sample_tokens draws -1.
+ *
+ * tfe_matmul_fp8_status -- synchronises `stream`, reads the library's status word on the current device and clears what
+ * it read: 0, or bits set by waits inside the kernel that ran out (1 loader, 2 MMA issuer, 4 scales, 8 epilogue); then
+ * INTERNAL.  The word is one for all calls on the device, whatever their stream: it says that some product since the
+ * last report failed, and the NaN in its results which.
+ *
+ * tfe_matmul_fp8_wait_limit -- polls of one barrier after which a wait inside the product gives up, for the calls that
+ * follow, of the whole process: 0 (at once) .. 2^22, negative: 2^22, the library's own.  For tests of a caller's handling
+ * of failures.
+ * Errors of all four: INVALID_ARG, CUDA.
  */
 #define TFE_FP8_MAX_COLS (1 << 16)
 tfe_status tfe_quantize_fp8(const void *x, int32_t dtype, int32_t R, int32_t C, int64_t ld, int32_t block_rows,
@@ -535,6 +544,7 @@ tfe_status tfe_matmul_fp8(const void *a, int64_t lda, const float *a_scale, int3
                           const float *w_scale, int32_t N, int32_t K, void *out, int32_t out_dtype, int64_t ldo,
                           void *stream);
 tfe_status tfe_matmul_fp8_status(uint32_t *device_flags, void *stream);
+tfe_status tfe_matmul_fp8_wait_limit(int32_t polls);
 
 /*
  * tfe_sample_tokens -- the next token of every sequence from its logits and one given random number per sequence

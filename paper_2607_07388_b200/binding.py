@@ -36,7 +36,7 @@ EXPORTS = ["tfe_index_build", "tfe_index_build_device", "tfe_cache_install", "tf
            "tfe_cache_stats", "tfe_head_create", "tfe_head_destroy", "tfe_head_topk", "tfe_head_buffers",
            "tfe_head_status", "tfe_head_geometry", "tfe_mine_ngrams", "tfe_mine_workspace_bytes", "tfe_assign_residency", "tfe_stream_copy",
            "tfe_cache_select_tuning", "tfe_distill_forward", "tfe_distill_backward", "tfe_sample_tokens",
-           "tfe_quantize_fp8", "tfe_matmul_fp8", "tfe_matmul_fp8_status"]
+           "tfe_quantize_fp8", "tfe_matmul_fp8", "tfe_matmul_fp8_status", "tfe_matmul_fp8_wait_limit"]
 
 
 class TfeConfig(C.Structure):
@@ -124,6 +124,7 @@ def lib() -> C.CDLL:
         L.tfe_quantize_fp8.argtypes = [vp, i32, i32, i32, i64, i32, vp, vp, vp]
         L.tfe_matmul_fp8.argtypes = [vp, i64, vp, i32, vp, i64, vp, i32, i32, vp, i32, i64, vp]
         L.tfe_matmul_fp8_status.argtypes = [C.POINTER(C.c_uint32), vp]
+        L.tfe_matmul_fp8_wait_limit.argtypes = [i32]
         L.tfe_sample_tokens.argtypes = [vp, i32, i32, i32, i64, C.POINTER(TfeSampleParams), vp, vp, vp, vp]
         L.tfe_distill_forward.argtypes = [vp, i32, i32, i32, i64, vp, vp, i32, f32, vp, vp, vp]
         L.tfe_distill_backward.argtypes = [vp, i32, i32, i32, i64, vp, vp, i32, f32, vp, vp, vp, i64, vp]
@@ -134,7 +135,7 @@ def lib() -> C.CDLL:
                      "tfe_cache_stats", "tfe_head_create", "tfe_head_topk", "tfe_head_buffers", "tfe_head_status",
                      "tfe_head_geometry", "tfe_mine_ngrams", "tfe_assign_residency", "tfe_cache_select_tuning",
                      "tfe_distill_forward", "tfe_distill_backward", "tfe_sample_tokens", "tfe_quantize_fp8",
-                     "tfe_matmul_fp8", "tfe_matmul_fp8_status"):
+                     "tfe_matmul_fp8", "tfe_matmul_fp8_status", "tfe_matmul_fp8_wait_limit"):
             getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -503,9 +504,13 @@ def tfe_matmul_fp8(a, lda: int, a_scale, M: int, w, ldw: int, w_scale, N: int, K
 
 
 def tfe_matmul_fp8_status(stream=None) -> int:
-    """Synchronises; returns the device status word (0 = no wait ran out)."""
+    """Synchronises; returns the device status word and clears it (0 = no wait ran out since the last report)."""
     flags = C.c_uint32(0)
     st = lib().tfe_matmul_fp8_status(C.byref(flags), _stream(stream))
     if st not in (TFE_OK, TFE_ERR_INTERNAL):
         _check(st, "tfe_matmul_fp8_status")
     return flags.value
+
+
+def tfe_matmul_fp8_wait_limit(polls: int) -> None:
+    _check(lib().tfe_matmul_fp8_wait_limit(polls), "tfe_matmul_fp8_wait_limit")

@@ -24,6 +24,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cstdint>
 
 #include "../../include/tfe.h"
@@ -214,6 +215,11 @@ constexpr int kMatmulSmem = 224 * 1024;         // stages; the rest of an SM's 2
 // bits of the device status word
 constexpr uint32_t kTimeoutLoader = 1u, kTimeoutMma = 2u, kTimeoutScales = 4u, kTimeoutEpilogue = 8u;
 __device__ uint32_t g_matmul_status;
+const float not_a_number = __builtin_nanf("");
+std::atomic<uint32_t> g_wait_limit{TC_WAIT_LIMIT};
+
+// Only what the caller has been told goes: a bit that another stream sets meanwhile stays.
+__global__ void tfe_matmul_fp8_status_kernel(uint32_t told) { atomicAnd(&g_matmul_status, ~told); }
 
 struct MatmulParams {
     int32_t M, N, kb;                           // activation rows, weight rows, blocks of 128 along k
@@ -221,6 +227,7 @@ struct MatmulParams {
     int32_t rows_per_cta, tail_rows;            // few rows: weight rows of a CTA, rows of its last short tile
     int32_t m_tiles;                            // many rows: tiles of activation rows
     int64_t n_units;                            // ... and all tiles
+    uint32_t wait_limit;                        // polls of one mbarrier before a wait gives up
     const float *a_scale, *b_scale;             // [M][kb], [ceil(N / 128)][kb]
     void *out; int64_t ldo;
 };
@@ -310,7 +317,7 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
                 const bool tail = valid < kTileRows && valid == p.tail_rows;
                 const uint32_t w_bytes = tail ? (uint32_t)p.tail_rows * 128u : kTileRows * 128u;
                 for (int32_t kb = 0; kb < p.kb; kb += kGroup) {
-                    if (!mbar_wait(smem_u32(&s_empty[stage]), phase ^ 1u, &s_abort)) {
+                    if (!mbar_wait(smem_u32(&s_empty[stage]), phase ^ 1u, &s_abort, p.wait_limit)) {
                         atomicOr(&g_matmul_status, kTimeoutLoader);
                         s_abort = 1;
                         ok = false;
@@ -341,8 +348,8 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
             bool ok = true;
             for (int32_t t = 0; ok && t < n_tiles; ++t) {
                 for (int32_t kb = 0; kb < p.kb; kb += kGroup) {
-                    if (!mbar_wait(smem_u32(&s_acc_empty[buf]), buf_phase ^ 1u, &s_abort) ||
-                        !mbar_wait(smem_u32(&s_full[stage]), phase, &s_abort)) {
+                    if (!mbar_wait(smem_u32(&s_acc_empty[buf]), buf_phase ^ 1u, &s_abort, p.wait_limit) ||
+                        !mbar_wait(smem_u32(&s_full[stage]), phase, &s_abort, p.wait_limit)) {
                         atomicOr(&g_matmul_status, kTimeoutMma);
                         s_abort = 1;
                         ok = false;
@@ -382,7 +389,7 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
 #pragma unroll
                     for (int c = 0; c < kPer; ++c)
                         v[g][c] = c * 32 + lane < p.M && kb + g < p.kb ? __ldg(p.a_scale + (int64_t)(c * 32 + lane) * p.kb + kb + g) : 0.f;
-                ok = mbar_wait(smem_u32(&s_sc_empty[st]), phase ^ 1u, &s_abort);
+                ok = mbar_wait(smem_u32(&s_sc_empty[st]), phase ^ 1u, &s_abort, p.wait_limit);
                 if (!__all_sync(0xFFFFFFFFu, ok)) {
                     if (lane == 0) atomicOr(&g_matmul_status, kTimeoutScales);
                     s_abort = 1;
@@ -405,7 +412,8 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
         const int32_t row_in_tile = (int32_t)(quarter * 32u) + lane;
         uint32_t st = 0, phase = 0, buf = 0, buf_phase = 0;
         bool ok = true;
-        for (int32_t t = 0; ok && t < n_tiles; ++t) {
+        int32_t t = 0;
+        for (; t < n_tiles; ++t) {
             const int64_t n0 = r0 + (int64_t)t * kTileRows;
             const int32_t valid = min(kTileRows, n_rows - t * kTileRows);
             float2 acc[kCols / 2];
@@ -423,7 +431,7 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
 #pragma unroll
                 for (int g = 0; g < kGroup; ++g) sb[g] = sb_next[g];
                 fetch(kb + kGroup);
-                ok = mbar_wait(smem_u32(&s_sc_full[st]), phase, &s_abort) && mbar_wait(smem_u32(&s_acc_full[buf]), buf_phase, &s_abort);
+                ok = mbar_wait(smem_u32(&s_sc_full[st]), phase, &s_abort, p.wait_limit) && mbar_wait(smem_u32(&s_acc_full[buf]), buf_phase, &s_abort, p.wait_limit);
                 if (!__all_sync(0xFFFFFFFFu, ok)) {
                     if (lane == 0) atomicOr(&g_matmul_status, kTimeoutEpilogue);
                     s_abort = 1;
@@ -459,7 +467,8 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
                 if (++st == kScaleRing) { st = 0; phase ^= 1u; }
                 if (++buf == kBuffers) { buf = 0; buf_phase ^= 1u; }
             }
-            if (ok && row_in_tile < valid) {
+            if (!ok) break;
+            if (row_in_tile < valid) {
                 Out *at = static_cast<Out *>(p.out) + (int64_t)c0 * p.ldo + n0 + row_in_tile;
                 const int32_t left = p.M - c0;
 #pragma unroll
@@ -469,6 +478,12 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
                 }
             }
         }
+#pragma unroll 1
+        for (; t < n_tiles; ++t)                                    // a wait ran out: no results, and none that look like some
+            if (t * kTileRows + row_in_tile < n_rows)
+#pragma unroll 1
+                for (int32_t j = c0; j < min(c0 + kCols, p.M); ++j)
+                    Elem<Out>::put(static_cast<Out *>(p.out) + (int64_t)j * p.ldo + r0 + (int64_t)t * kTileRows + row_in_tile, not_a_number);
     }
 
     tc_fence_before();
@@ -606,7 +621,7 @@ tfe_matmul_fp8_many_kernel(const __grid_constant__ CUtensorMap map_w, const __gr
                 const int64_t nt = u / p.m_tiles;
                 const int32_t n0 = (int32_t)(nt * kN), m0 = (int32_t)(u - nt * p.m_tiles) * kTileRows;
                 for (int32_t kb = 0; kb < p.kb; ++kb) {
-                    if (!mbar_wait(smem_u32(&s_empty[stage]), phase ^ 1u, &s_abort)) {
+                    if (!mbar_wait(smem_u32(&s_empty[stage]), phase ^ 1u, &s_abort, p.wait_limit)) {
                         atomicOr(&g_matmul_status, kTimeoutLoader);
                         s_abort = 1;
                         ok = false;
@@ -632,8 +647,8 @@ tfe_matmul_fp8_many_kernel(const __grid_constant__ CUtensorMap map_w, const __gr
             bool ok = true;
             for (int64_t u = blockIdx.x; ok && u < p.n_units; u += gridDim.x)
                 for (int32_t kb = 0; kb < p.kb; ++kb) {
-                    if (!mbar_wait(smem_u32(&s_acc_empty[buf]), buf_phase ^ 1u, &s_abort) ||
-                        !mbar_wait(smem_u32(&s_full[stage]), phase, &s_abort)) {
+                    if (!mbar_wait(smem_u32(&s_acc_empty[buf]), buf_phase ^ 1u, &s_abort, p.wait_limit) ||
+                        !mbar_wait(smem_u32(&s_full[stage]), phase, &s_abort, p.wait_limit)) {
                         atomicOr(&g_matmul_status, kTimeoutMma);
                         s_abort = 1;
                         ok = false;
@@ -664,7 +679,8 @@ tfe_matmul_fp8_many_kernel(const __grid_constant__ CUtensorMap map_w, const __gr
         const uint32_t row_smem = smem_base + kStages * kManyStageBytes + (uint32_t)((e * 32 + lane) * kRowPitch);
         uint32_t buf = 0, buf_phase = 0;
         bool ok = true;
-        for (int64_t u = blockIdx.x; ok && u < p.n_units; u += gridDim.x) {
+        int64_t u = blockIdx.x;
+        for (; u < p.n_units; u += gridDim.x) {
             const int64_t nt = u / p.m_tiles;
             const int64_t n0 = nt * kN + c0;
             const int32_t m0 = (int32_t)(u - nt * p.m_tiles) * kTileRows + (int32_t)quarter * 32;
@@ -692,7 +708,7 @@ tfe_matmul_fp8_many_kernel(const __grid_constant__ CUtensorMap map_w, const __gr
                 }
                 const float2 scale = make_float2(scales[0], scales[0]);
                 scales[0] = scales[1]; scales[1] = scales[2]; scales[2] = scales[3];
-                ok = mbar_wait(smem_u32(&s_acc_full[buf]), buf_phase, &s_abort);
+                ok = mbar_wait(smem_u32(&s_acc_full[buf]), buf_phase, &s_abort, p.wait_limit);
                 if (!__all_sync(0xFFFFFFFFu, ok)) {
                     if (lane == 0) atomicOr(&g_matmul_status, kTimeoutEpilogue);
                     s_abort = 1;
@@ -728,6 +744,13 @@ tfe_matmul_fp8_many_kernel(const __grid_constant__ CUtensorMap map_w, const __gr
             }
         }
         asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+#pragma unroll 1
+        for (; u < p.n_units; u += gridDim.x) {                     // a wait ran out: no results, and none that look like some
+            const int64_t nt = u / p.m_tiles, n0 = nt * kN + c0, m = (u - nt * p.m_tiles) * kTileRows + quarter * 32u + lane;
+            if (m < p.M)
+#pragma unroll 1
+                for (int64_t n = n0; n < min(n0 + kCols, (int64_t)p.N); ++n) Elem<Out>::put(static_cast<Out *>(p.out) + m * p.ldo + n, not_a_number);
+        }
     }
 
     tc_fence_before();
@@ -838,6 +861,7 @@ tfe_status tfe_matmul_fp8(const void *a, int64_t lda, const float *a_scale, int3
     MatmulParams p{};
     p.M = M; p.N = N; p.kb = (K + kBlockK - 1) / kBlockK;
     p.a_scale = a_scale; p.b_scale = w_scale; p.out = out; p.ldo = ldo;
+    p.wait_limit = g_wait_limit.load(std::memory_order_relaxed);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     CUtensorMap map_w, map_a;
     if (M > kFewRows)
@@ -865,7 +889,18 @@ tfe_status tfe_matmul_fp8_status(uint32_t *device_flags, void *stream_)
     if (tfe_status st = tfe_note_cuda(cudaGetSymbolAddress(&at, g_matmul_status), "cudaGetSymbolAddress")) return st;
     if (tfe_status st = tfe_note_cuda(cudaMemcpyAsync(device_flags, at, sizeof(uint32_t), cudaMemcpyDeviceToHost, stream), "cudaMemcpyAsync")) return st;
     if (tfe_status st = tfe_note_cuda(cudaStreamSynchronize(stream), "cudaStreamSynchronize")) return st;
-    return *device_flags ? TFE_ERR_INTERNAL : TFE_OK;
+    if (*device_flags == 0) return TFE_OK;
+    tfe_matmul_fp8_status_kernel<<<1, 1, 0, stream>>>(*device_flags);
+    if (tfe_status st = tfe_note_cuda(cudaGetLastError(), "status launch")) return st;
+    if (tfe_status st = tfe_note_cuda(cudaStreamSynchronize(stream), "cudaStreamSynchronize")) return st;
+    return TFE_ERR_INTERNAL;
+}
+
+tfe_status tfe_matmul_fp8_wait_limit(int32_t polls)
+{
+    if (polls > (int32_t)TC_WAIT_LIMIT) return TFE_ERR_INVALID_ARG;
+    g_wait_limit.store(polls < 0 ? TC_WAIT_LIMIT : (uint32_t)polls, std::memory_order_relaxed);
+    return TFE_OK;
 }
 
 }  // extern "C"

@@ -320,7 +320,8 @@ def _fp8_matrix(t: torch.Tensor, what: str):
 def matmul_fp8(a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, *,
                out_dtype: torch.dtype = torch.float32, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """a [M, K] times the transpose of w [N, K], both as quantize_fp8 makes them (block_rows 1 and 128): [M, N] in fp32 or
-    bf16 (see tfe_matmul_fp8).  `out`: where it goes instead of a new tensor."""
+    bf16 (see tfe_matmul_fp8).  `out`: where it goes instead of a new tensor.  A product that fails on the device leaves NaN in
+    what it did not finish; matmul_fp8_status() tells."""
     if not _here(a.device, stream):
         with _elsewhere(a.device, stream):
             return _matmul_fp8(a, a_scale, w, w_scale, out_dtype, out, stream)
@@ -353,6 +354,12 @@ def _matmul_fp8(a, a_scale, w, w_scale, out_dtype, out, stream):
     return out
 
 
+def matmul_fp8_status(stream=None) -> int:
+    """0, or the device's status word if a product on it failed since the last report, which clears it (see
+    tfe_matmul_fp8_status).  Synchronises."""
+    return tfe.tfe_matmul_fp8_status(stream)
+
+
 class QuantizedHead:
     """The vocabulary projection in 8 bits: half the bytes of EarlyExitHead's weights to read per call, logits instead of a
     top-K.  ``w``: bf16 or fp32 [V, d], d a multiple of 16; it is converted once and not kept."""
@@ -379,6 +386,11 @@ class QuantizedHead:
             with _elsewhere(hidden.device, stream):
                 return self.sample(hidden, u, **settings)
         return sample_tokens(self.logits(hidden), u, **settings)
+
+    def status(self) -> int:
+        """matmul_fp8_status on the weights' device."""
+        with torch.cuda.device(self.w.device):
+            return matmul_fp8_status()
 
 
 def sample_tokens(logits: torch.Tensor, u: torch.Tensor, *, temperature: torch.Tensor | None = None,

@@ -301,3 +301,34 @@ def test_conversion_of_more_groups_than_32_bits_of_threads():
         got = q[a:b].view(torch.uint8).cpu().numpy()
         assert np.array_equal(got & 0x7F, bits) and np.array_equal(got >> 7, sign)
     assert int((scale == np.float32(3) / np.float32(448)).sum()) >= r - 3000
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("m,n,k", [(3, 1003, 640), (40, 30_001, 256), (64, 77, 128), (300, 1003, 640), (65, 90_001, 128)])
+def test_waits_that_run_out(m, n, k, kind):
+    """Every wait of the kernel gives up at once: all results are NaN, nothing beside them is touched, the status tells once, and the
+    next product is right again."""
+    from paper_2607_07388_b200 import binding as tfe
+    from paper_2607_07388_b200 import engine
+    a, sa, w, sw = operands(m + n, m, n, k)
+    args = (a.to(DEV), sa.to(DEV), w.to(DEV), sw.to(DEV))
+    store = torch.full((m, n + 8), 5.0, dtype=TYPES[kind], device=DEV)
+    out = store[:, 3:n + 3]
+    assert engine.matmul_fp8_status() == 0
+    tfe.tfe_matmul_fp8_wait_limit(0)
+    try:
+        engine.matmul_fp8(*args, out=out)
+        torch.cuda.synchronize()
+    finally:
+        tfe.tfe_matmul_fp8_wait_limit(-1)
+    assert torch.isnan(out).all()
+    token, prob = engine.sample_tokens(out, torch.full((m,), 0.5, device=DEV))
+    assert (token == -1).all() and (prob == 0).all()
+    good = engine.matmul_fp8(*args, out_dtype=TYPES[kind])
+    assert engine.matmul_fp8_status() != 0                       # of the call before: the good one has set nothing
+    assert engine.matmul_fp8_status() == 0
+    check_product(good, a, sa, w, sw, kind)
+    head = engine.QuantizedHead(torch.ones((16, 16), device=DEV))
+    assert head.status() == 0
+    out.fill_(5.0)
+    assert (store == 5.0).all()

@@ -96,3 +96,9 @@ def test_sizes_beyond_32_bits():
             engine._fp8_matrix(matrix(rows, cols, torch.float8_e4m3fn), "a")
     assert engine._row_matrix(matrix((1 << 31) - 1, 16, torch.float32), "x") == ((1 << 31) - 1, 16, 16, engine.tfe.DTYPE_F32)
     assert engine._fp8_matrix(matrix((1 << 31) - 1, 16, torch.float8_e4m3fn), "a") == ((1 << 31) - 1, 16, 16)
+
+
+def test_wait_limit_of_the_product(tfe):
+    L = tfe.lib()
+    assert L.tfe_matmul_fp8_wait_limit((1 << 22) + 1) == tfe.TFE_ERR_INVALID_ARG
+    assert L.tfe_matmul_fp8_wait_limit(1 << 22) == L.tfe_matmul_fp8_wait_limit(-1) == tfe.TFE_OK
