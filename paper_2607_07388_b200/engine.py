@@ -347,8 +347,8 @@ def _matmul_fp8(a, a_scale, w, w_scale, out_dtype, out, stream):
         if om != m or on != n or out.device != dev:
             raise ValueError("out: [M, N] on the operands' device is needed")
         at, end = out.data_ptr(), out.data_ptr() + ((m - 1) * ldo + n) * out.element_size()
-        for t, rows, ld in ((a, m, lda), (w, n, ldw)):
-            if m and at < t.data_ptr() + (rows - 1) * ld + k and t.data_ptr() < end:
+        for start, size in ((a.data_ptr(), (m - 1) * lda + k), (w.data_ptr(), (n - 1) * ldw + k), (a_s, 4 * m * kb), (w_s, 4 * w_scale.numel())):
+            if m and at < start + size and start < end:
                 raise ValueError("out: must not touch the operands")
     tfe.tfe_matmul_fp8(a.data_ptr(), lda, a_s, m, w.data_ptr(), ldw, w_s, n, k, out.data_ptr(), kind, ldo, _where(dev, stream))
     return out

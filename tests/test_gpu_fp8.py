@@ -332,3 +332,19 @@ def test_waits_that_run_out(m, n, k, kind):
     assert head.status() == 0
     out.fill_(5.0)
     assert (store == 5.0).all()
+
+
+@pytest.mark.parametrize("which", [1, 3])
+def test_output_on_the_scales_is_refused(which):
+    from paper_2607_07388_b200 import engine
+    args = [x.to(DEV) for x in operands(5, 3, 100, 1024)]
+    want = engine.matmul_fp8(*args)
+    size = args[which].numel()
+    room = torch.zeros(size + 300, device=DEV)
+    held = room[:size].view(args[which].shape)
+    held.copy_(args[which])
+    args[which] = held
+    for first in (0, size - 1):
+        with pytest.raises(ValueError):
+            engine.matmul_fp8(*args, out=room[first: first + 300].view(3, 100))
+    assert torch.equal(engine.matmul_fp8(*args, out=room[size: size + 300].view(3, 100)), want)
