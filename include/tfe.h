@@ -596,7 +596,8 @@ tfe_status tfe_sample_tokens(const void *logits, int32_t dtype, int32_t B, int32
  *   loss, lse        DEVICE float [N].  Sums run in fp32 and are joined in fp64; each result is rounded once.
  *   grad_loss        DEVICE float [N]: the gradient that arrives at each row's loss.
  *   grad_logits      DEVICE [N][ld_grad] of the logits' type, rounded once; may be the logits themselves (same
- *                    pointer and ld_grad = ld), and must not touch them otherwise.  Elements beyond V stay as they were.
+ *                    pointer and ld_grad = ld), and must not touch them otherwise, nor any other operand (refused).
+ *                    Elements beyond V stay as they were.
  * A row without a teacher weight, or without an unmasked logit, has loss 0 and gradient 0 (lse = -inf for the
  * latter), and so has a row whose grad_loss is 0.  A masked logit has probability 0; a teacher weight on it makes the
  * loss +inf and its gradient -grad_loss * tau * q.  NaN propagates.  One launch each.  Errors: INVALID_ARG, CUDA.

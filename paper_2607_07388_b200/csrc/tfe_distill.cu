@@ -440,15 +440,17 @@ tfe_status tfe_distill_backward(const void *logits, int32_t dtype, int32_t N, in
     if (N == 0) return TFE_OK;
     if (!lse || !grad_loss) return TFE_ERR_INVALID_ARG;
     // the same rows in place, or buffers that do not touch
-    if (grad_logits == logits) {
-        if (ld_grad != ld) return TFE_ERR_INVALID_ARG;
-    } else {
-        const uintptr_t a0 = reinterpret_cast<uintptr_t>(logits), b0 = reinterpret_cast<uintptr_t>(grad_logits);
-        const uintptr_t es = elem_size(dtype);
-        const uintptr_t a1 = a0 + ((uintptr_t)(N - 1) * (uintptr_t)ld + (uintptr_t)V) * es;
-        const uintptr_t b1 = b0 + ((uintptr_t)(N - 1) * (uintptr_t)ld_grad + (uintptr_t)V) * es;
-        if (a0 < b1 && b0 < a1) return TFE_ERR_INVALID_ARG;
-    }
+    const uintptr_t es = elem_size(dtype), out = reinterpret_cast<uintptr_t>(grad_logits);
+    const uintptr_t out_bytes = ((uintptr_t)(N - 1) * (uintptr_t)ld_grad + (uintptr_t)V) * es;
+    auto touches = [&](const void *operand, uintptr_t bytes) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(operand);
+        return at < out + out_bytes && out < at + bytes;
+    };
+    if (grad_logits == logits ? ld_grad != ld : touches(logits, ((uintptr_t)(N - 1) * (uintptr_t)ld + (uintptr_t)V) * es)) return TFE_ERR_INVALID_ARG;
+    const uintptr_t teacher_bytes = (uintptr_t)N * (uintptr_t)K * 4;
+    if (touches(teacher_ids, teacher_bytes) || touches(teacher_logits, teacher_bytes) || touches(lse, (uintptr_t)N * 4) ||
+        touches(grad_loss, (uintptr_t)N * 4))
+        return TFE_ERR_INVALID_ARG;
     int sms = 0;
     if (tfe_status st = device_sms(&sms)) return st;
     DistillParams p{};

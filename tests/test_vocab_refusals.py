@@ -102,3 +102,15 @@ def test_wait_limit_of_the_product(tfe):
     L = tfe.lib()
     assert L.tfe_matmul_fp8_wait_limit((1 << 22) + 1) == tfe.TFE_ERR_INVALID_ARG
     assert L.tfe_matmul_fp8_wait_limit(1 << 22) == L.tfe_matmul_fp8_wait_limit(-1) == tfe.TFE_OK
+
+
+def test_gradient_on_its_other_operands_is_refused(tfe):
+    """A gradient that would be written over the teacher's entries, the log-sum-exps or the incoming gradient."""
+    L, Q = tfe.lib(), 16 * P
+
+    def backward(ids=P, t=2 * P, lse=3 * P, g=4 * P, grad=Q, V=8):
+        return L.tfe_distill_backward(5 * P, 1, 2, V, V, ids, t, 4, 1.0, lse, g, grad, V, None)
+
+    for name, size in (("ids", 32), ("t", 32), ("lse", 8), ("g", 8)):
+        for at in (Q, Q + 60, Q - size + 4):
+            assert backward(**{name: at}) == tfe.TFE_ERR_INVALID_ARG, (name, at)
