@@ -283,6 +283,12 @@ def _vector(t: torch.Tensor, shape, dtype, device, what: str) -> int:
     return t.data_ptr()
 
 
+def _written(out: torch.Tensor):
+    """Tells autograd that the caller's tensor has new contents, as torch's own in-place operations do."""
+    if not out.is_inference():
+        torch.autograd.graph.increment_version(out)
+
+
 def quantize_fp8(x: torch.Tensor, block_rows: int = 1, *, stream=None):
     """(q float8_e4m3fn [R, C], scale float32): `x` [R, C] in 8 bits with a scale for every `block_rows` x 128 values -- 1
     for activations, 128 for weights (see tfe_quantize_fp8)."""
@@ -337,7 +343,8 @@ def _matmul_fp8(a, a_scale, w, w_scale, out_dtype, out, stream):
     kb = -(-k // 128)
     a_s = _vector(a_scale, (m, kb), torch.float32, dev, "a_scale")
     w_s = _vector(w_scale, (-(-n // 128), kb), torch.float32, dev, "w_scale")
-    if out is None:
+    given = out
+    if given is None:
         if out_dtype not in _ROW_DTYPES:
             raise ValueError("out_dtype: bfloat16 or float32")
         out = torch.empty(m, n, dtype=out_dtype, device=dev)
@@ -351,6 +358,8 @@ def _matmul_fp8(a, a_scale, w, w_scale, out_dtype, out, stream):
             if m and at < start + size and start < end:
                 raise ValueError("out: must not touch the operands")
     tfe.tfe_matmul_fp8(a.data_ptr(), lda, a_s, m, w.data_ptr(), ldw, w_s, n, k, out.data_ptr(), kind, ldo, _where(dev, stream))
+    if given is not None:
+        _written(out)
     return out
 
 
@@ -464,13 +473,16 @@ def _distill_backward(grad_loss, logits, teacher_ids, teacher_logits, lse, tau, 
     dev, kind, n, v = logits.device, rows[1], rows[2], rows[3]
     g = _vector(grad_loss, (n,), torch.float32, dev, "grad_loss")
     norm = _vector(lse, (n,), torch.float32, dev, "lse")
-    if out is None:
+    given = out
+    if given is None:
         out, ld_out = logits.new_empty(n, v), v
     else:
         on, ov, ld_out, out_kind = _row_matrix(out, "out")
         if on != n or ov != v or out_kind != kind or out.device != dev:
             raise ValueError("out: the logits' shape, type and device are needed")
     tfe.tfe_distill_backward(*rows, tau, norm, g, out.data_ptr(), ld_out, _where(dev, stream))
+    if given is not None:
+        _written(out)
     return out
 
 

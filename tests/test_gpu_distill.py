@@ -272,3 +272,29 @@ def test_empty_batch_and_refusals():
     overlap = torch.as_strided(store, (4, 64), (64, 1), 32)
     with pytest.raises(tfe.TfeError):                                   # touches the logits without being them
         engine.distill_backward(g, torch.as_strided(store, (4, 64), (64, 1), 0), ids, t, lse, 1.0, out=overlap)
+
+
+def test_autograd_sees_what_is_written_over():
+    """A tensor that a graph has saved and a call's `out` then overwrites: backward refuses, as after torch's own in-place operations."""
+    from paper_2607_07388_b200 import engine
+    z, ids, t, g = (x.to(DEV) for x in make(3, 4, 200, 3, "f32"))
+    zr = z.clone().requires_grad_()
+    loss = engine.distill_loss(zr, ids, t, 1.0)
+    _, lse = engine.distill_forward(zr.detach(), ids, t, 1.0)
+    engine.distill_backward(g, zr.detach(), ids, t, lse, 1.0, out=zr.detach())
+    with pytest.raises(RuntimeError):
+        loss.sum().backward()
+    zr = z.clone().requires_grad_()
+    loss = engine.distill_loss(zr, ids, t, 1.0)
+    a, s = engine.quantize_fp8(torch.ones((4, 64), device=DEV))
+    w, ws = engine.quantize_fp8(torch.ones((200, 64), device=DEV), 128)
+    engine.matmul_fp8(a, s, w, ws, out=zr.detach())
+    with pytest.raises(RuntimeError):
+        loss.sum().backward()
+    with torch.inference_mode():
+        z2 = z.clone()
+        _, lse = engine.distill_forward(z2, ids, t, 1.0)
+        want = engine.distill_backward(g, z2, ids, t, lse, 1.0)
+        assert torch.equal(engine.distill_backward(g, z2, ids, t, lse, 1.0, out=z2), want)
+    engine.distill_backward(g, z, ids, t, lse.clone(), 1.0, out=z)          # outside, of an ordinary tensor
+    assert torch.equal(z, want)
