@@ -516,6 +516,9 @@ enum { TFE_DTYPE_BF16 = 0, TFE_DTYPE_F32 = 1 };
  * q = x / scale, the quotients correctly rounded to fp32 and then to the nearest e4m3 (ties to even).  A
  * block that holds an infinity or NaN has it as its scale and reads back as NaN.  One launch.
  *
+ * tfe_quantize_fp8_ld -- the same with q's rows `ldq` bytes apart (C <= ldq <= 2^34; the bytes between them stay as they
+ * were): the operands of tfe_matmul_fp8 have rows a multiple of 16 bytes apart.
+ *
  * tfe_matmul_fp8 --
  *     out[m][n] = sum_b a_scale[m][b] * w_scale[n / 128][b] * (sum of a[m][k] * w[n][k] over block b's 128 k)
  *   a DEVICE e4m3 [M][lda], a_scale DEVICE float [M][kb];  w DEVICE e4m3 [N][ldw], w_scale DEVICE float
@@ -535,11 +538,13 @@ enum { TFE_DTYPE_BF16 = 0, TFE_DTYPE_F32 = 1 };
  * tfe_matmul_fp8_wait_limit -- polls of one barrier after which a wait inside the product gives up, for the calls that
  * follow, of the whole process: 0 (at once) .. 2^22, negative: 2^22, the library's own.  For tests of a caller's handling
  * of failures.
- * Errors of all four: INVALID_ARG, CUDA.
+ * Errors of all five: INVALID_ARG, CUDA.
  */
 #define TFE_FP8_MAX_COLS (1 << 16)
 tfe_status tfe_quantize_fp8(const void *x, int32_t dtype, int32_t R, int32_t C, int64_t ld, int32_t block_rows,
                             void *q, float *scale, void *stream);
+tfe_status tfe_quantize_fp8_ld(const void *x, int32_t dtype, int32_t R, int32_t C, int64_t ld, int32_t block_rows,
+                               void *q, int64_t ldq, float *scale, void *stream);
 tfe_status tfe_matmul_fp8(const void *a, int64_t lda, const float *a_scale, int32_t M, const void *w, int64_t ldw,
                           const float *w_scale, int32_t N, int32_t K, void *out, int32_t out_dtype, int64_t ldo,
                           void *stream);

@@ -36,7 +36,7 @@ EXPORTS = ["tfe_index_build", "tfe_index_build_device", "tfe_cache_install", "tf
            "tfe_cache_stats", "tfe_head_create", "tfe_head_destroy", "tfe_head_topk", "tfe_head_buffers",
            "tfe_head_status", "tfe_head_geometry", "tfe_mine_ngrams", "tfe_mine_workspace_bytes", "tfe_assign_residency", "tfe_stream_copy",
            "tfe_cache_select_tuning", "tfe_distill_forward", "tfe_distill_backward", "tfe_sample_tokens",
-           "tfe_quantize_fp8", "tfe_matmul_fp8", "tfe_matmul_fp8_status", "tfe_matmul_fp8_wait_limit"]
+           "tfe_quantize_fp8", "tfe_quantize_fp8_ld", "tfe_matmul_fp8", "tfe_matmul_fp8_status", "tfe_matmul_fp8_wait_limit"]
 
 
 class TfeConfig(C.Structure):
@@ -122,6 +122,7 @@ def lib() -> C.CDLL:
         L.tfe_cache_select_tuning.argtypes = [vp, i32, i32, i32]
         f32 = C.c_float
         L.tfe_quantize_fp8.argtypes = [vp, i32, i32, i32, i64, i32, vp, vp, vp]
+        L.tfe_quantize_fp8_ld.argtypes = [vp, i32, i32, i32, i64, i32, vp, i64, vp, vp]
         L.tfe_matmul_fp8.argtypes = [vp, i64, vp, i32, vp, i64, vp, i32, i32, vp, i32, i64, vp]
         L.tfe_matmul_fp8_status.argtypes = [C.POINTER(C.c_uint32), vp]
         L.tfe_matmul_fp8_wait_limit.argtypes = [i32]
@@ -134,7 +135,7 @@ def lib() -> C.CDLL:
                      "tfe_cache_policy_enable", "tfe_cache_select_victims", "tfe_cache_select_victims_device",
                      "tfe_cache_stats", "tfe_head_create", "tfe_head_topk", "tfe_head_buffers", "tfe_head_status",
                      "tfe_head_geometry", "tfe_mine_ngrams", "tfe_assign_residency", "tfe_cache_select_tuning",
-                     "tfe_distill_forward", "tfe_distill_backward", "tfe_sample_tokens", "tfe_quantize_fp8",
+                     "tfe_distill_forward", "tfe_distill_backward", "tfe_sample_tokens", "tfe_quantize_fp8", "tfe_quantize_fp8_ld",
                      "tfe_matmul_fp8", "tfe_matmul_fp8_status", "tfe_matmul_fp8_wait_limit"):
             getattr(L, name).restype = C.c_int
         _lib = L
@@ -494,6 +495,12 @@ def tfe_quantize_fp8(x, dtype: int, R: int, C_: int, ld: int, block_rows: int, q
     st = lib().tfe_quantize_fp8(x, dtype, R, C_, ld, block_rows, q, scale, _stream(stream))
     if st:
         raise TfeError(st, "tfe_quantize_fp8")
+
+
+def tfe_quantize_fp8_ld(x, dtype: int, R: int, C_: int, ld: int, block_rows: int, q, ldq: int, scale, stream=None) -> None:
+    st = lib().tfe_quantize_fp8_ld(x, dtype, R, C_, ld, block_rows, q, ldq, scale, _stream(stream))
+    if st:
+        raise TfeError(st, "tfe_quantize_fp8_ld")
 
 
 def tfe_matmul_fp8(a, lda: int, a_scale, M: int, w, ldw: int, w_scale, N: int, K: int, out, out_dtype: int, ldo: int,

@@ -44,7 +44,7 @@ constexpr int kGroupLanes = 16;                 // lanes that share a group of 1
 struct QuantParams {
     const void *x; int64_t ld;
     int32_t R, C, kb;                           // kb: groups of 128 columns
-    uint8_t *q;                                 // [R][C]
+    uint8_t *q; int64_t ldq;
     float *scale;
 };
 
@@ -131,7 +131,7 @@ struct Eight {
     template <bool kVector>
     __device__ __forceinline__ void store(const QuantParams &p, int64_t row, int32_t c0, int l, const Divisor &by) const
     {
-        uint8_t *at = p.q + row * p.C + c0;
+        uint8_t *at = p.q + row * p.ldq + c0;
         const uint32_t lo = by.to_e4m3x4(get(0), get(1), get(2), get(3)), hi = by.to_e4m3x4(get(4), get(5), get(6), get(7));
         if constexpr (kVector) {
             if (c0 + 8 * l < p.C) *reinterpret_cast<uint2 *>(at + 8 * l) = make_uint2(lo, hi);
@@ -818,11 +818,17 @@ bool aligned(const void *ptr, uintptr_t to) { return ptr && reinterpret_cast<uin
 
 extern "C" {
 
-tfe_status tfe_quantize_fp8(const void *x, int32_t dtype, int32_t R, int32_t C, int64_t ld, int32_t block_rows, void *q, float *scale, void *stream_)
+tfe_status tfe_quantize_fp8(const void *x, int32_t dtype, int32_t R, int32_t C, int64_t ld, int32_t block_rows, void *q, float *scale, void *stream)
+{
+    return tfe_quantize_fp8_ld(x, dtype, R, C, ld, block_rows, q, C, scale, stream);
+}
+
+tfe_status tfe_quantize_fp8_ld(const void *x, int32_t dtype, int32_t R, int32_t C, int64_t ld, int32_t block_rows, void *q, int64_t ldq, float *scale,
+                               void *stream_)
 {
     if (dtype != TFE_DTYPE_BF16 && dtype != TFE_DTYPE_F32) return TFE_ERR_INVALID_ARG;
     if (block_rows != 1 && block_rows != 128) return TFE_ERR_INVALID_ARG;
-    if (R < 0 || C < 1 || C > TFE_FP8_MAX_COLS || ld < C || ld > (1ll << 34)) return TFE_ERR_INVALID_ARG;
+    if (R < 0 || C < 1 || C > TFE_FP8_MAX_COLS || ld < C || ld > (1ll << 34) || ldq < C || ldq > (1ll << 34)) return TFE_ERR_INVALID_ARG;
     QuantParams p{};
     p.kb = (C + 127) / 128;
     const int64_t groups = ((int64_t)R + block_rows - 1) / block_rows * p.kb;
@@ -830,9 +836,9 @@ tfe_status tfe_quantize_fp8(const void *x, int32_t dtype, int32_t R, int32_t C, 
     if (R == 0) return TFE_OK;
     const int es = dtype == TFE_DTYPE_BF16 ? 2 : 4;
     if (!aligned(x, es) || !q || !aligned(scale, 4)) return TFE_ERR_INVALID_ARG;
-    p.x = x; p.ld = ld; p.R = R; p.C = C; p.q = static_cast<uint8_t *>(q); p.scale = scale;
+    p.x = x; p.ld = ld; p.R = R; p.C = C; p.q = static_cast<uint8_t *>(q); p.ldq = ldq; p.scale = scale;
     // 16-byte loads and 8-byte stores where every row starts on such a boundary
-    const bool vec = aligned(x, 16) && ld * es % 16 == 0 && C % 8 == 0 && aligned(q, 8);
+    const bool vec = aligned(x, 16) && ld * es % 16 == 0 && C % 8 == 0 && aligned(q, 8) && ldq % 8 == 0;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     const unsigned grid = block_rows == 1 ? (unsigned)((groups * kGroupLanes + kQuantThreads - 1) / kQuantThreads) : (unsigned)groups;
     auto go = [&](auto rows_kernel, auto blocks_kernel) {

@@ -291,7 +291,8 @@ def _written(out: torch.Tensor):
 
 def quantize_fp8(x: torch.Tensor, block_rows: int = 1, *, stream=None):
     """(q float8_e4m3fn [R, C], scale float32): `x` [R, C] in 8 bits with a scale for every `block_rows` x 128 values -- 1
-    for activations, 128 for weights (see tfe_quantize_fp8)."""
+    for activations, 128 for weights (see tfe_quantize_fp8).  q's rows start on 16-byte boundaries, as matmul_fp8 takes them: where
+    C is not a multiple of 16 they lie that much further apart."""
     if not _here(x.device, stream):
         with _elsewhere(x.device, stream):
             return _quantize_fp8(x, block_rows, stream)
@@ -303,9 +304,12 @@ def _quantize_fp8(x, block_rows, stream):
     if block_rows != 1 and block_rows != 128:
         raise ValueError("block_rows: 1 or 128")
     dev = x.device
-    q = torch.empty(r, c, dtype=torch.float8_e4m3fn, device=dev)
+    pitch = -(-c // 16) * 16
+    q = torch.empty(r, pitch, dtype=torch.float8_e4m3fn, device=dev)
+    if pitch != c:
+        q = q[:, :c]
     scale = torch.empty(-(-r // block_rows), -(-c // 128), dtype=torch.float32, device=dev)
-    tfe.tfe_quantize_fp8(x.data_ptr(), kind, r, c, ld, block_rows, q.data_ptr(), scale.data_ptr(), _where(dev, stream))
+    tfe.tfe_quantize_fp8_ld(x.data_ptr(), kind, r, c, ld, block_rows, q.data_ptr(), pitch, scale.data_ptr(), _where(dev, stream))
     return q, scale
 
 

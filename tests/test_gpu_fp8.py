@@ -348,3 +348,40 @@ def test_output_on_the_scales_is_refused(which):
         with pytest.raises(ValueError):
             engine.matmul_fp8(*args, out=room[first: first + 300].view(3, 100))
     assert torch.equal(engine.matmul_fp8(*args, out=room[size: size + 300].view(3, 100)), want)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("m,n,k", [(1, 1, 1), (3, 200, 8), (40, 129, 1000), (70, 300, 100), (130, 257, 2051)])
+def test_converted_matrices_of_any_width_are_operands(m, n, k, kind):
+    """What quantize_fp8 gives goes into matmul_fp8 as it is, whatever the width."""
+    from paper_2607_07388_b200 import engine
+    rng = np.random.default_rng(m + n + k)
+    x, w = (torch.from_numpy(rng.standard_normal((r, k)).astype(np.float32)).to(TYPES[kind]).to(DEV) for r in (m, n))
+    (q, sa), (qw, sw) = engine.quantize_fp8(x), engine.quantize_fp8(w, 128)
+    for t, src, rows in ((q, x, 1), (qw, w, 128)):
+        assert t.shape == src.shape
+        bits, sign, _ = quantize64(src.float().cpu().numpy(), rows)
+        got = t.view(torch.uint8).cpu().numpy()
+        assert np.array_equal(got & 0x7F, bits) and np.array_equal((got >> 7).astype(bool)[bits > 0], sign[bits > 0])
+    check_product(engine.matmul_fp8(q, sa, qw, sw), q, sa, qw, sw, "f32")
+
+
+@pytest.mark.parametrize("block_rows", [1, 128])
+@pytest.mark.parametrize("c,ldq,off", [(100, 100, 0), (100, 112, 0), (1000, 1008, 0), (1000, 1003, 0), (64, 70, 5), (136, 144, 8)])
+def test_conversion_into_rows_apart(c, ldq, off, block_rows):
+    """Rows of q at any distance; what lies between them is not touched."""
+    from paper_2607_07388_b200 import binding as tfe
+    from paper_2607_07388_b200 import engine
+    r = 131
+    x = torch.randn((r, c), generator=torch.Generator().manual_seed(c)).to(DEV)
+    want, want_scale = engine.quantize_fp8(x, block_rows)
+    store = torch.full((off + r * ldq,), 0x55, dtype=torch.uint8, device=DEV)
+    q = torch.as_strided(store, (r, c), (ldq, 1), off)
+    scale = torch.empty_like(want_scale)
+    tfe.tfe_quantize_fp8_ld(x.data_ptr(), tfe.DTYPE_F32, r, c, c, block_rows, q.data_ptr(), ldq, scale.data_ptr())
+    assert torch.equal(q, want.view(torch.uint8)) and torch.equal(scale, want_scale)
+    q.fill_(0x55)
+    assert (store == 0x55).all()
+    dense = torch.empty((r, c), dtype=torch.uint8, device=DEV)
+    tfe.tfe_quantize_fp8(x.data_ptr(), tfe.DTYPE_F32, r, c, c, block_rows, dense.data_ptr(), scale.data_ptr())
+    assert torch.equal(dense, want.view(torch.uint8))

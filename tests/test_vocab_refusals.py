@@ -114,3 +114,10 @@ def test_gradient_on_its_other_operands_is_refused(tfe):
     for name, size in (("ids", 32), ("t", 32), ("lse", 8), ("g", 8)):
         for at in (Q, Q + 60, Q - size + 4):
             assert backward(**{name: at}) == tfe.TFE_ERR_INVALID_ARG, (name, at)
+
+
+def test_conversion_into_rows_apart(tfe):
+    L = tfe.lib()
+    for ldq in (7, 0, -8, (1 << 34) + 1):
+        assert L.tfe_quantize_fp8_ld(P, 1, 2, 8, 8, 1, P, ldq, P, None) == tfe.TFE_ERR_INVALID_ARG
+    assert L.tfe_quantize_fp8_ld(None, 1, 0, 8, 8, 1, None, 16, None, None) == tfe.TFE_OK
