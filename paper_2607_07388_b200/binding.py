@@ -36,7 +36,7 @@ EXPORTS = ["tfe_index_build", "tfe_index_build_device", "tfe_cache_install", "tf
            "tfe_cache_stats", "tfe_head_create", "tfe_head_destroy", "tfe_head_topk", "tfe_head_buffers",
            "tfe_head_status", "tfe_head_geometry", "tfe_mine_ngrams", "tfe_mine_workspace_bytes", "tfe_assign_residency", "tfe_stream_copy",
            "tfe_cache_select_tuning", "tfe_distill_forward", "tfe_distill_backward", "tfe_sample_tokens",
-           "tfe_quantize_fp8", "tfe_quantize_fp8_ld", "tfe_matmul_fp8", "tfe_matmul_fp8_status", "tfe_matmul_fp8_wait_limit"]
+           "tfe_quantize_fp8", "tfe_quantize_fp8_ld", "tfe_matmul_fp8", "tfe_matmul_fp8_status", "tfe_matmul_fp8_give_up"]
 
 
 class TfeConfig(C.Structure):
@@ -125,7 +125,7 @@ def lib() -> C.CDLL:
         L.tfe_quantize_fp8_ld.argtypes = [vp, i32, i32, i32, i64, i32, vp, i64, vp, vp]
         L.tfe_matmul_fp8.argtypes = [vp, i64, vp, i32, vp, i64, vp, i32, i32, vp, i32, i64, vp]
         L.tfe_matmul_fp8_status.argtypes = [C.POINTER(C.c_uint32), vp]
-        L.tfe_matmul_fp8_wait_limit.argtypes = [i32]
+        L.tfe_matmul_fp8_give_up.argtypes = [i32]
         L.tfe_sample_tokens.argtypes = [vp, i32, i32, i32, i64, C.POINTER(TfeSampleParams), vp, vp, vp, vp]
         L.tfe_distill_forward.argtypes = [vp, i32, i32, i32, i64, vp, vp, i32, f32, vp, vp, vp]
         L.tfe_distill_backward.argtypes = [vp, i32, i32, i32, i64, vp, vp, i32, f32, vp, vp, vp, i64, vp]
@@ -136,7 +136,7 @@ def lib() -> C.CDLL:
                      "tfe_cache_stats", "tfe_head_create", "tfe_head_topk", "tfe_head_buffers", "tfe_head_status",
                      "tfe_head_geometry", "tfe_mine_ngrams", "tfe_assign_residency", "tfe_cache_select_tuning",
                      "tfe_distill_forward", "tfe_distill_backward", "tfe_sample_tokens", "tfe_quantize_fp8", "tfe_quantize_fp8_ld",
-                     "tfe_matmul_fp8", "tfe_matmul_fp8_status", "tfe_matmul_fp8_wait_limit"):
+                     "tfe_matmul_fp8", "tfe_matmul_fp8_status", "tfe_matmul_fp8_give_up"):
             getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -519,5 +519,6 @@ def tfe_matmul_fp8_status(stream=None) -> int:
     return flags.value
 
 
-def tfe_matmul_fp8_wait_limit(polls: int) -> None:
-    _check(lib().tfe_matmul_fp8_wait_limit(polls), "tfe_matmul_fp8_wait_limit")
+def tfe_matmul_fp8_give_up(at_once: bool) -> None:
+    """The waits of the products that follow count as run out from the start, until it is called with False."""
+    _check(lib().tfe_matmul_fp8_give_up(int(at_once)), "tfe_matmul_fp8_give_up")

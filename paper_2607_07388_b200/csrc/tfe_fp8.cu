@@ -216,7 +216,7 @@ constexpr int kMatmulSmem = 224 * 1024;         // stages; the rest of an SM's 2
 constexpr uint32_t kTimeoutLoader = 1u, kTimeoutMma = 2u, kTimeoutScales = 4u, kTimeoutEpilogue = 8u;
 __device__ uint32_t g_matmul_status;
 const float not_a_number = __builtin_nanf("");
-std::atomic<uint32_t> g_wait_limit{TC_WAIT_LIMIT};
+std::atomic<uint32_t> g_give_up{0};
 
 // Only what the caller has been told goes: a bit that another stream sets meanwhile stays.
 __global__ void tfe_matmul_fp8_status_kernel(uint32_t told) { atomicAnd(&g_matmul_status, ~told); }
@@ -227,7 +227,7 @@ struct MatmulParams {
     int32_t rows_per_cta, tail_rows;            // few rows: weight rows of a CTA, rows of its last short tile
     int32_t m_tiles;                            // many rows: tiles of activation rows
     int64_t n_units;                            // ... and all tiles
-    uint32_t wait_limit;                        // polls of one mbarrier before a wait gives up
+    uint32_t give_up;                           // every role's waits count as run out from the start
     const float *a_scale, *b_scale;             // [M][kb], [ceil(N / 128)][kb]
     void *out; int64_t ldo;
 };
@@ -291,7 +291,7 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
         for (int a = 0; a < kBuffers; ++a) { mbar_init(smem_u32(&s_acc_full[a]), 1); mbar_init(smem_u32(&s_acc_empty[a]), kEpilogueWarps); }
         for (int a = 0; a < kScaleRing; ++a) { mbar_init(smem_u32(&s_sc_full[a]), 32); mbar_init(smem_u32(&s_sc_empty[a]), kEpilogueWarps); }
         mbar_init(smem_u32(&s_drain), 1);
-        s_abort = 0;
+        s_abort = p.give_up;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) tmem_alloc(smem_u32(&s_tmem_base), kTmemCols);
@@ -310,14 +310,14 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
             const uint64_t hint_w = 0x12F0000000000000ull;          // evict first: the weights are read once
             const uint64_t hint_a = 0x14F0000000000000ull;          // evict last: the activations are read by every tile
             uint32_t stage = 0, phase = 0, issued = 0;
-            bool ok = true;
+            bool ok = s_abort == 0;
             for (int32_t t = 0; ok && t < n_tiles; ++t) {
                 const int32_t valid = min(kTileRows, n_rows - t * kTileRows);
                 // a short last tile is fetched with the short box: only its rows are read
                 const bool tail = valid < kTileRows && valid == p.tail_rows;
                 const uint32_t w_bytes = tail ? (uint32_t)p.tail_rows * 128u : kTileRows * 128u;
                 for (int32_t kb = 0; kb < p.kb; kb += kGroup) {
-                    if (!mbar_wait(smem_u32(&s_empty[stage]), phase ^ 1u, &s_abort, p.wait_limit)) {
+                    if (!mbar_wait(smem_u32(&s_empty[stage]), phase ^ 1u, &s_abort)) {
                         atomicOr(&g_matmul_status, kTimeoutLoader);
                         s_abort = 1;
                         ok = false;
@@ -345,11 +345,11 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
         if (lane == 0) {
             constexpr uint32_t idesc = umma_idesc_e4m3(kTileRows, TN);
             uint32_t stage = 0, phase = 0, buf = 0, buf_phase = 0;
-            bool ok = true;
+            bool ok = s_abort == 0;
             for (int32_t t = 0; ok && t < n_tiles; ++t) {
                 for (int32_t kb = 0; kb < p.kb; kb += kGroup) {
-                    if (!mbar_wait(smem_u32(&s_acc_empty[buf]), buf_phase ^ 1u, &s_abort, p.wait_limit) ||
-                        !mbar_wait(smem_u32(&s_full[stage]), phase, &s_abort, p.wait_limit)) {
+                    if (!mbar_wait(smem_u32(&s_acc_empty[buf]), buf_phase ^ 1u, &s_abort) ||
+                        !mbar_wait(smem_u32(&s_full[stage]), phase, &s_abort)) {
                         atomicOr(&g_matmul_status, kTimeoutMma);
                         s_abort = 1;
                         ok = false;
@@ -379,7 +379,7 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
     } else if (warp == 2) {
         // ============================ activation scales =======================
         uint32_t st = 0, phase = 0;
-        bool ok = true;
+        bool ok = !__any_sync(0xFFFFFFFFu, s_abort != 0);
         for (int32_t t = 0; ok && t < n_tiles; ++t) {
             for (int32_t kb = 0; kb < p.kb; kb += kGroup) {
                 constexpr int kPer = (TN + 31) / 32;
@@ -389,7 +389,7 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
 #pragma unroll
                     for (int c = 0; c < kPer; ++c)
                         v[g][c] = c * 32 + lane < p.M && kb + g < p.kb ? __ldg(p.a_scale + (int64_t)(c * 32 + lane) * p.kb + kb + g) : 0.f;
-                ok = mbar_wait(smem_u32(&s_sc_empty[st]), phase ^ 1u, &s_abort, p.wait_limit);
+                ok = mbar_wait(smem_u32(&s_sc_empty[st]), phase ^ 1u, &s_abort);
                 if (!__all_sync(0xFFFFFFFFu, ok)) {
                     if (lane == 0) atomicOr(&g_matmul_status, kTimeoutScales);
                     s_abort = 1;
@@ -411,9 +411,10 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
         const int32_t c0 = ((warp - 3) >> 2) * kCols;               // this warp's columns
         const int32_t row_in_tile = (int32_t)(quarter * 32u) + lane;
         uint32_t st = 0, phase = 0, buf = 0, buf_phase = 0;
-        bool ok = true;
+        bool ok = !__any_sync(0xFFFFFFFFu, s_abort != 0);
+        if (!ok && lane == 0) atomicOr(&g_matmul_status, kTimeoutEpilogue);
         int32_t t = 0;
-        for (; t < n_tiles; ++t) {
+        for (; ok && t < n_tiles; ++t) {
             const int64_t n0 = r0 + (int64_t)t * kTileRows;
             const int32_t valid = min(kTileRows, n_rows - t * kTileRows);
             float2 acc[kCols / 2];
@@ -431,7 +432,7 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
 #pragma unroll
                 for (int g = 0; g < kGroup; ++g) sb[g] = sb_next[g];
                 fetch(kb + kGroup);
-                ok = mbar_wait(smem_u32(&s_sc_full[st]), phase, &s_abort, p.wait_limit) && mbar_wait(smem_u32(&s_acc_full[buf]), buf_phase, &s_abort, p.wait_limit);
+                ok = mbar_wait(smem_u32(&s_sc_full[st]), phase, &s_abort) && mbar_wait(smem_u32(&s_acc_full[buf]), buf_phase, &s_abort);
                 if (!__all_sync(0xFFFFFFFFu, ok)) {
                     if (lane == 0) atomicOr(&g_matmul_status, kTimeoutEpilogue);
                     s_abort = 1;
@@ -600,7 +601,7 @@ tfe_matmul_fp8_many_kernel(const __grid_constant__ CUtensorMap map_w, const __gr
         for (int s = 0; s < kStages; ++s) { mbar_init(smem_u32(&s_full[s]), 1); mbar_init(smem_u32(&s_empty[s]), 1); }
         for (int a = 0; a < kBuffers; ++a) { mbar_init(smem_u32(&s_acc_full[a]), 1); mbar_init(smem_u32(&s_acc_empty[a]), kManyEpilogueWarps); }
         mbar_init(smem_u32(&s_drain), 1);
-        s_abort = 0;
+        s_abort = p.give_up;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) tmem_alloc(smem_u32(&s_tmem_base), 512);
@@ -616,12 +617,12 @@ tfe_matmul_fp8_many_kernel(const __grid_constant__ CUtensorMap map_w, const __gr
             // ============================ TMA producer ============================
             const uint64_t hint = 0x14F0000000000000ull;            // evict last: both operands are read by other tiles too
             uint32_t stage = 0, phase = 0, issued = 0;
-            bool ok = true;
+            bool ok = s_abort == 0;
             for (int64_t u = blockIdx.x; ok && u < p.n_units; u += gridDim.x) {
                 const int64_t nt = u / p.m_tiles;
                 const int32_t n0 = (int32_t)(nt * kN), m0 = (int32_t)(u - nt * p.m_tiles) * kTileRows;
                 for (int32_t kb = 0; kb < p.kb; ++kb) {
-                    if (!mbar_wait(smem_u32(&s_empty[stage]), phase ^ 1u, &s_abort, p.wait_limit)) {
+                    if (!mbar_wait(smem_u32(&s_empty[stage]), phase ^ 1u, &s_abort)) {
                         atomicOr(&g_matmul_status, kTimeoutLoader);
                         s_abort = 1;
                         ok = false;
@@ -644,11 +645,11 @@ tfe_matmul_fp8_many_kernel(const __grid_constant__ CUtensorMap map_w, const __gr
             // ============================ MMA issuer ==============================
             constexpr uint32_t idesc = umma_idesc_e4m3(kTileRows, kN);
             uint32_t stage = 0, phase = 0, buf = 0, buf_phase = 0;
-            bool ok = true;
+            bool ok = s_abort == 0;
             for (int64_t u = blockIdx.x; ok && u < p.n_units; u += gridDim.x)
                 for (int32_t kb = 0; kb < p.kb; ++kb) {
-                    if (!mbar_wait(smem_u32(&s_acc_empty[buf]), buf_phase ^ 1u, &s_abort, p.wait_limit) ||
-                        !mbar_wait(smem_u32(&s_full[stage]), phase, &s_abort, p.wait_limit)) {
+                    if (!mbar_wait(smem_u32(&s_acc_empty[buf]), buf_phase ^ 1u, &s_abort) ||
+                        !mbar_wait(smem_u32(&s_full[stage]), phase, &s_abort)) {
                         atomicOr(&g_matmul_status, kTimeoutMma);
                         s_abort = 1;
                         ok = false;
@@ -678,9 +679,10 @@ tfe_matmul_fp8_many_kernel(const __grid_constant__ CUtensorMap map_w, const __gr
         const int32_t c0 = (e >> 2) * kCols;                        // this warp's columns, all in one scale block of the weights
         const uint32_t row_smem = smem_base + kStages * kManyStageBytes + (uint32_t)((e * 32 + lane) * kRowPitch);
         uint32_t buf = 0, buf_phase = 0;
-        bool ok = true;
+        bool ok = !__any_sync(0xFFFFFFFFu, s_abort != 0);
+        if (!ok && lane == 0) atomicOr(&g_matmul_status, kTimeoutEpilogue);
         int64_t u = blockIdx.x;
-        for (; u < p.n_units; u += gridDim.x) {
+        for (; ok && u < p.n_units; u += gridDim.x) {
             const int64_t nt = u / p.m_tiles;
             const int64_t n0 = nt * kN + c0;
             const int32_t m0 = (int32_t)(u - nt * p.m_tiles) * kTileRows + (int32_t)quarter * 32;
@@ -708,7 +710,7 @@ tfe_matmul_fp8_many_kernel(const __grid_constant__ CUtensorMap map_w, const __gr
                 }
                 const float2 scale = make_float2(scales[0], scales[0]);
                 scales[0] = scales[1]; scales[1] = scales[2]; scales[2] = scales[3];
-                ok = mbar_wait(smem_u32(&s_acc_full[buf]), buf_phase, &s_abort, p.wait_limit);
+                ok = mbar_wait(smem_u32(&s_acc_full[buf]), buf_phase, &s_abort);
                 if (!__all_sync(0xFFFFFFFFu, ok)) {
                     if (lane == 0) atomicOr(&g_matmul_status, kTimeoutEpilogue);
                     s_abort = 1;
@@ -867,7 +869,7 @@ tfe_status tfe_matmul_fp8(const void *a, int64_t lda, const float *a_scale, int3
     MatmulParams p{};
     p.M = M; p.N = N; p.kb = (K + kBlockK - 1) / kBlockK;
     p.a_scale = a_scale; p.b_scale = w_scale; p.out = out; p.ldo = ldo;
-    p.wait_limit = g_wait_limit.load(std::memory_order_relaxed);
+    p.give_up = g_give_up.load(std::memory_order_relaxed);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     CUtensorMap map_w, map_a;
     if (M > kFewRows)
@@ -902,10 +904,9 @@ tfe_status tfe_matmul_fp8_status(uint32_t *device_flags, void *stream_)
     return TFE_ERR_INTERNAL;
 }
 
-tfe_status tfe_matmul_fp8_wait_limit(int32_t polls)
+tfe_status tfe_matmul_fp8_give_up(int32_t at_once)
 {
-    if (polls > (int32_t)TC_WAIT_LIMIT) return TFE_ERR_INVALID_ARG;
-    g_wait_limit.store(polls < 0 ? TC_WAIT_LIMIT : (uint32_t)polls, std::memory_order_relaxed);
+    g_give_up.store(at_once != 0, std::memory_order_relaxed);
     return TFE_OK;
 }
 

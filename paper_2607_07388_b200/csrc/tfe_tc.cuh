@@ -38,10 +38,10 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity)
         : "memory");
     return ok != 0;
 }
-// Bounded wait: gives up after `limit` polls or when another role has given up.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t *abort_flag, uint32_t limit = TC_WAIT_LIMIT)
+// Bounded wait: gives up after TC_WAIT_LIMIT polls or when another role has given up.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t *abort_flag)
 {
-    for (uint32_t i = 0; i < limit; ++i) {
+    for (uint32_t i = 0; i < TC_WAIT_LIMIT; ++i) {
         if (mbar_try_wait(bar, parity)) return true;
         if ((i & 1023u) == 1023u && *abort_flag) return false;
     }

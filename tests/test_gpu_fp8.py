@@ -306,7 +306,7 @@ def test_conversion_of_more_groups_than_32_bits_of_threads():
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
 @pytest.mark.parametrize("m,n,k", [(3, 1003, 640), (40, 30_001, 256), (64, 77, 128), (300, 1003, 640), (65, 90_001, 128)])
 def test_waits_that_run_out(m, n, k, kind):
-    """Every wait of the kernel gives up at once: all results are NaN, nothing beside them is touched, the status tells once, and the
+    """Every wait of the kernel counts as run out: all results are NaN, nothing beside them is touched, the status tells once, and the
     next product is right again."""
     from paper_2607_07388_b200 import binding as tfe
     from paper_2607_07388_b200 import engine
@@ -315,12 +315,12 @@ def test_waits_that_run_out(m, n, k, kind):
     store = torch.full((m, n + 8), 5.0, dtype=TYPES[kind], device=DEV)
     out = store[:, 3:n + 3]
     assert engine.matmul_fp8_status() == 0
-    tfe.tfe_matmul_fp8_wait_limit(0)
+    tfe.tfe_matmul_fp8_give_up(True)
     try:
         engine.matmul_fp8(*args, out=out)
         torch.cuda.synchronize()
     finally:
-        tfe.tfe_matmul_fp8_wait_limit(-1)
+        tfe.tfe_matmul_fp8_give_up(False)
     assert torch.isnan(out).all()
     token, prob = engine.sample_tokens(out, torch.full((m,), 0.5, device=DEV))
     assert (token == -1).all() and (prob == 0).all()

@@ -98,12 +98,6 @@ def test_sizes_beyond_32_bits():
     assert engine._fp8_matrix(matrix((1 << 31) - 1, 16, torch.float8_e4m3fn), "a") == ((1 << 31) - 1, 16, 16)
 
 
-def test_wait_limit_of_the_product(tfe):
-    L = tfe.lib()
-    assert L.tfe_matmul_fp8_wait_limit((1 << 22) + 1) == tfe.TFE_ERR_INVALID_ARG
-    assert L.tfe_matmul_fp8_wait_limit(1 << 22) == L.tfe_matmul_fp8_wait_limit(-1) == tfe.TFE_OK
-
-
 def test_gradient_on_its_other_operands_is_refused(tfe):
     """A gradient that would be written over the teacher's entries, the log-sum-exps or the incoming gradient."""
     L, Q = tfe.lib(), 16 * P
