@@ -365,3 +365,29 @@ def test_top_k_among_infinite_logits(kind, v):
             check(z, np.full(b, u), k=np.full(b, k), p=np.full(b, 0.7), T=np.full(b, 0.5))
     check(z, rng.random(b), k=np.full(b, 2), T=np.full(b, np.inf))
     check(z, rng.random(b), k=np.full(b, 2), mp=np.full(b, 0.3), T=np.full(b, 1e-12))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("b,v", [(2, 151_936), (6, 50_000), (70, 9001)])
+def test_calls_at_the_same_time(kind, b, v):
+    """Two streams draw from different rows by different numbers, over and over: each gets what it gets alone."""
+    from paper_2607_07388_b200 import engine
+    calls = []
+    for i in range(2):
+        z, rng = logits(17 * b + i, b, v, kind, 1.5)
+        u = torch.from_numpy(rng.random(b).astype(np.float32)).to(DEV)
+        p = torch.from_numpy(rng.choice([0.8, 0.95, 1.0], b).astype(np.float32)).to(DEV)
+        calls.append((z.to(DEV), u, p))
+    want = [engine.sample_tokens(z, u, top_p=p) for z, u, p in calls]
+    assert not torch.equal(want[0][0], want[1][0])
+    streams = [torch.cuda.Stream() for _ in calls]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    got = [[], []]
+    for _ in range(10):
+        for i, (z, u, p) in enumerate(calls):
+            got[i].append(engine.sample_tokens(z, u, top_p=p, stream=streams[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for token, prob in got[i]:
+            assert torch.equal(token, want[i][0]) and torch.equal(prob, want[i][1])
