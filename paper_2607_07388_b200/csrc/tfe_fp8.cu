@@ -291,7 +291,7 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
         for (int a = 0; a < kBuffers; ++a) { mbar_init(smem_u32(&s_acc_full[a]), 1); mbar_init(smem_u32(&s_acc_empty[a]), kEpilogueWarps); }
         for (int a = 0; a < kScaleRing; ++a) { mbar_init(smem_u32(&s_sc_full[a]), 32); mbar_init(smem_u32(&s_sc_empty[a]), kEpilogueWarps); }
         mbar_init(smem_u32(&s_drain), 1);
-        s_abort = p.give_up;
+        s_abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) tmem_alloc(smem_u32(&s_tmem_base), kTmemCols);
@@ -310,7 +310,7 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
             const uint64_t hint_w = 0x12F0000000000000ull;          // evict first: the weights are read once
             const uint64_t hint_a = 0x14F0000000000000ull;          // evict last: the activations are read by every tile
             uint32_t stage = 0, phase = 0, issued = 0;
-            bool ok = s_abort == 0;
+            bool ok = !p.give_up;
             for (int32_t t = 0; ok && t < n_tiles; ++t) {
                 const int32_t valid = min(kTileRows, n_rows - t * kTileRows);
                 // a short last tile is fetched with the short box: only its rows are read
@@ -345,7 +345,7 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
         if (lane == 0) {
             constexpr uint32_t idesc = umma_idesc_e4m3(kTileRows, TN);
             uint32_t stage = 0, phase = 0, buf = 0, buf_phase = 0;
-            bool ok = s_abort == 0;
+            bool ok = !p.give_up;
             for (int32_t t = 0; ok && t < n_tiles; ++t) {
                 for (int32_t kb = 0; kb < p.kb; kb += kGroup) {
                     if (!mbar_wait(smem_u32(&s_acc_empty[buf]), buf_phase ^ 1u, &s_abort) ||
@@ -379,7 +379,7 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
     } else if (warp == 2) {
         // ============================ activation scales =======================
         uint32_t st = 0, phase = 0;
-        bool ok = !__any_sync(0xFFFFFFFFu, s_abort != 0);
+        bool ok = !p.give_up;
         for (int32_t t = 0; ok && t < n_tiles; ++t) {
             for (int32_t kb = 0; kb < p.kb; kb += kGroup) {
                 constexpr int kPer = (TN + 31) / 32;
@@ -411,7 +411,7 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
         const int32_t c0 = ((warp - 3) >> 2) * kCols;               // this warp's columns
         const int32_t row_in_tile = (int32_t)(quarter * 32u) + lane;
         uint32_t st = 0, phase = 0, buf = 0, buf_phase = 0;
-        bool ok = !__any_sync(0xFFFFFFFFu, s_abort != 0);
+        bool ok = !p.give_up;
         if (!ok && lane == 0) atomicOr(&g_matmul_status, kTimeoutEpilogue);
         int32_t t = 0;
         for (; ok && t < n_tiles; ++t) {
@@ -601,7 +601,7 @@ tfe_matmul_fp8_many_kernel(const __grid_constant__ CUtensorMap map_w, const __gr
         for (int s = 0; s < kStages; ++s) { mbar_init(smem_u32(&s_full[s]), 1); mbar_init(smem_u32(&s_empty[s]), 1); }
         for (int a = 0; a < kBuffers; ++a) { mbar_init(smem_u32(&s_acc_full[a]), 1); mbar_init(smem_u32(&s_acc_empty[a]), kManyEpilogueWarps); }
         mbar_init(smem_u32(&s_drain), 1);
-        s_abort = p.give_up;
+        s_abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) tmem_alloc(smem_u32(&s_tmem_base), 512);
@@ -617,7 +617,7 @@ tfe_matmul_fp8_many_kernel(const __grid_constant__ CUtensorMap map_w, const __gr
             // ============================ TMA producer ============================
             const uint64_t hint = 0x14F0000000000000ull;            // evict last: both operands are read by other tiles too
             uint32_t stage = 0, phase = 0, issued = 0;
-            bool ok = s_abort == 0;
+            bool ok = !p.give_up;
             for (int64_t u = blockIdx.x; ok && u < p.n_units; u += gridDim.x) {
                 const int64_t nt = u / p.m_tiles;
                 const int32_t n0 = (int32_t)(nt * kN), m0 = (int32_t)(u - nt * p.m_tiles) * kTileRows;
@@ -645,7 +645,7 @@ tfe_matmul_fp8_many_kernel(const __grid_constant__ CUtensorMap map_w, const __gr
             // ============================ MMA issuer ==============================
             constexpr uint32_t idesc = umma_idesc_e4m3(kTileRows, kN);
             uint32_t stage = 0, phase = 0, buf = 0, buf_phase = 0;
-            bool ok = s_abort == 0;
+            bool ok = !p.give_up;
             for (int64_t u = blockIdx.x; ok && u < p.n_units; u += gridDim.x)
                 for (int32_t kb = 0; kb < p.kb; ++kb) {
                     if (!mbar_wait(smem_u32(&s_acc_empty[buf]), buf_phase ^ 1u, &s_abort) ||
@@ -679,7 +679,7 @@ tfe_matmul_fp8_many_kernel(const __grid_constant__ CUtensorMap map_w, const __gr
         const int32_t c0 = (e >> 2) * kCols;                        // this warp's columns, all in one scale block of the weights
         const uint32_t row_smem = smem_base + kStages * kManyStageBytes + (uint32_t)((e * 32 + lane) * kRowPitch);
         uint32_t buf = 0, buf_phase = 0;
-        bool ok = !__any_sync(0xFFFFFFFFu, s_abort != 0);
+        bool ok = !p.give_up;
         if (!ok && lane == 0) atomicOr(&g_matmul_status, kTimeoutEpilogue);
         int64_t u = blockIdx.x;
         for (; ok && u < p.n_units; u += gridDim.x) {
