@@ -264,7 +264,7 @@ def _row_matrix(t: torch.Tensor, what: str):
     if kind is None or not t.is_cuda or t.dim() != 2:
         raise ValueError(f"{what}: a 2-D bf16 or fp32 CUDA tensor is needed")
     n, v = t.shape
-    if n > _SIZE_MAX or v > _SIZE_MAX:
+    if (n | v) > _SIZE_MAX:
         raise ValueError(f"{what}: more than 2^31 - 1 rows or columns")
     ld, step = t.stride()
     if v < 1 or (step != 1 and v != 1):
@@ -304,10 +304,8 @@ def _quantize_fp8(x, block_rows, stream):
     if block_rows != 1 and block_rows != 128:
         raise ValueError("block_rows: 1 or 128")
     dev = x.device
-    pitch = -(-c // 16) * 16
-    q = torch.empty(r, pitch, dtype=torch.float8_e4m3fn, device=dev)
-    if pitch != c:
-        q = q[:, :c]
+    pitch = (c + 15) & ~15
+    q = torch.empty_strided((r, c), (pitch, 1), dtype=torch.float8_e4m3fn, device=dev)
     scale = torch.empty(-(-r // block_rows), -(-c // 128), dtype=torch.float32, device=dev)
     tfe.tfe_quantize_fp8_ld(x.data_ptr(), kind, r, c, ld, block_rows, q.data_ptr(), pitch, scale.data_ptr(), _where(dev, stream))
     return q, scale
@@ -317,7 +315,7 @@ def _fp8_matrix(t: torch.Tensor, what: str):
     if not t.is_cuda or t.dim() != 2 or t.dtype != torch.float8_e4m3fn:
         raise ValueError(f"{what}: a 2-D float8_e4m3fn CUDA tensor is needed")
     n, k = t.shape
-    if n > _SIZE_MAX or k > _SIZE_MAX:
+    if (n | k) > _SIZE_MAX:
         raise ValueError(f"{what}: more than 2^31 - 1 rows or columns")
     ld, step = t.stride()
     if n <= 1:
