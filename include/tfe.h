@@ -604,7 +604,9 @@ tfe_status tfe_sample_tokens(const void *logits, int32_t dtype, int32_t B, int32
  *                    Elements beyond V stay as they were.
  * A row without a teacher weight, or without an unmasked logit, has loss 0 and gradient 0 (lse = -inf for the
  * latter), and so has a row whose grad_loss is 0.  A masked logit has probability 0; a teacher weight on it makes the
- * loss +inf and its gradient -grad_loss * tau * q.  NaN propagates.  One launch each.  Errors: INVALID_ARG, CUDA.
+ * loss +inf and its gradient -grad_loss * tau * q.  NaN propagates, and a logit of +inf makes its row's results NaN.  The loss
+ * keeps its precision for logits of any size; the gradient's probabilities are relative to lse as it is given, which
+ * as an fp32 number is off by up to |lse| 2^-24.  One launch each.  Errors: INVALID_ARG, CUDA.
  */
 #define TFE_DISTILL_MAX_TOP 1024
 tfe_status tfe_distill_forward(const void *logits, int32_t dtype, int32_t N, int32_t V, int64_t ld,

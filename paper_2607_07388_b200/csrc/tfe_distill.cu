@@ -154,6 +154,19 @@ __device__ __forceinline__ void stream_row(const T *row, int64_t n, int slice, i
     s = sum.x + sum.y;
 }
 
+// The rounding of a reference beyond this is whole powers of two of every term, which leave fp32 from about 2^31 on (logits of -1e10
+// where a mask has left nothing, say): such a row is summed once more, relative to its largest logit itself.
+constexpr float kFarRef = 0x1p24f;
+__device__ __forceinline__ bool far_row(float m, float c) { return m > kMasked && fabsf(ref(m, c)) >= kFarRef; }
+template <typename T>
+__device__ __noinline__ float far_sum(const T *row, int64_t n, int slice, int slices, int tid, int threads, float c, float m)
+{
+    const int64_t e0 = n * slice / slices, e1 = n * (slice + 1) / slices;
+    float s = 0.f;
+    for (int64_t i = e0 + tid; i < e1; i += threads) s += exp2_approx((Elem<T>::get(row + i) - m) * c);
+    return s;
+}
+
 // sum_k q_k (ln q_k - z[id_k] / tau) in 64 bits, on every lane; +inf where a teacher weight meets a masked logit
 template <typename T>
 __device__ __forceinline__ double teacher_term(const DistillParams &p, const T *row, int64_t r, int lane, bool &any)
@@ -184,10 +197,10 @@ __device__ __forceinline__ void finish_row(const DistillParams &p, int64_t r, fl
 {
     // m still at the mask value: no logit above it (s counts masked ones then); NaN has made s NaN.  s is relative to the rounded
     // reference; relative to the largest logit it is s 2^(ref - m c), and every ratio exp2((z - m) c) in it has c's error on a
-    // small difference only.
+    // small difference only.  A far row's s is relative to the largest logit already.
     const bool empty = m <= kMasked && !isnan(s);
-    const double lse = empty ? -INFINITY
-                             : (double)m / (double)p.tau + log((double)s) + ((double)ref(m, c) - (double)m * (double)c) * 0.6931471805599453;
+    const double shift = far_row(m, c) ? 0.0 : ((double)ref(m, c) - (double)m * (double)c) * 0.6931471805599453;
+    const double lse = empty ? -INFINITY : (double)m / (double)p.tau + log((double)s) + shift;
     p.lse[r] = (float)lse;
     p.loss[r] = !any || empty ? 0.f : (float)((double)p.tau * (double)p.tau * (term + lse));
 }
@@ -208,12 +221,18 @@ tfe_distill_forward_kernel(const DistillParams p)
         stream_row<T, 2>(row, p.V, 0, 1, lane, 32, c, m, s);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) fold(m, s, __shfl_xor_sync(0xFFFFFFFFu, m, o), __shfl_xor_sync(0xFFFFFFFFu, s, o), c);
+        if (far_row(m, c)) {
+            s = far_sum(row, p.V, 0, 1, lane, 32, c, m);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+        }
         bool any;
         const double term = teacher_term<T>(p, row, r, lane, any);
         if (lane == 0) finish_row(p, r, m, s, c, term, any);
     } else {
         __shared__ float s_m[kBlock / 32], s_s[kBlock / 32];
         __shared__ float2 s_part;
+        __shared__ float s_far;
         const int64_t r = blockIdx.x / p.slices;
         const int slice = (int)(blockIdx.x % p.slices);
         const T *row = static_cast<const T *>(p.logits) + r * p.ld;
@@ -231,7 +250,10 @@ tfe_distill_forward_kernel(const DistillParams p)
             s = lane < kBlock / 32 ? s_s[lane] : 0.f;
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) fold(m, s, __shfl_xor_sync(0xFFFFFFFFu, m, o), __shfl_xor_sync(0xFFFFFFFFu, s, o), c);
-            if (lane == 0) s_part = make_float2(m, s);
+            if (lane == 0) {
+                s_part = make_float2(m, s);
+                s_far = p.slices == 1 && far_row(m, c) ? m : kMasked;
+            }
         }
         if (p.slices > 1) {
             cg::cluster_group cluster = cg::this_cluster();
@@ -241,8 +263,32 @@ tfe_distill_forward_kernel(const DistillParams p)
                     const float2 other = *cluster.map_shared_rank(&s_part, b);
                     fold(m, s, other.x, other.y, c);
                 }
+                if (far_row(m, c))
+                    for (int b = 0; b < p.slices; ++b) *cluster.map_shared_rank(&s_far, b) = m;
             }
             cluster.sync();                 // a block's shared memory lives until its partner has read it
+        } else {
+            __syncthreads();
+        }
+        const float row_m = s_far;
+        if (row_m > kMasked) {              // the row's largest logit, if the row is a far one: the same in every thread
+            float part = far_sum(row, p.V, slice, p.slices, threadIdx.x, kBlock, c, row_m);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) part += __shfl_xor_sync(0xFFFFFFFFu, part, o);
+            if (lane == 0) s_s[warp] = part;
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                s = 0.f;
+                for (int w = 0; w < kBlock / 32; ++w) s += s_s[w];
+                s_part.y = s;
+            }
+            if (p.slices > 1) {
+                cg::cluster_group cluster = cg::this_cluster();
+                cluster.sync();
+                if (slice == 0 && threadIdx.x == 0)
+                    for (int b = 1; b < p.slices; ++b) s += cluster.map_shared_rank(&s_part, b)->y;
+                cluster.sync();
+            }
         }
         if (slice == 0 && threadIdx.x == 0) finish_row(p, r, m, s, c, term, any);
     }

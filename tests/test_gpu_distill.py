@@ -298,3 +298,47 @@ def test_autograd_sees_what_is_written_over():
         assert torch.equal(engine.distill_backward(g, z2, ids, t, lse, 1.0, out=z2), want)
     engine.distill_backward(g, z, ids, t, lse.clone(), 1.0, out=z)          # outside, of an ordinary tensor
     assert torch.equal(z, want)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("n,v", [(9, 300), (4, 20_000), (400, 20_001), (4, 150_000)])
+def test_logits_far_from_zero(kind, n, v):
+    """Rows whose logits are so large against tau that fp32 holds z / tau to whole units only, or not at all: the loss is a
+    difference and keeps its precision.  Among them rows that a mask of -1e10 has left nothing of."""
+    from paper_2607_07388_b200 import engine
+    rng = np.random.default_rng(n + v)
+    k = 6
+    for size, tau in ((1e6, 1.0), (3e7, 1.0), (1e10, 0.5), (1e10, 1000.0), (3e4, 1e-6), (1e20, 3.0), (2e38, 1.0), (3e38, 1e-6), (3e38, 0.7)):
+        t = torch.tensor(size, dtype=torch.float32).to(TYPES[kind])
+        steps = [t]                                     # the largest logits: a few steps of the type apart
+        for _ in range(4):
+            steps.append(torch.nextafter(steps[-1], torch.tensor(0.0, dtype=TYPES[kind])))
+        steps = torch.stack(steps)
+        z = steps[torch.from_numpy(rng.integers(0, 5, (n, v)))]
+        if size < 1e30:                                 # (below -1e30 they would be masked ones)
+            z[1::2] = -z[1::2]
+        z[0], z[1] = z[0, 0].clone(), z[1, 0].clone()   # equal logits
+        z[2, : v // 2] = torch.finfo(TYPES[kind]).min
+        z[3, v // 3:] = float("-inf")
+        ids = torch.from_numpy(rng.integers(0, v // 3, (n, k)).astype(np.int32)) + v // 2 * (torch.arange(n) == 2)[:, None].int()
+        te = torch.from_numpy(rng.standard_normal((n, k)).astype(np.float32))
+        loss, lse = engine.distill_forward(z.to(DEV), ids.to(DEV), te.to(DEV), tau)
+        # the definition, relative to the largest logit: differences of logits are exact in 64 bits
+        zd = z.to(DEV).double()
+        d = torch.where(zd > MASKED, zd, float("-inf"))
+        top = d.amax(1, keepdim=True)
+        d = (d - top) / tau
+        norm = torch.log(torch.exp(d).sum(1))
+        q = torch.softmax(te.to(DEV).double() / tau, 1)
+        terms = torch.where(q > 0, q * (torch.log(q) - d.gather(1, ids.to(DEV).long()) + norm[:, None]), 0.0)
+        want = tau * tau * terms.sum(1)
+        # the sum: as in `tolerances`; the terms are 64-bit numbers of the size of z / tau, where q-weighted ones cancel
+        far = float(top.abs().max()) / tau
+        tol = tau * tau * (2.0 ** -22 + 3 * 2.0 ** -24 + (v / 32 + 16) * 2.0 ** -24 + (k + 8) * 2.0 ** -52 * far) + 2.0 ** -23 * want.abs()
+        got = loss.double()
+        assert not torch.isnan(got).any() and ((got - want).abs() <= tol).all(), (size, tau, float(((got - want).abs() / tol).max()))
+        e_lse = top[:, 0] / tau + norm
+        assert ((lse.double() - e_lse).abs() <= 2.0 ** -24 * e_lse.abs() + tol / tau ** 2)[e_lse.abs() < 3.4e38].all()
+    z[0, 7] = float("inf")
+    loss, lse = engine.distill_forward(z.to(DEV), ids.to(DEV), te.to(DEV), tau)
+    assert torch.isnan(loss[0]) and torch.isnan(lse[0]) and not torch.isnan(loss[1:]).any()
