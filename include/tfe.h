@@ -498,7 +498,8 @@ tfe_status tfe_assign_residency(const uint32_t *count, int64_t N, int64_t gpu_sl
  * row r starting `ld` elements after row r - 1 (ld >= V, at most 2^34; rows need no alignment beyond the
  * element's own), as fp32 or bf16.  They come from a head (tfe_head_buffers, tfe_matmul_fp8) or from the model
  * itself.  A logit at or below -1e30 is a masked one: -inf, or the lowest value of either type.
- * These calls keep no state (but tfe_matmul_fp8's status word), allocate nothing, never synchronise and may be captured into a CUDA graph; they
+ * These calls keep no state (but tfe_matmul_fp8's status word and switch), allocate nothing, never synchronise (but
+ * tfe_matmul_fp8_status) and may be captured into a CUDA graph; they
  * work on the current device, which has to be the one that holds the buffers.  Calls on different streams are
  * independent.  Argument errors are found on the host before anything is launched.  Results must not touch
  * operands unless a call says that they may.
@@ -524,7 +525,8 @@ enum { TFE_DTYPE_BF16 = 0, TFE_DTYPE_F32 = 1 };
  *   a DEVICE e4m3 [M][lda], a_scale DEVICE float [M][kb];  w DEVICE e4m3 [N][ldw], w_scale DEVICE float
  *   [ceil(N / 128)][kb], kb = ceil(K / 128);  out DEVICE [M][ldo], fp32 or bf16.  0 <= M, 1 <= N <= TFE_ROWS_MAX,
  *   1 <= K <= TFE_FP8_MAX_COLS; a and w 16-byte aligned, lda and ldw multiples of 16.  A block's products are
- *   summed by the tensor cores, blocks in fp32, and the result is rounded once.  Elements of out beyond N stay as
+ *   summed by the tensor cores, blocks in fp32, and the result is rounded once.  The product of a block's two scales is
+ *   formed in fp32 first: below 2^-126 it loses bits, from 2^128 on the results are infinite or NaN.  Elements of out beyond N stay as
  *   they were.  One launch.
  *
  *   Every wait inside the kernel is bounded.  Should one run out, the results that the call has not stored by then are NaN,
@@ -569,7 +571,8 @@ tfe_status tfe_matmul_fp8_give_up(int32_t at_once);
  *   tokens, prob  DEVICE int32 [B], DEVICE float [B] (prob may be NULL).
  * Weights are evaluated in fp64 and summed as whole numbers of a unit, 2^-45 of the greatest weight (beyond 2^17
  * entries coarser by as many bits), so a row's result does not depend on the rest of the batch, on its place in it, or on
- * the order of any addition; an entry that weighs less than half a unit adds nothing and is not drawn.  One launch.
+ * the order of any addition; an entry that weighs less than half a unit adds nothing and is not drawn.  Every entry is
+ * rounded for itself: an end may lie off by half a unit for each entry before it.  One launch.
  * Errors: INVALID_ARG, CUDA.
  */
 #define TFE_SAMPLE_MAX_VOCAB (1 << 24)

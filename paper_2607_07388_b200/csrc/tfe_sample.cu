@@ -24,11 +24,11 @@
 // evaluated in 64 bits (relative error below 1e-14) and summed as 64-bit integers in units of 2^-shift -- exact, and the
 // same in any order.
 //
-// What bounds it: 256 flat rows of 151,936 bf16 logits take 81 us (210 when they go by bins of distance, of about 110
+// What bounds it: 256 flat rows of 151,936 bf16 logits take 82 us (216 as fp32, by bins of distance, of about 110
 // instructions a logit with 15 fp64 ones): 11 us the first read, 32 us the counting -- 10 instructions and an addition in
 // shared memory a logit, and no faster with 2 or 4 loads ahead (86, 84 us) --, 14 us the second look, the rest steps of one
-// block.  One fp32 row takes 28 us, the latency of the steps of a cluster of eight blocks; 64 with k up to 40,000 take 75 us.
-// HBM would need 12, 0.1 and 6 us.
+// block.  One fp32 row takes 29 us, the latency of the steps of a cluster of eight blocks; 64 with settings of their own take
+// 74 us, where a row whose ends need sums weighs all its entries.  HBM would need 12, 0.1 and 6 us.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
