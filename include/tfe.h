@@ -621,6 +621,49 @@ tfe_status tfe_distill_backward(const void *logits, int32_t dtype, int32_t N, in
                                 void *stream);
 
 /*
+ * Softmax cross entropy from hidden states and the vocabulary projection, without keeping the logits (paper Sec. 4.4: the
+ * early-exit projection predicts the next token; the paper gives no training rule, this is the library's).  Per row, with
+ * z_v = weight[v] . hidden[n], t the target and lse = ln sum_v exp(z_v):
+ *     loss = lse - z_t
+ *     grad_hidden[n] = sum_v G[n][v] weight[v],  grad_weight[v] = sum_n G[n][v] hidden[n],  G[n][v] = grad_loss[n] (exp(z_v - lse) - [v = t])
+ *
+ *   hidden, weight   DEVICE bf16 [N][ld_hidden], [V][ld_weight]: rows of d elements, 16-byte aligned, distances multiples of 8;
+ *                    0 <= N, 1 <= V <= TFE_XENT_MAX_ROWS, d a multiple of 8 up to TFE_XENT_MAX_COLS.
+ *   target           DEVICE int32 [N]; a row whose target is outside [0, V) has loss, lse and gradient 0 and takes part in no sum,
+ *                    whatever its hidden state holds; so does, for the gradients, a row whose grad_loss is 0.
+ *   loss, lse        DEVICE float [N].  Products are summed by the tensor cores in fp32, exponentials in fp32, and joined in fp64.
+ *   grad_loss        DEVICE float [N]: the gradient that arrives at each row's loss.  lse: as tfe_xent_forward left it.
+ *   grad_hidden, grad_weight   DEVICE bf16, rows as above, every row written; one of them may be NULL.  They must touch no operand
+ *                    and not each other.  G is rounded to bf16 for the two products with it (the tensor cores take both operands in one
+ *                    type; a G of its own error 2^-9 on average adds as much to a gradient as the gradient's own rounding); sums
+ *                    are fp32 and rounded once.
+ *   workspace        DEVICE scratch, 256-byte aligned, of at least tfe_xent_*_workspace_bytes(N, V, d) bytes (smaller: TFE_ERR_CAPACITY);
+ *                    contents undefined before and after.  It bounds what exists of the logits at a time: a piece of G of 64 MB
+ *                    (N <= 8,192; 4,096 columns beyond).
+ * NaN propagates, and a logit of +inf makes its row's results NaN.  The order of every sum is fixed by the sizes and the targets.
+ * The backward call launches two kernels for each piece of the vocabulary and two more.
+ *
+ * Every wait inside the kernels is bounded.  Should one run out, the loss and lse of the rows concerned, or all gradients, are NaN.
+ * tfe_xent_status synchronises `stream`, reads the status word of the current device and clears what it read: 0, or bits set by
+ * waits that ran out (1 loader, 2 MMA issuer, 4 epilogue); then INTERNAL.  tfe_xent_give_up -- at_once != 0: the waits of the calls
+ * that follow, of the whole process, count as run out from the start; 0: as usual again.  For tests of how a caller takes a failure.
+ * Errors: INVALID_ARG, CAPACITY, CUDA.
+ */
+#define TFE_XENT_MAX_ROWS (1 << 24)
+#define TFE_XENT_MAX_COLS (1 << 16)
+int64_t tfe_xent_forward_workspace_bytes(int32_t N, int32_t V, int32_t d);     /* -1 for invalid arguments */
+int64_t tfe_xent_backward_workspace_bytes(int32_t N, int32_t V, int32_t d);
+tfe_status tfe_xent_forward(const void *hidden, int64_t ld_hidden, int32_t N, const void *weight, int64_t ld_weight, int32_t V,
+                            int32_t d, const int32_t *target, float *loss, float *lse, void *workspace,
+                            int64_t workspace_bytes, void *stream);
+tfe_status tfe_xent_backward(const void *hidden, int64_t ld_hidden, int32_t N, const void *weight, int64_t ld_weight, int32_t V,
+                             int32_t d, const int32_t *target, const float *lse, const float *grad_loss, void *grad_hidden,
+                             int64_t ld_grad_hidden, void *grad_weight, int64_t ld_grad_weight, void *workspace,
+                             int64_t workspace_bytes, void *stream);
+tfe_status tfe_xent_status(uint32_t *device_flags, void *stream);
+tfe_status tfe_xent_give_up(int32_t at_once);
+
+/*
  * Streaming copy (the paper has no counterpart: a yardstick for the measurements, not a step of the method).
  * Copies `bytes` bytes from `src` to `dst` (DEVICE, 16-byte aligned, bytes a multiple of 16, ranges must not
  * overlap) with the load / store instructions the lookup kernels stream hidden states with, one asynchronous

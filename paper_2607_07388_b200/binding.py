@@ -36,7 +36,9 @@ EXPORTS = ["tfe_index_build", "tfe_index_build_device", "tfe_cache_install", "tf
            "tfe_cache_stats", "tfe_head_create", "tfe_head_destroy", "tfe_head_topk", "tfe_head_buffers",
            "tfe_head_status", "tfe_head_geometry", "tfe_mine_ngrams", "tfe_mine_workspace_bytes", "tfe_assign_residency", "tfe_stream_copy",
            "tfe_cache_select_tuning", "tfe_distill_forward", "tfe_distill_backward", "tfe_sample_tokens",
-           "tfe_quantize_fp8", "tfe_quantize_fp8_ld", "tfe_matmul_fp8", "tfe_matmul_fp8_status", "tfe_matmul_fp8_give_up"]
+           "tfe_quantize_fp8", "tfe_quantize_fp8_ld", "tfe_matmul_fp8", "tfe_matmul_fp8_status", "tfe_matmul_fp8_give_up",
+           "tfe_xent_forward_workspace_bytes", "tfe_xent_backward_workspace_bytes", "tfe_xent_forward", "tfe_xent_backward",
+           "tfe_xent_status", "tfe_xent_give_up"]
 
 
 class TfeConfig(C.Structure):
@@ -126,6 +128,12 @@ def lib() -> C.CDLL:
         L.tfe_matmul_fp8.argtypes = [vp, i64, vp, i32, vp, i64, vp, i32, i32, vp, i32, i64, vp]
         L.tfe_matmul_fp8_status.argtypes = [C.POINTER(C.c_uint32), vp]
         L.tfe_matmul_fp8_give_up.argtypes = [i32]
+        L.tfe_xent_forward_workspace_bytes.argtypes = L.tfe_xent_backward_workspace_bytes.argtypes = [i32, i32, i32]
+        L.tfe_xent_forward_workspace_bytes.restype = L.tfe_xent_backward_workspace_bytes.restype = i64
+        L.tfe_xent_forward.argtypes = [vp, i64, i32, vp, i64, i32, i32, vp, vp, vp, vp, i64, vp]
+        L.tfe_xent_backward.argtypes = [vp, i64, i32, vp, i64, i32, i32, vp, vp, vp, vp, i64, vp, i64, vp, i64, vp]
+        L.tfe_xent_status.argtypes = [C.POINTER(C.c_uint32), vp]
+        L.tfe_xent_give_up.argtypes = [i32]
         L.tfe_sample_tokens.argtypes = [vp, i32, i32, i32, i64, C.POINTER(TfeSampleParams), vp, vp, vp, vp]
         L.tfe_distill_forward.argtypes = [vp, i32, i32, i32, i64, vp, vp, i32, f32, vp, vp, vp]
         L.tfe_distill_backward.argtypes = [vp, i32, i32, i32, i64, vp, vp, i32, f32, vp, vp, vp, i64, vp]
@@ -136,7 +144,8 @@ def lib() -> C.CDLL:
                      "tfe_cache_stats", "tfe_head_create", "tfe_head_topk", "tfe_head_buffers", "tfe_head_status",
                      "tfe_head_geometry", "tfe_mine_ngrams", "tfe_assign_residency", "tfe_cache_select_tuning",
                      "tfe_distill_forward", "tfe_distill_backward", "tfe_sample_tokens", "tfe_quantize_fp8", "tfe_quantize_fp8_ld",
-                     "tfe_matmul_fp8", "tfe_matmul_fp8_status", "tfe_matmul_fp8_give_up"):
+                     "tfe_matmul_fp8", "tfe_matmul_fp8_status", "tfe_matmul_fp8_give_up", "tfe_xent_forward", "tfe_xent_backward",
+                     "tfe_xent_status", "tfe_xent_give_up"):
             getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -522,3 +531,46 @@ def tfe_matmul_fp8_status(stream=None) -> int:
 def tfe_matmul_fp8_give_up(at_once: bool) -> None:
     """The waits of the products that follow count as run out from the start, until it is called with False."""
     _check(lib().tfe_matmul_fp8_give_up(int(at_once)), "tfe_matmul_fp8_give_up")
+
+
+# -- cross entropy from hidden states -----------------------------------------------------------
+XENT_MAX_ROWS = 1 << 24
+XENT_MAX_COLS = 1 << 16
+
+
+def tfe_xent_forward_workspace_bytes(N: int, V: int, d: int) -> int:
+    return lib().tfe_xent_forward_workspace_bytes(N, V, d)
+
+
+def tfe_xent_backward_workspace_bytes(N: int, V: int, d: int) -> int:
+    return lib().tfe_xent_backward_workspace_bytes(N, V, d)
+
+
+def tfe_xent_forward(hidden, ld_hidden: int, N: int, weight, ld_weight: int, V: int, d: int, target, loss, lse, workspace,
+                     workspace_bytes: int, stream=None) -> None:
+    st = lib().tfe_xent_forward(hidden, ld_hidden, N, weight, ld_weight, V, d, target, loss, lse, workspace, workspace_bytes,
+                                _stream(stream))
+    if st:
+        raise TfeError(st, "tfe_xent_forward")
+
+
+def tfe_xent_backward(hidden, ld_hidden: int, N: int, weight, ld_weight: int, V: int, d: int, target, lse, grad_loss, grad_hidden,
+                      ld_grad_hidden: int, grad_weight, ld_grad_weight: int, workspace, workspace_bytes: int, stream=None) -> None:
+    st = lib().tfe_xent_backward(hidden, ld_hidden, N, weight, ld_weight, V, d, target, lse, grad_loss, grad_hidden, ld_grad_hidden,
+                                 grad_weight, ld_grad_weight, workspace, workspace_bytes, _stream(stream))
+    if st:
+        raise TfeError(st, "tfe_xent_backward")
+
+
+def tfe_xent_status(stream=None) -> int:
+    """Synchronises; returns the device status word and clears it (0 = no wait ran out since the last report)."""
+    flags = C.c_uint32(0)
+    st = lib().tfe_xent_status(C.byref(flags), _stream(stream))
+    if st not in (TFE_OK, TFE_ERR_INTERNAL):
+        _check(st, "tfe_xent_status")
+    return flags.value
+
+
+def tfe_xent_give_up(at_once: bool) -> None:
+    """The waits of the cross entropy calls that follow count as run out from the start, until it is called with False."""
+    _check(lib().tfe_xent_give_up(int(at_once)), "tfe_xent_give_up")

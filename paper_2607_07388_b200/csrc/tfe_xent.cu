@@ -1,0 +1,876 @@
+// Softmax cross entropy of hidden states against a vocabulary projection, loss and gradients, without keeping the logits: the
+// loss that trains an early-exit projection (paper Sec. 4.4) on the tokens themselves.
+//
+// Per row n with target t:   z_v = W_v . h_n      lse = ln sum_v exp z_v      loss = lse - z_t
+//     G_nv = g_n (exp(z_v - lse) - [v = t])       grad H = G W                grad W = G^T H
+//
+//   tfe_xent_compact_kernel   lists the rows that have a target (and a gradient) and copies their hidden states together: the
+//                             products below run over those rows only, and a row that has none takes part in no sum.
+//   tfe_xent_gemm_kernel      one persistent, warp-specialised tcgen05 kernel with three epilogues:
+//       kLse    z tile by tile, each kept only as its row maxima, row sums of exponentials and the targets' logits;
+//       kProb   z of a piece of the vocabulary once more, turned into that piece of G (bf16, in the workspace);
+//       kGrads  both products of the piece with G: grad W is complete with its piece, grad H adds up over the pieces in fp32.
+//   tfe_xent_loss_kernel      joins a row's partial maxima and sums.
+//   tfe_xent_rows_kernel      joins grad H's sums, rounds them and puts them back to their rows.
+//
+// All products are 2 N V d operations; the loss makes one, the gradients three (z again and the two with G).
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <atomic>
+#include <cstdint>
+
+#include "../../include/tfe.h"
+#include "tfe_internal.h"
+#include "tfe_rows.cuh"
+#include "tfe_tc.cuh"
+
+namespace {
+
+using bf16 = __nv_bfloat16;
+
+constexpr int kCtas = 1;                        // CTAs that share a tile
+constexpr int kRowsA = 128;                     // rows of A per CTA (MMA M per CTA)
+constexpr int kM = kRowsA * kCtas;              // rows of a tile
+constexpr int kN = 256;                         // columns of a tile at most (MMA N)
+constexpr int kStepK = 64;                      // k of a stage: 128 bytes, one swizzle row
+constexpr uint32_t kBytesA = kRowsA * kStepK * 2, kBytesB = kN / kCtas * kStepK * 2, kStageBytes = kBytesA + kBytesB;
+constexpr int kStages = 196608 / kStageBytes;
+constexpr int kBuffers = 2;                     // accumulators of kN columns: all of tensor memory
+constexpr int kEpilogueWarps = 8;               // two per lane quarter of tensor memory, half of the tile's columns each
+constexpr int kThreads = 32 * (4 + kEpilogueWarps);
+constexpr uint32_t kRoom = 32 * 128;            // bytes of an epilogue warp's outgoing piece: 32 rows of 64 bf16
+constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kEpilogueWarps * kRoom;
+constexpr float kLog2e = 1.4426950408889634f;
+
+constexpr uint32_t kTimeoutLoader = 1u, kTimeoutMma = 2u, kTimeoutEpilogue = 4u;
+__device__ uint32_t g_xent_status;
+std::atomic<uint32_t> g_xent_give_up{0};
+
+__global__ void tfe_xent_status_kernel(uint32_t told) { atomicAnd(&g_xent_status, ~told); }
+
+enum Op { kLse, kProb, kGrads };
+
+struct GemmParams {
+    int32_t N, V, d;
+    int32_t tn;                                 // columns of a tile
+    int32_t per_unit, n_tiles;                  // kLse: tiles of a unit, all column tiles
+    int32_t v0, width;                          // kProb, kGrads: the piece, [v0, v0 + width)
+    int32_t splits, first;                      // kGrads: parts of the sums over a piece for grad H; the first piece
+    int32_t m_room;                             // row tiles that there is room for
+    int32_t want_h, want_w;
+    uint32_t give_up;
+    const int32_t *n_live;                      // rows taken part in (null: N)
+    const int32_t *target;
+    const float *lse, *coef;
+    float2 *part; int64_t ld_part;              // kLse: [2 * units per row][ld_part] maxima and sums
+    float *z_target;
+    float *sum_h;                               // kGrads: [splits][m_room][column tiles][kN / 4][kM][4]
+    uint32_t *failed;                           // set if a wait ran out
+};
+
+// ------------------------------------------------------------------ rows that take part
+
+struct CompactParams {
+    int32_t N, V, d, rows_per_block;
+    const bf16 *h; int64_t ld;
+    const int32_t *target;
+    const float *lse, *grad;                    // null: the loss
+    bf16 *h_out;
+    int32_t *pos, *target_out, *n_live;
+    float *lse_out, *coef_out;
+    uint32_t *failed;
+};
+
+constexpr int kCompactThreads = 256;
+
+__global__ void __launch_bounds__(kCompactThreads)
+tfe_xent_compact_kernel(const CompactParams p)
+{
+    __shared__ int32_t s_before[kCompactThreads / 32], s_all[kCompactThreads / 32];
+    __shared__ int32_t s_pos[kCompactThreads];
+    tfe_wait_for_stream();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int64_t r0 = (int64_t)blockIdx.x * p.rows_per_block, r1 = min((int64_t)p.N, r0 + p.rows_per_block);
+    auto live = [&](int64_t r) {
+        const int32_t t = p.target[r];
+        return t >= 0 && t < p.V && (!p.grad || !(p.grad[r] == 0.f));
+    };
+    // how many before this block's rows, and in all (every block counts for itself: the targets are a few KB in L2)
+    int32_t before = 0, all = 0;
+    for (int64_t r = tid; r < p.N; r += kCompactThreads) {
+        const int32_t one = live(r);
+        all += one;
+        before += r < r0 ? one : 0;
+    }
+    before = __reduce_add_sync(0xFFFFFFFFu, before);
+    all = __reduce_add_sync(0xFFFFFFFFu, all);
+    if (lane == 0) { s_before[warp] = before; s_all[warp] = all; }
+    __syncthreads();
+    before = all = 0;
+    for (int w = 0; w < kCompactThreads / 32; ++w) { before += s_before[w]; all += s_all[w]; }
+    if (blockIdx.x == 0 && tid == 0) { *p.n_live = all; if (p.failed) *p.failed = 0; }
+    const int vecs = p.d / 8;
+    for (int64_t base = r0; base < r1; base += kCompactThreads) {
+        const int64_t r = base + tid;
+        const bool one = r < r1 && live(r);
+        const uint32_t vote = __ballot_sync(0xFFFFFFFFu, one);
+        __syncthreads();
+        if (lane == 0) s_before[warp] = __popc(vote);
+        __syncthreads();
+        int32_t at = before, total = 0;
+        for (int w = 0; w < kCompactThreads / 32; ++w) { at += w < warp ? s_before[w] : 0; total += s_before[w]; }
+        at += __popc(vote & ((1u << lane) - 1u));
+        if (r < r1) p.pos[r] = one ? at : -1;
+        s_pos[tid] = one ? at : -1;
+        if (one) {
+            p.target_out[at] = p.target[r];
+            if (p.grad) { p.lse_out[at] = p.lse[r]; p.coef_out[at] = p.grad[r]; }
+        }
+        __syncthreads();
+        for (int i = warp; i < kCompactThreads && base + i < r1; i += kCompactThreads / 32) {
+            const int32_t to = s_pos[i];
+            if (to < 0) continue;
+            const uint4 *src = reinterpret_cast<const uint4 *>(p.h + (base + i) * p.ld);
+            uint4 *dst = reinterpret_cast<uint4 *>(p.h_out + (int64_t)to * p.d);
+            for (int v = lane; v < vecs; v += 32) dst[v] = tfe_rows::load_stream(src + v);
+        }
+        before += total;
+    }
+    // zeros up to the end of the last tile: the sums over rows run to there
+    const int64_t end = max((int64_t)(all + kM - 1) / kM, (int64_t)1) * kM;
+    const int64_t n_zero = (end - all) * vecs;
+    uint4 *dst = reinterpret_cast<uint4 *>(p.h_out + (int64_t)all * p.d);
+    for (int64_t i = (int64_t)blockIdx.x * kCompactThreads + tid; i < n_zero; i += (int64_t)gridDim.x * kCompactThreads) dst[i] = make_uint4(0, 0, 0, 0);
+}
+
+// ------------------------------------------------------------------ the products
+
+// Shared-memory operand whose rows are 64 consecutive bf16 along M or N for one k (written by TMA with the 128-byte swizzle): rows
+// 128 bytes apart, groups of 8 k 1,024 bytes apart (stride offset), the next 64 along M or N 64 rows further (leading offset).
+__device__ __forceinline__ uint64_t umma_desc_mn_sw128(uint32_t smem_addr)
+{
+    uint64_t d = (uint64_t)((smem_addr & 0x3FFFFu) >> 4);
+    d |= (uint64_t)(kStepK * 128 >> 4) << 16;
+    d |= (uint64_t)(1024 >> 4) << 32;
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)2 << 61;
+    return d;
+}
+// kind::f16: D fp32 ([4,6) = 1), A and B bf16 ([7,10) = [10,13) = 1), bit 15 / 16: A / B run along M / N in memory
+__host__ __device__ constexpr uint32_t umma_idesc(uint32_t M, uint32_t N, bool a_mn, bool b_mn)
+{
+    return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((N >> 3) << 17) | ((M >> 4) << 24);
+}
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t from, int32_t x, int32_t y)
+{
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(from),
+                 "r"(x), "r"(y)
+                 : "memory");
+}
+
+// What a unit of work multiplies.  A's tile is kM rows (or columns of G) from a_at, B's tn from b_at, the sum runs over steps of 64 from k_at.
+struct Unit {
+    int32_t a_at, b_at, k_at, steps, tiles;
+    bool grad_h;                                // kGrads: G W, else G^T H
+    int32_t index;                              // kLse: column unit; kGrads: place of grad H's sum
+};
+
+template <int kOp>
+struct Units {
+    int32_t m_tiles, n_live, cols;              // row tiles, rows, column tiles of d (kGrads)
+    int64_t n_h, n_w, n;                        // units of grad H, of grad W, all
+    int32_t steps_h, steps_w;
+
+    __device__ __forceinline__ explicit Units(const GemmParams &p)
+    {
+        n_live = p.n_live ? *p.n_live : p.N;
+        m_tiles = max(1, (n_live + kM - 1) / kM);
+        cols = (p.d + p.tn - 1) / p.tn;
+        n_h = n_w = 0; steps_h = steps_w = 0;
+        if constexpr (kOp == kLse) {
+            n = n_live ? (int64_t)m_tiles * ((p.n_tiles + p.per_unit - 1) / p.per_unit) : 0;
+        } else if constexpr (kOp == kProb) {
+            n = (int64_t)m_tiles * ((p.width + p.tn - 1) / p.tn);
+        } else {
+            const int32_t all = (p.width + kStepK - 1) / kStepK;
+            steps_h = (all + p.splits - 1) / p.splits;
+            steps_w = max(1, (n_live + kStepK - 1) / kStepK);
+            n_h = p.want_h ? (int64_t)m_tiles * cols * p.splits : 0;
+            n_w = p.want_w ? (int64_t)((p.width + kM - 1) / kM) * cols : 0;
+            n = n_h + n_w;
+        }
+    }
+    __device__ __forceinline__ Unit at(const GemmParams &p, int64_t u) const
+    {
+        Unit w{};
+        w.tiles = 1;
+        if constexpr (kOp != kGrads) {          // neighbours share the column tile
+            const int32_t mt = (int32_t)(u % m_tiles), nt = (int32_t)(u / m_tiles);
+            w.a_at = mt * kM;
+            w.steps = (p.d + kStepK - 1) / kStepK;
+            if constexpr (kOp == kLse) {
+                w.b_at = nt * p.per_unit * p.tn;
+                w.tiles = min(p.per_unit, p.n_tiles - nt * p.per_unit);
+                w.index = nt;
+            } else {
+                w.b_at = nt * p.tn;             // within the piece
+            }
+        } else {
+            const bool h_first = steps_h >= steps_w;        // the longer units first
+            w.grad_h = h_first ? u < n_h : u >= n_w;
+            if (w.grad_h) {
+                const int32_t i = (int32_t)(h_first ? u : u - n_w), ct = i % cols, mt = i / cols % m_tiles, s = i / cols / m_tiles;
+                const int32_t all = (p.width + kStepK - 1) / kStepK;
+                w.a_at = mt * kM;
+                w.b_at = ct * p.tn;
+                w.k_at = s * steps_h * kStepK;
+                w.steps = max(0, min(steps_h, all - s * steps_h));
+                w.index = (s * p.m_room + mt) * cols + ct;
+            } else {
+                const int32_t i = (int32_t)(h_first ? u - n_h : u);
+                w.a_at = i / cols * kM;         // within the piece
+                w.b_at = i % cols * p.tn;
+                w.steps = steps_w;
+            }
+        }
+        return w;
+    }
+};
+
+struct Maps { CUtensorMap a, b, a_w, b_w, out; };           // kLse, kProb: H, W, -, -, G;  kGrads: G by rows, W, G by columns, H, grad W
+
+template <int kOp>
+__global__ void __launch_bounds__(kThreads, 1)
+tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_acc_full[kBuffers], s_acc_empty[kBuffers], s_drain;
+    __shared__ uint32_t s_tmem_base;
+    __shared__ volatile uint32_t s_abort;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) { mbar_init(smem_u32(&s_full[s]), 1); mbar_init(smem_u32(&s_empty[s]), 1); }
+        for (int a = 0; a < kBuffers; ++a) { mbar_init(smem_u32(&s_acc_full[a]), 1); mbar_init(smem_u32(&s_acc_empty[a]), kEpilogueWarps); }
+        mbar_init(smem_u32(&s_drain), 1);
+        s_abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc(smem_u32(&s_tmem_base), kBuffers * kN);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = s_tmem_base;
+    tfe_wait_for_stream();
+    const Units<kOp> units(p);
+
+    if (warp == 0) {
+        // ============================ TMA producer ============================
+        if (lane == 0) {
+            const uint64_t hint = 0x1000000000000000ull;            // no preference
+            uint32_t stage = 0, phase = 0, issued = 0;
+            bool ok = !p.give_up;
+            for (int64_t u = blockIdx.x; ok && u < units.n; u += gridDim.x) {
+                const Unit w = units.at(p, u);
+                for (int32_t t = 0; ok && t < w.tiles; ++t)
+                    for (int32_t ks = 0; ks < w.steps; ++ks) {
+                        if (!mbar_wait(smem_u32(&s_empty[stage]), phase ^ 1u, &s_abort)) {
+                            atomicOr(&g_xent_status, kTimeoutLoader);
+                            s_abort = 1;
+                            ok = false;
+                            break;
+                        }
+                        const uint32_t bar = smem_u32(&s_full[stage]), a = smem_base + stage * kStageBytes, b = a + kBytesA;
+                        const int32_t k = w.k_at + ks * kStepK;
+                        mbar_expect_tx(bar, kBytesA + (uint32_t)p.tn * kStepK * 2);
+                        if constexpr (kOp != kGrads) {
+                            tma_load_2d(a, &maps.a, bar, k, w.a_at, hint);
+                            tma_load_2d(b, &maps.b, bar, k, (kOp == kProb ? p.v0 : 0) + w.b_at + t * p.tn, hint);
+                        } else if (w.grad_h) {
+                            tma_load_2d(a, &maps.a, bar, k, w.a_at, hint);
+                            for (int32_t j = 0; j < p.tn / 64; ++j) tma_load_2d(b + j * kStepK * 128, &maps.b, bar, w.b_at + j * 64, p.v0 + k, hint);
+                        } else {
+                            for (int32_t j = 0; j < kRowsA / 64; ++j) tma_load_2d(a + j * kStepK * 128, &maps.a_w, bar, w.a_at + j * 64, k, hint);
+                            for (int32_t j = 0; j < p.tn / 64; ++j) tma_load_2d(b + j * kStepK * 128, &maps.b_w, bar, w.b_at + j * 64, k, hint);
+                        }
+                        ++issued;
+                        if (++stage == kStages) { stage = 0; phase ^= 1u; }
+                    }
+            }
+            if (!ok)                            // copies in flight land before the shared memory goes
+                for (uint32_t s = 0; s < kStages; ++s) {
+                    const uint32_t fills = (issued + kStages - 1u - s) / kStages;
+                    for (uint32_t t = 0; fills && t < TC_WAIT_LIMIT && !mbar_try_wait(smem_u32(&s_full[s]), (fills - 1u) & 1u); ++t) { }
+                }
+        }
+    } else if (warp == 1) {
+        // ============================ MMA issuer ==============================
+        if (lane == 0) {
+            uint32_t stage = 0, phase = 0, buf = 0, buf_phase = 0;
+            bool ok = !p.give_up;
+            for (int64_t u = blockIdx.x; ok && u < units.n; u += gridDim.x) {
+                const Unit w = units.at(p, u);
+                const bool a_mn = kOp == kGrads && !w.grad_h, b_mn = kOp == kGrads;
+                const uint32_t idesc = umma_idesc(kM, (uint32_t)p.tn, a_mn, b_mn);
+                // 16 k further: 32 bytes along the swizzled row, or 16 rows of 128 bytes
+                const uint64_t a_step = a_mn ? 128u : 2u, b_step = b_mn ? 128u : 2u;
+                for (int32_t t = 0; ok && t < w.tiles && w.steps > 0; ++t) {
+                    ok = mbar_wait(smem_u32(&s_acc_empty[buf]), buf_phase ^ 1u, &s_abort);
+                    for (int32_t ks = 0; ok && ks < w.steps; ++ks) {
+                        ok = mbar_wait(smem_u32(&s_full[stage]), phase, &s_abort);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint32_t a = smem_base + stage * kStageBytes, b = a + kBytesA;
+                        const uint64_t a_desc = a_mn ? umma_desc_mn_sw128(a) : umma_desc_sw128(a), b_desc = b_mn ? umma_desc_mn_sw128(b) : umma_desc_sw128(b);
+#pragma unroll
+                        for (int k = 0; k < kStepK / 16; ++k)
+                            umma_bf16(tmem_base + buf * kN, a_desc + k * a_step, b_desc + k * b_step, idesc, ks > 0 || k > 0 ? 1u : 0u);
+                        umma_commit(smem_u32(&s_empty[stage]));
+                        if (++stage == kStages) { stage = 0; phase ^= 1u; }
+                    }
+                    if (!ok) {
+                        atomicOr(&g_xent_status, kTimeoutMma);
+                        s_abort = 1;
+                        break;
+                    }
+                    umma_commit(smem_u32(&s_acc_full[buf]));
+                    if (++buf == kBuffers) { buf = 0; buf_phase ^= 1u; }
+                }
+            }
+            if (!ok) {                          // MMAs in flight end before their tensor memory is freed
+                umma_commit(smem_u32(&s_drain));
+                for (uint32_t t = 0; t < TC_WAIT_LIMIT && !mbar_try_wait(smem_u32(&s_drain), 0); ++t) { }
+            }
+        }
+    } else if (warp >= 4) {
+        // ============================ epilogue ================================
+        const int e = warp - 4;
+        const uint32_t quarter = (uint32_t)warp & 3u;               // tensor-memory lanes 32 * quarter .. + 31
+        const int32_t half = e >> 2, cols = p.tn / 2, c0 = half * cols;     // this warp's columns: a multiple of 16
+        const int32_t row_in_tile = (int32_t)(quarter * 32u) + lane;
+        const uint32_t room = smem_base + kStages * kStageBytes + (uint32_t)e * kRoom;
+        uint32_t buf = 0, buf_phase = 0;
+        bool ok = !p.give_up;
+        int64_t u = blockIdx.x;
+        for (; ok && u < units.n; u += gridDim.x) {
+            const Unit w = units.at(p, u);
+            const int32_t row = w.a_at + row_in_tile;
+            const bool live = kOp == kGrads || row < units.n_live;
+            int32_t target = -1;
+            float lse = 0.f, coef = 0.f, top = -3.4e38f, sum = 0.f;
+            if (kOp != kGrads && live) target = p.target[row];
+            if (kOp == kProb && live) { lse = p.lse[row]; coef = p.coef[row]; }
+            for (int32_t t = 0; t < w.tiles; ++t) {
+                if (w.steps == 0) {             // (a part of a short last piece that has nothing to add)
+                    if constexpr (kOp == kGrads)
+                        if (p.first) {
+                            float4 *at = reinterpret_cast<float4 *>(p.sum_h) + ((int64_t)w.index * (kN / 4) + c0 / 4) * kM + row_in_tile;
+                            for (int32_t c = 0; c < cols; c += 4) at[(int64_t)(c / 4) * kM] = make_float4(0.f, 0.f, 0.f, 0.f);
+                        }
+                    continue;
+                }
+                ok = mbar_wait(smem_u32(&s_acc_full[buf]), buf_phase, &s_abort);
+                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
+                tc_fence_after();
+                const uint32_t taddr = tmem_base + ((quarter * 32u) << 16) + buf * kN + (uint32_t)c0;
+                auto release = [&] {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&s_acc_empty[buf]));
+                };
+                if constexpr (kOp == kLse) {
+                    const int32_t v0 = w.b_at + t * p.tn + c0, left = p.V - v0, mine = target - v0;
+                    for (int32_t c = 0; c < cols; c += 16) {
+                        uint32_t r[16];
+                        float z[16];
+                        tmem_ld16(taddr + (uint32_t)c, r);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) z[j] = c + j < left ? __uint_as_float(r[j]) : -INFINITY;
+                        if ((uint32_t)(mine - c) < 16u) {
+                            float zt = 0.f;
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) zt = mine - c == j ? z[j] : zt;
+                            p.z_target[row] = zt;
+                        }
+                        float best = top;
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) best = fmaxf(best, z[j]);
+                        sum *= tfe_rows::exp2_approx((top - best) * kLog2e);
+                        top = best;
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) sum += tfe_rows::exp2_approx((z[j] - top) * kLog2e);
+                    }
+                    release();
+                } else if constexpr (kOp == kProb) {
+                    const int32_t v0 = p.v0 + w.b_at + c0, left = p.V - v0, mine = target - v0;
+                    for (int32_t c = 0; c < cols; c += 64) {
+                        uint32_t out[32];
+#pragma unroll
+                        for (int q = 0; q < 64; q += 16) {
+                            uint32_t r[16];
+                            tmem_ld16(taddr + (uint32_t)(c + q), r);
+                            tmem_ld_wait();
+                            float g[16];
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) {
+                                const float x = __uint_as_float(r[j]) - lse;
+                                float y = tfe_rows::exp2_approx(x * kLog2e);
+                                if (mine == c + q + j) y = expm1f(x);
+                                g[j] = live && c + q + j < left ? coef * y : 0.f;
+                            }
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                const __nv_bfloat162 b2 = __floats2bfloat162_rn(g[2 * j], g[2 * j + 1]);
+                                out[q / 2 + j] = *reinterpret_cast<const uint32_t *>(&b2);
+                            }
+                        }
+                        if (c + 64 >= cols) release();
+                        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                        __syncwarp();
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(room + (uint32_t)(lane * 128 + ((i ^ (lane & 7)) * 16))), "r"(out[4 * i]),
+                                         "r"(out[4 * i + 1]), "r"(out[4 * i + 2]), "r"(out[4 * i + 3])
+                                         : "memory");
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) {
+                            tma_store_2d(&maps.out, room, w.b_at + c0 + c, w.a_at + (int32_t)(quarter * 32u));
+                            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                        }
+                    }
+                } else if (w.grad_h) {
+                    float4 *at = reinterpret_cast<float4 *>(p.sum_h) + ((int64_t)w.index * (kN / 4) + c0 / 4) * kM + row_in_tile;
+                    for (int32_t c = 0; c < cols; c += 16) {
+                        uint32_t r[16];
+                        float4 old[4];
+                        if (!p.first)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) old[i] = at[(int64_t)(c / 4 + i) * kM];
+                        tmem_ld16(taddr + (uint32_t)c, r);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            float4 x = make_float4(__uint_as_float(r[4 * i]), __uint_as_float(r[4 * i + 1]), __uint_as_float(r[4 * i + 2]), __uint_as_float(r[4 * i + 3]));
+                            if (!p.first) { x.x += old[i].x; x.y += old[i].y; x.z += old[i].z; x.w += old[i].w; }
+                            at[(int64_t)(c / 4 + i) * kM] = x;
+                        }
+                    }
+                    release();
+                } else {
+                    for (int32_t c = 0; c < cols; c += 64) {
+                        uint32_t out[32];
+#pragma unroll
+                        for (int q = 0; q < 64; q += 16) {
+                            uint32_t r[16];
+                            tmem_ld16(taddr + (uint32_t)(c + q), r);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                const __nv_bfloat162 b2 = __floats2bfloat162_rn(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
+                                out[q / 2 + j] = *reinterpret_cast<const uint32_t *>(&b2);
+                            }
+                        }
+                        if (c + 64 >= cols) release();
+                        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                        __syncwarp();
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(room + (uint32_t)(lane * 128 + ((i ^ (lane & 7)) * 16))), "r"(out[4 * i]),
+                                         "r"(out[4 * i + 1]), "r"(out[4 * i + 2]), "r"(out[4 * i + 3])
+                                         : "memory");
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) {        // (what lies beyond the matrix is not written)
+                            const int32_t x = w.b_at + c0 + c, y = p.v0 + w.a_at + (int32_t)(quarter * 32u);
+                            if (x < p.d && y < p.V) tma_store_2d(&maps.out, room, x, y);
+                            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                        }
+                    }
+                }
+                if (++buf == kBuffers) { buf = 0; buf_phase ^= 1u; }
+            }
+            if (!ok) break;
+            if constexpr (kOp == kLse)
+                if (live) p.part[(int64_t)(2 * w.index + half) * p.ld_part + row] = make_float2(top, sum);
+        }
+        asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        if (!ok) {                              // a wait ran out: no results that look like some
+            if (lane == 0) {
+                atomicOr(&g_xent_status, kTimeoutEpilogue);
+                if (kOp != kLse) *p.failed = 1;
+            }
+            s_abort = 1;
+            if constexpr (kOp == kLse)
+                for (; u < units.n; u += gridDim.x) {
+                    const Unit w = units.at(p, u);
+                    const int32_t row = w.a_at + row_in_tile;
+                    if (row < units.n_live) p.part[(int64_t)(2 * w.index + half) * p.ld_part + row] = make_float2(0.f, __int_as_float(0x7FFFFFFF));
+                }
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        __syncwarp();
+        tc_fence_after();
+        tmem_dealloc(tmem_base, kBuffers * kN);
+    }
+}
+
+// ------------------------------------------------------------------ joining
+
+struct LossParams {
+    int32_t N, V, chunks;
+    const float2 *part; int64_t ld_part;
+    const float *z_target;
+    const int32_t *target, *pos;                // pos null: rows are where they were
+    float *loss, *lse;
+};
+constexpr int kLossLanes = 16;                  // threads that share a row's partial results
+
+__global__ void __launch_bounds__(32 * kLossLanes)
+tfe_xent_loss_kernel(const LossParams p)
+{
+    __shared__ float s_top[kLossLanes][32];
+    __shared__ double s_sum[kLossLanes][32];
+    tfe_wait_for_stream();
+    const int lane = threadIdx.x & 31, part = threadIdx.x >> 5;
+    const int64_t r = (int64_t)blockIdx.x * 32 + lane;
+    const int32_t t = r < p.N ? p.target[r] : -1;
+    int64_t at = t >= 0 && t < p.V ? r : -1;
+    if (p.pos && r < p.N) at = p.pos[r];
+    float top = -INFINITY;
+    double sum = 0.0;
+    if (at >= 0) {
+        for (int32_t c = part; c < p.chunks; c += kLossLanes) top = fmaxf(top, p.part[(int64_t)c * p.ld_part + at].x);
+        for (int32_t c = part; c < p.chunks; c += kLossLanes) {
+            const float2 x = p.part[(int64_t)c * p.ld_part + at];
+            sum += (double)(x.y * tfe_rows::exp2_approx((x.x - top) * kLog2e));
+        }
+    }
+    s_top[part][lane] = top;
+    s_sum[part][lane] = sum;
+    __syncthreads();
+    if (part != 0 || r >= p.N) return;
+    if (at < 0) { p.loss[r] = p.lse[r] = 0.f; return; }
+    for (int i = 1; i < kLossLanes; ++i) top = fmaxf(top, s_top[i][lane]);
+    sum = 0.0;
+    for (int i = 0; i < kLossLanes; ++i)
+        if (s_sum[i][lane] != 0.0) sum += s_sum[i][lane] * exp((double)s_top[i][lane] - (double)top);
+    const double lse = (double)top + log(sum);
+    p.lse[r] = (float)lse;
+    p.loss[r] = (float)(lse - (double)p.z_target[at]);
+}
+
+struct RowsParams {
+    int32_t N, V, d, splits, m_room, cols, tn;
+    const float *sum_h;
+    const int32_t *pos;
+    const uint32_t *failed;
+    bf16 *grad_h; int64_t ld_h;
+    bf16 *grad_w; int64_t ld_w;
+};
+constexpr int kRowsThreads = 256;
+
+// grad H's sums over the parts, rounded, to their rows; NaN everywhere if a product before it failed
+__global__ void __launch_bounds__(kRowsThreads)
+tfe_xent_rows_kernel(const RowsParams p)
+{
+    tfe_wait_for_stream();
+    const bool failed = *p.failed != 0;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const bf16 nan = __float2bfloat16_rn(__int_as_float(0x7FFFFFFF));
+    if (p.grad_h)
+        for (int64_t base = (int64_t)blockIdx.x * 32; base < p.N; base += (int64_t)gridDim.x * 32) {
+            const int64_t r = base + lane;
+            const int32_t at = r < p.N ? p.pos[r] : -1;
+            if (r < p.N)
+                for (int32_t c = warp * 4; c < p.d; c += kRowsThreads / 32 * 4) {
+                    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (at >= 0)
+                        for (int32_t s = 0; s < p.splits; ++s) {
+                            const int64_t tile = ((int64_t)s * p.m_room + at / kM) * p.cols + c / p.tn;
+                            const float4 x = reinterpret_cast<const float4 *>(p.sum_h)[(tile * (kN / 4) + c % p.tn / 4) * kM + at % kM];
+                            sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
+                        }
+                    bf16 *to = p.grad_h + r * p.ld_h + c;
+                    to[0] = failed ? nan : __float2bfloat16_rn(sum.x);
+                    to[1] = failed ? nan : __float2bfloat16_rn(sum.y);
+                    to[2] = failed ? nan : __float2bfloat16_rn(sum.z);
+                    to[3] = failed ? nan : __float2bfloat16_rn(sum.w);
+                }
+        }
+    if (failed && p.grad_w)
+        for (int64_t v = blockIdx.x; v < p.V; v += gridDim.x)
+            for (int32_t c = threadIdx.x; c < p.d; c += kRowsThreads) p.grad_w[v * p.ld_w + c] = nan;
+}
+
+// ------------------------------------------------------------------ host side
+
+// bf16 matrix [rows][cols], rows `ld` elements apart; box = 64 columns x box_rows rows, 128-byte swizzle, zeros outside
+bool make_map(CUtensorMap *map, const void *base, int64_t rows, int64_t cols, int64_t ld, uint32_t box_rows)
+{
+    encode_tiled_fn enc = get_encode_tiled();
+    if (!enc) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
+    const cuuint32_t box[2] = {64, box_rows};
+    const cuuint32_t estr[2] = {1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The sizes that workspace and launches go by.
+struct Plan {
+    int64_t n_pad;                              // room for rows: whole tiles
+    int32_t m_room;
+    int32_t tn, n_tiles, per_unit, chunks;      // loss
+    int64_t piece; int32_t pieces, splits;      // gradients
+    int32_t cols, tn_d;
+    bool gather;
+};
+constexpr int64_t kUnits = 8192;                // units of the loss beyond which tiles are joined: bounds the partial results
+constexpr int64_t kPieceElements = 32 << 20;    // of G: 64 MB stay in L2 until both products have read them
+constexpr int64_t kPieceMin = 4096;             // columns of a piece at least
+
+int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+Plan make_plan(int32_t N, int32_t V, int32_t d)
+{
+    Plan q{};
+    q.n_pad = std::max<int64_t>(kM, round_up(N, kM));
+    q.m_room = (int32_t)(q.n_pad / kM);
+    q.gather = N > kM;
+    q.tn = kN;
+    q.n_tiles = (V + q.tn - 1) / q.tn;
+    q.per_unit = (int32_t)std::max<int64_t>(1, (int64_t)q.n_tiles * q.m_room / kUnits);
+    q.chunks = 2 * ((q.n_tiles + q.per_unit - 1) / q.per_unit);
+    const int64_t most = std::max(kPieceMin, kPieceElements / q.n_pad / kN * kN);
+    q.pieces = (int32_t)((V + most - 1) / most);
+    q.piece = round_up((V + q.pieces - 1) / q.pieces, kN);
+    q.pieces = (int32_t)((V + q.piece - 1) / q.piece);
+    q.splits = (int32_t)std::min<int64_t>(8, std::max<int64_t>(1, q.piece / q.n_pad));
+    q.tn_d = d >= kN ? kN : 128;
+    q.cols = (d + q.tn_d - 1) / q.tn_d;
+    return q;
+}
+
+struct Room {                                   // hands out pieces of the workspace
+    uint8_t *base;
+    int64_t used;
+    template <typename T> T *take(int64_t n)
+    {
+        T *at = reinterpret_cast<T *>(base + used);
+        used += round_up(n * (int64_t)sizeof(T), 256);
+        return at;
+    }
+};
+struct ForwardRoom {
+    float2 *part; float *z_target; bf16 *h; int32_t *pos, *target, *n_live;
+    int64_t bytes;
+    ForwardRoom(const Plan &q, int32_t N, int32_t d, void *ws)
+    {
+        Room r{static_cast<uint8_t *>(ws), 0};
+        part = r.take<float2>((int64_t)q.chunks * q.n_pad);
+        z_target = r.take<float>(q.n_pad);
+        if (q.gather) { h = r.take<bf16>(q.n_pad * d); pos = r.take<int32_t>(N); target = r.take<int32_t>(q.n_pad); n_live = r.take<int32_t>(1); }
+        else { h = nullptr; pos = target = n_live = nullptr; }
+        bytes = r.used;
+    }
+};
+struct BackwardRoom {
+    bf16 *g, *h; float *sum_h, *lse, *coef; int32_t *pos, *target, *n_live; uint32_t *failed;
+    int64_t bytes;
+    BackwardRoom(const Plan &q, int32_t N, int32_t d, void *ws)
+    {
+        Room r{static_cast<uint8_t *>(ws), 0};
+        g = r.take<bf16>(q.n_pad * q.piece);
+        h = r.take<bf16>(q.n_pad * d);
+        sum_h = r.take<float>((int64_t)q.splits * q.m_room * q.cols * kM * kN);
+        lse = r.take<float>(q.n_pad); coef = r.take<float>(q.n_pad);
+        pos = r.take<int32_t>(N); target = r.take<int32_t>(q.n_pad); n_live = r.take<int32_t>(1); failed = r.take<uint32_t>(1);
+        bytes = r.used;
+    }
+};
+
+bool aligned(const void *ptr, uintptr_t to) { return ptr && reinterpret_cast<uintptr_t>(ptr) % to == 0; }
+bool sizes_ok(int32_t N, int32_t V, int32_t d)
+{
+    return N >= 0 && N <= TFE_XENT_MAX_ROWS && V >= 1 && V <= TFE_XENT_MAX_ROWS && d >= 8 && d % 8 == 0 && d <= TFE_XENT_MAX_COLS;
+}
+bool rows_ok(const void *at, int64_t ld, int32_t d) { return aligned(at, 16) && ld >= d && ld % 8 == 0 && ld <= (1ll << 34); }
+
+tfe_status device_sms(int *sms)
+{
+    int dev = 0;
+    tfe_status st = tfe_note_cuda(cudaGetDevice(&dev), "cudaGetDevice");
+    return st != TFE_OK ? st : tfe_note_cuda(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev), "cudaDeviceGetAttribute");
+}
+
+tfe_status bad_map() { return tfe_note_cuda(cudaErrorInvalidValue, "cuTensorMapEncodeTiled"); }
+
+template <int kOp>
+tfe_status launch_gemm(int64_t most_units, int sms, cudaStream_t stream, const Maps &maps, const GemmParams &p)
+{
+    auto kernel = tfe_xent_gemm_kernel<kOp>;
+    if (tfe_status st = tfe_note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem), "cross entropy attribute")) return st;
+    const unsigned grid = (unsigned)(std::max<int64_t>(1, std::min<int64_t>(sms / kCtas, most_units)) * kCtas);
+    return tfe_launch_serial(kernel, grid, kThreads, kCtas, kSmem, stream, "cross entropy launch", maps, p);
+}
+
+tfe_status launch_compact(CompactParams c, int sms, cudaStream_t stream)
+{
+    c.rows_per_block = (int32_t)std::max<int64_t>(8, (c.N + 2ll * sms - 1) / (2ll * sms));
+    const unsigned grid = (unsigned)(((int64_t)c.N + c.rows_per_block - 1) / c.rows_per_block);
+    return tfe_launch_serial(tfe_xent_compact_kernel, grid, kCompactThreads, 1, 0, stream, "cross entropy rows launch", c);
+}
+
+bool touch(const void *a, int64_t a_bytes, const void *b, int64_t b_bytes)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return a && b && x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t tfe_xent_forward_workspace_bytes(int32_t N, int32_t V, int32_t d)
+{
+    if (!sizes_ok(N, V, d)) return -1;
+    return N == 0 ? 0 : ForwardRoom(make_plan(N, V, d), N, d, nullptr).bytes;
+}
+
+int64_t tfe_xent_backward_workspace_bytes(int32_t N, int32_t V, int32_t d)
+{
+    if (!sizes_ok(N, V, d)) return -1;
+    return N == 0 ? 0 : BackwardRoom(make_plan(N, V, d), N, d, nullptr).bytes;
+}
+
+tfe_status tfe_xent_forward(const void *hidden, int64_t ld_hidden, int32_t N, const void *weight, int64_t ld_weight, int32_t V, int32_t d,
+                            const int32_t *target, float *loss, float *lse, void *workspace, int64_t workspace_bytes, void *stream_)
+{
+    if (!sizes_ok(N, V, d)) return TFE_ERR_INVALID_ARG;
+    if (N == 0) return TFE_OK;
+    if (!rows_ok(hidden, ld_hidden, d) || !rows_ok(weight, ld_weight, d) || !aligned(target, 4) || !aligned(loss, 4) || !aligned(lse, 4) ||
+        !aligned(workspace, 256))
+        return TFE_ERR_INVALID_ARG;
+    const Plan q = make_plan(N, V, d);
+    const ForwardRoom room(q, N, d, workspace);
+    if (workspace_bytes < room.bytes) return TFE_ERR_CAPACITY;
+    const struct { const void *at; int64_t bytes; } in[] = {{hidden, ((int64_t)(N - 1) * ld_hidden + d) * 2}, {weight, ((int64_t)(V - 1) * ld_weight + d) * 2},
+                                                            {target, 4ll * N}, {workspace, room.bytes}};
+    for (const auto &x : in)
+        if (touch(x.at, x.bytes, loss, 4ll * N) || touch(x.at, x.bytes, lse, 4ll * N)) return TFE_ERR_INVALID_ARG;
+    if (touch(loss, 4ll * N, lse, 4ll * N)) return TFE_ERR_INVALID_ARG;
+    int sms = 0;
+    if (tfe_status st = device_sms(&sms)) return st;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    if (q.gather) {
+        CompactParams c{};
+        c.N = N; c.V = V; c.d = d; c.h = static_cast<const bf16 *>(hidden); c.ld = ld_hidden; c.target = target;
+        c.h_out = room.h; c.pos = room.pos; c.target_out = room.target; c.n_live = room.n_live;
+        if (tfe_status st = launch_compact(c, sms, stream)) return st;
+    }
+    Maps maps{};
+    if (!(q.gather ? make_map(&maps.a, room.h, q.n_pad, d, d, kRowsA) : make_map(&maps.a, hidden, N, d, ld_hidden, kRowsA)) ||
+        !make_map(&maps.b, weight, V, d, ld_weight, (uint32_t)(q.tn / kCtas)))
+        return bad_map();
+    GemmParams p{};
+    p.N = N; p.V = V; p.d = d; p.tn = q.tn; p.per_unit = q.per_unit; p.n_tiles = q.n_tiles; p.m_room = q.m_room;
+    p.give_up = g_xent_give_up.load(std::memory_order_relaxed);
+    p.n_live = room.n_live; p.target = q.gather ? room.target : target;
+    p.part = room.part; p.ld_part = q.n_pad; p.z_target = room.z_target;
+    if (tfe_status st = launch_gemm<kLse>((int64_t)q.m_room * (q.chunks / 2), sms, stream, maps, p)) return st;
+    LossParams l{};
+    l.N = N; l.V = V; l.chunks = q.chunks; l.part = room.part; l.ld_part = q.n_pad; l.z_target = room.z_target; l.target = target; l.pos = room.pos;
+    l.loss = loss; l.lse = lse;
+    return tfe_launch_serial(tfe_xent_loss_kernel, (unsigned)(((int64_t)N + 31) / 32), 32 * kLossLanes, 1, 0, stream, "cross entropy loss launch", l);
+}
+
+tfe_status tfe_xent_backward(const void *hidden, int64_t ld_hidden, int32_t N, const void *weight, int64_t ld_weight, int32_t V, int32_t d,
+                             const int32_t *target, const float *lse, const float *grad_loss, void *grad_hidden, int64_t ld_grad_hidden,
+                             void *grad_weight, int64_t ld_grad_weight, void *workspace, int64_t workspace_bytes, void *stream_)
+{
+    if (!sizes_ok(N, V, d) || (!grad_hidden && !grad_weight)) return TFE_ERR_INVALID_ARG;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    if (grad_weight && !rows_ok(grad_weight, ld_grad_weight, d)) return TFE_ERR_INVALID_ARG;
+    if (N == 0) {                               // nothing to sum: zeros
+        if (!grad_weight) return TFE_OK;
+        return tfe_note_cuda(cudaMemset2DAsync(grad_weight, (size_t)ld_grad_weight * 2, 0, (size_t)d * 2, (size_t)V, stream), "cudaMemset2DAsync");
+    }
+    if (!rows_ok(hidden, ld_hidden, d) || !rows_ok(weight, ld_weight, d) || !aligned(target, 4) || !aligned(lse, 4) || !aligned(grad_loss, 4) ||
+        !aligned(workspace, 256) || (grad_hidden && !rows_ok(grad_hidden, ld_grad_hidden, d)))
+        return TFE_ERR_INVALID_ARG;
+    const Plan q = make_plan(N, V, d);
+    const BackwardRoom room(q, N, d, workspace);
+    if (workspace_bytes < room.bytes) return TFE_ERR_CAPACITY;
+    const int64_t b_h = ((int64_t)(N - 1) * ld_hidden + d) * 2, b_w = ((int64_t)(V - 1) * ld_weight + d) * 2;
+    const int64_t b_gh = ((int64_t)(N - 1) * ld_grad_hidden + d) * 2, b_gw = ((int64_t)(V - 1) * ld_grad_weight + d) * 2;
+    const struct { const void *at; int64_t bytes; } in[] = {{hidden, b_h}, {weight, b_w}, {target, 4ll * N}, {lse, 4ll * N}, {grad_loss, 4ll * N}, {workspace, room.bytes}};
+    for (const auto &x : in)
+        if (touch(x.at, x.bytes, grad_hidden, b_gh) || touch(x.at, x.bytes, grad_weight, b_gw)) return TFE_ERR_INVALID_ARG;
+    if (touch(grad_hidden, b_gh, grad_weight, b_gw)) return TFE_ERR_INVALID_ARG;
+    int sms = 0;
+    if (tfe_status st = device_sms(&sms)) return st;
+    CompactParams c{};
+    c.N = N; c.V = V; c.d = d; c.h = static_cast<const bf16 *>(hidden); c.ld = ld_hidden; c.target = target; c.lse = lse; c.grad = grad_loss;
+    c.h_out = room.h; c.pos = room.pos; c.target_out = room.target; c.n_live = room.n_live; c.lse_out = room.lse; c.coef_out = room.coef; c.failed = room.failed;
+    if (tfe_status st = launch_compact(c, sms, stream)) return st;
+
+    Maps probs{}, grads{};
+    if (!make_map(&probs.a, room.h, q.n_pad, d, d, kRowsA) || !make_map(&probs.b, weight, V, d, ld_weight, kN / kCtas) ||
+        !make_map(&probs.out, room.g, q.n_pad, q.piece, q.piece, 32) || !make_map(&grads.a, room.g, q.n_pad, q.piece, q.piece, kRowsA) ||
+        !make_map(&grads.b, weight, V, d, ld_weight, 64) || !make_map(&grads.a_w, room.g, q.n_pad, q.piece, q.piece, 64) ||
+        !make_map(&grads.b_w, room.h, q.n_pad, d, d, 64) || (grad_weight && !make_map(&grads.out, grad_weight, V, d, ld_grad_weight, 32)))
+        return bad_map();
+    GemmParams p{};
+    p.N = N; p.V = V; p.d = d; p.m_room = q.m_room; p.splits = q.splits;
+    p.want_h = grad_hidden != nullptr; p.want_w = grad_weight != nullptr;
+    p.give_up = g_xent_give_up.load(std::memory_order_relaxed);
+    p.n_live = room.n_live; p.target = room.target; p.lse = room.lse; p.coef = room.coef; p.sum_h = room.sum_h; p.failed = room.failed;
+    for (int32_t i = 0; i < q.pieces; ++i) {
+        p.v0 = (int32_t)(i * q.piece);
+        p.width = (int32_t)std::min<int64_t>(q.piece, V - (int64_t)i * q.piece);
+        p.first = i == 0;
+        p.tn = kN;
+        if (tfe_status st = launch_gemm<kProb>((int64_t)q.m_room * ((p.width + kN - 1) / kN), sms, stream, probs, p)) return st;
+        p.tn = q.tn_d;
+        const int64_t most = (int64_t)q.cols * ((int64_t)p.want_h * q.m_room * q.splits + (int64_t)p.want_w * ((p.width + kM - 1) / kM));
+        if (tfe_status st = launch_gemm<kGrads>(most, sms, stream, grads, p)) return st;
+    }
+    RowsParams r{};
+    r.N = N; r.V = V; r.d = d; r.splits = q.splits; r.m_room = q.m_room; r.cols = q.cols; r.tn = q.tn_d; r.sum_h = room.sum_h; r.pos = room.pos;
+    r.failed = room.failed; r.grad_h = static_cast<bf16 *>(grad_hidden); r.ld_h = ld_grad_hidden; r.grad_w = static_cast<bf16 *>(grad_weight); r.ld_w = ld_grad_weight;
+    const unsigned grid = (unsigned)std::min<int64_t>(4ll * sms, ((int64_t)N + 31) / 32);
+    return tfe_launch_serial(tfe_xent_rows_kernel, grid, kRowsThreads, 1, 0, stream, "cross entropy gradient launch", r);
+}
+
+tfe_status tfe_xent_status(uint32_t *device_flags, void *stream_)
+{
+    if (!device_flags) return TFE_ERR_INVALID_ARG;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    void *at = nullptr;
+    if (tfe_status st = tfe_note_cuda(cudaGetSymbolAddress(&at, g_xent_status), "cudaGetSymbolAddress")) return st;
+    if (tfe_status st = tfe_note_cuda(cudaMemcpyAsync(device_flags, at, sizeof(uint32_t), cudaMemcpyDeviceToHost, stream), "cudaMemcpyAsync")) return st;
+    if (tfe_status st = tfe_note_cuda(cudaStreamSynchronize(stream), "cudaStreamSynchronize")) return st;
+    if (*device_flags == 0) return TFE_OK;
+    tfe_xent_status_kernel<<<1, 1, 0, stream>>>(*device_flags);
+    if (tfe_status st = tfe_note_cuda(cudaGetLastError(), "status launch")) return st;
+    if (tfe_status st = tfe_note_cuda(cudaStreamSynchronize(stream), "cudaStreamSynchronize")) return st;
+    return TFE_ERR_INTERNAL;
+}
+
+tfe_status tfe_xent_give_up(int32_t at_once)
+{
+    g_xent_give_up.store(at_once != 0, std::memory_order_relaxed);
+    return TFE_OK;
+}
+
+}  // extern "C"

@@ -507,3 +507,106 @@ def distill_loss(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_logits
     """distill_forward's loss [N] as a node of autograd: the gradient goes to the logits, none to the teacher.  Reduce it
     as the training wants, e.g. ``(distill_loss(z, ids, t) * weight).sum()``."""
     return _DistillLoss.apply(logits, teacher_ids, teacher_logits, tau)
+
+
+# ---- cross entropy from hidden states ----------------------------------------------------------
+
+
+def _bf16_rows(t: torch.Tensor, what: str):
+    """(rows, columns, elements between rows) of a bf16 matrix as the tensor cores' copies read it."""
+    if not t.is_cuda or t.dim() != 2 or t.dtype != torch.bfloat16:
+        raise ValueError(f"{what}: a 2-D bf16 CUDA tensor is needed")
+    n, d = t.shape
+    if n > tfe.XENT_MAX_ROWS or d > tfe.XENT_MAX_COLS or d < 8 or d % 8 != 0:
+        raise ValueError(f"{what}: at most 2^24 rows of a multiple of 8 up to 2^16 columns")
+    ld, step = t.stride()
+    if n <= 1:
+        ld = d
+    if step != 1 or ld < d or ld % 8 != 0 or (n and t.data_ptr() % 16 != 0):
+        raise ValueError(f"{what}: contiguous rows that start on 16-byte boundaries are needed")
+    return n, d, ld
+
+
+def _xent_operands(hidden, weight, target):
+    n, d, ld_h = _bf16_rows(hidden, "hidden")
+    v, dw, ld_w = _bf16_rows(weight, "weight")
+    dev = hidden.device
+    if v < 1 or dw != d or weight.device != dev:
+        raise ValueError("weight: rows of hidden's width on its device are needed")
+    t = _vector(target, (n,), torch.int32, dev, "target")
+    return (hidden.data_ptr(), ld_h, n, weight.data_ptr(), ld_w, v, d, t)
+
+
+def xent_forward(hidden: torch.Tensor, weight: torch.Tensor, target: torch.Tensor, *, stream=None):
+    """(loss, lse), fp32 [N] each: the softmax cross entropy of ``hidden @ weight.T`` against `target` (int32 [N]; an id outside
+    the vocabulary: no target, loss 0), without the logits (see tfe_xent_forward), and the log-sum-exp that the gradients need.
+    hidden [N, d] and weight [V, d] are bf16."""
+    if not _here(hidden.device, stream):
+        with _elsewhere(hidden.device, stream):
+            return _xent_forward(hidden, weight, target, stream)
+    return _xent_forward(hidden, weight, target, None)
+
+
+def _xent_forward(hidden, weight, target, stream):
+    rows = _xent_operands(hidden, weight, target)
+    dev, n, v, d = hidden.device, rows[2], rows[5], rows[6]
+    loss = torch.empty(n, dtype=torch.float32, device=dev)
+    lse = torch.empty(n, dtype=torch.float32, device=dev)
+    size = tfe.tfe_xent_forward_workspace_bytes(n, v, d)
+    workspace = torch.empty(size, dtype=torch.uint8, device=dev)
+    tfe.tfe_xent_forward(*rows, loss.data_ptr(), lse.data_ptr(), workspace.data_ptr(), size, _where(dev, stream))
+    return loss, lse
+
+
+def xent_backward(grad_loss: torch.Tensor, hidden: torch.Tensor, weight: torch.Tensor, target: torch.Tensor, lse: torch.Tensor, *,
+                  want_hidden: bool = True, want_weight: bool = True, stream=None):
+    """(grad_hidden, grad_weight), bf16, of sum(grad_loss * loss); None for one that is not wanted (see tfe_xent_backward)."""
+    if not _here(hidden.device, stream):
+        with _elsewhere(hidden.device, stream):
+            return _xent_backward(grad_loss, hidden, weight, target, lse, want_hidden, want_weight, stream)
+    return _xent_backward(grad_loss, hidden, weight, target, lse, want_hidden, want_weight, None)
+
+
+def _xent_backward(grad_loss, hidden, weight, target, lse, want_hidden, want_weight, stream):
+    rows = _xent_operands(hidden, weight, target)
+    dev, n, v, d = hidden.device, rows[2], rows[5], rows[6]
+    g = _vector(grad_loss, (n,), torch.float32, dev, "grad_loss")
+    norm = _vector(lse, (n,), torch.float32, dev, "lse")
+    if not want_hidden and not want_weight:
+        return None, None
+    gh = torch.empty((n, d), dtype=torch.bfloat16, device=dev) if want_hidden else None
+    gw = torch.empty((v, d), dtype=torch.bfloat16, device=dev) if want_weight else None
+    size = tfe.tfe_xent_backward_workspace_bytes(n, v, d)
+    workspace = torch.empty(size, dtype=torch.uint8, device=dev)
+    if n or want_weight:                # (no rows and no weights' gradient: nothing to write)
+        tfe.tfe_xent_backward(*rows, norm, g, gh.data_ptr() if want_hidden and n else None, d, gw.data_ptr() if want_weight else None, d,
+                              workspace.data_ptr(), size, _where(dev, stream))
+    return gh, gw
+
+
+def xent_status(stream=None) -> int:
+    """0, or the device's status word if a cross entropy call on it failed since the last report, which clears it (see
+    tfe_xent_status).  Synchronises."""
+    return tfe.tfe_xent_status(stream)
+
+
+class _LinearCrossEntropy(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, hidden, weight, target):
+        loss, lse = xent_forward(hidden, weight, target)
+        ctx.save_for_backward(hidden, weight, target, lse)
+        return loss
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_loss):
+        hidden, weight, target, lse = ctx.saved_tensors
+        want = ctx.needs_input_grad
+        grads = xent_backward(grad_loss.contiguous(), hidden, weight, target, lse, want_hidden=want[0], want_weight=want[1])
+        return *grads, None
+
+
+def linear_cross_entropy(hidden: torch.Tensor, weight: torch.Tensor, target: torch.Tensor) -> torch.Tensor:
+    """xent_forward's loss [N] as a node of autograd: gradients go to `hidden` and `weight`.  Reduce it as the training wants, e.g.
+    ``linear_cross_entropy(h, w, t).sum() / (t >= 0).sum()``."""
+    return _LinearCrossEntropy.apply(hidden, weight, target)
