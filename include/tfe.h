@@ -664,6 +664,75 @@ tfe_status tfe_xent_status(uint32_t *device_flags, void *stream);
 tfe_status tfe_xent_give_up(int32_t at_once);
 
 /*
+ * Injection between two norms (paper Sec. 2.2: h' = h + g m with a gate that is a "scalar, vector, or learned function"; the norms are
+ * this library's): a norm on the memory vector, a learned gate, the residual scale lam, and the norm that the next block starts
+ * with, in one pass, and its gradients in another.  Per row, with rms(x) = sqrt(mean(x^2) + eps) and s = gate, or 1 / (1 + exp(-gate))
+ * with `sigmoid`, or 1 without a gate:
+ *     out = h + lam s (post_weight m / rms(m)),      normed = next_weight out / rms(out)
+ *
+ *   h, m             DEVICE [Q][ld], rows of d elements of type dtype (TFE_DTYPE_*); 0 <= Q <= TFE_ROWS_MAX,
+ *                    1 <= d <= TFE_INJECT_NORM_MAX_COLS, ld >= d; rows need no alignment beyond the element's own (16-byte rows
+ *                    of a multiple of 8 elements are faster).
+ *   gate             TFE_GATE_SCALAR: DEVICE float [Q];  TFE_GATE_VECTOR: DEVICE [Q][ld_gate] of type dtype;  TFE_GATE_NONE: not read.
+ *   weights          DEVICE [d] each, of type weight_dtype.
+ *   lam, eps         lam finite, 0 <= eps <= 1.
+ *   out, normed      DEVICE [Q][ld] of type dtype, rounded once each (normed comes from out before its rounding).  out may be h itself
+ *                    (same pointer and distance); they must not touch an operand or each other otherwise.
+ *   grads            gradients that arrive (grad_out, grad_normed; NULL: zero, one at least is given) and those to make, of the
+ *                    operands' types and shapes (grad_gate float [Q] for a scalar gate), NULL where not wanted; none may touch
+ *                    anything else.  Sums run in fp32 in an order that the sizes fix; each result is rounded once.
+ *   workspace        for grad_post and grad_next: DEVICE scratch, 16-byte aligned, of tfe_inject_norm_workspace_bytes(Q, d) bytes
+ *                    (smaller: TFE_ERR_CAPACITY), contents undefined before and after.
+ * A row of zeros has a norm of sqrt(eps) (with eps = 0 it gives NaN); mean squares must lie within fp32's range.  NaN stays in its row
+ * and in the weights' gradients.  One launch forward, one or two backward.  Errors: INVALID_ARG, CAPACITY, CUDA.
+ */
+#define TFE_INJECT_NORM_MAX_COLS 8192
+enum { TFE_GATE_NONE = 0, TFE_GATE_SCALAR = 1, TFE_GATE_VECTOR = 2 };
+typedef struct {
+    int32_t     dtype, Q, d;
+    int32_t     gate_kind, sigmoid, weight_dtype;
+    const void *h, *m, *gate;
+    int64_t     ld_h, ld_m, ld_gate;
+    const void *post_weight, *next_weight;
+    float       lam, eps;
+} tfe_inject_norm_params;
+typedef struct {
+    const void *grad_out, *grad_normed;
+    int64_t     ld_grad_out, ld_grad_normed;
+    void       *grad_h, *grad_m, *grad_gate;
+    int64_t     ld_grad_h, ld_grad_m, ld_grad_gate;
+    void       *grad_post, *grad_next;
+} tfe_inject_norm_grads;
+tfe_status tfe_inject_norm_forward(const tfe_inject_norm_params *params, void *out, int64_t ld_out, void *normed, int64_t ld_normed,
+                                   void *stream);
+int64_t tfe_inject_norm_workspace_bytes(int32_t Q, int32_t d);      /* -1 for invalid arguments */
+tfe_status tfe_inject_norm_backward(const tfe_inject_norm_params *params, const tfe_inject_norm_grads *grads, void *workspace,
+                                    int64_t workspace_bytes, void *stream);
+
+/*
+ * The norm of many gradients taken together, and clipping by it (no counterpart in the paper: the end of a training step).
+ *     norm = sqrt(sum of x^2 over all elements of all tensors),   results = x min(1, max_norm / norm)
+ *   tensors          HOST array of n DEVICE addresses; numel HOST int64 [n] (0 is a tensor without elements; at most 2^40 each, fewer
+ *                    than 2^45 together); dtype HOST int32 [n], TFE_DTYPE_*.  0 <= n <= TFE_CLIP_MAX_TENSORS.  Elements lie side by side.
+ *   results          HOST array of n DEVICE addresses of the same sizes and types, or NULL: in place.  A result may be its own tensor;
+ *                    otherwise nothing that is written may touch anything else.  In place, nothing is written where norm <= max_norm.
+ *   max_norm         >= 0 (+inf: clips nothing).
+ *   norm             DEVICE float: the norm before clipping.  Squares are summed in fp32 by fours or eights, those sums in fp64; no
+ *                    element is too large or too small.  Where it is not finite (an element was not, or it is beyond fp64) the
+ *                    elements stay as they are.
+ *   workspace        DEVICE scratch, 8-byte aligned, of tfe_clip_workspace_bytes(n) bytes (smaller: TFE_ERR_CAPACITY), contents
+ *                    undefined before and after.
+ * Each result is rounded once; the order of the sums depends on the sizes alone.  The lists are read before the calls return.  Two
+ * launches for each 900 tensors.  tfe_grad_norm gives the norm alone.  Errors: INVALID_ARG, CAPACITY, CUDA, INTERNAL (no host memory).
+ */
+#define TFE_CLIP_MAX_TENSORS (1 << 20)
+int64_t tfe_clip_workspace_bytes(int32_t n);                        /* -1 for invalid arguments */
+tfe_status tfe_grad_norm(const uint64_t *tensors, const int64_t *numel, const int32_t *dtype, int32_t n, float *norm, void *workspace,
+                         int64_t workspace_bytes, void *stream);
+tfe_status tfe_clip_grad_norm(const uint64_t *tensors, const uint64_t *results, const int64_t *numel, const int32_t *dtype, int32_t n,
+                              float max_norm, float *norm, void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
  * Streaming copy (the paper has no counterpart: a yardstick for the measurements, not a step of the method).
  * Copies `bytes` bytes from `src` to `dst` (DEVICE, 16-byte aligned, bytes a multiple of 16, ranges must not
  * overlap) with the load / store instructions the lookup kernels stream hidden states with, one asynchronous

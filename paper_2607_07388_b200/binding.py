@@ -38,7 +38,8 @@ EXPORTS = ["tfe_index_build", "tfe_index_build_device", "tfe_cache_install", "tf
            "tfe_cache_select_tuning", "tfe_distill_forward", "tfe_distill_backward", "tfe_sample_tokens",
            "tfe_quantize_fp8", "tfe_quantize_fp8_ld", "tfe_matmul_fp8", "tfe_matmul_fp8_status", "tfe_matmul_fp8_give_up",
            "tfe_xent_forward_workspace_bytes", "tfe_xent_backward_workspace_bytes", "tfe_xent_forward", "tfe_xent_backward",
-           "tfe_xent_status", "tfe_xent_give_up"]
+           "tfe_xent_status", "tfe_xent_give_up", "tfe_inject_norm_forward", "tfe_inject_norm_backward", "tfe_inject_norm_workspace_bytes",
+           "tfe_grad_norm", "tfe_clip_grad_norm", "tfe_clip_workspace_bytes"]
 
 
 class TfeConfig(C.Structure):
@@ -58,6 +59,19 @@ class TfePrefetchParams(C.Structure):
 
 class TfeSampleParams(C.Structure):
     _fields_ = [("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p)]
+
+
+class TfeInjectNormParams(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("Q", C.c_int32), ("d", C.c_int32), ("gate_kind", C.c_int32), ("sigmoid", C.c_int32),
+                ("weight_dtype", C.c_int32), ("h", C.c_void_p), ("m", C.c_void_p), ("gate", C.c_void_p), ("ld_h", C.c_int64),
+                ("ld_m", C.c_int64), ("ld_gate", C.c_int64), ("post_weight", C.c_void_p), ("next_weight", C.c_void_p),
+                ("lam", C.c_float), ("eps", C.c_float)]
+
+
+class TfeInjectNormGrads(C.Structure):
+    _fields_ = [("grad_out", C.c_void_p), ("grad_normed", C.c_void_p), ("ld_grad_out", C.c_int64), ("ld_grad_normed", C.c_int64),
+                ("grad_h", C.c_void_p), ("grad_m", C.c_void_p), ("grad_gate", C.c_void_p), ("ld_grad_h", C.c_int64),
+                ("ld_grad_m", C.c_int64), ("ld_grad_gate", C.c_int64), ("grad_post", C.c_void_p), ("grad_next", C.c_void_p)]
 
 
 class TfeError(RuntimeError):
@@ -134,6 +148,13 @@ def lib() -> C.CDLL:
         L.tfe_xent_backward.argtypes = [vp, i64, i32, vp, i64, i32, i32, vp, vp, vp, vp, i64, vp, i64, vp, i64, vp]
         L.tfe_xent_status.argtypes = [C.POINTER(C.c_uint32), vp]
         L.tfe_xent_give_up.argtypes = [i32]
+        L.tfe_inject_norm_forward.argtypes = [C.POINTER(TfeInjectNormParams), vp, i64, vp, i64, vp]
+        L.tfe_inject_norm_backward.argtypes = [C.POINTER(TfeInjectNormParams), C.POINTER(TfeInjectNormGrads), vp, i64, vp]
+        L.tfe_inject_norm_workspace_bytes.argtypes = [i32, i32]
+        L.tfe_grad_norm.argtypes = [vp, vp, vp, i32, vp, vp, i64, vp]
+        L.tfe_clip_grad_norm.argtypes = [vp, vp, vp, vp, i32, f32, vp, vp, i64, vp]
+        L.tfe_clip_workspace_bytes.argtypes = [i32]
+        L.tfe_inject_norm_workspace_bytes.restype = L.tfe_clip_workspace_bytes.restype = i64
         L.tfe_sample_tokens.argtypes = [vp, i32, i32, i32, i64, C.POINTER(TfeSampleParams), vp, vp, vp, vp]
         L.tfe_distill_forward.argtypes = [vp, i32, i32, i32, i64, vp, vp, i32, f32, vp, vp, vp]
         L.tfe_distill_backward.argtypes = [vp, i32, i32, i32, i64, vp, vp, i32, f32, vp, vp, vp, i64, vp]
@@ -145,7 +166,8 @@ def lib() -> C.CDLL:
                      "tfe_head_geometry", "tfe_mine_ngrams", "tfe_assign_residency", "tfe_cache_select_tuning",
                      "tfe_distill_forward", "tfe_distill_backward", "tfe_sample_tokens", "tfe_quantize_fp8", "tfe_quantize_fp8_ld",
                      "tfe_matmul_fp8", "tfe_matmul_fp8_status", "tfe_matmul_fp8_give_up", "tfe_xent_forward", "tfe_xent_backward",
-                     "tfe_xent_status", "tfe_xent_give_up"):
+                     "tfe_xent_status", "tfe_xent_give_up", "tfe_inject_norm_forward", "tfe_inject_norm_backward", "tfe_grad_norm",
+                     "tfe_clip_grad_norm"):
             getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -574,3 +596,47 @@ def tfe_xent_status(stream=None) -> int:
 def tfe_xent_give_up(at_once: bool) -> None:
     """The waits of the cross entropy calls that follow count as run out from the start, until it is called with False."""
     _check(lib().tfe_xent_give_up(int(at_once)), "tfe_xent_give_up")
+
+
+# -- injection between two norms ----------------------------------------------------------------
+INJECT_NORM_MAX_COLS = 8192
+GATE_NONE, GATE_SCALAR, GATE_VECTOR = 0, 1, 2
+
+
+def tfe_inject_norm_workspace_bytes(Q: int, d: int) -> int:
+    return lib().tfe_inject_norm_workspace_bytes(Q, d)
+
+
+def tfe_inject_norm_forward(params: TfeInjectNormParams, out, ld_out: int, normed, ld_normed: int, stream=None) -> None:
+    st = lib().tfe_inject_norm_forward(C.byref(params), out, ld_out, normed, ld_normed, _stream(stream))
+    if st:
+        raise TfeError(st, "tfe_inject_norm_forward")
+
+
+def tfe_inject_norm_backward(params: TfeInjectNormParams, grads: TfeInjectNormGrads, workspace, workspace_bytes: int, stream=None) -> None:
+    st = lib().tfe_inject_norm_backward(C.byref(params), C.byref(grads), workspace, workspace_bytes, _stream(stream))
+    if st:
+        raise TfeError(st, "tfe_inject_norm_backward")
+
+
+# -- the norm of many gradients, and clipping by it ---------------------------------------------
+CLIP_MAX_TENSORS = 1 << 20
+
+
+def tfe_clip_workspace_bytes(n: int) -> int:
+    return lib().tfe_clip_workspace_bytes(n)
+
+
+def tfe_grad_norm(tensors, numel, dtype, n: int, norm, workspace, workspace_bytes: int, stream=None) -> None:
+    """The lists are host arrays: addresses uint64, numel int64, dtype int32."""
+    st = lib().tfe_grad_norm(_addr(tensors), _addr(numel), _addr(dtype), n, norm, workspace, workspace_bytes, _stream(stream))
+    if st:
+        raise TfeError(st, "tfe_grad_norm")
+
+
+def tfe_clip_grad_norm(tensors, results, numel, dtype, n: int, max_norm: float, norm, workspace, workspace_bytes: int, stream=None) -> None:
+    """As tfe_grad_norm; results: addresses uint64, or None for in place."""
+    st = lib().tfe_clip_grad_norm(_addr(tensors), _addr(results), _addr(numel), _addr(dtype), n, max_norm, norm, workspace,
+                                  workspace_bytes, _stream(stream))
+    if st:
+        raise TfeError(st, "tfe_clip_grad_norm")

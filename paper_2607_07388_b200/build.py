@@ -10,7 +10,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtfe.so")
 SOURCES = [os.path.join(CSRC, "tfe_api.cu"), os.path.join(CSRC, "tfe_head.cu"), os.path.join(CSRC, "tfe_mine.cu"),
            os.path.join(CSRC, "tfe_distill.cu"), os.path.join(CSRC, "tfe_sample.cu"),
-           os.path.join(CSRC, "tfe_fp8.cu"), os.path.join(CSRC, "tfe_xent.cu")]
+           os.path.join(CSRC, "tfe_fp8.cu"), os.path.join(CSRC, "tfe_xent.cu"),
+           os.path.join(CSRC, "tfe_inject_norm.cu"), os.path.join(CSRC, "tfe_clip.cu")]
 DEPS = SOURCES + [os.path.join(CSRC, "tfe_kernels.cuh"), os.path.join(CSRC, "tfe_key.cuh"), os.path.join(CSRC, "tfe_rows.cuh"), os.path.join(CSRC, "tfe_tc.cuh"),
                   os.path.join(CSRC, "tfe_internal.h"), os.path.join(os.path.dirname(HERE), "include", "tfe.h")]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",

@@ -1,0 +1,524 @@
+// Injection between two norms, forward and backward: the injection rule h' = h + g m (paper Sec. 2.2) with a norm on the memory
+// vector, a learned gate (the paper: "scalar, vector, or learned function") and the norm that the next block starts with.
+//
+//   a = 1 / sqrt(mean(m^2) + eps)    y = w_post a m          s = gate or sigmoid(gate), 1 without a gate
+//   u = h + lam s y                  b = 1 / sqrt(mean(u^2) + eps)        n = w_next b u
+// With U, N the gradients that arrive at u and n, and t = w_next N:
+//   dh = U + b t - b^3 u mean(u t)                           dw_next = sum over rows of N b u
+//   ds = lam y dh  (summed over the columns for a scalar gate, times s (1 - s) for a sigmoid)
+//   x = lam s w_post dh              dm = a x - a^3 m mean(m x)            dw_post = sum over rows of lam s dh a m
+//
+// HBM bounds both.  A row is held in the registers of `row_threads` threads, eight columns each, so every operand is read once and every
+// intermediate stays on the chip; backward makes a, y, u and b again rather than reading them.  Several rows share a block, and a
+// block walks rows with the next row's loads under way.  u is rounded once for the output, n and the gradients come from it as it was
+// before.  The weights' gradients are summed over a block's rows in registers, over its groups in shared memory, and over the blocks
+// by a second kernel: no atomics, the order depends on the sizes alone.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+
+#include "../../include/tfe.h"
+#include "tfe_internal.h"
+#include "tfe_rows.cuh"
+
+namespace {
+
+using tfe_rows::Elem;
+
+constexpr int kCols = 8;                        // columns of a thread
+constexpr int kBlock = 512;                     // threads of a block that holds several rows, at most
+constexpr int kMaxBlocks = 592;                 // whatever the device has: bounds the partial sums of the backward pass
+
+struct NormParams {
+    int32_t Q, d;
+    int32_t row_threads, groups;                // threads of a row, rows of a block at a time
+    const void *h, *m, *gate; int64_t ld_h, ld_m, ld_gate;
+    int32_t gate_kind, sigmoid, weights_f32;
+    const void *w_post, *w_next;
+    float lam, eps;
+    void *out, *normed; int64_t ld_out, ld_normed;
+    const void *g_out, *g_normed; int64_t ld_g_out, ld_g_normed;
+    void *g_h, *g_m, *g_gate; int64_t ld_g_h, ld_g_m, ld_g_gate;
+    float *part;                                // [blocks][2][d]: sums for w_post and w_next
+};
+
+// A thread's eight columns of a row as they were read: 8 t .. 8 t + 7 for thread t (kVector: 16-byte vectors), or t, t + row_threads, ...;
+// zeros beyond the row.
+template <typename T, bool kVector>
+struct Eight {
+    static constexpr int kWords = (int)sizeof(T) * 2;
+    uint32_t w[kWords];
+
+    __device__ __forceinline__ void load(const void *base, int64_t ld, int64_t row, int32_t d, int t, int threads, bool any)
+    {
+        const T *at = static_cast<const T *>(base) + row * ld;
+        if constexpr (kVector) {
+#pragma unroll
+            for (int i = 0; i < kWords / 4; ++i) {
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (any && kCols * t < d) v = tfe_rows::load_stream(reinterpret_cast<const uint4 *>(at + kCols * t) + i);
+                w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < kCols; ++e) {
+                const int32_t c = t + e * threads;
+                const bool in = any && c < d;
+                if constexpr (sizeof(T) == 4) {
+                    w[e] = in ? __float_as_uint(at[c]) : 0u;
+                } else {
+                    const uint32_t x = in ? (uint32_t)__bfloat16_as_ushort(at[c]) : 0u;
+                    w[e / 2] = e & 1 ? w[e / 2] | (x << 16) : x;
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ float get(int e) const
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
+        else return __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
+    }
+};
+
+template <typename T, bool kVector>
+__device__ __forceinline__ void store(void *base, int64_t ld, int64_t row, int32_t d, int t, int threads, const float (&x)[kCols])
+{
+    T *at = static_cast<T *>(base) + row * ld;
+    if constexpr (kVector) {
+        if (kCols * t >= d) return;
+        uint4 *to = reinterpret_cast<uint4 *>(at + kCols * t);
+        constexpr int E = Elem<T>::kPerVec;
+#pragma unroll
+        for (int i = 0; i < kCols / E; ++i) {
+            float part[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) part[e] = x[i * E + e];
+            __stcs(to + i, Elem<T>::pack(part));
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < kCols; ++e)
+            if (t + e * threads < d) Elem<T>::put(at + t + e * threads, x[e]);
+    }
+}
+
+template <bool kVector>
+__device__ __forceinline__ int32_t column(int e, int t, int threads) { return kVector ? kCols * t + e : t + e * threads; }
+
+template <bool kVector>
+__device__ __forceinline__ void load_weight(const void *w, bool f32, int32_t d, int t, int threads, float (&x)[kCols])
+{
+#pragma unroll
+    for (int e = 0; e < kCols; ++e) {
+        const int32_t c = column<kVector>(e, t, threads);
+        x[e] = c >= d ? 0.f : f32 ? static_cast<const float *>(w)[c] : __bfloat162float(static_cast<const __nv_bfloat16 *>(w)[c]);
+    }
+}
+
+// Sums over the threads of a row.  Each use needs a slot of its own until every thread has passed the next one's barrier: two in turn.
+struct RowSum {
+    float2 *slots;                              // [2][32] of this row's group
+    int warps, warp, barrier, threads, turn;
+
+    __device__ __forceinline__ float2 operator()(float2 x)
+    {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            x.x += __shfl_xor_sync(0xFFFFFFFFu, x.x, o);
+            x.y += __shfl_xor_sync(0xFFFFFFFFu, x.y, o);
+        }
+        if (warps == 1) return x;
+        float2 *s = slots + 32 * turn;
+        turn ^= 1;
+        if ((threadIdx.x & 31) == 0) s[warp] = x;
+        asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(threads) : "memory");
+        x = s[0];
+        for (int i = 1; i < warps; ++i) { x.x += s[i].x; x.y += s[i].y; }
+        return x;
+    }
+};
+
+__device__ __forceinline__ float inverse_root(float square, float inv_d, float eps) { return __frsqrt_rn(fmaf(square, inv_d, eps)); }
+template <typename T> __device__ __forceinline__ float sigmoid(float x) { return __frcp_rn(1.f + (sizeof(T) == 4 ? expf(-x) : __expf(-x))); }
+
+// What both directions make of a row: the gate, a and y, u and (with the next sum) b.
+template <typename T, bool kVector>
+struct Row {
+    Eight<T, kVector> h, m, gate;
+    float scalar;
+
+    __device__ __forceinline__ void load(const NormParams &p, int64_t row, int t)
+    {
+        const bool any = row < p.Q;
+        h.load(p.h, p.ld_h, row, p.d, t, p.row_threads, any);
+        m.load(p.m, p.ld_m, row, p.d, t, p.row_threads, any);
+        if (p.gate_kind == TFE_GATE_VECTOR) gate.load(p.gate, p.ld_gate, row, p.d, t, p.row_threads, any);
+        scalar = any && p.gate_kind == TFE_GATE_SCALAR ? static_cast<const float *>(p.gate)[row] : 1.f;
+    }
+    __device__ __forceinline__ void gates(const NormParams &p, float (&s)[kCols]) const
+    {
+        if (p.gate_kind == TFE_GATE_VECTOR) {
+#pragma unroll
+            for (int e = 0; e < kCols; ++e) s[e] = p.sigmoid ? sigmoid<T>(gate.get(e)) : gate.get(e);
+        } else {
+            const float x = p.gate_kind == TFE_GATE_SCALAR && p.sigmoid ? sigmoid<T>(scalar) : scalar;
+#pragma unroll
+            for (int e = 0; e < kCols; ++e) s[e] = x;
+        }
+    }
+    __device__ __forceinline__ float square_m() const
+    {
+        float s = 0.f;
+#pragma unroll
+        for (int e = 0; e < kCols; ++e) s = fmaf(m.get(e), m.get(e), s);
+        return s;
+    }
+};
+
+// Whether a thread has registers to hold the next row's operands beside this row's: 16-bit rows in blocks of up to kBlock threads.
+template <typename T, int kThreads> constexpr bool kAhead = sizeof(T) == 2 && kThreads <= kBlock;
+
+template <typename T, bool kVector, int kThreads>
+__global__ void __launch_bounds__(kThreads, kThreads <= kBlock ? 2 : 1)
+tfe_inject_norm_forward_kernel(const NormParams p)
+{
+    __shared__ float2 s_slots[kThreads / 32][2][32];
+    tfe_wait_for_stream();
+    const int group = threadIdx.x / p.row_threads, t = threadIdx.x - group * p.row_threads;
+    RowSum row_sum{&s_slots[group][0][0], p.row_threads / 32, t / 32, group + 1, p.row_threads, 0};
+    float wp[kCols], wn[kCols];
+    load_weight<kVector>(p.w_post, p.weights_f32, p.d, t, p.row_threads, wp);
+    load_weight<kVector>(p.w_next, p.weights_f32, p.d, t, p.row_threads, wn);
+    const float inv_d = 1.f / (float)p.d;
+    const int64_t step = (int64_t)gridDim.x * p.groups;
+    int64_t row = (int64_t)blockIdx.x * p.groups + group;
+    Row<T, kVector> x, next;
+    if (kAhead<T, kThreads>) next.load(p, row, t);
+    for (; row < p.Q; row += step) {
+        if constexpr (kAhead<T, kThreads>) {
+            x = next;
+            if (row + step < p.Q) next.load(p, row + step, t);
+        } else {
+            x.load(p, row, t);
+        }
+        const float a = inverse_root(row_sum(make_float2(x.square_m(), 0.f)).x, inv_d, p.eps);
+        float u[kCols], square = 0.f;
+        x.gates(p, u);
+#pragma unroll
+        for (int e = 0; e < kCols; ++e) {
+            u[e] = fmaf(p.lam * u[e], x.m.get(e) * a * wp[e], x.h.get(e));
+            square = fmaf(u[e], u[e], square);
+        }
+        const float b = inverse_root(row_sum(make_float2(square, 0.f)).x, inv_d, p.eps);
+        store<T, kVector>(p.out, p.ld_out, row, p.d, t, p.row_threads, u);
+#pragma unroll
+        for (int e = 0; e < kCols; ++e) u[e] *= b * wn[e];
+        store<T, kVector>(p.normed, p.ld_normed, row, p.d, t, p.row_threads, u);
+    }
+}
+
+template <typename T, bool kVector, int kThreads>
+__global__ void __launch_bounds__(kThreads, 1)
+tfe_inject_norm_backward_kernel(const NormParams p)
+{
+    __shared__ float2 s_slots[kThreads / 32][2][32];
+    extern __shared__ float s_sum[];            // [2][d], for several groups
+    tfe_wait_for_stream();
+    const int group = threadIdx.x / p.row_threads, t = threadIdx.x - group * p.row_threads;
+    RowSum row_sum{&s_slots[group][0][0], p.row_threads / 32, t / 32, group + 1, p.row_threads, 0};
+    float wp[kCols], wn[kCols], sum_p[kCols], sum_n[kCols];
+    load_weight<kVector>(p.w_post, p.weights_f32, p.d, t, p.row_threads, wp);
+    load_weight<kVector>(p.w_next, p.weights_f32, p.d, t, p.row_threads, wn);
+#pragma unroll
+    for (int e = 0; e < kCols; ++e) sum_p[e] = sum_n[e] = 0.f;
+    const float inv_d = 1.f / (float)p.d;
+    const int64_t step = (int64_t)gridDim.x * p.groups;
+    int64_t row = (int64_t)blockIdx.x * p.groups + group;
+    struct All {
+        Row<T, kVector> x;
+        Eight<T, kVector> gu, gn;
+        __device__ __forceinline__ void load(const NormParams &p, int64_t r, int t)
+        {
+            x.load(p, r, t);
+            gu.load(p.g_out, p.ld_g_out, r, p.d, t, p.row_threads, r < p.Q && p.g_out);
+            gn.load(p.g_normed, p.ld_g_normed, r, p.d, t, p.row_threads, r < p.Q && p.g_normed);
+        }
+    };
+    All all, next;
+    if (kAhead<T, kThreads>) next.load(p, row, t);
+    for (; row < p.Q; row += step) {
+        if constexpr (kAhead<T, kThreads>) {
+            all = next;
+            if (row + step < p.Q) next.load(p, row + step, t);
+        } else {
+            all.load(p, row, t);
+        }
+        const Row<T, kVector> &x = all.x;
+        const float a = inverse_root(row_sum(make_float2(x.square_m(), 0.f)).x, inv_d, p.eps);
+        float s[kCols], u[kCols];
+        x.gates(p, s);
+        float2 two = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int e = 0; e < kCols; ++e) {
+            u[e] = fmaf(p.lam * s[e], x.m.get(e) * a * wp[e], x.h.get(e));
+            two.x = fmaf(u[e], u[e], two.x);
+            two.y = fmaf(u[e], wn[e] * all.gn.get(e), two.y);
+        }
+        two = row_sum(two);
+        const float b = inverse_root(two.x, inv_d, p.eps), by_u = b * b * b * two.y * inv_d;
+        two = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int e = 0; e < kCols; ++e) {
+            const float n = all.gn.get(e);
+            sum_n[e] = fmaf(n, b * u[e], sum_n[e]);
+            u[e] = fmaf(-by_u, u[e], fmaf(b, wn[e] * n, all.gu.get(e)));       // dh
+            const float dy = p.lam * s[e] * u[e], ma = x.m.get(e) * a;
+            sum_p[e] = fmaf(dy, ma, sum_p[e]);
+            two.x = fmaf(x.m.get(e), wp[e] * dy, two.x);
+            two.y = fmaf(u[e], ma * wp[e], two.y);
+        }
+        if (p.g_h) store<T, kVector>(p.g_h, p.ld_g_h, row, p.d, t, p.row_threads, u);
+        two = row_sum(two);
+        const float by_m = a * a * a * two.x * inv_d;
+        if (p.g_m) {
+            float dm[kCols];
+#pragma unroll
+            for (int e = 0; e < kCols; ++e) dm[e] = fmaf(-by_m, x.m.get(e), a * wp[e] * (p.lam * s[e] * u[e]));
+            store<T, kVector>(p.g_m, p.ld_g_m, row, p.d, t, p.row_threads, dm);
+        }
+        if (p.g_gate && p.gate_kind == TFE_GATE_VECTOR) {
+#pragma unroll
+            for (int e = 0; e < kCols; ++e) u[e] = p.lam * u[e] * (x.m.get(e) * a * wp[e]) * (p.sigmoid ? s[e] * (1.f - s[e]) : 1.f);
+            store<T, kVector>(p.g_gate, p.ld_g_gate, row, p.d, t, p.row_threads, u);
+        } else if (p.g_gate && t == 0) {
+            static_cast<float *>(p.g_gate)[row] = p.lam * two.y * (p.sigmoid ? s[0] * (1.f - s[0]) : 1.f);
+        }
+    }
+    if (!p.part) return;
+    float *to = p.groups > 1 ? s_sum : p.part + (int64_t)blockIdx.x * 2 * p.d;
+    for (int g = 0; g < p.groups; ++g) {
+        if (group == g)
+#pragma unroll
+            for (int e = 0; e < kCols; ++e) {
+                const int32_t c = column<kVector>(e, t, p.row_threads);
+                if (c < p.d) {
+                    to[c] = g == 0 ? sum_p[e] : to[c] + sum_p[e];
+                    to[p.d + c] = g == 0 ? sum_n[e] : to[p.d + c] + sum_n[e];
+                }
+            }
+        if (p.groups > 1) __syncthreads();
+    }
+    if (p.groups > 1)
+        for (int32_t c = threadIdx.x; c < 2 * p.d; c += blockDim.x) p.part[(int64_t)blockIdx.x * 2 * p.d + c] = s_sum[c];
+}
+
+struct JoinParams {
+    int32_t blocks, d, f32;
+    const float *part;
+    void *g_post, *g_next;
+};
+constexpr int kJoinCols = 32, kJoinParts = 32;
+
+__global__ void __launch_bounds__(kJoinCols * kJoinParts)
+tfe_inject_norm_join_kernel(const JoinParams p)
+{
+    __shared__ float s_sum[kJoinParts][kJoinCols + 1];
+    tfe_wait_for_stream();
+    const int lane = threadIdx.x & 31, part = threadIdx.x >> 5;
+    const int32_t c = blockIdx.x * kJoinCols + lane;
+    float sum = 0.f;
+    if (c < 2 * p.d)
+#pragma unroll 4
+        for (int32_t b = part; b < p.blocks; b += kJoinParts) sum += p.part[(int64_t)b * 2 * p.d + c];
+    s_sum[part][lane] = sum;
+    __syncthreads();
+    sum = s_sum[lane][part];                    // column `part` now, from 32 parts
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+    const int32_t mine = blockIdx.x * kJoinCols + part;
+    if (lane != 0 || mine >= 2 * p.d) return;
+    void *to = mine < p.d ? p.g_post : p.g_next;
+    if (!to) return;
+    if (p.f32) static_cast<float *>(to)[mine % p.d] = sum;
+    else static_cast<__nv_bfloat16 *>(to)[mine % p.d] = __float2bfloat16_rn(sum);
+}
+
+// ------------------------------------------------------------------ host side
+
+struct Matrix { const void *at; int64_t ld; };
+
+int64_t elem_size(int32_t dtype) { return dtype == TFE_DTYPE_BF16 ? 2 : 4; }
+bool aligned(const void *p, uintptr_t to) { return p && reinterpret_cast<uintptr_t>(p) % to == 0; }
+bool matrix_ok(const void *at, int64_t ld, int32_t d, int64_t es) { return aligned(at, es) && ld >= d && ld <= (1ll << 34); }
+
+struct Span { const void *at; int64_t bytes; };
+bool touch(const Span &a, const Span &b)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
+    return a.at && b.at && x < y + (uintptr_t)b.bytes && y < x + (uintptr_t)a.bytes;
+}
+
+bool params_ok(const tfe_inject_norm_params *q)
+{
+    if (!q || (q->dtype != TFE_DTYPE_BF16 && q->dtype != TFE_DTYPE_F32) || (q->weight_dtype != TFE_DTYPE_BF16 && q->weight_dtype != TFE_DTYPE_F32)) return false;
+    if (q->Q < 0 || q->Q > TFE_ROWS_MAX || q->d < 1 || q->d > TFE_INJECT_NORM_MAX_COLS) return false;
+    if (q->gate_kind < TFE_GATE_NONE || q->gate_kind > TFE_GATE_VECTOR) return false;
+    if (!(q->eps >= 0.f) || !(q->eps <= 1.f) || !(q->lam - q->lam == 0.f)) return false;
+    const int64_t ws = elem_size(q->weight_dtype);
+    if (!aligned(q->post_weight, ws) || !aligned(q->next_weight, ws)) return false;
+    if (q->Q == 0) return true;
+    const int64_t es = elem_size(q->dtype);
+    if (!matrix_ok(q->h, q->ld_h, q->d, es) || !matrix_ok(q->m, q->ld_m, q->d, es)) return false;
+    if (q->gate_kind == TFE_GATE_SCALAR && !aligned(q->gate, 4)) return false;
+    if (q->gate_kind == TFE_GATE_VECTOR && !matrix_ok(q->gate, q->ld_gate, q->d, es)) return false;
+    return true;
+}
+
+NormParams shared_params(const tfe_inject_norm_params *q)
+{
+    NormParams p{};
+    p.Q = q->Q; p.d = q->d; p.h = q->h; p.m = q->m; p.gate = q->gate; p.ld_h = q->ld_h; p.ld_m = q->ld_m; p.ld_gate = q->ld_gate;
+    p.gate_kind = q->gate_kind; p.sigmoid = q->sigmoid != 0; p.weights_f32 = q->weight_dtype == TFE_DTYPE_F32;
+    p.w_post = q->post_weight; p.w_next = q->next_weight; p.lam = q->lam; p.eps = q->eps;
+    p.row_threads = (q->d + 32 * kCols - 1) / (32 * kCols) * 32;
+    return p;
+}
+int64_t span(int32_t Q, int64_t ld, int32_t d, int64_t es) { return ((int64_t)(Q - 1) * ld + d) * es; }
+
+tfe_status device_sms(int *sms)
+{
+    int dev = 0;
+    tfe_status st = tfe_note_cuda(cudaGetDevice(&dev), "cudaGetDevice");
+    return st != TFE_OK ? st : tfe_note_cuda(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev), "cudaDeviceGetAttribute");
+}
+
+// Rows of a block at a time, and the blocks.  Few rows are spread over the SMs.
+int plan_blocks(NormParams &p, int sms, int per_sm)
+{
+    p.groups = std::max(1, std::min({kBlock / p.row_threads, 15, (p.Q + sms - 1) / sms}));      // (named barriers 1..15)
+    return (int)std::min<int64_t>({((int64_t)p.Q + p.groups - 1) / p.groups, (int64_t)sms * per_sm, (int64_t)kMaxBlocks});
+}
+
+template <typename F>
+tfe_status pick(int32_t dtype, bool vec, bool wide, F go)
+{
+    if (dtype == TFE_DTYPE_BF16)
+        return vec ? (wide ? go.template operator()<__nv_bfloat16, true, 1024>() : go.template operator()<__nv_bfloat16, true, kBlock>())
+                   : (wide ? go.template operator()<__nv_bfloat16, false, 1024>() : go.template operator()<__nv_bfloat16, false, kBlock>());
+    return vec ? (wide ? go.template operator()<float, true, 1024>() : go.template operator()<float, true, kBlock>())
+               : (wide ? go.template operator()<float, false, 1024>() : go.template operator()<float, false, kBlock>());
+}
+
+struct GoForward {
+    NormParams p; int grid; cudaStream_t stream;
+    template <typename T, bool kVector, int kThreads> tfe_status operator()() const
+    {
+        return tfe_launch_serial(tfe_inject_norm_forward_kernel<T, kVector, kThreads>, (unsigned)grid, (unsigned)(p.row_threads * p.groups), 1, 0, stream,
+                                 "injection launch", p);
+    }
+};
+struct GoBackward {
+    NormParams p; int grid; cudaStream_t stream;
+    template <typename T, bool kVector, int kThreads> tfe_status operator()() const
+    {
+        const size_t smem = p.groups > 1 ? (size_t)2 * p.d * sizeof(float) : 0;
+        return tfe_launch_serial(tfe_inject_norm_backward_kernel<T, kVector, kThreads>, (unsigned)grid, (unsigned)(p.row_threads * p.groups), 1, smem, stream,
+                                 "injection gradient launch", p);
+    }
+};
+
+// 16-byte vectors where every row of every matrix starts on such a boundary
+bool vectors(int32_t dtype, int32_t d, std::initializer_list<Matrix> all)
+{
+    if (d % kCols != 0) return false;
+    for (const Matrix &x : all)
+        if (x.at && (reinterpret_cast<uintptr_t>(x.at) % 16 != 0 || x.ld * elem_size(dtype) % 16 != 0)) return false;
+    return true;
+}
+
+}  // namespace
+
+extern "C" {
+
+tfe_status tfe_inject_norm_forward(const tfe_inject_norm_params *q, void *out, int64_t ld_out, void *normed, int64_t ld_normed, void *stream_)
+{
+    if (!params_ok(q)) return TFE_ERR_INVALID_ARG;
+    if (q->Q == 0) return TFE_OK;
+    const int64_t es = elem_size(q->dtype);
+    if (!matrix_ok(out, ld_out, q->d, es) || !matrix_ok(normed, ld_normed, q->d, es)) return TFE_ERR_INVALID_ARG;
+    const int64_t ws = elem_size(q->weight_dtype) * q->d;
+    const Span o{out, span(q->Q, ld_out, q->d, es)}, n{normed, span(q->Q, ld_normed, q->d, es)}, h{q->h, span(q->Q, q->ld_h, q->d, es)};
+    const Span gate{q->gate_kind == TFE_GATE_NONE ? nullptr : q->gate, q->gate_kind == TFE_GATE_SCALAR ? 4ll * q->Q : span(q->Q, q->ld_gate, q->d, es)};
+    const Span others[] = {{q->m, span(q->Q, q->ld_m, q->d, es)}, gate, {q->post_weight, ws}, {q->next_weight, ws}};
+    for (const Span &x : others)
+        if (touch(o, x) || touch(n, x)) return TFE_ERR_INVALID_ARG;
+    // out may be h itself: a row is read before it is written
+    if (touch(o, n) || touch(n, h) || (touch(o, h) && !(out == q->h && ld_out == q->ld_h))) return TFE_ERR_INVALID_ARG;
+    int sms = 0;
+    if (tfe_status st = device_sms(&sms)) return st;
+    NormParams p = shared_params(q);
+    p.out = out; p.ld_out = ld_out; p.normed = normed; p.ld_normed = ld_normed;
+    const int grid = plan_blocks(p, sms, 4);
+    const bool vec = vectors(q->dtype, q->d, {{q->h, q->ld_h}, {q->m, q->ld_m}, {q->gate_kind == TFE_GATE_VECTOR ? q->gate : nullptr, q->ld_gate}, {out, ld_out}, {normed, ld_normed}});
+    return pick(q->dtype, vec, p.row_threads > kBlock, GoForward{p, grid, static_cast<cudaStream_t>(stream_)});
+}
+
+int64_t tfe_inject_norm_workspace_bytes(int32_t Q, int32_t d)
+{
+    if (Q < 0 || Q > TFE_ROWS_MAX || d < 1 || d > TFE_INJECT_NORM_MAX_COLS) return -1;
+    return std::min<int64_t>(Q, kMaxBlocks) * 2 * d * (int64_t)sizeof(float);
+}
+
+tfe_status tfe_inject_norm_backward(const tfe_inject_norm_params *q, const tfe_inject_norm_grads *g, void *workspace, int64_t workspace_bytes, void *stream_)
+{
+    if (!params_ok(q) || !g) return TFE_ERR_INVALID_ARG;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    const int64_t es = elem_size(q->dtype), wes = elem_size(q->weight_dtype), ws = wes * q->d;
+    if ((g->grad_post && !aligned(g->grad_post, wes)) || (g->grad_next && !aligned(g->grad_next, wes))) return TFE_ERR_INVALID_ARG;
+    if (q->Q == 0) {                            // sums over no rows
+        if (g->grad_post)
+            if (tfe_status st = tfe_note_cuda(cudaMemsetAsync(g->grad_post, 0, (size_t)ws, stream), "cudaMemsetAsync")) return st;
+        return g->grad_next ? tfe_note_cuda(cudaMemsetAsync(g->grad_next, 0, (size_t)ws, stream), "cudaMemsetAsync") : TFE_OK;
+    }
+    const bool scalar = q->gate_kind == TFE_GATE_SCALAR, vector = q->gate_kind == TFE_GATE_VECTOR;
+    if (!g->grad_out && !g->grad_normed) return TFE_ERR_INVALID_ARG;
+    if ((g->grad_out && !matrix_ok(g->grad_out, g->ld_grad_out, q->d, es)) || (g->grad_normed && !matrix_ok(g->grad_normed, g->ld_grad_normed, q->d, es)))
+        return TFE_ERR_INVALID_ARG;
+    if ((g->grad_h && !matrix_ok(g->grad_h, g->ld_grad_h, q->d, es)) || (g->grad_m && !matrix_ok(g->grad_m, g->ld_grad_m, q->d, es))) return TFE_ERR_INVALID_ARG;
+    if (g->grad_gate && !(scalar ? aligned(g->grad_gate, 4) : vector && matrix_ok(g->grad_gate, g->ld_grad_gate, q->d, es))) return TFE_ERR_INVALID_ARG;
+    const bool sums = g->grad_post || g->grad_next;
+    const int64_t need = tfe_inject_norm_workspace_bytes(q->Q, q->d);
+    if (sums && !aligned(workspace, 16)) return TFE_ERR_INVALID_ARG;
+    if (sums && workspace_bytes < need) return TFE_ERR_CAPACITY;
+    const Span in[] = {{q->h, span(q->Q, q->ld_h, q->d, es)}, {q->m, span(q->Q, q->ld_m, q->d, es)},
+                       {q->gate_kind == TFE_GATE_NONE ? nullptr : q->gate, scalar ? 4ll * q->Q : span(q->Q, q->ld_gate, q->d, es)},
+                       {q->post_weight, ws}, {q->next_weight, ws}, {g->grad_out, span(q->Q, g->ld_grad_out, q->d, es)},
+                       {g->grad_normed, span(q->Q, g->ld_grad_normed, q->d, es)}, {sums ? workspace : nullptr, need}};
+    const Span made[] = {{g->grad_h, span(q->Q, g->ld_grad_h, q->d, es)}, {g->grad_m, span(q->Q, g->ld_grad_m, q->d, es)},
+                         {g->grad_gate, scalar ? 4ll * q->Q : span(q->Q, g->ld_grad_gate, q->d, es)}, {g->grad_post, ws}, {g->grad_next, ws}};
+    for (int i = 0; i < 5; ++i) {
+        for (const Span &x : in)
+            if (touch(made[i], x)) return TFE_ERR_INVALID_ARG;
+        for (int j = 0; j < i; ++j)
+            if (touch(made[i], made[j])) return TFE_ERR_INVALID_ARG;
+    }
+    int sms = 0;
+    if (tfe_status st = device_sms(&sms)) return st;
+    NormParams p = shared_params(q);
+    p.g_out = g->grad_out; p.ld_g_out = g->ld_grad_out; p.g_normed = g->grad_normed; p.ld_g_normed = g->ld_grad_normed;
+    p.g_h = g->grad_h; p.ld_g_h = g->ld_grad_h; p.g_m = g->grad_m; p.ld_g_m = g->ld_grad_m; p.g_gate = g->grad_gate; p.ld_g_gate = g->ld_grad_gate;
+    p.part = sums ? static_cast<float *>(workspace) : nullptr;
+    const int grid = plan_blocks(p, sms, 1);
+    const bool vec = vectors(q->dtype, q->d, {{q->h, q->ld_h}, {q->m, q->ld_m}, {vector ? q->gate : nullptr, q->ld_gate}, {g->grad_out, g->ld_grad_out},
+                                              {g->grad_normed, g->ld_grad_normed}, {g->grad_h, g->ld_grad_h}, {g->grad_m, g->ld_grad_m},
+                                              {vector ? g->grad_gate : nullptr, g->ld_grad_gate}});
+    if (tfe_status st = pick(q->dtype, vec, p.row_threads > kBlock, GoBackward{p, grid, stream})) return st;
+    if (!sums) return TFE_OK;
+    JoinParams j{};
+    j.blocks = grid; j.d = q->d; j.f32 = p.weights_f32; j.part = p.part; j.g_post = g->grad_post; j.g_next = g->grad_next;
+    return tfe_launch_serial(tfe_inject_norm_join_kernel, (unsigned)((2 * q->d + kJoinCols - 1) / kJoinCols), kJoinCols * kJoinParts, 1, 0, stream, "injection join launch", j);
+}
+
+}  // extern "C"

@@ -30,7 +30,7 @@ namespace {
 
 using bf16 = __nv_bfloat16;
 
-constexpr int kCtas = 1;                        // CTAs that share a tile
+constexpr int kCtas = 2;                        // CTAs that share a tile: a cluster
 constexpr int kRowsA = 128;                     // rows of A per CTA (MMA M per CTA)
 constexpr int kM = kRowsA * kCtas;              // rows of a tile
 constexpr int kN = 256;                         // columns of a tile at most (MMA N)
@@ -64,6 +64,8 @@ struct GemmParams {
     const int32_t *n_live;                      // rows taken part in (null: N)
     const int32_t *target;
     const float *lse, *coef;
+    const bf16 *h;                              // kGrads: the rows together, d apart
+    float *rest;                                // what rounding took from G at each row's target
     float2 *part; int64_t ld_part;              // kLse: [2 * units per row][ld_part] maxima and sums
     float *z_target;
     float *sum_h;                               // kGrads: [splits][m_room][column tiles][kN / 4][kM][4]
@@ -143,6 +145,8 @@ tfe_xent_compact_kernel(const CompactParams p)
     const int64_t n_zero = (end - all) * vecs;
     uint4 *dst = reinterpret_cast<uint4 *>(p.h_out + (int64_t)all * p.d);
     for (int64_t i = (int64_t)blockIdx.x * kCompactThreads + tid; i < n_zero; i += (int64_t)gridDim.x * kCompactThreads) dst[i] = make_uint4(0, 0, 0, 0);
+    if (blockIdx.x == 0)
+        for (int64_t i = all + tid; i < end; i += kCompactThreads) p.target_out[i] = -1;
 }
 
 // ------------------------------------------------------------------ the products
@@ -239,6 +243,106 @@ struct Units {
     }
 };
 
+// Instructions of a pair of CTAs: the first issues the MMAs, each holds its rows of A and of the sums, and half of B.
+__device__ __forceinline__ uint32_t cluster_rank()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t in_first(uint32_t smem_addr)        // the same place in the first CTA's shared memory
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem_addr));
+    return r;
+}
+__device__ __forceinline__ void arrive_cluster(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void pair_load_2d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int32_t x, int32_t y, uint64_t hint)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
+        " [%0], [%1, {%3, %4}], [%2], %5;"
+        :
+        : "r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y), "l"(hint)
+        : "memory");
+}
+__device__ __forceinline__ void pair_mma(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        :
+        : "r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// One arrival at this place in both CTAs when every MMA issued so far by this thread has completed.
+__device__ __forceinline__ void pair_commit(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+__device__ __forceinline__ void pair_tmem_alloc(uint32_t dst_smem, uint32_t cols)
+{
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst_smem), "r"(cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void pair_tmem_dealloc(uint32_t taddr, uint32_t cols)
+{
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(cols) : "memory");
+}
+
+// What rounding G to bf16 takes away weighs most at a row's target, where G is largest and its error is one factor for a whole row of
+// grad W.  That difference is kept in fp32 and added to the sums: to grad H where its parts are joined, to grad W by the epilogue
+// that rounds it.  A thread holds one row v of grad W and adds the first kHits rows whose target is v; among more the errors
+// average out.  (33 x 32,003: the gradients are off by 1.53 times their own rounding without it.)
+constexpr int kHits = 4;
+
+// The first rows whose target is v0 + lane, ascending, -1 where there are none.
+__device__ __forceinline__ void find_targets(const GemmParams &p, int32_t n_live, int32_t v0, int lane, int32_t (&hit)[kHits])
+{
+#pragma unroll
+    for (int i = 0; i < kHits; ++i) hit[i] = -1;
+    for (int32_t base = 0; base < n_live; base += 128) {            // (targets beyond the last row are -1)
+        const int4 t = *reinterpret_cast<const int4 *>(p.target + base + 4 * lane);
+        const bool any = (uint32_t)(t.x - v0) < 32u || (uint32_t)(t.y - v0) < 32u || (uint32_t)(t.z - v0) < 32u || (uint32_t)(t.w - v0) < 32u;
+        for (uint32_t from = __ballot_sync(0xFFFFFFFFu, any); from; from &= from - 1) {
+            const int l = __ffs(from) - 1;
+            const int32_t four[4] = {__shfl_sync(0xFFFFFFFFu, t.x, l), __shfl_sync(0xFFFFFFFFu, t.y, l), __shfl_sync(0xFFFFFFFFu, t.z, l), __shfl_sync(0xFFFFFFFFu, t.w, l)};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (four[e] == v0 + lane) {
+                    int32_t at = base + 4 * l + e;
+#pragma unroll
+                    for (int i = 0; i < kHits; ++i)
+                        if (hit[i] < 0) { hit[i] = at; at = -1; }
+                }
+        }
+        if (__all_sync(0xFFFFFFFFu, hit[kHits - 1] >= 0)) break;
+    }
+}
+// 16 columns from `col` of row `at`'s hidden state, times what is left of its G, to y
+__device__ __forceinline__ void add_rest(const GemmParams &p, int32_t at, int32_t col, float2 (&y)[8])
+{
+    if (at < 0) return;
+    const float rest = p.rest[at];
+    const float2 by = make_float2(rest, rest);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (col + 8 * i < p.d) {
+            float f[8];
+            tfe_rows::Elem<bf16>::unpack(*reinterpret_cast<const uint4 *>(p.h + (int64_t)at * p.d + col + 8 * i), f);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y[4 * i + j] = __ffma2_rn(make_float2(f[2 * j], f[2 * j + 1]), by, y[4 * i + j]);
+        }
+}
+
 struct Maps { CUtensorMap a, b, a_w, b_w, out; };           // kLse, kProb: H, W, -, -, G;  kGrads: G by rows, W, G by columns, H, grad W
 
 template <int kOp>
@@ -254,14 +358,17 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) { mbar_init(smem_u32(&s_full[s]), 1); mbar_init(smem_u32(&s_empty[s]), 1); }
-        for (int a = 0; a < kBuffers; ++a) { mbar_init(smem_u32(&s_acc_full[a]), 1); mbar_init(smem_u32(&s_acc_empty[a]), kEpilogueWarps); }
+        for (int a = 0; a < kBuffers; ++a) { mbar_init(smem_u32(&s_acc_full[a]), 1); mbar_init(smem_u32(&s_acc_empty[a]), kCtas * kEpilogueWarps); }
         mbar_init(smem_u32(&s_drain), 1);
         s_abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 1) tmem_alloc(smem_u32(&s_tmem_base), kBuffers * kN);
+    __syncwarp();
+    const uint32_t rank = cluster_rank();
+    const int64_t pair = blockIdx.x / kCtas, pairs = gridDim.x / kCtas;
+    if (warp == 1) pair_tmem_alloc(smem_u32(&s_tmem_base), kBuffers * kN);
     tc_fence_before();
-    __syncthreads();
+    cluster_sync();
     tc_fence_after();
     const uint32_t tmem_base = s_tmem_base;
     tfe_wait_for_stream();
@@ -271,9 +378,10 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
         // ============================ TMA producer ============================
         if (lane == 0) {
             const uint64_t hint = 0x1000000000000000ull;            // no preference
+            const int32_t b_part = p.tn / kCtas;
             uint32_t stage = 0, phase = 0, issued = 0;
             bool ok = !p.give_up;
-            for (int64_t u = blockIdx.x; ok && u < units.n; u += gridDim.x) {
+            for (int64_t u = pair; ok && u < units.n; u += pairs) {
                 const Unit w = units.at(p, u);
                 for (int32_t t = 0; ok && t < w.tiles; ++t)
                     for (int32_t ks = 0; ks < w.steps; ++ks) {
@@ -283,35 +391,39 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                             ok = false;
                             break;
                         }
-                        const uint32_t bar = smem_u32(&s_full[stage]), a = smem_base + stage * kStageBytes, b = a + kBytesA;
-                        const int32_t k = w.k_at + ks * kStepK;
-                        mbar_expect_tx(bar, kBytesA + (uint32_t)p.tn * kStepK * 2);
+                        // both CTAs' copies are counted where the MMAs are issued
+                        const uint32_t bar = in_first(smem_u32(&s_full[stage])), a = smem_base + stage * kStageBytes, b = a + kBytesA;
+                        const int32_t k = w.k_at + ks * kStepK, a_at = w.a_at + (int32_t)rank * kRowsA, b_at = w.b_at + t * p.tn + (int32_t)rank * b_part;
+                        if (rank == 0) mbar_expect_tx(smem_u32(&s_full[stage]), kCtas * (kBytesA + (uint32_t)b_part * kStepK * 2));
                         if constexpr (kOp != kGrads) {
-                            tma_load_2d(a, &maps.a, bar, k, w.a_at, hint);
-                            tma_load_2d(b, &maps.b, bar, k, (kOp == kProb ? p.v0 : 0) + w.b_at + t * p.tn, hint);
+                            pair_load_2d(a, &maps.a, bar, k, a_at, hint);
+                            pair_load_2d(b, &maps.b, bar, k, (kOp == kProb ? p.v0 : 0) + b_at, hint);
                         } else if (w.grad_h) {
-                            tma_load_2d(a, &maps.a, bar, k, w.a_at, hint);
-                            for (int32_t j = 0; j < p.tn / 64; ++j) tma_load_2d(b + j * kStepK * 128, &maps.b, bar, w.b_at + j * 64, p.v0 + k, hint);
+                            pair_load_2d(a, &maps.a, bar, k, a_at, hint);
+                            for (int32_t j = 0; j < b_part; j += 64) pair_load_2d(b + j * kStepK * 2, &maps.b, bar, b_at + j, p.v0 + k, hint);
                         } else {
-                            for (int32_t j = 0; j < kRowsA / 64; ++j) tma_load_2d(a + j * kStepK * 128, &maps.a_w, bar, w.a_at + j * 64, k, hint);
-                            for (int32_t j = 0; j < p.tn / 64; ++j) tma_load_2d(b + j * kStepK * 128, &maps.b_w, bar, w.b_at + j * 64, k, hint);
+                            for (int32_t j = 0; j < kRowsA; j += 64) pair_load_2d(a + j * kStepK * 2, &maps.a_w, bar, a_at + j, k, hint);
+                            for (int32_t j = 0; j < b_part; j += 64) pair_load_2d(b + j * kStepK * 2, &maps.b_w, bar, b_at + j, k, hint);
                         }
                         ++issued;
                         if (++stage == kStages) { stage = 0; phase ^= 1u; }
                     }
             }
-            if (!ok)                            // copies in flight land before the shared memory goes
+            // copies in flight land before the shared memory goes; the second CTA's are counted in the first, so it only waits a while
+            if (!ok && rank == 0)
                 for (uint32_t s = 0; s < kStages; ++s) {
                     const uint32_t fills = (issued + kStages - 1u - s) / kStages;
                     for (uint32_t t = 0; fills && t < TC_WAIT_LIMIT && !mbar_try_wait(smem_u32(&s_full[s]), (fills - 1u) & 1u); ++t) { }
                 }
+            else if (!ok && issued)
+                __nanosleep(1000000);
         }
     } else if (warp == 1) {
         // ============================ MMA issuer ==============================
-        if (lane == 0) {
+        if (lane == 0 && rank == 0) {
             uint32_t stage = 0, phase = 0, buf = 0, buf_phase = 0;
             bool ok = !p.give_up;
-            for (int64_t u = blockIdx.x; ok && u < units.n; u += gridDim.x) {
+            for (int64_t u = pair; ok && u < units.n; u += pairs) {
                 const Unit w = units.at(p, u);
                 const bool a_mn = kOp == kGrads && !w.grad_h, b_mn = kOp == kGrads;
                 const uint32_t idesc = umma_idesc(kM, (uint32_t)p.tn, a_mn, b_mn);
@@ -327,8 +439,8 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                         const uint64_t a_desc = a_mn ? umma_desc_mn_sw128(a) : umma_desc_sw128(a), b_desc = b_mn ? umma_desc_mn_sw128(b) : umma_desc_sw128(b);
 #pragma unroll
                         for (int k = 0; k < kStepK / 16; ++k)
-                            umma_bf16(tmem_base + buf * kN, a_desc + k * a_step, b_desc + k * b_step, idesc, ks > 0 || k > 0 ? 1u : 0u);
-                        umma_commit(smem_u32(&s_empty[stage]));
+                            pair_mma(tmem_base + buf * kN, a_desc + k * a_step, b_desc + k * b_step, idesc, ks > 0 || k > 0 ? 1u : 0u);
+                        pair_commit(smem_u32(&s_empty[stage]));
                         if (++stage == kStages) { stage = 0; phase ^= 1u; }
                     }
                     if (!ok) {
@@ -336,12 +448,12 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                         s_abort = 1;
                         break;
                     }
-                    umma_commit(smem_u32(&s_acc_full[buf]));
+                    pair_commit(smem_u32(&s_acc_full[buf]));
                     if (++buf == kBuffers) { buf = 0; buf_phase ^= 1u; }
                 }
             }
             if (!ok) {                          // MMAs in flight end before their tensor memory is freed
-                umma_commit(smem_u32(&s_drain));
+                pair_commit(smem_u32(&s_drain));
                 for (uint32_t t = 0; t < TC_WAIT_LIMIT && !mbar_try_wait(smem_u32(&s_drain), 0); ++t) { }
             }
         }
@@ -350,27 +462,46 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
         const int e = warp - 4;
         const uint32_t quarter = (uint32_t)warp & 3u;               // tensor-memory lanes 32 * quarter .. + 31
         const int32_t half = e >> 2, cols = p.tn / 2, c0 = half * cols;     // this warp's columns: a multiple of 16
-        const int32_t row_in_tile = (int32_t)(quarter * 32u) + lane;
+        const int32_t first_row = (int32_t)(rank * kRowsA + quarter * 32u), row_in_tile = first_row + lane;
         const uint32_t room = smem_base + kStages * kStageBytes + (uint32_t)e * kRoom;
         uint32_t buf = 0, buf_phase = 0;
         bool ok = !p.give_up;
-        int64_t u = blockIdx.x;
-        for (; ok && u < units.n; u += gridDim.x) {
+        // 64 finished columns of this warp's rows leave by an asynchronous copy
+        auto send = [&](const uint32_t (&out)[32], int32_t x, int32_t y, bool there) {
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");     // the last ones have left
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(room + (uint32_t)(lane * 128 + ((i ^ (lane & 7)) * 16))), "r"(out[4 * i]),
+                             "r"(out[4 * i + 1]), "r"(out[4 * i + 2]), "r"(out[4 * i + 3])
+                             : "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) {
+                if (there) tma_store_2d(&maps.out, room, x, y);
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+            }
+        };
+        int64_t u = pair;
+        for (; ok && u < units.n; u += pairs) {
             const Unit w = units.at(p, u);
             const int32_t row = w.a_at + row_in_tile;
-            const bool live = kOp == kGrads || row < units.n_live;
-            int32_t target = -1;
-            float lse = 0.f, coef = 0.f, top = -3.4e38f, sum = 0.f;
+            const bool live = row < units.n_live;                   // (of no use to grad W, whose rows are the vocabulary's)
+            int32_t target = -1, hit[kHits];
+            float lse = 0.f, coef = 0.f, top = -3.4e38f;
+            float2 sum = make_float2(0.f, 0.f);
             if (kOp != kGrads && live) target = p.target[row];
             if (kOp == kProb && live) { lse = p.lse[row]; coef = p.coef[row]; }
+            if (kOp == kGrads && !w.grad_h) find_targets(p, units.n_live, p.v0 + w.a_at + first_row, lane, hit);
             for (int32_t t = 0; t < w.tiles; ++t) {
-                if (w.steps == 0) {             // (a part of a short last piece that has nothing to add)
-                    if constexpr (kOp == kGrads)
-                        if (p.first) {
-                            float4 *at = reinterpret_cast<float4 *>(p.sum_h) + ((int64_t)w.index * (kN / 4) + c0 / 4) * kM + row_in_tile;
+                float4 *at = nullptr;                               // grad H's sums of this row, four columns each
+                if constexpr (kOp == kGrads) {
+                    at = reinterpret_cast<float4 *>(p.sum_h) + ((int64_t)w.index * (kN / 4) + c0 / 4) * kM + row_in_tile;
+                    if (w.steps == 0) {         // (a part of a short last piece that has nothing to add)
+                        if (p.first)
                             for (int32_t c = 0; c < cols; c += 4) at[(int64_t)(c / 4) * kM] = make_float4(0.f, 0.f, 0.f, 0.f);
-                        }
-                    continue;
+                        continue;
+                    }
                 }
                 ok = mbar_wait(smem_u32(&s_acc_full[buf]), buf_phase, &s_abort);
                 if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
@@ -379,124 +510,142 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                 auto release = [&] {
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(smem_u32(&s_acc_empty[buf]));
+                    if (lane == 0) arrive_cluster(in_first(smem_u32(&s_acc_empty[buf])));
                 };
+                // 16 columns at a time, the next ones on their way meanwhile
+                uint32_t r[2][16];
+                tmem_ld16(taddr, r[0]);
                 if constexpr (kOp == kLse) {
                     const int32_t v0 = w.b_at + t * p.tn + c0, left = p.V - v0, mine = target - v0;
-                    for (int32_t c = 0; c < cols; c += 16) {
-                        uint32_t r[16];
+                    auto take = [&](const uint32_t (&x)[16], int32_t c) {
                         float z[16];
-                        tmem_ld16(taddr + (uint32_t)c, r);
-                        tmem_ld_wait();
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) z[j] = c + j < left ? __uint_as_float(r[j]) : -INFINITY;
+                        for (int j = 0; j < 16; ++j) z[j] = __uint_as_float(x[j]);
+                        if (c + 16 > left)
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) z[j] = c + j < left ? z[j] : -INFINITY;
                         if ((uint32_t)(mine - c) < 16u) {
                             float zt = 0.f;
 #pragma unroll
                             for (int j = 0; j < 16; ++j) zt = mine - c == j ? z[j] : zt;
                             p.z_target[row] = zt;
                         }
-                        float best = top;
+                        float best[4];
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) best = fmaxf(best, z[j]);
-                        sum *= tfe_rows::exp2_approx((top - best) * kLog2e);
-                        top = best;
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) sum += tfe_rows::exp2_approx((z[j] - top) * kLog2e);
-                    }
-                    release();
-                } else if constexpr (kOp == kProb) {
-                    const int32_t v0 = p.v0 + w.b_at + c0, left = p.V - v0, mine = target - v0;
-                    for (int32_t c = 0; c < cols; c += 64) {
-                        uint32_t out[32];
-#pragma unroll
-                        for (int q = 0; q < 64; q += 16) {
-                            uint32_t r[16];
-                            tmem_ld16(taddr + (uint32_t)(c + q), r);
-                            tmem_ld_wait();
-                            float g[16];
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) {
-                                const float x = __uint_as_float(r[j]) - lse;
-                                float y = tfe_rows::exp2_approx(x * kLog2e);
-                                if (mine == c + q + j) y = expm1f(x);
-                                g[j] = live && c + q + j < left ? coef * y : 0.f;
-                            }
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) {
-                                const __nv_bfloat162 b2 = __floats2bfloat162_rn(g[2 * j], g[2 * j + 1]);
-                                out[q / 2 + j] = *reinterpret_cast<const uint32_t *>(&b2);
-                            }
+                        for (int j = 0; j < 4; ++j) best[j] = fmaxf(fmaxf(z[j], z[j + 4]), fmaxf(z[j + 8], z[j + 12]));
+                        best[0] = fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3]));
+                        if (best[0] > top) {
+                            const float by = tfe_rows::exp2_approx((top - best[0]) * kLog2e);
+                            sum.x *= by; sum.y *= by;
+                            top = best[0];
                         }
-                        if (c + 64 >= cols) release();
-                        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                        __syncwarp();
+                        const float2 minus = make_float2(-top, -top), by = make_float2(kLog2e, kLog2e);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(room + (uint32_t)(lane * 128 + ((i ^ (lane & 7)) * 16))), "r"(out[4 * i]),
-                                         "r"(out[4 * i + 1]), "r"(out[4 * i + 2]), "r"(out[4 * i + 3])
-                                         : "memory");
-                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                        __syncwarp();
-                        if (lane == 0) {
-                            tma_store_2d(&maps.out, room, w.b_at + c0 + c, w.a_at + (int32_t)(quarter * 32u));
-                            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                        for (int j = 0; j < 16; j += 2) {
+                            const float2 y = __fmul2_rn(__fadd2_rn(make_float2(z[j], z[j + 1]), minus), by);
+                            sum = __fadd2_rn(sum, make_float2(tfe_rows::exp2_approx(y.x), tfe_rows::exp2_approx(y.y)));
                         }
-                    }
-                } else if (w.grad_h) {
-                    float4 *at = reinterpret_cast<float4 *>(p.sum_h) + ((int64_t)w.index * (kN / 4) + c0 / 4) * kM + row_in_tile;
-                    for (int32_t c = 0; c < cols; c += 16) {
-                        uint32_t r[16];
-                        float4 old[4];
-                        if (!p.first)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) old[i] = at[(int64_t)(c / 4 + i) * kM];
-                        tmem_ld16(taddr + (uint32_t)c, r);
+                    };
+                    for (int32_t c = 0; c < cols; c += 32) {
                         tmem_ld_wait();
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            float4 x = make_float4(__uint_as_float(r[4 * i]), __uint_as_float(r[4 * i + 1]), __uint_as_float(r[4 * i + 2]), __uint_as_float(r[4 * i + 3]));
-                            if (!p.first) { x.x += old[i].x; x.y += old[i].y; x.z += old[i].z; x.w += old[i].w; }
-                            at[(int64_t)(c / 4 + i) * kM] = x;
-                        }
+                        if (c + 16 < cols) tmem_ld16(taddr + (uint32_t)(c + 16), r[1]);
+                        take(r[0], c);
+                        tmem_ld_wait();
+                        if (c + 32 < cols) tmem_ld16(taddr + (uint32_t)(c + 32), r[0]);
+                        if (c + 16 < cols) take(r[1], c + 16);
                     }
                     release();
-                } else {
-                    for (int32_t c = 0; c < cols; c += 64) {
-                        uint32_t out[32];
+                } else if (kOp == kProb || !w.grad_h) {
+                    const int32_t v0 = p.v0 + w.b_at + c0, left = p.V - v0, mine = target - v0;
+                    const float2 minus = make_float2(-lse, -lse), by = make_float2(kLog2e, kLog2e), times = make_float2(coef, coef);
+                    // 16 columns in bf16: of G, or of grad W
+                    auto take = [&](const uint32_t (&x)[16], int32_t c, uint32_t (&out)[8]) {
+                        float2 y[8];
 #pragma unroll
-                        for (int q = 0; q < 64; q += 16) {
-                            uint32_t r[16];
-                            tmem_ld16(taddr + (uint32_t)(c + q), r);
-                            tmem_ld_wait();
+                        for (int j = 0; j < 8; ++j) y[j] = make_float2(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1]));
+                        if constexpr (kOp == kProb) {
 #pragma unroll
                             for (int j = 0; j < 8; ++j) {
-                                const __nv_bfloat162 b2 = __floats2bfloat162_rn(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
-                                out[q / 2 + j] = *reinterpret_cast<const uint32_t *>(&b2);
+                                y[j] = __fmul2_rn(__fadd2_rn(y[j], minus), by);
+                                y[j] = __fmul2_rn(make_float2(tfe_rows::exp2_approx(y[j].x), tfe_rows::exp2_approx(y[j].y)), times);
+                            }
+                            if ((uint32_t)(mine - c) < 16u) {
+                                float z = 0.f;
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) z = mine - c == j ? __uint_as_float(x[j]) : z;
+                                const float g = coef * expm1f(z - lse), kept = __bfloat162float(__float2bfloat16_rn(g));
+                                p.rest[row] = g - kept;
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) {
+                                    y[j].x = mine - c == 2 * j ? kept : y[j].x;
+                                    y[j].y = mine - c == 2 * j + 1 ? kept : y[j].y;
+                                }
+                            }
+                            if (c + 16 > left)
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) {
+                                    y[j].x = c + 2 * j < left ? y[j].x : 0.f;
+                                    y[j].y = c + 2 * j + 1 < left ? y[j].y : 0.f;
+                                }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < kHits; ++i) {
+                                if (!__any_sync(0xFFFFFFFFu, hit[i] >= 0)) break;
+                                add_rest(p, hit[i], w.b_at + c0 + c, y);
                             }
                         }
-                        if (c + 64 >= cols) release();
-                        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                        __syncwarp();
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(room + (uint32_t)(lane * 128 + ((i ^ (lane & 7)) * 16))), "r"(out[4 * i]),
-                                         "r"(out[4 * i + 1]), "r"(out[4 * i + 2]), "r"(out[4 * i + 3])
-                                         : "memory");
-                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                        __syncwarp();
-                        if (lane == 0) {        // (what lies beyond the matrix is not written)
-                            const int32_t x = w.b_at + c0 + c, y = p.v0 + w.a_at + (int32_t)(quarter * 32u);
-                            if (x < p.d && y < p.V) tma_store_2d(&maps.out, room, x, y);
-                            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                        for (int j = 0; j < 8; ++j) {
+                            const __nv_bfloat162 b2 = __floats2bfloat162_rn(y[j].x, y[j].y);
+                            out[j] = *reinterpret_cast<const uint32_t *>(&b2);
+                        }
+                    };
+                    for (int32_t c = 0; c < cols; c += 64) {        // (cols: 64 or 128)
+                        uint32_t out[4][8];
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            tmem_ld_wait();
+                            if (q < 3 || c + 64 < cols) tmem_ld16(taddr + (uint32_t)(c + 16 * (q + 1)), r[(q + 1) & 1]);
+                            take(r[q & 1], c + 16 * q, out[q]);
+                        }
+                        if (c + 64 >= cols) release();
+                        if constexpr (kOp == kProb) {
+                            send(reinterpret_cast<const uint32_t (&)[32]>(out), w.b_at + c0 + c, w.a_at + first_row, true);
+                        } else {                // (what lies beyond the matrix is not written)
+                            const int32_t x0 = w.b_at + c0 + c, y0 = p.v0 + w.a_at + first_row;
+                            send(reinterpret_cast<const uint32_t (&)[32]>(out), x0, y0, x0 < p.d && y0 < p.V);
                         }
                     }
+                } else {
+                    float4 old[2][4];
+                    auto fetch = [&](int32_t c, float4 (&x)[4]) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) x[i] = p.first ? make_float4(0.f, 0.f, 0.f, 0.f) : at[(int64_t)(c / 4 + i) * kM];
+                    };
+                    auto take = [&](const uint32_t (&x)[16], int32_t c, const float4 (&was)[4]) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            at[(int64_t)(c / 4 + i) * kM] = make_float4(__uint_as_float(x[4 * i]) + was[i].x, __uint_as_float(x[4 * i + 1]) + was[i].y,
+                                                                        __uint_as_float(x[4 * i + 2]) + was[i].z, __uint_as_float(x[4 * i + 3]) + was[i].w);
+                    };
+                    fetch(0, old[0]);
+                    for (int32_t c = 0; c < cols; c += 32) {        // (cols: 64 or 128)
+                        fetch(c + 16, old[1]);
+                        tmem_ld_wait();
+                        tmem_ld16(taddr + (uint32_t)(c + 16), r[1]);
+                        take(r[0], c, old[0]);
+                        if (c + 32 < cols) fetch(c + 32, old[0]);
+                        tmem_ld_wait();
+                        if (c + 32 < cols) tmem_ld16(taddr + (uint32_t)(c + 32), r[0]);
+                        take(r[1], c + 16, old[1]);
+                    }
+                    release();
                 }
                 if (++buf == kBuffers) { buf = 0; buf_phase ^= 1u; }
             }
             if (!ok) break;
             if constexpr (kOp == kLse)
-                if (live) p.part[(int64_t)(2 * w.index + half) * p.ld_part + row] = make_float2(top, sum);
+                if (live) p.part[(int64_t)(2 * w.index + half) * p.ld_part + row] = make_float2(top, sum.x + sum.y);
         }
         asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         if (!ok) {                              // a wait ran out: no results that look like some
@@ -506,7 +655,7 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
             }
             s_abort = 1;
             if constexpr (kOp == kLse)
-                for (; u < units.n; u += gridDim.x) {
+                for (; u < units.n; u += pairs) {
                     const Unit w = units.at(p, u);
                     const int32_t row = w.a_at + row_in_tile;
                     if (row < units.n_live) p.part[(int64_t)(2 * w.index + half) * p.ld_part + row] = make_float2(0.f, __int_as_float(0x7FFFFFFF));
@@ -515,97 +664,151 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
     }
 
     tc_fence_before();
-    __syncthreads();
+    __syncwarp();
+    cluster_sync();                             // neither leaves while the other may still reach its shared or tensor memory
     if (warp == 1) {
-        __syncwarp();
         tc_fence_after();
-        tmem_dealloc(tmem_base, kBuffers * kN);
+        pair_tmem_dealloc(tmem_base, kBuffers * kN);
     }
 }
 
 // ------------------------------------------------------------------ joining
 
 struct LossParams {
-    int32_t N, V, chunks;
+    int32_t N, V, d, chunks, rows;              // rows: of a block, a power of two
     const float2 *part; int64_t ld_part;
     const float *z_target;
     const int32_t *target, *pos;                // pos null: rows are where they were
+    const bf16 *h, *w; int64_t ld_h, ld_w;
     float *loss, *lse;
 };
-constexpr int kLossLanes = 16;                  // threads that share a row's partial results
+constexpr int kLossThreads = 512, kLossRows = 32;
 
-__global__ void __launch_bounds__(32 * kLossLanes)
+// Joins maxima and sums, relative to the greater of the maxima.
+__device__ __forceinline__ void fold(float &top, double &sum, float top2, double sum2)
+{
+    if (top2 > top) { const float t = top; top = top2; top2 = t; const double x = sum; sum = sum2; sum2 = x; }
+    if (!(sum2 == 0.0)) sum += sum2 * exp((double)top2 - (double)top);
+}
+
+// A row's partial results joined by kLossThreads / rows threads.  The tensor cores' sum of a target's logit is off by some 1e-7 of its
+// terms, which is all of a loss near zero; so it is summed once more, and takes its place in the sum of exponentials.
+__global__ void __launch_bounds__(kLossThreads)
 tfe_xent_loss_kernel(const LossParams p)
 {
-    __shared__ float s_top[kLossLanes][32];
-    __shared__ double s_sum[kLossLanes][32];
+    __shared__ float s_top[kLossThreads / 32][kLossRows], s_z[kLossRows];
+    __shared__ double s_sum[kLossThreads / 32][kLossRows];
     tfe_wait_for_stream();
-    const int lane = threadIdx.x & 31, part = threadIdx.x >> 5;
-    const int64_t r = (int64_t)blockIdx.x * 32 + lane;
-    const int32_t t = r < p.N ? p.target[r] : -1;
-    int64_t at = t >= 0 && t < p.V ? r : -1;
-    if (p.pos && r < p.N) at = p.pos[r];
-    float top = -INFINITY;
-    double sum = 0.0;
-    if (at >= 0) {
-        for (int32_t c = part; c < p.chunks; c += kLossLanes) top = fmaxf(top, p.part[(int64_t)c * p.ld_part + at].x);
-        for (int32_t c = part; c < p.chunks; c += kLossLanes) {
-            const float2 x = p.part[(int64_t)c * p.ld_part + at];
-            sum += (double)(x.y * tfe_rows::exp2_approx((x.x - top) * kLog2e));
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t r0 = (int64_t)blockIdx.x * p.rows;
+    auto place = [&](int64_t r) -> int64_t {    // of a row among those that took part, -1 if it did not
+        const int32_t t = r < p.N ? p.target[r] : -1;
+        return t < 0 || t >= p.V ? -1 : p.pos ? p.pos[r] : r;
+    };
+    {
+        const int i = threadIdx.x & (p.rows - 1), step = kLossThreads / p.rows;
+        const int64_t at = place(r0 + i);
+        float top = -INFINITY, sum = 0.f;
+        if (at >= 0) {
+#pragma unroll 4
+            for (int32_t c = threadIdx.x / p.rows; c < p.chunks; c += step) {
+                const float2 x = p.part[(int64_t)c * p.ld_part + at];
+                const float best = fmaxf(top, x.x);
+                sum = sum * tfe_rows::exp2_approx((top - best) * kLog2e) + x.y * tfe_rows::exp2_approx((x.x - best) * kLog2e);
+                top = best;
+            }
         }
+        double all = (double)sum;
+        for (int o = 16; o >= p.rows; o >>= 1) fold(top, all, __shfl_xor_sync(0xFFFFFFFFu, top, o), __shfl_xor_sync(0xFFFFFFFFu, all, o));
+        if (lane < p.rows) { s_top[warp][i] = top; s_sum[warp][i] = all; }
     }
-    s_top[part][lane] = top;
-    s_sum[part][lane] = sum;
+    for (int i = warp; i < p.rows; i += kLossThreads / 32) {
+        const int64_t r = r0 + i;
+        if (place(r) < 0) continue;
+        const uint4 *h = reinterpret_cast<const uint4 *>(p.h + r * p.ld_h), *w = reinterpret_cast<const uint4 *>(p.w + (int64_t)p.target[r] * p.ld_w);
+        double z = 0.0;
+        for (int32_t v = lane; v < p.d / 8; v += 32) {
+            float a[8], b[8], x = 0.f;
+            tfe_rows::Elem<bf16>::unpack(h[v], a);
+            tfe_rows::Elem<bf16>::unpack(w[v], b);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x = fmaf(a[j], b[j], x);
+            z += (double)x;
+        }
+        for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xFFFFFFFFu, z, o);
+        if (lane == 0) s_z[i] = (float)z;
+    }
     __syncthreads();
-    if (part != 0 || r >= p.N) return;
+    if (threadIdx.x >= p.rows || r0 + threadIdx.x >= p.N) return;
+    const int64_t r = r0 + threadIdx.x, at = place(r);
     if (at < 0) { p.loss[r] = p.lse[r] = 0.f; return; }
-    for (int i = 1; i < kLossLanes; ++i) top = fmaxf(top, s_top[i][lane]);
-    sum = 0.0;
-    for (int i = 0; i < kLossLanes; ++i)
-        if (s_sum[i][lane] != 0.0) sum += s_sum[i][lane] * exp((double)s_top[i][lane] - (double)top);
-    const double lse = (double)top + log(sum);
+    float top = s_top[0][threadIdx.x];
+    double sum = s_sum[0][threadIdx.x];
+    for (int i = 1; i < kLossThreads / 32; ++i) fold(top, sum, s_top[i][threadIdx.x], s_sum[i][threadIdx.x]);
+    const double z = (double)s_z[threadIdx.x], was = (double)p.z_target[at];
+    double lse = (double)top + log(sum);
+    lse += log1p(exp(was - lse) * expm1(z - was));
     p.lse[r] = (float)lse;
-    p.loss[r] = (float)(lse - (double)p.z_target[at]);
+    p.loss[r] = (float)(lse - z);
 }
 
 struct RowsParams {
-    int32_t N, V, d, splits, m_room, cols, tn;
-    const float *sum_h;
-    const int32_t *pos;
+    int32_t N, V, d, splits, m_room, cols, tn, groups;          // groups: of 32 columns
+    const float *sum_h, *rest;
+    const int32_t *pos, *target;
+    const bf16 *w; int64_t ld_weight;
     const uint32_t *failed;
     bf16 *grad_h; int64_t ld_h;
     bf16 *grad_w; int64_t ld_w;
 };
 constexpr int kRowsThreads = 256;
 
-// grad H's sums over the parts, rounded, to their rows; NaN everywhere if a product before it failed
+// grad H's sums over the parts, rounded, to their rows, a block for 32 rows and 32 columns; NaN everywhere if a product before it failed
 __global__ void __launch_bounds__(kRowsThreads)
 tfe_xent_rows_kernel(const RowsParams p)
 {
+    __shared__ float4 s_sum[32][kRowsThreads / 32 + 1];
     tfe_wait_for_stream();
     const bool failed = *p.failed != 0;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const bf16 nan = __float2bfloat16_rn(__int_as_float(0x7FFFFFFF));
-    if (p.grad_h)
-        for (int64_t base = (int64_t)blockIdx.x * 32; base < p.N; base += (int64_t)gridDim.x * 32) {
-            const int64_t r = base + lane;
-            const int32_t at = r < p.N ? p.pos[r] : -1;
-            if (r < p.N)
-                for (int32_t c = warp * 4; c < p.d; c += kRowsThreads / 32 * 4) {
-                    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (at >= 0)
-                        for (int32_t s = 0; s < p.splits; ++s) {
-                            const int64_t tile = ((int64_t)s * p.m_room + at / kM) * p.cols + c / p.tn;
-                            const float4 x = reinterpret_cast<const float4 *>(p.sum_h)[(tile * (kN / 4) + c % p.tn / 4) * kM + at % kM];
-                            sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
-                        }
-                    bf16 *to = p.grad_h + r * p.ld_h + c;
-                    to[0] = failed ? nan : __float2bfloat16_rn(sum.x);
-                    to[1] = failed ? nan : __float2bfloat16_rn(sum.y);
-                    to[2] = failed ? nan : __float2bfloat16_rn(sum.z);
-                    to[3] = failed ? nan : __float2bfloat16_rn(sum.w);
+    if (p.grad_h) {
+        const int64_t r0 = blockIdx.x / p.groups * 32ll;
+        const int32_t c0 = (int32_t)(blockIdx.x % p.groups) * 32;
+        {
+            const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+            const int32_t at = r0 + lane < p.N ? p.pos[r0 + lane] : -1, c = c0 + 4 * warp;
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (at >= 0 && c < p.d) {
+                const float4 *from = reinterpret_cast<const float4 *>(p.sum_h) + (((int64_t)(at / kM) * p.cols + c / p.tn) * (kN / 4) + c % p.tn / 4) * kM + at % kM;
+                const int64_t step = (int64_t)p.m_room * p.cols * (kN / 4) * kM;
+#pragma unroll 4
+                for (int32_t s = 0; s < p.splits; ++s) {
+                    const float4 x = from[s * step];
+                    sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
                 }
+            }
+            s_sum[lane][warp] = sum;
         }
+        __syncthreads();
+        const int i = threadIdx.x >> 3, q = threadIdx.x & 7;
+        const int64_t r = r0 + i;
+        const int32_t c = c0 + 4 * q;
+        if (r < p.N && c < p.d) {
+            float4 sum = s_sum[i][q];
+            const int32_t at = p.pos[r];
+            if (at >= 0) {
+                const float rest = p.rest[at];
+                const uint2 x = *reinterpret_cast<const uint2 *>(p.w + (int64_t)p.target[at] * p.ld_weight + c);
+                sum.x = fmaf(rest, __uint_as_float(x.x << 16), sum.x);
+                sum.y = fmaf(rest, __uint_as_float(x.x & 0xFFFF0000u), sum.y);
+                sum.z = fmaf(rest, __uint_as_float(x.y << 16), sum.z);
+                sum.w = fmaf(rest, __uint_as_float(x.y & 0xFFFF0000u), sum.w);
+            }
+            if (failed) sum.x = sum.y = sum.z = sum.w = __int_as_float(0x7FFFFFFF);
+            const __nv_bfloat162 lo = __floats2bfloat162_rn(sum.x, sum.y), hi = __floats2bfloat162_rn(sum.z, sum.w);
+            *reinterpret_cast<uint2 *>(p.grad_h + r * p.ld_h + c) = make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
+        }
+    }
     if (failed && p.grad_w)
         for (int64_t v = blockIdx.x; v < p.V; v += gridDim.x)
             for (int32_t c = threadIdx.x; c < p.d; c += kRowsThreads) p.grad_w[v * p.ld_w + c] = nan;
@@ -685,7 +888,7 @@ struct ForwardRoom {
     }
 };
 struct BackwardRoom {
-    bf16 *g, *h; float *sum_h, *lse, *coef; int32_t *pos, *target, *n_live; uint32_t *failed;
+    bf16 *g, *h; float *sum_h, *lse, *coef, *rest; int32_t *pos, *target, *n_live; uint32_t *failed;
     int64_t bytes;
     BackwardRoom(const Plan &q, int32_t N, int32_t d, void *ws)
     {
@@ -693,7 +896,7 @@ struct BackwardRoom {
         g = r.take<bf16>(q.n_pad * q.piece);
         h = r.take<bf16>(q.n_pad * d);
         sum_h = r.take<float>((int64_t)q.splits * q.m_room * q.cols * kM * kN);
-        lse = r.take<float>(q.n_pad); coef = r.take<float>(q.n_pad);
+        lse = r.take<float>(q.n_pad); coef = r.take<float>(q.n_pad); rest = r.take<float>(q.n_pad);
         pos = r.take<int32_t>(N); target = r.take<int32_t>(q.n_pad); n_live = r.take<int32_t>(1); failed = r.take<uint32_t>(1);
         bytes = r.used;
     }
@@ -790,8 +993,11 @@ tfe_status tfe_xent_forward(const void *hidden, int64_t ld_hidden, int32_t N, co
     if (tfe_status st = launch_gemm<kLse>((int64_t)q.m_room * (q.chunks / 2), sms, stream, maps, p)) return st;
     LossParams l{};
     l.N = N; l.V = V; l.chunks = q.chunks; l.part = room.part; l.ld_part = q.n_pad; l.z_target = room.z_target; l.target = target; l.pos = room.pos;
-    l.loss = loss; l.lse = lse;
-    return tfe_launch_serial(tfe_xent_loss_kernel, (unsigned)(((int64_t)N + 31) / 32), 32 * kLossLanes, 1, 0, stream, "cross entropy loss launch", l);
+    l.loss = loss; l.lse = lse; l.d = d;
+    l.h = static_cast<const bf16 *>(hidden); l.ld_h = ld_hidden; l.w = static_cast<const bf16 *>(weight); l.ld_w = ld_weight;
+    l.rows = 1;                                 // few rows: a block each
+    while (l.rows < kLossRows && N / l.rows >= 2 * sms) l.rows *= 2;
+    return tfe_launch_serial(tfe_xent_loss_kernel, (unsigned)((N + l.rows - 1) / l.rows), kLossThreads, 1, 0, stream, "cross entropy loss launch", l);
 }
 
 tfe_status tfe_xent_backward(const void *hidden, int64_t ld_hidden, int32_t N, const void *weight, int64_t ld_weight, int32_t V, int32_t d,
@@ -834,7 +1040,7 @@ tfe_status tfe_xent_backward(const void *hidden, int64_t ld_hidden, int32_t N, c
     p.N = N; p.V = V; p.d = d; p.m_room = q.m_room; p.splits = q.splits;
     p.want_h = grad_hidden != nullptr; p.want_w = grad_weight != nullptr;
     p.give_up = g_xent_give_up.load(std::memory_order_relaxed);
-    p.n_live = room.n_live; p.target = room.target; p.lse = room.lse; p.coef = room.coef; p.sum_h = room.sum_h; p.failed = room.failed;
+    p.n_live = room.n_live; p.target = room.target; p.lse = room.lse; p.coef = room.coef; p.sum_h = room.sum_h; p.failed = room.failed; p.h = room.h; p.rest = room.rest;
     for (int32_t i = 0; i < q.pieces; ++i) {
         p.v0 = (int32_t)(i * q.piece);
         p.width = (int32_t)std::min<int64_t>(q.piece, V - (int64_t)i * q.piece);
@@ -847,8 +1053,9 @@ tfe_status tfe_xent_backward(const void *hidden, int64_t ld_hidden, int32_t N, c
     }
     RowsParams r{};
     r.N = N; r.V = V; r.d = d; r.splits = q.splits; r.m_room = q.m_room; r.cols = q.cols; r.tn = q.tn_d; r.sum_h = room.sum_h; r.pos = room.pos;
-    r.failed = room.failed; r.grad_h = static_cast<bf16 *>(grad_hidden); r.ld_h = ld_grad_hidden; r.grad_w = static_cast<bf16 *>(grad_weight); r.ld_w = ld_grad_weight;
-    const unsigned grid = (unsigned)std::min<int64_t>(4ll * sms, ((int64_t)N + 31) / 32);
+    r.failed = room.failed; r.rest = room.rest; r.target = room.target; r.w = static_cast<const bf16 *>(weight); r.ld_weight = ld_weight; r.grad_h = static_cast<bf16 *>(grad_hidden); r.ld_h = ld_grad_hidden; r.grad_w = static_cast<bf16 *>(grad_weight); r.ld_w = ld_grad_weight;
+    r.groups = grad_hidden ? (d + 31) / 32 : 1;
+    const unsigned grid = (unsigned)((N + 31) / 32 * r.groups);
     return tfe_launch_serial(tfe_xent_rows_kernel, grid, kRowsThreads, 1, 0, stream, "cross entropy gradient launch", r);
 }
 

@@ -6,6 +6,7 @@ Nothing is computed here -- every call goes straight to libtfe.so.
 from __future__ import annotations
 
 import contextlib
+import operator
 from dataclasses import dataclass
 
 import numpy as np
@@ -610,3 +611,187 @@ def linear_cross_entropy(hidden: torch.Tensor, weight: torch.Tensor, target: tor
     """xent_forward's loss [N] as a node of autograd: gradients go to `hidden` and `weight`.  Reduce it as the training wants, e.g.
     ``linear_cross_entropy(h, w, t).sum() / (t >= 0).sum()``."""
     return _LinearCrossEntropy.apply(hidden, weight, target)
+
+
+# ---- injection between two norms ---------------------------------------------------------------
+
+
+def _norm_operands(h, m, post_weight, next_weight, gate, sigmoid, lam, eps):
+    """(parameters, rows, columns, kind of gate) of a call; checked here, and by the library again for what torch does not show."""
+    n, d, ld_h, kind = _row_matrix(h, "h")
+    mn, md, ld_m, m_kind = _row_matrix(m, "m")
+    dev = h.device
+    if mn != n or md != d or m_kind != kind or m.device != dev:
+        raise ValueError("m: h's shape, type and device are needed")
+    w_kind = _ROW_DTYPES.get(post_weight.dtype)
+    if w_kind is None or next_weight.dtype != post_weight.dtype:
+        raise ValueError("post_weight, next_weight: both bf16 or both fp32")
+    wp = _vector(post_weight, (d,), post_weight.dtype, dev, "post_weight")
+    wn = _vector(next_weight, (d,), post_weight.dtype, dev, "next_weight")
+    at, ld_gate, gate_kind = None, 0, tfe.GATE_NONE
+    if gate is not None:
+        if gate.dim() == 1:
+            at, gate_kind = _vector(gate, (n,), torch.float32, dev, "gate"), tfe.GATE_SCALAR
+        else:
+            gn, gd, ld_gate, g_kind = _row_matrix(gate, "gate")
+            if gn != n or gd != d or g_kind != kind or gate.device != dev:
+                raise ValueError("gate: fp32 [rows], or h's shape, type and device")
+            at, gate_kind = gate.data_ptr(), tfe.GATE_VECTOR
+    return tfe.TfeInjectNormParams(kind, n, d, gate_kind, bool(sigmoid), w_kind, h.data_ptr(), m.data_ptr(), at, ld_h, ld_m, ld_gate,
+                                   wp, wn, lam, eps), n, d, gate_kind
+
+
+def normed_inject_forward(h: torch.Tensor, m: torch.Tensor, post_weight: torch.Tensor, next_weight: torch.Tensor,
+                          gate: torch.Tensor | None = None, *, sigmoid: bool = False, lam: float = 1.0, eps: float = 1e-6,
+                          out: torch.Tensor | None = None, stream=None):
+    """(out, normed): ``out = h + lam * s * norm(m) * post_weight`` with s the gate (fp32 [rows], one of h's shape, or None) or its
+    sigmoid, and ``normed = norm(out) * next_weight``, what the next block starts with (see tfe_inject_norm_forward).
+    `out`: where the first goes instead of a new tensor; `out=h` overwrites the hidden states."""
+    if not _here(h.device, stream):
+        with _elsewhere(h.device, stream):
+            return _normed_inject_forward(h, m, post_weight, next_weight, gate, sigmoid, lam, eps, out, stream)
+    return _normed_inject_forward(h, m, post_weight, next_weight, gate, sigmoid, lam, eps, out, None)
+
+
+def _normed_inject_forward(h, m, post_weight, next_weight, gate, sigmoid, lam, eps, out, stream):
+    params, n, d, _ = _norm_operands(h, m, post_weight, next_weight, gate, sigmoid, lam, eps)
+    given, ld_out = out, d
+    if given is None:
+        out = h.new_empty(n, d)
+    else:
+        on, od, ld_out, kind = _row_matrix(out, "out")
+        if on != n or od != d or kind != params.dtype or out.device != h.device:
+            raise ValueError("out: h's shape, type and device are needed")
+    normed = h.new_empty(n, d)
+    tfe.tfe_inject_norm_forward(params, out.data_ptr(), ld_out, normed.data_ptr(), d, _where(h.device, stream))
+    if given is not None:
+        _written(out)
+    return out, normed
+
+
+def normed_inject_backward(grad_out: torch.Tensor | None, grad_normed: torch.Tensor | None, h: torch.Tensor, m: torch.Tensor,
+                           post_weight: torch.Tensor, next_weight: torch.Tensor, gate: torch.Tensor | None = None, *,
+                           sigmoid: bool = False, lam: float = 1.0, eps: float = 1e-6, want=(True,) * 5, stream=None):
+    """(grad_h, grad_m, grad_post_weight, grad_next_weight, grad_gate) of normed_inject_forward's two results, from the gradients
+    that arrive at them (None: zero; not both).  None for the gate's where there is none, and for what `want` leaves out."""
+    if not _here(h.device, stream):
+        with _elsewhere(h.device, stream):
+            return _normed_inject_backward(grad_out, grad_normed, h, m, post_weight, next_weight, gate, sigmoid, lam, eps, want, stream)
+    return _normed_inject_backward(grad_out, grad_normed, h, m, post_weight, next_weight, gate, sigmoid, lam, eps, want, None)
+
+
+def _normed_inject_backward(grad_out, grad_normed, h, m, post_weight, next_weight, gate, sigmoid, lam, eps, want, stream):
+    params, n, d, gate_kind = _norm_operands(h, m, post_weight, next_weight, gate, sigmoid, lam, eps)
+    if grad_out is None and grad_normed is None:
+        raise ValueError("grad_out, grad_normed: one at least is needed")
+    arrived = []
+    for x, what in ((grad_out, "grad_out"), (grad_normed, "grad_normed")):
+        if x is None:
+            arrived += [None, 0]
+            continue
+        xn, xd, ld, kind = _row_matrix(x, what)
+        if xn != n or xd != d or kind != params.dtype or x.device != h.device:
+            raise ValueError(f"{what}: h's shape, type and device are needed")
+        arrived += [x.data_ptr(), ld]
+    gh = h.new_empty(n, d) if want[0] else None
+    gm = h.new_empty(n, d) if want[1] else None
+    gp = torch.empty_like(post_weight) if want[2] else None
+    gx = torch.empty_like(next_weight) if want[3] else None
+    gg = None if gate is None or not want[4] else gate.new_empty(gate.shape)
+    sums = gp is not None or gx is not None
+    size = tfe.tfe_inject_norm_workspace_bytes(n, d) if sums else 0
+    workspace = torch.empty(size, dtype=torch.uint8, device=h.device) if sums else None
+    at = [None if x is None else x.data_ptr() for x in (gh, gm, gg, gp, gx, workspace)]
+    grads = tfe.TfeInjectNormGrads(arrived[0], arrived[2], arrived[1], arrived[3], at[0], at[1], at[2], d, d, d, at[3], at[4])
+    tfe.tfe_inject_norm_backward(params, grads, at[5], size, _where(h.device, stream))
+    return gh, gm, gp, gx, gg
+
+
+class _NormedInject(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, h, m, post_weight, next_weight, gate, sigmoid, lam, eps):
+        ctx.set_materialize_grads(False)
+        ctx.save_for_backward(h, m, post_weight, next_weight, gate)
+        ctx.settings = dict(sigmoid=sigmoid, lam=lam, eps=eps)
+        return normed_inject_forward(h, m, post_weight, next_weight, gate, **ctx.settings)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_out, grad_normed):
+        if grad_out is None and grad_normed is None:
+            return (None,) * 8
+        rows = [x if x is None or x.stride(-1) == 1 and x.stride(0) >= x.shape[1] else x.contiguous() for x in (grad_out, grad_normed)]
+        grads = normed_inject_backward(*rows, *ctx.saved_tensors, want=ctx.needs_input_grad[:5], **ctx.settings)
+        return *grads, None, None, None
+
+
+def normed_inject(h: torch.Tensor, m: torch.Tensor, post_weight: torch.Tensor, next_weight: torch.Tensor,
+                  gate: torch.Tensor | None = None, *, sigmoid: bool = False, lam: float = 1.0, eps: float = 1e-6):
+    """normed_inject_forward's (out, normed) as a node of autograd: gradients go to the hidden states, the memory vectors, both
+    weights and the gate."""
+    return _NormedInject.apply(h, m, post_weight, next_weight, gate, sigmoid, lam, eps)
+
+
+# ---- the norm of many gradients, and clipping by it --------------------------------------------
+
+
+def _gradients(tensors, what):
+    """(tensors, device, addresses, sizes, the library's type numbers), host arrays.  The lists run to hundreds: no python step per tensor
+    beyond what torch has to be asked."""
+    tensors = [tensors] if torch.is_tensor(tensors) else list(tensors)
+    if len(tensors) > tfe.CLIP_MAX_TENSORS:
+        raise ValueError(f"{what}: at most {tfe.CLIP_MAX_TENSORS} tensors")
+    if not tensors:
+        raise ValueError(f"{what}: one tensor at least is needed")
+    kinds = list(map(_ROW_DTYPES.get, map(_dtype_of, tensors)))
+    if None in kinds or len(set(map(torch.Tensor.get_device, tensors))) != 1 or not tensors[0].is_cuda:
+        raise ValueError(f"{what}: bf16 or fp32 CUDA tensors on one device are needed")
+    if not all(map(torch.Tensor.is_contiguous, tensors)):
+        raise ValueError(f"{what}: contiguous tensors are needed")
+    return (tensors, tensors[0].device, np.fromiter(map(torch.Tensor.data_ptr, tensors), np.uint64, len(tensors)),
+            np.fromiter(map(torch.Tensor.numel, tensors), np.int64, len(tensors)), np.array(kinds, np.int32))
+
+
+_dtype_of = operator.attrgetter("dtype")
+
+
+def grad_norm(tensors, *, stream=None) -> torch.Tensor:
+    """fp32 scalar on the device: the 2-norm of all elements of `tensors` (one, or a list; bf16 and fp32 may be mixed) together."""
+    return _clip(tensors, None, None, stream)
+
+
+def clip_grad_norm(tensors, max_norm: float, *, out=None, stream=None) -> torch.Tensor:
+    """grad_norm of `tensors`, which are scaled by min(1, max_norm / norm) in place (see tfe_clip_grad_norm); a norm that is not
+    finite scales nothing.  `out`: tensors of the same sizes and types that take the result instead.  Nothing synchronises."""
+    if not max_norm >= 0:
+        raise ValueError("max_norm: a number that is not negative is needed")
+    return _clip(tensors, float(max_norm), out, stream)
+
+
+def _clip(tensors, max_norm, out, stream):
+    lists = _gradients(tensors, "tensors")
+    dev = lists[1]
+    if not _here(dev, stream):
+        with _elsewhere(dev, stream):
+            return _clip_here(lists, max_norm, out, stream)
+    return _clip_here(lists, max_norm, out, None)
+
+
+def _clip_here(lists, max_norm, out, stream):
+    tensors, dev, at, numel, kinds = lists
+    n = len(tensors)
+    results = None
+    if out is not None:
+        made, out_dev, results, out_numel, out_kinds = _gradients(out, "out")
+        if out_dev != dev or len(made) != n or not np.array_equal(numel, out_numel) or not np.array_equal(kinds, out_kinds):
+            raise ValueError("out: the tensors' sizes, types and device are needed")
+    norm = torch.empty((), dtype=torch.float32, device=dev)
+    size = tfe.tfe_clip_workspace_bytes(n)
+    workspace = torch.empty(size, dtype=torch.uint8, device=dev)
+    if max_norm is None:
+        tfe.tfe_grad_norm(at, numel, kinds, n, norm.data_ptr(), workspace.data_ptr(), size, _where(dev, stream))
+        return norm
+    tfe.tfe_clip_grad_norm(at, results, numel, kinds, n, max_norm, norm.data_ptr(), workspace.data_ptr(), size, _where(dev, stream))
+    for x in tensors if out is None else made:
+        _written(x)
+    return norm
