@@ -627,16 +627,24 @@ def tfe_clip_workspace_bytes(n: int) -> int:
     return lib().tfe_clip_workspace_bytes(n)
 
 
+def _list(x, code: str):
+    """Address of a host list for the length of a call: the caller holds the object meanwhile."""
+    if x is None:
+        return None
+    assert x.typecode == code
+    return x.buffer_info()[0]
+
+
 def tfe_grad_norm(tensors, numel, dtype, n: int, norm, workspace, workspace_bytes: int, stream=None) -> None:
-    """The lists are host arrays: addresses uint64, numel int64, dtype int32."""
-    st = lib().tfe_grad_norm(_addr(tensors), _addr(numel), _addr(dtype), n, norm, workspace, workspace_bytes, _stream(stream))
+    """The lists are array.array objects: tensors "Q", numel "q", dtype "i"."""
+    st = lib().tfe_grad_norm(_list(tensors, "Q"), _list(numel, "q"), _list(dtype, "i"), n, norm, workspace, workspace_bytes, _stream(stream))
     if st:
         raise TfeError(st, "tfe_grad_norm")
 
 
 def tfe_clip_grad_norm(tensors, results, numel, dtype, n: int, max_norm: float, norm, workspace, workspace_bytes: int, stream=None) -> None:
-    """As tfe_grad_norm; results: addresses uint64, or None for in place."""
-    st = lib().tfe_clip_grad_norm(_addr(tensors), _addr(results), _addr(numel), _addr(dtype), n, max_norm, norm, workspace,
-                                  workspace_bytes, _stream(stream))
+    """As tfe_grad_norm; results: "Q" too, or None for in place."""
+    st = lib().tfe_clip_grad_norm(_list(tensors, "Q"), _list(results, "Q"), _list(numel, "q"), _list(dtype, "i"), n, max_norm, norm,
+                                  workspace, workspace_bytes, _stream(stream))
     if st:
         raise TfeError(st, "tfe_clip_grad_norm")

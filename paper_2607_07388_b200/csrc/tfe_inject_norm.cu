@@ -27,7 +27,7 @@ namespace {
 
 using tfe_rows::Elem;
 
-constexpr int kCols = 8;                        // columns of a thread
+constexpr int kCols = 8, kPairs = kCols / 2;    // columns of a thread, taken in pairs: an instruction for two
 constexpr int kBlock = 512;                     // threads of a block that holds several rows, at most
 constexpr int kMaxBlocks = 592;                 // whatever the device has: bounds the partial sums of the backward pass
 
@@ -75,15 +75,15 @@ struct Eight {
             }
         }
     }
-    __device__ __forceinline__ float get(int e) const
+    __device__ __forceinline__ float2 two(int i) const      // elements 2 i and 2 i + 1
     {
-        if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
-        else return __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
+        if constexpr (sizeof(T) == 4) return make_float2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+        else return make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
     }
 };
 
 template <typename T, bool kVector>
-__device__ __forceinline__ void store(void *base, int64_t ld, int64_t row, int32_t d, int t, int threads, const float (&x)[kCols])
+__device__ __forceinline__ void store(void *base, int64_t ld, int64_t row, int32_t d, int t, int threads, const float2 (&x)[kPairs])
 {
     T *at = static_cast<T *>(base) + row * ld;
     if constexpr (kVector) {
@@ -94,13 +94,13 @@ __device__ __forceinline__ void store(void *base, int64_t ld, int64_t row, int32
         for (int i = 0; i < kCols / E; ++i) {
             float part[E];
 #pragma unroll
-            for (int e = 0; e < E; ++e) part[e] = x[i * E + e];
+            for (int e = 0; e < E; ++e) part[e] = e & 1 ? x[(i * E + e) / 2].y : x[(i * E + e) / 2].x;
             __stcs(to + i, Elem<T>::pack(part));
         }
     } else {
 #pragma unroll
         for (int e = 0; e < kCols; ++e)
-            if (t + e * threads < d) Elem<T>::put(at + t + e * threads, x[e]);
+            if (t + e * threads < d) Elem<T>::put(at + t + e * threads, e & 1 ? x[e / 2].y : x[e / 2].x);
     }
 }
 
@@ -108,12 +108,13 @@ template <bool kVector>
 __device__ __forceinline__ int32_t column(int e, int t, int threads) { return kVector ? kCols * t + e : t + e * threads; }
 
 template <bool kVector>
-__device__ __forceinline__ void load_weight(const void *w, bool f32, int32_t d, int t, int threads, float (&x)[kCols])
+__device__ __forceinline__ void load_weight(const void *w, bool f32, int32_t d, int t, int threads, float2 (&x)[kPairs])
 {
 #pragma unroll
     for (int e = 0; e < kCols; ++e) {
         const int32_t c = column<kVector>(e, t, threads);
-        x[e] = c >= d ? 0.f : f32 ? static_cast<const float *>(w)[c] : __bfloat162float(static_cast<const __nv_bfloat16 *>(w)[c]);
+        const float v = c >= d ? 0.f : f32 ? static_cast<const float *>(w)[c] : __bfloat162float(static_cast<const __nv_bfloat16 *>(w)[c]);
+        (e & 1 ? x[e / 2].y : x[e / 2].x) = v;
     }
 }
 
@@ -141,9 +142,14 @@ struct RowSum {
 };
 
 __device__ __forceinline__ float inverse_root(float square, float inv_d, float eps) { return __frsqrt_rn(fmaf(square, inv_d, eps)); }
-template <typename T> __device__ __forceinline__ float sigmoid(float x) { return __frcp_rn(1.f + (sizeof(T) == 4 ? expf(-x) : __expf(-x))); }
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+__device__ __forceinline__ float2 mul(float2 a, float2 b) { return __fmul2_rn(a, b); }
+__device__ __forceinline__ float2 fma(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
+__device__ __forceinline__ float join(float2 a) { return a.x + a.y; }
+// The reciprocal is the approximate one (1 unit in the last place; 0 where the exponential is beyond 2^126).
+template <typename T> __device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + (sizeof(T) == 4 ? expf(-x) : __expf(-x))); }
 
-// What both directions make of a row: the gate, a and y, u and (with the next sum) b.
+// A row's operands, and what both directions make of them first.
 template <typename T, bool kVector>
 struct Row {
     Eight<T, kVector> h, m, gate;
@@ -157,23 +163,26 @@ struct Row {
         if (p.gate_kind == TFE_GATE_VECTOR) gate.load(p.gate, p.ld_gate, row, p.d, t, p.row_threads, any);
         scalar = any && p.gate_kind == TFE_GATE_SCALAR ? static_cast<const float *>(p.gate)[row] : 1.f;
     }
-    __device__ __forceinline__ void gates(const NormParams &p, float (&s)[kCols]) const
+    __device__ __forceinline__ void gates(const NormParams &p, float2 (&s)[kPairs]) const
     {
         if (p.gate_kind == TFE_GATE_VECTOR) {
 #pragma unroll
-            for (int e = 0; e < kCols; ++e) s[e] = p.sigmoid ? sigmoid<T>(gate.get(e)) : gate.get(e);
+            for (int i = 0; i < kPairs; ++i) {
+                s[i] = gate.two(i);
+                if (p.sigmoid) s[i] = make_float2(sigmoid<T>(s[i].x), sigmoid<T>(s[i].y));
+            }
         } else {
             const float x = p.gate_kind == TFE_GATE_SCALAR && p.sigmoid ? sigmoid<T>(scalar) : scalar;
 #pragma unroll
-            for (int e = 0; e < kCols; ++e) s[e] = x;
+            for (int i = 0; i < kPairs; ++i) s[i] = both(x);
         }
     }
     __device__ __forceinline__ float square_m() const
     {
-        float s = 0.f;
+        float2 s = both(0.f);
 #pragma unroll
-        for (int e = 0; e < kCols; ++e) s = fmaf(m.get(e), m.get(e), s);
-        return s;
+        for (int i = 0; i < kPairs; ++i) s = fma(m.two(i), m.two(i), s);
+        return join(s);
     }
 };
 
@@ -188,7 +197,7 @@ tfe_inject_norm_forward_kernel(const NormParams p)
     tfe_wait_for_stream();
     const int group = threadIdx.x / p.row_threads, t = threadIdx.x - group * p.row_threads;
     RowSum row_sum{&s_slots[group][0][0], p.row_threads / 32, t / 32, group + 1, p.row_threads, 0};
-    float wp[kCols], wn[kCols];
+    float2 wp[kPairs], wn[kPairs];
     load_weight<kVector>(p.w_post, p.weights_f32, p.d, t, p.row_threads, wp);
     load_weight<kVector>(p.w_next, p.weights_f32, p.d, t, p.row_threads, wn);
     const float inv_d = 1.f / (float)p.d;
@@ -204,17 +213,17 @@ tfe_inject_norm_forward_kernel(const NormParams p)
             x.load(p, row, t);
         }
         const float a = inverse_root(row_sum(make_float2(x.square_m(), 0.f)).x, inv_d, p.eps);
-        float u[kCols], square = 0.f;
+        float2 u[kPairs], square = both(0.f);
         x.gates(p, u);
 #pragma unroll
-        for (int e = 0; e < kCols; ++e) {
-            u[e] = fmaf(p.lam * u[e], x.m.get(e) * a * wp[e], x.h.get(e));
-            square = fmaf(u[e], u[e], square);
+        for (int i = 0; i < kPairs; ++i) {
+            u[i] = fma(mul(u[i], both(p.lam * a)), mul(x.m.two(i), wp[i]), x.h.two(i));
+            square = fma(u[i], u[i], square);
         }
-        const float b = inverse_root(row_sum(make_float2(square, 0.f)).x, inv_d, p.eps);
+        const float b = inverse_root(row_sum(make_float2(join(square), 0.f)).x, inv_d, p.eps);
         store<T, kVector>(p.out, p.ld_out, row, p.d, t, p.row_threads, u);
 #pragma unroll
-        for (int e = 0; e < kCols; ++e) u[e] *= b * wn[e];
+        for (int i = 0; i < kPairs; ++i) u[i] = mul(mul(u[i], both(b)), wn[i]);
         store<T, kVector>(p.normed, p.ld_normed, row, p.d, t, p.row_threads, u);
     }
 }
@@ -228,11 +237,11 @@ tfe_inject_norm_backward_kernel(const NormParams p)
     tfe_wait_for_stream();
     const int group = threadIdx.x / p.row_threads, t = threadIdx.x - group * p.row_threads;
     RowSum row_sum{&s_slots[group][0][0], p.row_threads / 32, t / 32, group + 1, p.row_threads, 0};
-    float wp[kCols], wn[kCols], sum_p[kCols], sum_n[kCols];
+    float2 wp[kPairs], wn[kPairs], sum_p[kPairs], sum_n[kPairs];
     load_weight<kVector>(p.w_post, p.weights_f32, p.d, t, p.row_threads, wp);
     load_weight<kVector>(p.w_next, p.weights_f32, p.d, t, p.row_threads, wn);
 #pragma unroll
-    for (int e = 0; e < kCols; ++e) sum_p[e] = sum_n[e] = 0.f;
+    for (int i = 0; i < kPairs; ++i) sum_p[i] = sum_n[i] = both(0.f);
     const float inv_d = 1.f / (float)p.d;
     const int64_t step = (int64_t)gridDim.x * p.groups;
     int64_t row = (int64_t)blockIdx.x * p.groups + group;
@@ -257,43 +266,45 @@ tfe_inject_norm_backward_kernel(const NormParams p)
         }
         const Row<T, kVector> &x = all.x;
         const float a = inverse_root(row_sum(make_float2(x.square_m(), 0.f)).x, inv_d, p.eps);
-        float s[kCols], u[kCols];
+        float2 s[kPairs], u[kPairs], uu = both(0.f), ut = both(0.f);
         x.gates(p, s);
-        float2 two = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int e = 0; e < kCols; ++e) {
-            u[e] = fmaf(p.lam * s[e], x.m.get(e) * a * wp[e], x.h.get(e));
-            two.x = fmaf(u[e], u[e], two.x);
-            two.y = fmaf(u[e], wn[e] * all.gn.get(e), two.y);
+        for (int i = 0; i < kPairs; ++i) {
+            u[i] = fma(mul(s[i], both(p.lam * a)), mul(x.m.two(i), wp[i]), x.h.two(i));
+            uu = fma(u[i], u[i], uu);
+            ut = fma(u[i], mul(wn[i], all.gn.two(i)), ut);
         }
-        two = row_sum(two);
+        float2 two = row_sum(make_float2(join(uu), join(ut)));
         const float b = inverse_root(two.x, inv_d, p.eps), by_u = b * b * b * two.y * inv_d;
-        two = make_float2(0.f, 0.f);
+        float2 mx = both(0.f), uy = both(0.f);
 #pragma unroll
-        for (int e = 0; e < kCols; ++e) {
-            const float n = all.gn.get(e);
-            sum_n[e] = fmaf(n, b * u[e], sum_n[e]);
-            u[e] = fmaf(-by_u, u[e], fmaf(b, wn[e] * n, all.gu.get(e)));       // dh
-            const float dy = p.lam * s[e] * u[e], ma = x.m.get(e) * a;
-            sum_p[e] = fmaf(dy, ma, sum_p[e]);
-            two.x = fmaf(x.m.get(e), wp[e] * dy, two.x);
-            two.y = fmaf(u[e], ma * wp[e], two.y);
+        for (int i = 0; i < kPairs; ++i) {
+            const float2 n = mul(all.gn.two(i), both(b)), am = mul(x.m.two(i), both(a));
+            sum_n[i] = fma(n, u[i], sum_n[i]);
+            u[i] = fma(both(-by_u), u[i], fma(n, wn[i], all.gu.two(i)));       // dh
+            const float2 dy = mul(mul(s[i], both(p.lam)), u[i]);
+            sum_p[i] = fma(dy, am, sum_p[i]);
+            mx = fma(x.m.two(i), mul(wp[i], dy), mx);
+            uy = fma(u[i], mul(am, wp[i]), uy);
         }
         if (p.g_h) store<T, kVector>(p.g_h, p.ld_g_h, row, p.d, t, p.row_threads, u);
-        two = row_sum(two);
+        two = row_sum(make_float2(join(mx), join(uy)));
         const float by_m = a * a * a * two.x * inv_d;
         if (p.g_m) {
-            float dm[kCols];
+            float2 dm[kPairs];
 #pragma unroll
-            for (int e = 0; e < kCols; ++e) dm[e] = fmaf(-by_m, x.m.get(e), a * wp[e] * (p.lam * s[e] * u[e]));
+            for (int i = 0; i < kPairs; ++i) dm[i] = fma(both(-by_m), x.m.two(i), mul(mul(wp[i], both(p.lam * a)), mul(s[i], u[i])));
             store<T, kVector>(p.g_m, p.ld_g_m, row, p.d, t, p.row_threads, dm);
         }
         if (p.g_gate && p.gate_kind == TFE_GATE_VECTOR) {
 #pragma unroll
-            for (int e = 0; e < kCols; ++e) u[e] = p.lam * u[e] * (x.m.get(e) * a * wp[e]) * (p.sigmoid ? s[e] * (1.f - s[e]) : 1.f);
+            for (int i = 0; i < kPairs; ++i) {
+                u[i] = mul(mul(u[i], both(p.lam * a)), mul(x.m.two(i), wp[i]));
+                if (p.sigmoid) u[i] = mul(u[i], mul(s[i], make_float2(1.f - s[i].x, 1.f - s[i].y)));
+            }
             store<T, kVector>(p.g_gate, p.ld_g_gate, row, p.d, t, p.row_threads, u);
         } else if (p.g_gate && t == 0) {
-            static_cast<float *>(p.g_gate)[row] = p.lam * two.y * (p.sigmoid ? s[0] * (1.f - s[0]) : 1.f);
+            static_cast<float *>(p.g_gate)[row] = p.lam * two.y * (p.sigmoid ? s[0].x * (1.f - s[0].x) : 1.f);
         }
     }
     if (!p.part) return;
@@ -303,9 +314,10 @@ tfe_inject_norm_backward_kernel(const NormParams p)
 #pragma unroll
             for (int e = 0; e < kCols; ++e) {
                 const int32_t c = column<kVector>(e, t, p.row_threads);
+                const float sp = e & 1 ? sum_p[e / 2].y : sum_p[e / 2].x, sn = e & 1 ? sum_n[e / 2].y : sum_n[e / 2].x;
                 if (c < p.d) {
-                    to[c] = g == 0 ? sum_p[e] : to[c] + sum_p[e];
-                    to[p.d + c] = g == 0 ? sum_n[e] : to[p.d + c] + sum_n[e];
+                    to[c] = g == 0 ? sp : to[c] + sp;
+                    to[p.d + c] = g == 0 ? sn : to[p.d + c] + sn;
                 }
             }
         if (p.groups > 1) __syncthreads();

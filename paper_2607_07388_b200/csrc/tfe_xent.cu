@@ -10,6 +10,7 @@
 //       kLse    z tile by tile, each kept only as its row maxima, row sums of exponentials and the targets' logits;
 //       kProb   z of a piece of the vocabulary once more, turned into that piece of G (bf16, in the workspace);
 //       kGrads  both products of the piece with G: grad W is complete with its piece, grad H adds up over the pieces in fp32.
+//   tfe_xent_few_kernel       the loss of up to 64 rows.
 //   tfe_xent_loss_kernel      joins a row's partial maxima and sums.
 //   tfe_xent_rows_kernel      joins grad H's sums, rounds them and puts them back to their rows.
 //
@@ -43,6 +44,12 @@ constexpr int kThreads = 32 * (4 + kEpilogueWarps);
 constexpr uint32_t kRoom = 32 * 128;            // bytes of an epilogue warp's outgoing piece: 32 rows of 64 bf16
 constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kEpilogueWarps * kRoom;
 constexpr float kLog2e = 1.4426950408889634f;
+// The tensor cores cut what they add to a sum in fp32, always towards zero, so a long sum comes out too small: the loss's logits over 1,024
+// k were off by 6e-7 that way.  A sum of the loss therefore takes at most this many steps, and the epilogue adds those up.
+constexpr int kSumSteps = 4;
+// Registers per thread in the loss's kernel: the first four warps give most of theirs to the epilogue's, which hold 128 sums each.  The
+// sum, 128 x 40 + 256 x 216, must not exceed what the block is launched with; the host checks that before the launch.
+constexpr int kFewRegs = 40, kManyRegs = 216;
 
 constexpr uint32_t kTimeoutLoader = 1u, kTimeoutMma = 2u, kTimeoutEpilogue = 4u;
 __device__ uint32_t g_xent_status;
@@ -374,9 +381,10 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
     tfe_wait_for_stream();
     const Units<kOp> units(p);
 
-    if (warp == 0) {
-        // ============================ TMA producer ============================
-        if (lane == 0) {
+    if (warp < 4) {
+        if constexpr (kOp == kLse) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegs));
+        if (warp == 0 && lane == 0) {
+            // ============================ TMA producer ============================
             const uint64_t hint = 0x1000000000000000ull;            // no preference
             const int32_t b_part = p.tn / kCtas;
             uint32_t stage = 0, phase = 0, issued = 0;
@@ -417,10 +425,8 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                 }
             else if (!ok && issued)
                 __nanosleep(1000000);
-        }
-    } else if (warp == 1) {
-        // ============================ MMA issuer ==============================
-        if (lane == 0 && rank == 0) {
+        } else if (warp == 1 && lane == 0 && rank == 0) {
+            // ============================ MMA issuer ==============================
             uint32_t stage = 0, phase = 0, buf = 0, buf_phase = 0;
             bool ok = !p.give_up;
             for (int64_t u = pair; ok && u < units.n; u += pairs) {
@@ -429,36 +435,39 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                 const uint32_t idesc = umma_idesc(kM, (uint32_t)p.tn, a_mn, b_mn);
                 // 16 k further: 32 bytes along the swizzled row, or 16 rows of 128 bytes
                 const uint64_t a_step = a_mn ? 128u : 2u, b_step = b_mn ? 128u : 2u;
-                for (int32_t t = 0; ok && t < w.tiles && w.steps > 0; ++t) {
-                    ok = mbar_wait(smem_u32(&s_acc_empty[buf]), buf_phase ^ 1u, &s_abort);
-                    for (int32_t ks = 0; ok && ks < w.steps; ++ks) {
-                        ok = mbar_wait(smem_u32(&s_full[stage]), phase, &s_abort);
-                        if (!ok) break;
-                        tc_fence_after();
-                        const uint32_t a = smem_base + stage * kStageBytes, b = a + kBytesA;
-                        const uint64_t a_desc = a_mn ? umma_desc_mn_sw128(a) : umma_desc_sw128(a), b_desc = b_mn ? umma_desc_mn_sw128(b) : umma_desc_sw128(b);
+                const int32_t span = kOp == kLse ? kSumSteps : w.steps;         // steps of a sum
+                for (int32_t t = 0; ok && t < w.tiles; ++t)
+                    for (int32_t k0 = 0; ok && k0 < w.steps; k0 += span) {
+                        ok = mbar_wait(smem_u32(&s_acc_empty[buf]), buf_phase ^ 1u, &s_abort);
+                        for (int32_t ks = k0; ok && ks < min(k0 + span, w.steps); ++ks) {
+                            ok = mbar_wait(smem_u32(&s_full[stage]), phase, &s_abort);
+                            if (!ok) break;
+                            tc_fence_after();
+                            const uint32_t a = smem_base + stage * kStageBytes, b = a + kBytesA;
+                            const uint64_t a_desc = a_mn ? umma_desc_mn_sw128(a) : umma_desc_sw128(a), b_desc = b_mn ? umma_desc_mn_sw128(b) : umma_desc_sw128(b);
 #pragma unroll
-                        for (int k = 0; k < kStepK / 16; ++k)
-                            pair_mma(tmem_base + buf * kN, a_desc + k * a_step, b_desc + k * b_step, idesc, ks > 0 || k > 0 ? 1u : 0u);
-                        pair_commit(smem_u32(&s_empty[stage]));
-                        if (++stage == kStages) { stage = 0; phase ^= 1u; }
+                            for (int k = 0; k < kStepK / 16; ++k)
+                                pair_mma(tmem_base + buf * kN, a_desc + k * a_step, b_desc + k * b_step, idesc, ks > k0 || k > 0 ? 1u : 0u);
+                            pair_commit(smem_u32(&s_empty[stage]));
+                            if (++stage == kStages) { stage = 0; phase ^= 1u; }
+                        }
+                        if (!ok) {
+                            atomicOr(&g_xent_status, kTimeoutMma);
+                            s_abort = 1;
+                            break;
+                        }
+                        pair_commit(smem_u32(&s_acc_full[buf]));
+                        if (++buf == kBuffers) { buf = 0; buf_phase ^= 1u; }
                     }
-                    if (!ok) {
-                        atomicOr(&g_xent_status, kTimeoutMma);
-                        s_abort = 1;
-                        break;
-                    }
-                    pair_commit(smem_u32(&s_acc_full[buf]));
-                    if (++buf == kBuffers) { buf = 0; buf_phase ^= 1u; }
-                }
             }
             if (!ok) {                          // MMAs in flight end before their tensor memory is freed
                 pair_commit(smem_u32(&s_drain));
                 for (uint32_t t = 0; t < TC_WAIT_LIMIT && !mbar_try_wait(smem_u32(&s_drain), 0); ++t) { }
             }
         }
-    } else if (warp >= 4) {
+    } else {
         // ============================ epilogue ================================
+        if constexpr (kOp == kLse) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegs));
         const int e = warp - 4;
         const uint32_t quarter = (uint32_t)warp & 3u;               // tensor-memory lanes 32 * quarter .. + 31
         const int32_t half = e >> 2, cols = p.tn / 2, c0 = half * cols;     // this warp's columns: a multiple of 16
@@ -503,6 +512,64 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                         continue;
                     }
                 }
+                if constexpr (kOp == kLse) {
+                    float2 z[kN / 4];
+#pragma unroll
+                    for (int j = 0; j < kN / 4; ++j) z[j] = make_float2(0.f, 0.f);
+                    for (int32_t k0 = 0; k0 < w.steps; k0 += kSumSteps) {
+                        ok = mbar_wait(smem_u32(&s_acc_full[buf]), buf_phase, &s_abort);
+                        if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
+                        tc_fence_after();
+                        const uint32_t taddr = tmem_base + ((quarter * 32u) << 16) + buf * kN + (uint32_t)c0;
+#pragma unroll
+                        for (int c = 0; c < kN / 2; c += 16) {
+                            uint32_t r[16];
+                            tmem_ld16(taddr + (uint32_t)c, r);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) z[c / 2 + j] = __fadd2_rn(z[c / 2 + j], make_float2(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1])));
+                        }
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) arrive_cluster(in_first(smem_u32(&s_acc_empty[buf])));
+                        if (++buf == kBuffers) { buf = 0; buf_phase ^= 1u; }
+                    }
+                    if (!ok) break;
+                    const int32_t v0 = w.b_at + t * p.tn + c0, left = p.V - v0, mine = target - v0;
+                    if (left < kN / 2)
+#pragma unroll
+                        for (int j = 0; j < kN / 4; ++j) {
+                            z[j].x = 2 * j < left ? z[j].x : -INFINITY;
+                            z[j].y = 2 * j + 1 < left ? z[j].y : -INFINITY;
+                        }
+                    if ((uint32_t)mine < (uint32_t)(kN / 2)) {
+                        float zt = 0.f;
+#pragma unroll
+                        for (int j = 0; j < kN / 2; ++j) zt = mine == j ? (j & 1 ? z[j / 2].y : z[j / 2].x) : zt;
+                        p.z_target[row] = zt;
+                    }
+                    float best[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) best[i] = top;
+#pragma unroll
+                    for (int j = 0; j < kN / 4; ++j) best[j & 7] = fmaxf(best[j & 7], fmaxf(z[j].x, z[j].y));
+#pragma unroll
+                    for (int i = 4; i > 0; i >>= 1)
+#pragma unroll
+                        for (int j = 0; j < i; ++j) best[j] = fmaxf(best[j], best[j + i]);
+                    const float by = tfe_rows::exp2_approx((top - best[0]) * kLog2e);
+                    top = best[0];
+                    sum.x *= by; sum.y *= by;
+                    float2 more = make_float2(0.f, 0.f);
+                    const float2 minus = make_float2(-top, -top), times = make_float2(kLog2e, kLog2e);
+#pragma unroll
+                    for (int j = 0; j < kN / 4; ++j) {
+                        const float2 y = __fmul2_rn(__fadd2_rn(z[j], minus), times), x = make_float2(tfe_rows::exp2_approx(y.x), tfe_rows::exp2_approx(y.y));
+                        if (j & 1) more = __fadd2_rn(more, x); else sum = __fadd2_rn(sum, x);
+                    }
+                    sum = __fadd2_rn(sum, more);
+                    continue;
+                }
                 ok = mbar_wait(smem_u32(&s_acc_full[buf]), buf_phase, &s_abort);
                 if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
                 tc_fence_after();
@@ -515,47 +582,7 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                 // 16 columns at a time, the next ones on their way meanwhile
                 uint32_t r[2][16];
                 tmem_ld16(taddr, r[0]);
-                if constexpr (kOp == kLse) {
-                    const int32_t v0 = w.b_at + t * p.tn + c0, left = p.V - v0, mine = target - v0;
-                    auto take = [&](const uint32_t (&x)[16], int32_t c) {
-                        float z[16];
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) z[j] = __uint_as_float(x[j]);
-                        if (c + 16 > left)
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) z[j] = c + j < left ? z[j] : -INFINITY;
-                        if ((uint32_t)(mine - c) < 16u) {
-                            float zt = 0.f;
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) zt = mine - c == j ? z[j] : zt;
-                            p.z_target[row] = zt;
-                        }
-                        float best[4];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) best[j] = fmaxf(fmaxf(z[j], z[j + 4]), fmaxf(z[j + 8], z[j + 12]));
-                        best[0] = fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3]));
-                        if (best[0] > top) {
-                            const float by = tfe_rows::exp2_approx((top - best[0]) * kLog2e);
-                            sum.x *= by; sum.y *= by;
-                            top = best[0];
-                        }
-                        const float2 minus = make_float2(-top, -top), by = make_float2(kLog2e, kLog2e);
-#pragma unroll
-                        for (int j = 0; j < 16; j += 2) {
-                            const float2 y = __fmul2_rn(__fadd2_rn(make_float2(z[j], z[j + 1]), minus), by);
-                            sum = __fadd2_rn(sum, make_float2(tfe_rows::exp2_approx(y.x), tfe_rows::exp2_approx(y.y)));
-                        }
-                    };
-                    for (int32_t c = 0; c < cols; c += 32) {
-                        tmem_ld_wait();
-                        if (c + 16 < cols) tmem_ld16(taddr + (uint32_t)(c + 16), r[1]);
-                        take(r[0], c);
-                        tmem_ld_wait();
-                        if (c + 32 < cols) tmem_ld16(taddr + (uint32_t)(c + 32), r[0]);
-                        if (c + 16 < cols) take(r[1], c + 16);
-                    }
-                    release();
-                } else if (kOp == kProb || !w.grad_h) {
+                if (kOp == kProb || !w.grad_h) {
                     const int32_t v0 = p.v0 + w.b_at + c0, left = p.V - v0, mine = target - v0;
                     const float2 minus = make_float2(-lse, -lse), by = make_float2(kLog2e, kLog2e), times = make_float2(coef, coef);
                     // 16 columns in bf16: of G, or of grad W
@@ -669,6 +696,199 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
     if (warp == 1) {
         tc_fence_after();
         pair_tmem_dealloc(tmem_base, kBuffers * kN);
+    }
+}
+
+// ------------------------------------------------------------------ few rows
+
+// The loss of up to this many rows: the read of the weights bounds it.  The weights' rows are the MMA's M (128), the hidden states' its
+// N (16..64), so no tensor time goes to rows that are not there: one row of 151,936 x 1,024 took 65 us in tiles of 256 rows.  The
+// vocabulary is cut into equal row ranges, one per SM.  A thread holds one vocabulary row at a time and keeps the running maxima and
+// sums of its columns, the hidden states, in registers until the end.
+constexpr int kFewRows = 64;
+constexpr int kFewCtas = 160;                   // at most: bounds the partial results
+constexpr int kFewM = 128, kFewSteps = 2;       // rows of a tile, steps of a stage
+constexpr int kFewMaxStages = 6, kFewBuffers = 4;
+constexpr int kFewEpilogueWarps = 8, kFewThreads = 32 * (2 + kFewEpilogueWarps);
+__host__ __device__ constexpr int few_stage(int tn) { return kFewSteps * (kFewM + tn) * kStepK * 2; }       // bytes
+__host__ __device__ constexpr int few_stages(int tn) { return 223 * 1024 / few_stage(tn) < kFewMaxStages ? 223 * 1024 / few_stage(tn) : kFewMaxStages; }
+
+struct FewParams {
+    int32_t N, V, steps, rows_per_cta, tail_rows;
+    uint32_t give_up;
+    const int32_t *target;
+    float2 *part; int64_t ld_part;              // [4 * CTAs][ld_part]
+    float *z_target;
+};
+
+template <int TN>
+__global__ void __launch_bounds__(kFewThreads, 1)
+tfe_xent_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_w_tail, const __grid_constant__ CUtensorMap map_h,
+                    const FewParams p)
+{
+    constexpr int kStagesHere = few_stages(TN), kCols = TN / 2;
+    constexpr uint32_t kTmemCols = kFewBuffers * TN, kW = kFewM * kStepK * 2, kH = TN * kStepK * 2, kBytes = kFewSteps * (kW + kH);
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t s_full[kFewMaxStages], s_empty[kFewMaxStages], s_acc_full[kFewBuffers], s_acc_empty[kFewBuffers], s_drain;
+    __shared__ uint32_t s_tmem_base;
+    __shared__ volatile uint32_t s_abort;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStagesHere; ++s) { mbar_init(smem_u32(&s_full[s]), 1); mbar_init(smem_u32(&s_empty[s]), 1); }
+        for (int a = 0; a < kFewBuffers; ++a) { mbar_init(smem_u32(&s_acc_full[a]), 1); mbar_init(smem_u32(&s_acc_empty[a]), kFewEpilogueWarps); }
+        mbar_init(smem_u32(&s_drain), 1);
+        s_abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc(smem_u32(&s_tmem_base), kTmemCols);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = s_tmem_base;
+    tfe_wait_for_stream();
+    const int64_t r0 = (int64_t)blockIdx.x * p.rows_per_cta;
+    const int32_t n_rows = (int32_t)min((int64_t)p.rows_per_cta, p.V - r0), n_tiles = (n_rows + kFewM - 1) / kFewM;
+
+    if (warp == 0) {
+        // ============================ TMA producer ============================
+        if (lane == 0) {
+            const uint64_t hint_w = 0x12F0000000000000ull, hint_h = 0x14F0000000000000ull;      // evict first, evict last
+            uint32_t stage = 0, phase = 0, issued = 0;
+            bool ok = !p.give_up;
+            for (int32_t t = 0; ok && t < n_tiles; ++t) {
+                const int32_t valid = min(kFewM, n_rows - t * kFewM);
+                // a short last tile is fetched with the short box: only its rows are read
+                const bool tail = valid < kFewM && valid == p.tail_rows;
+                const uint32_t w_bytes = tail ? (uint32_t)p.tail_rows * kStepK * 2 : kW;
+                for (int32_t ks = 0; ks < p.steps; ks += kFewSteps) {
+                    if (!mbar_wait(smem_u32(&s_empty[stage]), phase ^ 1u, &s_abort)) {
+                        atomicOr(&g_xent_status, kTimeoutLoader);
+                        s_abort = 1;
+                        ok = false;
+                        break;
+                    }
+                    const uint32_t bar = smem_u32(&s_full[stage]), dst = smem_base + stage * kBytes;
+                    const int32_t n = min(kFewSteps, p.steps - ks);
+                    mbar_expect_tx(bar, (uint32_t)n * (w_bytes + kH));
+                    for (int32_t i = 0; i < n; ++i) {
+                        tma_load_2d(dst + i * (kW + kH), tail ? &map_w_tail : &map_w, bar, (ks + i) * kStepK, (int32_t)(r0 + (int64_t)t * kFewM), hint_w);
+                        tma_load_2d(dst + i * (kW + kH) + kW, &map_h, bar, (ks + i) * kStepK, 0, hint_h);
+                    }
+                    ++issued;
+                    if (++stage == kStagesHere) { stage = 0; phase ^= 1u; }
+                }
+            }
+            if (!ok)                            // copies in flight land before the shared memory goes
+                for (uint32_t s = 0; s < kStagesHere; ++s) {
+                    const uint32_t fills = (issued + kStagesHere - 1u - s) / kStagesHere;
+                    for (uint32_t t = 0; fills && t < TC_WAIT_LIMIT && !mbar_try_wait(smem_u32(&s_full[s]), (fills - 1u) & 1u); ++t) { }
+                }
+        }
+    } else if (warp == 1) {
+        // ============================ MMA issuer ==============================
+        if (lane == 0) {
+            constexpr uint32_t idesc = umma_idesc(kFewM, TN, false, false);
+            uint32_t stage = 0, phase = 0, buf = 0, buf_phase = 0;
+            bool ok = !p.give_up;
+            for (int32_t t = 0; ok && t < n_tiles; ++t)
+                for (int32_t k0 = 0; ok && k0 < p.steps; k0 += kSumSteps) {
+                    ok = mbar_wait(smem_u32(&s_acc_empty[buf]), buf_phase ^ 1u, &s_abort);
+                    for (int32_t ks = k0; ok && ks < min(k0 + kSumSteps, p.steps); ks += kFewSteps) {
+                        ok = mbar_wait(smem_u32(&s_full[stage]), phase, &s_abort);
+                        if (!ok) break;
+                        tc_fence_after();
+                        for (int32_t i = 0; i < min(kFewSteps, p.steps - ks); ++i) {
+                            const uint32_t at = smem_base + stage * kBytes + i * (kW + kH);
+                            const uint64_t w_desc = umma_desc_sw128(at), h_desc = umma_desc_sw128(at + kW);
+#pragma unroll
+                            for (int k = 0; k < kStepK / 16; ++k)
+                                umma_bf16(tmem_base + buf * TN, w_desc + 2 * k, h_desc + 2 * k, idesc, ks > k0 || i > 0 || k > 0 ? 1u : 0u);
+                        }
+                        umma_commit(smem_u32(&s_empty[stage]));
+                        if (++stage == kStagesHere) { stage = 0; phase ^= 1u; }
+                    }
+                    if (!ok) {
+                        atomicOr(&g_xent_status, kTimeoutMma);
+                        s_abort = 1;
+                        break;
+                    }
+                    umma_commit(smem_u32(&s_acc_full[buf]));
+                    if (++buf == kFewBuffers) { buf = 0; buf_phase ^= 1u; }
+                }
+            if (!ok) {                          // MMAs in flight end before their tensor memory is freed
+                umma_commit(smem_u32(&s_drain));
+                for (uint32_t t = 0; t < TC_WAIT_LIMIT && !mbar_try_wait(smem_u32(&s_drain), 0); ++t) { }
+            }
+        }
+    } else {
+        // ============================ epilogue ================================
+        const uint32_t quarter = (uint32_t)warp & 3u;               // tensor-memory lanes 32 * quarter .. + 31
+        const int32_t c0 = ((warp - 2) >> 2) * kCols, row_in_tile = (int32_t)(quarter * 32u) + lane;
+        float top[kCols], sum[kCols];
+        int32_t target[kCols];
+#pragma unroll
+        for (int j = 0; j < kCols; ++j) {
+            top[j] = -3.4e38f;
+            sum[j] = 0.f;
+            target[j] = c0 + j < p.N ? p.target[c0 + j] : -1;
+        }
+        uint32_t buf = 0, buf_phase = 0;
+        bool ok = !p.give_up;
+        for (int32_t t = 0; ok && t < n_tiles; ++t) {
+            float z[kCols];
+            for (int32_t k0 = 0; k0 < p.steps; k0 += kSumSteps) {
+                ok = mbar_wait(smem_u32(&s_acc_full[buf]), buf_phase, &s_abort);
+                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
+                tc_fence_after();
+                const uint32_t taddr = tmem_base + ((quarter * 32u) << 16) + buf * TN + (uint32_t)c0;
+                uint32_t r[kCols];
+                if constexpr (kCols == 32) tmem_ld32(taddr, r);
+                else if constexpr (kCols == 16) tmem_ld16(taddr, r);
+                else tmem_ld8(taddr, r);
+                tmem_ld_wait();
+#pragma unroll
+                for (int j = 0; j < kCols; ++j) z[j] = k0 == 0 ? __uint_as_float(r[j]) : z[j] + __uint_as_float(r[j]);
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&s_acc_empty[buf]));
+                if (++buf == kFewBuffers) { buf = 0; buf_phase ^= 1u; }
+            }
+            if (!ok) break;
+            const int32_t row = t * kFewM + row_in_tile, v = (int32_t)r0 + row;
+            if (row >= n_rows) continue;
+#pragma unroll
+            for (int j = 0; j < kCols; ++j) {
+                if (target[j] == v) p.z_target[c0 + j] = z[j];
+                const float best = fmaxf(top[j], z[j]);
+                sum[j] = sum[j] * tfe_rows::exp2_approx((top[j] - best) * kLog2e) + tfe_rows::exp2_approx((z[j] - best) * kLog2e);
+                top[j] = best;
+            }
+        }
+        if (!ok) {                              // a wait ran out: no results that look like some
+            if (lane == 0) atomicOr(&g_xent_status, kTimeoutEpilogue);
+            s_abort = 1;
+#pragma unroll
+            for (int j = 0; j < kCols; ++j) sum[j] = __int_as_float(0x7FFFFFFF);
+        }
+#pragma unroll
+        for (int j = 0; j < kCols; ++j) {
+            for (int o = 16; o > 0; o >>= 1) {
+                const float top2 = __shfl_xor_sync(0xFFFFFFFFu, top[j], o), sum2 = __shfl_xor_sync(0xFFFFFFFFu, sum[j], o), best = fmaxf(top[j], top2);
+                sum[j] = sum[j] * tfe_rows::exp2_approx((top[j] - best) * kLog2e) + sum2 * tfe_rows::exp2_approx((top2 - best) * kLog2e);
+                top[j] = best;
+            }
+            if (lane == 0 && c0 + j < p.N) p.part[(int64_t)(4 * blockIdx.x + quarter) * p.ld_part + c0 + j] = make_float2(top[j], sum[j]);
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        __syncwarp();
+        tc_fence_after();
+        tmem_dealloc(tmem_base, kTmemCols);
     }
 }
 
@@ -836,7 +1056,7 @@ struct Plan {
     int32_t tn, n_tiles, per_unit, chunks;      // loss
     int64_t piece; int32_t pieces, splits;      // gradients
     int32_t cols, tn_d;
-    bool gather;
+    bool few, gather;
 };
 constexpr int64_t kUnits = 8192;                // units of the loss beyond which tiles are joined: bounds the partial results
 constexpr int64_t kPieceElements = 32 << 20;    // of G: 64 MB stay in L2 until both products have read them
@@ -849,11 +1069,12 @@ Plan make_plan(int32_t N, int32_t V, int32_t d)
     Plan q{};
     q.n_pad = std::max<int64_t>(kM, round_up(N, kM));
     q.m_room = (int32_t)(q.n_pad / kM);
-    q.gather = N > kM;
+    q.gather = N > kM;                          // fewer are one row of tiles, with or without the rows that have no target
     q.tn = kN;
     q.n_tiles = (V + q.tn - 1) / q.tn;
     q.per_unit = (int32_t)std::max<int64_t>(1, (int64_t)q.n_tiles * q.m_room / kUnits);
-    q.chunks = 2 * ((q.n_tiles + q.per_unit - 1) / q.per_unit);
+    q.few = N <= kFewRows;
+    q.chunks = q.few ? 4 * kFewCtas : 2 * ((q.n_tiles + q.per_unit - 1) / q.per_unit);
     const int64_t most = std::max(kPieceMin, kPieceElements / q.n_pad / kN * kN);
     q.pieces = (int32_t)((V + most - 1) / most);
     q.piece = round_up((V + q.pieces - 1) / q.pieces, kN);
@@ -918,10 +1139,23 @@ tfe_status device_sms(int *sms)
 
 tfe_status bad_map() { return tfe_note_cuda(cudaErrorInvalidValue, "cuTensorMapEncodeTiled"); }
 
+template <int TN>
+tfe_status launch_few(int grid, cudaStream_t stream, const CUtensorMap &w, const CUtensorMap &w_tail, const CUtensorMap &h, const FewParams &p)
+{
+    constexpr size_t smem = few_stages(TN) * few_stage(TN) + 1024;
+    if (tfe_status st = tfe_note_cuda(cudaFuncSetAttribute(tfe_xent_few_kernel<TN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem), "cross entropy attribute")) return st;
+    return tfe_launch_serial(tfe_xent_few_kernel<TN>, (unsigned)grid, kFewThreads, 1, smem, stream, "cross entropy launch", w, w_tail, h, p);
+}
+
 template <int kOp>
 tfe_status launch_gemm(int64_t most_units, int sms, cudaStream_t stream, const Maps &maps, const GemmParams &p)
 {
     auto kernel = tfe_xent_gemm_kernel<kOp>;
+    if (kOp == kLse) {                          // the registers that its warps ask for have to be there (they would wait for good)
+        cudaFuncAttributes attr;
+        if (tfe_status st = tfe_note_cuda(cudaFuncGetAttributes(&attr, kernel), "cross entropy attributes")) return st;
+        if (attr.numRegs * kThreads < 128 * kFewRegs + 32 * kEpilogueWarps * kManyRegs) return TFE_ERR_INTERNAL;
+    }
     if (tfe_status st = tfe_note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem), "cross entropy attribute")) return st;
     const unsigned grid = (unsigned)(std::max<int64_t>(1, std::min<int64_t>(sms / kCtas, most_units)) * kCtas);
     return tfe_launch_serial(kernel, grid, kThreads, kCtas, kSmem, stream, "cross entropy launch", maps, p);
@@ -975,6 +1209,32 @@ tfe_status tfe_xent_forward(const void *hidden, int64_t ld_hidden, int32_t N, co
     int sms = 0;
     if (tfe_status st = device_sms(&sms)) return st;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    LossParams l{};
+    l.N = N; l.V = V; l.chunks = q.chunks; l.part = room.part; l.ld_part = q.n_pad; l.z_target = room.z_target; l.target = target; l.pos = room.pos;
+    l.loss = loss; l.lse = lse; l.d = d;
+    l.h = static_cast<const bf16 *>(hidden); l.ld_h = ld_hidden; l.w = static_cast<const bf16 *>(weight); l.ld_w = ld_weight;
+    l.rows = 1;                                 // few rows: a block each
+    while (l.rows < kLossRows && N / l.rows >= 2 * sms) l.rows *= 2;
+    auto join = [&] { return tfe_launch_serial(tfe_xent_loss_kernel, (unsigned)((N + l.rows - 1) / l.rows), kLossThreads, 1, 0, stream, "cross entropy loss launch", l); };
+    if (q.few) {
+        FewParams f{};
+        f.N = N; f.V = V; f.steps = (d + kStepK - 1) / kStepK;
+        const int ctas = std::min(sms, kFewCtas), tn = N <= 16 ? 16 : N <= 32 ? 32 : 64;
+        f.rows_per_cta = (V + ctas - 1) / ctas;
+        f.rows_per_cta = (f.rows_per_cta + 7) / 8 * 8;
+        f.tail_rows = f.rows_per_cta % kFewM;
+        f.give_up = g_xent_give_up.load(std::memory_order_relaxed);
+        f.target = target; f.part = room.part; f.ld_part = q.n_pad; f.z_target = room.z_target;
+        const int grid = (V + f.rows_per_cta - 1) / f.rows_per_cta;
+        CUtensorMap w, w_tail, h;
+        if (!make_map(&w, weight, V, d, ld_weight, kFewM) || !make_map(&w_tail, weight, V, d, ld_weight, f.tail_rows ? (uint32_t)f.tail_rows : 8u) ||
+            !make_map(&h, hidden, N, d, ld_hidden, (uint32_t)tn))
+            return bad_map();
+        const tfe_status st = tn == 16 ? launch_few<16>(grid, stream, w, w_tail, h, f) : tn == 32 ? launch_few<32>(grid, stream, w, w_tail, h, f) : launch_few<64>(grid, stream, w, w_tail, h, f);
+        if (st != TFE_OK) return st;
+        l.chunks = 4 * grid;
+        return join();
+    }
     if (q.gather) {
         CompactParams c{};
         c.N = N; c.V = V; c.d = d; c.h = static_cast<const bf16 *>(hidden); c.ld = ld_hidden; c.target = target;
@@ -991,13 +1251,7 @@ tfe_status tfe_xent_forward(const void *hidden, int64_t ld_hidden, int32_t N, co
     p.n_live = room.n_live; p.target = q.gather ? room.target : target;
     p.part = room.part; p.ld_part = q.n_pad; p.z_target = room.z_target;
     if (tfe_status st = launch_gemm<kLse>((int64_t)q.m_room * (q.chunks / 2), sms, stream, maps, p)) return st;
-    LossParams l{};
-    l.N = N; l.V = V; l.chunks = q.chunks; l.part = room.part; l.ld_part = q.n_pad; l.z_target = room.z_target; l.target = target; l.pos = room.pos;
-    l.loss = loss; l.lse = lse; l.d = d;
-    l.h = static_cast<const bf16 *>(hidden); l.ld_h = ld_hidden; l.w = static_cast<const bf16 *>(weight); l.ld_w = ld_weight;
-    l.rows = 1;                                 // few rows: a block each
-    while (l.rows < kLossRows && N / l.rows >= 2 * sms) l.rows *= 2;
-    return tfe_launch_serial(tfe_xent_loss_kernel, (unsigned)((N + l.rows - 1) / l.rows), kLossThreads, 1, 0, stream, "cross entropy loss launch", l);
+    return join();
 }
 
 tfe_status tfe_xent_backward(const void *hidden, int64_t ld_hidden, int32_t N, const void *weight, int64_t ld_weight, int32_t V, int32_t d,
