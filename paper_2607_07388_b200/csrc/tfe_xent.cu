@@ -44,9 +44,10 @@ constexpr int kThreads = 32 * (4 + kEpilogueWarps);
 constexpr uint32_t kRoom = 32 * 128;            // bytes of an epilogue warp's outgoing piece: 32 rows of 64 bf16
 constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kEpilogueWarps * kRoom;
 constexpr float kLog2e = 1.4426950408889634f;
-// The tensor cores cut what they add to a sum in fp32, always towards zero, so a long sum comes out too small: the loss's logits over 1,024
-// k were off by 6e-7 that way.  A sum of the loss therefore takes at most this many steps, and the epilogue adds those up.
-constexpr int kSumSteps = 4;
+// The tensor cores cut what they add to a sum in fp32, always towards zero, so a long sum comes out too small: a loss over 1,024 k was off by
+// 6e-7 that way.  A sum of the loss therefore takes at most this many steps, and the epilogue adds those up: 3e-7, whatever d.  (With 4
+// steps 1.4e-7 and 624 us instead of 561 for 2,048 x 151,936 x 1,024; the few-row kernel has time for a sum per stage.)
+constexpr int kSumSteps = 8;
 // Registers per thread in the loss's kernel: the first four warps give most of theirs to the epilogue's, which hold 128 sums each.  The
 // sum, 128 x 40 + 256 x 216, must not exceed what the block is launched with; the host checks that before the launch.
 constexpr int kFewRegs = 40, kManyRegs = 216;
@@ -522,12 +523,12 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                         tc_fence_after();
                         const uint32_t taddr = tmem_base + ((quarter * 32u) << 16) + buf * kN + (uint32_t)c0;
 #pragma unroll
-                        for (int c = 0; c < kN / 2; c += 16) {
-                            uint32_t r[16];
-                            tmem_ld16(taddr + (uint32_t)c, r);
+                        for (int c = 0; c < kN / 2; c += 32) {
+                            uint32_t r[32];
+                            tmem_ld32(taddr + (uint32_t)c, r);
                             tmem_ld_wait();
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) z[c / 2 + j] = __fadd2_rn(z[c / 2 + j], make_float2(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1])));
+                            for (int j = 0; j < 16; ++j) z[c / 2 + j] = __fadd2_rn(z[c / 2 + j], make_float2(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1])));
                         }
                         tc_fence_before();
                         __syncwarp();
@@ -793,18 +794,16 @@ tfe_xent_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
             uint32_t stage = 0, phase = 0, buf = 0, buf_phase = 0;
             bool ok = !p.give_up;
             for (int32_t t = 0; ok && t < n_tiles; ++t)
-                for (int32_t k0 = 0; ok && k0 < p.steps; k0 += kSumSteps) {
-                    ok = mbar_wait(smem_u32(&s_acc_empty[buf]), buf_phase ^ 1u, &s_abort);
-                    for (int32_t ks = k0; ok && ks < min(k0 + kSumSteps, p.steps); ks += kFewSteps) {
-                        ok = mbar_wait(smem_u32(&s_full[stage]), phase, &s_abort);
-                        if (!ok) break;
+                for (int32_t ks = 0; ok && ks < p.steps; ks += kFewSteps) {
+                    ok = mbar_wait(smem_u32(&s_acc_empty[buf]), buf_phase ^ 1u, &s_abort) && mbar_wait(smem_u32(&s_full[stage]), phase, &s_abort);
+                    if (ok) {
                         tc_fence_after();
                         for (int32_t i = 0; i < min(kFewSteps, p.steps - ks); ++i) {
                             const uint32_t at = smem_base + stage * kBytes + i * (kW + kH);
                             const uint64_t w_desc = umma_desc_sw128(at), h_desc = umma_desc_sw128(at + kW);
 #pragma unroll
                             for (int k = 0; k < kStepK / 16; ++k)
-                                umma_bf16(tmem_base + buf * TN, w_desc + 2 * k, h_desc + 2 * k, idesc, ks > k0 || i > 0 || k > 0 ? 1u : 0u);
+                                umma_bf16(tmem_base + buf * TN, w_desc + 2 * k, h_desc + 2 * k, idesc, i > 0 || k > 0 ? 1u : 0u);
                         }
                         umma_commit(smem_u32(&s_empty[stage]));
                         if (++stage == kStagesHere) { stage = 0; phase ^= 1u; }
@@ -838,7 +837,7 @@ tfe_xent_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
         bool ok = !p.give_up;
         for (int32_t t = 0; ok && t < n_tiles; ++t) {
             float z[kCols];
-            for (int32_t k0 = 0; k0 < p.steps; k0 += kSumSteps) {
+            for (int32_t k0 = 0; k0 < p.steps; k0 += kFewSteps) {
                 ok = mbar_wait(smem_u32(&s_acc_full[buf]), buf_phase, &s_abort);
                 if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
                 tc_fence_after();
