@@ -45,27 +45,28 @@ struct NormParams {
 };
 
 // A thread's eight columns of a row as they were read: 8 t .. 8 t + 7 for thread t (kVector: 16-byte vectors), or t, t + row_threads, ...;
-// zeros beyond the row.
+// beyond the row zeros, or with vectors the row's first columns (a thread is in the row with all of its columns or with none, and those
+// that are not add nothing to a sum: see RowSum).
 template <typename T, bool kVector>
 struct Eight {
     static constexpr int kWords = (int)sizeof(T) * 2;
     uint32_t w[kWords];
 
-    __device__ __forceinline__ void load(const void *base, int64_t ld, int64_t row, int32_t d, int t, int threads, bool any)
+    __device__ __forceinline__ void load(const void *base, int64_t ld, int64_t row, int32_t d, int t, int threads)
     {
         const T *at = static_cast<const T *>(base) + row * ld;
         if constexpr (kVector) {
+            const int32_t c = kCols * t < d ? kCols * t : 0;
 #pragma unroll
             for (int i = 0; i < kWords / 4; ++i) {
-                uint4 v = make_uint4(0, 0, 0, 0);
-                if (any && kCols * t < d) v = tfe_rows::load_stream(reinterpret_cast<const uint4 *>(at + kCols * t) + i);
+                const uint4 v = tfe_rows::load_stream(reinterpret_cast<const uint4 *>(at + c) + i);
                 w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
             }
         } else {
 #pragma unroll
             for (int e = 0; e < kCols; ++e) {
                 const int32_t c = t + e * threads;
-                const bool in = any && c < d;
+                const bool in = c < d;
                 if constexpr (sizeof(T) == 4) {
                     w[e] = in ? __float_as_uint(at[c]) : 0u;
                 } else {
@@ -74,6 +75,11 @@ struct Eight {
                 }
             }
         }
+    }
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = 0;
     }
     __device__ __forceinline__ float2 two(int i) const      // elements 2 i and 2 i + 1
     {
@@ -122,9 +128,12 @@ __device__ __forceinline__ void load_weight(const void *w, bool f32, int32_t d, 
 struct RowSum {
     float2 *slots;                              // [2][32] of this row's group
     int warps, warp, barrier, threads, turn;
+    bool in;                                    // this thread's columns are in the row
 
     __device__ __forceinline__ float2 operator()(float2 x)
     {
+        x.x = in ? x.x : 0.f;
+        x.y = in ? x.y : 0.f;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
             x.x += __shfl_xor_sync(0xFFFFFFFFu, x.x, o);
@@ -141,13 +150,26 @@ struct RowSum {
     }
 };
 
-__device__ __forceinline__ float inverse_root(float square, float inv_d, float eps) { return __frsqrt_rn(fmaf(square, inv_d, eps)); }
+// The approximate root, reciprocal and exponential are off by 2^-22 at most, which is less than the sums before them; the exact ones are
+// sequences of instructions, and issue slots are what bounds these kernels next to HBM.
+__device__ __forceinline__ float inverse_root(float square, float inv_d, float eps)
+{
+    float y;
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(fmaf(square, inv_d, eps)));
+    return y;
+}
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 __device__ __forceinline__ float2 mul(float2 a, float2 b) { return __fmul2_rn(a, b); }
 __device__ __forceinline__ float2 fma(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
 __device__ __forceinline__ float join(float2 a) { return a.x + a.y; }
-// The reciprocal is the approximate one (1 unit in the last place; 0 where the exponential is beyond 2^126).
-template <typename T> __device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + (sizeof(T) == 4 ? expf(-x) : __expf(-x))); }
+template <typename T>
+__device__ __forceinline__ float sigmoid(float x)
+{
+    if constexpr (sizeof(T) == 4) return __fdividef(1.f, 1.f + expf(-x));      // (an exponent of 15 alone costs the fast one 1e-6)
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(1.f + tfe_rows::exp2_approx(x * -1.4426950408889634f)));
+    return y;
+}
 
 // A row's operands, and what both directions make of them first.
 template <typename T, bool kVector>
@@ -157,11 +179,10 @@ struct Row {
 
     __device__ __forceinline__ void load(const NormParams &p, int64_t row, int t)
     {
-        const bool any = row < p.Q;
-        h.load(p.h, p.ld_h, row, p.d, t, p.row_threads, any);
-        m.load(p.m, p.ld_m, row, p.d, t, p.row_threads, any);
-        if (p.gate_kind == TFE_GATE_VECTOR) gate.load(p.gate, p.ld_gate, row, p.d, t, p.row_threads, any);
-        scalar = any && p.gate_kind == TFE_GATE_SCALAR ? static_cast<const float *>(p.gate)[row] : 1.f;
+        h.load(p.h, p.ld_h, row, p.d, t, p.row_threads);
+        m.load(p.m, p.ld_m, row, p.d, t, p.row_threads);
+        if (p.gate_kind == TFE_GATE_VECTOR) gate.load(p.gate, p.ld_gate, row, p.d, t, p.row_threads);
+        scalar = p.gate_kind == TFE_GATE_SCALAR ? static_cast<const float *>(p.gate)[row] : 1.f;
     }
     __device__ __forceinline__ void gates(const NormParams &p, float2 (&s)[kPairs]) const
     {
@@ -195,8 +216,9 @@ tfe_inject_norm_forward_kernel(const NormParams p)
 {
     __shared__ float2 s_slots[kThreads / 32][2][32];
     tfe_wait_for_stream();
-    const int group = threadIdx.x / p.row_threads, t = threadIdx.x - group * p.row_threads;
-    RowSum row_sum{&s_slots[group][0][0], p.row_threads / 32, t / 32, group + 1, p.row_threads, 0};
+    // (the same number in all lanes of a warp, and taken from one of them: the rows' addresses are then computed once per warp)
+    const int group = __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x / p.row_threads, 0), t = threadIdx.x - group * p.row_threads;
+    RowSum row_sum{&s_slots[group][0][0], p.row_threads / 32, t / 32, group + 1, p.row_threads, 0, !kVector || kCols * t < p.d};
     float2 wp[kPairs], wn[kPairs];
     load_weight<kVector>(p.w_post, p.weights_f32, p.d, t, p.row_threads, wp);
     load_weight<kVector>(p.w_next, p.weights_f32, p.d, t, p.row_threads, wn);
@@ -204,7 +226,7 @@ tfe_inject_norm_forward_kernel(const NormParams p)
     const int64_t step = (int64_t)gridDim.x * p.groups;
     int64_t row = (int64_t)blockIdx.x * p.groups + group;
     Row<T, kVector> x, next;
-    if (kAhead<T, kThreads>) next.load(p, row, t);
+    if (kAhead<T, kThreads> && row < p.Q) next.load(p, row, t);
     for (; row < p.Q; row += step) {
         if constexpr (kAhead<T, kThreads>) {
             x = next;
@@ -235,8 +257,9 @@ tfe_inject_norm_backward_kernel(const NormParams p)
     __shared__ float2 s_slots[kThreads / 32][2][32];
     extern __shared__ float s_sum[];            // [2][d], for several groups
     tfe_wait_for_stream();
-    const int group = threadIdx.x / p.row_threads, t = threadIdx.x - group * p.row_threads;
-    RowSum row_sum{&s_slots[group][0][0], p.row_threads / 32, t / 32, group + 1, p.row_threads, 0};
+    // (the same number in all lanes of a warp, and taken from one of them: the rows' addresses are then computed once per warp)
+    const int group = __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x / p.row_threads, 0), t = threadIdx.x - group * p.row_threads;
+    RowSum row_sum{&s_slots[group][0][0], p.row_threads / 32, t / 32, group + 1, p.row_threads, 0, !kVector || kCols * t < p.d};
     float2 wp[kPairs], wn[kPairs], sum_p[kPairs], sum_n[kPairs];
     load_weight<kVector>(p.w_post, p.weights_f32, p.d, t, p.row_threads, wp);
     load_weight<kVector>(p.w_next, p.weights_f32, p.d, t, p.row_threads, wn);
@@ -251,12 +274,12 @@ tfe_inject_norm_backward_kernel(const NormParams p)
         __device__ __forceinline__ void load(const NormParams &p, int64_t r, int t)
         {
             x.load(p, r, t);
-            gu.load(p.g_out, p.ld_g_out, r, p.d, t, p.row_threads, r < p.Q && p.g_out);
-            gn.load(p.g_normed, p.ld_g_normed, r, p.d, t, p.row_threads, r < p.Q && p.g_normed);
+            if (p.g_out) gu.load(p.g_out, p.ld_g_out, r, p.d, t, p.row_threads); else gu.zero();
+            if (p.g_normed) gn.load(p.g_normed, p.ld_g_normed, r, p.d, t, p.row_threads); else gn.zero();
         }
     };
     All all, next;
-    if (kAhead<T, kThreads>) next.load(p, row, t);
+    if (kAhead<T, kThreads> && row < p.Q) next.load(p, row, t);
     for (; row < p.Q; row += step) {
         if constexpr (kAhead<T, kThreads>) {
             all = next;
