@@ -127,26 +127,52 @@ __device__ __forceinline__ void load_weight(const void *w, bool f32, int32_t d, 
 // Sums over the threads of a row.  Each use needs a slot of its own until every thread has passed the next one's barrier: two in turn.
 struct RowSum {
     float2 *slots;                              // [2][32] of this row's group
-    int warps, warp, barrier, threads, turn;
+    int warps, warp, barrier, threads;
     bool in;                                    // this thread's columns are in the row
+    int turn, span;                             // span: half the warps, rounded up to a power of two; 0 for one warp
 
-    __device__ __forceinline__ float2 operator()(float2 x)
+    __device__ __forceinline__ RowSum(float2 *slots_, int group, int row_threads, int t, bool in_)
+        : slots(slots_), warps(row_threads / 32), warp(t / 32), barrier(group + 1), threads(row_threads), in(in_), turn(0), span(0)
     {
-        x.x = in ? x.x : 0.f;
-        x.y = in ? x.y : 0.f;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            x.x += __shfl_xor_sync(0xFFFFFFFFu, x.x, o);
-            x.y += __shfl_xor_sync(0xFFFFFFFFu, x.y, o);
-        }
+        for (int w = 1; w < warps; w *= 2) span = w;
+        if (t < 32) slots[t] = slots[32 + t] = make_float2(0.f, 0.f);
+        asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(threads) : "memory");
+    }
+
+    template <typename X> __device__ __forceinline__ X shared(X x)
+    {
         if (warps == 1) return x;
-        float2 *s = slots + 32 * turn;
+        X *s = reinterpret_cast<X *>(slots + 32 * turn);
         turn ^= 1;
         if ((threadIdx.x & 31) == 0) s[warp] = x;
         asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(threads) : "memory");
-        x = s[0];
-        for (int i = 1; i < warps; ++i) { x.x += s[i].x; x.y += s[i].y; }
+        return s[threadIdx.x & (2 * span - 1)];         // (slots beyond the warps hold zeros from the start)
+    }
+    // one sum, or two
+    __device__ __forceinline__ float operator()(float x)
+    {
+        x = in ? x : 0.f;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
+        x = shared(x);
+        for (int o = span; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
         return x;
+    }
+    __device__ __forceinline__ float2 operator()(float x, float y)
+    {
+        x = in ? x : 0.f;
+        y = in ? y : 0.f;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
+            y += __shfl_xor_sync(0xFFFFFFFFu, y, o);
+        }
+        float2 two = shared(make_float2(x, y));
+        for (int o = span; o > 0; o >>= 1) {
+            two.x += __shfl_xor_sync(0xFFFFFFFFu, two.x, o);
+            two.y += __shfl_xor_sync(0xFFFFFFFFu, two.y, o);
+        }
+        return two;
     }
 };
 
@@ -218,7 +244,7 @@ tfe_inject_norm_forward_kernel(const NormParams p)
     tfe_wait_for_stream();
     // (the same number in all lanes of a warp, and taken from one of them: the rows' addresses are then computed once per warp)
     const int group = __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x / p.row_threads, 0), t = threadIdx.x - group * p.row_threads;
-    RowSum row_sum{&s_slots[group][0][0], p.row_threads / 32, t / 32, group + 1, p.row_threads, 0, !kVector || kCols * t < p.d};
+    RowSum row_sum(&s_slots[group][0][0], group, p.row_threads, t, !kVector || kCols * t < p.d);
     float2 wp[kPairs], wn[kPairs];
     load_weight<kVector>(p.w_post, p.weights_f32, p.d, t, p.row_threads, wp);
     load_weight<kVector>(p.w_next, p.weights_f32, p.d, t, p.row_threads, wn);
@@ -234,7 +260,7 @@ tfe_inject_norm_forward_kernel(const NormParams p)
         } else {
             x.load(p, row, t);
         }
-        const float a = inverse_root(row_sum(make_float2(x.square_m(), 0.f)).x, inv_d, p.eps);
+        const float a = inverse_root(row_sum(x.square_m()), inv_d, p.eps);
         float2 u[kPairs], square = both(0.f);
         x.gates(p, u);
 #pragma unroll
@@ -242,7 +268,7 @@ tfe_inject_norm_forward_kernel(const NormParams p)
             u[i] = fma(mul(u[i], both(p.lam * a)), mul(x.m.two(i), wp[i]), x.h.two(i));
             square = fma(u[i], u[i], square);
         }
-        const float b = inverse_root(row_sum(make_float2(join(square), 0.f)).x, inv_d, p.eps);
+        const float b = inverse_root(row_sum(join(square)), inv_d, p.eps);
         store<T, kVector>(p.out, p.ld_out, row, p.d, t, p.row_threads, u);
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) u[i] = mul(mul(u[i], both(b)), wn[i]);
@@ -259,7 +285,7 @@ tfe_inject_norm_backward_kernel(const NormParams p)
     tfe_wait_for_stream();
     // (the same number in all lanes of a warp, and taken from one of them: the rows' addresses are then computed once per warp)
     const int group = __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x / p.row_threads, 0), t = threadIdx.x - group * p.row_threads;
-    RowSum row_sum{&s_slots[group][0][0], p.row_threads / 32, t / 32, group + 1, p.row_threads, 0, !kVector || kCols * t < p.d};
+    RowSum row_sum(&s_slots[group][0][0], group, p.row_threads, t, !kVector || kCols * t < p.d);
     float2 wp[kPairs], wn[kPairs], sum_p[kPairs], sum_n[kPairs];
     load_weight<kVector>(p.w_post, p.weights_f32, p.d, t, p.row_threads, wp);
     load_weight<kVector>(p.w_next, p.weights_f32, p.d, t, p.row_threads, wn);
@@ -288,48 +314,52 @@ tfe_inject_norm_backward_kernel(const NormParams p)
             all.load(p, row, t);
         }
         const Row<T, kVector> &x = all.x;
-        const float a = inverse_root(row_sum(make_float2(x.square_m(), 0.f)).x, inv_d, p.eps);
-        float2 s[kPairs], u[kPairs], uu = both(0.f), ut = both(0.f);
+        const float a = inverse_root(row_sum(x.square_m()), inv_d, p.eps);
+        const float la = p.lam * a;
+        float2 s[kPairs], q[kPairs], u[kPairs], uu = both(0.f), ut = both(0.f);
         x.gates(p, s);
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) {
-            u[i] = fma(mul(s[i], both(p.lam * a)), mul(x.m.two(i), wp[i]), x.h.two(i));
+            q[i] = mul(x.m.two(i), wp[i]);      // y / a
+            u[i] = fma(mul(s[i], both(la)), q[i], x.h.two(i));
             uu = fma(u[i], u[i], uu);
             ut = fma(u[i], mul(wn[i], all.gn.two(i)), ut);
         }
-        float2 two = row_sum(make_float2(join(uu), join(ut)));
+        const float2 two = row_sum(join(uu), join(ut));
         const float b = inverse_root(two.x, inv_d, p.eps), by_u = b * b * b * two.y * inv_d;
-        float2 mx = both(0.f), uy = both(0.f);
+        float2 sdh[kPairs], mx = both(0.f), uy = both(0.f);         // sdh: s dh; mx, uy and sum_p without their factors lam and a
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) {
-            const float2 n = mul(all.gn.two(i), both(b)), am = mul(x.m.two(i), both(a));
+            const float2 n = mul(all.gn.two(i), both(b));
             sum_n[i] = fma(n, u[i], sum_n[i]);
             u[i] = fma(both(-by_u), u[i], fma(n, wn[i], all.gu.two(i)));       // dh
-            const float2 dy = mul(mul(s[i], both(p.lam)), u[i]);
-            sum_p[i] = fma(dy, am, sum_p[i]);
-            mx = fma(x.m.two(i), mul(wp[i], dy), mx);
-            uy = fma(u[i], mul(am, wp[i]), uy);
+            sdh[i] = mul(s[i], u[i]);
+            sum_p[i] = fma(sdh[i], mul(x.m.two(i), both(a)), sum_p[i]);
+            mx = fma(q[i], sdh[i], mx);
         }
         if (p.g_h) store<T, kVector>(p.g_h, p.ld_g_h, row, p.d, t, p.row_threads, u);
-        two = row_sum(make_float2(join(mx), join(uy)));
-        const float by_m = a * a * a * two.x * inv_d;
+        if (p.g_gate && p.gate_kind == TFE_GATE_SCALAR) {
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) uy = fma(u[i], q[i], uy);
+            const float dot = row_sum(join(uy));
+            if (t == 0) static_cast<float *>(p.g_gate)[row] = la * dot * (p.sigmoid ? s[0].x * (1.f - s[0].x) : 1.f);
+        }
         if (p.g_m) {
+            const float by_m = a * a * row_sum(join(mx)) * inv_d;
             float2 dm[kPairs];
 #pragma unroll
-            for (int i = 0; i < kPairs; ++i) dm[i] = fma(both(-by_m), x.m.two(i), mul(mul(wp[i], both(p.lam * a)), mul(s[i], u[i])));
+            for (int i = 0; i < kPairs; ++i) dm[i] = mul(fma(both(-by_m), x.m.two(i), mul(wp[i], sdh[i])), both(la));
             store<T, kVector>(p.g_m, p.ld_g_m, row, p.d, t, p.row_threads, dm);
         }
         if (p.g_gate && p.gate_kind == TFE_GATE_VECTOR) {
 #pragma unroll
-            for (int i = 0; i < kPairs; ++i) {
-                u[i] = mul(mul(u[i], both(p.lam * a)), mul(x.m.two(i), wp[i]));
-                if (p.sigmoid) u[i] = mul(u[i], mul(s[i], make_float2(1.f - s[i].x, 1.f - s[i].y)));
-            }
-            store<T, kVector>(p.g_gate, p.ld_g_gate, row, p.d, t, p.row_threads, u);
-        } else if (p.g_gate && t == 0) {
-            static_cast<float *>(p.g_gate)[row] = p.lam * two.y * (p.sigmoid ? s[0].x * (1.f - s[0].x) : 1.f);
+            for (int i = 0; i < kPairs; ++i)
+                q[i] = mul(mul(q[i], both(la)), p.sigmoid ? mul(sdh[i], fma(s[i], both(-1.f), both(1.f))) : u[i]);
+            store<T, kVector>(p.g_gate, p.ld_g_gate, row, p.d, t, p.row_threads, q);
         }
     }
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) sum_p[i] = mul(sum_p[i], both(p.lam));
     if (!p.part) return;
     float *to = p.groups > 1 ? s_sum : p.part + (int64_t)blockIdx.x * 2 * p.d;
     for (int g = 0; g < p.groups; ++g) {
