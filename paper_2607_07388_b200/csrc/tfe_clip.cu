@@ -26,7 +26,8 @@ using tfe_rows::Elem;
 
 constexpr int kThreads = 256;
 constexpr int64_t kChunk = 8192;                // elements
-constexpr int kBlocks = 148 * 6;                // most blocks of a launch
+constexpr int kPerSm = 6;                       // blocks, all resident
+constexpr int kBlocks = 148 * kPerSm;           // most blocks of a launch
 
 struct Entry { uint64_t in, out; int64_t n; uint32_t first; int32_t dtype; };       // first: the tensor's first chunk
 template <int kRoom> struct Table {
@@ -104,7 +105,7 @@ __device__ __forceinline__ double block_sum(double x, double *s_warp)
 }
 
 template <int kRoom>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kPerSm)
 tfe_grad_norm_kernel(const __grid_constant__ Table<kRoom> t)
 {
     __shared__ double s_warp[kThreads / 32];
@@ -212,7 +213,7 @@ tfe_status run_pass(const Job &j, int pass, int32_t lo, int32_t hi, int32_t *par
     t.chunks = (uint32_t)chunks;
     t.parts = parts; t.part0 = *part0; t.part = j.part; t.norm = j.norm; t.max_norm = j.max_norm;
     t.write_norm = first; t.in_place = j.out == nullptr; t.only_norm = j.only_norm;
-    const unsigned grid = pass == 1 && j.only_norm ? 1u : (unsigned)std::max<uint64_t>(1, std::min<uint64_t>(chunks, (uint64_t)std::min(kBlocks, 6 * j.sms)));
+    const unsigned grid = pass == 1 && j.only_norm ? 1u : (unsigned)std::max<uint64_t>(1, std::min<uint64_t>(chunks, (uint64_t)std::min(kBlocks, kPerSm * j.sms)));
     if (pass == 0) *part0 += (int32_t)grid;
     return tfe_launch_serial(pass == 0 ? tfe_grad_norm_kernel<kRoom> : tfe_grad_clip_kernel<kRoom>, grid, kThreads, 1, 0, j.stream, "gradient norm launch", t);
 }

@@ -37,12 +37,17 @@ constexpr int kM = kRowsA * kCtas;              // rows of a tile
 constexpr int kN = 256;                         // columns of a tile at most (MMA N)
 constexpr int kStepK = 64;                      // k of a stage: 128 bytes, one swizzle row
 constexpr uint32_t kBytesA = kRowsA * kStepK * 2, kBytesB = kN / kCtas * kStepK * 2, kStageBytes = kBytesA + kBytesB;
-constexpr int kStages = 196608 / kStageBytes;
+#ifndef TST
+#define TST 6
+#define TROOM 1
+#endif
+constexpr int kStages = TST;
 constexpr int kBuffers = 2;                     // accumulators of kN columns: all of tensor memory
 constexpr int kEpilogueWarps = 8;               // two per lane quarter of tensor memory, half of the tile's columns each
 constexpr int kThreads = 32 * (4 + kEpilogueWarps);
 constexpr uint32_t kRoom = 32 * 128;            // bytes of an epilogue warp's outgoing piece: 32 rows of 64 bf16
-constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kEpilogueWarps * kRoom;
+constexpr uint32_t kRooms = TROOM;              // pieces of a warp on their way
+constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kEpilogueWarps * kRooms * kRoom;
 constexpr float kLog2e = 1.4426950408889634f;
 // The tensor cores cut what they add to a sum in fp32, always towards zero, so a long sum comes out too small: a loss over 1,024 k was off by
 // 6e-7 that way.  A sum of the loss therefore takes at most this many steps, and the epilogue adds those up: 3e-7, whatever d.  (With 4
@@ -59,9 +64,11 @@ std::atomic<uint32_t> g_xent_give_up{0};
 __global__ void tfe_xent_status_kernel(uint32_t told) { atomicAnd(&g_xent_status, ~told); }
 
 enum Op { kLse, kProb, kGrads };
+// What units of the gradients' products cost, in steps: each a little besides its steps, and grad W at least the time its tile takes to leave.
+constexpr int32_t kUnitCost = 1, kSendCost = 6;
 
 struct GemmParams {
-    int32_t N, V, d;
+    int32_t N, V, d, n_pad;
     int32_t tn;                                 // columns of a tile
     int32_t per_unit, n_tiles;                  // kLse: tiles of a unit, all column tiles
     int32_t v0, width;                          // kProb, kGrads: the piece, [v0, v0 + width)
@@ -214,6 +221,22 @@ struct Units {
             n = n_h + n_w;
         }
     }
+    // A pair's units: [first, last) in steps of step.
+    __device__ __forceinline__ void share(int64_t pair, int64_t pairs, int64_t &first, int64_t &last, int64_t &step) const
+    {
+        if constexpr (kOp != kGrads) {
+            first = pair; last = n; step = pairs;
+        } else {
+            // Two lengths: equal shares of all steps, to within a unit.  The columns of d change last, so that a pair keeps to one part of W or H,
+            // and the pairs that are at the other columns read the same tiles of G at about the same time.
+            const int64_t cost_h = steps_h + kUnitCost, cost_w = max(steps_w, kSendCost) + kUnitCost, all = n_h * cost_h + n_w * cost_w;
+            auto bound = [&](int64_t i) {
+                const int64_t x = all * i / pairs, h = n_h * cost_h;
+                return x <= h ? (x + cost_h / 2) / cost_h : n_h + (x - h + cost_w / 2) / cost_w;
+            };
+            first = bound(pair); last = pair + 1 == pairs ? n : bound(pair + 1); step = 1;
+        }
+    }
     __device__ __forceinline__ Unit at(const GemmParams &p, int64_t u) const
     {
         Unit w{};
@@ -230,10 +253,9 @@ struct Units {
                 w.b_at = nt * p.tn;             // within the piece
             }
         } else {
-            const bool h_first = steps_h >= steps_w;        // the longer units first
-            w.grad_h = h_first ? u < n_h : u >= n_w;
+            w.grad_h = u < n_h;
             if (w.grad_h) {
-                const int32_t i = (int32_t)(h_first ? u : u - n_w), ct = i % cols, mt = i / cols % m_tiles, s = i / cols / m_tiles;
+                const int32_t i = (int32_t)u, mt = i % m_tiles, s = i / m_tiles % p.splits, ct = i / m_tiles / p.splits;
                 const int32_t all = (p.width + kStepK - 1) / kStepK;
                 w.a_at = mt * kM;
                 w.b_at = ct * p.tn;
@@ -241,9 +263,9 @@ struct Units {
                 w.steps = max(0, min(steps_h, all - s * steps_h));
                 w.index = (s * p.m_room + mt) * cols + ct;
             } else {
-                const int32_t i = (int32_t)(h_first ? u - n_h : u);
-                w.a_at = i / cols * kM;         // within the piece
-                w.b_at = i % cols * p.tn;
+                const int32_t i = (int32_t)(u - n_h), tall = (int32_t)(n_w / cols);
+                w.a_at = i % tall * kM;         // within the piece
+                w.b_at = i / tall * p.tn;
                 w.steps = steps_w;
             }
         }
@@ -381,6 +403,8 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
     const uint32_t tmem_base = s_tmem_base;
     tfe_wait_for_stream();
     const Units<kOp> units(p);
+    int64_t u_first, u_last, u_step;
+    units.share(pair, pairs, u_first, u_last, u_step);
 
     if (warp < 4) {
         if constexpr (kOp == kLse) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegs));
@@ -390,7 +414,7 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
             const int32_t b_part = p.tn / kCtas;
             uint32_t stage = 0, phase = 0, issued = 0;
             bool ok = !p.give_up;
-            for (int64_t u = pair; ok && u < units.n; u += pairs) {
+            for (int64_t u = u_first; ok && u < u_last; u += u_step) {
                 const Unit w = units.at(p, u);
                 for (int32_t t = 0; ok && t < w.tiles; ++t)
                     for (int32_t ks = 0; ks < w.steps; ++ks) {
@@ -408,10 +432,10 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                             pair_load_2d(a, &maps.a, bar, k, a_at, hint);
                             pair_load_2d(b, &maps.b, bar, k, (kOp == kProb ? p.v0 : 0) + b_at, hint);
                         } else if (w.grad_h) {
-                            pair_load_2d(a, &maps.a, bar, k, a_at, hint);
+                            pair_load_2d(a, &maps.a, bar, 0, k / 64 * p.n_pad + a_at, hint);
                             for (int32_t j = 0; j < b_part; j += 64) pair_load_2d(b + j * kStepK * 2, &maps.b, bar, b_at + j, p.v0 + k, hint);
                         } else {
-                            for (int32_t j = 0; j < kRowsA; j += 64) pair_load_2d(a + j * kStepK * 2, &maps.a_w, bar, a_at + j, k, hint);
+                            for (int32_t j = 0; j < kRowsA; j += 64) pair_load_2d(a + j * kStepK * 2, &maps.a_w, bar, 0, (a_at + j) / 64 * p.n_pad + k, hint);
                             for (int32_t j = 0; j < b_part; j += 64) pair_load_2d(b + j * kStepK * 2, &maps.b_w, bar, b_at + j, k, hint);
                         }
                         ++issued;
@@ -430,7 +454,7 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
             // ============================ MMA issuer ==============================
             uint32_t stage = 0, phase = 0, buf = 0, buf_phase = 0;
             bool ok = !p.give_up;
-            for (int64_t u = pair; ok && u < units.n; u += pairs) {
+            for (int64_t u = u_first; ok && u < u_last; u += u_step) {
                 const Unit w = units.at(p, u);
                 const bool a_mn = kOp == kGrads && !w.grad_h, b_mn = kOp == kGrads;
                 const uint32_t idesc = umma_idesc(kM, (uint32_t)p.tn, a_mn, b_mn);
@@ -473,12 +497,15 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
         const uint32_t quarter = (uint32_t)warp & 3u;               // tensor-memory lanes 32 * quarter .. + 31
         const int32_t half = e >> 2, cols = p.tn / 2, c0 = half * cols;     // this warp's columns: a multiple of 16
         const int32_t first_row = (int32_t)(rank * kRowsA + quarter * 32u), row_in_tile = first_row + lane;
-        const uint32_t room = smem_base + kStages * kStageBytes + (uint32_t)e * kRoom;
+        const uint32_t rooms = smem_base + kStages * kStageBytes + (uint32_t)e * kRooms * kRoom;
+        uint32_t turn = 0;
         uint32_t buf = 0, buf_phase = 0;
         bool ok = !p.give_up;
         // 64 finished columns of this warp's rows leave by an asynchronous copy
         auto send = [&](const uint32_t (&out)[32], int32_t x, int32_t y, bool there) {
-            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");     // the last ones have left
+            const uint32_t room = rooms + turn * kRoom;
+            turn = (turn + 1) % kRooms;
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kRooms - 1) : "memory");     // what was there has left
             __syncwarp();
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -492,8 +519,8 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                 asm volatile("cp.async.bulk.commit_group;" ::: "memory");
             }
         };
-        int64_t u = pair;
-        for (; ok && u < units.n; u += pairs) {
+        int64_t u = u_first;
+        for (; ok && u < u_last; u += u_step) {
             const Unit w = units.at(p, u);
             const int32_t row = w.a_at + row_in_tile;
             const bool live = row < units.n_live;                   // (of no use to grad W, whose rows are the vocabulary's)
@@ -638,7 +665,7 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                         }
                         if (c + 64 >= cols) release();
                         if constexpr (kOp == kProb) {
-                            send(reinterpret_cast<const uint32_t (&)[32]>(out), w.b_at + c0 + c, w.a_at + first_row, true);
+                            send(reinterpret_cast<const uint32_t (&)[32]>(out), 0, (w.b_at + c0 + c) / 64 * p.n_pad + w.a_at + first_row, true);
                         } else {                // (what lies beyond the matrix is not written)
                             const int32_t x0 = w.b_at + c0 + c, y0 = p.v0 + w.a_at + first_row;
                             send(reinterpret_cast<const uint32_t (&)[32]>(out), x0, y0, x0 < p.d && y0 < p.V);
@@ -683,7 +710,7 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
             }
             s_abort = 1;
             if constexpr (kOp == kLse)
-                for (; u < units.n; u += pairs) {
+                for (; u < u_last; u += u_step) {
                     const Unit w = units.at(p, u);
                     const int32_t row = w.a_at + row_in_tile;
                     if (row < units.n_live) p.part[(int64_t)(2 * w.index + half) * p.ld_part + row] = make_float2(0.f, __int_as_float(0x7FFFFFFF));
@@ -903,11 +930,12 @@ struct LossParams {
 };
 constexpr int kLossThreads = 512, kLossRows = 32;
 
-// Joins maxima and sums, relative to the greater of the maxima.
-__device__ __forceinline__ void fold(float &top, double &sum, float top2, double sum2)
+// Joins maxima and sums, relative to the greater of the maxima (which is never -inf: tiles begin at -3.4e38).
+__device__ __forceinline__ void fold(float &top, float &sum, float top2, float sum2)
 {
-    if (top2 > top) { const float t = top; top = top2; top2 = t; const double x = sum; sum = sum2; sum2 = x; }
-    if (!(sum2 == 0.0)) sum += sum2 * exp((double)top2 - (double)top);
+    const float best = fmaxf(top, top2);
+    sum = sum * tfe_rows::exp2_approx((top - best) * kLog2e) + sum2 * tfe_rows::exp2_approx((top2 - best) * kLog2e);
+    top = best;
 }
 
 // A row's partial results joined by kLossThreads / rows threads.  The tensor cores' sum of a target's logit is off by some 1e-7 of its
@@ -915,8 +943,9 @@ __device__ __forceinline__ void fold(float &top, double &sum, float top2, double
 __global__ void __launch_bounds__(kLossThreads)
 tfe_xent_loss_kernel(const LossParams p)
 {
-    __shared__ float s_top[kLossThreads / 32][kLossRows], s_z[kLossRows];
-    __shared__ double s_sum[kLossThreads / 32][kLossRows];
+    constexpr int kWarps = kLossThreads / 32;
+    __shared__ float s_top[kLossRows][kWarps], s_sum[kLossRows][kWarps];
+    __shared__ double s_z[kLossRows];
     tfe_wait_for_stream();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t r0 = (int64_t)blockIdx.x * p.rows;
@@ -924,28 +953,13 @@ tfe_xent_loss_kernel(const LossParams p)
         const int32_t t = r < p.N ? p.target[r] : -1;
         return t < 0 || t >= p.V ? -1 : p.pos ? p.pos[r] : r;
     };
-    {
-        const int i = threadIdx.x & (p.rows - 1), step = kLossThreads / p.rows;
-        const int64_t at = place(r0 + i);
-        float top = -INFINITY, sum = 0.f;
-        if (at >= 0) {
-#pragma unroll 4
-            for (int32_t c = threadIdx.x / p.rows; c < p.chunks; c += step) {
-                const float2 x = p.part[(int64_t)c * p.ld_part + at];
-                const float best = fmaxf(top, x.x);
-                sum = sum * tfe_rows::exp2_approx((top - best) * kLog2e) + x.y * tfe_rows::exp2_approx((x.x - best) * kLog2e);
-                top = best;
-            }
-        }
-        double all = (double)sum;
-        for (int o = 16; o >= p.rows; o >>= 1) fold(top, all, __shfl_xor_sync(0xFFFFFFFFu, top, o), __shfl_xor_sync(0xFFFFFFFFu, all, o));
-        if (lane < p.rows) { s_top[warp][i] = top; s_sum[warp][i] = all; }
-    }
-    for (int i = warp; i < p.rows; i += kLossThreads / 32) {
+    for (int i = warp; i < p.rows; i += kWarps) {
         const int64_t r = r0 + i;
-        if (place(r) < 0) continue;
-        const uint4 *h = reinterpret_cast<const uint4 *>(p.h + r * p.ld_h), *w = reinterpret_cast<const uint4 *>(p.w + (int64_t)p.target[r] * p.ld_w);
+        const int32_t t = r < p.N ? p.target[r] : -1;
+        if (t < 0 || t >= p.V) continue;
+        const uint4 *h = reinterpret_cast<const uint4 *>(p.h + r * p.ld_h), *w = reinterpret_cast<const uint4 *>(p.w + (int64_t)t * p.ld_w);
         double z = 0.0;
+#pragma unroll 4
         for (int32_t v = lane; v < p.d / 8; v += 32) {
             float a[8], b[8], x = 0.f;
             tfe_rows::Elem<bf16>::unpack(h[v], a);
@@ -955,20 +969,36 @@ tfe_xent_loss_kernel(const LossParams p)
             z += (double)x;
         }
         for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xFFFFFFFFu, z, o);
-        if (lane == 0) s_z[i] = (float)z;
+        if (lane == 0) s_z[i] = z;
+    }
+    {
+        const int i = threadIdx.x & (p.rows - 1), step = kLossThreads / p.rows;
+        const int64_t at = place(r0 + i);
+        float top = -3.4e38f, sum = 0.f;
+        if (at >= 0) {
+#pragma unroll 4
+            for (int32_t c = threadIdx.x / p.rows; c < p.chunks; c += step) {
+                const float2 x = p.part[(int64_t)c * p.ld_part + at];
+                fold(top, sum, x.x, x.y);
+            }
+        }
+        for (int o = 16; o >= p.rows; o >>= 1) fold(top, sum, __shfl_xor_sync(0xFFFFFFFFu, top, o), __shfl_xor_sync(0xFFFFFFFFu, sum, o));
+        if (lane < p.rows) { s_top[i][warp] = top; s_sum[i][warp] = sum; }
     }
     __syncthreads();
-    if (threadIdx.x >= p.rows || r0 + threadIdx.x >= p.N) return;
-    const int64_t r = r0 + threadIdx.x, at = place(r);
-    if (at < 0) { p.loss[r] = p.lse[r] = 0.f; return; }
-    float top = s_top[0][threadIdx.x];
-    double sum = s_sum[0][threadIdx.x];
-    for (int i = 1; i < kLossThreads / 32; ++i) fold(top, sum, s_top[i][threadIdx.x], s_sum[i][threadIdx.x]);
-    const double z = (double)s_z[threadIdx.x], was = (double)p.z_target[at];
-    double lse = (double)top + log(sum);
-    lse += log1p(exp(was - lse) * expm1(z - was));
-    p.lse[r] = (float)lse;
-    p.loss[r] = (float)(lse - z);
+    for (int i = warp; i < p.rows; i += kWarps) {
+        const int64_t r = r0 + i, at = place(r);
+        float top = s_top[i][lane & (kWarps - 1)], sum = s_sum[i][lane & (kWarps - 1)];
+        for (int o = kWarps / 2; o > 0; o >>= 1) fold(top, sum, __shfl_xor_sync(0xFFFFFFFFu, top, o), __shfl_xor_sync(0xFFFFFFFFu, sum, o));
+        if (lane != 0 || r >= p.N) continue;
+        if (at < 0) { p.loss[r] = p.lse[r] = 0.f; continue; }
+        const double z = s_z[i];
+        const float was = p.z_target[at];
+        double lse = (double)top + log((double)sum);
+        lse += (double)log1pf(expf((float)((double)was - lse)) * expm1f((float)(z - (double)was)));
+        p.lse[r] = (float)lse;
+        p.loss[r] = (float)(lse - z);
+    }
 }
 
 struct RowsParams {
@@ -1058,7 +1088,11 @@ struct Plan {
     bool few, gather;
 };
 constexpr int64_t kUnits = 8192;                // units of the loss beyond which tiles are joined: bounds the partial results
-constexpr int64_t kPieceElements = 32 << 20;    // of G: 64 MB stay in L2 until both products have read them
+#ifndef TPIECE
+#define TPIECE 128
+#endif
+constexpr int64_t kPieceElements = TPIECE << 20;    // of G: 64 MB stay in L2 until both products have read them
+constexpr int64_t kMaxSplits = 64, kPairs = 74; // kPairs: of the device that the sizes are meant for
 constexpr int64_t kPieceMin = 4096;             // columns of a piece at least
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
@@ -1078,9 +1112,11 @@ Plan make_plan(int32_t N, int32_t V, int32_t d)
     q.pieces = (int32_t)((V + most - 1) / most);
     q.piece = round_up((V + q.pieces - 1) / q.pieces, kN);
     q.pieces = (int32_t)((V + q.piece - 1) / q.piece);
-    q.splits = (int32_t)std::min<int64_t>(8, std::max<int64_t>(1, q.piece / q.n_pad));
     q.tn_d = d >= kN ? kN : 128;
     q.cols = (d + q.tn_d - 1) / q.tn_d;
+    // parts of grad H's sums: units of about a sixth of a pair's share of the work, so that the shares come out even
+    const int64_t steps = q.piece / kStepK, work = q.cols * (q.m_room * steps + q.piece / kM * std::max<int64_t>(kSendCost, q.n_pad / kStepK));
+    q.splits = (int32_t)std::min<int64_t>(kMaxSplits, (steps + std::max<int64_t>(16, work / kPairs / 6) - 1) / std::max<int64_t>(16, work / kPairs / 6));
     return q;
 }
 
@@ -1283,14 +1319,16 @@ tfe_status tfe_xent_backward(const void *hidden, int64_t ld_hidden, int32_t N, c
     c.h_out = room.h; c.pos = room.pos; c.target_out = room.target; c.n_live = room.n_live; c.lse_out = room.lse; c.coef_out = room.coef; c.failed = room.failed;
     if (tfe_status st = launch_compact(c, sms, stream)) return st;
 
+    // G lies in blocks of 64 columns, one below the other: whichever way a product reads it, a tile is one run of memory
+    const int64_t g_rows = q.n_pad * (q.piece / 64);
     Maps probs{}, grads{};
     if (!make_map(&probs.a, room.h, q.n_pad, d, d, kRowsA) || !make_map(&probs.b, weight, V, d, ld_weight, kN / kCtas) ||
-        !make_map(&probs.out, room.g, q.n_pad, q.piece, q.piece, 32) || !make_map(&grads.a, room.g, q.n_pad, q.piece, q.piece, kRowsA) ||
-        !make_map(&grads.b, weight, V, d, ld_weight, 64) || !make_map(&grads.a_w, room.g, q.n_pad, q.piece, q.piece, 64) ||
+        !make_map(&probs.out, room.g, g_rows, 64, 64, 32) || !make_map(&grads.a, room.g, g_rows, 64, 64, kRowsA) ||
+        !make_map(&grads.b, weight, V, d, ld_weight, 64) || !make_map(&grads.a_w, room.g, g_rows, 64, 64, 64) ||
         !make_map(&grads.b_w, room.h, q.n_pad, d, d, 64) || (grad_weight && !make_map(&grads.out, grad_weight, V, d, ld_grad_weight, 32)))
         return bad_map();
     GemmParams p{};
-    p.N = N; p.V = V; p.d = d; p.m_room = q.m_room; p.splits = q.splits;
+    p.N = N; p.V = V; p.d = d; p.n_pad = (int32_t)q.n_pad; p.m_room = q.m_room; p.splits = q.splits;
     p.want_h = grad_hidden != nullptr; p.want_w = grad_weight != nullptr;
     p.give_up = g_xent_give_up.load(std::memory_order_relaxed);
     p.n_live = room.n_live; p.target = room.target; p.lse = room.lse; p.coef = room.coef; p.sum_h = room.sum_h; p.failed = room.failed; p.h = room.h; p.rest = room.rest;
