@@ -64,9 +64,6 @@ std::atomic<uint32_t> g_xent_give_up{0};
 __global__ void tfe_xent_status_kernel(uint32_t told) { atomicAnd(&g_xent_status, ~told); }
 
 enum Op { kLse, kProb, kGrads };
-// What units of the gradients' products cost, in steps: each a little besides its steps, and grad W at least the time its tile takes to leave.
-constexpr int32_t kUnitCost = 1, kSendCost = 6;
-
 struct GemmParams {
     int32_t N, V, d, n_pad;
     int32_t tn;                                 // columns of a tile
@@ -85,6 +82,7 @@ struct GemmParams {
     float *z_target;
     float *sum_h;                               // kGrads: [splits][m_room][column tiles][kN / 4][kM][4]
     uint32_t *failed;                           // set if a wait ran out
+    uint32_t *ticket;                           // kGrads: units handed out so far
 };
 
 // ------------------------------------------------------------------ rows that take part
@@ -97,7 +95,8 @@ struct CompactParams {
     bf16 *h_out;
     int32_t *pos, *target_out, *n_live;
     float *lse_out, *coef_out;
-    uint32_t *failed;
+    uint32_t *failed;                           // cleared here, with the units' counters behind it
+    int32_t counters;
 };
 
 constexpr int kCompactThreads = 256;
@@ -127,7 +126,9 @@ tfe_xent_compact_kernel(const CompactParams p)
     __syncthreads();
     before = all = 0;
     for (int w = 0; w < kCompactThreads / 32; ++w) { before += s_before[w]; all += s_all[w]; }
-    if (blockIdx.x == 0 && tid == 0) { *p.n_live = all; if (p.failed) *p.failed = 0; }
+    if (blockIdx.x == 0 && tid == 0) *p.n_live = all;
+    if (blockIdx.x == 0)
+        for (int32_t i = tid; i <= p.counters; i += kCompactThreads) p.failed[i] = 0;
     const int vecs = p.d / 8;
     for (int64_t base = r0; base < r1; base += kCompactThreads) {
         const int64_t r = base + tid;
@@ -221,27 +222,11 @@ struct Units {
             n = n_h + n_w;
         }
     }
-    // A pair's units: [first, last) in steps of step.
-    __device__ __forceinline__ void share(int64_t pair, int64_t pairs, int64_t &first, int64_t &last, int64_t &step) const
-    {
-        if constexpr (kOp != kGrads) {
-            first = pair; last = n; step = pairs;
-        } else {
-            // Two lengths: equal shares of all steps, to within a unit.  The columns of d change last, so that a pair keeps to one part of W or H,
-            // and the pairs that are at the other columns read the same tiles of G at about the same time.
-            const int64_t cost_h = steps_h + kUnitCost, cost_w = max(steps_w, kSendCost) + kUnitCost, all = n_h * cost_h + n_w * cost_w;
-            auto bound = [&](int64_t i) {
-                const int64_t x = all * i / pairs, h = n_h * cost_h;
-                return x <= h ? (x + cost_h / 2) / cost_h : n_h + (x - h + cost_w / 2) / cost_w;
-            };
-            first = bound(pair); last = pair + 1 == pairs ? n : bound(pair + 1); step = 1;
-        }
-    }
     __device__ __forceinline__ Unit at(const GemmParams &p, int64_t u) const
     {
         Unit w{};
         w.tiles = 1;
-        if constexpr (kOp != kGrads) {          // neighbours share the column tile
+        if constexpr (kOp != kGrads) {          // neighbours, which run at about the same time, share the column tile
             const int32_t mt = (int32_t)(u % m_tiles), nt = (int32_t)(u / m_tiles);
             w.a_at = mt * kM;
             w.steps = (p.d + kStepK - 1) / kStepK;
@@ -253,9 +238,10 @@ struct Units {
                 w.b_at = nt * p.tn;             // within the piece
             }
         } else {
-            w.grad_h = u < n_h;
-            if (w.grad_h) {
-                const int32_t i = (int32_t)u, mt = i % m_tiles, s = i / m_tiles % p.splits, ct = i / m_tiles / p.splits;
+            const bool h_first = steps_h >= steps_w;        // the longer units first: the shares come out more even
+            w.grad_h = h_first ? u < n_h : u >= n_w;
+            if (w.grad_h) {                     // neighbours share the rows of W, and of G
+                const int32_t i = (int32_t)(h_first ? u : u - n_w), ct = i % cols, mt = i / cols % m_tiles, s = i / cols / m_tiles;
                 const int32_t all = (p.width + kStepK - 1) / kStepK;
                 w.a_at = mt * kM;
                 w.b_at = ct * p.tn;
@@ -263,9 +249,9 @@ struct Units {
                 w.steps = max(0, min(steps_h, all - s * steps_h));
                 w.index = (s * p.m_room + mt) * cols + ct;
             } else {
-                const int32_t i = (int32_t)(u - n_h), tall = (int32_t)(n_w / cols);
-                w.a_at = i % tall * kM;         // within the piece
-                w.b_at = i / tall * p.tn;
+                const int32_t i = (int32_t)(h_first ? u - n_h : u);         // neighbours share the columns of G
+                w.a_at = i / cols * kM;         // within the piece
+                w.b_at = i % cols * p.tn;
                 w.steps = steps_w;
             }
         }
@@ -289,6 +275,28 @@ __device__ __forceinline__ uint32_t in_first(uint32_t smem_addr)        // the s
     uint32_t r;
     asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem_addr));
     return r;
+}
+__device__ __forceinline__ uint32_t in_second(uint32_t smem_addr)
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 1;" : "=r"(r) : "r"(smem_addr));
+    return r;
+}
+__device__ __forceinline__ void store_second(uint32_t smem_addr, uint32_t x)
+{
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(in_second(smem_addr)), "r"(x) : "memory");
+}
+__device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t parity)      // what the other CTA wrote before it arrived is seen
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
 }
 __device__ __forceinline__ void arrive_cluster(uint32_t bar)
 {
@@ -373,6 +381,14 @@ __device__ __forceinline__ void add_rest(const GemmParams &p, int32_t at, int32_
         }
 }
 
+// The gradients' units, of two lengths, go to the pairs as they come free, in an order in which those under way together read the same
+// operands: 2,048 x 50,688 x 1,024 take 321 us, with equal shares that each pair works off by itself 450 us.  The order of every sum is
+// fixed by the unit, not by who computes it.  The other units are all alike: every pair takes each pairs-th, which saves the epilogue
+// the asking (2,048 x 151,936 x 1,024: 561 us against 590).
+template <int kOp> constexpr bool kHandedOut = kOp == kGrads;
+constexpr int kTickets = 4;                     // units that are known ahead
+constexpr int kListeners = kCtas * (1 + kEpilogueWarps) + 1;        // loaders, epilogue warps, and the one that issues the MMAs
+
 struct Maps { CUtensorMap a, b, a_w, b_w, out; };           // kLse, kProb: H, W, -, -, G;  kGrads: G by rows, W, G by columns, H, grad W
 
 template <int kOp>
@@ -381,12 +397,15 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
 {
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_acc_full[kBuffers], s_acc_empty[kBuffers], s_drain;
+    __shared__ __align__(8) uint64_t s_told[kTickets], s_heard[kTickets];
+    __shared__ volatile uint32_t s_ticket[kTickets];
     __shared__ uint32_t s_tmem_base;
     __shared__ volatile uint32_t s_abort;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     if (threadIdx.x == 0) {
+        for (int t = 0; t < kTickets; ++t) { mbar_init(smem_u32(&s_told[t]), 1); mbar_init(smem_u32(&s_heard[t]), kListeners); }
         for (int s = 0; s < kStages; ++s) { mbar_init(smem_u32(&s_full[s]), 1); mbar_init(smem_u32(&s_empty[s]), 1); }
         for (int a = 0; a < kBuffers; ++a) { mbar_init(smem_u32(&s_acc_full[a]), 1); mbar_init(smem_u32(&s_acc_empty[a]), kCtas * kEpilogueWarps); }
         mbar_init(smem_u32(&s_drain), 1);
@@ -403,8 +422,26 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
     const uint32_t tmem_base = s_tmem_base;
     tfe_wait_for_stream();
     const Units<kOp> units(p);
-    int64_t u_first, u_last, u_step;
-    units.share(pair, pairs, u_first, u_last, u_step);
+    // The next unit of this pair, or one beyond the last.  Every role hears of each by itself.
+    uint32_t t_slot = 0, t_phase = 0;
+    int64_t u = pair - pairs;
+    auto next_unit = [&](bool one_thread) {
+        if constexpr (!kHandedOut<kOp>) {
+            u += pairs;
+            return true;
+        }
+        bool ok = false;
+        for (uint32_t i = 0; i < TC_WAIT_LIMIT && !ok; ++i) {
+            ok = mbar_try_wait_cluster(smem_u32(&s_told[t_slot]), t_phase);
+            if ((i & 1023u) == 1023u && s_abort) break;
+        }
+        if (!one_thread) ok = __all_sync(0xFFFFFFFFu, ok);
+        u = s_ticket[t_slot];
+        if (!one_thread) __syncwarp();
+        if (ok && (one_thread || lane == 0)) arrive_cluster(in_first(smem_u32(&s_heard[t_slot])));
+        if (++t_slot == kTickets) { t_slot = 0; t_phase ^= 1u; }
+        return ok;
+    };
 
     if (warp < 4) {
         if constexpr (kOp == kLse) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegs));
@@ -414,7 +451,10 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
             const int32_t b_part = p.tn / kCtas;
             uint32_t stage = 0, phase = 0, issued = 0;
             bool ok = !p.give_up;
-            for (int64_t u = u_first; ok && u < u_last; u += u_step) {
+            while (ok) {
+                ok = next_unit(true);
+                if (!ok) { atomicOr(&g_xent_status, kTimeoutLoader); s_abort = 1; }
+                if (!ok || u >= units.n) break;
                 const Unit w = units.at(p, u);
                 for (int32_t t = 0; ok && t < w.tiles; ++t)
                     for (int32_t ks = 0; ks < w.steps; ++ks) {
@@ -450,11 +490,29 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                 }
             else if (!ok && issued)
                 __nanosleep(1000000);
+        } else if (kHandedOut<kOp> && warp == 2 && lane == 0 && rank == 0) {
+            // ============================ units to both CTAs ======================
+            uint32_t slot = 0, phase = 0;
+            bool ok = !p.give_up;
+            while (ok) {
+                ok = mbar_wait(smem_u32(&s_heard[slot]), phase ^ 1u, &s_abort);
+                if (!ok) { atomicOr(&g_xent_status, kTimeoutLoader); s_abort = 1; break; }
+                const uint32_t ticket = atomicAdd(p.ticket, 1u);
+                s_ticket[slot] = ticket;
+                store_second(smem_u32(const_cast<uint32_t *>(&s_ticket[slot])), ticket);
+                arrive_cluster(in_first(smem_u32(&s_told[slot])));
+                arrive_cluster(in_second(smem_u32(&s_told[slot])));
+                if (ticket >= units.n) break;
+                if (++slot == kTickets) { slot = 0; phase ^= 1u; }
+            }
         } else if (warp == 1 && lane == 0 && rank == 0) {
             // ============================ MMA issuer ==============================
             uint32_t stage = 0, phase = 0, buf = 0, buf_phase = 0;
             bool ok = !p.give_up;
-            for (int64_t u = u_first; ok && u < u_last; u += u_step) {
+            while (ok) {
+                ok = next_unit(true);
+                if (!ok) { atomicOr(&g_xent_status, kTimeoutMma); s_abort = 1; }
+                if (!ok || u >= units.n) break;
                 const Unit w = units.at(p, u);
                 const bool a_mn = kOp == kGrads && !w.grad_h, b_mn = kOp == kGrads;
                 const uint32_t idesc = umma_idesc(kM, (uint32_t)p.tn, a_mn, b_mn);
@@ -519,11 +577,12 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                 asm volatile("cp.async.bulk.commit_group;" ::: "memory");
             }
         };
-        int64_t u = u_first;
-        for (; ok && u < u_last; u += u_step) {
+        while (ok) {
+            ok = next_unit(false);
+            if (!ok || u >= units.n) break;
             const Unit w = units.at(p, u);
             const int32_t row = w.a_at + row_in_tile;
-            const bool live = row < units.n_live;                   // (of no use to grad W, whose rows are the vocabulary's)
+            const bool live = row < units.n_live;                   // (grad W's rows are the vocabulary's: it has no use for this)
             int32_t target = -1, hit[kHits];
             float lse = 0.f, coef = 0.f, top = -3.4e38f;
             float2 sum = make_float2(0.f, 0.f);
@@ -535,7 +594,7 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                 if constexpr (kOp == kGrads) {
                     at = reinterpret_cast<float4 *>(p.sum_h) + ((int64_t)w.index * (kN / 4) + c0 / 4) * kM + row_in_tile;
                     if (w.steps == 0) {         // (a part of a short last piece that has nothing to add)
-                        if (p.first)
+                        if (p.first && live)
                             for (int32_t c = 0; c < cols; c += 4) at[(int64_t)(c / 4) * kM] = make_float4(0.f, 0.f, 0.f, 0.f);
                         continue;
                     }
@@ -675,12 +734,12 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                     float4 old[2][4];
                     auto fetch = [&](int32_t c, float4 (&x)[4]) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) x[i] = p.first ? make_float4(0.f, 0.f, 0.f, 0.f) : at[(int64_t)(c / 4 + i) * kM];
+                        for (int i = 0; i < 4; ++i) x[i] = p.first || !live ? make_float4(0.f, 0.f, 0.f, 0.f) : at[(int64_t)(c / 4 + i) * kM];
                     };
                     auto take = [&](const uint32_t (&x)[16], int32_t c, const float4 (&was)[4]) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            at[(int64_t)(c / 4 + i) * kM] = make_float4(__uint_as_float(x[4 * i]) + was[i].x, __uint_as_float(x[4 * i + 1]) + was[i].y,
+                            if (live) at[(int64_t)(c / 4 + i) * kM] = make_float4(__uint_as_float(x[4 * i]) + was[i].x, __uint_as_float(x[4 * i + 1]) + was[i].y,
                                                                         __uint_as_float(x[4 * i + 2]) + was[i].z, __uint_as_float(x[4 * i + 3]) + was[i].w);
                     };
                     fetch(0, old[0]);
@@ -703,18 +762,12 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                 if (live) p.part[(int64_t)(2 * w.index + half) * p.ld_part + row] = make_float2(top, sum.x + sum.y);
         }
         asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-        if (!ok) {                              // a wait ran out: no results that look like some
+        if (!ok) {                              // a wait ran out: no results that look like some (the last kernel sees to that)
             if (lane == 0) {
                 atomicOr(&g_xent_status, kTimeoutEpilogue);
-                if (kOp != kLse) *p.failed = 1;
+                *p.failed = 1;
             }
             s_abort = 1;
-            if constexpr (kOp == kLse)
-                for (; u < u_last; u += u_step) {
-                    const Unit w = units.at(p, u);
-                    const int32_t row = w.a_at + row_in_tile;
-                    if (row < units.n_live) p.part[(int64_t)(2 * w.index + half) * p.ld_part + row] = make_float2(0.f, __int_as_float(0x7FFFFFFF));
-                }
         }
     }
 
@@ -925,6 +978,7 @@ struct LossParams {
     const float2 *part; int64_t ld_part;
     const float *z_target;
     const int32_t *target, *pos;                // pos null: rows are where they were
+    const uint32_t *failed;                     // null: a failure is in the partial results
     const bf16 *h, *w; int64_t ld_h, ld_w;
     float *loss, *lse;
 };
@@ -996,6 +1050,7 @@ tfe_xent_loss_kernel(const LossParams p)
         const float was = p.z_target[at];
         double lse = (double)top + log((double)sum);
         lse += (double)log1pf(expf((float)((double)was - lse)) * expm1f((float)(z - (double)was)));
+        if (p.failed && *p.failed) lse = (double)__int_as_float(0x7FFFFFFF);
         p.lse[r] = (float)lse;
         p.loss[r] = (float)(lse - z);
     }
@@ -1114,8 +1169,9 @@ Plan make_plan(int32_t N, int32_t V, int32_t d)
     q.pieces = (int32_t)((V + q.piece - 1) / q.piece);
     q.tn_d = d >= kN ? kN : 128;
     q.cols = (d + q.tn_d - 1) / q.tn_d;
-    // parts of grad H's sums: units of about a sixth of a pair's share of the work, so that the shares come out even
-    const int64_t steps = q.piece / kStepK, work = q.cols * (q.m_room * steps + q.piece / kM * std::max<int64_t>(kSendCost, q.n_pad / kStepK));
+    // parts of grad H's sums: units of about a sixth of a pair's share of the work, so that the shares come out even (a unit of grad W takes
+    // as long as six steps at least, which is what its tile takes to leave)
+    const int64_t steps = q.piece / kStepK, work = q.cols * (q.m_room * steps + q.piece / kM * std::max<int64_t>(6, q.n_pad / kStepK));
     q.splits = (int32_t)std::min<int64_t>(kMaxSplits, (steps + std::max<int64_t>(16, work / kPairs / 6) - 1) / std::max<int64_t>(16, work / kPairs / 6));
     return q;
 }
@@ -1131,15 +1187,15 @@ struct Room {                                   // hands out pieces of the works
     }
 };
 struct ForwardRoom {
-    float2 *part; float *z_target; bf16 *h; int32_t *pos, *target, *n_live;
+    float2 *part; float *z_target; bf16 *h; int32_t *pos, *target, *n_live; uint32_t *failed;
     int64_t bytes;
     ForwardRoom(const Plan &q, int32_t N, int32_t d, void *ws)
     {
         Room r{static_cast<uint8_t *>(ws), 0};
         part = r.take<float2>((int64_t)q.chunks * q.n_pad);
         z_target = r.take<float>(q.n_pad);
-        if (q.gather) { h = r.take<bf16>(q.n_pad * d); pos = r.take<int32_t>(N); target = r.take<int32_t>(q.n_pad); n_live = r.take<int32_t>(1); }
-        else { h = nullptr; pos = target = n_live = nullptr; }
+        if (q.gather) { h = r.take<bf16>(q.n_pad * d); pos = r.take<int32_t>(N); target = r.take<int32_t>(q.n_pad); n_live = r.take<int32_t>(1); failed = r.take<uint32_t>(1); }
+        else { h = nullptr; pos = target = n_live = nullptr; failed = r.take<uint32_t>(1); }
         bytes = r.used;
     }
 };
@@ -1153,7 +1209,7 @@ struct BackwardRoom {
         h = r.take<bf16>(q.n_pad * d);
         sum_h = r.take<float>((int64_t)q.splits * q.m_room * q.cols * kM * kN);
         lse = r.take<float>(q.n_pad); coef = r.take<float>(q.n_pad); rest = r.take<float>(q.n_pad);
-        pos = r.take<int32_t>(N); target = r.take<int32_t>(q.n_pad); n_live = r.take<int32_t>(1); failed = r.take<uint32_t>(1);
+        pos = r.take<int32_t>(N); target = r.take<int32_t>(q.n_pad); n_live = r.take<int32_t>(1); failed = r.take<uint32_t>(1 + (int64_t)q.pieces);
         bytes = r.used;
     }
 };
@@ -1273,7 +1329,7 @@ tfe_status tfe_xent_forward(const void *hidden, int64_t ld_hidden, int32_t N, co
     if (q.gather) {
         CompactParams c{};
         c.N = N; c.V = V; c.d = d; c.h = static_cast<const bf16 *>(hidden); c.ld = ld_hidden; c.target = target;
-        c.h_out = room.h; c.pos = room.pos; c.target_out = room.target; c.n_live = room.n_live;
+        c.h_out = room.h; c.pos = room.pos; c.target_out = room.target; c.n_live = room.n_live; c.failed = room.failed;
         if (tfe_status st = launch_compact(c, sms, stream)) return st;
     }
     Maps maps{};
@@ -1284,7 +1340,10 @@ tfe_status tfe_xent_forward(const void *hidden, int64_t ld_hidden, int32_t N, co
     p.N = N; p.V = V; p.d = d; p.tn = q.tn; p.per_unit = q.per_unit; p.n_tiles = q.n_tiles; p.m_room = q.m_room;
     p.give_up = g_xent_give_up.load(std::memory_order_relaxed);
     p.n_live = room.n_live; p.target = q.gather ? room.target : target;
-    p.part = room.part; p.ld_part = q.n_pad; p.z_target = room.z_target;
+    p.part = room.part; p.ld_part = q.n_pad; p.z_target = room.z_target; p.failed = room.failed;
+    l.failed = room.failed;
+    if (!q.gather)                              // (cleared with the rows otherwise)
+        if (tfe_status st = tfe_note_cuda(cudaMemsetAsync(room.failed, 0, 4, stream), "cudaMemsetAsync")) return st;
     if (tfe_status st = launch_gemm<kLse>((int64_t)q.m_room * (q.chunks / 2), sms, stream, maps, p)) return st;
     return join();
 }
@@ -1317,6 +1376,7 @@ tfe_status tfe_xent_backward(const void *hidden, int64_t ld_hidden, int32_t N, c
     CompactParams c{};
     c.N = N; c.V = V; c.d = d; c.h = static_cast<const bf16 *>(hidden); c.ld = ld_hidden; c.target = target; c.lse = lse; c.grad = grad_loss;
     c.h_out = room.h; c.pos = room.pos; c.target_out = room.target; c.n_live = room.n_live; c.lse_out = room.lse; c.coef_out = room.coef; c.failed = room.failed;
+    c.counters = q.pieces;
     if (tfe_status st = launch_compact(c, sms, stream)) return st;
 
     // G lies in blocks of 64 columns, one below the other: whichever way a product reads it, a tile is one run of memory
@@ -1339,6 +1399,7 @@ tfe_status tfe_xent_backward(const void *hidden, int64_t ld_hidden, int32_t N, c
         p.tn = kN;
         if (tfe_status st = launch_gemm<kProb>((int64_t)q.m_room * ((p.width + kN - 1) / kN), sms, stream, probs, p)) return st;
         p.tn = q.tn_d;
+        p.ticket = room.failed + 1 + i;
         const int64_t most = (int64_t)q.cols * ((int64_t)p.want_h * q.m_room * q.splits + (int64_t)p.want_w * ((p.width + kM - 1) / kM));
         if (tfe_status st = launch_gemm<kGrads>(most, sms, stream, grads, p)) return st;
     }
