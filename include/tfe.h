@@ -638,10 +638,12 @@ tfe_status tfe_distill_backward(const void *logits, int32_t dtype, int32_t N, in
  *                    type; a G of its own error 2^-9 on average adds as much to a gradient as the gradient's own rounding); sums
  *                    are fp32 and rounded once.
  *   workspace        DEVICE scratch, 256-byte aligned, of at least tfe_xent_*_workspace_bytes(N, V, d) bytes (smaller: TFE_ERR_CAPACITY);
- *                    contents undefined before and after.  It bounds what exists of the logits at a time: a piece of G of 64 MB
- *                    (N <= 8,192; 4,096 columns beyond).
+ *                    contents undefined before and after.  It bounds what exists of the logits at a time: forward some 40 MB of
+ *                    partial results, backward a piece of G of up to 256 MB (4,096 columns where N > 32,768) and sums of as much
+ *                    at most (or 4 N d bytes).
  * NaN propagates, and a logit of +inf makes its row's results NaN.  The order of every sum is fixed by the sizes and the targets.
- * The backward call launches two kernels for each piece of the vocabulary and two more.
+ * Forward two or three launches; backward two for each piece of the vocabulary and
+ * two more.
  *
  * Every wait inside the kernels is bounded.  Should one run out, the loss and lse of the rows concerned, or all gradients, are NaN.
  * tfe_xent_status synchronises `stream`, reads the status word of the current device and clears what it read: 0, or bits set by

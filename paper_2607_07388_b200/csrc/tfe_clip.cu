@@ -25,7 +25,7 @@ namespace {
 using tfe_rows::Elem;
 
 constexpr int kThreads = 256;
-constexpr int64_t kChunk = 8192;                // elements
+constexpr int64_t kChunkMin = 2048, kChunkMax = 16384;        // elements of a chunk: few tensors are spread over the SMs, many read in long runs
 constexpr int kPerSm = 6;                       // blocks, all resident
 constexpr int kBlocks = 148 * kPerSm;           // most blocks of a launch
 
@@ -33,6 +33,7 @@ struct Entry { uint64_t in, out; int64_t n; uint32_t first; int32_t dtype; };   
 template <int kRoom> struct Table {
     int32_t tensors, parts, part0;              // parts: sums of all launches; part0: this launch's first
     uint32_t chunks;
+    int64_t chunk;
     int32_t write_norm, in_place, only_norm;
     float max_norm;
     double *part;
@@ -116,7 +117,7 @@ tfe_grad_norm_kernel(const __grid_constant__ Table<kRoom> t)
         int i = find_tensor(t, c0);
         for (uint32_t c = c0; c < c1; ++c) {
             while (i + 1 < t.tensors && t.at[i + 1].first <= c) ++i;
-            const int64_t from = (int64_t)(c - t.at[i].first) * kChunk, n = min(kChunk, t.at[i].n - from);
+            const int64_t from = (int64_t)(c - t.at[i].first) * t.chunk, n = min(t.chunk, t.at[i].n - from);
             sum += t.at[i].dtype == TFE_DTYPE_BF16 ? chunk_squares(reinterpret_cast<const __nv_bfloat16 *>(t.at[i].in) + from, n)
                                                    : chunk_squares(reinterpret_cast<const float *>(t.at[i].in) + from, n);
         }
@@ -176,7 +177,7 @@ tfe_grad_clip_kernel(const __grid_constant__ Table<kRoom> t)
     int i = find_tensor(t, c1 - 1);
     for (uint32_t c = c1; c-- > c0;) {
         while (t.at[i].first > c) --i;
-        const int64_t from = (int64_t)(c - t.at[i].first) * kChunk, n = min(kChunk, t.at[i].n - from);
+        const int64_t from = (int64_t)(c - t.at[i].first) * t.chunk, n = min(t.chunk, t.at[i].n - from);
         if (t.at[i].dtype == TFE_DTYPE_BF16)
             chunk_scale(reinterpret_cast<const __nv_bfloat16 *>(t.at[i].in) + from, reinterpret_cast<__nv_bfloat16 *>(t.at[i].out) + from, n, by);
         else
@@ -193,6 +194,7 @@ struct Job {
     const int64_t *n; const int32_t *dtype;
     int32_t tensors; bool only_norm;
     float max_norm, *norm; double *part; cudaStream_t stream; int sms;
+    int64_t chunk;
 };
 
 int64_t launches(int32_t tensors) { return std::max<int64_t>(1, ((int64_t)tensors + kLarge - 1) / kLarge); }
@@ -207,10 +209,10 @@ tfe_status run_pass(const Job &j, int pass, int32_t lo, int32_t hi, int32_t *par
     for (int32_t i = lo; i < hi; ++i) {
         if (j.n[i] == 0) continue;
         t.at[t.tensors++] = {j.in[i], j.out ? j.out[i] : j.in[i], j.n[i], (uint32_t)chunks, j.dtype[i]};
-        chunks += (uint64_t)((j.n[i] + kChunk - 1) / kChunk);
+        chunks += (uint64_t)((j.n[i] + j.chunk - 1) / j.chunk);
     }
     if (chunks > 0xFFFFFFFFull) return TFE_ERR_INVALID_ARG;
-    t.chunks = (uint32_t)chunks;
+    t.chunks = (uint32_t)chunks; t.chunk = j.chunk;
     t.parts = parts; t.part0 = *part0; t.part = j.part; t.norm = j.norm; t.max_norm = j.max_norm;
     t.write_norm = first; t.in_place = j.out == nullptr; t.only_norm = j.only_norm;
     const unsigned grid = pass == 1 && j.only_norm ? 1u : (unsigned)std::max<uint64_t>(1, std::min<uint64_t>(chunks, (uint64_t)std::min(kBlocks, kPerSm * j.sms)));
@@ -276,7 +278,10 @@ tfe_status check_and_run(const uint64_t *in, const uint64_t *out, const int64_t 
     int dev = 0, sms = 0;
     if (tfe_status st = tfe_note_cuda(cudaGetDevice(&dev), "cudaGetDevice")) return st;
     if (tfe_status st = tfe_note_cuda(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev), "cudaDeviceGetAttribute")) return st;
-    return run({in, out, numel, dtype, n, only_norm, max_norm, norm, static_cast<double *>(workspace), static_cast<cudaStream_t>(stream), sms});
+    int64_t total = 0, chunk = kChunkMin;
+    for (int32_t i = 0; i < n; ++i) total += numel[i];
+    while (chunk < kChunkMax && total / (chunk * 2) >= 4 * kBlocks) chunk *= 2;
+    return run({in, out, numel, dtype, n, only_norm, max_norm, norm, static_cast<double *>(workspace), static_cast<cudaStream_t>(stream), sms, chunk});
 }
 
 }  // namespace

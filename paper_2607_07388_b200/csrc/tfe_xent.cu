@@ -37,17 +37,12 @@ constexpr int kM = kRowsA * kCtas;              // rows of a tile
 constexpr int kN = 256;                         // columns of a tile at most (MMA N)
 constexpr int kStepK = 64;                      // k of a stage: 128 bytes, one swizzle row
 constexpr uint32_t kBytesA = kRowsA * kStepK * 2, kBytesB = kN / kCtas * kStepK * 2, kStageBytes = kBytesA + kBytesB;
-#ifndef TST
-#define TST 6
-#define TROOM 1
-#endif
-constexpr int kStages = TST;
+constexpr int kStages = 6;
 constexpr int kBuffers = 2;                     // accumulators of kN columns: all of tensor memory
 constexpr int kEpilogueWarps = 8;               // two per lane quarter of tensor memory, half of the tile's columns each
 constexpr int kThreads = 32 * (4 + kEpilogueWarps);
 constexpr uint32_t kRoom = 32 * 128;            // bytes of an epilogue warp's outgoing piece: 32 rows of 64 bf16
-constexpr uint32_t kRooms = TROOM;              // pieces of a warp on their way
-constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kEpilogueWarps * kRooms * kRoom;
+constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kEpilogueWarps * kRoom;
 constexpr float kLog2e = 1.4426950408889634f;
 // The tensor cores cut what they add to a sum in fp32, always towards zero, so a long sum comes out too small: a loss over 1,024 k was off by
 // 6e-7 that way.  A sum of the loss therefore takes at most this many steps, and the epilogue adds those up: 3e-7, whatever d.  (With 4
@@ -78,6 +73,7 @@ struct GemmParams {
     const float *lse, *coef;
     const bf16 *h;                              // kGrads: the rows together, d apart
     float *rest;                                // what rounding took from G at each row's target
+    uint8_t *wanted;                            // [V / 32]: whether one of these 32 ids is a target
     float2 *part; int64_t ld_part;              // kLse: [2 * units per row][ld_part] maxima and sums
     float *z_target;
     float *sum_h;                               // kGrads: [splits][m_room][column tiles][kN / 4][kM][4]
@@ -97,6 +93,7 @@ struct CompactParams {
     float *lse_out, *coef_out;
     uint32_t *failed;                           // cleared here, with the units' counters behind it
     int32_t counters;
+    uint8_t *wanted;                            // cleared here (null: the loss)
 };
 
 constexpr int kCompactThreads = 256;
@@ -163,6 +160,8 @@ tfe_xent_compact_kernel(const CompactParams p)
     for (int64_t i = (int64_t)blockIdx.x * kCompactThreads + tid; i < n_zero; i += (int64_t)gridDim.x * kCompactThreads) dst[i] = make_uint4(0, 0, 0, 0);
     if (blockIdx.x == 0)
         for (int64_t i = all + tid; i < end; i += kCompactThreads) p.target_out[i] = -1;
+    if (p.wanted)
+        for (int64_t i = (int64_t)blockIdx.x * kCompactThreads + tid; i <= p.V >> 5; i += (int64_t)gridDim.x * kCompactThreads) p.wanted[i] = 0;
 }
 
 // ------------------------------------------------------------------ the products
@@ -555,15 +554,12 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
         const uint32_t quarter = (uint32_t)warp & 3u;               // tensor-memory lanes 32 * quarter .. + 31
         const int32_t half = e >> 2, cols = p.tn / 2, c0 = half * cols;     // this warp's columns: a multiple of 16
         const int32_t first_row = (int32_t)(rank * kRowsA + quarter * 32u), row_in_tile = first_row + lane;
-        const uint32_t rooms = smem_base + kStages * kStageBytes + (uint32_t)e * kRooms * kRoom;
-        uint32_t turn = 0;
+        const uint32_t room = smem_base + kStages * kStageBytes + (uint32_t)e * kRoom;
         uint32_t buf = 0, buf_phase = 0;
         bool ok = !p.give_up;
         // 64 finished columns of this warp's rows leave by an asynchronous copy
         auto send = [&](const uint32_t (&out)[32], int32_t x, int32_t y, bool there) {
-            const uint32_t room = rooms + turn * kRoom;
-            turn = (turn + 1) % kRooms;
-            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kRooms - 1) : "memory");     // what was there has left
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");     // what was there has left
             __syncwarp();
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -588,7 +584,8 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
             float2 sum = make_float2(0.f, 0.f);
             if (kOp != kGrads && live) target = p.target[row];
             if (kOp == kProb && live) { lse = p.lse[row]; coef = p.coef[row]; }
-            if (kOp == kGrads && !w.grad_h) find_targets(p, units.n_live, p.v0 + w.a_at + first_row, lane, hit);
+            const int32_t v_first = p.v0 + w.a_at + first_row;      // grad W: this warp's first vocabulary row, a multiple of 32
+            const bool wanted = kOp == kGrads && !w.grad_h && v_first < p.V && p.wanted[v_first >> 5];
             for (int32_t t = 0; t < w.tiles; ++t) {
                 float4 *at = nullptr;                               // grad H's sums of this row, four columns each
                 if constexpr (kOp == kGrads) {
@@ -660,6 +657,8 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                 ok = mbar_wait(smem_u32(&s_acc_full[buf]), buf_phase, &s_abort);
                 if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
                 tc_fence_after();
+                if constexpr (kOp == kGrads)
+                    if (wanted) find_targets(p, units.n_live, v_first, lane, hit);
                 const uint32_t taddr = tmem_base + ((quarter * 32u) << 16) + buf * kN + (uint32_t)c0;
                 auto release = [&] {
                     tc_fence_before();
@@ -689,6 +688,7 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                                 for (int j = 0; j < 16; ++j) z = mine - c == j ? __uint_as_float(x[j]) : z;
                                 const float g = coef * expm1f(z - lse), kept = __bfloat162float(__float2bfloat16_rn(g));
                                 p.rest[row] = g - kept;
+                                p.wanted[target >> 5] = 1;
 #pragma unroll
                                 for (int j = 0; j < 8; ++j) {
                                     y[j].x = mine - c == 2 * j ? kept : y[j].x;
@@ -702,11 +702,12 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                                     y[j].y = c + 2 * j + 1 < left ? y[j].y : 0.f;
                                 }
                         } else {
+                            if (wanted)
 #pragma unroll
-                            for (int i = 0; i < kHits; ++i) {
-                                if (!__any_sync(0xFFFFFFFFu, hit[i] >= 0)) break;
-                                add_rest(p, hit[i], w.b_at + c0 + c, y);
-                            }
+                                for (int i = 0; i < kHits; ++i) {
+                                    if (!__any_sync(0xFFFFFFFFu, hit[i] >= 0)) break;
+                                    add_rest(p, hit[i], w.b_at + c0 + c, y);
+                                }
                         }
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
@@ -1007,6 +1008,20 @@ tfe_xent_loss_kernel(const LossParams p)
         const int32_t t = r < p.N ? p.target[r] : -1;
         return t < 0 || t >= p.V ? -1 : p.pos ? p.pos[r] : r;
     };
+    {
+        const int i = threadIdx.x & (p.rows - 1), step = kLossThreads / p.rows;
+        const int64_t r = r0 + i, at = r < p.N ? p.pos ? p.pos[r] : r : -1;         // (rows without a target have results too, or none)
+        float top = -3.4e38f, sum = 0.f;
+        if (at >= 0) {
+#pragma unroll 4
+            for (int32_t c = threadIdx.x / p.rows; c < p.chunks; c += step) {
+                const float2 x = p.part[(int64_t)c * p.ld_part + at];
+                fold(top, sum, x.x, x.y);
+            }
+        }
+        for (int o = 16; o >= p.rows; o >>= 1) fold(top, sum, __shfl_xor_sync(0xFFFFFFFFu, top, o), __shfl_xor_sync(0xFFFFFFFFu, sum, o));
+        if (lane < p.rows) { s_top[i][warp] = top; s_sum[i][warp] = sum; }
+    }
     for (int i = warp; i < p.rows; i += kWarps) {
         const int64_t r = r0 + i;
         const int32_t t = r < p.N ? p.target[r] : -1;
@@ -1024,20 +1039,6 @@ tfe_xent_loss_kernel(const LossParams p)
         }
         for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xFFFFFFFFu, z, o);
         if (lane == 0) s_z[i] = z;
-    }
-    {
-        const int i = threadIdx.x & (p.rows - 1), step = kLossThreads / p.rows;
-        const int64_t at = place(r0 + i);
-        float top = -3.4e38f, sum = 0.f;
-        if (at >= 0) {
-#pragma unroll 4
-            for (int32_t c = threadIdx.x / p.rows; c < p.chunks; c += step) {
-                const float2 x = p.part[(int64_t)c * p.ld_part + at];
-                fold(top, sum, x.x, x.y);
-            }
-        }
-        for (int o = 16; o >= p.rows; o >>= 1) fold(top, sum, __shfl_xor_sync(0xFFFFFFFFu, top, o), __shfl_xor_sync(0xFFFFFFFFu, sum, o));
-        if (lane < p.rows) { s_top[i][warp] = top; s_sum[i][warp] = sum; }
     }
     __syncthreads();
     for (int i = warp; i < p.rows; i += kWarps) {
@@ -1085,7 +1086,7 @@ tfe_xent_rows_kernel(const RowsParams p)
             if (at >= 0 && c < p.d) {
                 const float4 *from = reinterpret_cast<const float4 *>(p.sum_h) + (((int64_t)(at / kM) * p.cols + c / p.tn) * (kN / 4) + c % p.tn / 4) * kM + at % kM;
                 const int64_t step = (int64_t)p.m_room * p.cols * (kN / 4) * kM;
-#pragma unroll 4
+#pragma unroll 8
                 for (int32_t s = 0; s < p.splits; ++s) {
                     const float4 x = from[s * step];
                     sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
@@ -1143,10 +1144,8 @@ struct Plan {
     bool few, gather;
 };
 constexpr int64_t kUnits = 8192;                // units of the loss beyond which tiles are joined: bounds the partial results
-#ifndef TPIECE
-#define TPIECE 128
-#endif
-constexpr int64_t kPieceElements = TPIECE << 20;    // of G: 64 MB stay in L2 until both products have read them
+constexpr int64_t kPieceElements = 128 << 20;   // of G: 256 MB; a boundary between pieces costs some 30 us (4,096 rows: 3,430 us with 128 MB, 3,195 with 512)
+constexpr int64_t kSumElements = 64 << 20;      // of all parts of grad H's sums together: 256 MB
 constexpr int64_t kMaxSplits = 64, kPairs = 74; // kPairs: of the device that the sizes are meant for
 constexpr int64_t kPieceMin = 4096;             // columns of a piece at least
 
@@ -1172,7 +1171,8 @@ Plan make_plan(int32_t N, int32_t V, int32_t d)
     // parts of grad H's sums: units of about a sixth of a pair's share of the work, so that the shares come out even (a unit of grad W takes
     // as long as six steps at least, which is what its tile takes to leave)
     const int64_t steps = q.piece / kStepK, work = q.cols * (q.m_room * steps + q.piece / kM * std::max<int64_t>(6, q.n_pad / kStepK));
-    q.splits = (int32_t)std::min<int64_t>(kMaxSplits, (steps + std::max<int64_t>(16, work / kPairs / 6) - 1) / std::max<int64_t>(16, work / kPairs / 6));
+    const int64_t most_splits = std::min<int64_t>(kMaxSplits, std::max<int64_t>(1, kSumElements / ((int64_t)q.m_room * q.cols * kM * kN)));
+    q.splits = (int32_t)std::min<int64_t>(most_splits, (steps + std::max<int64_t>(16, work / kPairs / 6) - 1) / std::max<int64_t>(16, work / kPairs / 6));
     return q;
 }
 
@@ -1200,9 +1200,9 @@ struct ForwardRoom {
     }
 };
 struct BackwardRoom {
-    bf16 *g, *h; float *sum_h, *lse, *coef, *rest; int32_t *pos, *target, *n_live; uint32_t *failed;
+    bf16 *g, *h; float *sum_h, *lse, *coef, *rest; int32_t *pos, *target, *n_live; uint32_t *failed; uint8_t *wanted;
     int64_t bytes;
-    BackwardRoom(const Plan &q, int32_t N, int32_t d, void *ws)
+    BackwardRoom(const Plan &q, int32_t N, int32_t V, int32_t d, void *ws)
     {
         Room r{static_cast<uint8_t *>(ws), 0};
         g = r.take<bf16>(q.n_pad * q.piece);
@@ -1210,6 +1210,7 @@ struct BackwardRoom {
         sum_h = r.take<float>((int64_t)q.splits * q.m_room * q.cols * kM * kN);
         lse = r.take<float>(q.n_pad); coef = r.take<float>(q.n_pad); rest = r.take<float>(q.n_pad);
         pos = r.take<int32_t>(N); target = r.take<int32_t>(q.n_pad); n_live = r.take<int32_t>(1); failed = r.take<uint32_t>(1 + (int64_t)q.pieces);
+        wanted = r.take<uint8_t>((V >> 5) + 1);
         bytes = r.used;
     }
 };
@@ -1278,7 +1279,7 @@ int64_t tfe_xent_forward_workspace_bytes(int32_t N, int32_t V, int32_t d)
 int64_t tfe_xent_backward_workspace_bytes(int32_t N, int32_t V, int32_t d)
 {
     if (!sizes_ok(N, V, d)) return -1;
-    return N == 0 ? 0 : BackwardRoom(make_plan(N, V, d), N, d, nullptr).bytes;
+    return N == 0 ? 0 : BackwardRoom(make_plan(N, V, d), N, V, d, nullptr).bytes;
 }
 
 tfe_status tfe_xent_forward(const void *hidden, int64_t ld_hidden, int32_t N, const void *weight, int64_t ld_weight, int32_t V, int32_t d,
@@ -1363,7 +1364,7 @@ tfe_status tfe_xent_backward(const void *hidden, int64_t ld_hidden, int32_t N, c
         !aligned(workspace, 256) || (grad_hidden && !rows_ok(grad_hidden, ld_grad_hidden, d)))
         return TFE_ERR_INVALID_ARG;
     const Plan q = make_plan(N, V, d);
-    const BackwardRoom room(q, N, d, workspace);
+    const BackwardRoom room(q, N, V, d, workspace);
     if (workspace_bytes < room.bytes) return TFE_ERR_CAPACITY;
     const int64_t b_h = ((int64_t)(N - 1) * ld_hidden + d) * 2, b_w = ((int64_t)(V - 1) * ld_weight + d) * 2;
     const int64_t b_gh = ((int64_t)(N - 1) * ld_grad_hidden + d) * 2, b_gw = ((int64_t)(V - 1) * ld_grad_weight + d) * 2;
@@ -1376,7 +1377,7 @@ tfe_status tfe_xent_backward(const void *hidden, int64_t ld_hidden, int32_t N, c
     CompactParams c{};
     c.N = N; c.V = V; c.d = d; c.h = static_cast<const bf16 *>(hidden); c.ld = ld_hidden; c.target = target; c.lse = lse; c.grad = grad_loss;
     c.h_out = room.h; c.pos = room.pos; c.target_out = room.target; c.n_live = room.n_live; c.lse_out = room.lse; c.coef_out = room.coef; c.failed = room.failed;
-    c.counters = q.pieces;
+    c.counters = q.pieces; c.wanted = room.wanted;
     if (tfe_status st = launch_compact(c, sms, stream)) return st;
 
     // G lies in blocks of 64 columns, one below the other: whichever way a product reads it, a tile is one run of memory
@@ -1391,7 +1392,7 @@ tfe_status tfe_xent_backward(const void *hidden, int64_t ld_hidden, int32_t N, c
     p.N = N; p.V = V; p.d = d; p.n_pad = (int32_t)q.n_pad; p.m_room = q.m_room; p.splits = q.splits;
     p.want_h = grad_hidden != nullptr; p.want_w = grad_weight != nullptr;
     p.give_up = g_xent_give_up.load(std::memory_order_relaxed);
-    p.n_live = room.n_live; p.target = room.target; p.lse = room.lse; p.coef = room.coef; p.sum_h = room.sum_h; p.failed = room.failed; p.h = room.h; p.rest = room.rest;
+    p.n_live = room.n_live; p.target = room.target; p.lse = room.lse; p.coef = room.coef; p.sum_h = room.sum_h; p.failed = room.failed; p.h = room.h; p.rest = room.rest; p.wanted = room.wanted;
     for (int32_t i = 0; i < q.pieces; ++i) {
         p.v0 = (int32_t)(i * q.piece);
         p.width = (int32_t)std::min<int64_t>(q.piece, V - (int64_t)i * q.piece);

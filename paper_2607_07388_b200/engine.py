@@ -696,12 +696,12 @@ def _normed_inject_backward(grad_out, grad_normed, h, m, post_weight, next_weigh
         arrived += [x.data_ptr(), ld]
     gh = h.new_empty(n, d) if want[0] else None
     gm = h.new_empty(n, d) if want[1] else None
-    gp = torch.empty_like(post_weight) if want[2] else None
-    gx = torch.empty_like(next_weight) if want[3] else None
+    gp = post_weight.new_empty(d) if want[2] else None
+    gx = next_weight.new_empty(d) if want[3] else None
     gg = None if gate is None or not want[4] else gate.new_empty(gate.shape)
     sums = gp is not None or gx is not None
     size = tfe.tfe_inject_norm_workspace_bytes(n, d) if sums else 0
-    workspace = torch.empty(size, dtype=torch.uint8, device=h.device) if sums else None
+    workspace = h.new_empty(size // h.element_size()) if sums else None
     at = [None if x is None else x.data_ptr() for x in (gh, gm, gg, gp, gx, workspace)]
     grads = tfe.TfeInjectNormGrads(arrived[0], arrived[2], arrived[1], arrived[3], at[0], at[1], at[2], d, d, d, at[3], at[4])
     tfe.tfe_inject_norm_backward(params, grads, at[5], size, _where(h.device, stream))
@@ -746,7 +746,8 @@ def _gradients(tensors, what):
     tensors = [tensors] if torch.is_tensor(tensors) else list(tensors)
     if not 1 <= len(tensors) <= tfe.CLIP_MAX_TENSORS:
         raise ValueError(f"{what}: one tensor at least and {tfe.CLIP_MAX_TENSORS} at most")
-    kinds = list(map(_ROW_DTYPES.get, map(_dtype_of, tensors)))
+    types = set(map(_dtype_of, tensors))
+    kinds = [_ROW_DTYPES.get(types.pop())] * len(tensors) if len(types) == 1 else list(map(_ROW_DTYPES.get, map(_dtype_of, tensors)))
     devices = set(map(_device_of, tensors))
     if None in kinds or len(devices) != 1 or -1 in devices:
         raise ValueError(f"{what}: bf16 or fp32 CUDA tensors on one device are needed")
@@ -791,5 +792,8 @@ def _clip_here(lists, max_norm, out, stream):
         tfe.tfe_grad_norm(at, numel, kinds, n, norm.data_ptr(), workspace.data_ptr(), size, _where(dev, stream))
         return norm
     tfe.tfe_clip_grad_norm(at, made_at, numel, kinds, n, max_norm, norm.data_ptr(), workspace.data_ptr(), size, _where(dev, stream))
-    torch.autograd.graph.increment_version([x for x in made if not x.is_inference()])
+    try:
+        torch.autograd.graph.increment_version(made)
+    except RuntimeError:                # inference tensors, which have no version, among them
+        torch.autograd.graph.increment_version([x for x in made if not x.is_inference()])
     return norm
