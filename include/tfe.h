@@ -719,9 +719,9 @@ tfe_status tfe_inject_norm_backward(const tfe_inject_norm_params *params, const 
  *   results          HOST array of n DEVICE addresses of the same sizes and types, or NULL: in place.  A result may be its own tensor;
  *                    otherwise nothing that is written may touch anything else.  In place, nothing is written where norm <= max_norm.
  *   max_norm         >= 0 (+inf: clips nothing).
- *   norm             DEVICE float: the norm before clipping.  Squares are summed in fp32 by fours or eights, those sums in fp64; no
- *                    element is too large or too small.  Where it is not finite (an element was not, or it is beyond fp64) the
- *                    elements stay as they are.
+ *   norm             DEVICE float: the norm before clipping.  Squares are summed in fp32 by fours or eights, those sums in fp64, and
+ *                    squares beyond fp32's range are formed in fp64.  Where it is not finite (an element was not, or it is beyond
+ *                    fp32) the elements stay as they are.
  *   workspace        DEVICE scratch, 8-byte aligned, of tfe_clip_workspace_bytes(n) bytes (smaller: TFE_ERR_CAPACITY), contents
  *                    undefined before and after.
  * Each result is rounded once; the order of the sums depends on the sizes alone.  The lists are read before the calls return.  Two

@@ -169,8 +169,8 @@ tfe_grad_clip_kernel(const __grid_constant__ Table<kRoom> t)
     const double norm = sqrt(block_sum(sum, s_warp));
     if (t.write_norm && blockIdx.x == 0 && threadIdx.x == 0) *t.norm = (float)norm;
     if (t.only_norm) return;
-    // a norm that is not finite scales nothing: the caller sees it
-    const float by = norm > (double)t.max_norm && norm <= 1.7e308 ? (float)((double)t.max_norm / norm) : 1.f;
+    // a norm that is not finite, as the caller sees it, scales nothing
+    const float by = norm > (double)t.max_norm && (float)norm <= 3.402823466e38f ? (float)((double)t.max_norm / norm) : 1.f;
     if (by == 1.f && t.in_place) return;
     const uint32_t c0 = (uint32_t)((uint64_t)t.chunks * blockIdx.x / gridDim.x), c1 = (uint32_t)((uint64_t)t.chunks * (blockIdx.x + 1) / gridDim.x);
     if (c0 >= c1) return;
