@@ -610,7 +610,9 @@ class _LinearCrossEntropy(torch.autograd.Function):
 
 def linear_cross_entropy(hidden: torch.Tensor, weight: torch.Tensor, target: torch.Tensor) -> torch.Tensor:
     """xent_forward's loss [N] as a node of autograd: gradients go to `hidden` and `weight`.  Reduce it as the training wants, e.g.
-    ``linear_cross_entropy(h, w, t).sum() / (t >= 0).sum()``."""
+    ``linear_cross_entropy(h, w, t).sum() / (t >= 0).sum()``.  A step that is captured into a CUDA graph takes its gradients with
+    torch.autograd.grad (or xent_backward): .backward() adds to the leaves on the stream on which an eager graph of them was made,
+    if one is still alive, and a capture does not allow that."""
     return _LinearCrossEntropy.apply(hidden, weight, target)
 
 
@@ -729,7 +731,7 @@ class _NormedInject(torch.autograd.Function):
 def normed_inject(h: torch.Tensor, m: torch.Tensor, post_weight: torch.Tensor, next_weight: torch.Tensor,
                   gate: torch.Tensor | None = None, *, sigmoid: bool = False, lam: float = 1.0, eps: float = 1e-6):
     """normed_inject_forward's (out, normed) as a node of autograd: gradients go to the hidden states, the memory vectors, both
-    weights and the gate."""
+    weights and the gate.  (For a captured step see linear_cross_entropy.)"""
     return _NormedInject.apply(h, m, post_weight, next_weight, gate, sigmoid, lam, eps)
 
 
