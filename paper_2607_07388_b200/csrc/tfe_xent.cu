@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(kCompactThreads)
 tfe_xent_compact_kernel(const CompactParams p)
 {
     __shared__ int32_t s_before[kCompactThreads / 32], s_all[kCompactThreads / 32];
-    __shared__ int32_t s_pos[kCompactThreads];
+    __shared__ int32_t s_from[kCompactThreads];
     tfe_wait_for_stream();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int64_t r0 = (int64_t)blockIdx.x * p.rows_per_block, r1 = min((int64_t)p.N, r0 + p.rows_per_block);
@@ -112,6 +112,7 @@ tfe_xent_compact_kernel(const CompactParams p)
     };
     // how many before this block's rows, and in all (every block counts for itself: the targets are a few KB in L2)
     int32_t before = 0, all = 0;
+#pragma unroll 8
     for (int64_t r = tid; r < p.N; r += kCompactThreads) {
         const int32_t one = live(r);
         all += one;
@@ -138,18 +139,16 @@ tfe_xent_compact_kernel(const CompactParams p)
         for (int w = 0; w < kCompactThreads / 32; ++w) { at += w < warp ? s_before[w] : 0; total += s_before[w]; }
         at += __popc(vote & ((1u << lane) - 1u));
         if (r < r1) p.pos[r] = one ? at : -1;
-        s_pos[tid] = one ? at : -1;
         if (one) {
+            s_from[at - before] = tid;
             p.target_out[at] = p.target[r];
             if (p.grad) { p.lse_out[at] = p.lse[r]; p.coef_out[at] = p.grad[r]; }
         }
         __syncthreads();
-        for (int i = warp; i < kCompactThreads && base + i < r1; i += kCompactThreads / 32) {
-            const int32_t to = s_pos[i];
-            if (to < 0) continue;
-            const uint4 *src = reinterpret_cast<const uint4 *>(p.h + (base + i) * p.ld);
-            uint4 *dst = reinterpret_cast<uint4 *>(p.h_out + (int64_t)to * p.d);
-            for (int v = lane; v < vecs; v += 32) dst[v] = tfe_rows::load_stream(src + v);
+#pragma unroll 4
+        for (int32_t i = tid; i < total * vecs; i += kCompactThreads) {        // whose row it is does not matter: all loads at once
+            const int32_t k = i / vecs, v = i - k * vecs;
+            reinterpret_cast<uint4 *>(p.h_out + (int64_t)(before + k) * p.d)[v] = __ldg(reinterpret_cast<const uint4 *>(p.h + (base + s_from[k]) * p.ld) + v);
         }
         before += total;
     }
@@ -346,9 +345,12 @@ __device__ __forceinline__ void find_targets(const GemmParams &p, int32_t n_live
 {
 #pragma unroll
     for (int i = 0; i < kHits; ++i) hit[i] = -1;
-    for (int32_t base = 0; base < n_live; base += 128) {            // (targets beyond the last row are -1)
+    uint32_t seek = 0xFFFFFFFFu;                // the ids that may have more rows
+    if (p.V - v0 < 32) seek = (1u << (p.V - v0)) - 1u;
+    for (int32_t base = 0; base < n_live && seek; base += 128) {    // (targets beyond the last row are -1)
         const int4 t = *reinterpret_cast<const int4 *>(p.target + base + 4 * lane);
-        const bool any = (uint32_t)(t.x - v0) < 32u || (uint32_t)(t.y - v0) < 32u || (uint32_t)(t.z - v0) < 32u || (uint32_t)(t.w - v0) < 32u;
+        auto sought = [&](int32_t id) { return (uint32_t)(id - v0) < 32u && (seek >> (id - v0) & 1u); };
+        const bool any = sought(t.x) || sought(t.y) || sought(t.z) || sought(t.w);
         for (uint32_t from = __ballot_sync(0xFFFFFFFFu, any); from; from &= from - 1) {
             const int l = __ffs(from) - 1;
             const int32_t four[4] = {__shfl_sync(0xFFFFFFFFu, t.x, l), __shfl_sync(0xFFFFFFFFu, t.y, l), __shfl_sync(0xFFFFFFFFu, t.z, l), __shfl_sync(0xFFFFFFFFu, t.w, l)};
@@ -361,7 +363,7 @@ __device__ __forceinline__ void find_targets(const GemmParams &p, int32_t n_live
                         if (hit[i] < 0) { hit[i] = at; at = -1; }
                 }
         }
-        if (__all_sync(0xFFFFFFFFu, hit[kHits - 1] >= 0)) break;
+        seek &= ~__ballot_sync(0xFFFFFFFFu, hit[kHits - 1] >= 0);
     }
 }
 // 16 columns from `col` of row `at`'s hidden state, times what is left of its G, to y
@@ -382,9 +384,10 @@ __device__ __forceinline__ void add_rest(const GemmParams &p, int32_t at, int32_
 
 // The gradients' units, of two lengths, go to the pairs as they come free, in an order in which those under way together read the same
 // operands: 2,048 x 50,688 x 1,024 take 321 us, with equal shares that each pair works off by itself 450 us.  The order of every sum is
-// fixed by the unit, not by who computes it.  The other units are all alike: every pair takes each pairs-th, which saves the epilogue
-// the asking (2,048 x 151,936 x 1,024: 561 us against 590).
-template <int kOp> constexpr bool kHandedOut = kOp == kGrads;
+// fixed by the unit, not by who computes it.  The other units are all alike, and short ones of the gradients' cost less than the asking:
+// there every pair takes each pairs-th (the loss of 2,048 x 151,936 x 1,024: 561 us against 590; gradients of 256 rows, 4 steps a unit
+// of grad W: 201 against 221).
+constexpr int32_t kShort = 16;                  // steps of a unit of grad W
 constexpr int kTickets = 4;                     // units that are known ahead
 constexpr int kListeners = kCtas * (1 + kEpilogueWarps) + 1;        // loaders, epilogue warps, and the one that issues the MMAs
 
@@ -422,10 +425,11 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
     tfe_wait_for_stream();
     const Units<kOp> units(p);
     // The next unit of this pair, or one beyond the last.  Every role hears of each by itself.
+    const bool handed_out = kOp == kGrads && units.steps_w >= kShort;
     uint32_t t_slot = 0, t_phase = 0;
     int64_t u = pair - pairs;
     auto next_unit = [&](bool one_thread) {
-        if constexpr (!kHandedOut<kOp>) {
+        if (!handed_out) {
             u += pairs;
             return true;
         }
@@ -489,7 +493,7 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                 }
             else if (!ok && issued)
                 __nanosleep(1000000);
-        } else if (kHandedOut<kOp> && warp == 2 && lane == 0 && rank == 0) {
+        } else if (handed_out && warp == 2 && lane == 0 && rank == 0) {
             // ============================ units to both CTAs ======================
             uint32_t slot = 0, phase = 0;
             bool ok = !p.give_up;
@@ -1256,7 +1260,7 @@ tfe_status launch_gemm(int64_t most_units, int sms, cudaStream_t stream, const M
 tfe_status launch_compact(CompactParams c, int sms, cudaStream_t stream)
 {
     c.rows_per_block = (int32_t)std::max<int64_t>(8, (c.N + 2ll * sms - 1) / (2ll * sms));
-    const unsigned grid = (unsigned)(((int64_t)c.N + c.rows_per_block - 1) / c.rows_per_block);
+    const unsigned grid = (unsigned)std::max<int64_t>(64, ((int64_t)c.N + c.rows_per_block - 1) / c.rows_per_block);     // (few rows: zeros to write)
     return tfe_launch_serial(tfe_xent_compact_kernel, grid, kCompactThreads, 1, 0, stream, "cross entropy rows launch", c);
 }
 
