@@ -296,6 +296,14 @@ __device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t par
         : "memory");
     return ok != 0;
 }
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile uint32_t *abort_flag)         // bounded, as mbar_wait
+{
+    for (uint32_t i = 0; i < TC_WAIT_LIMIT; ++i) {
+        if (mbar_try_wait_cluster(bar, parity)) return true;
+        if ((i & 1023u) == 1023u && *abort_flag) return false;
+    }
+    return false;
+}
 __device__ __forceinline__ void arrive_cluster(uint32_t bar)
 {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
@@ -433,11 +441,7 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
             u += pairs;
             return true;
         }
-        bool ok = false;
-        for (uint32_t i = 0; i < TC_WAIT_LIMIT && !ok; ++i) {
-            ok = mbar_try_wait_cluster(smem_u32(&s_told[t_slot]), t_phase);
-            if ((i & 1023u) == 1023u && s_abort) break;
-        }
+        bool ok = mbar_wait_cluster(smem_u32(&s_told[t_slot]), t_phase, &s_abort);
         if (!one_thread) ok = __all_sync(0xFFFFFFFFu, ok);
         u = s_ticket[t_slot];
         if (!one_thread) __syncwarp();
@@ -498,7 +502,7 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
             uint32_t slot = 0, phase = 0;
             bool ok = !p.give_up;
             while (ok) {
-                ok = mbar_wait(smem_u32(&s_heard[slot]), phase ^ 1u, &s_abort);
+                ok = mbar_wait_cluster(smem_u32(&s_heard[slot]), phase ^ 1u, &s_abort);
                 if (!ok) { atomicOr(&g_xent_status, kTimeoutLoader); s_abort = 1; break; }
                 const uint32_t ticket = atomicAdd(p.ticket, 1u);
                 s_ticket[slot] = ticket;
@@ -524,7 +528,7 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                 const int32_t span = kOp == kLse ? kSumSteps : w.steps;         // steps of a sum
                 for (int32_t t = 0; ok && t < w.tiles; ++t)
                     for (int32_t k0 = 0; ok && k0 < w.steps; k0 += span) {
-                        ok = mbar_wait(smem_u32(&s_acc_empty[buf]), buf_phase ^ 1u, &s_abort);
+                        ok = mbar_wait_cluster(smem_u32(&s_acc_empty[buf]), buf_phase ^ 1u, &s_abort);
                         for (int32_t ks = k0; ok && ks < min(k0 + span, w.steps); ++ks) {
                             ok = mbar_wait(smem_u32(&s_full[stage]), phase, &s_abort);
                             if (!ok) break;
@@ -699,6 +703,9 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                                     y[j].y = mine - c == 2 * j + 1 ? kept : y[j].y;
                                 }
                             }
+                            if (!live)          // (not 0 times what may be NaN where a weight is infinite)
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) y[j] = make_float2(0.f, 0.f);
                             if (c + 16 > left)
 #pragma unroll
                                 for (int j = 0; j < 8; ++j) {
@@ -1302,6 +1309,8 @@ tfe_status tfe_xent_forward(const void *hidden, int64_t ld_hidden, int32_t N, co
     for (const auto &x : in)
         if (touch(x.at, x.bytes, loss, 4ll * N) || touch(x.at, x.bytes, lse, 4ll * N)) return TFE_ERR_INVALID_ARG;
     if (touch(loss, 4ll * N, lse, 4ll * N)) return TFE_ERR_INVALID_ARG;
+    for (int i = 0; i < 3; ++i)
+        if (touch(in[i].at, in[i].bytes, workspace, room.bytes)) return TFE_ERR_INVALID_ARG;
     int sms = 0;
     if (tfe_status st = device_sms(&sms)) return st;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
@@ -1376,6 +1385,8 @@ tfe_status tfe_xent_backward(const void *hidden, int64_t ld_hidden, int32_t N, c
     for (const auto &x : in)
         if (touch(x.at, x.bytes, grad_hidden, b_gh) || touch(x.at, x.bytes, grad_weight, b_gw)) return TFE_ERR_INVALID_ARG;
     if (touch(grad_hidden, b_gh, grad_weight, b_gw)) return TFE_ERR_INVALID_ARG;
+    for (int i = 0; i < 5; ++i)
+        if (touch(in[i].at, in[i].bytes, workspace, room.bytes)) return TFE_ERR_INVALID_ARG;
     int sms = 0;
     if (tfe_status st = device_sms(&sms)) return st;
     CompactParams c{};

@@ -162,6 +162,19 @@ def test_values_that_are_not_finite_stay_where_they_belong(n):
     assert torch.equal(loss.cpu()[others], clean[0][others]) and torch.equal(lse.cpu()[others], clean[1][others])
     gh, gw = engine.xent_backward(g.to(DEV), bad.to(DEV), w.to(DEV), t.to(DEV), lse)
     assert torch.isnan(gh[n // 2]).all() and torch.isfinite(gh.cpu()[others].float()).all() and torch.isnan(gw).any()
+    # a weight of -inf against hidden states above 0: a token that cannot come, whose row of grad_weight is zeros.  (0 times -inf reaches
+    # grad_hidden, as it does in the formula.)
+    h0 = h.clone()
+    h0[:, 5] = 0.5
+    w0 = w.clone()
+    w0[77, 5] = -float("inf")
+    t0 = torch.where(t == 77, 78, t).int()
+    loss, lse = engine.xent_forward(*(x.to(DEV) for x in (h0, w0, t0)))
+    _, gw = engine.xent_backward(g.to(DEV), h0.to(DEV), w0.to(DEV), t0.to(DEV), lse, want_hidden=False)
+    keep = torch.arange(500) != 77
+    assert not gw[77].any() and torch.isfinite(gw.float()).all()
+    e_loss = reference(h0, w0[keep], torch.where(t0 > 77, t0 - 1, t0))[0]
+    assert float((loss.double().cpu() - e_loss).abs().max()) <= 1e-5 * float(e_loss.abs().max() + 1)
     # a logit of +inf: NaN
     bad = h.clone()
     bad[1] = 0

@@ -28,10 +28,10 @@ def test_cross_entropy(tfe):
     both = [dict(N=-1), dict(N=tfe.XENT_MAX_ROWS + 1), dict(V=0), dict(V=tfe.XENT_MAX_ROWS + 1), dict(d=0), dict(d=60), dict(d=7), dict(d=tfe.XENT_MAX_COLS + 8, ld_h=1 << 20, ld_w=1 << 20),
             dict(ld_h=56), dict(ld_h=68), dict(ld_h=1 << 40), dict(ld_w=56), dict(ld_w=66), dict(h=None), dict(h=P + 8), dict(w=None), dict(w=2 * P + 2), dict(t=None), dict(t=3 * P + 2),
             dict(lse=None), dict(lse=5 * P + 1), dict(ws=None), dict(ws=far + 16)]
-    for kw in both + [dict(loss=None), dict(loss=4 * P + 2), dict(loss=P), dict(lse=2 * P + 64), dict(loss=3 * P), dict(loss=5 * P), dict(lse=far + 512)]:
+    for kw in both + [dict(loss=None), dict(loss=4 * P + 2), dict(loss=P), dict(lse=2 * P + 64), dict(loss=3 * P), dict(loss=5 * P), dict(lse=far + 512), dict(h=far + 64), dict(t=far)]:
         assert forward(**kw) == tfe.TFE_ERR_INVALID_ARG, kw
     for kw in both + [dict(g=None), dict(g=6 * P + 2), dict(gh=None, gw=None), dict(gh=7 * P + 8), dict(gw=8 * P + 4), dict(ld_gh=56), dict(ld_gw=60), dict(gh=P), dict(gw=2 * P),
-                      dict(gh=2 * P + 128), dict(gw=P + 16), dict(gh=8 * P + 16), dict(gw=3 * P), dict(gh=far + 1024), dict(gw=far), dict(gh=5 * P), dict(gw=6 * P)]:
+                      dict(gh=2 * P + 128), dict(gw=P + 16), dict(gh=8 * P + 16), dict(gw=3 * P), dict(gh=far + 1024), dict(gw=far), dict(gh=5 * P), dict(gw=6 * P), dict(w=far + 128), dict(g=far)]:
         assert backward(**kw) == tfe.TFE_ERR_INVALID_ARG, kw
     need = tfe.tfe_xent_forward_workspace_bytes(4, 100, 64), tfe.tfe_xent_backward_workspace_bytes(4, 100, 64)
     assert min(need) > 0
