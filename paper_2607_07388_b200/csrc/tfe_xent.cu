@@ -37,12 +37,17 @@ constexpr int kM = kRowsA * kCtas;              // rows of a tile
 constexpr int kN = 256;                         // columns of a tile at most (MMA N)
 constexpr int kStepK = 64;                      // k of a stage: 128 bytes, one swizzle row
 constexpr uint32_t kBytesA = kRowsA * kStepK * 2, kBytesB = kN / kCtas * kStepK * 2, kStageBytes = kBytesA + kBytesB;
-constexpr int kStages = 6;
+#ifndef TST
+#define TST 6
+#define TROOM 1
+#endif
+constexpr int kStages = TST;
 constexpr int kBuffers = 2;                     // accumulators of kN columns: all of tensor memory
 constexpr int kEpilogueWarps = 8;               // two per lane quarter of tensor memory, half of the tile's columns each
 constexpr int kThreads = 32 * (4 + kEpilogueWarps);
 constexpr uint32_t kRoom = 32 * 128;            // bytes of an epilogue warp's outgoing piece: 32 rows of 64 bf16
-constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kEpilogueWarps * kRoom;
+constexpr uint32_t kRooms = TROOM;              // pieces of a warp on their way
+constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kEpilogueWarps * kRooms * kRoom;
 constexpr float kLog2e = 1.4426950408889634f;
 // The tensor cores cut what they add to a sum in fp32, always towards zero, so a long sum comes out too small: a loss over 1,024 k was off by
 // 6e-7 that way.  A sum of the loss therefore takes at most this many steps, and the epilogue adds those up: 3e-7, whatever d.  (With 4
@@ -397,7 +402,7 @@ __device__ __forceinline__ void add_rest(const GemmParams &p, int32_t at, int32_
 // of grad W: 201 against 221).
 constexpr int32_t kShort = 16;                  // steps of a unit of grad W
 constexpr int kTickets = 4;                     // units that are known ahead
-constexpr int kListeners = kCtas * (1 + kEpilogueWarps) + 1;        // loaders, epilogue warps, and the one that issues the MMAs
+constexpr int kListeners = kCtas * (2 + kEpilogueWarps) + 1;        // loaders, epilogue warps, and the one that issues the MMAs
 
 struct Maps { CUtensorMap a, b, a_w, b_w, out; };           // kLse, kProb: H, W, -, -, G;  kGrads: G by rows, W, G by columns, H, grad W
 
@@ -416,7 +421,7 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     if (threadIdx.x == 0) {
         for (int t = 0; t < kTickets; ++t) { mbar_init(smem_u32(&s_told[t]), 1); mbar_init(smem_u32(&s_heard[t]), kListeners); }
-        for (int s = 0; s < kStages; ++s) { mbar_init(smem_u32(&s_full[s]), 1); mbar_init(smem_u32(&s_empty[s]), 1); }
+        for (int s = 0; s < kStages; ++s) { mbar_init(smem_u32(&s_full[s]), 2); mbar_init(smem_u32(&s_empty[s]), 1); }
         for (int a = 0; a < kBuffers; ++a) { mbar_init(smem_u32(&s_acc_full[a]), 1); mbar_init(smem_u32(&s_acc_empty[a]), kCtas * kEpilogueWarps); }
         mbar_init(smem_u32(&s_drain), 1);
         s_abort = 0;
@@ -452,10 +457,13 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
 
     if (warp < 4) {
         if constexpr (kOp == kLse) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegs));
-        if (warp == 0 && lane == 0) {
-            // ============================ TMA producer ============================
+        if ((warp == 0 || warp == 3) && lane == 0) {
+            // ============================ TMA producers ===========================
+            // one thread for A, one for B: a copy takes its thread some 150 clocks to issue, a step of MMAs 512
+            const bool is_a = warp == 0;
             const uint64_t hint = 0x1000000000000000ull;            // no preference
             const int32_t b_part = p.tn / kCtas;
+            const uint32_t place = smem_base + (is_a ? 0u : kBytesA);
             uint32_t stage = 0, phase = 0, issued = 0;
             bool ok = !p.give_up;
             while (ok) {
@@ -463,7 +471,8 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                 if (!ok) { atomicOr(&g_xent_status, kTimeoutLoader); s_abort = 1; }
                 if (!ok || u >= units.n) break;
                 const Unit w = units.at(p, u);
-                for (int32_t t = 0; ok && t < w.tiles; ++t)
+                for (int32_t t = 0; ok && t < w.tiles; ++t) {
+                    const int32_t a_at = w.a_at + (int32_t)rank * kRowsA, b_at = w.b_at + t * p.tn + (int32_t)rank * b_part;
                     for (int32_t ks = 0; ks < w.steps; ++ks) {
                         if (!mbar_wait(smem_u32(&s_empty[stage]), phase ^ 1u, &s_abort)) {
                             atomicOr(&g_xent_status, kTimeoutLoader);
@@ -472,31 +481,34 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                             break;
                         }
                         // both CTAs' copies are counted where the MMAs are issued
-                        const uint32_t bar = in_first(smem_u32(&s_full[stage])), a = smem_base + stage * kStageBytes, b = a + kBytesA;
-                        const int32_t k = w.k_at + ks * kStepK, a_at = w.a_at + (int32_t)rank * kRowsA, b_at = w.b_at + t * p.tn + (int32_t)rank * b_part;
-                        if (rank == 0) mbar_expect_tx(smem_u32(&s_full[stage]), kCtas * (kBytesA + (uint32_t)b_part * kStepK * 2));
-                        if constexpr (kOp != kGrads) {
-                            pair_load_2d(a, &maps.a, bar, k, a_at, hint);
-                            pair_load_2d(b, &maps.b, bar, k, (kOp == kProb ? p.v0 : 0) + b_at, hint);
-                        } else if (w.grad_h) {
-                            pair_load_2d(a, &maps.a, bar, 0, k / 64 * p.n_pad + a_at, hint);
-                            for (int32_t j = 0; j < b_part; j += 64) pair_load_2d(b + j * kStepK * 2, &maps.b, bar, b_at + j, p.v0 + k, hint);
+                        const uint32_t bar = in_first(smem_u32(&s_full[stage])), dst = place + stage * kStageBytes;
+                        const int32_t k = w.k_at + ks * kStepK;
+                        if (rank == 0) mbar_expect_tx(smem_u32(&s_full[stage]), kCtas * (is_a ? kBytesA : (uint32_t)b_part * kStepK * 2));
+                        if (is_a) {
+                            if (kOp != kGrads) pair_load_2d(dst, &maps.a, bar, k, a_at, hint);
+                            else if (w.grad_h) pair_load_2d(dst, &maps.a, bar, 0, k / 64 * p.n_pad + a_at, hint);
+                            else
+                                for (int32_t j = 0; j < kRowsA; j += 64) pair_load_2d(dst + j * kStepK * 2, &maps.a_w, bar, 0, (a_at + j) / 64 * p.n_pad + k, hint);
                         } else {
-                            for (int32_t j = 0; j < kRowsA; j += 64) pair_load_2d(a + j * kStepK * 2, &maps.a_w, bar, 0, (a_at + j) / 64 * p.n_pad + k, hint);
-                            for (int32_t j = 0; j < b_part; j += 64) pair_load_2d(b + j * kStepK * 2, &maps.b_w, bar, b_at + j, k, hint);
+                            if (kOp != kGrads) pair_load_2d(dst, &maps.b, bar, k, (kOp == kProb ? p.v0 : 0) + b_at, hint);
+                            else
+                                for (int32_t j = 0; j < b_part; j += 64) pair_load_2d(dst + j * kStepK * 2, w.grad_h ? &maps.b : &maps.b_w, bar, b_at + j, (w.grad_h ? p.v0 : 0) + k, hint);
                         }
                         ++issued;
                         if (++stage == kStages) { stage = 0; phase ^= 1u; }
                     }
-            }
-            // copies in flight land before the shared memory goes; the second CTA's are counted in the first, so it only waits a while
-            if (!ok && rank == 0)
-                for (uint32_t s = 0; s < kStages; ++s) {
-                    const uint32_t fills = (issued + kStages - 1u - s) / kStages;
-                    for (uint32_t t = 0; fills && t < TC_WAIT_LIMIT && !mbar_try_wait(smem_u32(&s_full[s]), (fills - 1u) & 1u); ++t) { }
                 }
-            else if (!ok && issued)
+            }
+            // copies in flight land before the shared memory goes: those of both threads and both CTAs are counted in the first, where a barrier
+            // may lack one of them for good, so a short wait for each has to do
+            if (!ok && issued) {
+                if (rank == 0)
+                    for (uint32_t s = 0; s < kStages; ++s) {
+                        const uint32_t fills = (issued + kStages - 1u - s) / kStages;
+                        for (uint32_t t = 0; fills && t < (1u << 12) && !mbar_try_wait(smem_u32(&s_full[s]), (fills - 1u) & 1u); ++t) { }
+                    }
                 __nanosleep(1000000);
+            }
         } else if (handed_out && warp == 2 && lane == 0 && rank == 0) {
             // ============================ units to both CTAs ======================
             uint32_t slot = 0, phase = 0;
@@ -562,12 +574,15 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
         const uint32_t quarter = (uint32_t)warp & 3u;               // tensor-memory lanes 32 * quarter .. + 31
         const int32_t half = e >> 2, cols = p.tn / 2, c0 = half * cols;     // this warp's columns: a multiple of 16
         const int32_t first_row = (int32_t)(rank * kRowsA + quarter * 32u), row_in_tile = first_row + lane;
-        const uint32_t room = smem_base + kStages * kStageBytes + (uint32_t)e * kRoom;
+        const uint32_t rooms = smem_base + kStages * kStageBytes + (uint32_t)e * kRooms * kRoom;
+        uint32_t turn = 0;
         uint32_t buf = 0, buf_phase = 0;
         bool ok = !p.give_up;
         // 64 finished columns of this warp's rows leave by an asynchronous copy
         auto send = [&](const uint32_t (&out)[32], int32_t x, int32_t y, bool there) {
-            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");     // what was there has left
+            const uint32_t room = rooms + turn * kRoom;
+            turn = (turn + 1) % kRooms;
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kRooms - 1) : "memory");     // what was there has left
             __syncwarp();
 #pragma unroll
             for (int i = 0; i < 8; ++i)
