@@ -7,7 +7,8 @@
 //   tfe_grad_clip_kernel   every block adds up those sums in the same order, and scales its run of chunks, from its end to its
 //                          beginning: what was read last is in L2.  Where nothing is to be scaled in place it reads no tensor.
 //
-// HBM bounds both: one read for the norm, one read and one write to scale.  A thread's eight or four squares are summed in fp32 and
+// HBM bounds both: one read for the norm, one read and one write to scale (155.6 M bf16 elements: 53 + 98 us; writing 311 MB alone takes
+// 80, so what L2 saves in reads shows little).  A thread's eight or four squares are summed in fp32 and
 // joined in fp64; where they leave fp32's range they are formed in fp64.  No atomics: the order depends on the sizes alone.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -26,6 +27,7 @@ using tfe_rows::Elem;
 
 constexpr int kThreads = 256;
 constexpr int64_t kChunkMin = 2048, kChunkMax = 16384;        // elements of a chunk: few tensors are spread over the SMs, many read in long runs
+constexpr int64_t kKeepBytes = 80 << 20;       // what the norm leaves in L2 for the scaling (126 MB, and its writes pass through it)
 constexpr int kPerSm = 6;                       // blocks, all resident
 constexpr int kBlocks = 148 * kPerSm;           // most blocks of a launch
 
@@ -34,6 +36,7 @@ template <int kRoom> struct Table {
     int32_t tensors, parts, part0;              // parts: sums of all launches; part0: this launch's first
     uint32_t chunks;
     int64_t chunk;
+    uint32_t keep;                              // chunks of a block's run that L2 has room for
     int32_t write_norm, in_place, only_norm;
     float max_norm;
     double *part;
@@ -72,8 +75,23 @@ __device__ __forceinline__ int find_tensor(const Table<kRoom> &t, uint32_t chunk
     return lo;
 }
 
+// Policies of the L2 cache for what will be read again and for what will not.
+__device__ __forceinline__ uint64_t policy(bool keep)
+{
+    uint64_t p;
+    if (keep) asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(p));
+    else asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+    return p;
+}
+__device__ __forceinline__ uint4 load_hint(const uint4 *at, uint64_t hint)
+{
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(at), "l"(hint) : "memory");
+    return v;
+}
+
 template <typename T>
-__device__ __forceinline__ double chunk_squares(const T *x, int64_t n)
+__device__ __forceinline__ double chunk_squares(const T *x, int64_t n, uint64_t hint)
 {
     const tfe_rows::Cut cut = tfe_rows::cut_row(x, n);
     const uint4 *body = reinterpret_cast<const uint4 *>(x + cut.head);
@@ -85,11 +103,11 @@ __device__ __forceinline__ double chunk_squares(const T *x, int64_t n)
     for (; v + (U - 1) * kThreads < cut.n_vec; v += U * kThreads) {
         uint4 raw[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) raw[u] = __ldcg(body + v + u * kThreads);
+        for (int u = 0; u < U; ++u) raw[u] = load_hint(body + v + u * kThreads, hint);
 #pragma unroll
         for (int u = 0; u < U; ++u) sum += squares<T>(raw[u]);
     }
-    for (; v < cut.n_vec; v += kThreads) sum += squares<T>(__ldcg(body + v));
+    for (; v < cut.n_vec; v += kThreads) sum += squares<T>(load_hint(body + v, hint));
     return sum;
 }
 
@@ -113,13 +131,16 @@ tfe_grad_norm_kernel(const __grid_constant__ Table<kRoom> t)
     tfe_wait_for_stream();
     const uint32_t c0 = (uint32_t)((uint64_t)t.chunks * blockIdx.x / gridDim.x), c1 = (uint32_t)((uint64_t)t.chunks * (blockIdx.x + 1) / gridDim.x);
     double sum = 0.0;
+    // the end of this block's run stays in L2 for the scaling, which begins there; the rest makes room for it
+    const uint32_t kept = c1 - (uint32_t)min((uint64_t)(c1 - c0), (uint64_t)t.keep);
+    const uint64_t last = policy(true), first = policy(false);
     if (c0 < c1) {
         int i = find_tensor(t, c0);
         for (uint32_t c = c0; c < c1; ++c) {
             while (i + 1 < t.tensors && t.at[i + 1].first <= c) ++i;
             const int64_t from = (int64_t)(c - t.at[i].first) * t.chunk, n = min(t.chunk, t.at[i].n - from);
-            sum += t.at[i].dtype == TFE_DTYPE_BF16 ? chunk_squares(reinterpret_cast<const __nv_bfloat16 *>(t.at[i].in) + from, n)
-                                                   : chunk_squares(reinterpret_cast<const float *>(t.at[i].in) + from, n);
+            sum += t.at[i].dtype == TFE_DTYPE_BF16 ? chunk_squares(reinterpret_cast<const __nv_bfloat16 *>(t.at[i].in) + from, n, c >= kept ? last : first)
+                                                   : chunk_squares(reinterpret_cast<const float *>(t.at[i].in) + from, n, c >= kept ? last : first);
         }
     }
     sum = block_sum(sum, s_warp);
@@ -127,7 +148,7 @@ tfe_grad_norm_kernel(const __grid_constant__ Table<kRoom> t)
 }
 
 template <typename T>
-__device__ __forceinline__ void chunk_scale(const T *x, T *y, int64_t n, float by)
+__device__ __forceinline__ void chunk_scale(const T *x, T *y, int64_t n, float by, uint64_t hint)
 {
     if (((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(y)) & 15u) != 0) {
         for (int64_t i = threadIdx.x; i < n; i += kThreads) Elem<T>::put(y + i, Elem<T>::get(x + i) * by);
@@ -151,11 +172,11 @@ __device__ __forceinline__ void chunk_scale(const T *x, T *y, int64_t n, float b
     for (; v + (U - 1) * kThreads < cut.n_vec; v += U * kThreads) {
         uint4 raw[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) raw[u] = tfe_rows::load_stream(from + v + u * kThreads);
+        for (int u = 0; u < U; ++u) raw[u] = load_hint(from + v + u * kThreads, hint);
 #pragma unroll
         for (int u = 0; u < U; ++u) __stcs(to + v + u * kThreads, scale(raw[u]));
     }
-    for (; v < cut.n_vec; v += kThreads) __stcs(to + v, scale(tfe_rows::load_stream(from + v)));
+    for (; v < cut.n_vec; v += kThreads) __stcs(to + v, scale(load_hint(from + v, hint)));
 }
 
 template <int kRoom>
@@ -174,14 +195,15 @@ tfe_grad_clip_kernel(const __grid_constant__ Table<kRoom> t)
     if (by == 1.f && t.in_place) return;
     const uint32_t c0 = (uint32_t)((uint64_t)t.chunks * blockIdx.x / gridDim.x), c1 = (uint32_t)((uint64_t)t.chunks * (blockIdx.x + 1) / gridDim.x);
     if (c0 >= c1) return;
+    const uint64_t hint = policy(false);
     int i = find_tensor(t, c1 - 1);
     for (uint32_t c = c1; c-- > c0;) {
         while (t.at[i].first > c) --i;
         const int64_t from = (int64_t)(c - t.at[i].first) * t.chunk, n = min(t.chunk, t.at[i].n - from);
         if (t.at[i].dtype == TFE_DTYPE_BF16)
-            chunk_scale(reinterpret_cast<const __nv_bfloat16 *>(t.at[i].in) + from, reinterpret_cast<__nv_bfloat16 *>(t.at[i].out) + from, n, by);
+            chunk_scale(reinterpret_cast<const __nv_bfloat16 *>(t.at[i].in) + from, reinterpret_cast<__nv_bfloat16 *>(t.at[i].out) + from, n, by, hint);
         else
-            chunk_scale(reinterpret_cast<const float *>(t.at[i].in) + from, reinterpret_cast<float *>(t.at[i].out) + from, n, by);
+            chunk_scale(reinterpret_cast<const float *>(t.at[i].in) + from, reinterpret_cast<float *>(t.at[i].out) + from, n, by, hint);
     }
 }
 
@@ -213,6 +235,7 @@ tfe_status run_pass(const Job &j, int pass, int32_t lo, int32_t hi, int32_t *par
     }
     if (chunks > 0xFFFFFFFFull) return TFE_ERR_INVALID_ARG;
     t.chunks = (uint32_t)chunks; t.chunk = j.chunk;
+    t.keep = (uint32_t)(j.only_norm ? 0 : kKeepBytes / (j.chunk * 2) / (kPerSm * j.sms));
     t.parts = parts; t.part0 = *part0; t.part = j.part; t.norm = j.norm; t.max_norm = j.max_norm;
     t.write_norm = first; t.in_place = j.out == nullptr; t.only_norm = j.only_norm;
     const unsigned grid = pass == 1 && j.only_norm ? 1u : (unsigned)std::max<uint64_t>(1, std::min<uint64_t>(chunks, (uint64_t)std::min(kBlocks, kPerSm * j.sms)));
