@@ -37,17 +37,12 @@ constexpr int kM = kRowsA * kCtas;              // rows of a tile
 constexpr int kN = 256;                         // columns of a tile at most (MMA N)
 constexpr int kStepK = 64;                      // k of a stage: 128 bytes, one swizzle row
 constexpr uint32_t kBytesA = kRowsA * kStepK * 2, kBytesB = kN / kCtas * kStepK * 2, kStageBytes = kBytesA + kBytesB;
-#ifndef TST
-#define TST 6
-#define TROOM 1
-#endif
-constexpr int kStages = TST;
+constexpr int kStages = 6;
 constexpr int kBuffers = 2;                     // accumulators of kN columns: all of tensor memory
 constexpr int kEpilogueWarps = 8;               // two per lane quarter of tensor memory, half of the tile's columns each
 constexpr int kThreads = 32 * (4 + kEpilogueWarps);
 constexpr uint32_t kRoom = 32 * 128;            // bytes of an epilogue warp's outgoing piece: 32 rows of 64 bf16
-constexpr uint32_t kRooms = TROOM;              // pieces of a warp on their way
-constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kEpilogueWarps * kRooms * kRoom;
+constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kEpilogueWarps * kRoom;
 constexpr float kLog2e = 1.4426950408889634f;
 // The tensor cores cut what they add to a sum in fp32, always towards zero, so a long sum comes out too small: a loss over 1,024 k was off by
 // 6e-7 that way.  A sum of the loss therefore takes at most this many steps, and the epilogue adds those up: 3e-7, whatever d.  (With 4
@@ -574,15 +569,12 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
         const uint32_t quarter = (uint32_t)warp & 3u;               // tensor-memory lanes 32 * quarter .. + 31
         const int32_t half = e >> 2, cols = p.tn / 2, c0 = half * cols;     // this warp's columns: a multiple of 16
         const int32_t first_row = (int32_t)(rank * kRowsA + quarter * 32u), row_in_tile = first_row + lane;
-        const uint32_t rooms = smem_base + kStages * kStageBytes + (uint32_t)e * kRooms * kRoom;
-        uint32_t turn = 0;
+        const uint32_t room = smem_base + kStages * kStageBytes + (uint32_t)e * kRoom;
         uint32_t buf = 0, buf_phase = 0;
         bool ok = !p.give_up;
         // 64 finished columns of this warp's rows leave by an asynchronous copy
         auto send = [&](const uint32_t (&out)[32], int32_t x, int32_t y, bool there) {
-            const uint32_t room = rooms + turn * kRoom;
-            turn = (turn + 1) % kRooms;
-            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kRooms - 1) : "memory");     // what was there has left
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");     // what was there has left
             __syncwarp();
 #pragma unroll
             for (int i = 0; i < 8; ++i)
