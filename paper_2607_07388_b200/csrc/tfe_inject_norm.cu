@@ -139,14 +139,14 @@ struct RowSum {
         asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(threads) : "memory");
     }
 
-    template <typename X> __device__ __forceinline__ X shared(X x)
+    __device__ __forceinline__ float2 shared(float2 x)
     {
         if (warps == 1) return x;
-        X *s = reinterpret_cast<X *>(slots + 32 * turn);
+        float2 *s = slots + 32 * turn;          // (one layout for one sum and for two: what lies beyond the warps stays zero)
         turn ^= 1;
         if ((threadIdx.x & 31) == 0) s[warp] = x;
         asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(threads) : "memory");
-        return s[threadIdx.x & (2 * span - 1)];         // (slots beyond the warps hold zeros from the start)
+        return s[threadIdx.x & (2 * span - 1)];
     }
     // one sum, or two
     __device__ __forceinline__ float operator()(float x)
@@ -154,7 +154,7 @@ struct RowSum {
         x = in ? x : 0.f;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
-        x = shared(x);
+        x = shared(make_float2(x, 0.f)).x;
         for (int o = span; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
         return x;
     }

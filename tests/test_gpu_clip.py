@@ -1,5 +1,7 @@
 """The norm of many gradients and clipping by it, against the formula in 64 bits."""
 import math
+import os
+import random
 
 import pytest
 import torch
@@ -181,3 +183,19 @@ def test_refusals():
             call()
     assert float(engine.grad_norm([x, x])) == pytest.approx(200 ** 0.5, rel=1e-6)       # nothing is written: the same tensor may count twice
     assert torch.equal(x, torch.ones(100, device=DEV)) and torch.equal(y, torch.ones(200, device=DEV))
+
+
+@pytest.mark.parametrize("seed", range(int(os.environ.get("TFE_RANDOM_CASES", "12"))))
+def test_random_sizes(seed):
+    rng = random.Random(3000 + seed)
+    log = lambda lo, hi: int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+    sizes = [rng.choice([0, 1, log(1, 200_000)]) for _ in range(log(1, 1200))] + [log(1, 300_000)]
+    x = make(seed, sizes, rng.choice([[torch.bfloat16], [torch.float32], [torch.bfloat16, torch.float32, torch.float32]]), rng.choice([1.0, 1e-6, 1e4]))
+    flat = {t: torch.cat([y for y in x if y.dtype == t] + [torch.zeros(0, dtype=t)]).to(DEV) for t in (torch.bfloat16, torch.float32)}
+    at, dev = {torch.bfloat16: 0, torch.float32: 0}, []
+    for y in x:                         # side by side, at whatever boundary
+        dev.append(flat[y.dtype][at[y.dtype]:at[y.dtype] + y.numel()])
+        at[y.dtype] += y.numel()
+    out = None if rng.random() < 0.5 else [torch.empty_like(y) for y in dev]
+    norm = reference(x)
+    check(x, norm * rng.choice([0.3, 0.9, 1.5]) if norm > 0 else 1.0, out=out, dev=dev)

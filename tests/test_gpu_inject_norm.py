@@ -1,4 +1,8 @@
 """Injection between two norms, forward and gradients, against the formulas in 64 bits."""
+import math
+import os
+import random
+
 import pytest
 import torch
 
@@ -83,7 +87,7 @@ def check(data, sigmoid=False, lam=0.75, eps=1e-6, move=lambda x: None if x is N
 
 
 @pytest.mark.parametrize("n,d", [(1, 1), (1, 1024), (2, 7), (3, 32), (5, 257), (7, 1001), (33, 264), (149, 1024), (300, 96), (2, 4096), (3, 8192), (2, 8191),
-                                 (5000, 40), (1200, 1024)])
+                                 (5000, 40), (1200, 1024), (3000, 700), (1200, 1300), (700, 2900)])
 @pytest.mark.parametrize("kind,gate,weights", [("bf16", "vector", "bf16"), ("f32", "scalar", "f32"), ("bf16", "none", "f32"), ("f32", "vector", "bf16"),
                                                ("bf16", "scalar", "f32")])
 def test_sizes(n, d, kind, gate, weights):
@@ -291,3 +295,13 @@ def test_refusals():
         engine.normed_inject_backward(None, None, h, m, wp, wn, g)
     with pytest.raises(ValueError):
         engine.normed_inject_backward(gu.float(), gn, h, m, wp, wn, g)
+
+
+@pytest.mark.parametrize("seed", range(int(os.environ.get("TFE_RANDOM_CASES", "12"))))
+def test_random_sizes(seed):
+    rng = random.Random(2000 + seed)
+    log = lambda lo, hi: int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+    d = log(1, 8192)
+    n = log(1, max(2, 400_000 // d))
+    check(make(seed, n, d, rng.choice(["bf16", "f32"]), rng.choice(["none", "scalar", "vector"]), rng.choice(["bf16", "f32"])), sigmoid=rng.random() < 0.5,
+          lam=rng.choice([1.0, -0.5, 0.0, 3.0]), eps=rng.choice([1e-6, 1e-5, 1e-2]))

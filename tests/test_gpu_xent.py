@@ -1,5 +1,8 @@
 """Softmax cross entropy from hidden states, loss and gradients, against the formulas in 64 bits."""
-import numpy as np
+import math
+import os
+import random
+
 import pytest
 import torch
 
@@ -429,3 +432,18 @@ def test_refusals():
         with pytest.raises(ValueError):
             engine.xent_backward(**a)
     assert engine.xent_backward(g, h, w, t, lse, want_hidden=False, want_weight=False) == (None, None)
+
+
+@pytest.mark.parametrize("seed", range(int(os.environ.get("TFE_RANDOM_CASES", "12"))))
+def test_random_sizes(seed):
+    rng = random.Random(1000 + seed)
+    log = lambda lo, hi: int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+    n, d = log(1, 4000), 8 * log(1, 90)
+    v = log(1, max(2, min(6000, 500_000_000 // (n * d))))
+    h, w, t, g = make(seed, n, v, d, rng.choice([0.0, 0.0, 0.3, 0.9]), rng.choice([0.0, 1.5, 4.0]))
+    pick = torch.Generator().manual_seed(seed)
+    if rng.random() < 0.3:              # one id for half of the rows
+        t = torch.where(torch.rand(n, generator=pick) < 0.5, torch.full_like(t, rng.randrange(v)), t)
+    if rng.random() < 0.3:              # gradients of either sign, and none
+        g = torch.where(torch.rand(n, generator=pick) < 0.4, 0.0, g - 0.6)
+    check(h, w, t, g)
