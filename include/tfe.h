@@ -735,6 +735,20 @@ tfe_status tfe_clip_grad_norm(const uint64_t *tensors, const uint64_t *results, 
                               float max_norm, float *norm, void *workspace, int64_t workspace_bytes, void *stream);
 
 /*
+ * tfe_describe_tensors -- the lists of the two calls above from n tensors that a Python program holds, HOST only: asking for each
+ * property of each tensor from Python takes longer than clipping 400 of them.
+ *   objects, item    a list object, and the function that gives its i-th element as a borrowed reference (PyList_GetItem)
+ *   describe         dltensor_from_py_object_no_sync of the DLPack exchange interface (DLPack 1.3) that the tensors' class offers;
+ *                    every element must be of that class.  The caller holds the interpreter's lock.
+ *   outputs          HOST [n] each; device: the CUDA device of all.  reason: HOST, 0 or why a tensor is refused: 1 not on a CUDA
+ *                    device, or on another than the first, 2 neither bf16 nor fp32, 3 its elements do not lie side by side in order,
+ *                    4 describe failed and has set the interpreter's error.
+ * Errors: INVALID_ARG.
+ */
+tfe_status tfe_describe_tensors(void *objects, void *(*item)(void *, int64_t), int (*describe)(void *, void *), int32_t n, uint64_t *tensors,
+                                int64_t *numel, int32_t *dtype, int32_t *device, int32_t *reason);
+
+/*
  * Streaming copy (the paper has no counterpart: a yardstick for the measurements, not a step of the method).
  * Copies `bytes` bytes from `src` to `dst` (DEVICE, 16-byte aligned, bytes a multiple of 16, ranges must not
  * overlap) with the load / store instructions the lookup kernels stream hidden states with, one asynchronous

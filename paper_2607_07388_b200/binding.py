@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from array import array
 
 import numpy as np
 
@@ -39,7 +40,7 @@ EXPORTS = ["tfe_index_build", "tfe_index_build_device", "tfe_cache_install", "tf
            "tfe_quantize_fp8", "tfe_quantize_fp8_ld", "tfe_matmul_fp8", "tfe_matmul_fp8_status", "tfe_matmul_fp8_give_up",
            "tfe_xent_forward_workspace_bytes", "tfe_xent_backward_workspace_bytes", "tfe_xent_forward", "tfe_xent_backward",
            "tfe_xent_status", "tfe_xent_give_up", "tfe_inject_norm_forward", "tfe_inject_norm_backward", "tfe_inject_norm_workspace_bytes",
-           "tfe_grad_norm", "tfe_clip_grad_norm", "tfe_clip_workspace_bytes"]
+           "tfe_grad_norm", "tfe_clip_grad_norm", "tfe_clip_workspace_bytes", "tfe_describe_tensors"]
 
 
 class TfeConfig(C.Structure):
@@ -154,6 +155,7 @@ def lib() -> C.CDLL:
         L.tfe_grad_norm.argtypes = [vp, vp, vp, i32, vp, vp, i64, vp]
         L.tfe_clip_grad_norm.argtypes = [vp, vp, vp, vp, i32, f32, vp, vp, i64, vp]
         L.tfe_clip_workspace_bytes.argtypes = [i32]
+        L.tfe_describe_tensors.argtypes = [vp, vp, vp, i32, vp, vp, vp, vp, vp]
         L.tfe_inject_norm_workspace_bytes.restype = L.tfe_clip_workspace_bytes.restype = i64
         L.tfe_sample_tokens.argtypes = [vp, i32, i32, i32, i64, C.POINTER(TfeSampleParams), vp, vp, vp, vp]
         L.tfe_distill_forward.argtypes = [vp, i32, i32, i32, i64, vp, vp, i32, f32, vp, vp, vp]
@@ -625,6 +627,41 @@ CLIP_MAX_TENSORS = 1 << 20
 
 def tfe_clip_workspace_bytes(n: int) -> int:
     return lib().tfe_clip_workspace_bytes(n)
+
+
+_describe = None        # (the library with the interpreter's lock held, PyList_GetItem, the tensors' describing function), on first use
+
+
+class _DlpackExchange(C.Structure):     # DLPackExchangeAPI of the DLPack standard, version 1.3
+    _fields_ = [("major", C.c_uint32), ("minor", C.c_uint32), ("previous", C.c_void_p), ("allocator", C.c_void_p), ("managed_from_object", C.c_void_p),
+                ("managed_to_object", C.c_void_p), ("tensor_from_object", C.c_void_p), ("work_stream", C.c_void_p)]
+
+
+def _describer():
+    global _describe
+    if _describe is None:
+        import torch
+        lib()
+        pointer = C.pythonapi.PyCapsule_GetPointer
+        pointer.restype, pointer.argtypes = C.c_void_p, [C.py_object, C.c_char_p]
+        exchange = _DlpackExchange.from_address(pointer(torch.Tensor.__dlpack_c_exchange_api__, b"dlpack_exchange_api"))
+        if exchange.major != 1 or not exchange.tensor_from_object:
+            raise RuntimeError("the DLPack exchange interface of this torch is not version 1")
+        f = C.PyDLL(LIB_PATH).tfe_describe_tensors
+        f.restype, f.argtypes = C.c_int, [C.py_object, C.c_void_p, C.c_void_p, C.c_int32] + [C.c_void_p] * 5
+        _describe = (f, C.cast(C.pythonapi.PyList_GetItem, C.c_void_p).value, exchange.tensor_from_object)
+    return _describe
+
+
+def tfe_describe_tensors(tensors: list):
+    """(addresses, sizes, the library's type numbers, CUDA device, reason) of a list of torch tensors, the first three as array.array
+    objects; the reason is 0, or why a tensor is refused (see the header)."""
+    f, item, describe = _describe or _describer()
+    n = len(tensors)
+    at, numel, kinds, told = array("Q", bytes(8 * n)), array("q", bytes(8 * n)), array("i", bytes(4 * n)), array("i", (0, 0))
+    device = told.buffer_info()[0]
+    f(tensors, item, describe, n, at.buffer_info()[0], numel.buffer_info()[0], kinds.buffer_info()[0], device, device + 4)
+    return at, numel, kinds, told[0], told[1]
 
 
 def _list(x, code: str):

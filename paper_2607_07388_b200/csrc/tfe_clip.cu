@@ -307,9 +307,46 @@ tfe_status check_and_run(const uint64_t *in, const uint64_t *out, const int64_t 
     return run({in, out, numel, dtype, n, only_norm, max_norm, norm, static_cast<double *>(workspace), static_cast<cudaStream_t>(stream), sms, chunk});
 }
 
+// DLTensor of the DLPack standard, version 1
+struct DlTensor {
+    void *data;
+    struct { int32_t type, id; } device;        // type 2: CUDA
+    int32_t ndim;
+    struct { uint8_t code, bits; uint16_t lanes; } dtype;       // code 2: float, 4: bfloat
+    int64_t *shape, *strides;                   // strides null: side by side in order
+    uint64_t byte_offset;
+};
+
 }  // namespace
 
 extern "C" {
+
+tfe_status tfe_describe_tensors(void *objects, void *(*item)(void *, int64_t), int (*describe)(void *, void *), int32_t n, uint64_t *tensors, int64_t *numel,
+                                int32_t *dtype, int32_t *device, int32_t *reason)
+{
+    if (!objects || !item || !describe || n < 1 || !tensors || !numel || !dtype || !device || !reason) return TFE_ERR_INVALID_ARG;
+    *reason = 0;
+    for (int32_t i = 0; i < n; ++i) {
+        DlTensor t{};
+        if (describe(item(objects, i), &t) != 0) { *reason = 4; return TFE_ERR_INVALID_ARG; }
+        if (i == 0) *device = t.device.id;
+        if (t.device.type != 2 || t.device.id != *device) *reason = 1;
+        const bool bf16 = t.dtype.code == 4 && t.dtype.bits == 16 && t.dtype.lanes == 1, f32 = t.dtype.code == 2 && t.dtype.bits == 32 && t.dtype.lanes == 1;
+        if (!*reason && !bf16 && !f32) *reason = 2;
+        int64_t count = 1;
+        bool in_order = true;
+        for (int32_t k = t.ndim; k-- > 0;) {
+            if (t.strides && t.shape[k] != 1 && t.strides[k] != count) in_order = false;
+            count *= t.shape[k];
+        }
+        if (!*reason && !in_order && count != 0) *reason = 3;
+        if (*reason) return TFE_ERR_INVALID_ARG;
+        tensors[i] = count ? reinterpret_cast<uintptr_t>(t.data) + t.byte_offset : 0;
+        numel[i] = count;
+        dtype[i] = bf16 ? TFE_DTYPE_BF16 : TFE_DTYPE_F32;
+    }
+    return TFE_OK;
+}
 
 int64_t tfe_clip_workspace_bytes(int32_t n)
 {

@@ -6,8 +6,6 @@ Nothing is computed here -- every call goes straight to libtfe.so.
 from __future__ import annotations
 
 import contextlib
-import operator
-from array import array
 from dataclasses import dataclass
 
 import numpy as np
@@ -738,9 +736,7 @@ def normed_inject(h: torch.Tensor, m: torch.Tensor, post_weight: torch.Tensor, n
 # ---- the norm of many gradients, and clipping by it --------------------------------------------
 
 
-# The lists run to hundreds of tensors: torch is asked for one property of all of them at a time, some 0.06 us each.
-_dtype_of = operator.attrgetter("dtype")
-_device_of, _address_of, _numel_of, _contiguous = (torch.Tensor.get_device, torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.is_contiguous)
+_REFUSED = {1: "CUDA tensors on one device are needed", 2: "bf16 or fp32 tensors are needed", 3: "contiguous tensors are needed"}
 
 
 def _gradients(tensors, what):
@@ -748,14 +744,15 @@ def _gradients(tensors, what):
     tensors = [tensors] if torch.is_tensor(tensors) else list(tensors)
     if not 1 <= len(tensors) <= tfe.CLIP_MAX_TENSORS:
         raise ValueError(f"{what}: one tensor at least and {tfe.CLIP_MAX_TENSORS} at most")
-    types = set(map(_dtype_of, tensors))
-    kinds = [_ROW_DTYPES.get(types.pop())] * len(tensors) if len(types) == 1 else list(map(_ROW_DTYPES.get, map(_dtype_of, tensors)))
-    devices = set(map(_device_of, tensors))
-    if None in kinds or len(devices) != 1 or -1 in devices:
-        raise ValueError(f"{what}: bf16 or fp32 CUDA tensors on one device are needed")
-    if not all(map(_contiguous, tensors)):
-        raise ValueError(f"{what}: contiguous tensors are needed")
-    return tensors, devices.pop(), array("Q", map(_address_of, tensors)), array("q", map(_numel_of, tensors)), array("i", kinds)
+    if not all(issubclass(kind, torch.Tensor) for kind in set(map(type, tensors))):
+        raise ValueError(f"{what}: tensors are needed")
+    try:
+        at, numel, kinds, device, reason = tfe.tfe_describe_tensors(tensors)
+    except (RuntimeError, BufferError) as e:            # a tensor without elements in memory (sparse, meta)
+        raise ValueError(f"{what}: {_REFUSED[3]}") from e
+    if reason:
+        raise ValueError(f"{what}: {_REFUSED[reason]}")
+    return tensors, device, at, numel, kinds
 
 
 def grad_norm(tensors, *, stream=None) -> torch.Tensor:

@@ -97,3 +97,21 @@ def test_clipping(tfe):
         assert clip(**kw) == tfe.TFE_ERR_INVALID_ARG, kw
     assert clip(size=tfe.tfe_clip_workspace_bytes(2) - 1) == tfe.TFE_ERR_CAPACITY
     assert tfe.tfe_clip_workspace_bytes(-1) == -1 and tfe.tfe_clip_workspace_bytes(2000) > tfe.tfe_clip_workspace_bytes(2) > 0
+
+
+def test_describing_tensors(tfe):
+    """On the CPU every tensor is refused for where it is; what describes it runs all the same."""
+    import torch
+    for t in (torch.ones(3), torch.nn.Parameter(torch.ones(2, 2)), torch.ones(4, dtype=torch.float64), torch.ones(4, 4).t()):
+        at, numel, kinds, device, reason = tfe.tfe_describe_tensors([t])
+        assert reason == 1 and len(at) == len(numel) == len(kinds) == 1
+    with pytest.raises(RuntimeError):
+        tfe.tfe_describe_tensors([torch.ones(3).to_sparse()])
+    from paper_2607_07388_b200 import engine
+    for bad in ([], [None], [torch.ones(3), 1.0], [torch.ones(3)], [torch.ones(3).to_sparse()], [torch.ones(3, device="meta")], torch.ones(3)):
+        with pytest.raises(ValueError):
+            engine.grad_norm(bad)
+        with pytest.raises(ValueError):
+            engine.clip_grad_norm(bad, 1.0)
+    L = tfe.lib()
+    assert L.tfe_describe_tensors(None, None, None, 1, None, None, None, None, None) == tfe.TFE_ERR_INVALID_ARG
