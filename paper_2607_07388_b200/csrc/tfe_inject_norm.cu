@@ -8,7 +8,8 @@
 //   ds = lam y dh  (summed over the columns for a scalar gate, times s (1 - s) for a sigmoid)
 //   x = lam s w_post dh              dm = a x - a^3 m mean(m x)            dw_post = sum over rows of lam s dh a m
 //
-// HBM bounds both.  A row is held in the registers of `row_threads` threads, eight columns each, so every operand is read once and every
+// HBM bounds both, and nearly as much the issue slots: 32,768 x 1,024 bf16 with a vector gate take 57 us forward (5.9 TB/s of the operands'
+// bytes, 73 % of the slots) and 105 us backward (5.1 TB/s, 62 %).  A row is held in the registers of `row_threads` threads, eight columns each, so every operand is read once and every
 // intermediate stays on the chip; backward makes a, y, u and b again rather than reading them.  Several rows share a block, and a
 // block walks rows with the next row's loads under way.  u is rounded once for the output, n and the gradients come from it as it was
 // before.  The weights' gradients are summed over a block's rows in registers, over its groups in shared memory, and over the blocks

@@ -199,3 +199,16 @@ def test_random_sizes(seed):
     out = None if rng.random() < 0.5 else [torch.empty_like(y) for y in dev]
     norm = reference(x)
     check(x, norm * rng.choice([0.3, 0.9, 1.5]) if norm > 0 else 1.0, out=out, dev=dev)
+
+
+def test_inference_tensors_and_parameters():
+    """Tensors that have no version among others that have one; parameters, and a generator instead of a list."""
+    from paper_2607_07388_b200 import engine
+    with torch.inference_mode():
+        a = torch.ones(300, device=DEV)
+    b, p = torch.ones(500, device=DEV), torch.nn.Parameter(torch.ones(10, 20, device=DEV).bfloat16())
+    version = b._version
+    with torch.no_grad():
+        norm = engine.clip_grad_norm((x for x in (a, b, p)), 1.0)
+    assert abs(float(norm) - 1000 ** 0.5) <= 1e-4 and b._version > version
+    assert abs(float(engine.grad_norm([a, b, p])) - 1.0) <= 2.0 ** -8
