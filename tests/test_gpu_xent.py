@@ -447,3 +447,32 @@ def test_random_sizes(seed):
     if rng.random() < 0.3:              # gradients of either sign, and none
         g = torch.where(torch.rand(n, generator=pick) < 0.4, 0.0, g - 0.6)
     check(h, w, t, g)
+
+
+@pytest.mark.parametrize("n,v,d", [(70, 300, 65_536), (300, 700, 40_008), (70_000, 500, 64), (33_000, 3000, 128), (5, 1_000_000, 64), (300, 1_000_000, 64)])
+def test_long_sides(n, v, d):
+    """The widest rows, many rows, a large vocabulary; the reference runs on the GPU in 64 bits, 2-norms.  A gradient carries its own rounding and
+    what is left of G's, 2^-8 at most each and of random signs: 2^-8 together.  A loss of some units carries logits that are sums of parts of
+    512 k, each part off by at most 32 steps of 2^-23 of its size and those parts' sum by d / 512 half-steps: 5e-6."""
+    from paper_2607_07388_b200 import engine
+    rng = torch.Generator(device=DEV).manual_seed(n + v + d)
+    w = (torch.randn((v, d), generator=rng, device=DEV) * (2.5 / d ** 0.5)).bfloat16()
+    t = torch.randint(0, v, (n,), generator=rng, device=DEV).int()
+    h = (torch.randn((n, d), generator=rng, device=DEV) + w[t.long()].float()).bfloat16()
+    t[torch.rand(n, generator=rng, device=DEV) < 0.2] = -1
+    g = torch.rand(n, generator=rng, device=DEV) - 0.3
+    loss, lse = engine.xent_forward(h, w, t)
+    gh, gw = engine.xent_backward(g, h, w, t, lse)
+    e_loss, e_gh, e_gw = (torch.zeros(s, dtype=torch.float64, device=DEV) for s in ((n,), (n, d), (v, d)))
+    for rows in (t >= 0).nonzero()[:, 0].split(max(1, (1 << 26) // v)):
+        z, at = h[rows].double() @ w.double().T, t[rows].long()
+        k, norm = torch.arange(len(rows), device=DEV), torch.logsumexp(z, 1)
+        e_loss[rows] = norm - z[k, at]
+        p = z.sub_(norm[:, None]).exp_()
+        p[k, at] -= 1
+        p *= g[rows].double()[:, None]
+        e_gh[rows] = p @ w.double()
+        e_gw += p.T @ h[rows].double()
+    for got, want, most in ((loss, e_loss, 5e-6), (gh, e_gh, 2.0 ** -8), (gw, e_gw, 2.0 ** -8)):
+        assert float((got.double() - want).norm() / want.norm()) <= most
+    assert engine.xent_status() == 0
