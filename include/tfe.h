@@ -641,7 +641,7 @@ tfe_status tfe_distill_backward(const void *logits, int32_t dtype, int32_t N, in
  *                    contents undefined before and after.  It bounds what exists of the logits at a time: forward some 40 MB of
  *                    partial results, backward a piece of G of up to 256 MB (4,096 columns where N > 32,768) and sums of as much
  *                    at most (or 4 N d bytes).
- * NaN propagates, and a logit of +inf makes its row's results NaN.  The order of every sum is fixed by the sizes and the targets.
+ * NaN propagates, and a logit of +inf makes its row's results NaN; a target whose logit is -inf has a loss of +inf.  The order of every sum is fixed by the sizes and the targets.
  * Forward two or three launches; backward two for each piece of the vocabulary and
  * two more.
  *

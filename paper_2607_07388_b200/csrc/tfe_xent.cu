@@ -7,11 +7,11 @@
 //   tfe_xent_compact_kernel   lists the rows that have a target (and a gradient) and copies their hidden states together: the
 //                             products below run over those rows only, and a row that has none takes part in no sum.
 //   tfe_xent_gemm_kernel      one persistent, warp-specialised tcgen05 kernel with three epilogues:
-//       kLse    z tile by tile, each kept only as its row maxima, row sums of exponentials and the targets' logits;
+//       kLse    z tile by tile, each kept only as its row maxima and row sums of exponentials, the rows' targets left out;
 //       kProb   z of a piece of the vocabulary once more, turned into that piece of G (bf16, in the workspace);
 //       kGrads  both products of the piece with G: grad W is complete with its piece, grad H adds up over the pieces in fp32.
 //   tfe_xent_few_kernel       the loss of up to 64 rows.
-//   tfe_xent_loss_kernel      joins a row's partial maxima and sums.
+//   tfe_xent_loss_kernel      joins a row's partial maxima and sums with its target's logit.
 //   tfe_xent_rows_kernel      joins grad H's sums, rounds them and puts them back to their rows.
 //
 // All products are 2 N V d operations; the loss makes one, the gradients three (z again and the two with G).  For 2,048 x 151,936 x 1,024 the
@@ -78,7 +78,6 @@ struct GemmParams {
     float *rest;                                // what rounding took from G at each row's target
     uint8_t *wanted;                            // [V / 32]: whether one of these 32 ids is a target
     float2 *part; int64_t ld_part;              // kLse: [2 * units per row][ld_part] maxima and sums
-    float *z_target;
     float *sum_h;                               // kGrads: [splits][m_room][column tiles][kN / 4][kM][4]
     uint32_t *failed;                           // set if a wait ran out
     uint32_t *ticket;                           // kGrads: units handed out so far
@@ -645,12 +644,12 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                             z[j].x = 2 * j < left ? z[j].x : -INFINITY;
                             z[j].y = 2 * j + 1 < left ? z[j].y : -INFINITY;
                         }
-                    if ((uint32_t)mine < (uint32_t)(kN / 2)) {
-                        float zt = 0.f;
+                    if ((uint32_t)mine < (uint32_t)(kN / 2))        // the target takes part where the sums are joined
 #pragma unroll
-                        for (int j = 0; j < kN / 2; ++j) zt = mine == j ? (j & 1 ? z[j / 2].y : z[j / 2].x) : zt;
-                        p.z_target[row] = zt;
-                    }
+                        for (int j = 0; j < kN / 4; ++j) {
+                            z[j].x = mine == 2 * j ? -INFINITY : z[j].x;
+                            z[j].y = mine == 2 * j + 1 ? -INFINITY : z[j].y;
+                        }
                     float best[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) best[i] = top;
@@ -822,7 +821,6 @@ struct FewParams {
     uint32_t give_up;
     const int32_t *target;
     float2 *part; int64_t ld_part;              // [4 * CTAs][ld_part]
-    float *z_target;
 };
 
 template <int TN>
@@ -962,9 +960,9 @@ tfe_xent_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
             if (row >= n_rows) continue;
 #pragma unroll
             for (int j = 0; j < kCols; ++j) {
-                if (target[j] == v) p.z_target[c0 + j] = z[j];
-                const float best = fmaxf(top[j], z[j]);
-                sum[j] = sum[j] * tfe_rows::exp2_approx((top[j] - best) * kLog2e) + tfe_rows::exp2_approx((z[j] - best) * kLog2e);
+                const float x = target[j] == v ? -INFINITY : z[j];  // (the target takes part where the sums are joined)
+                const float best = fmaxf(top[j], x);
+                sum[j] = sum[j] * tfe_rows::exp2_approx((top[j] - best) * kLog2e) + tfe_rows::exp2_approx((x - best) * kLog2e);
                 top[j] = best;
             }
         }
@@ -999,7 +997,6 @@ tfe_xent_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
 struct LossParams {
     int32_t N, V, d, chunks, rows;              // rows: of a block, a power of two
     const float2 *part; int64_t ld_part;
-    const float *z_target;
     const int32_t *target, *pos;                // pos null: rows are where they were
     const uint32_t *failed;                     // null: a failure is in the partial results
     const bf16 *h, *w; int64_t ld_h, ld_w;
@@ -1015,8 +1012,9 @@ __device__ __forceinline__ void fold(float &top, float &sum, float top2, float s
     top = best;
 }
 
-// A row's partial results joined by kLossThreads / rows threads: 5 us for one row (a chain of loads), 16 us for 4,096.  The tensor cores' sum of a target's logit is off by some 1e-7 of its
-// terms, which is all of a loss near zero; so it is summed once more, and takes its place in the sum of exponentials.
+// A row's partial results joined by kLossThreads / rows threads: 5 us for one row (a chain of loads), 16 us for 4,096.  With o the log of
+// the other ids' sum, loss = ln(1 + exp(o - z_t)): however near zero, it is as exact as a fraction as the logits are.  (As lse - z_t with the
+// target in the sums it was off by 1e-7, a tenth of a loss of 1e-6.)  z_t is summed here: the tensor cores cut what they add.
 __global__ void __launch_bounds__(kLossThreads)
 tfe_xent_loss_kernel(const LossParams p)
 {
@@ -1069,13 +1067,11 @@ tfe_xent_loss_kernel(const LossParams p)
         for (int o = kWarps / 2; o > 0; o >>= 1) fold(top, sum, __shfl_xor_sync(0xFFFFFFFFu, top, o), __shfl_xor_sync(0xFFFFFFFFu, sum, o));
         if (lane != 0 || r >= p.N) continue;
         if (at < 0) { p.loss[r] = p.lse[r] = 0.f; continue; }
-        const double z = s_z[i];
-        const float was = p.z_target[at];
-        double lse = (double)top + log((double)sum);
-        lse += (double)log1pf(expf((float)((double)was - lse)) * expm1f((float)(z - (double)was)));
-        if (p.failed && *p.failed) lse = (double)__int_as_float(0x7FFFFFFF);
-        p.lse[r] = (float)lse;
-        p.loss[r] = (float)(lse - z);
+        const double z = s_z[i], others = (double)top + log((double)sum), x = others - z, more = log1p(exp(-fabs(x)));
+        // z_t = -inf: a loss of +inf, the log-sum-exp of the others.  +inf: NaN, as lse - z_t is
+        const bool bad = !(z < INFINITY) || (p.failed && *p.failed);
+        p.lse[r] = bad ? __int_as_float(0x7FFFFFFF) : (float)(fmax(others, z) + more);
+        p.loss[r] = bad ? __int_as_float(0x7FFFFFFF) : (float)(fmax(x, 0.0) + more);
     }
 }
 
@@ -1127,10 +1123,13 @@ tfe_xent_rows_kernel(const RowsParams p)
             if (at >= 0) {
                 const float rest = p.rest[at];
                 const uint2 x = *reinterpret_cast<const uint2 *>(p.w + (int64_t)p.target[at] * p.ld_weight + c);
-                sum.x = fmaf(rest, __uint_as_float(x.x << 16), sum.x);
-                sum.y = fmaf(rest, __uint_as_float(x.x & 0xFFFF0000u), sum.y);
-                sum.z = fmaf(rest, __uint_as_float(x.y << 16), sum.z);
-                sum.w = fmaf(rest, __uint_as_float(x.y & 0xFFFF0000u), sum.w);
+                auto add = [&](float &to, uint32_t weight) {         // (an infinite weight has made the sum what it is)
+                    to = (weight & 0x7FFFFFFFu) == 0x7F800000u ? to : fmaf(rest, __uint_as_float(weight), to);
+                };
+                add(sum.x, x.x << 16);
+                add(sum.y, x.x & 0xFFFF0000u);
+                add(sum.z, x.y << 16);
+                add(sum.w, x.y & 0xFFFF0000u);
             }
             if (failed) sum.x = sum.y = sum.z = sum.w = __int_as_float(0x7FFFFFFF);
             const __nv_bfloat162 lo = __floats2bfloat162_rn(sum.x, sum.y), hi = __floats2bfloat162_rn(sum.z, sum.w);
@@ -1210,13 +1209,12 @@ struct Room {                                   // hands out pieces of the works
     }
 };
 struct ForwardRoom {
-    float2 *part; float *z_target; bf16 *h; int32_t *pos, *target, *n_live; uint32_t *failed;
+    float2 *part; bf16 *h; int32_t *pos, *target, *n_live; uint32_t *failed;
     int64_t bytes;
     ForwardRoom(const Plan &q, int32_t N, int32_t d, void *ws)
     {
         Room r{static_cast<uint8_t *>(ws), 0};
         part = r.take<float2>((int64_t)q.chunks * q.n_pad);
-        z_target = r.take<float>(q.n_pad);
         if (q.gather) { h = r.take<bf16>(q.n_pad * d); pos = r.take<int32_t>(N); target = r.take<int32_t>(q.n_pad); n_live = r.take<int32_t>(1); failed = r.take<uint32_t>(1); }
         else { h = nullptr; pos = target = n_live = nullptr; failed = r.take<uint32_t>(1); }
         bytes = r.used;
@@ -1327,7 +1325,7 @@ tfe_status tfe_xent_forward(const void *hidden, int64_t ld_hidden, int32_t N, co
     if (tfe_status st = device_sms(&sms)) return st;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     LossParams l{};
-    l.N = N; l.V = V; l.chunks = q.chunks; l.part = room.part; l.ld_part = q.n_pad; l.z_target = room.z_target; l.target = target; l.pos = room.pos;
+    l.N = N; l.V = V; l.chunks = q.chunks; l.part = room.part; l.ld_part = q.n_pad; l.target = target; l.pos = room.pos;
     l.loss = loss; l.lse = lse; l.d = d;
     l.h = static_cast<const bf16 *>(hidden); l.ld_h = ld_hidden; l.w = static_cast<const bf16 *>(weight); l.ld_w = ld_weight;
     l.rows = 1;                                 // few rows: a block each
@@ -1341,7 +1339,7 @@ tfe_status tfe_xent_forward(const void *hidden, int64_t ld_hidden, int32_t N, co
         f.rows_per_cta = (f.rows_per_cta + 7) / 8 * 8;
         f.tail_rows = f.rows_per_cta % kFewM;
         f.give_up = g_xent_give_up.load(std::memory_order_relaxed);
-        f.target = target; f.part = room.part; f.ld_part = q.n_pad; f.z_target = room.z_target;
+        f.target = target; f.part = room.part; f.ld_part = q.n_pad;
         const int grid = (V + f.rows_per_cta - 1) / f.rows_per_cta;
         CUtensorMap w, w_tail, h;
         if (!make_map(&w, weight, V, d, ld_weight, kFewM) || !make_map(&w_tail, weight, V, d, ld_weight, f.tail_rows ? (uint32_t)f.tail_rows : 8u) ||
@@ -1366,7 +1364,7 @@ tfe_status tfe_xent_forward(const void *hidden, int64_t ld_hidden, int32_t N, co
     p.N = N; p.V = V; p.d = d; p.tn = q.tn; p.per_unit = q.per_unit; p.n_tiles = q.n_tiles; p.m_room = q.m_room;
     p.give_up = g_xent_give_up.load(std::memory_order_relaxed);
     p.n_live = room.n_live; p.target = q.gather ? room.target : target;
-    p.part = room.part; p.ld_part = q.n_pad; p.z_target = room.z_target; p.failed = room.failed;
+    p.part = room.part; p.ld_part = q.n_pad; p.failed = room.failed;
     l.failed = room.failed;
     if (!q.gather)                              // (cleared with the rows otherwise)
         if (tfe_status st = tfe_note_cuda(cudaMemsetAsync(room.failed, 0, 4, stream), "cudaMemsetAsync")) return st;

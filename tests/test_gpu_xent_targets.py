@@ -1,0 +1,125 @@
+"""Softmax cross entropy where the target decides: logits of -inf, rows that are sure of their target, ids of many rows."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = torch.device("cuda:0")
+HALF_BF16 = 2.0 ** -8
+
+
+def exact(h, w, t, g):
+    """(loss, lse, G, grad_hidden, grad_weight) in float64, G at the target as minus the sum of the others: nothing cancels.  Every row has a target."""
+    h, w, t = h.double(), w.double(), t.long()
+    rows = torch.arange(len(t))
+    z = h @ w.T
+    zt = z[rows, t].clone()
+    z[rows, t] = -float("inf")
+    others = torch.logsumexp(z, 1)
+    x = others - zt
+    loss = torch.clamp(x, min=0) + torch.log1p(torch.exp(-x.abs()))
+    lse = torch.maximum(others, zt) + torch.log1p(torch.exp(-x.abs()))
+    G = torch.exp(z - lse[:, None])
+    G[rows, t] = -G.sum(1)
+    G *= g.double()[:, None]
+    return loss, lse, G, G @ w, G.T @ h
+
+
+def logit_error(h, w):
+    """A logit is a sum of d exact products in fp32: each of its d / 16 joined steps off by at most two half steps (2^-23) of the sum of magnitudes."""
+    return (h.double().abs() @ w.double().abs().T).amax(1) * (h.shape[1] / 16 + 2) * 2.0 ** -23
+
+
+def relative(h, w, lse):
+    """How far a probability, or a sum of them, may be off as a fraction: the errors of two logits, an exponential (2^-22) with four half-steps
+    of its exponent, and a sum over the vocabulary."""
+    return 2 * logit_error(h, w) + 2.0 ** -20 + 4 * 2.0 ** -24 * (2 * lse.abs() + 40) + (len(w) / 512 + 64) * 2.0 ** -24
+
+
+def check_loss(h, w, t):
+    """The loss as a fraction of itself, however near zero."""
+    from paper_2607_07388_b200 import engine
+    loss, lse = engine.xent_forward(*(x.to(DEV) for x in (h, w, t)))
+    e_loss, e_lse, *_ = exact(h, w, t, torch.ones(len(t)))
+    rel = relative(h, w, e_lse)
+    off = (loss.double().cpu() - e_loss).abs()
+    assert bool((off <= e_loss * (rel + 2.0 ** -23)).all()), ("loss", float((off / e_loss).max()))
+    assert bool(((lse.double().cpu() - e_lse).abs() <= rel + 2.0 ** -23 * e_lse.abs()).all())
+    assert engine.xent_status() == 0
+    return loss, lse
+
+
+def weights(rng, v, d):
+    return (torch.randn((v, d), generator=rng) * (2.5 / d ** 0.5)).bfloat16()
+
+
+@pytest.mark.parametrize("n", [9, 150, 700])
+def test_a_target_that_cannot_come(n):
+    """A weight of -inf: the id's logit is -inf in every row.  A row that has it as its target has a loss of +inf and a finite log-sum-exp, and
+    its gradient is finite but where it meets that weight itself."""
+    from paper_2607_07388_b200 import engine
+    rng = torch.Generator().manual_seed(n)
+    w = weights(rng, 500, 64)
+    t = torch.randint(0, 500, (n,), generator=rng)
+    h = (torch.randn((n, 64), generator=rng) + 1.5 * w[t].float()).bfloat16()
+    t = torch.where(t == 77, 78, t).int()
+    g = torch.rand(n, generator=rng) + 0.1
+    h[:, 5] = 0.5
+    w[77, 5] = -float("inf")
+    r = n // 2
+    t[r] = 77
+    loss, lse = engine.xent_forward(*(x.to(DEV) for x in (h, w, t)))
+    keep = torch.arange(500) != 77
+    z = h.double() @ w[keep].double().T
+    e_lse = torch.logsumexp(z, 1)
+    assert float((lse.double().cpu() - e_lse).abs().max()) <= 1e-5 * float(e_lse.abs().max() + 1)
+    rest = torch.arange(n) != r
+    assert float(loss[r]) == float("inf") and bool(torch.isfinite(loss.cpu()[rest]).all())
+    gh, gw = engine.xent_backward(*(x.to(DEV) for x in (g, h, w, t)), lse)
+    G = torch.zeros((n, 500), dtype=torch.float64)
+    G[:, keep] = torch.exp(z - e_lse[:, None])
+    G[torch.arange(n), t.long()] -= 1
+    G *= g.double()[:, None]
+    e_gw = G.T @ h.double()
+    assert bool(torch.isfinite(gw.float()).all())
+    # both roundings, of G and of the result, are 2^-8 at most of what is rounded
+    assert float((gw.double().cpu() - e_gw).norm() / e_gw.norm()) <= 2.0 ** -7
+    assert float((gw[77].double().cpu() - e_gw[77]).norm() / e_gw[77].norm()) <= 2.0 ** -8 + 1e-5
+    columns = torch.arange(64) != 5
+    e_gh = (G[:, keep] @ w[keep].double() + G[:, 77:78] * torch.where(columns, w[77].double(), 0.0))[:, columns]
+    assert float((gh.double().cpu()[:, columns] - e_gh).norm() / e_gh.norm()) <= 2.0 ** -7
+    assert float(gh[r, 5]) == float("inf")
+    # +inf at the target: NaN, as anywhere
+    w[77, 5] = float("inf")
+    loss, lse = engine.xent_forward(*(x.to(DEV) for x in (h, w, t)))
+    assert torch.isnan(loss[r]) and torch.isnan(lse[r])
+    assert engine.xent_status() == 0
+
+
+def sure_rows(seed, n, v, d):
+    """Rows whose 1 - p runs from 1e-2 to 1e-6: hidden states along their target's weights, as far as it takes."""
+    rng = torch.Generator().manual_seed(seed)
+    w = weights(rng, v, d)
+    t = torch.randperm(v, generator=rng)[:n].int()
+    h = 0.3 * torch.randn((n, d), generator=rng)
+    z = h.double() @ w.double().T
+    own, along = w[t.long()].double(), w[t.long()].double() @ w.double().T
+    want = torch.logspace(-2, -6, n, dtype=torch.float64)
+    lo, hi = torch.zeros(n, dtype=torch.float64), torch.full((n,), 20.0, dtype=torch.float64)
+    rows = torch.arange(n)
+    for _ in range(40):
+        k = (lo + hi) / 2
+        p = torch.softmax(z + k[:, None] * along, 1)
+        p[rows, t.long()] = 0
+        more = p.sum(1) > want
+        lo, hi = torch.where(more, k, lo), torch.where(more, hi, k)
+    h = (h.double() + lo[:, None] * own).bfloat16()
+    return h, w, t, torch.rand(n, generator=rng) + 0.5
+
+
+SURE = [(1, 300, 1024), (40, 2000, 1024), (150, 2000, 1024), (300, 3001, 1024), (40, 2000, 4096), (270, 1200, 4096), (300, 3001, 64)]
+
+
+@pytest.mark.parametrize("n,v,d", SURE)
+def test_loss_of_rows_that_are_sure_of_their_target(n, v, d):
+    loss, _ = check_loss(*sure_rows(n + d, n, v, d)[:3])
+    assert float(loss.min()) > 0 and (float(loss.min()) < 1e-4 or n == 1)
