@@ -5,14 +5,15 @@
 //     G_nv = g_n (exp(z_v - lse) - [v = t])       grad H = G W                grad W = G^T H
 //
 //   tfe_xent_compact_kernel   lists the rows that have a target (and a gradient) and copies their hidden states together: the
-//                             products below run over those rows only, and a row that has none takes part in no sum.
+//                             products below run over those rows only, and a row that has none takes part in no sum.  For the
+//                             gradients the rows are put in the order of their targets.
 //   tfe_xent_gemm_kernel      one persistent, warp-specialised tcgen05 kernel with three epilogues:
 //       kLse    z tile by tile, each kept only as its row maxima and row sums of exponentials, the rows' targets left out;
 //       kProb   z of a piece of the vocabulary once more, turned into that piece of G (bf16, in the workspace);
 //       kGrads  both products of the piece with G: grad W is complete with its piece, grad H adds up over the pieces in fp32.
 //   tfe_xent_few_kernel       the loss of up to 64 rows.
 //   tfe_xent_loss_kernel      joins a row's partial maxima and sums with its target's logit.
-//   tfe_xent_rows_kernel      joins grad H's sums, rounds them and puts them back to their rows.
+//   tfe_xent_rows_kernel      joins grad H's sums, rounds them and puts them back to their rows; completes grad W's rows of the targets.
 //
 // All products are 2 N V d operations; the loss makes one, the gradients three (z again and the two with G).  For 2,048 x 151,936 x 1,024 the
 // tensor cores bound all of it: 479 us the loss (1.33 PFLOP/s), 462 us z again, 1,030 us both products with G with the card idle before; back
@@ -74,9 +75,9 @@ struct GemmParams {
     const int32_t *n_live;                      // rows taken part in (null: N)
     const int32_t *target;
     const float *lse, *coef;
-    const bf16 *h;                              // kGrads: the rows together, d apart
     float *rest;                                // what rounding took from G at each row's target
-    uint8_t *wanted;                            // [V / 32]: whether one of these 32 ids is a target
+    uint32_t *first_row;                        // [V]: the first row whose target is this id, kNone where there is none
+    float *sum_w; int32_t by_id;                // kGrads: rows of grad W before they are rounded, d apart: of the ids that are targets, by their first row, or of all ids
     float2 *part; int64_t ld_part;              // kLse: [2 * units per row][ld_part] maxima and sums
     float *sum_h;                               // kGrads: [splits][m_room][column tiles][kN / 4][kM][4]
     uint32_t *failed;                           // set if a wait ran out
@@ -95,31 +96,44 @@ struct CompactParams {
     float *lse_out, *coef_out;
     uint32_t *failed;                           // cleared here, with the units' counters behind it
     int32_t counters;
-    uint8_t *wanted;                            // cleared here (null: the loss)
+    uint32_t *first_row;                        // set to kNone here
+    int32_t *group_at;                          // where each kGroup rows begin among those that take part, and their end
 };
+constexpr uint32_t kNone = 0xFFFFFFFFu;
+// Rows are ordered by their targets within this many: every row is compared with all others of its group, so the work is linear in
+// the rows.  131,072 rows x 256: 300 us (of 10.8 ms for both gradients against 32,003 ids); in groups of 32,768 830 us, and 50 us less
+// where an id's runs are put together.
+constexpr int32_t kGroup = 8192;
 
-// Every block counts the rows before its own by itself, so one launch does: 4 us for 256 rows of 1,024, 9.5 us for 4,096 of which 30 % are left out.
-constexpr int kCompactThreads = 256;
+// Every block counts the rows before its own by itself, so one launch does.
+constexpr int kCompactThreads = 256, kTile = 4 * kCompactThreads;
 
+template <bool kOrdered>
 __global__ void __launch_bounds__(kCompactThreads)
 tfe_xent_compact_kernel(const CompactParams p)
 {
     __shared__ int32_t s_before[kCompactThreads / 32], s_all[kCompactThreads / 32];
-    __shared__ int32_t s_from[kCompactThreads];
+    __shared__ int32_t s_from[kCompactThreads], s_to[kCompactThreads];
+    __shared__ __align__(16) int32_t s_key[kOrdered ? kTile : 4];
     tfe_wait_for_stream();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int64_t r0 = (int64_t)blockIdx.x * p.rows_per_block, r1 = min((int64_t)p.N, r0 + p.rows_per_block);
-    auto live = [&](int64_t r) {
-        const int32_t t = p.target[r];
-        return t >= 0 && t < p.V && (!p.grad || !(p.grad[r] == 0.f));
+    const int64_t from = kOrdered ? r0 / kGroup * kGroup : r0;      // what lies before it comes before all of this block's
+    constexpr int32_t kNever = 1 << 30;
+    auto key = [&](int64_t r) {                 // a row's target, or more than any (no branches: loads in a loop stay together)
+        const int64_t at = min(r, (int64_t)p.N - 1);
+        const int32_t t = p.target[at];
+        const float g = kOrdered ? p.grad[at] : 1.f;
+        const bool ok = (r < p.N) & ((uint32_t)t < (uint32_t)p.V) & !(g == 0.f);
+        return ok ? t : kNever;
     };
     // how many before this block's rows, and in all (every block counts for itself: the targets are a few KB in L2)
     int32_t before = 0, all = 0;
 #pragma unroll 8
     for (int64_t r = tid; r < p.N; r += kCompactThreads) {
-        const int32_t one = live(r);
+        const int32_t one = key(r) != kNever;
         all += one;
-        before += r < r0 ? one : 0;
+        before += r < from ? one : 0;
     }
     before = __reduce_add_sync(0xFFFFFFFFu, before);
     all = __reduce_add_sync(0xFFFFFFFFu, all);
@@ -130,30 +144,78 @@ tfe_xent_compact_kernel(const CompactParams p)
     if (blockIdx.x == 0 && tid == 0) *p.n_live = all;
     if (blockIdx.x == 0)
         for (int32_t i = tid; i <= p.counters; i += kCompactThreads) p.failed[i] = 0;
+    if (kOrdered && r0 == from && r0 < p.N && tid == 0) p.group_at[r0 / kGroup] = before;
+    if (kOrdered && blockIdx.x == 0 && tid == 0) p.group_at[(p.N + kGroup - 1) / kGroup] = all;
     const int vecs = p.d / 8;
-    for (int64_t base = r0; base < r1; base += kCompactThreads) {
-        const int64_t r = base + tid;
-        const bool one = r < r1 && live(r);
-        const uint32_t vote = __ballot_sync(0xFFFFFFFFu, one);
+    const int32_t batch = kOrdered ? min(p.rows_per_block, kCompactThreads) : kCompactThreads;      // rows at a time
+    for (int64_t base = r0; base < r1; base += batch) {
+        int32_t total = 0;
         __syncthreads();
-        if (lane == 0) s_before[warp] = __popc(vote);
-        __syncthreads();
-        int32_t at = before, total = 0;
-        for (int w = 0; w < kCompactThreads / 32; ++w) { at += w < warp ? s_before[w] : 0; total += s_before[w]; }
-        at += __popc(vote & ((1u << lane) - 1u));
-        if (r < r1) p.pos[r] = one ? at : -1;
-        if (one) {
-            s_from[at - before] = tid;
-            p.target_out[at] = p.target[r];
-            if (p.grad) { p.lse_out[at] = p.lse[r]; p.coef_out[at] = p.grad[r]; }
+        if constexpr (kOrdered) {
+            // a row's place is the number of those of its group that come before it: by their targets, and as they were where those are the same
+            const int32_t parts = kCompactThreads / batch, mine = tid & (batch - 1), part = tid / batch;
+            const int32_t t = key(base + mine);
+            if (tid < batch) s_to[tid] = before;
+            int32_t count = 0;
+            const int64_t end = min((int64_t)p.N, from + kGroup);
+            int32_t next[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) next[i] = key(from + tid + i * kCompactThreads);
+            for (int64_t at = from; at < end; at += kTile) {
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s_key[tid + i * kCompactThreads] = next[i];
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < 4; ++i) next[i] = key(at + kTile + tid + i * kCompactThreads);
+                if (at + kTile <= base || at >= base + batch) {
+                    const int32_t below = t + (at < base ? 1 : 0);          // (if t is kNever, its place is not used)
+#pragma unroll 8
+                    for (int32_t i = part; i < kTile / 4; i += parts) {
+                        const int4 x = reinterpret_cast<const int4 *>(s_key)[i];
+                        count += (x.x < below) + (x.y < below) + (x.z < below) + (x.w < below);
+                    }
+                } else {
+                    const int32_t own = (int32_t)(base + mine - at);
+#pragma unroll 8
+                    for (int32_t i = part; i < kTile / 4; i += parts) {
+                        const int4 x = reinterpret_cast<const int4 *>(s_key)[i];
+                        count += (x.x < t + (4 * i < own)) + (x.y < t + (4 * i + 1 < own)) + (x.z < t + (4 * i + 2 < own)) + (x.w < t + (4 * i + 3 < own));
+                    }
+                }
+            }
+            atomicAdd(&s_to[mine], count);
+            __syncthreads();
+            if (tid < batch) {
+                const int64_t r = base + tid;
+                const int32_t at = t != kNever ? s_to[tid] : -1;
+                s_to[tid] = at;
+                if (r < r1) p.pos[r] = at;
+                if (at >= 0) { p.target_out[at] = t; p.lse_out[at] = p.lse[r]; p.coef_out[at] = p.grad[r]; }
+            }
+            total = batch;
+        } else {
+            const int64_t r = base + tid;
+            const bool one = r < r1 && key(r) != kNever;
+            const uint32_t vote = __ballot_sync(0xFFFFFFFFu, one);
+            if (lane == 0) s_before[warp] = __popc(vote);
+            __syncthreads();
+            int32_t at = before;
+            for (int w = 0; w < kCompactThreads / 32; ++w) { at += w < warp ? s_before[w] : 0; total += s_before[w]; }
+            at += __popc(vote & ((1u << lane) - 1u));
+            if (r < r1) p.pos[r] = one ? at : -1;
+            if (one) {
+                s_from[at - before] = tid;
+                p.target_out[at] = p.target[r];
+            }
         }
         __syncthreads();
 #pragma unroll 4
         for (int32_t i = tid; i < total * vecs; i += kCompactThreads) {        // whose row it is does not matter: all loads at once
-            const int32_t k = i / vecs, v = i - k * vecs;
-            reinterpret_cast<uint4 *>(p.h_out + (int64_t)(before + k) * p.d)[v] = __ldg(reinterpret_cast<const uint4 *>(p.h + (base + s_from[k]) * p.ld) + v);
+            const int32_t k = i / vecs, v = i - k * vecs, row = kOrdered ? k : s_from[k], at = kOrdered ? s_to[k] : before + k;
+            if (at >= 0) reinterpret_cast<uint4 *>(p.h_out + (int64_t)at * p.d)[v] = __ldg(reinterpret_cast<const uint4 *>(p.h + (base + row) * p.ld) + v);
         }
-        before += total;
+        if (!kOrdered) before += total;
     }
     // zeros up to the end of the last tile: the sums over rows run to there
     const int64_t end = max((int64_t)(all + kM - 1) / kM, (int64_t)1) * kM;
@@ -162,8 +224,9 @@ tfe_xent_compact_kernel(const CompactParams p)
     for (int64_t i = (int64_t)blockIdx.x * kCompactThreads + tid; i < n_zero; i += (int64_t)gridDim.x * kCompactThreads) dst[i] = make_uint4(0, 0, 0, 0);
     if (blockIdx.x == 0)
         for (int64_t i = all + tid; i < end; i += kCompactThreads) p.target_out[i] = -1;
-    if (p.wanted)
-        for (int64_t i = (int64_t)blockIdx.x * kCompactThreads + tid; i <= p.V >> 5; i += (int64_t)gridDim.x * kCompactThreads) p.wanted[i] = 0;
+    if constexpr (kOrdered)                     // (there is room up to the next multiple of 4)
+        for (int64_t i = (int64_t)blockIdx.x * kCompactThreads + tid; i < (p.V + 3) / 4; i += (int64_t)gridDim.x * kCompactThreads)
+            reinterpret_cast<uint4 *>(p.first_row)[i] = make_uint4(kNone, kNone, kNone, kNone);
 }
 
 // ------------------------------------------------------------------ the products
@@ -346,52 +409,9 @@ __device__ __forceinline__ void pair_tmem_dealloc(uint32_t taddr, uint32_t cols)
 }
 
 // What rounding G to bf16 takes away weighs most at a row's target, where G is largest and its error is one factor for a whole row of
-// grad W.  That difference is kept in fp32 and added to the sums: to grad H where its parts are joined, to grad W by the epilogue
-// that rounds it.  A thread holds one row v of grad W and adds the first kHits rows whose target is v; among more the errors
-// average out.  (33 x 32,003: the gradients are off by 1.53 times their own rounding without it.)
-constexpr int kHits = 4;
-
-// The first rows whose target is v0 + lane, ascending, -1 where there are none.
-__device__ __forceinline__ void find_targets(const GemmParams &p, int32_t n_live, int32_t v0, int lane, int32_t (&hit)[kHits])
-{
-#pragma unroll
-    for (int i = 0; i < kHits; ++i) hit[i] = -1;
-    uint32_t seek = 0xFFFFFFFFu;                // the ids that may have more rows
-    if (p.V - v0 < 32) seek = (1u << (p.V - v0)) - 1u;
-    for (int32_t base = 0; base < n_live && seek; base += 128) {    // (targets beyond the last row are -1)
-        const int4 t = *reinterpret_cast<const int4 *>(p.target + base + 4 * lane);
-        auto sought = [&](int32_t id) { return (uint32_t)(id - v0) < 32u && (seek >> (id - v0) & 1u); };
-        const bool any = sought(t.x) || sought(t.y) || sought(t.z) || sought(t.w);
-        for (uint32_t from = __ballot_sync(0xFFFFFFFFu, any); from; from &= from - 1) {
-            const int l = __ffs(from) - 1;
-            const int32_t four[4] = {__shfl_sync(0xFFFFFFFFu, t.x, l), __shfl_sync(0xFFFFFFFFu, t.y, l), __shfl_sync(0xFFFFFFFFu, t.z, l), __shfl_sync(0xFFFFFFFFu, t.w, l)};
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (four[e] == v0 + lane) {
-                    int32_t at = base + 4 * l + e;
-#pragma unroll
-                    for (int i = 0; i < kHits; ++i)
-                        if (hit[i] < 0) { hit[i] = at; at = -1; }
-                }
-        }
-        seek &= ~__ballot_sync(0xFFFFFFFFu, hit[kHits - 1] >= 0);
-    }
-}
-// 16 columns from `col` of row `at`'s hidden state, times what is left of its G, to y
-__device__ __forceinline__ void add_rest(const GemmParams &p, int32_t at, int32_t col, float2 (&y)[8])
-{
-    if (at < 0) return;
-    const float rest = p.rest[at];
-    const float2 by = make_float2(rest, rest);
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-        if (col + 8 * i < p.d) {
-            float f[8];
-            tfe_rows::Elem<bf16>::unpack(*reinterpret_cast<const uint4 *>(p.h + (int64_t)at * p.d + col + 8 * i), f);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) y[4 * i + j] = __ffma2_rn(make_float2(f[2 * j], f[2 * j + 1]), by, y[4 * i + j]);
-        }
-}
+// grad W; and with one coefficient for all rows, a mean, it is nearly the same factor in every row of an id.  That difference is kept in
+// fp32 (rest), and the sums over it are added to the products before those are rounded: grad H's where its parts are joined, grad W's in the
+// same kernel, for which the rows of the ids that are targets are kept in fp32 (sum_w).
 
 // The gradients' units, of two lengths, go to the pairs as they come free, in an order in which those under way together read the same
 // operands: 2,048 x 50,688 x 1,024 take 321 us, with equal shares that each pair works off by itself 450 us.  The order of every sum is
@@ -597,13 +617,16 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
             const Unit w = units.at(p, u);
             const int32_t row = w.a_at + row_in_tile;
             const bool live = row < units.n_live;                   // (grad W's rows are the vocabulary's: it has no use for this)
-            int32_t target = -1, hit[kHits];
+            int32_t target = -1;
             float lse = 0.f, coef = 0.f, top = -3.4e38f;
             float2 sum = make_float2(0.f, 0.f);
             if (kOp != kGrads && live) target = p.target[row];
             if (kOp == kProb && live) { lse = p.lse[row]; coef = p.coef[row]; }
-            const int32_t v_first = p.v0 + w.a_at + first_row;      // grad W: this warp's first vocabulary row, a multiple of 32
-            const bool wanted = kOp == kGrads && !w.grad_h && v_first < p.V && p.wanted[v_first >> 5];
+            float *kept_row = nullptr;                              // grad W: where this thread's vocabulary row is kept in fp32, if it is a target
+            if (kOp == kGrads && !w.grad_h && p.v0 + row < p.V) {
+                const uint32_t at = p.first_row[p.v0 + row];
+                if (at != kNone) kept_row = p.sum_w + (p.by_id ? (int64_t)(p.v0 + row) : (int64_t)at) * p.d + w.b_at + c0;
+            }
             for (int32_t t = 0; t < w.tiles; ++t) {
                 float4 *at = nullptr;                               // grad H's sums of this row, four columns each
                 if constexpr (kOp == kGrads) {
@@ -675,8 +698,6 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                 ok = mbar_wait(smem_u32(&s_acc_full[buf]), buf_phase, &s_abort);
                 if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
                 tc_fence_after();
-                if constexpr (kOp == kGrads)
-                    if (wanted) find_targets(p, units.n_live, v_first, lane, hit);
                 const uint32_t taddr = tmem_base + ((quarter * 32u) << 16) + buf * kN + (uint32_t)c0;
                 auto release = [&] {
                     tc_fence_before();
@@ -706,7 +727,7 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                                 for (int j = 0; j < 16; ++j) z = mine - c == j ? __uint_as_float(x[j]) : z;
                                 const float g = coef * expm1f(z - lse), kept = __bfloat162float(__float2bfloat16_rn(g));
                                 p.rest[row] = g - kept;
-                                p.wanted[target >> 5] = 1;
+                                atomicMin(p.first_row + target, (uint32_t)row);
 #pragma unroll
                                 for (int j = 0; j < 8; ++j) {
                                     y[j].x = mine - c == 2 * j ? kept : y[j].x;
@@ -723,12 +744,11 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                                     y[j].y = c + 2 * j + 1 < left ? y[j].y : 0.f;
                                 }
                         } else {
-                            if (wanted)
+                            if (kept_row)
 #pragma unroll
-                                for (int i = 0; i < kHits; ++i) {
-                                    if (!__any_sync(0xFFFFFFFFu, hit[i] >= 0)) break;
-                                    add_rest(p, hit[i], w.b_at + c0 + c, y);
-                                }
+                                for (int i = 0; i < 4; ++i)
+                                    if (w.b_at + c0 + c + 4 * i < p.d)
+                                        *reinterpret_cast<float4 *>(kept_row + c + 4 * i) = make_float4(y[2 * i].x, y[2 * i].y, y[2 * i + 1].x, y[2 * i + 1].y);
                         }
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
@@ -1078,13 +1098,130 @@ tfe_xent_loss_kernel(const LossParams p)
 struct RowsParams {
     int32_t N, V, d, splits, m_room, cols, tn, groups;          // groups: of 32 columns
     const float *sum_h, *rest;
-    const int32_t *pos, *target;
-    const bf16 *w; int64_t ld_weight;
-    const uint32_t *failed;
+    const int32_t *pos, *target, *n_live;
+    const bf16 *h, *w; int64_t ld_weight;       // h: the rows together, d apart
+    const uint32_t *failed, *first_row;
+    float *sum_w; int32_t by_id;
+    const int32_t *group_at;
+    int32_t slices, id_blocks;                  // slices of columns; blocks for the targets' rows of grad W, which are the first
     bf16 *grad_h; int64_t ld_h;
     bf16 *grad_w; int64_t ld_w;
 };
 constexpr int kRowsThreads = 256;
+
+// Completes the rows of grad W of the targets: the row that was kept, and the sum over the id's rows of rest h, rounded.  The rows lie in
+// the order of their targets, so those of an id are one run in each group.  A block looks at kSpan rows and takes the ids whose first row
+// is among them, 256 columns: a warp for each id, or the whole block where the first run is longer than kLong, its warps in turn.
+constexpr int kSpan = 32, kLong = 64, kSlice = 256;
+
+struct Run { int32_t at, end; };
+// The run of an id that begins at `at`, or is sought from there to `end` (a warp's work).
+__device__ __forceinline__ int32_t run_end(const int32_t *target, int32_t at, int32_t end, int32_t id, int lane)
+{
+    for (; at < end; at += 32) {
+        const uint32_t other = __ballot_sync(0xFFFFFFFFu, at + lane >= end || target[at + lane] != id);
+        if (other) return at + __ffs(other) - 1;
+    }
+    return end;
+}
+__device__ __forceinline__ int32_t find_run(const int32_t *target, int32_t lo, int32_t hi, int32_t id, int lane)      // the first that is not below id
+{
+    while (lo < hi) {
+        const int32_t step = (hi - lo + 31) / 32, at = lo + lane * step;
+        const uint32_t below = __ballot_sync(0xFFFFFFFFu, at < hi && target[at] < id);        // a run of ones from lane 0
+        const int32_t n = __popc(below);
+        if (n == 0) return lo;
+        hi = min(hi, lo + n * step);
+        lo += (n - 1) * step + 1;
+    }
+    return lo;
+}
+// rest h over the rows from `at`, every step-th, eight columns
+__device__ __forceinline__ void add_rows(const RowsParams &p, int32_t at, int32_t end, int32_t step, int32_t c, float (&acc)[8])
+{
+#pragma unroll 4
+    for (int32_t k = at; k < end; k += step) {
+        float f[8];
+        tfe_rows::Elem<bf16>::unpack(__ldg(reinterpret_cast<const uint4 *>(p.h + (int64_t)k * p.d + c)), f);
+        const float by = p.rest[k];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] = fmaf(by, f[j], acc[j]);
+    }
+}
+__device__ __forceinline__ void finish_row(const RowsParams &p, int32_t id, int32_t first, int32_t c, const float (&acc)[8])
+{
+    const float4 *kept = reinterpret_cast<const float4 *>(p.sum_w + (p.by_id ? (int64_t)id : (int64_t)first) * p.d + c);
+    const float4 a = kept[0], b = kept[1];
+    const float f[8] = {a.x + acc[0], a.y + acc[1], a.z + acc[2], a.w + acc[3], b.x + acc[4], b.y + acc[5], b.z + acc[6], b.w + acc[7]};
+    *reinterpret_cast<uint4 *>(p.grad_w + (int64_t)id * p.ld_w + c) = tfe_rows::Elem<bf16>::pack(f);
+}
+
+__device__ __forceinline__ void finish_targets(const RowsParams &p, int32_t first, int32_t column)
+{
+    __shared__ float4 s_part[kRowsThreads / 32][2][32];
+    __shared__ uint32_t s_long;
+    constexpr int kWarps = kRowsThreads / 32;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int32_t n_live = *p.n_live, all_groups = (p.N + kGroup - 1) / kGroup, c = column + lane * 8;
+    if (first >= n_live) return;
+    const int32_t mine = first + lane < n_live ? p.target[first + lane] : -1;
+    const uint32_t heads = __ballot_sync(0xFFFFFFFFu, mine >= 0 && p.first_row[mine] == (uint32_t)(first + lane));
+    if (threadIdx.x == 0) s_long = 0;
+    __syncthreads();
+    int32_t group = 0;                          // that these rows are in
+    while (group + 1 < all_groups && p.group_at[group + 1] <= first) ++group;
+    auto next_run = [&](Run &r, int32_t &g, int32_t id) {           // in the groups behind
+        for (++g; g < all_groups; ++g) {
+            const int32_t end = p.group_at[g + 1];
+            r.at = find_run(p.target, p.group_at[g], end, id, lane);
+            r.end = run_end(p.target, r.at, end, id, lane);
+            if (r.at < r.end) return true;
+        }
+        return false;
+    };
+    int32_t turn = 0;
+    for (uint32_t left = heads; left; left &= left - 1, ++turn) {
+        if (turn % kWarps != warp) continue;
+        const int32_t l = __ffs(left) - 1, id = __shfl_sync(0xFFFFFFFFu, mine, l);
+        int32_t g = group;
+        while (g + 1 < all_groups && p.group_at[g + 1] <= first + l) ++g;      // (the block's rows may run over a group's end)
+        Run r{first + l, 0};
+        r.end = run_end(p.target, r.at, p.group_at[g + 1], id, lane);
+        if (r.end - r.at > kLong) {
+            if (lane == 0) atomicOr(&s_long, 1u << l);
+            continue;
+        }
+        float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        do {
+            if (c < p.d) add_rows(p, r.at, r.end, 1, c, acc);
+        } while (next_run(r, g, id));
+        if (c < p.d) finish_row(p, id, first + l, c, acc);
+    }
+    __syncthreads();
+    for (uint32_t left = s_long; left; left &= left - 1) {
+        const int32_t l = __ffs(left) - 1, id = __shfl_sync(0xFFFFFFFFu, mine, l);
+        int32_t g = group;
+        while (g + 1 < all_groups && p.group_at[g + 1] <= first + l) ++g;
+        Run r{first + l, 0};
+        r.end = run_end(p.target, r.at, p.group_at[g + 1], id, lane);
+        float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        do {
+            if (c < p.d) add_rows(p, r.at + warp, r.end, kWarps, c, acc);
+        } while (next_run(r, g, id));
+        __syncthreads();
+        s_part[warp][0][lane] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+        s_part[warp][1][lane] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+        __syncthreads();
+        if (warp == 0) {
+            for (int w = 1; w < kWarps; ++w) {
+                const float4 x = s_part[w][0][lane], y = s_part[w][1][lane];
+                acc[0] += x.x; acc[1] += x.y; acc[2] += x.z; acc[3] += x.w;
+                acc[4] += y.x; acc[5] += y.y; acc[6] += y.z; acc[7] += y.w;
+            }
+            if (c < p.d) finish_row(p, id, first + l, c, acc);
+        }
+    }
+}
 
 // grad H's sums over the parts, rounded, to their rows, a block for 32 rows and 32 columns; NaN everywhere if a product before it failed.
 // Bound by the read of the parts: 17 us for 4,096 x 1,024.
@@ -1095,9 +1232,12 @@ tfe_xent_rows_kernel(const RowsParams p)
     tfe_wait_for_stream();
     const bool failed = *p.failed != 0;
     const bf16 nan = __float2bfloat16_rn(__int_as_float(0x7FFFFFFF));
-    if (p.grad_h) {
-        const int64_t r0 = blockIdx.x / p.groups * 32ll;
-        const int32_t c0 = (int32_t)(blockIdx.x % p.groups) * 32;
+    if (blockIdx.x < p.id_blocks) {
+        if (!failed) finish_targets(p, (int32_t)(blockIdx.x / p.slices) * kSpan, (int32_t)(blockIdx.x % p.slices) * kSlice);
+    } else {
+        const uint32_t block = blockIdx.x - p.id_blocks;
+        const int64_t r0 = block / p.groups * 32ll;
+        const int32_t c0 = (int32_t)(block % p.groups) * 32;
         {
             const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
             const int32_t at = r0 + lane < p.N ? p.pos[r0 + lane] : -1, c = c0 + 4 * warp;
@@ -1221,7 +1361,7 @@ struct ForwardRoom {
     }
 };
 struct BackwardRoom {
-    bf16 *g, *h; float *sum_h, *lse, *coef, *rest; int32_t *pos, *target, *n_live; uint32_t *failed; uint8_t *wanted;
+    bf16 *g, *h; float *sum_h, *sum_w, *lse, *coef, *rest; int32_t *pos, *target, *n_live, *group_at; uint32_t *failed, *first_row;
     int64_t bytes;
     BackwardRoom(const Plan &q, int32_t N, int32_t V, int32_t d, void *ws)
     {
@@ -1231,7 +1371,9 @@ struct BackwardRoom {
         sum_h = r.take<float>((int64_t)q.splits * q.m_room * q.cols * kM * kN);
         lse = r.take<float>(q.n_pad); coef = r.take<float>(q.n_pad); rest = r.take<float>(q.n_pad);
         pos = r.take<int32_t>(N); target = r.take<int32_t>(q.n_pad); n_live = r.take<int32_t>(1); failed = r.take<uint32_t>(1 + (int64_t)q.pieces);
-        wanted = r.take<uint8_t>((V >> 5) + 1);
+        first_row = r.take<uint32_t>(V);
+        group_at = r.take<int32_t>((N + kGroup - 1) / kGroup + 1);
+        sum_w = r.take<float>(std::min<int64_t>(q.n_pad, V) * d);
         bytes = r.used;
     }
 };
@@ -1276,9 +1418,15 @@ tfe_status launch_gemm(int64_t most_units, int sms, cudaStream_t stream, const M
 
 tfe_status launch_compact(CompactParams c, int sms, cudaStream_t stream)
 {
+    const bool ordered = c.first_row != nullptr;
     c.rows_per_block = (int32_t)std::max<int64_t>(8, (c.N + 2ll * sms - 1) / (2ll * sms));
+    if (ordered) {                              // a power of two: no block lies in two groups
+        int32_t rows = 8;
+        while (rows < c.rows_per_block && rows < kGroup) rows *= 2;
+        c.rows_per_block = rows;
+    }
     const unsigned grid = (unsigned)std::max<int64_t>(64, ((int64_t)c.N + c.rows_per_block - 1) / c.rows_per_block);     // (few rows: zeros to write)
-    return tfe_launch_serial(tfe_xent_compact_kernel, grid, kCompactThreads, 1, 0, stream, "cross entropy rows launch", c);
+    return tfe_launch_serial(ordered ? tfe_xent_compact_kernel<true> : tfe_xent_compact_kernel<false>, grid, kCompactThreads, 1, 0, stream, "cross entropy rows launch", c);
 }
 
 bool touch(const void *a, int64_t a_bytes, const void *b, int64_t b_bytes)
@@ -1402,7 +1550,7 @@ tfe_status tfe_xent_backward(const void *hidden, int64_t ld_hidden, int32_t N, c
     CompactParams c{};
     c.N = N; c.V = V; c.d = d; c.h = static_cast<const bf16 *>(hidden); c.ld = ld_hidden; c.target = target; c.lse = lse; c.grad = grad_loss;
     c.h_out = room.h; c.pos = room.pos; c.target_out = room.target; c.n_live = room.n_live; c.lse_out = room.lse; c.coef_out = room.coef; c.failed = room.failed;
-    c.counters = q.pieces; c.wanted = room.wanted;
+    c.counters = q.pieces; c.first_row = room.first_row; c.group_at = room.group_at;
     if (tfe_status st = launch_compact(c, sms, stream)) return st;
 
     // G lies in blocks of 64 columns, one below the other: whichever way a product reads it, a tile is one run of memory
@@ -1417,7 +1565,7 @@ tfe_status tfe_xent_backward(const void *hidden, int64_t ld_hidden, int32_t N, c
     p.N = N; p.V = V; p.d = d; p.n_pad = (int32_t)q.n_pad; p.m_room = q.m_room; p.splits = q.splits;
     p.want_h = grad_hidden != nullptr; p.want_w = grad_weight != nullptr;
     p.give_up = g_xent_give_up.load(std::memory_order_relaxed);
-    p.n_live = room.n_live; p.target = room.target; p.lse = room.lse; p.coef = room.coef; p.sum_h = room.sum_h; p.failed = room.failed; p.h = room.h; p.rest = room.rest; p.wanted = room.wanted;
+    p.n_live = room.n_live; p.target = room.target; p.lse = room.lse; p.coef = room.coef; p.sum_h = room.sum_h; p.failed = room.failed; p.rest = room.rest; p.first_row = room.first_row; p.sum_w = room.sum_w; p.by_id = V <= q.n_pad;
     for (int32_t i = 0; i < q.pieces; ++i) {
         p.v0 = (int32_t)(i * q.piece);
         p.width = (int32_t)std::min<int64_t>(q.piece, V - (int64_t)i * q.piece);
@@ -1432,8 +1580,12 @@ tfe_status tfe_xent_backward(const void *hidden, int64_t ld_hidden, int32_t N, c
     RowsParams r{};
     r.N = N; r.V = V; r.d = d; r.splits = q.splits; r.m_room = q.m_room; r.cols = q.cols; r.tn = q.tn_d; r.sum_h = room.sum_h; r.pos = room.pos;
     r.failed = room.failed; r.rest = room.rest; r.target = room.target; r.w = static_cast<const bf16 *>(weight); r.ld_weight = ld_weight; r.grad_h = static_cast<bf16 *>(grad_hidden); r.ld_h = ld_grad_hidden; r.grad_w = static_cast<bf16 *>(grad_weight); r.ld_w = ld_grad_weight;
-    r.groups = grad_hidden ? (d + 31) / 32 : 1;
-    const unsigned grid = (unsigned)((N + 31) / 32 * r.groups);
+    r.h = room.h; r.n_live = room.n_live; r.first_row = room.first_row; r.sum_w = room.sum_w; r.by_id = p.by_id;
+    r.groups = (d + 31) / 32;
+    r.group_at = room.group_at;
+    r.slices = (d + kSlice - 1) / kSlice;
+    r.id_blocks = grad_weight ? (N + kSpan - 1) / kSpan * r.slices : 0;
+    const unsigned grid = (unsigned)r.id_blocks + (unsigned)(grad_hidden ? (N + 31) / 32 * r.groups : 0);
     return tfe_launch_serial(tfe_xent_rows_kernel, grid, kRowsThreads, 1, 0, stream, "cross entropy gradient launch", r);
 }
 

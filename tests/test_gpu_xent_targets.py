@@ -7,6 +7,11 @@ DEV = torch.device("cuda:0")
 HALF_BF16 = 2.0 ** -8
 
 
+def half_step(x):
+    """Half the distance between bf16 numbers at x: no rounding is off by more."""
+    return torch.exp2(torch.floor(torch.log2(x.abs().clamp_min(2.0 ** -126))) - 8)
+
+
 def exact(h, w, t, g):
     """(loss, lse, G, grad_hidden, grad_weight) in float64, G at the target as minus the sum of the others: nothing cancels.  Every row has a target."""
     h, w, t = h.double(), w.double(), t.long()
@@ -46,6 +51,30 @@ def check_loss(h, w, t):
     assert bool(((lse.double().cpu() - e_lse).abs() <= rel + 2.0 ** -23 * e_lse.abs()).all())
     assert engine.xent_status() == 0
     return loss, lse
+
+
+def check(h, w, t, g):
+    """Loss and gradients: everything as a fraction of what it is a sum of.  G's entries are rounded to bf16 but for the targets', whose rounding
+    is made up for; sums in fp32 add 2^-23 per 16 terms; results are rounded once."""
+    from paper_2607_07388_b200 import engine
+    loss, lse = check_loss(h, w, t)
+    hd, wd, td, gd = (x.to(DEV) for x in (h, w, t, g))
+    gh, gw = engine.xent_backward(gd, hd, wd, td, lse)
+    _, e_lse, G, e_gh, e_gw = exact(h, w, t, g)
+    n, (v, d) = len(t), w.shape
+    rel = relative(h, w, e_lse)
+    onehot = torch.zeros_like(G)
+    onehot[torch.arange(n), t.long()] = 1
+    err = G.abs() * (rel[:, None] + HALF_BF16 * (1 - onehot))
+    A, B = w.double().abs(), h.double().abs()
+    tol_h = err @ A + (G.abs() @ A) * (v / 16 + 16) * 2.0 ** -23
+    tol_w = err.T @ B + (G.abs().T @ B) * (n / 16 + 16) * 2.0 ** -23
+    for got, want, tol, what in ((gh, e_gh, tol_h, "grad_hidden"), (gw, e_gw, tol_w, "grad_weight")):
+        off = (got.double().cpu() - want).abs()
+        allowed = tol + half_step(want.abs() + tol)
+        assert bool((off <= allowed).all()), (what, float((off / allowed).max()), float((off - allowed).max()))
+    assert engine.xent_status() == 0
+    return loss, lse, gh, gw
 
 
 def weights(rng, v, d):
@@ -123,3 +152,24 @@ SURE = [(1, 300, 1024), (40, 2000, 1024), (150, 2000, 1024), (300, 3001, 1024), 
 def test_loss_of_rows_that_are_sure_of_their_target(n, v, d):
     loss, _ = check_loss(*sure_rows(n + d, n, v, d)[:3])
     assert float(loss.min()) > 0 and (float(loss.min()) < 1e-4 or n == 1)
+
+
+@pytest.mark.parametrize("n,v,d", [(30, 4000, 512), (243, 4000, 512), (600, 4000, 512), (30, 20, 64), (900, 50, 64), (3000, 5000, 128), (70_000, 40, 64)])
+def test_one_id_in_half_of_the_rows(n, v, d):
+    """A plain mean over unsure rows: G at the target is nearly the same number in every row of an id, and so is its rounding.  Elementwise, within
+    half a step of the result and what G's other entries allow."""
+    rng = torch.Generator().manual_seed(n + v)
+    w = (weights(rng, v, d).float() * 0.01).bfloat16()
+    h = torch.randn((n, d), generator=rng).bfloat16()
+    t = torch.randint(0, v, (n,), generator=rng).int()
+    t[torch.rand(n, generator=rng) < 0.5] = v // 3
+    t[:5] = v - 1
+    check(h, w, t, torch.full((n,), 1 / n))
+
+
+def test_identical_rows():
+    """The same hidden state and target over and over, as padding that was not masked gives: all errors of one sign."""
+    rng = torch.Generator().manual_seed(3)
+    w = weights(rng, 700, 256)
+    h = torch.randn((1, 256), generator=rng).bfloat16().expand(1500, 256).contiguous()
+    check(h, w, torch.full((1500,), 123, dtype=torch.int32), torch.full((1500,), 1 / 1500))
