@@ -636,14 +636,15 @@ tfe_status tfe_distill_backward(const void *logits, int32_t dtype, int32_t N, in
  *   grad_hidden, grad_weight   DEVICE bf16, rows as above, every row written; one of them may be NULL.  They must touch no operand
  *                    and not each other.  G is rounded to bf16 for the two products with it (the tensor cores take both operands in one
  *                    type; a G of its own error 2^-9 on average adds as much to a gradient as the gradient's own rounding), but for its
- *                    entries at the targets, whose rounding is made up for in fp32; sums are fp32 and rounded once.
+ *                    entries at the targets, whose rounding is made up for in fp32 and which are minus the sum of the row's others: a row
+ *                    that is sure of its target has gradients as exact as any other.  Sums are fp32 and rounded once.
  *   workspace        DEVICE scratch, 256-byte aligned, of at least tfe_xent_*_workspace_bytes(N, V, d) bytes (smaller: TFE_ERR_CAPACITY);
  *                    contents undefined before and after.  It bounds what exists of the logits at a time: forward some 40 MB of
  *                    partial results, backward a piece of G of up to 256 MB (4,096 columns where N > 32,768) and sums of as much
  *                    at most (or 4 N d bytes), and 4 min(N, V) d bytes for the rows of grad_weight that targets have.
  * NaN propagates, and a logit of +inf makes its row's results NaN; a target whose logit is -inf has a loss of +inf.  The order of every sum is fixed by the sizes and the targets.
  * Forward two or three launches; backward two for each piece of the vocabulary and
- * two more.
+ * three more.
  *
  * Every wait inside the kernels is bounded.  Should one run out, the loss and lse of the rows concerned, or all gradients, are NaN.
  * tfe_xent_status synchronises `stream`, reads the status word of the current device and clears what it read: 0, or bits set by

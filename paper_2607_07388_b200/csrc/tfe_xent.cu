@@ -13,6 +13,7 @@
 //       kGrads  both products of the piece with G: grad W is complete with its piece, grad H adds up over the pieces in fp32.
 //   tfe_xent_few_kernel       the loss of up to 64 rows.
 //   tfe_xent_loss_kernel      joins a row's partial maxima and sums with its target's logit.
+//   tfe_xent_rest_kernel      G at the targets, and what its rounding took from it.
 //   tfe_xent_rows_kernel      joins grad H's sums, rounds them and puts them back to their rows; completes grad W's rows of the targets.
 //
 // All products are 2 N V d operations; the loss makes one, the gradients three (z again and the two with G).  For 2,048 x 151,936 x 1,024 the
@@ -75,7 +76,8 @@ struct GemmParams {
     const int32_t *n_live;                      // rows taken part in (null: N)
     const int32_t *target;
     const float *lse, *coef;
-    float *rest;                                // what rounding took from G at each row's target
+    float *rest;                                // kProb: G at each row's target as the products have it
+    float *part_p; int64_t ld_p;                // kProb: [2 * column tiles of a piece][ld_p] sums of probabilities, the targets' left out, over all pieces so far
     uint32_t *first_row;                        // [V]: the first row whose target is this id, kNone where there is none
     float *sum_w; int32_t by_id;                // kGrads: rows of grad W before they are rounded, d apart: of the ids that are targets, by their first row, or of all ids
     float2 *part; int64_t ld_part;              // kLse: [2 * units per row][ld_part] maxima and sums
@@ -412,6 +414,10 @@ __device__ __forceinline__ void pair_tmem_dealloc(uint32_t taddr, uint32_t cols)
 // grad W; and with one coefficient for all rows, a mean, it is nearly the same factor in every row of an id.  That difference is kept in
 // fp32 (rest), and the sums over it are added to the products before those are rounded: grad H's where its parts are joined, grad W's in the
 // same kernel, for which the rows of the ids that are targets are kept in fp32 (sum_w).
+// G at the target, g (p - 1), is minus the sum of the row's other probabilities: from p it would be off by the error of z_t and of lse, which for
+// a logit of 28 over 1,024 k is 4e-5, and so wrong in every digit where 1 - p is less.  That sum is known after the last piece; the products have
+// what z_t gives in its place, or nothing where p is near 1, and the difference is part of the rest.
+constexpr float kSure = 0x1p-8f;                // 1 - p below which the products have nothing
 
 // The gradients' units, of two lengths, go to the pairs as they come free, in an order in which those under way together read the same
 // operands: 2,048 x 50,688 x 1,024 take 321 us, with equal shares that each pair works off by itself 450 us.  The order of every sum is
@@ -619,9 +625,16 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
             const bool live = row < units.n_live;                   // (grad W's rows are the vocabulary's: it has no use for this)
             int32_t target = -1;
             float lse = 0.f, coef = 0.f, top = -3.4e38f;
-            float2 sum = make_float2(0.f, 0.f);
+            float2 sum = make_float2(0.f, 0.f);                     // kLse: relative to the top; kProb: of probabilities
+            float was = 0.f;
+            float *part_p = nullptr;
             if (kOp != kGrads && live) target = p.target[row];
-            if (kOp == kProb && live) { lse = p.lse[row]; coef = p.coef[row]; }
+            if (kOp == kProb && live) {
+                lse = p.lse[row];
+                coef = p.coef[row];
+                part_p = p.part_p + (int64_t)(2 * (w.b_at / p.tn) + half) * p.ld_p + row;
+                if (!p.first) was = *part_p;
+            }
             float *kept_row = nullptr;                              // grad W: where this thread's vocabulary row is kept in fp32, if it is a target
             if (kOp == kGrads && !w.grad_h && p.v0 + row < p.V) {
                 const uint32_t at = p.first_row[p.v0 + row];
@@ -719,14 +732,31 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
 #pragma unroll
                             for (int j = 0; j < 8; ++j) {
                                 y[j] = __fmul2_rn(__fadd2_rn(y[j], minus), by);
-                                y[j] = __fmul2_rn(make_float2(tfe_rows::exp2_approx(y[j].x), tfe_rows::exp2_approx(y[j].y)), times);
+                                y[j] = make_float2(tfe_rows::exp2_approx(y[j].x), tfe_rows::exp2_approx(y[j].y));
                             }
-                            if ((uint32_t)(mine - c) < 16u) {
-                                float z = 0.f;
+                            if (c + 16 > left)
 #pragma unroll
-                                for (int j = 0; j < 16; ++j) z = mine - c == j ? __uint_as_float(x[j]) : z;
-                                const float g = coef * expm1f(z - lse), kept = __bfloat162float(__float2bfloat16_rn(g));
-                                p.rest[row] = g - kept;
+                                for (int j = 0; j < 8; ++j) {
+                                    y[j].x = c + 2 * j < left ? y[j].x : 0.f;
+                                    y[j].y = c + 2 * j + 1 < left ? y[j].y : 0.f;
+                                }
+                            const bool here = (uint32_t)(mine - c) < 16u;
+                            float z = 0.f;
+                            if (here)
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) {
+                                    z = mine - c == j ? __uint_as_float(x[j]) : z;
+                                    (j & 1 ? y[j / 2].y : y[j / 2].x) = mine - c == j ? 0.f : (j & 1 ? y[j / 2].y : y[j / 2].x);
+                                }
+                            float2 more = __fadd2_rn(y[0], y[1]);
+#pragma unroll
+                            for (int j = 2; j < 8; ++j) more = __fadd2_rn(more, y[j]);
+                            sum = __fadd2_rn(sum, more);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) y[j] = __fmul2_rn(y[j], times);
+                            if (here) {
+                                const float g = expm1f(z - lse), kept = g > -kSure ? 0.f : __bfloat162float(__float2bfloat16_rn(coef * g));
+                                p.rest[row] = kept;
                                 atomicMin(p.first_row + target, (uint32_t)row);
 #pragma unroll
                                 for (int j = 0; j < 8; ++j) {
@@ -737,12 +767,6 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                             if (!live)          // (not 0 times what may be NaN where a weight is infinite)
 #pragma unroll
                                 for (int j = 0; j < 8; ++j) y[j] = make_float2(0.f, 0.f);
-                            if (c + 16 > left)
-#pragma unroll
-                                for (int j = 0; j < 8; ++j) {
-                                    y[j].x = c + 2 * j < left ? y[j].x : 0.f;
-                                    y[j].y = c + 2 * j + 1 < left ? y[j].y : 0.f;
-                                }
                         } else {
                             if (kept_row)
 #pragma unroll
@@ -802,6 +826,8 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
             if (!ok) break;
             if constexpr (kOp == kLse)
                 if (live) p.part[(int64_t)(2 * w.index + half) * p.ld_part + row] = make_float2(top, sum.x + sum.y);
+            if constexpr (kOp == kProb)
+                if (live) *part_p = was + (sum.x + sum.y);
         }
         asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         if (!ok) {                              // a wait ran out: no results that look like some (the last kernel sees to that)
@@ -1095,6 +1121,38 @@ tfe_xent_loss_kernel(const LossParams p)
     }
 }
 
+struct RestParams {
+    int32_t chunks;
+    const int32_t *n_live;
+    const float *part_p; int64_t ld_p;
+    const float *coef;
+    float *rest;                                // in: what the products have; out: G less that
+};
+constexpr int kRestWarps = 32;
+
+// A block for 32 rows, whose sums lie side by side: a chain of loads, 4 us of the 91 that both gradients of 33 x 32,003 x 1,000 take.
+__global__ void __launch_bounds__(32 * kRestWarps)
+tfe_xent_rest_kernel(const RestParams p)
+{
+    __shared__ float s_sum[kRestWarps][33];
+    tfe_wait_for_stream();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int32_t row = blockIdx.x * 32 + lane, n_live = *p.n_live;
+    float sum = 0.f;
+    if (row < n_live)
+#pragma unroll 16
+        for (int32_t c = warp; c < p.chunks; c += kRestWarps) sum += p.part_p[(int64_t)c * p.ld_p + row];
+    s_sum[warp][lane] = sum;
+    __syncthreads();
+    sum = s_sum[lane][warp];                    // row `warp` now, from 32 parts
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+    const int32_t mine = blockIdx.x * 32 + warp;
+    if (lane != 0 || mine >= n_live) return;
+    const float kept = p.rest[mine];            // (where it is not finite the products have made the results what they are)
+    p.rest[mine] = fabsf(kept) <= 3.402823466e38f ? fmaf(-p.coef[mine], sum, -kept) : 0.f;
+}
+
 struct RowsParams {
     int32_t N, V, d, splits, m_room, cols, tn, groups;          // groups: of 32 columns
     const float *sum_h, *rest;
@@ -1361,7 +1419,7 @@ struct ForwardRoom {
     }
 };
 struct BackwardRoom {
-    bf16 *g, *h; float *sum_h, *sum_w, *lse, *coef, *rest; int32_t *pos, *target, *n_live, *group_at; uint32_t *failed, *first_row;
+    bf16 *g, *h; float *sum_h, *sum_w, *lse, *coef, *rest, *part_p; int32_t *pos, *target, *n_live, *group_at; uint32_t *failed, *first_row;
     int64_t bytes;
     BackwardRoom(const Plan &q, int32_t N, int32_t V, int32_t d, void *ws)
     {
@@ -1370,6 +1428,7 @@ struct BackwardRoom {
         h = r.take<bf16>(q.n_pad * d);
         sum_h = r.take<float>((int64_t)q.splits * q.m_room * q.cols * kM * kN);
         lse = r.take<float>(q.n_pad); coef = r.take<float>(q.n_pad); rest = r.take<float>(q.n_pad);
+        part_p = r.take<float>(2 * (q.piece / kN) * q.n_pad);
         pos = r.take<int32_t>(N); target = r.take<int32_t>(q.n_pad); n_live = r.take<int32_t>(1); failed = r.take<uint32_t>(1 + (int64_t)q.pieces);
         first_row = r.take<uint32_t>(V);
         group_at = r.take<int32_t>((N + kGroup - 1) / kGroup + 1);
@@ -1565,7 +1624,7 @@ tfe_status tfe_xent_backward(const void *hidden, int64_t ld_hidden, int32_t N, c
     p.N = N; p.V = V; p.d = d; p.n_pad = (int32_t)q.n_pad; p.m_room = q.m_room; p.splits = q.splits;
     p.want_h = grad_hidden != nullptr; p.want_w = grad_weight != nullptr;
     p.give_up = g_xent_give_up.load(std::memory_order_relaxed);
-    p.n_live = room.n_live; p.target = room.target; p.lse = room.lse; p.coef = room.coef; p.sum_h = room.sum_h; p.failed = room.failed; p.rest = room.rest; p.first_row = room.first_row; p.sum_w = room.sum_w; p.by_id = V <= q.n_pad;
+    p.n_live = room.n_live; p.target = room.target; p.lse = room.lse; p.coef = room.coef; p.sum_h = room.sum_h; p.failed = room.failed; p.rest = room.rest; p.first_row = room.first_row; p.part_p = room.part_p; p.ld_p = q.n_pad; p.sum_w = room.sum_w; p.by_id = V <= q.n_pad;
     for (int32_t i = 0; i < q.pieces; ++i) {
         p.v0 = (int32_t)(i * q.piece);
         p.width = (int32_t)std::min<int64_t>(q.piece, V - (int64_t)i * q.piece);
@@ -1577,6 +1636,9 @@ tfe_status tfe_xent_backward(const void *hidden, int64_t ld_hidden, int32_t N, c
         const int64_t most = (int64_t)q.cols * ((int64_t)p.want_h * q.m_room * q.splits + (int64_t)p.want_w * ((p.width + kM - 1) / kM));
         if (tfe_status st = launch_gemm<kGrads>(most, sms, stream, grads, p)) return st;
     }
+    RestParams t{};
+    t.chunks = 2 * (int32_t)((std::min<int64_t>(q.piece, V) + kN - 1) / kN); t.n_live = room.n_live; t.part_p = room.part_p; t.ld_p = q.n_pad; t.coef = room.coef; t.rest = room.rest;
+    if (tfe_status st = tfe_launch_serial(tfe_xent_rest_kernel, (unsigned)((N + 31) / 32), 32 * kRestWarps, 1, 0, stream, "cross entropy targets launch", t)) return st;
     RowsParams r{};
     r.N = N; r.V = V; r.d = d; r.splits = q.splits; r.m_room = q.m_room; r.cols = q.cols; r.tn = q.tn_d; r.sum_h = room.sum_h; r.pos = room.pos;
     r.failed = room.failed; r.rest = room.rest; r.target = room.target; r.w = static_cast<const bf16 *>(weight); r.ld_weight = ld_weight; r.grad_h = static_cast<bf16 *>(grad_hidden); r.ld_h = ld_grad_hidden; r.grad_w = static_cast<bf16 *>(grad_weight); r.ld_w = ld_grad_weight;

@@ -124,6 +124,18 @@ def test_a_target_that_cannot_come(n):
     assert engine.xent_status() == 0
 
 
+def test_one_id_alone():
+    """A vocabulary of one: the loss is 0 and so are the gradients."""
+    from paper_2607_07388_b200 import engine
+    h, w = torch.randn((70, 64), device=DEV).bfloat16(), torch.randn((1, 64), device=DEV).bfloat16()
+    t = torch.zeros(70, dtype=torch.int32, device=DEV)
+    for n in (3, 70):
+        loss, lse = engine.xent_forward(h[:n], w, t[:n])
+        gh, gw = engine.xent_backward(torch.ones(n, device=DEV), h[:n], w, t[:n], lse)
+        z = h[:n].double() @ w[0].double()
+        assert not loss.any() and not gh.any() and not gw.any() and float((lse.double() - z).abs().max()) <= 1e-5 * float(z.abs().max())
+
+
 def sure_rows(seed, n, v, d):
     """Rows whose 1 - p runs from 1e-2 to 1e-6: hidden states along their target's weights, as far as it takes."""
     rng = torch.Generator().manual_seed(seed)
@@ -152,6 +164,31 @@ SURE = [(1, 300, 1024), (40, 2000, 1024), (150, 2000, 1024), (300, 3001, 1024), 
 def test_loss_of_rows_that_are_sure_of_their_target(n, v, d):
     loss, _ = check_loss(*sure_rows(n + d, n, v, d)[:3])
     assert float(loss.min()) > 0 and (float(loss.min()) < 1e-4 or n == 1)
+
+
+@pytest.mark.parametrize("n,v,d", SURE)
+def test_gradients_of_rows_that_are_sure_of_their_target(n, v, d):
+    check(*sure_rows(n + d, n, v, d))
+
+
+def test_sure_rows_in_several_pieces():
+    """4,096 rows x 70,001 ids: the gradient of the logits takes three pieces; the rows' sums run over all of them."""
+    from paper_2607_07388_b200 import engine
+    h, w, t, g = sure_rows(5, 48, 70_001, 256)
+    rng = torch.Generator().manual_seed(6)
+    n = 4096
+    many_h, many_t, many_g = (0.3 * torch.randn((n, 256), generator=rng)).bfloat16(), torch.full((n,), -1, dtype=torch.int32), torch.ones(n)
+    at = torch.randperm(n, generator=rng)[:48].sort().values
+    many_h[at], many_t[at], many_g[at] = h, t, g
+    hd, wd, td, gd = (x.to(DEV) for x in (many_h, w, many_t, many_g))
+    loss, lse = engine.xent_forward(hd, wd, td)
+    gh, gw = engine.xent_backward(gd, hd, wd, td, lse)
+    e_loss, e_lse, G, e_gh, e_gw = exact(h, w, t, g)
+    rel = relative(h, w, e_lse)
+    assert bool(((loss.double().cpu()[at] - e_loss).abs() <= e_loss * (rel + 2.0 ** -23)).all())
+    # per row, in the 2-norm: G's rounding of the other ids and the result's own, 2^-8 at most each
+    for got, want in ((gh.double().cpu()[at], e_gh), (gw.double().cpu()[t.long()], e_gw[t.long()])):
+        assert bool(((got - want).norm(dim=1) <= (2.0 ** -7 + 2 * rel) * want.norm(dim=1)).all())
 
 
 @pytest.mark.parametrize("n,v,d", [(30, 4000, 512), (243, 4000, 512), (600, 4000, 512), (30, 20, 64), (900, 50, 64), (3000, 5000, 128), (70_000, 40, 64)])
