@@ -639,10 +639,13 @@ tfe_status tfe_distill_backward(const void *logits, int32_t dtype, int32_t N, in
  *                    entries at the targets, whose rounding is made up for in fp32 and which are minus the sum of the row's others: a row
  *                    that is sure of its target has gradients as exact as any other.  Sums are fp32 and rounded once.
  *   workspace        DEVICE scratch, 256-byte aligned, of at least tfe_xent_*_workspace_bytes(N, V, d) bytes (smaller: TFE_ERR_CAPACITY);
- *                    contents undefined before and after.  It bounds what exists of the logits at a time: forward some 40 MB of
- *                    partial results, backward a piece of G of up to 256 MB (4,096 columns where N > 32,768) and sums of as much
- *                    at most (or 4 N d bytes), and 4 min(N, V) d bytes for the rows of grad_weight that targets have.
- * NaN propagates, and a logit of +inf makes its row's results NaN; a target whose logit is -inf has a loss of +inf.  The order of every sum is fixed by the sizes and the targets.
+ *                    contents undefined before and after.  It bounds what exists of the logits at a time.  With N rounded up to a multiple of
+ *                    256, forward takes up to 64 MiB + 16 N bytes of partial results and, where N > 256, the hidden states once more (2 N d)
+ *                    and 12 N; backward a piece of G of up to 256 MiB (of 4,096 columns where N > 32,768) and a 64th of that, the hidden states
+ *                    (2 N d), sums for grad_hidden of up to 256 MiB (or 4 N d, d rounded up to 256, up to 128 where it is less than 256), the rows of
+ *                    grad_weight that targets have (4 min(N, V) d), and 32 N + 5 V bytes.
+ * NaN propagates, and a logit of +inf makes its row's results NaN; a target whose logit is -inf has a loss of +inf.  The order of every sum
+ * is fixed by the sizes and the targets.
  * Forward two or three launches; backward two for each piece of the vocabulary and
  * three more.
  *

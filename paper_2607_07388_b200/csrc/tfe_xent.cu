@@ -81,7 +81,7 @@ struct GemmParams {
     uint32_t *first_row;                        // [V]: the first row whose target is this id, kNone where there is none
     float *sum_w; int32_t by_id;                // kGrads: rows of grad W before they are rounded, d apart: of the ids that are targets, by their first row, or of all ids
     float2 *part; int64_t ld_part;              // kLse: [2 * units per row][ld_part] maxima and sums
-    float *sum_h;                               // kGrads: [splits][m_room][column tiles][kN / 4][kM][4]
+    float *sum_h;                               // kGrads: [splits][m_room][column tiles][tn / 4][kM][4]
     uint32_t *failed;                           // set if a wait ran out
     uint32_t *ticket;                           // kGrads: units handed out so far
 };
@@ -643,7 +643,7 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
             for (int32_t t = 0; t < w.tiles; ++t) {
                 float4 *at = nullptr;                               // grad H's sums of this row, four columns each
                 if constexpr (kOp == kGrads) {
-                    at = reinterpret_cast<float4 *>(p.sum_h) + ((int64_t)w.index * (kN / 4) + c0 / 4) * kM + row_in_tile;
+                    at = reinterpret_cast<float4 *>(p.sum_h) + ((int64_t)w.index * (p.tn / 4) + c0 / 4) * kM + row_in_tile;
                     if (w.steps == 0) {         // (a part of a short last piece that has nothing to add)
                         if (p.first && live)
                             for (int32_t c = 0; c < cols; c += 4) at[(int64_t)(c / 4) * kM] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -1301,8 +1301,8 @@ tfe_xent_rows_kernel(const RowsParams p)
             const int32_t at = r0 + lane < p.N ? p.pos[r0 + lane] : -1, c = c0 + 4 * warp;
             float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
             if (at >= 0 && c < p.d) {
-                const float4 *from = reinterpret_cast<const float4 *>(p.sum_h) + (((int64_t)(at / kM) * p.cols + c / p.tn) * (kN / 4) + c % p.tn / 4) * kM + at % kM;
-                const int64_t step = (int64_t)p.m_room * p.cols * (kN / 4) * kM;
+                const float4 *from = reinterpret_cast<const float4 *>(p.sum_h) + (((int64_t)(at / kM) * p.cols + c / p.tn) * (p.tn / 4) + c % p.tn / 4) * kM + at % kM;
+                const int64_t step = (int64_t)p.m_room * p.cols * (p.tn / 4) * kM;
 #pragma unroll 8
                 for (int32_t s = 0; s < p.splits; ++s) {
                     const float4 x = from[s * step];
@@ -1391,7 +1391,7 @@ Plan make_plan(int32_t N, int32_t V, int32_t d)
     // parts of grad H's sums: units of about a sixth of a pair's share of the work, so that the shares come out even (a unit of grad W takes
     // as long as six steps at least, which is what its tile takes to leave)
     const int64_t steps = q.piece / kStepK, work = q.cols * (q.m_room * steps + q.piece / kM * std::max<int64_t>(6, q.n_pad / kStepK));
-    const int64_t most_splits = std::min<int64_t>(kMaxSplits, std::max<int64_t>(1, kSumElements / ((int64_t)q.m_room * q.cols * kM * kN)));
+    const int64_t most_splits = std::min<int64_t>(kMaxSplits, std::max<int64_t>(1, kSumElements / ((int64_t)q.m_room * q.cols * kM * q.tn_d)));
     q.splits = (int32_t)std::min<int64_t>(most_splits, (steps + std::max<int64_t>(16, work / kPairs / 6) - 1) / std::max<int64_t>(16, work / kPairs / 6));
     return q;
 }
@@ -1426,7 +1426,7 @@ struct BackwardRoom {
         Room r{static_cast<uint8_t *>(ws), 0};
         g = r.take<bf16>(q.n_pad * q.piece);
         h = r.take<bf16>(q.n_pad * d);
-        sum_h = r.take<float>((int64_t)q.splits * q.m_room * q.cols * kM * kN);
+        sum_h = r.take<float>((int64_t)q.splits * q.m_room * q.cols * kM * q.tn_d);
         lse = r.take<float>(q.n_pad); coef = r.take<float>(q.n_pad); rest = r.take<float>(q.n_pad);
         part_p = r.take<float>(2 * (q.piece / kN) * q.n_pad);
         pos = r.take<int32_t>(N); target = r.take<int32_t>(q.n_pad); n_live = r.take<int32_t>(1); failed = r.take<uint32_t>(1 + (int64_t)q.pieces);
