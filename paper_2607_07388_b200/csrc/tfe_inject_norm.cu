@@ -189,14 +189,24 @@ __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 __device__ __forceinline__ float2 mul(float2 a, float2 b) { return __fmul2_rn(a, b); }
 __device__ __forceinline__ float2 fma(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
 __device__ __forceinline__ float join(float2 a) { return a.x + a.y; }
+// s = 1 / (1 + e) of a gate x, e = exp(-x)
 template <typename T>
-__device__ __forceinline__ float sigmoid(float x)
+__device__ __forceinline__ float sigmoid(float x, float &e)
 {
-    if constexpr (sizeof(T) == 4) return __fdividef(1.f, 1.f + expf(-x));      // (an exponent of 15 alone costs the fast one 1e-6)
+    if constexpr (sizeof(T) == 4) {             // (an exponent of 15 alone costs the fast one 1e-6)
+        e = expf(-x);
+        return __fdividef(1.f, 1.f + e);
+    }
     float y;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(1.f + tfe_rows::exp2_approx(x * -1.4426950408889634f)));
+    e = tfe_rows::exp2_approx(x * -1.4426950408889634f);
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(1.f + e));
     return y;
 }
+// 1 - s for its derivative: as e s, since the subtraction loses every digit of an open gate (from x = 17 on it gives 0).  Where e is
+// beyond fp32 s is 0, and so is the derivative.  16-bit rows hold it for a vector gate from the sigmoid on, fp32 rows make the sigmoid of
+// -x where it is needed: gradients of 32,768 x 1,024 take 107 and 182 us so (111 and 208 the other way round).
+__device__ __forceinline__ float shut(float e, float s) { return fminf(e, 0x1p126f) * s; }
+template <typename T> constexpr bool kHoldShut = sizeof(T) == 2;
 
 // A row's operands, and what both directions make of them first.
 template <typename T, bool kVector>
@@ -211,16 +221,26 @@ struct Row {
         if (p.gate_kind == TFE_GATE_VECTOR) gate.load(p.gate, p.ld_gate, row, p.d, t, p.row_threads);
         scalar = p.gate_kind == TFE_GATE_SCALAR ? static_cast<const float *>(p.gate)[row] : 1.f;
     }
-    __device__ __forceinline__ void gates(const NormParams &p, float2 (&s)[kPairs]) const
+    // s, and for a sigmoid's derivative 1 - s of a vector gate (with kHoldShut), s (1 - s) of a scalar one
+    __device__ __forceinline__ void gates(const NormParams &p, float2 (&s)[kPairs], float2 (&by)[kPairs], float &slope) const
     {
+        float2 e;
+        slope = 1.f;
         if (p.gate_kind == TFE_GATE_VECTOR) {
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) {
                 s[i] = gate.two(i);
-                if (p.sigmoid) s[i] = make_float2(sigmoid<T>(s[i].x), sigmoid<T>(s[i].y));
+                if (p.sigmoid) {
+                    s[i] = make_float2(sigmoid<T>(s[i].x, e.x), sigmoid<T>(s[i].y, e.y));
+                    if constexpr (kHoldShut<T>) by[i] = make_float2(shut(e.x, s[i].x), shut(e.y, s[i].y));
+                }
             }
         } else {
-            const float x = p.gate_kind == TFE_GATE_SCALAR && p.sigmoid ? sigmoid<T>(scalar) : scalar;
+            float x = scalar;
+            if (p.gate_kind == TFE_GATE_SCALAR && p.sigmoid) {
+                x = sigmoid<T>(scalar, e.x);
+                slope = x * shut(e.x, x);
+            }
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) s[i] = both(x);
         }
@@ -262,8 +282,9 @@ tfe_inject_norm_forward_kernel(const NormParams p)
             x.load(p, row, t);
         }
         const float a = inverse_root(row_sum(x.square_m()), inv_d, p.eps);
-        float2 u[kPairs], square = both(0.f);
-        x.gates(p, u);
+        float2 u[kPairs], by[kPairs], square = both(0.f);
+        float slope;
+        x.gates(p, u, by, slope);
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) {
             u[i] = fma(mul(u[i], both(p.lam * a)), mul(x.m.two(i), wp[i]), x.h.two(i));
@@ -317,8 +338,9 @@ tfe_inject_norm_backward_kernel(const NormParams p)
         const Row<T, kVector> &x = all.x;
         const float a = inverse_root(row_sum(x.square_m()), inv_d, p.eps);
         const float la = p.lam * a;
-        float2 s[kPairs], q[kPairs], u[kPairs], uu = both(0.f), ut = both(0.f);
-        x.gates(p, s);
+        float2 s[kPairs], by[kPairs], q[kPairs], u[kPairs], uu = both(0.f), ut = both(0.f);
+        float slope;
+        x.gates(p, s, by, slope);
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) {
             q[i] = mul(x.m.two(i), wp[i]);      // y / a
@@ -343,7 +365,7 @@ tfe_inject_norm_backward_kernel(const NormParams p)
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) uy = fma(u[i], q[i], uy);
             const float dot = row_sum(join(uy));
-            if (t == 0) static_cast<float *>(p.g_gate)[row] = la * dot * (p.sigmoid ? s[0].x * (1.f - s[0].x) : 1.f);
+            if (t == 0) static_cast<float *>(p.g_gate)[row] = la * dot * slope;
         }
         if (p.g_m) {
             const float by_m = a * a * row_sum(join(mx)) * inv_d;
@@ -354,8 +376,21 @@ tfe_inject_norm_backward_kernel(const NormParams p)
         }
         if (p.g_gate && p.gate_kind == TFE_GATE_VECTOR) {
 #pragma unroll
-            for (int i = 0; i < kPairs; ++i)
-                q[i] = mul(mul(q[i], both(la)), p.sigmoid ? mul(sdh[i], fma(s[i], both(-1.f), both(1.f))) : u[i]);
+            for (int i = 0; i < kPairs; ++i) q[i] = mul(q[i], both(la));
+            if (p.sigmoid) {
+#pragma unroll
+                for (int i = 0; i < kPairs; ++i) {
+                    if constexpr (!kHoldShut<T>) {
+                        float2 e;
+                        const float2 g = x.gate.two(i);
+                        by[i] = make_float2(sigmoid<T>(-g.x, e.x), sigmoid<T>(-g.y, e.y));
+                    }
+                    q[i] = mul(q[i], mul(sdh[i], by[i]));
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < kPairs; ++i) q[i] = mul(q[i], u[i]);
+            }
             store<T, kVector>(p.g_gate, p.ld_g_gate, row, p.d, t, p.row_threads, q);
         }
     }
