@@ -9,7 +9,7 @@
 //   x = lam s w_post dh              dm = a x - a^3 m mean(m x)            dw_post = sum over rows of lam s dh a m
 //
 // HBM bounds both, and nearly as much the issue slots: 32,768 x 1,024 bf16 with a vector gate take 57 us forward (5.9 TB/s of the operands'
-// bytes, 73 % of the slots) and 105 us backward (5.1 TB/s, 62 %).  A row is held in the registers of `row_threads` threads, eight columns each, so every operand is read once and every
+// bytes, 73 % of the slots) and 107 us backward (5.0 TB/s).  A row is held in the registers of `row_threads` threads, eight columns each, so every operand is read once and every
 // intermediate stays on the chip; backward makes a, y, u and b again rather than reading them.  Several rows share a block, and a
 // block walks rows with the next row's loads under way.  u is rounded once for the output, n and the gradients come from it as it was
 // before.  The weights' gradients are summed over a block's rows in registers, over its groups in shared memory, and over the blocks
@@ -349,13 +349,13 @@ tfe_inject_norm_backward_kernel(const NormParams p)
             ut = fma(u[i], mul(wn[i], all.gn.two(i)), ut);
         }
         const float2 two = row_sum(join(uu), join(ut));
-        const float b = inverse_root(two.x, inv_d, p.eps), by_u = b * b * b * two.y * inv_d;
+        const float b = inverse_root(two.x, inv_d, p.eps), by_u = b * (b * (two.y * inv_d));      // (products in an order that stays within fp32 as long as b does)
         float2 sdh[kPairs], mx = both(0.f), uy = both(0.f);         // sdh: s dh; mx, uy and sum_p without their factors lam and a
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) {
-            const float2 n = mul(all.gn.two(i), both(b));
-            sum_n[i] = fma(n, u[i], sum_n[i]);
-            u[i] = fma(both(-by_u), u[i], fma(n, wn[i], all.gu.two(i)));       // dh
+            const float2 bu = mul(u[i], both(b));
+            sum_n[i] = fma(all.gn.two(i), bu, sum_n[i]);
+            u[i] = fma(both(-by_u), bu, fma(mul(all.gn.two(i), both(b)), wn[i], all.gu.two(i)));      // dh
             sdh[i] = mul(s[i], u[i]);
             sum_p[i] = fma(sdh[i], mul(x.m.two(i), both(a)), sum_p[i]);
             mx = fma(q[i], sdh[i], mx);
@@ -368,7 +368,7 @@ tfe_inject_norm_backward_kernel(const NormParams p)
             if (t == 0) static_cast<float *>(p.g_gate)[row] = la * dot * slope;
         }
         if (p.g_m) {
-            const float by_m = a * a * row_sum(join(mx)) * inv_d;
+            const float by_m = a * (a * (row_sum(join(mx)) * inv_d));
             float2 dm[kPairs];
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) dm[i] = mul(fma(both(-by_m), x.m.two(i), mul(wp[i], sdh[i])), both(la));

@@ -56,3 +56,38 @@ def test_gates_that_are_open_or_shut(kind, gate, d):
     off = (got[4] - want[4]).abs()
     own = HALF[torch.float32 if gate == "scalar" else TYPES[kind]]
     assert bool((off <= tol + own * (want[4].abs() + tol)).all()), float((off / want[4].abs()).max())
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("eps", [1e-30, 1e-37])
+def test_rows_of_zeros_with_a_small_eps(kind, eps):
+    """Padding: h and m are zeros, both norms are sqrt(eps), and the gradient is what arrives divided by it."""
+    data = make(2, 40, 200, kind, "scalar")
+    for x in data[:2]:
+        x[::3] = 0
+    if eps < 1e-30:
+        data[6].mul_(2.0 ** -20)         # (what arrives at a norm leaves it times 1 / sqrt(eps), and times that again at m)
+        data[5].mul_(2.0 ** -20)
+    got, want = both(data, sigmoid=False, lam=0.75, eps=eps)
+    for i, (a, e) in enumerate(zip(got, want)):
+        assert bool(torch.isfinite(a).all()), i
+    zeros = torch.arange(40) % 3 == 0
+    for i in (0, 1):
+        own = HALF[TYPES[kind]]
+        assert bool(((got[i][zeros] - want[i][zeros]).abs() <= (2.0 ** -18 + own) * want[i][zeros].abs()).all()), i
+
+
+@pytest.mark.parametrize("scale", [-18, -19])
+def test_rows_near_the_end_of_the_range(scale):
+    """Rows whose mean squares are near 1e-38, without eps: the norm's gradient is of the size of what arrives, over the row's."""
+    data = [x.clone() for x in make(3, 20, 96, "f32", "scalar")]
+    data[0] *= 10.0 ** scale * 3
+    data[1] *= 10.0 ** scale * 3
+    data[4] *= 10.0 ** scale
+    data[5] *= 0.0
+    got, want = both(data, sigmoid=False, lam=1.0, eps=0.0)
+    for i in (0, 3):
+        assert bool(torch.isfinite(got[i]).all()), i
+        # the two parts of a norm's gradient are of one size: taken by the row's largest element
+        most = want[i].abs().amax(-1, keepdim=True)
+        assert bool(((got[i] - want[i]).abs() <= 2.0 ** -15 * most).all()), (i, float(((got[i] - want[i]).abs() / most).max()))
