@@ -148,23 +148,23 @@ tfe_grad_norm_kernel(const __grid_constant__ Table<kRoom> t)
 }
 
 template <typename T>
-__device__ __forceinline__ void chunk_scale(const T *x, T *y, int64_t n, float by, uint64_t hint)
+__device__ __forceinline__ void chunk_scale(const T *x, T *y, int64_t n, float by, float pre, uint64_t hint)
 {
     if (((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(y)) & 15u) != 0) {
-        for (int64_t i = threadIdx.x; i < n; i += kThreads) Elem<T>::put(y + i, Elem<T>::get(x + i) * by);
+        for (int64_t i = threadIdx.x; i < n; i += kThreads) Elem<T>::put(y + i, Elem<T>::get(x + i) * pre * by);
         return;
     }
     constexpr int E = Elem<T>::kPerVec;
     const tfe_rows::Cut cut = tfe_rows::cut_row(x, n);
     const uint4 *from = reinterpret_cast<const uint4 *>(x + cut.head);
     uint4 *to = reinterpret_cast<uint4 *>(y + cut.head);
-    for (int64_t i = threadIdx.x; i < cut.head; i += kThreads) Elem<T>::put(y + i, Elem<T>::get(x + i) * by);
-    for (int64_t i = cut.head + cut.n_vec * E + threadIdx.x; i < n; i += kThreads) Elem<T>::put(y + i, Elem<T>::get(x + i) * by);
+    for (int64_t i = threadIdx.x; i < cut.head; i += kThreads) Elem<T>::put(y + i, Elem<T>::get(x + i) * pre * by);
+    for (int64_t i = cut.head + cut.n_vec * E + threadIdx.x; i < n; i += kThreads) Elem<T>::put(y + i, Elem<T>::get(x + i) * pre * by);
     auto scale = [&](const uint4 &raw) {
         float f[E];
         Elem<T>::unpack(raw, f);
 #pragma unroll
-        for (int e = 0; e < E; ++e) f[e] *= by;
+        for (int e = 0; e < E; ++e) f[e] = f[e] * pre * by;
         return Elem<T>::pack(f);
     };
     constexpr int U = 4;
@@ -191,7 +191,10 @@ tfe_grad_clip_kernel(const __grid_constant__ Table<kRoom> t)
     if (t.write_norm && blockIdx.x == 0 && threadIdx.x == 0) *t.norm = (float)norm;
     if (t.only_norm) return;
     // a norm that is not finite, as the caller sees it, scales nothing
-    const float by = norm > (double)t.max_norm && (float)norm <= 3.402823466e38f ? (float)((double)t.max_norm / norm) : 1.f;
+    const double factor = norm > (double)t.max_norm && (float)norm <= 3.402823466e38f ? (double)t.max_norm / norm : 1.0;
+    // a factor that fp32 holds with fewer digits, below 2^-126, is taken in two steps, of which the first is exact (elements that it is not
+    // exact for end as 0 in any case)
+    const float pre = factor < 0x1p-100 ? 0x1p-64f : 1.f, by = (float)(factor / (double)pre);
     if (by == 1.f && t.in_place) return;
     const uint32_t c0 = (uint32_t)((uint64_t)t.chunks * blockIdx.x / gridDim.x), c1 = (uint32_t)((uint64_t)t.chunks * (blockIdx.x + 1) / gridDim.x);
     if (c0 >= c1) return;
@@ -201,9 +204,9 @@ tfe_grad_clip_kernel(const __grid_constant__ Table<kRoom> t)
         while (t.at[i].first > c) --i;
         const int64_t from = (int64_t)(c - t.at[i].first) * t.chunk, n = min(t.chunk, t.at[i].n - from);
         if (t.at[i].dtype == TFE_DTYPE_BF16)
-            chunk_scale(reinterpret_cast<const __nv_bfloat16 *>(t.at[i].in) + from, reinterpret_cast<__nv_bfloat16 *>(t.at[i].out) + from, n, by, hint);
+            chunk_scale(reinterpret_cast<const __nv_bfloat16 *>(t.at[i].in) + from, reinterpret_cast<__nv_bfloat16 *>(t.at[i].out) + from, n, by, pre, hint);
         else
-            chunk_scale(reinterpret_cast<const float *>(t.at[i].in) + from, reinterpret_cast<float *>(t.at[i].out) + from, n, by, hint);
+            chunk_scale(reinterpret_cast<const float *>(t.at[i].in) + from, reinterpret_cast<float *>(t.at[i].out) + from, n, by, pre, hint);
     }
 }
 

@@ -91,3 +91,21 @@ def test_rows_near_the_end_of_the_range(scale):
         # the two parts of a norm's gradient are of one size: taken by the row's largest element
         most = want[i].abs().amax(-1, keepdim=True)
         assert bool(((got[i] - want[i]).abs() <= 2.0 ** -15 * most).all()), (i, float(((got[i] - want[i]).abs() / most).max()))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("max_norm", [1.0, 1e-5, 1e-6])
+def test_clipping_by_a_factor_below_the_normal_numbers(kind, max_norm):
+    """max_norm / norm below 2^-126: the results are ordinary numbers, off by the factor's rounding and their own."""
+    from paper_2607_07388_b200 import engine
+    rng = torch.Generator().manual_seed(4)
+    x = [(torch.randn(n, generator=rng) * 3e36).to(TYPES[kind]) for n in (1000, 7, 2000)]
+    norm = float(torch.cat([t.double() for t in x]).norm())
+    assert norm < 3e38
+    for out in (None, [torch.empty_like(t, device=DEV) for t in x]):
+        a = [t.to(DEV) for t in x]
+        got = engine.clip_grad_norm(a, max_norm, out=out)
+        assert abs(float(got) - norm) <= 2.0 ** -22 * norm
+        for t, r in zip(x, out or a):
+            want = t.double() * (max_norm / norm)
+            assert bool(((r.double().cpu() - want).abs() <= (2.0 ** -23 + HALF[TYPES[kind]]) * want.abs() + 2.0 ** -149).all())
