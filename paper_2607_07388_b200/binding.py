@@ -644,9 +644,10 @@ def _describer():
         lib()
         pointer = C.pythonapi.PyCapsule_GetPointer
         pointer.restype, pointer.argtypes = C.c_void_p, [C.py_object, C.c_char_p]
-        exchange = _DlpackExchange.from_address(pointer(torch.Tensor.__dlpack_c_exchange_api__, b"dlpack_exchange_api"))
-        if exchange.major != 1 or not exchange.tensor_from_object:
-            raise RuntimeError("the DLPack exchange interface of this torch is not version 1")
+        offered = getattr(torch.Tensor, "__dlpack_c_exchange_api__", None)
+        exchange = None if offered is None else _DlpackExchange.from_address(pointer(offered, b"dlpack_exchange_api"))
+        if exchange is None or exchange.major != 1 or not exchange.tensor_from_object:
+            raise NotImplementedError(f"torch {torch.__version__}: its tensors do not offer the DLPack exchange interface, version 1")
         f = C.PyDLL(LIB_PATH).tfe_describe_tensors
         f.restype, f.argtypes = C.c_int, [C.py_object, C.c_void_p, C.c_void_p, C.c_int32] + [C.c_void_p] * 5
         _describe = (f, C.cast(C.pythonapi.PyList_GetItem, C.c_void_p).value, exchange.tensor_from_object)
@@ -655,7 +656,7 @@ def _describer():
 
 def tfe_describe_tensors(tensors: list):
     """(addresses, sizes, the library's type numbers, CUDA device, reason) of a list of torch tensors, the first three as array.array
-    objects; the reason is 0, or why a tensor is refused (see the header)."""
+    objects; the reason is 0, or why a tensor is refused (see the header).  NotImplementedError: a torch whose tensors cannot be asked."""
     f, item, describe = _describe or _describer()
     n = len(tensors)
     at, numel, kinds, told = array("Q", bytes(8 * n)), array("q", bytes(8 * n)), array("i", bytes(4 * n)), array("i", (0, 0))

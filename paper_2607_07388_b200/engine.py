@@ -746,6 +746,8 @@ def _gradients(tensors, what):
         raise ValueError(f"{what}: one tensor at least and {tfe.CLIP_MAX_TENSORS} at most")
     if not all(issubclass(kind, torch.Tensor) for kind in set(map(type, tensors))):
         raise ValueError(f"{what}: tensors are needed")
+    if tfe._describe is None:           # NotImplementedError: this torch, whatever the tensors
+        tfe._describer()
     try:
         at, numel, kinds, device, reason = tfe.tfe_describe_tensors(tensors)
     except (RuntimeError, BufferError) as e:            # a tensor without elements in memory (sparse, meta)

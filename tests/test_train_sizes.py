@@ -45,3 +45,23 @@ def test_narrow_rows_take_no_room_for_wide_ones(tfe):
     n = N
     g = 8192 * n
     assert tfe.tfe_xent_backward_workspace_bytes(N, V, 64) <= g + g // 64 + 128 * n + 512 * n + 256 * V + 32 * n + 5 * V + 4096
+
+
+@pytest.mark.parametrize("how", ["missing", "version", "function"])
+def test_a_torch_that_cannot_be_asked_about_its_tensors(tfe, monkeypatch, how):
+    """Said as what it is, by its own name, and not as a refusal of the tensors."""
+    import ctypes as C
+
+    import torch
+
+    from paper_2607_07388_b200 import engine
+    monkeypatch.setattr(tfe, "_describe", None)
+    exchange = tfe._DlpackExchange(2 if how == "version" else 1, 0, None, None, None, None, None if how == "function" else 1, None)
+    new = C.pythonapi.PyCapsule_New
+    new.restype, new.argtypes = C.py_object, [C.c_void_p, C.c_char_p, C.c_void_p]
+    name = b"dlpack_exchange_api"
+    monkeypatch.setattr(torch.Tensor, "__dlpack_c_exchange_api__", None if how == "missing" else new(C.addressof(exchange), name, None), raising=False)
+    for call in (lambda: engine.grad_norm([torch.ones(3)]), lambda: engine.clip_grad_norm([torch.ones(3)], 1.0)):
+        with pytest.raises(NotImplementedError, match="DLPack"):
+            call()
+    assert tfe._describe is None
