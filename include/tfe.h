@@ -651,8 +651,9 @@ tfe_status tfe_distill_backward(const void *logits, int32_t dtype, int32_t N, in
  *
  * Every wait inside the kernels is bounded.  Should one run out, the loss and lse of the rows concerned, or all gradients, are NaN.
  * tfe_xent_status synchronises `stream`, reads the status word of the current device and clears what it read: 0, or bits set by
- * waits that ran out (1 loader, 2 MMA issuer, 4 epilogue); then INTERNAL.  tfe_xent_give_up -- at_once != 0: the waits of the calls
- * that follow, of the whole process, count as run out from the start; 0: as usual again.  For tests of how a caller takes a failure.
+ * waits that ran out (1 loader, 2 MMA issuer, 4 epilogue); then INTERNAL.  tfe_xent_give_up, for tests of how a caller takes a failure --
+ * 0: as usual; 2: in the calls that follow, of the whole process, the MMA issuers' waits count as run out after their first sum, with copies and
+ * MMAs under way; another number: all waits do from the start.
  * Errors: INVALID_ARG, CAPACITY, CUDA.
  */
 #define TFE_XENT_MAX_ROWS (1 << 24)
@@ -667,7 +668,7 @@ tfe_status tfe_xent_backward(const void *hidden, int64_t ld_hidden, int32_t N, c
                              int64_t ld_grad_hidden, void *grad_weight, int64_t ld_grad_weight, void *workspace,
                              int64_t workspace_bytes, void *stream);
 tfe_status tfe_xent_status(uint32_t *device_flags, void *stream);
-tfe_status tfe_xent_give_up(int32_t at_once);
+tfe_status tfe_xent_give_up(int32_t how);
 
 /*
  * Injection between two norms (paper Sec. 2.2: h' = h + g m with a gate that is a "scalar, vector, or learned function"; the norms are

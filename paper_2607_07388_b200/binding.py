@@ -595,9 +595,10 @@ def tfe_xent_status(stream=None) -> int:
     return flags.value
 
 
-def tfe_xent_give_up(at_once: bool) -> None:
-    """The waits of the cross entropy calls that follow count as run out from the start, until it is called with False."""
-    _check(lib().tfe_xent_give_up(int(at_once)), "tfe_xent_give_up")
+def tfe_xent_give_up(how: int) -> None:
+    """1 (True): the waits of the cross entropy calls that follow count as run out from the start; 2: those of the MMA issuers after
+    their first sum; 0 (False): as usual again."""
+    _check(lib().tfe_xent_give_up(int(how)), "tfe_xent_give_up")
 
 
 # -- injection between two norms ----------------------------------------------------------------

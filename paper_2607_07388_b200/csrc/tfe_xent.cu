@@ -59,6 +59,8 @@ constexpr int kFewRegs = 40, kManyRegs = 216;
 
 constexpr uint32_t kTimeoutLoader = 1u, kTimeoutMma = 2u, kTimeoutEpilogue = 4u;
 __device__ uint32_t g_xent_status;
+// For tests: all waits run out at once, or those of who issues the MMAs at the end of its first sum, with copies and MMAs under way.
+constexpr uint32_t kAtOnce = 1, kUnderWay = 2;
 std::atomic<uint32_t> g_xent_give_up{0};
 
 __global__ void tfe_xent_status_kernel(uint32_t told) { atomicAnd(&g_xent_status, ~told); }
@@ -348,9 +350,9 @@ __device__ __forceinline__ uint32_t in_second(uint32_t smem_addr)
     asm volatile("mapa.shared::cluster.u32 %0, %1, 1;" : "=r"(r) : "r"(smem_addr));
     return r;
 }
-__device__ __forceinline__ void store_second(uint32_t smem_addr, uint32_t x)
+__device__ __forceinline__ void store_cluster(uint32_t cluster_addr, uint32_t x)
 {
-    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(in_second(smem_addr)), "r"(x) : "memory");
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr), "r"(x) : "memory");
 }
 __device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t parity)      // what the other CTA wrote before it arrived is seen
 {
@@ -439,7 +441,7 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
     __shared__ __align__(8) uint64_t s_told[kTickets], s_heard[kTickets];
     __shared__ volatile uint32_t s_ticket[kTickets];
     __shared__ uint32_t s_tmem_base;
-    __shared__ volatile uint32_t s_abort;
+    __shared__ volatile uint32_t s_abort, s_issued[kCtas][2];       // alike in both CTAs at the end: whether a wait ran out, steps that each loader has issued
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -449,6 +451,7 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
         for (int a = 0; a < kBuffers; ++a) { mbar_init(smem_u32(&s_acc_full[a]), 1); mbar_init(smem_u32(&s_acc_empty[a]), kCtas * kEpilogueWarps); }
         mbar_init(smem_u32(&s_drain), 1);
         s_abort = 0;
+        for (int c = 0; c < kCtas; ++c) s_issued[c][0] = s_issued[c][1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncwarp();
@@ -461,6 +464,19 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
     const uint32_t tmem_base = s_tmem_base;
     tfe_wait_for_stream();
     const Units<kOp> units(p);
+    auto in_both = [&](volatile uint32_t *at, uint32_t x) {
+        const uint32_t here = smem_u32(const_cast<uint32_t *>(at));
+        store_cluster(in_first(here), x);
+        store_cluster(in_second(here), x);
+    };
+    auto give_up = [&](uint32_t who) {          // a wait ran out
+        atomicOr(&g_xent_status, who);
+        in_both(&s_abort, 1u);
+    };
+    // A step's copies of one operand, counted in the first CTA; both CTAs' are awaited where the MMAs are issued.
+    auto expect = [&](uint32_t stage, bool is_a) {
+        if (rank == 0) mbar_expect_tx(smem_u32(&s_full[stage]), kCtas * (is_a ? kBytesA : (uint32_t)(p.tn / kCtas) * kStepK * 2));
+    };
     // The next unit of this pair, or one beyond the last.  Every role hears of each by itself.
     const bool handed_out = kOp == kGrads && units.steps_w >= kShort;
     uint32_t t_slot = 0, t_phase = 0;
@@ -489,25 +505,23 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
             const int32_t b_part = p.tn / kCtas;
             const uint32_t place = smem_base + (is_a ? 0u : kBytesA);
             uint32_t stage = 0, phase = 0, issued = 0;
-            bool ok = !p.give_up;
+            bool ok = p.give_up != kAtOnce;
             while (ok) {
                 ok = next_unit(true);
-                if (!ok) { atomicOr(&g_xent_status, kTimeoutLoader); s_abort = 1; }
+                if (!ok) give_up(kTimeoutLoader);
                 if (!ok || u >= units.n) break;
                 const Unit w = units.at(p, u);
                 for (int32_t t = 0; ok && t < w.tiles; ++t) {
                     const int32_t a_at = w.a_at + (int32_t)rank * kRowsA, b_at = w.b_at + t * p.tn + (int32_t)rank * b_part;
                     for (int32_t ks = 0; ks < w.steps; ++ks) {
                         if (!mbar_wait(smem_u32(&s_empty[stage]), phase ^ 1u, &s_abort)) {
-                            atomicOr(&g_xent_status, kTimeoutLoader);
-                            s_abort = 1;
+                            give_up(kTimeoutLoader);
                             ok = false;
                             break;
                         }
-                        // both CTAs' copies are counted where the MMAs are issued
                         const uint32_t bar = in_first(smem_u32(&s_full[stage])), dst = place + stage * kStageBytes;
                         const int32_t k = w.k_at + ks * kStepK;
-                        if (rank == 0) mbar_expect_tx(smem_u32(&s_full[stage]), kCtas * (is_a ? kBytesA : (uint32_t)b_part * kStepK * 2));
+                        expect(stage, is_a);
                         if (is_a) {
                             if (kOp != kGrads) pair_load_2d(dst, &maps.a, bar, k, a_at, hint);
                             else if (w.grad_h) pair_load_2d(dst, &maps.a, bar, 0, k / 64 * p.n_pad + a_at, hint);
@@ -523,26 +537,17 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                     }
                 }
             }
-            // copies in flight land before the shared memory goes: those of both threads and both CTAs are counted in the first, where a barrier
-            // may lack one of them for good, so a short wait for each has to do
-            if (!ok && issued) {
-                if (rank == 0)
-                    for (uint32_t s = 0; s < kStages; ++s) {
-                        const uint32_t fills = (issued + kStages - 1u - s) / kStages;
-                        for (uint32_t t = 0; fills && t < (1u << 12) && !mbar_try_wait(smem_u32(&s_full[s]), (fills - 1u) & 1u); ++t) { }
-                    }
-                __nanosleep(1000000);
-            }
+            in_both(&s_issued[rank][is_a], issued);
         } else if (handed_out && warp == 2 && lane == 0 && rank == 0) {
             // ============================ units to both CTAs ======================
             uint32_t slot = 0, phase = 0;
-            bool ok = !p.give_up;
+            bool ok = p.give_up != kAtOnce;
             while (ok) {
                 ok = mbar_wait_cluster(smem_u32(&s_heard[slot]), phase ^ 1u, &s_abort);
-                if (!ok) { atomicOr(&g_xent_status, kTimeoutLoader); s_abort = 1; break; }
+                if (!ok) { give_up(kTimeoutLoader); break; }
                 const uint32_t ticket = atomicAdd(p.ticket, 1u);
                 s_ticket[slot] = ticket;
-                store_second(smem_u32(const_cast<uint32_t *>(&s_ticket[slot])), ticket);
+                store_cluster(in_second(smem_u32(const_cast<uint32_t *>(&s_ticket[slot]))), ticket);
                 arrive_cluster(in_first(smem_u32(&s_told[slot])));
                 arrive_cluster(in_second(smem_u32(&s_told[slot])));
                 if (ticket >= units.n) break;
@@ -551,10 +556,10 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
         } else if (warp == 1 && lane == 0 && rank == 0) {
             // ============================ MMA issuer ==============================
             uint32_t stage = 0, phase = 0, buf = 0, buf_phase = 0;
-            bool ok = !p.give_up;
+            bool ok = p.give_up != kAtOnce;
             while (ok) {
                 ok = next_unit(true);
-                if (!ok) { atomicOr(&g_xent_status, kTimeoutMma); s_abort = 1; }
+                if (!ok) give_up(kTimeoutMma);
                 if (!ok || u >= units.n) break;
                 const Unit w = units.at(p, u);
                 const bool a_mn = kOp == kGrads && !w.grad_h, b_mn = kOp == kGrads;
@@ -577,19 +582,46 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                             pair_commit(smem_u32(&s_empty[stage]));
                             if (++stage == kStages) { stage = 0; phase ^= 1u; }
                         }
+                        if (p.give_up == kUnderWay) ok = false;     // (once a sum: asked at every step it costs 4 % of the products)
                         if (!ok) {
-                            atomicOr(&g_xent_status, kTimeoutMma);
-                            s_abort = 1;
+                            give_up(kTimeoutMma);
                             break;
                         }
                         pair_commit(smem_u32(&s_acc_full[buf]));
                         if (++buf == kBuffers) { buf = 0; buf_phase ^= 1u; }
                     }
             }
-            if (!ok) {                          // MMAs in flight end before their tensor memory is freed
-                pair_commit(smem_u32(&s_drain));
+        }
+        tc_fence_before();
+        __syncwarp();
+        cluster_sync();                         // neither leaves while the other may still reach its shared or tensor memory
+        if (s_abort) {                          // (alike in both)
+            // Copies and MMAs in flight end before their memory goes, whoever gave up and whoever came to an end.  A step's barrier in the first CTA
+            // counts the copies of both operands and CTAs, so each loader makes up for the steps that another has issued before it (one round of the
+            // stages at most, since no stage is filled again before all have filled it); what it loads is not used.
+            if ((warp == 0 || warp == 3) && lane == 0) {
+                const bool is_a = warp == 0;
+                uint32_t most = 0;
+                for (int c = 0; c < kCtas; ++c) most = max(most, max(s_issued[c][0], s_issued[c][1]));
+                for (uint32_t k = s_issued[rank][is_a]; k < most; ++k) {
+                    const uint32_t stage = k % kStages, bar = in_first(smem_u32(&s_full[stage])), dst = smem_base + stage * kStageBytes + (is_a ? 0u : kBytesA);
+                    expect(stage, is_a);
+                    if (is_a) pair_load_2d(dst, &maps.a, bar, 0, 0, 0x1000000000000000ull);
+                    else
+                        for (int32_t j = 0; j < p.tn / kCtas; j += kOp == kGrads ? 64 : p.tn / kCtas) pair_load_2d(dst + j * kStepK * 2, &maps.b, bar, 0, 0, 0x1000000000000000ull);
+                }
+                if (is_a && rank == 0)
+                    for (uint32_t st = 0; st < kStages; ++st) {
+                        const uint32_t fills = (most + kStages - 1u - st) / kStages;
+                        for (uint32_t t = 0; fills && t < TC_WAIT_LIMIT && !mbar_try_wait(smem_u32(&s_full[st]), (fills - 1u) & 1u); ++t) { }
+                    }
+            }
+            if (warp == 1 && lane == 0) {
+                if (rank == 0) pair_commit(smem_u32(&s_drain));
                 for (uint32_t t = 0; t < TC_WAIT_LIMIT && !mbar_try_wait(smem_u32(&s_drain), 0); ++t) { }
             }
+            __syncwarp();
+            cluster_sync();
         }
     } else {
         // ============================ epilogue ================================
@@ -600,7 +632,7 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
         const int32_t first_row = (int32_t)(rank * kRowsA + quarter * 32u), row_in_tile = first_row + lane;
         const uint32_t room = smem_base + kStages * kStageBytes + (uint32_t)e * kRoom;
         uint32_t buf = 0, buf_phase = 0;
-        bool ok = !p.give_up;
+        bool ok = p.give_up != kAtOnce;
         // 64 finished columns of this warp's rows leave by an asynchronous copy
         auto send = [&](const uint32_t (&out)[32], int32_t x, int32_t y, bool there) {
             if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");     // what was there has left
@@ -830,18 +862,15 @@ tfe_xent_gemm_kernel(const __grid_constant__ Maps maps, const GemmParams p)
                 if (live) *part_p = was + (sum.x + sum.y);
         }
         asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-        if (!ok) {                              // a wait ran out: no results that look like some (the last kernel sees to that)
-            if (lane == 0) {
-                atomicOr(&g_xent_status, kTimeoutEpilogue);
-                *p.failed = 1;
-            }
-            s_abort = 1;
+        if (!ok && lane == 0) {                 // a wait ran out: no results that look like some (the last kernel sees to that)
+            give_up(kTimeoutEpilogue);
+            *p.failed = 1;
         }
+        tc_fence_before();
+        __syncwarp();
+        cluster_sync();                         // as the others: once, and once more for what is in flight
+        if (s_abort) cluster_sync();
     }
-
-    tc_fence_before();
-    __syncwarp();
-    cluster_sync();                             // neither leaves while the other may still reach its shared or tensor memory
     if (warp == 1) {
         tc_fence_after();
         pair_tmem_dealloc(tmem_base, kBuffers * kN);
@@ -879,7 +908,7 @@ tfe_xent_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t s_full[kFewMaxStages], s_empty[kFewMaxStages], s_acc_full[kFewBuffers], s_acc_empty[kFewBuffers], s_drain;
     __shared__ uint32_t s_tmem_base;
-    __shared__ volatile uint32_t s_abort;
+    __shared__ volatile uint32_t s_abort, s_issued;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -887,7 +916,7 @@ tfe_xent_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
         for (int s = 0; s < kStagesHere; ++s) { mbar_init(smem_u32(&s_full[s]), 1); mbar_init(smem_u32(&s_empty[s]), 1); }
         for (int a = 0; a < kFewBuffers; ++a) { mbar_init(smem_u32(&s_acc_full[a]), 1); mbar_init(smem_u32(&s_acc_empty[a]), kFewEpilogueWarps); }
         mbar_init(smem_u32(&s_drain), 1);
-        s_abort = 0;
+        s_abort = s_issued = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) tmem_alloc(smem_u32(&s_tmem_base), kTmemCols);
@@ -904,7 +933,7 @@ tfe_xent_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
         if (lane == 0) {
             const uint64_t hint_w = 0x12F0000000000000ull, hint_h = 0x14F0000000000000ull;      // evict first, evict last
             uint32_t stage = 0, phase = 0, issued = 0;
-            bool ok = !p.give_up;
+            bool ok = p.give_up != kAtOnce;
             for (int32_t t = 0; ok && t < n_tiles; ++t) {
                 const int32_t valid = min(kFewM, n_rows - t * kFewM);
                 // a short last tile is fetched with the short box: only its rows are read
@@ -928,18 +957,14 @@ tfe_xent_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
                     if (++stage == kStagesHere) { stage = 0; phase ^= 1u; }
                 }
             }
-            if (!ok)                            // copies in flight land before the shared memory goes
-                for (uint32_t s = 0; s < kStagesHere; ++s) {
-                    const uint32_t fills = (issued + kStagesHere - 1u - s) / kStagesHere;
-                    for (uint32_t t = 0; fills && t < TC_WAIT_LIMIT && !mbar_try_wait(smem_u32(&s_full[s]), (fills - 1u) & 1u); ++t) { }
-                }
+            s_issued = issued;
         }
     } else if (warp == 1) {
         // ============================ MMA issuer ==============================
         if (lane == 0) {
             constexpr uint32_t idesc = umma_idesc(kFewM, TN, false, false);
             uint32_t stage = 0, phase = 0, buf = 0, buf_phase = 0;
-            bool ok = !p.give_up;
+            bool ok = p.give_up != kAtOnce;
             for (int32_t t = 0; ok && t < n_tiles; ++t)
                 for (int32_t ks = 0; ok && ks < p.steps; ks += kFewSteps) {
                     ok = mbar_wait(smem_u32(&s_acc_empty[buf]), buf_phase ^ 1u, &s_abort) && mbar_wait(smem_u32(&s_full[stage]), phase, &s_abort);
@@ -955,6 +980,7 @@ tfe_xent_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
                         umma_commit(smem_u32(&s_empty[stage]));
                         if (++stage == kStagesHere) { stage = 0; phase ^= 1u; }
                     }
+                    if (p.give_up == kUnderWay) ok = false;
                     if (!ok) {
                         atomicOr(&g_xent_status, kTimeoutMma);
                         s_abort = 1;
@@ -963,10 +989,6 @@ tfe_xent_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
                     umma_commit(smem_u32(&s_acc_full[buf]));
                     if (++buf == kFewBuffers) { buf = 0; buf_phase ^= 1u; }
                 }
-            if (!ok) {                          // MMAs in flight end before their tensor memory is freed
-                umma_commit(smem_u32(&s_drain));
-                for (uint32_t t = 0; t < TC_WAIT_LIMIT && !mbar_try_wait(smem_u32(&s_drain), 0); ++t) { }
-            }
         }
     } else {
         // ============================ epilogue ================================
@@ -981,7 +1003,7 @@ tfe_xent_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
             target[j] = c0 + j < p.N ? p.target[c0 + j] : -1;
         }
         uint32_t buf = 0, buf_phase = 0;
-        bool ok = !p.give_up;
+        bool ok = p.give_up != kAtOnce;
         for (int32_t t = 0; ok && t < n_tiles; ++t) {
             float z[kCols];
             for (int32_t k0 = 0; k0 < p.steps; k0 += kFewSteps) {
@@ -1031,6 +1053,18 @@ tfe_xent_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
 
     tc_fence_before();
     __syncthreads();
+    if (s_abort) {                              // copies and MMAs in flight end before their memory goes
+        if (warp == 0 && lane == 0)
+            for (uint32_t s = 0; s < kStagesHere; ++s) {
+                const uint32_t fills = (s_issued + kStagesHere - 1u - s) / kStagesHere;
+                for (uint32_t t = 0; fills && t < TC_WAIT_LIMIT && !mbar_try_wait(smem_u32(&s_full[s]), (fills - 1u) & 1u); ++t) { }
+            }
+        if (warp == 1 && lane == 0) {
+            umma_commit(smem_u32(&s_drain));
+            for (uint32_t t = 0; t < TC_WAIT_LIMIT && !mbar_try_wait(smem_u32(&s_drain), 0); ++t) { }
+        }
+        __syncthreads();
+    }
     if (warp == 1) {
         __syncwarp();
         tc_fence_after();
@@ -1666,9 +1700,9 @@ tfe_status tfe_xent_status(uint32_t *device_flags, void *stream_)
     return TFE_ERR_INTERNAL;
 }
 
-tfe_status tfe_xent_give_up(int32_t at_once)
+tfe_status tfe_xent_give_up(int32_t how)
 {
-    g_xent_give_up.store(at_once != 0, std::memory_order_relaxed);
+    g_xent_give_up.store(how == 0 ? 0u : how == (int32_t)kUnderWay ? kUnderWay : kAtOnce, std::memory_order_relaxed);
     return TFE_OK;
 }
 

@@ -210,3 +210,35 @@ def test_identical_rows():
     w = weights(rng, 700, 256)
     h = torch.randn((1, 256), generator=rng).bfloat16().expand(1500, 256).contiguous()
     check(h, w, torch.full((1500,), 123, dtype=torch.int32), torch.full((1500,), 1 / 1500))
+
+
+@pytest.mark.parametrize("n", [10, 50, 100, 400])
+def test_a_wait_that_runs_out_under_way(n):
+    """The MMA issuers give up after their first sum, with copies and MMAs under way, and the other roles find out: NaN in all that has a target, a
+    report once, and the next calls as if nothing had been."""
+    from paper_2607_07388_b200 import binding as tfe, engine
+    rng = torch.Generator().manual_seed(n)
+    w, t = weights(rng, 40_000, 1024), torch.randint(-1, 40_000, (n,), generator=rng).int()
+    h = torch.randn((n, 1024), generator=rng).bfloat16()
+    h, w, t, g = (x.to(DEV) for x in (h, w, t, torch.rand(n, generator=rng) + 0.1))
+    loss, lse = engine.xent_forward(h, w, t)
+    gh, gw = engine.xent_backward(g, h, w, t, lse)
+    assert engine.xent_status() == 0
+    tfe.tfe_xent_give_up(2)
+    try:
+        for _ in range(2):
+            bad, bad_lse = engine.xent_forward(h, w, t)
+            assert engine.xent_status() != 0 and engine.xent_status() == 0
+            bh, bw = engine.xent_backward(g, h, w, t, lse)
+            assert engine.xent_status() != 0 and engine.xent_status() == 0
+    finally:
+        tfe.tfe_xent_give_up(0)
+    live = t >= 0
+    assert torch.isnan(bad[live]).all() and torch.isnan(bad_lse[live]).all() and not bad[~live].any()
+    assert torch.isnan(bh[live]).all() and torch.isnan(bw).all()
+    for _ in range(2):
+        again = engine.xent_forward(h, w, t)
+        grads = engine.xent_backward(g, h, w, t, lse)
+        for a, b in zip((*again, *grads), (loss, lse, gh, gw)):
+            assert torch.equal(a, b)
+    assert engine.xent_status() == 0
