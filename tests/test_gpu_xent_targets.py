@@ -1,4 +1,6 @@
 """Softmax cross entropy where the target decides: logits of -inf, rows that are sure of their target, ids of many rows."""
+import math
+
 import pytest
 import torch
 
@@ -242,3 +244,44 @@ def test_a_wait_that_runs_out_under_way(n):
         for a, b in zip((*again, *grads), (loss, lse, gh, gw)):
             assert torch.equal(a, b)
     assert engine.xent_status() == 0
+
+
+@pytest.mark.parametrize("n,v,d", [(4096, 70_001, 64), (20_000, 30_000, 72), (9000, 600, 1032)])
+def test_ids_of_a_text(n, v, d):
+    """Ids as often as words are, a few in many rows and many in few, over several groups of rows and pieces of the vocabulary, some rows without a
+    target and some without a gradient.  The reference runs on the GPU in 64 bits; every target's row of grad_weight by itself, in the 2-norm: its
+    own rounding is 2^-8 at most, and what G's other entries are off by, of random signs and 2^-9 in the mean, of their own size.  A row of
+    grad_hidden has both roundings, 2^-8 at most each of what is rounded, and of the largest entry where it is one entry."""
+    from paper_2607_07388_b200 import engine
+    rng = torch.Generator(device=DEV).manual_seed(n)
+    w = (torch.randn((v, d), generator=rng, device=DEV) * (2.5 / d ** 0.5)).bfloat16()
+    t = (torch.exp(torch.rand(n, generator=rng, device=DEV).double() * math.log(v)) - 1).long().clamp(0, v - 1)
+    t = (t * 7919) % v
+    h = (torch.randn((n, d), generator=rng, device=DEV) + w[t].float() * torch.rand((n, 1), generator=rng, device=DEV) * 2).bfloat16()
+    t = torch.where(torch.rand(n, generator=rng, device=DEV) < 0.1, -1, t).int()
+    g = torch.where(torch.rand(n, generator=rng, device=DEV) < 0.1, 0.0, torch.full((n,), 1 / n, device=DEV))
+    _, lse = engine.xent_forward(h, w, t)
+    gh, gw = engine.xent_backward(g, h, w, t, lse)
+    live = ((t >= 0) & (g != 0)).nonzero()[:, 0]
+    e_gw = torch.zeros((v, d), dtype=torch.float64, device=DEV)
+    size = torch.zeros(v, dtype=torch.float64, device=DEV)       # of a row of grad_weight without the targets' part
+    for rows in live.split(1500):
+        z, at = h[rows].double() @ w.double().T, t[rows].long()
+        k = torch.arange(len(rows), device=DEV)
+        p = torch.exp(z - torch.logsumexp(z, 1)[:, None])
+        p[k, at] = 0
+        size += (p * g[rows].double()[:, None]).square().T @ h[rows].double().square().sum(1)
+        p[k, at] = -p.sum(1)
+        p *= g[rows].double()[:, None]
+        e_gw += p.T @ h[rows].double()
+        e_gh = p @ w.double()
+        off = (gh[rows].double() - e_gh).norm(dim=1)
+        assert bool((off <= 2.0 ** -7 * e_gh.norm(dim=1) + 2.0 ** -8 * p.abs().amax(1)).all()), float((off / e_gh.norm(dim=1)).max())
+    ids = t[live].long().unique()
+    off = (gw.double() - e_gw)[ids].norm(dim=1)
+    assert bool((off <= 2.0 ** -8 * e_gw[ids].norm(dim=1) + 2.0 ** -9 * size[ids].sqrt()).all()), float((off / e_gw[ids].norm(dim=1)).max())
+    away = torch.ones(n, dtype=torch.bool, device=DEV)
+    away[live] = False
+    assert not gh[away].any()
+    again = engine.xent_backward(g, h, w, t, lse)
+    assert torch.equal(again[0], gh) and torch.equal(again[1], gw) and engine.xent_status() == 0
