@@ -5,10 +5,11 @@
 //   tfe_grad_norm_kernel   sums of squares of all tensors in one launch.  The tensors' list travels in the launch's parameters; the
 //                          elements are cut into chunks, every block takes an equal run of chunks and leaves one fp64 sum.
 //   tfe_grad_clip_kernel   every block adds up those sums in the same order, and scales its run of chunks, from its end to its
-//                          beginning: what was read last is in L2.  Where nothing is to be scaled in place it reads no tensor.
+//                          beginning: what was read last is in L2 (with more than kLarge tensors, each launch's own).  Where nothing is to be
+//                          scaled in place it reads no tensor.
 //
-// HBM bounds both: one read for the norm, one read and one write to scale (155.6 M bf16 elements: 53 + 98 us; writing 311 MB alone takes
-// 80, so what L2 saves in reads shows little).  A thread's eight or four squares are summed in fp32 and
+// HBM bounds both: one read for the norm, one read and one write to scale (155.6 M bf16 elements: 51 + 98 us, 51 + 91 in place; writing 311 MB
+// alone takes 80, so what L2 saves in reads shows little; 155.6 M fp32: 102 + 203 us).  A thread's eight or four squares are summed in fp32 and
 // joined in fp64; where they leave fp32's range they are formed in fp64.  No atomics: the order depends on the sizes alone.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -27,7 +28,9 @@ using tfe_rows::Elem;
 
 constexpr int kThreads = 256;
 constexpr int64_t kChunkMin = 2048, kChunkMax = 16384;        // elements of a chunk: few tensors are spread over the SMs, many read in long runs
-constexpr int64_t kKeepBytes = 80 << 20;       // what the norm leaves in L2 for the scaling (126 MB, and its writes pass through it)
+// What the norm leaves in L2 for the scaling (126 MB, and its writes pass through it), with elements of two bytes; of fp32 twice as much is
+// marked, more than stays.
+constexpr int64_t kKeepBytes = 80 << 20;
 constexpr int kPerSm = 6;                       // blocks, all resident
 constexpr int kBlocks = 148 * kPerSm;           // most blocks of a launch
 
