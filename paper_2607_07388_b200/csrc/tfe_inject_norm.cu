@@ -255,6 +255,8 @@ struct Row {
 };
 
 // Whether a thread has registers to hold the next row's operands beside this row's: 16-bit rows in blocks of up to kBlock threads.
+// 32,768 x 1,024 with a vector gate, forward and backward: bf16 57 and 107 us with it, 62 and 129 without; fp32 117 and 198 with it, 108 and
+// 182 without.
 template <typename T, int kThreads> constexpr bool kAhead = sizeof(T) == 2 && kThreads <= kBlock;
 
 template <typename T, bool kVector, int kThreads>
