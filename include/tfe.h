@@ -537,8 +537,8 @@ enum { TFE_DTYPE_BF16 = 0, TFE_DTYPE_F32 = 1 };
  * INTERNAL.  The word is one for all calls on the device, whatever their stream: it says that some product since the
  * last report failed, and the NaN in its results which.
  *
- * tfe_matmul_fp8_give_up -- at_once != 0: the waits of the products that follow, of the whole process, count as run out
- * from the start; 0: as usual again.  For tests of how a caller takes a failure.
+ * tfe_matmul_fp8_give_up, for tests of how a caller takes a failure -- 0: as usual; 2: in the products that follow, of the whole process, the
+ * MMA issuers' waits count as run out after their first tile, with copies and MMAs under way; another number: all waits do from the start.
  * Errors of all five: INVALID_ARG, CUDA.
  */
 #define TFE_FP8_MAX_COLS (1 << 16)
@@ -550,7 +550,7 @@ tfe_status tfe_matmul_fp8(const void *a, int64_t lda, const float *a_scale, int3
                           const float *w_scale, int32_t N, int32_t K, void *out, int32_t out_dtype, int64_t ldo,
                           void *stream);
 tfe_status tfe_matmul_fp8_status(uint32_t *device_flags, void *stream);
-tfe_status tfe_matmul_fp8_give_up(int32_t at_once);
+tfe_status tfe_matmul_fp8_give_up(int32_t how);
 
 /*
  * tfe_sample_tokens -- the next token of every sequence from its logits and one given random number per sequence

@@ -552,9 +552,10 @@ def tfe_matmul_fp8_status(stream=None) -> int:
     return flags.value
 
 
-def tfe_matmul_fp8_give_up(at_once: bool) -> None:
-    """The waits of the products that follow count as run out from the start, until it is called with False."""
-    _check(lib().tfe_matmul_fp8_give_up(int(at_once)), "tfe_matmul_fp8_give_up")
+def tfe_matmul_fp8_give_up(how: int) -> None:
+    """1 (True): the waits of the products that follow count as run out from the start; 2: those of the MMA issuers after their first
+    tile; 0 (False): as usual again."""
+    _check(lib().tfe_matmul_fp8_give_up(int(how)), "tfe_matmul_fp8_give_up")
 
 
 # -- cross entropy from hidden states -----------------------------------------------------------

@@ -216,6 +216,8 @@ constexpr int kMatmulSmem = 224 * 1024;         // stages; the rest of an SM's 2
 constexpr uint32_t kTimeoutLoader = 1u, kTimeoutMma = 2u, kTimeoutScales = 4u, kTimeoutEpilogue = 8u;
 __device__ uint32_t g_matmul_status;
 const float not_a_number = __builtin_nanf("");
+// For tests: all waits run out at once, or those of who issues the MMAs at the end of its first tile, with copies and MMAs under way.
+constexpr uint32_t kAtOnce = 1, kUnderWay = 2;
 std::atomic<uint32_t> g_give_up{0};
 
 // Only what the caller has been told goes: a bit that another stream sets meanwhile stays.
@@ -227,7 +229,7 @@ struct MatmulParams {
     int32_t rows_per_cta, tail_rows;            // few rows: weight rows of a CTA, rows of its last short tile
     int32_t m_tiles;                            // many rows: tiles of activation rows
     int64_t n_units;                            // ... and all tiles
-    uint32_t give_up;                           // every role's waits count as run out from the start
+    uint32_t give_up;                           // 0, kAtOnce or kUnderWay
     const float *a_scale, *b_scale;             // [M][kb], [ceil(N / 128)][kb]
     void *out; int64_t ldo;
 };
@@ -262,7 +264,7 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
     __shared__ __align__(8) uint64_t s_sc_full[kScaleRing], s_sc_empty[kScaleRing], s_drain;
     __shared__ __align__(16) float s_scale[kScaleRing][kGroup][TN];
     __shared__ uint32_t s_tmem_base;
-    __shared__ volatile uint32_t s_abort;
+    __shared__ volatile uint32_t s_abort, s_issued;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -271,7 +273,7 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
         for (int a = 0; a < kBuffers; ++a) { mbar_init(smem_u32(&s_acc_full[a]), 1); mbar_init(smem_u32(&s_acc_empty[a]), kEpilogueWarps); }
         for (int a = 0; a < kScaleRing; ++a) { mbar_init(smem_u32(&s_sc_full[a]), 32); mbar_init(smem_u32(&s_sc_empty[a]), kEpilogueWarps); }
         mbar_init(smem_u32(&s_drain), 1);
-        s_abort = 0;
+        s_abort = s_issued = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) tmem_alloc(smem_u32(&s_tmem_base), kTmemCols);
@@ -290,7 +292,7 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
             const uint64_t hint_w = 0x12F0000000000000ull;          // evict first: the weights are read once
             const uint64_t hint_a = 0x14F0000000000000ull;          // evict last: the activations are read by every tile
             uint32_t stage = 0, phase = 0, issued = 0;
-            bool ok = !p.give_up;
+            bool ok = p.give_up != kAtOnce;
             for (int32_t t = 0; ok && t < n_tiles; ++t) {
                 const int32_t valid = min(kTileRows, n_rows - t * kTileRows);
                 // a short last tile is fetched with the short box: only its rows are read
@@ -314,18 +316,14 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
                     if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
                 }
             }
-            if (!ok)                            // copies in flight land before the shared memory goes
-                for (uint32_t s = 0; s < (uint32_t)p.stages; ++s) {
-                    const uint32_t fills = (issued + (uint32_t)p.stages - 1u - s) / (uint32_t)p.stages;
-                    for (uint32_t t = 0; fills && t < TC_WAIT_LIMIT && !mbar_try_wait(smem_u32(&s_full[s]), (fills - 1u) & 1u); ++t) { }
-                }
+            s_issued = issued;
         }
     } else if (warp == 1) {
         // ============================ MMA issuer ==============================
         if (lane == 0) {
             constexpr uint32_t idesc = umma_idesc_e4m3(kTileRows, TN);
             uint32_t stage = 0, phase = 0, buf = 0, buf_phase = 0;
-            bool ok = !p.give_up;
+            bool ok = p.give_up != kAtOnce;
             for (int32_t t = 0; ok && t < n_tiles; ++t) {
                 for (int32_t kb = 0; kb < p.kb; kb += kGroup) {
                     if (!mbar_wait(smem_u32(&s_acc_empty[buf]), buf_phase ^ 1u, &s_abort) ||
@@ -350,16 +348,17 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
                     if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
                     if (++buf == kBuffers) { buf = 0; buf_phase ^= 1u; }
                 }
-            }
-            if (!ok) {                          // MMAs in flight end before their tensor memory is freed
-                umma_commit(smem_u32(&s_drain));
-                for (uint32_t t = 0; t < TC_WAIT_LIMIT && !mbar_try_wait(smem_u32(&s_drain), 0); ++t) { }
+                if (ok && p.give_up == kUnderWay) {
+                    atomicOr(&g_matmul_status, kTimeoutMma);
+                    s_abort = 1;
+                    ok = false;
+                }
             }
         }
     } else if (warp == 2) {
         // ============================ activation scales =======================
         uint32_t st = 0, phase = 0;
-        bool ok = !p.give_up;
+        bool ok = p.give_up != kAtOnce;
         for (int32_t t = 0; ok && t < n_tiles; ++t) {
             for (int32_t kb = 0; kb < p.kb; kb += kGroup) {
                 constexpr int kPer = (TN + 31) / 32;
@@ -391,7 +390,7 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
         const int32_t c0 = ((warp - 3) >> 2) * kCols;               // this warp's columns
         const int32_t row_in_tile = (int32_t)(quarter * 32u) + lane;
         uint32_t st = 0, phase = 0, buf = 0, buf_phase = 0;
-        bool ok = !p.give_up;
+        bool ok = p.give_up != kAtOnce;
         if (!ok && lane == 0) atomicOr(&g_matmul_status, kTimeoutEpilogue);
         int32_t t = 0;
         for (; ok && t < n_tiles; ++t) {
@@ -469,6 +468,18 @@ tfe_matmul_fp8_few_kernel(const __grid_constant__ CUtensorMap map_w, const __gri
 
     tc_fence_before();
     __syncthreads();
+    if (s_abort) {                              // copies and MMAs in flight end before their memory goes, whoever gave up
+        if (warp == 0 && lane == 0)
+            for (uint32_t s = 0; s < (uint32_t)p.stages; ++s) {
+                const uint32_t fills = (s_issued + (uint32_t)p.stages - 1u - s) / (uint32_t)p.stages;
+                for (uint32_t t = 0; fills && t < TC_WAIT_LIMIT && !mbar_try_wait(smem_u32(&s_full[s]), (fills - 1u) & 1u); ++t) { }
+            }
+        if (warp == 1 && lane == 0) {
+            umma_commit(smem_u32(&s_drain));
+            for (uint32_t t = 0; t < TC_WAIT_LIMIT && !mbar_try_wait(smem_u32(&s_drain), 0); ++t) { }
+        }
+        __syncthreads();
+    }
     if (warp == 1) {
         __syncwarp();
         tc_fence_after();
@@ -573,7 +584,7 @@ tfe_matmul_fp8_many_kernel(const __grid_constant__ CUtensorMap map_w, const __gr
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_acc_full[kBuffers], s_acc_empty[kBuffers], s_drain;
     __shared__ uint32_t s_tmem_base;
-    __shared__ volatile uint32_t s_abort;
+    __shared__ volatile uint32_t s_abort, s_issued;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -581,7 +592,7 @@ tfe_matmul_fp8_many_kernel(const __grid_constant__ CUtensorMap map_w, const __gr
         for (int s = 0; s < kStages; ++s) { mbar_init(smem_u32(&s_full[s]), 1); mbar_init(smem_u32(&s_empty[s]), 1); }
         for (int a = 0; a < kBuffers; ++a) { mbar_init(smem_u32(&s_acc_full[a]), 1); mbar_init(smem_u32(&s_acc_empty[a]), kManyEpilogueWarps); }
         mbar_init(smem_u32(&s_drain), 1);
-        s_abort = 0;
+        s_abort = s_issued = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) tmem_alloc(smem_u32(&s_tmem_base), 512);
@@ -597,7 +608,7 @@ tfe_matmul_fp8_many_kernel(const __grid_constant__ CUtensorMap map_w, const __gr
             // ============================ TMA producer ============================
             const uint64_t hint = 0x14F0000000000000ull;            // evict last: both operands are read by other tiles too
             uint32_t stage = 0, phase = 0, issued = 0;
-            bool ok = !p.give_up;
+            bool ok = p.give_up != kAtOnce;
             for (int64_t u = blockIdx.x; ok && u < p.n_units; u += gridDim.x) {
                 const int64_t nt = u / p.m_tiles;
                 const int32_t n0 = (int32_t)(nt * kN), m0 = (int32_t)(u - nt * p.m_tiles) * kTileRows;
@@ -616,17 +627,13 @@ tfe_matmul_fp8_many_kernel(const __grid_constant__ CUtensorMap map_w, const __gr
                     if (++stage == kStages) { stage = 0; phase ^= 1u; }
                 }
             }
-            if (!ok)                            // copies in flight land before the shared memory goes
-                for (uint32_t s = 0; s < kStages; ++s) {
-                    const uint32_t fills = (issued + kStages - 1u - s) / kStages;
-                    for (uint32_t t = 0; fills && t < TC_WAIT_LIMIT && !mbar_try_wait(smem_u32(&s_full[s]), (fills - 1u) & 1u); ++t) { }
-                }
+            s_issued = issued;
         } else if (warp == 1 && lane == 0) {
             // ============================ MMA issuer ==============================
             constexpr uint32_t idesc = umma_idesc_e4m3(kTileRows, kN);
             uint32_t stage = 0, phase = 0, buf = 0, buf_phase = 0;
-            bool ok = !p.give_up;
-            for (int64_t u = blockIdx.x; ok && u < p.n_units; u += gridDim.x)
+            bool ok = p.give_up != kAtOnce;
+            for (int64_t u = blockIdx.x; ok && u < p.n_units; u += gridDim.x) {
                 for (int32_t kb = 0; kb < p.kb; ++kb) {
                     if (!mbar_wait(smem_u32(&s_acc_empty[buf]), buf_phase ^ 1u, &s_abort) ||
                         !mbar_wait(smem_u32(&s_full[stage]), phase, &s_abort)) {
@@ -646,10 +653,26 @@ tfe_matmul_fp8_many_kernel(const __grid_constant__ CUtensorMap map_w, const __gr
                     if (++stage == kStages) { stage = 0; phase ^= 1u; }
                     if (++buf == kBuffers) { buf = 0; buf_phase ^= 1u; }
                 }
-            if (!ok) {                          // MMAs in flight end before their tensor memory is freed
+                if (ok && p.give_up == kUnderWay) {
+                    atomicOr(&g_matmul_status, kTimeoutMma);
+                    s_abort = 1;
+                    ok = false;
+                }
+            }
+        }
+        tc_fence_before();
+        __syncthreads();
+        if (s_abort) {                          // copies and MMAs in flight end before their memory goes, whoever gave up
+            if (warp == 0 && lane == 0)
+                for (uint32_t s = 0; s < kStages; ++s) {
+                    const uint32_t fills = (s_issued + kStages - 1u - s) / kStages;
+                    for (uint32_t t = 0; fills && t < TC_WAIT_LIMIT && !mbar_try_wait(smem_u32(&s_full[s]), (fills - 1u) & 1u); ++t) { }
+                }
+            if (warp == 1 && lane == 0) {
                 umma_commit(smem_u32(&s_drain));
                 for (uint32_t t = 0; t < TC_WAIT_LIMIT && !mbar_try_wait(smem_u32(&s_drain), 0); ++t) { }
             }
+            __syncwarp();
         }
     } else {
         // ============================ epilogue ================================
@@ -659,7 +682,7 @@ tfe_matmul_fp8_many_kernel(const __grid_constant__ CUtensorMap map_w, const __gr
         const int32_t c0 = (e >> 2) * kCols;                        // this warp's columns, all in one scale block of the weights
         const uint32_t row_smem = smem_base + kStages * kManyStageBytes + (uint32_t)((e * 32 + lane) * kRowPitch);
         uint32_t buf = 0, buf_phase = 0;
-        bool ok = !p.give_up;
+        bool ok = p.give_up != kAtOnce;
         if (!ok && lane == 0) atomicOr(&g_matmul_status, kTimeoutEpilogue);
         int64_t u = blockIdx.x;
         for (; ok && u < p.n_units; u += gridDim.x) {
@@ -733,10 +756,9 @@ tfe_matmul_fp8_many_kernel(const __grid_constant__ CUtensorMap map_w, const __gr
 #pragma unroll 1
                 for (int64_t n = n0; n < min(n0 + kCols, (int64_t)p.N); ++n) Elem<Out>::put(static_cast<Out *>(p.out) + m * p.ldo + n, not_a_number);
         }
+        tc_fence_before();
+        __syncthreads();                        // (as the others)
     }
-
-    tc_fence_before();
-    __syncthreads();
     if (warp == 1) {
         __syncwarp();
         tc_fence_after();
@@ -884,9 +906,9 @@ tfe_status tfe_matmul_fp8_status(uint32_t *device_flags, void *stream_)
     return TFE_ERR_INTERNAL;
 }
 
-tfe_status tfe_matmul_fp8_give_up(int32_t at_once)
+tfe_status tfe_matmul_fp8_give_up(int32_t how)
 {
-    g_give_up.store(at_once != 0, std::memory_order_relaxed);
+    g_give_up.store(how == 0 ? 0u : how == (int32_t)kUnderWay ? kUnderWay : kAtOnce, std::memory_order_relaxed);
     return TFE_OK;
 }
 
