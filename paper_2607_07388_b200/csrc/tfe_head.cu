@@ -101,9 +101,9 @@ tfe_head_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
                      const __grid_constant__ CUtensorMap map_h, const HeadGemmParams p)
 {
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t s_full[HEAD_MAX_STAGES], s_empty[HEAD_MAX_STAGES], s_acc_full[2], s_acc_empty[2];
+    __shared__ __align__(8) uint64_t s_full[HEAD_MAX_STAGES], s_empty[HEAD_MAX_STAGES], s_acc_full[2], s_acc_empty[2], s_drain;
     __shared__ uint32_t s_tmem_base;
-    __shared__ volatile uint32_t s_abort;
+    __shared__ volatile uint32_t s_abort, s_issued;
     __shared__ float s_gmax[4][HEAD_MAX_N];            // running column maxima of the four epilogue warps
     __shared__ float s_gsum[4][HEAD_MAX_N];            // sums of exp(z - running maximum) over the warps' rows
 
@@ -122,7 +122,8 @@ tfe_head_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) { mbar_init(smem_u32(&s_full[s]), 1); mbar_init(smem_u32(&s_empty[s]), 1); }
         for (int a = 0; a < 2; ++a) { mbar_init(smem_u32(&s_acc_full[a]), 1); mbar_init(smem_u32(&s_acc_empty[a]), 4 * HEAD_EPI_PER_QUARTER); }
-        s_abort = 0;
+        mbar_init(smem_u32(&s_drain), 1);
+        s_abort = s_issued = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) tmem_alloc(smem_u32(&s_tmem_base), p.tmem_cols);
@@ -142,7 +143,7 @@ tfe_head_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
         if (lane == 0) {
             const uint64_t hint_stream = 0x12F0000000000000ull;     // evict first: W is read once
             const uint64_t hint_keep = 0x14F0000000000000ull;       // evict last: h is read by every tile
-            uint32_t stage = 0, phase = 0;
+            uint32_t stage = 0, phase = 0, issued = 0;
             bool ok = true;
             for (int32_t t = 0; t < n_tiles && ok; ++t) {
                 const int32_t valid = min(HEAD_TILE_M, n_rows - t * HEAD_TILE_M);
@@ -163,9 +164,11 @@ tfe_head_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
                     const int32_t piece = ((int32_t)blockIdx.x * p.tiles_per_cta + t) * num_kb + kb;
                     tma_load_2d(dst, use_tail ? &map_w_tail : &map_w, bar, 0, piece * HEAD_TILE_M, hint_stream);
                     tma_load_2d(dst + HEAD_TILE_M * 128u, &map_h, bar, kb * HEAD_TILE_K, 0, hint_keep);
+                    ++issued;
                     if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
                 }
             }
+            s_issued = issued;
         }
     } else if (warp == 1) {
         // ============================ MMA issuer ==============================
@@ -221,7 +224,8 @@ tfe_head_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
                     p.fine_max[(int64_t)(c0 + lane) * p.n_fine + ((int64_t)blockIdx.x * p.tiles_per_cta + t) * 4 + quarter] = -INFINITY;
         for (int32_t t = 0; t < n_tiles; ++t) {
             const uint32_t acc = (uint32_t)t & 1u, acc_phase = ((uint32_t)t >> 1) & 1u;
-            if (!mbar_wait(smem_u32(&s_acc_full[acc]), acc_phase, &s_abort)) {
+            const bool there = mbar_wait(smem_u32(&s_acc_full[acc]), acc_phase, &s_abort);
+            if (!__all_sync(0xFFFFFFFFu, there)) {
                 if (lane == 0) atomicOr(p.status, HEAD_ST_TIMEOUT_EPILOGUE);
                 s_abort = 1;
                 break;
@@ -291,6 +295,18 @@ tfe_head_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
 
     tc_fence_before();
     __syncthreads();
+    if (s_abort) {                              // copies and MMAs in flight end before their memory goes, whoever gave up
+        if (warp == 0 && lane == 0)
+            for (uint32_t s = 0; s < (uint32_t)p.stages; ++s) {
+                const uint32_t fills = (s_issued + (uint32_t)p.stages - 1u - s) / (uint32_t)p.stages;
+                for (uint32_t t = 0; fills && t < TC_WAIT_LIMIT && !mbar_try_wait(smem_u32(&s_full[s]), (fills - 1u) & 1u); ++t) { }
+            }
+        if (warp == 1 && lane == 0) {
+            umma_commit(smem_u32(&s_drain));
+            for (uint32_t t = 0; t < TC_WAIT_LIMIT && !mbar_try_wait(smem_u32(&s_drain), 0); ++t) { }
+        }
+        __syncthreads();
+    }
     if (warp == 1) {
         __syncwarp();
         tc_fence_after();
